@@ -56,7 +56,11 @@ typedef enum {
   LACACHE_CHECK_BOTH = 2    /* both of the above */
 } lacache_check_mode;
 
-typedef enum { LACACHE_BF16 = 0, LACACHE_F32 = 1 } lacache_dtype;
+typedef enum {
+  LACACHE_BF16 = 0,
+  LACACHE_F32 = 1,
+  LACACHE_F16 = 2 /* the decoding operators only (rotary positions, key-value cache); lacache_insert refuses it */
+} lacache_dtype;
 
 /* Which stage-1 kernel lookups run. */
 typedef enum {
@@ -369,6 +373,158 @@ typedef struct {
  * asynchronously on cuda_stream. */
 lacache_status lacache_merge_shards(int32_t G, const lacache_shard_result* shards, int32_t B, int32_t top_c,
                                     int32_t m, const lacache_result* out, void* cuda_stream);
+
+/* ----------------------------------------------------------------------------------------------------------------
+ * Decoding a miss. A query that is not served is decoded (Algorithm 1): a draft model produces its lookahead prefix
+ * token by token and the target model verifies the k drafts in one forward pass (section 3.3; lacache_verify_draft takes
+ * the probabilities). Both passes run on a key-value cache. These calls are the cache's side of an attention layer:
+ * rotary positions, the write of new keys and values into a paged cache (quantised or not), the attention of the new
+ * tokens over it, and reading cached tokens back. The models' products and weights are the caller's.
+ *
+ * Rows of heads. A lacache_rows names a device array of [tokens x heads x head_dim] elements with any token and head
+ * strides (slices of one fused projection, or transposed heads); a row's elements are dense. data is 16-byte aligned and
+ * the strides are multiples of 16 bytes, else LACACHE_ERR_INVALID_ARG. */
+typedef struct {
+  void* data;
+  int64_t token_stride; /* elements */
+  int64_t head_stride;  /* elements */
+} lacache_rows;
+
+#define LACACHE_MAX_HEAD_DIM 256
+
+/* Rotary positions: pair i of a row's first rot_dim elements is rotated by the angle position * w_i,
+ *   y_a = amplitude * (x_a cos - x_b sin),  y_b = amplitude * (x_b cos + x_a sin),
+ * and the other elements are copied. Pairs are (i, i + rot_dim / 2) in the half layout and (2i, 2i + 1) in the interleaved
+ * one. w_i = base^(-2i / rot_dim), or one of the scalings for contexts longer than the model was trained on. */
+typedef enum { LACACHE_ROPE_HALF = 0, LACACHE_ROPE_INTERLEAVED = 1 } lacache_rope_layout;
+typedef enum {
+  LACACHE_ROPE_PLAIN = 0,
+  LACACHE_ROPE_LINEAR = 1, /* w_i / factor: positions interpolated */
+  LACACHE_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)) for base: the slowest pair is stretched by factor,
+                              the fastest not at all */
+  LACACHE_ROPE_BANDED = 3  /* by the turns r_i = original_len * w_i / 2 pi that a pair makes in the original context:
+                              w_i / factor up to low_turns, w_i from high_turns on, and in between
+                              (1 - g) w_i / factor + g w_i with g = (r_i - low_turns) / (high_turns - low_turns) */
+} lacache_rope_scaling;
+/* A rotation's plan, filled by lacache_rope_init on the host and passed by value to the kernels: no device memory. turn[i]
+ * is w_i / 2 pi as a fraction of 2^64, so that position * turn[i] modulo 2^64 is the exact phase at every position. */
+typedef struct {
+  int32_t rot_dim;
+  int32_t layout;
+  float amplitude;
+  int32_t reserved;
+  uint64_t turn[LACACHE_MAX_HEAD_DIM / 2];
+} lacache_rope;
+
+/* Fill *out. rot_dim is even, 2..LACACHE_MAX_HEAD_DIM (for LACACHE_ROPE_BASE at least 4); base > 1; factor > 0 (ignored by
+ * LACACHE_ROPE_PLAIN); original_len > 0 and low_turns < high_turns for LACACHE_ROPE_BANDED (ignored otherwise); amplitude is
+ * finite (1 for none). */
+lacache_status lacache_rope_init(int32_t rot_dim, int32_t layout, double base, int32_t scaling, double factor,
+                                 double original_len, double low_turns, double high_turns, float amplitude,
+                                 lacache_rope* out);
+
+/* Rotate n tokens of `heads` heads from *x into *y (the same array, for in place, or one that does not overlap it), in
+ * `dtype` (bf16, f16 or f32; the arithmetic is fp32). pos_dev[i] is token i's position, any int32. inverse != 0 applies the
+ * transpose of the rotation (angles negated, the same amplitude): the gradient of the call with inverse == 0. head_dim is a
+ * multiple of 8, rope->rot_dim..LACACHE_MAX_HEAD_DIM. n = 0 does nothing. Runs on the current device, asynchronously on
+ * cuda_stream. */
+lacache_status lacache_rope_apply(const lacache_rope* rope, int64_t n, int32_t heads, int32_t head_dim, int32_t dtype,
+                                  const lacache_rows* x, const int32_t* pos_dev, int32_t inverse, const lacache_rows* y,
+                                  void* cuda_stream);
+
+/* A paged key-value cache. The handle owns, for each layer, pages of page_size token slots: K and V as
+ * [pages x kv_heads x page_size x head_dim] in the format, and for the 8-bit formats one fp32 scale a row,
+ * [pages x kv_heads x page_size]. Sequences are the caller's: an int32 table row names a sequence's pages in order, so that
+ * its token t lies in slot t % page_size of page table[t / page_size]. Pages may be shared between sequences.
+ *
+ * 8-bit rows: scale = amax / 448 (e4m3) or amax / 127 (int8) with amax the row's largest magnitude, codes = x / scale
+ * rounded to nearest, ties to even, all in fp32; a row reads back as codes * scale. A row of zeros has scale 0; a row that
+ * holds an infinity or a NaN is stored as zeros with a NaN scale and reads back as NaN. */
+typedef struct lacache_kv lacache_kv_t; /* opaque */
+typedef enum { LACACHE_KV_BF16 = 0, LACACHE_KV_F16 = 1, LACACHE_KV_E4M3 = 2, LACACHE_KV_INT8 = 3 } lacache_kv_format;
+typedef struct {
+  int32_t layers;
+  int32_t kv_heads;
+  int32_t head_dim;  /* multiple of 16, <= LACACHE_MAX_HEAD_DIM */
+  int32_t page_size; /* multiple of 16 */
+  int64_t pages;     /* per layer */
+  int32_t format;    /* lacache_kv_format */
+  int32_t device;
+} lacache_kv_config;
+
+/* Create an empty cache: one device allocation of the pools and the attention's scratch (a few MB, whatever the lengths). A
+ * handle is not thread-safe, and its calls share the scratch: issue them on one stream, or order the streams by events. The
+ * pools' contents are undefined until written. */
+lacache_status lacache_kv_create(const lacache_kv_config* cfg, lacache_kv_t** out);
+/* Free it; synchronizes the device first. NULL is accepted. */
+lacache_status lacache_kv_destroy(lacache_kv_t* h);
+
+/* One layer's arrays (device pointers; k_scale and v_scale are NULL in 16-bit formats), for checkpoints, page copies and
+ * checks. */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+} lacache_kv_pool;
+lacache_status lacache_kv_get_pool(const lacache_kv_t* h, int32_t layer, lacache_kv_pool* out);
+
+/* The sequences' pages: pages_dev[s * row_stride + i] is page i of sequence s. The kernels check what they use: a sequence
+ * index, position or page id outside its range skips the token (an attention treats it as masked), and lacache_kv_sync then
+ * reports LACACHE_ERR_INVALID_ARG. */
+typedef struct {
+  const int32_t* pages_dev;
+  int64_t row_stride; /* elements */
+  int32_t seqs;
+  int32_t width;      /* page ids a sequence has in its row */
+} lacache_kv_table;
+
+/* Write n tokens into the cache: token i goes to position pos_dev[i] of sequence seq_dev[i] (seq_dev[i] = -1 skips it:
+ * padding). No two of a call may name the same slot. k and v are [n x kv_heads] rows in `dtype` (bf16, f16 or f32),
+ * converted to the cache's format. With rope != NULL, k is rotated first, by rope_pos_dev[i] (NULL: pos_dev[i]); if
+ * q != NULL, its [n x q_heads] rows are rotated the same way into *q_out (same dtype; in place or not overlapping; skipped
+ * tokens' rows are not written). rope == NULL copies q. n = 0 does nothing. Asynchronous on cuda_stream; may be captured
+ * into a CUDA graph. */
+lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table, int64_t n,
+                                 const int32_t* seq_dev, const int32_t* pos_dev, const lacache_rope* rope,
+                                 const int32_t* rope_pos_dev, int32_t dtype, const lacache_rows* k,
+                                 const lacache_rows* v, int32_t q_heads, const lacache_rows* q,
+                                 const lacache_rows* q_out, void* cuda_stream);
+
+/* Read n cached tokens back as rows of `dtype` (bf16, f16 or f32); k or v may be NULL. Tokens are named as in
+ * lacache_kv_append; skipped tokens' rows are not written. */
+lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table, int64_t n,
+                               const int32_t* seq_dev, const int32_t* pos_dev, int32_t dtype, const lacache_rows* k,
+                               const lacache_rows* v, void* cuda_stream);
+
+/* Attention of the last new_tokens tokens of every sequence over its cached tokens (the new ones included: append first).
+ * Sequence s has lengths_dev[s] tokens; its query t (row s * new_tokens + t of q and out, of q_heads rows each) stands at
+ * position p = lengths_dev[s] - new_tokens + t and sees the positions j <= p with j >= starts_dev[s] (starts_dev may be
+ * NULL: 0) and, if window > 0, j > p - window. Head h reads kv head h / (q_heads / kv_heads). With
+ * s_j = scale * <q, k_j>:
+ *     out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + log(sum_j exp(s_j - m)),   m = max_j s_j
+ * A query that sees nothing (an empty sequence, p < 0, a start past it) gets a row of zeros and lse = -inf. What a masked
+ * position holds never reaches the result. new_tokens is 1..512; scale is finite; lse_dev ([seqs * new_tokens x q_heads])
+ * may be NULL. dtype is q's and out's: bf16 or f16, that of the cache in the 16-bit formats. seqs = 0 does nothing.
+ * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read the lengths and tables anew. */
+typedef struct {
+  int32_t new_tokens;
+  int32_t q_heads; /* a multiple of kv_heads */
+  int32_t window;  /* 0: none */
+  int32_t dtype;
+  float scale;
+  const int32_t* lengths_dev;
+  const int32_t* starts_dev;
+  lacache_rows q;
+  lacache_rows out;
+  float* lse_dev;
+} lacache_attention;
+lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table,
+                                 const lacache_attention* a, void* cuda_stream);
+
+/* Synchronize the handle's device and report what its kernels found since the previous call: LACACHE_ERR_INVALID_ARG for
+ * an index outside its range (see lacache_kv_table). */
+lacache_status lacache_kv_sync(lacache_kv_t* h);
 
 #ifdef __cplusplus
 }

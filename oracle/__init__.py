@@ -15,8 +15,9 @@ from .calibrate import calibrate, nearest_rank, pair_similarities
 from .lsh import LshKeyCheck, hamming, lookup_lsh, projections, signatures
 from .speculative import accepted_prefix
 from .shards import merge as merge_shards
+from . import decode
 
 __all__ = ["round_to_bf16", "widen", "CHECK_BOTH", "CHECK_EMB", "CHECK_TOKENS", "HIT", "MISS_KEY", "REJECT",
            "KeyCheck", "Params", "Result", "Store", "decide", "lookahead", "lookup", "passes", "ServeLoop",
            "calibrate", "nearest_rank", "pair_similarities", "LshKeyCheck", "hamming", "lookup_lsh", "projections", "signatures",
-           "accepted_prefix", "merge_shards"]
+           "accepted_prefix", "merge_shards", "decode"]

@@ -57,29 +57,11 @@ struct lacache {
 
 namespace {
 
+using lc::aligned16;
+using lc::DeviceGuard;
+using lc::from_cuda;
 using lc::Stage1Args;
 using lc::Stage2Args;
-
-class DeviceGuard {
- public:
-  explicit DeviceGuard(int dev) {
-    ok_ = cudaGetDevice(&prev_) == cudaSuccess;
-    if (ok_ && prev_ != dev) ok_ = cudaSetDevice(dev) == cudaSuccess;
-    dev_ = dev;
-  }
-  ~DeviceGuard() {
-    if (ok_ && prev_ != dev_) cudaSetDevice(prev_);
-  }
-  bool ok() const { return ok_; }
-
- private:
-  int prev_ = 0, dev_ = 0;
-  bool ok_ = false;
-};
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-lacache_status from_cuda(cudaError_t e) { return e == cudaSuccess ? LACACHE_OK : LACACHE_ERR_CUDA; }
 
 // f32 -> bf16 (round to nearest even) of the key rows (count_a elements) and prefix rows (count_b), into the store.
 __global__ void convert_rows_kernel(const float* __restrict__ a, const float* __restrict__ b,

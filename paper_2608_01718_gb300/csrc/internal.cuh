@@ -23,6 +23,28 @@ class NvtxRange {
   NvtxRange& operator=(const NvtxRange&) = delete;
 };
 
+// The handle's device for the enclosing scope.
+class DeviceGuard {
+ public:
+  explicit DeviceGuard(int dev) {
+    ok_ = cudaGetDevice(&prev_) == cudaSuccess;
+    if (ok_ && prev_ != dev) ok_ = cudaSetDevice(dev) == cudaSuccess;
+    dev_ = dev;
+  }
+  ~DeviceGuard() {
+    if (ok_ && prev_ != dev_) cudaSetDevice(prev_);
+  }
+  bool ok() const { return ok_; }
+
+ private:
+  int prev_ = 0, dev_ = 0;
+  bool ok_ = false;
+};
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+inline lacache_status from_cuda(cudaError_t e) { return e == cudaSuccess ? LACACHE_OK : LACACHE_ERR_CUDA; }
+
 constexpr int kMaxTopC = 32;
 constexpr int kMaxD = 8192;
 constexpr int kMaxK = 256;

@@ -14,14 +14,19 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_build", "l
 LACACHE_OK, LACACHE_ERR_INVALID_ARG, LACACHE_ERR_CAPACITY, LACACHE_ERR_OOM = 0, 1, 2, 3
 LACACHE_ERR_CUDA, LACACHE_ERR_DEVICE_TIMEOUT, LACACHE_ERR_UNSUPPORTED, LACACHE_ERR_IO = 4, 5, 6, 7
 LACACHE_CHECK_EMB, LACACHE_CHECK_TOKENS, LACACHE_CHECK_BOTH = 0, 1, 2
-LACACHE_BF16, LACACHE_F32 = 0, 1
+LACACHE_BF16, LACACHE_F32, LACACHE_F16 = 0, 1, 2
 LACACHE_STAGE1_AUTO, LACACHE_STAGE1_TENSOR, LACACHE_STAGE1_STREAM, LACACHE_STAGE1_LSH = 0, 1, 2, 3
 LACACHE_STAGE1_TENSOR_PAIR = 4   # reported by lacache_last_launch only
 LACACHE_STAGE1_LSH_TENSOR = 5    # reported by lacache_last_launch only
 LACACHE_MISS_KEY, LACACHE_HIT, LACACHE_REJECT = 0, 1, 2
 
+LACACHE_ROPE_HALF, LACACHE_ROPE_INTERLEAVED = 0, 1
+LACACHE_ROPE_PLAIN, LACACHE_ROPE_LINEAR, LACACHE_ROPE_BASE, LACACHE_ROPE_BANDED = 0, 1, 2, 3
+LACACHE_KV_BF16, LACACHE_KV_F16, LACACHE_KV_E4M3, LACACHE_KV_INT8 = 0, 1, 2, 3
+
 LACACHE_MAX_MODELS = 8
 LACACHE_MAX_SHARDS = 16
+LACACHE_MAX_HEAD_DIM = 256
 
 EXPORTS = ["lacache_create", "lacache_create_ensemble", "lacache_destroy", "lacache_insert", "lacache_lookup",
            "lacache_lookup_host", "lacache_lookup_host_async", "lacache_append_misses", "lacache_read_rows",
@@ -29,6 +34,8 @@ EXPORTS = ["lacache_create", "lacache_create_ensemble", "lacache_destroy", "laca
            "lacache_inject_stall", "lacache_enable_lsh", "lacache_read_signatures", "lacache_calibrate",
            "lacache_calibrate_workspace_bytes", "lacache_verify_draft", "lacache_lookup_noalloc",
            "lacache_merge_shards", "lacache_get_stats", "lacache_save", "lacache_load", "lacache_get_config",
+           "lacache_rope_init", "lacache_rope_apply", "lacache_kv_create", "lacache_kv_destroy", "lacache_kv_get_pool",
+           "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_sync",
            "lacache_status_string"]
 
 
@@ -60,6 +67,37 @@ class lacache_shard_result(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in
                 ("cand_id", "cand_score", "cand_prefix_score", "cand_matches", "cand_pass", "cand_prefix_scores",
                  "key_score", "n_cand")] + [("id_base", ctypes.c_int64)]
+
+
+class lacache_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class lacache_rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("amplitude", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("turn", ctypes.c_uint64 * (LACACHE_MAX_HEAD_DIM // 2))]
+
+
+class lacache_kv_config(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("pages", ctypes.c_int64), ("format", ctypes.c_int32),
+                ("device", ctypes.c_int32)]
+
+
+class lacache_kv_pool(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("k", "v", "k_scale", "v_scale")]
+
+
+class lacache_kv_table(ctypes.Structure):
+    _fields_ = [("pages_dev", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("seqs", ctypes.c_int32),
+                ("width", ctypes.c_int32)]
+
+
+class lacache_attention(ctypes.Structure):
+    _fields_ = [("new_tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("lengths_dev", ctypes.c_void_p),
+                ("starts_dev", ctypes.c_void_p), ("q", lacache_rows), ("out", lacache_rows),
+                ("lse_dev", ctypes.c_void_p)]
 
 
 class LacacheError(RuntimeError):
@@ -113,6 +151,16 @@ def load() -> ctypes.CDLL:
         "lacache_get_config": ([vp, ctypes.POINTER(lacache_config), ctypes.POINTER(lacache_ensemble)], i32),
         "lacache_merge_shards": ([i32, ctypes.POINTER(lacache_shard_result), i32, i32, i32,
                                   ctypes.POINTER(lacache_result), vp], i32),
+        "lacache_rope_init": ([i32, i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                               ctypes.c_double, ctypes.c_float, ctypes.POINTER(lacache_rope)], i32),
+        "lacache_rope_apply": ([vp, i64, i32, i32, i32, vp, vp, i32, vp, vp], i32),
+        "lacache_kv_create": ([ctypes.POINTER(lacache_kv_config), ctypes.POINTER(vp)], i32),
+        "lacache_kv_destroy": ([vp], i32),
+        "lacache_kv_get_pool": ([vp, i32, ctypes.POINTER(lacache_kv_pool)], i32),
+        "lacache_kv_append": ([vp, i32, vp, i64, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp], i32),
+        "lacache_kv_read": ([vp, i32, vp, i64, vp, vp, i32, vp, vp, vp], i32),
+        "lacache_kv_attend": ([vp, i32, vp, vp, vp], i32),
+        "lacache_kv_sync": ([vp], i32),
         "lacache_status_string": ([i32], ctypes.c_char_p),
     }
     for name, (args, res) in sig.items():
@@ -335,6 +383,71 @@ def lacache_lookup_noalloc(cfg: lacache_config, key, prefix, ids, q_emb, q_prefi
         _ptr(q_prefix), _ptr(q_ids), ctypes.byref(res), _stream(cuda_stream, cfg.device)))
 
 
+def lacache_rope_init(rot_dim: int, layout: int = LACACHE_ROPE_HALF, base: float = 10000.0,
+                      scaling: int = LACACHE_ROPE_PLAIN, factor: float = 1.0, original_len: float = 0.0,
+                      low_turns: float = 1.0, high_turns: float = 4.0, amplitude: float = 1.0) -> lacache_rope:
+    """The plan of a rotation (host only)."""
+    rope = lacache_rope()
+    _check("lacache_rope_init", load().lacache_rope_init(rot_dim, layout, base, scaling, factor, original_len, low_turns,
+                                                         high_turns, amplitude, ctypes.byref(rope)))
+    return rope
+
+
+def lacache_rope_apply(rope, n: int, heads: int, head_dim: int, dtype: int, x: lacache_rows, pos, inverse: bool,
+                       y: lacache_rows, cuda_stream=None) -> None:
+    """Rotate n x heads rows (lacache_rows of device memory) at the positions ``pos`` (int32 on the device)."""
+    _check("lacache_rope_apply", load().lacache_rope_apply(ctypes.addressof(rope), n, heads, head_dim, dtype,
+                                                           ctypes.addressof(x), _ptr(pos), int(inverse),
+                                                           ctypes.addressof(y), _stream(cuda_stream)))
+
+
+def _address(struct) -> int | None:
+    return None if struct is None else ctypes.addressof(struct)
+
+
+def lacache_kv_create(cfg: lacache_kv_config) -> int:
+    h = ctypes.c_void_p()
+    _check("lacache_kv_create", load().lacache_kv_create(ctypes.byref(cfg), ctypes.byref(h)))
+    return h.value
+
+
+def lacache_kv_destroy(h: int) -> None:
+    _check("lacache_kv_destroy", load().lacache_kv_destroy(h))
+
+
+def lacache_kv_get_pool(h: int, layer: int = 0) -> lacache_kv_pool:
+    pool = lacache_kv_pool()
+    _check("lacache_kv_get_pool", load().lacache_kv_get_pool(h, layer, ctypes.byref(pool)))
+    return pool
+
+
+def lacache_kv_append(h: int, layer: int, table: lacache_kv_table, n: int, seq, pos, rope, rope_pos, dtype: int,
+                      k: lacache_rows, v: lacache_rows, q_heads: int = 0, q: lacache_rows | None = None,
+                      q_out: lacache_rows | None = None, cuda_stream=None) -> None:
+    """Write n tokens into the cache (rope: a lacache_rope or None; q and q_out: rows rotated with k, or None)."""
+    _check("lacache_kv_append", load().lacache_kv_append(
+        h, layer, _address(table), n, _ptr(seq), _ptr(pos), _address(rope), _ptr(rope_pos), dtype, _address(k),
+        _address(v), q_heads, _address(q), _address(q_out), _stream(cuda_stream)))
+
+
+def lacache_kv_read(h: int, layer: int, table: lacache_kv_table, n: int, seq, pos, dtype: int, k: lacache_rows | None,
+                    v: lacache_rows | None, cuda_stream=None) -> None:
+    """Read n cached tokens back as rows of ``dtype``."""
+    _check("lacache_kv_read", load().lacache_kv_read(h, layer, _address(table), n, _ptr(seq), _ptr(pos), dtype,
+                                                     _address(k), _address(v), _stream(cuda_stream)))
+
+
+def lacache_kv_attend(h: int, layer: int, table: lacache_kv_table, attention: lacache_attention,
+                      cuda_stream=None) -> None:
+    """Attention of the last new tokens of every sequence over its cached tokens."""
+    _check("lacache_kv_attend", load().lacache_kv_attend(h, layer, _address(table), _address(attention),
+                                                         _stream(cuda_stream)))
+
+
+def lacache_kv_sync(h: int) -> None:
+    _check("lacache_kv_sync", load().lacache_kv_sync(h))
+
+
 def alloc_result(batch: int, top_c: int, device, candidates: bool = True, pinned: bool = False,
                  models: int = 0) -> dict:
     """Output buffers of one lookup: device tensors (or pinned host tensors with ``device="cpu"``). ``candidates``
@@ -435,3 +548,195 @@ class LaCache:
 
     def last_launch(self) -> tuple[int, int]:
         return lacache_last_launch(self.h)
+
+
+def _dtype(t) -> int:
+    """The lacache_dtype of a tensor's elements."""
+    import torch
+    got = {torch.bfloat16: LACACHE_BF16, torch.float16: LACACHE_F16, torch.float32: LACACHE_F32}.get(t.dtype)
+    if got is None:
+        raise ValueError(f"rows are bf16, f16 or f32, not {t.dtype}")
+    return got
+
+
+def _rows(name: str, t, n: int, heads: int | None, head_dim: int, device: int, like=None) -> lacache_rows:
+    """A [n x heads x head_dim] CUDA tensor (any strides, dense rows) as lacache_rows."""
+    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != head_dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} is [{n} x {'heads' if heads is None else heads} x {head_dim}], not {tuple(t.shape)}")
+    if t.stride(2) != 1 or not t.is_cuda or t.device.index != device or (like is not None and t.dtype != like):
+        raise ValueError(f"{name} has dense rows on cuda:{device}" + ("" if like is None else f" of {like}"))
+    return lacache_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _index(name: str, t, n: int, device: int) -> int:
+    """An int32 [n] CUDA tensor's address."""
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device.index != device \
+            or not t.is_cuda:
+        raise ValueError(f"{name} is a dense int32 tensor of {n} on cuda:{device}")
+    return t.data_ptr()
+
+
+class Rope:
+    """Rotary positions of the first ``rot_dim`` elements of a head: the plan lacache_rope_init makes.
+
+    ``scaling``: None, "linear" (positions divided by ``factor``), "base" (the base stretched so that the slowest pair is) or
+    "banded" (only pairs that make few turns within ``original_len`` are stretched)."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str | None = None,
+                 factor: float = 1.0, original_len: float = 0.0, low_turns: float = 1.0, high_turns: float = 4.0,
+                 amplitude: float = 1.0):
+        modes = {None: LACACHE_ROPE_PLAIN, "linear": LACACHE_ROPE_LINEAR, "base": LACACHE_ROPE_BASE,
+                 "banded": LACACHE_ROPE_BANDED}
+        if scaling not in modes:
+            raise ValueError(f"scaling is one of {list(modes)}, not {scaling!r}")
+        self.plan = lacache_rope_init(rot_dim, LACACHE_ROPE_INTERLEAVED if interleaved else LACACHE_ROPE_HALF, base,
+                                      modes[scaling], factor, original_len, low_turns, high_turns, amplitude)
+
+    def apply(self, x, pos, inverse: bool = False, out=None, cuda_stream=None):
+        """x [n x heads x head_dim] rotated at ``pos`` (int32 [n]) into ``out`` (new if None; x itself for in place).
+        ``inverse``: the transpose, which is the gradient."""
+        import torch
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        n, heads, head_dim = x.shape
+        device = x.device.index
+        rx = _rows("x", x, n, heads, head_dim, device)
+        ro = _rows("out", out, n, heads, head_dim, device, like=x.dtype)
+        _index("pos", pos, n, device)
+        with torch.cuda.device(device):
+            lacache_rope_apply(self.plan, n, heads, head_dim, _dtype(x), rx, pos, inverse, ro,
+                               _stream(cuda_stream, device))
+        return out
+
+
+class _DeviceArray:
+    """A view of a handle's device memory for torch.as_tensor (it keeps the handle alive)."""
+
+    def __init__(self, owner, ptr: int, shape, typestr: str):
+        self.owner = owner
+        self.__cuda_array_interface__ = {"data": (ptr, False), "shape": tuple(shape), "typestr": typestr, "version": 3}
+
+
+class KVCache:
+    """A paged key-value cache (lacache_kv_t) with its calls. ``format``: "bf16", "f16", "e4m3" or "int8".
+
+    Tables are int32 [sequences x pages] CUDA tensors, lengths and positions int32 vectors, rows [tokens x heads x head_dim]
+    tensors with dense rows. Calls run on torch's current stream of the cache's device unless given another."""
+
+    FORMATS = {"bf16": LACACHE_KV_BF16, "f16": LACACHE_KV_F16, "e4m3": LACACHE_KV_E4M3, "int8": LACACHE_KV_INT8}
+
+    def __init__(self, kv_heads: int, head_dim: int, pages: int, page_size: int = 16, format: str = "bf16",
+                 layers: int = 1, device: int = 0):
+        self.h = None
+        if format not in self.FORMATS:
+            raise ValueError(f"format is one of {list(self.FORMATS)}, not {format!r}")
+        self.cfg = lacache_kv_config(layers, kv_heads, head_dim, page_size, pages, self.FORMATS[format], device)
+        self.format, self.device = format, device
+        self.h = lacache_kv_create(self.cfg)
+
+    def close(self) -> None:
+        if self.h:
+            lacache_kv_destroy(self.h)
+            self.h = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def pool(self, layer: int = 0) -> dict:
+        """A layer's arrays as tensors on the handle's own memory (valid until close): k and v
+        [pages x kv_heads x page_size x head_dim] and, in 8-bit formats, their fp32 scales ks and vs."""
+        import torch
+        c, p = self.cfg, lacache_kv_get_pool(self.h, layer)
+        rows = (c.pages, c.kv_heads, c.page_size)
+        typestr, dtype = {"bf16": ("<i2", torch.bfloat16), "f16": ("<f2", torch.float16),
+                          "e4m3": ("|u1", torch.float8_e4m3fn), "int8": ("|i1", torch.int8)}[self.format]
+
+        def view(ptr, shape, kind):
+            return torch.as_tensor(_DeviceArray(self, ptr, shape, kind), device=f"cuda:{self.device}")
+
+        out = {name: view(ptr, (*rows, c.head_dim), typestr).view(dtype) for name, ptr in (("k", p.k), ("v", p.v))}
+        if p.k_scale:
+            out["ks"], out["vs"] = view(p.k_scale, rows, "<f4"), view(p.v_scale, rows, "<f4")
+        return out
+
+    def _table(self, table) -> lacache_kv_table:
+        import torch
+        if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1 or table.device.index != self.device:
+            raise ValueError(f"a table is an int32 [sequences x pages] tensor on cuda:{self.device} with dense rows")
+        return lacache_kv_table(table.data_ptr(), table.stride(0), table.shape[0], table.shape[1])
+
+    def append(self, k, v, seq, pos, table, layer: int = 0, rope: Rope | None = None, rope_pos=None, q=None, q_out=None,
+               cuda_stream=None):
+        """Write k and v [n x kv_heads x head_dim] at positions ``pos`` of sequences ``seq`` (int32 [n]; -1 skips a token),
+        k rotated by ``rope`` first. With ``q``, returns it rotated (in ``q_out`` if given)."""
+        import torch
+        n, D, dev = k.shape[0], self.cfg.head_dim, self.device
+        rk = _rows("k", k, n, self.cfg.kv_heads, D, dev)
+        rv = _rows("v", v, n, self.cfg.kv_heads, D, dev, like=k.dtype)
+        rq = ro = None
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            rq = _rows("q", q, n, None, D, dev, like=k.dtype)
+            ro = _rows("q_out", q_out, n, q.shape[1], D, dev, like=k.dtype)
+        _index("seq", seq, n, dev)
+        _index("pos", pos, n, dev)
+        if rope_pos is not None:
+            _index("rope_pos", rope_pos, n, dev)
+        lacache_kv_append(self.h, layer, self._table(table), n, seq, pos, None if rope is None else rope.plan, rope_pos,
+                          _dtype(k), rk, rv, 0 if q is None else q.shape[1], rq, ro, _stream(cuda_stream, dev))
+        return q_out
+
+    def read(self, seq, pos, table, layer: int = 0, dtype=None, k_out=None, v_out=None, cuda_stream=None):
+        """The cached rows (k, v) of n tokens, into ``k_out`` and ``v_out`` or new tensors of ``dtype`` (bf16)."""
+        import torch
+        n, D, dev = seq.shape[0], self.cfg.head_dim, self.device
+        if k_out is None and v_out is None:
+            dtype = torch.bfloat16 if dtype is None else dtype
+            k_out = torch.empty(n, self.cfg.kv_heads, D, dtype=dtype, device=f"cuda:{dev}")
+            v_out = torch.empty_like(k_out)
+        some = k_out if k_out is not None else v_out
+        rk, rv = (None if t is None else _rows(name, t, n, self.cfg.kv_heads, D, dev, like=some.dtype)
+                  for name, t in (("k_out", k_out), ("v_out", v_out)))
+        _index("seq", seq, n, dev)
+        _index("pos", pos, n, dev)
+        lacache_kv_read(self.h, layer, self._table(table), n, seq, pos, _dtype(some), rk, rv, _stream(cuda_stream, dev))
+        return k_out, v_out
+
+    def attend(self, q, table, lengths, new_tokens: int = 1, layer: int = 0, starts=None, window: int = 0,
+               scale: float | None = None, out=None, lse=None, cuda_stream=None):
+        """Attention of the last ``new_tokens`` tokens of each sequence: q [sequences * new_tokens x q_heads x head_dim],
+        ``lengths`` (int32) with the new tokens counted. Returns ``out``; ``lse`` (fp32 [tokens x q_heads]) is filled if
+        given. ``scale`` is 1 / sqrt(head_dim) if None."""
+        import torch
+        seqs, D, dev = table.shape[0], self.cfg.head_dim, self.device
+        n = seqs * new_tokens
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if q.dim() != 3:
+            raise ValueError("q is [tokens x heads x head_dim]")
+        heads = q.shape[1]
+        a = lacache_attention(new_tokens, heads, window, _dtype(q), D ** -0.5 if scale is None else scale,
+                              _index("lengths", lengths, seqs, dev),
+                              None if starts is None else _index("starts", starts, seqs, dev),
+                              _rows("q", q, n, heads, D, dev), _rows("out", out, n, heads, D, dev, like=q.dtype), None)
+        if lse is not None:
+            if lse.dtype != torch.float32 or tuple(lse.shape) != (n, heads) or not lse.is_contiguous() or \
+                    lse.device.index != dev:
+                raise ValueError(f"lse is a dense fp32 [{n} x {heads}] tensor on cuda:{dev}")
+            a.lse_dev = lse.data_ptr()
+        lacache_kv_attend(self.h, layer, self._table(table), a, _stream(cuda_stream, dev))
+        return out
+
+    def sync(self) -> None:
+        lacache_kv_sync(self.h)
