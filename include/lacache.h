@@ -452,7 +452,7 @@ typedef struct {
   int32_t device;
 } lacache_kv_config;
 
-/* Create an empty cache: one device allocation of the pools and the attention's scratch (a few MB, whatever the lengths). A
+/* Create an empty cache: one device allocation of the pools and the attention's scratch (10 to 20 MB, whatever the lengths). A
  * handle is not thread-safe, and its calls share the scratch: issue them on one stream, or order the streams by events. The
  * pools' contents are undefined until written. */
 lacache_status lacache_kv_create(const lacache_kv_config* cfg, lacache_kv_t** out);
@@ -505,7 +505,7 @@ lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const lacache_kv_
  *     out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + log(sum_j exp(s_j - m)),   m = max_j s_j
  * A query that sees nothing (an empty sequence, p < 0, a start past it) gets a row of zeros and lse = -inf. What a masked
  * position holds never reaches the result. new_tokens is 1..512; scale is finite; lse_dev ([seqs * new_tokens x q_heads])
- * may be NULL. dtype is q's and out's: bf16 or f16, that of the cache in the 16-bit formats. seqs = 0 does nothing.
+ * may be NULL. A table reaches at most 2^30 positions here. dtype is q's and out's: bf16 or f16, that of the cache in the 16-bit formats. seqs = 0 does nothing.
  * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read the lengths and tables anew. */
 typedef struct {
   int32_t new_tokens;

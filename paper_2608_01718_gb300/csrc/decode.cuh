@@ -13,13 +13,15 @@
 struct lacache_kv {
   lacache_kv_config cfg;
   int num_sms;
-  unsigned char* arena;      // one device allocation: pools, scales, status word
+  unsigned char* arena;      // one device allocation: pools, scales, the attention's scratch, status word
   size_t layer_bytes;        // K (or V) pages of one layer
   size_t layer_scales;       // scales of K (or V) of one layer, in floats (0 in 16-bit formats)
   unsigned char* k;          // [layers] pools
   unsigned char* v;
   float* ks;                 // [layers] scales, or nullptr
   float* vs;
+  float* partial;            // the attention's partial sums, two slots a block
+  unsigned int* arrived;     // its counters, one a block (each launch leaves them zero)
   unsigned int* dev_status;  // kBadIndex once a kernel met an index outside its range
 };
 

@@ -5,7 +5,7 @@
 // token's angles and its place are found once and serve all its heads.
 #include <new>
 
-#include "decode.cuh"
+#include "kv_attend.cuh"
 
 namespace lc {
 namespace {
@@ -185,16 +185,24 @@ extern "C" lacache_status lacache_kv_create(const lacache_kv_config* cfg, lacach
   lacache_status status = LACACHE_OK;
   if (!guard.ok() || cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess) {
     status = LACACHE_ERR_CUDA;
-  } else if (cudaMalloc(reinterpret_cast<void**>(&h->arena), 2 * pool + 2 * scales + 256) != cudaSuccess) {
+  }
+  const size_t blocks = (size_t)lc::kMaxBlocksPerSm * h->num_sms;
+  const size_t partial = lc::round_up(blocks * 2 * lc::partial_floats(lc::padded_dim(cfg->head_dim)) * 4, 256);
+  const size_t words = lc::round_up((blocks + 1) * 4, 256);   // counters and the status word: zeroed
+  if (status == LACACHE_OK &&
+      cudaMalloc(reinterpret_cast<void**>(&h->arena), 2 * pool + 2 * scales + partial + words) != cudaSuccess) {
     cudaGetLastError();   // the failed allocation is this call's to report, not a later one's
     status = LACACHE_ERR_OOM;
-  } else {
+  }
+  if (status == LACACHE_OK) {
     h->k = h->arena;
     h->v = h->k + pool;
     h->ks = quantised ? reinterpret_cast<float*>(h->v + pool) : nullptr;
     h->vs = quantised ? reinterpret_cast<float*>(h->v + pool + scales) : nullptr;
-    h->dev_status = reinterpret_cast<unsigned int*>(h->v + pool + 2 * scales);
-    if (cudaMemset(h->dev_status, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    h->partial = reinterpret_cast<float*>(h->v + pool + 2 * scales);
+    h->arrived = reinterpret_cast<unsigned int*>(h->v + pool + 2 * scales + partial);
+    h->dev_status = h->arrived + blocks;
+    if (cudaMemset(h->arrived, 0, words) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
       cudaFree(h->arena);
       status = LACACHE_ERR_CUDA;
     }
