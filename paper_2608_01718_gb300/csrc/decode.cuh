@@ -60,6 +60,28 @@ inline bool device_table(const lacache_kv_table* t, Table* out) {
   return true;
 }
 
+// The row kernels give a warp one token and a slab of its rows, kRowUnroll passes of 32 / lanes rows in flight. A slab is all
+// of a token's rows when the tokens alone fill the GPU; fewer tokens are cut into slabs of at least one pass.
+constexpr int kRowThreads = 128;
+constexpr int kRowUnroll = 4;
+constexpr int64_t kRowWarps = 4096;   // about 27 warps an SM
+struct RowPlan {
+  int slab;          // rows
+  int64_t tasks;     // tokens x slabs, one a warp
+  unsigned blocks;
+};
+inline RowPlan plan_rows(int64_t n, int rows, int lanes) {
+  const int pass = 32 / lanes, passes = (rows + pass - 1) / pass;
+  int64_t slabs = (kRowWarps + n - 1) / n;
+  if (slabs > passes) slabs = passes;
+  RowPlan p;
+  p.slab = (int)((passes + slabs - 1) / slabs) * pass;
+  p.tasks = n * ((rows + p.slab - 1) / p.slab);
+  const int64_t blocks = (p.tasks + kRowThreads / 32 - 1) / (kRowThreads / 32);
+  p.blocks = (unsigned)(blocks < (1 << 30) ? blocks : 1 << 30);
+  return p;
+}
+
 // Lanes of a group: the power of two that holds head_dim / 8 chunks.
 inline int lanes_for(int head_dim) {
   int n = 1;
@@ -69,9 +91,8 @@ inline int lanes_for(int head_dim) {
 
 namespace {
 
-// Eight elements of a row as fp32, and back.
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
+// Eight elements of a row, as loaded and as fp32, and back.
+__device__ __forceinline__ void widen8(uint4 u, float (&x)[8], __nv_bfloat16) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -79,8 +100,7 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
     x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void load8(const __half* p, float (&x)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ void widen8(uint4 u, float (&x)[8], __half) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -89,10 +109,24 @@ __device__ __forceinline__ void load8(const __half* p, float (&x)[8]) {
     x[2 * i + 1] = f.y;
   }
 }
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
+template <typename T>
+struct Chunk {
+  typedef uint4 raw;
+  static __device__ __forceinline__ raw load(const unsigned char* p) { return *reinterpret_cast<const uint4*>(p); }
+  static __device__ __forceinline__ void widen(raw u, float (&x)[8]) { widen8(u, x, T()); }
+};
+template <>
+struct Chunk<float> {
+  struct raw {
+    float4 a, b;
+  };
+  static __device__ __forceinline__ raw load(const unsigned char* p) {
+    return raw{reinterpret_cast<const float4*>(p)[0], reinterpret_cast<const float4*>(p)[1]};
+  }
+  static __device__ __forceinline__ void widen(const raw& u, float (&x)[8]) {
+    x[0] = u.a.x, x[1] = u.a.y, x[2] = u.a.z, x[3] = u.a.w, x[4] = u.b.x, x[5] = u.b.y, x[6] = u.b.z, x[7] = u.b.w;
+  }
+};
 __device__ __forceinline__ uint4 pack8(const float (&x)[8], __nv_bfloat16) {
   uint32_t w[4];
 #pragma unroll
@@ -136,22 +170,36 @@ __device__ __forceinline__ float2 rope_angle(const lacache_rope& r, int i, int p
 __device__ __forceinline__ float turn_first(float x, float y, float2 a) { return __fmaf_rn(x, a.x, -__fmul_rn(y, a.y)); }
 __device__ __forceinline__ float turn_second(float x, float y, float2 a) { return __fmaf_rn(x, a.x, __fmul_rn(y, a.y)); }
 
-// Rotates chunk c (elements 8c .. 8c+7) of the row whose chunk this lane holds in x, with the angles cs[i] of its token. All
-// lanes of the warp call it. In the half layout the partner of a chunk is a whole chunk of
-// another lane of the group (`lanes` wide) when rot_dim / 2 is a multiple of 8; `row` serves the other sizes, whose partners
-// lie across chunks: the row's elements in memory, still unrotated (the caller stores only after __syncwarp).
+// A warp's angles of one token: every pair once, through shared memory, then those of this lane's chunk c into registers,
+// where they serve all heads. a[i] belongs to element 8c + i in the half layout, to pair 4c + i (i < 4) in the other.
+__device__ __forceinline__ void warp_angles(const lacache_rope& r, int pos, float sign, int c, float2* cs, float2 (&a)[8]) {
+  const int lane = threadIdx.x & 31, h = r.rot_dim >> 1;
+  __syncwarp();
+  for (int i = lane; i < h; i += 32) cs[i] = rope_angle(r, i, pos, sign);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int d = c * 8 + i;
+    const int at = r.layout == LACACHE_ROPE_INTERLEAVED ? c * 4 + i : d < h ? d : d - h;
+    a[i] = at < h ? cs[at] : make_float2(1.f, 0.f);
+  }
+}
+
+// Rotates chunk c (elements 8c .. 8c+7) of the row whose chunk this lane holds in x, by the angles of warp_angles. All lanes
+// of the warp call it. In the half layout the partner of a chunk is a whole chunk of another lane of the group (`lanes`
+// wide) when rot_dim / 2 is a multiple of 8; `row` serves the other sizes, whose partners lie across chunks: the row's
+// elements in memory, still unrotated (the caller stores only after __syncwarp).
 template <typename T>
-__device__ __forceinline__ void rotate8(float (&x)[8], int c, int lanes, int rot, int layout, const float2* cs,
+__device__ __forceinline__ void rotate8(float (&x)[8], int c, int lanes, int rot, int layout, const float2 (&a)[8],
                                         const T* row) {
   const int d0 = c * 8;
   if (layout == LACACHE_ROPE_INTERLEAVED) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      if (d0 + i < rot) {
-        const float2 a = cs[(d0 + i) >> 1];
-        const float u = x[i], v = x[i + 1];
-        x[i] = turn_first(u, v, a);
-        x[i + 1] = turn_second(v, u, a);
+    for (int i = 0; i < 4; ++i) {
+      if (d0 + 2 * i < rot) {
+        const float u = x[2 * i], v = x[2 * i + 1];
+        x[2 * i] = turn_first(u, v, a[i]);
+        x[2 * i + 1] = turn_second(v, u, a[i]);
       }
     }
     return;
@@ -163,20 +211,21 @@ __device__ __forceinline__ void rotate8(float (&x)[8], int c, int lanes, int rot
     const int src = (threadIdx.x & 31 & ~(lanes - 1)) | ((first ? c + (h >> 3) : c - (h >> 3)) & (lanes - 1));
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], src);
-  } else {
+    if (d0 < rot) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int d = d0 + i;
-      y[i] = d < rot ? (float)row[d < h ? d + h : d - h] : 0.f;
+      for (int i = 0; i < 8; ++i) x[i] = first ? turn_first(x[i], y[i], a[i]) : turn_second(x[i], y[i], a[i]);
     }
+    return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int d = d0 + i;
-    if (d < rot) {
-      const float2 a = cs[d < h ? d : d - h];
-      x[i] = d < h ? turn_first(x[i], y[i], a) : turn_second(x[i], y[i], a);
-    }
+    y[i] = row && d < rot ? (float)row[d < h ? d + h : d - h] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int d = d0 + i;
+    if (d < rot) x[i] = d < h ? turn_first(x[i], y[i], a[i]) : turn_second(x[i], y[i], a[i]);
   }
 }
 

@@ -282,9 +282,8 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
       const bool has = live && d0 < D;
       uint4 raw = make_uint4(0, 0, 0, 0);
       if (has) {
-        if (a.q_f16) load8(reinterpret_cast<const __half*>(src) + d0, x);
-        else load8(reinterpret_cast<const __nv_bfloat16*>(src) + d0, x);
-        raw = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(src) + d0);
+        raw = *reinterpret_cast<const uint4*>(src + d0 * 2);
+        widen8(raw, x, __nv_bfloat16());   // used for bf16 rows alone
       }
       float back = 1.f;
       if (C::kEight && !a.q_f16) {

@@ -1,24 +1,23 @@
 // The paged key-value cache: the handle, the write of new tokens (rotation, quantisation and placement in one pass), and
 // reading cached tokens back.
 //
-// Both kernels are bound by memory: every input row is read once and every cached row written once (or the reverse). A
-// token's angles and its place are found once and serve all its heads.
+// Both kernels are bound by memory: every input row is read once and every cached row written once (or the reverse). A warp
+// takes a token, finds its place and its angles once, and runs over its rows.
 #include <new>
+#include <type_traits>
 
 #include "kv_attend.cuh"
 
 namespace lc {
 namespace {
 
-constexpr int kRowThreads = 256;
-
 struct AppendArgs {
-  int64_t n;
   const int32_t* seq;
   const int32_t* pos;
   const int32_t* rope_pos;
   Table table;
-  int q_heads, kv_heads, chunks, lanes, page_size, rotate;
+  int q_heads, kv_heads, chunks, lanes, page_size, rotate, slab;
+  int64_t tasks;
   int64_t pages;
   Rows k, v, q, q_out;
   void* pk;
@@ -51,55 +50,69 @@ __device__ __forceinline__ void store_cached(void* pool, float* scales, int64_t 
   }
 }
 
-// One token a block pass; its rows (q, then k, then v) go to the warps, 32 / lanes rows a warp at a time.
+// A warp takes a token and a slab of its rows: q, then k, then v.
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kRowThreads)
     append_kernel(const __grid_constant__ lacache_rope rope, const __grid_constant__ AppendArgs a) {
-  __shared__ float2 cs[kMaxHeadDim / 2];
+  __shared__ float2 cs[kRowThreads / 32][kMaxHeadDim / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rows_warp = 32 / a.lanes, c = lane & (a.lanes - 1), sub = lane / a.lanes;
-  const int rows = a.q_heads + 2 * a.kv_heads;
-  for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
-    const int64_t place = slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages,
-                                   threadIdx.x == 0 ? a.status : nullptr);
-    __syncthreads();
+  const int pass = 32 / a.lanes, c = lane & (a.lanes - 1), sub = lane / a.lanes;
+  const int rows = a.q_heads + 2 * a.kv_heads, slabs = (rows + a.slab - 1) / a.slab;
+  const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
+  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.tasks; task += step) {
+    const int64_t t = task / slabs;
+    const int first = (int)(task - t * slabs) * a.slab;
+    const int end = first + a.slab < rows ? first + a.slab : rows;
+    const int64_t place =
+        slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages, lane == 0 ? a.status : nullptr);
     if (place < 0) continue;
-    if (a.rotate && threadIdx.x < rope.rot_dim / 2)
-      cs[threadIdx.x] = rope_angle(rope, threadIdx.x, a.rope_pos[t], 1.f);
-    __syncthreads();
-    for (int r0 = warp * rows_warp; r0 < rows; r0 += (kRowThreads / 32) * rows_warp) {
-      const int r = r0 + sub;
-      const bool live = r < rows && c < a.chunks;
-      const int kind = r < a.q_heads ? 0 : r < a.q_heads + a.kv_heads ? 1 : 2;
-      const int h = r - (kind == 0 ? 0 : kind == 1 ? a.q_heads : a.q_heads + a.kv_heads);
-      const Rows& src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-      const T* row = reinterpret_cast<const T*>(src.p + t * src.token + (r < rows ? h : 0) * src.head);
-      float x[8] = {};
-      if (live) load8(row + c * 8, x);
-      // every lane takes part in the exchange; rows of v rotate a copy and keep their own elements
-      if (a.rotate) {
-        float y[8];
+    float2 angle[8];
+    if (a.rotate) warp_angles(rope, a.rope_pos[t], 1.f, c, cs[warp], angle);
+    for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
+      typename Chunk<T>::raw raw[kRowUnroll];
+      const unsigned char* src[kRowUnroll];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[i];
-        rotate8(y, c, a.lanes, rope.rot_dim, rope.layout, cs, row);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = kind == 2 ? x[i] : y[i];
+      for (int i = 0; i < kRowUnroll; ++i) {
+        const int r = r0 + i * pass + sub;
+        const Rows& from = r < a.q_heads ? a.q : r < a.q_heads + a.kv_heads ? a.k : a.v;
+        const int h = r < a.q_heads ? r : r < a.q_heads + a.kv_heads ? r - a.q_heads : r - a.q_heads - a.kv_heads;
+        src[i] = from.p + t * from.token + h * from.head;
+        if (r < end && c < a.chunks) raw[i] = Chunk<T>::load(src[i] + c * (8 * sizeof(T)));
+        else raw[i] = {};
       }
-      __syncwarp();
-      if (live && kind == 0)
-        store8(reinterpret_cast<T*>(a.q_out.p + t * a.q_out.token + h * a.q_out.head) + c * 8, x);
-      const int64_t at = place + (int64_t)h * a.page_size;
-      store_cached<FMT>(kind == 2 ? a.pv : a.pk, kind == 2 ? a.vs : a.ks, at, a.chunks, c, live && kind != 0, a.lanes, x);
+#pragma unroll
+      for (int i = 0; i < kRowUnroll; ++i) {
+        if (r0 + i * pass >= end) break;
+        const int r = r0 + i * pass + sub;
+        const bool live = r < end && c < a.chunks, is_q = r < a.q_heads, is_v = r >= a.q_heads + a.kv_heads;
+        float x[8];
+        Chunk<T>::widen(raw[i], x);
+        // every lane takes part in the exchange; rows of v keep their own elements
+        if (a.rotate && r0 + i * pass < a.q_heads + a.kv_heads) {
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = x[e];
+          rotate8(y, c, a.lanes, rope.rot_dim, rope.layout, angle, live ? reinterpret_cast<const T*>(src[i]) : nullptr);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = is_v ? x[e] : y[e];
+        }
+        __syncwarp();
+        if (live && is_q) store8(reinterpret_cast<T*>(a.q_out.p + t * a.q_out.token + r * a.q_out.head) + c * 8, x);
+        if (r0 + (i + 1) * pass > a.q_heads) {   // a pass with rows of k or v: its lanes share their rows' maxima
+          const int64_t at = place + (int64_t)(is_q ? 0 : is_v ? r - a.q_heads - a.kv_heads : r - a.q_heads) * a.page_size;
+          store_cached<FMT>(is_v ? a.pv : a.pk, is_v ? a.vs : a.ks, at, a.chunks, c, live && !is_q, a.lanes, x);
+        }
+      }
     }
   }
 }
 
 struct ReadArgs {
-  int64_t n;
   const int32_t* seq;
   const int32_t* pos;
   Table table;
-  int kv_heads, chunks, lanes, page_size;
+  int kv_heads, chunks, lanes, page_size, slab;
+  int64_t tasks;
   int64_t pages;
   Rows k, v;   // p == nullptr: not wanted
   const void* pk;
@@ -109,30 +122,50 @@ struct ReadArgs {
   unsigned int* status;
 };
 
+// As append_kernel: a warp takes a token and a slab of its rows, k, then v.
 template <typename T, int FMT>
 __global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant__ ReadArgs a) {
+  using Stored = typename std::conditional<FMT == LACACHE_KV_F16, __half, __nv_bfloat16>::type;
+  constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rows_warp = 32 / a.lanes, c = lane & (a.lanes - 1), sub = lane / a.lanes;
-  const int rows = 2 * a.kv_heads;
-  for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
-    const int64_t place = slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages,
-                                   threadIdx.x == 0 ? a.status : nullptr);
+  const int pass = 32 / a.lanes, c = lane & (a.lanes - 1), sub = lane / a.lanes;
+  const int rows = 2 * a.kv_heads, slabs = (rows + a.slab - 1) / a.slab;
+  const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
+  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.tasks; task += step) {
+    const int64_t t = task / slabs;
+    const int first = (int)(task - t * slabs) * a.slab;
+    const int end = first + a.slab < rows ? first + a.slab : rows;
+    const int64_t place =
+        slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages, lane == 0 ? a.status : nullptr);
     if (place < 0) continue;
-    for (int r = warp * rows_warp + sub; r < rows; r += (kRowThreads / 32) * rows_warp) {
-      const bool is_v = r >= a.kv_heads;
-      const int h = is_v ? r - a.kv_heads : r;
-      const Rows& dst = is_v ? a.v : a.k;
-      if (!dst.p || c >= a.chunks) continue;
-      const int64_t at = place + (int64_t)h * a.page_size;
-      const unsigned char* p = static_cast<const unsigned char*>(is_v ? a.pv : a.pk) + cached_at<FMT>(at, a.chunks);
-      float x[8];
-      if constexpr (FMT == LACACHE_KV_BF16)
-        load8(reinterpret_cast<const __nv_bfloat16*>(p) + c * 8, x);
-      else if constexpr (FMT == LACACHE_KV_F16)
-        load8(reinterpret_cast<const __half*>(p) + c * 8, x);
-      else
-        dequantise8<FMT>(reinterpret_cast<const uint2*>(p)[c], (is_v ? a.vs : a.ks)[at], x);
-      store8(reinterpret_cast<T*>(dst.p + t * dst.token + h * dst.head) + c * 8, x);
+    for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
+      typename std::conditional<kEight, uint2, uint4>::type raw[kRowUnroll];
+      float scale[kRowUnroll];
+#pragma unroll
+      for (int i = 0; i < kRowUnroll; ++i) {
+        const int r = r0 + i * pass + sub;
+        const bool is_v = r >= a.kv_heads;
+        if (r >= end || c >= a.chunks || !(is_v ? a.v.p : a.k.p)) continue;
+        const int64_t at = place + (int64_t)(is_v ? r - a.kv_heads : r) * a.page_size;
+        const unsigned char* p = static_cast<const unsigned char*>(is_v ? a.pv : a.pk) + cached_at<FMT>(at, a.chunks);
+        if constexpr (kEight) {
+          raw[i] = reinterpret_cast<const uint2*>(p)[c];
+          scale[i] = (is_v ? a.vs : a.ks)[at];
+        } else {
+          raw[i] = reinterpret_cast<const uint4*>(p)[c];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kRowUnroll; ++i) {
+        const int r = r0 + i * pass + sub;
+        const bool is_v = r >= a.kv_heads;
+        const Rows& dst = is_v ? a.v : a.k;
+        if (r >= end || c >= a.chunks || !dst.p) continue;
+        float x[8];
+        if constexpr (kEight) dequantise8<FMT>(raw[i], scale[i], x);
+        else widen8(raw[i], x, Stored());
+        store8(reinterpret_cast<T*>(dst.p + t * dst.token + (is_v ? r - a.kv_heads : r) * dst.head) + c * 8, x);
+      }
     }
   }
 }
@@ -252,7 +285,6 @@ extern "C" lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, cons
     return LACACHE_ERR_INVALID_ARG;
   lc::DeviceGuard guard(h->cfg.device);
   if (!guard.ok()) return LACACHE_ERR_CUDA;
-  a.n = n;
   a.seq = seq_dev;
   a.pos = pos_dev;
   a.rope_pos = rope_pos_dev ? rope_pos_dev : pos_dev;
@@ -270,7 +302,10 @@ extern "C" lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, cons
   a.status = h->dev_status;
   static const lacache_rope none = {};
   const lacache_rope& plan = rope ? *rope : none;
-  const unsigned grid = (unsigned)(n < 65536 ? n : 65536);
+  const lc::RowPlan rp = lc::plan_rows(n, a.q_heads + 2 * a.kv_heads, a.lanes);
+  a.slab = rp.slab;
+  a.tasks = rp.tasks;
+  const unsigned grid = rp.blocks;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   if (dtype == LACACHE_BF16) lc::launch_append<__nv_bfloat16>(h->cfg.format, plan, a, grid, st);
   else if (dtype == LACACHE_F16) lc::launch_append<__half>(h->cfg.format, plan, a, grid, st);
@@ -292,7 +327,6 @@ extern "C" lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const 
     return LACACHE_ERR_INVALID_ARG;
   lc::DeviceGuard guard(h->cfg.device);
   if (!guard.ok()) return LACACHE_ERR_CUDA;
-  a.n = n;
   a.seq = seq_dev;
   a.pos = pos_dev;
   a.kv_heads = h->cfg.kv_heads;
@@ -305,7 +339,10 @@ extern "C" lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const 
   a.ks = pool.k_scale;
   a.vs = pool.v_scale;
   a.status = h->dev_status;
-  const unsigned grid = (unsigned)(n < 65536 ? n : 65536);
+  const lc::RowPlan rp = lc::plan_rows(n, 2 * a.kv_heads, a.lanes);
+  a.slab = rp.slab;
+  a.tasks = rp.tasks;
+  const unsigned grid = rp.blocks;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   if (dtype == LACACHE_BF16) lc::launch_read<__nv_bfloat16>(h->cfg.format, a, grid, st);
   else if (dtype == LACACHE_F16) lc::launch_read<__half>(h->cfg.format, a, grid, st);

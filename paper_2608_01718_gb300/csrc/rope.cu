@@ -1,7 +1,7 @@
 // Rotary positions of rows of heads, and their gradient (the rotation by the negated angles).
 //
-// Bound by memory: each element is read and written once. A token's angles are computed once, into shared memory, and serve
-// all its heads. The plan (rotations as fractions of 2^64 a position) is a kernel argument.
+// Bound by memory: each element is read and written once. A warp takes a token, computes its angles once, holds those of its
+// lanes' chunks in registers, and runs over the heads. The plan (rotations as fractions of 2^64 a position) is a kernel argument.
 #include <math.h>
 
 #include "decode.cuh"
@@ -9,28 +9,42 @@
 namespace lc {
 namespace {
 
-constexpr int kRopeThreads = 256;
-
 template <typename T>
-__global__ void __launch_bounds__(kRopeThreads)
-    rope_kernel(const __grid_constant__ lacache_rope rope, int64_t n, int heads, int chunks, int lanes, Rows x,
+__global__ void __launch_bounds__(kRowThreads)
+    rope_kernel(const __grid_constant__ lacache_rope rope, int64_t tasks, int slab, int heads, int chunks, int lanes, Rows x,
                 const int32_t* __restrict__ pos, float sign, Rows y) {
-  __shared__ float2 cs[kMaxHeadDim / 2];
+  __shared__ float2 cs[kRowThreads / 32][kMaxHeadDim / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rows_warp = 32 / lanes, c = lane & (lanes - 1), sub = lane / lanes;
-  for (int64_t t = blockIdx.x; t < n; t += gridDim.x) {
-    __syncthreads();
-    if (threadIdx.x < rope.rot_dim / 2) cs[threadIdx.x] = rope_angle(rope, threadIdx.x, pos[t], sign);
-    __syncthreads();
-    for (int h0 = warp * rows_warp; h0 < heads; h0 += (kRopeThreads / 32) * rows_warp) {
-      const int h = h0 + sub;
-      const bool live = h < heads && c < chunks;
-      const T* row = reinterpret_cast<const T*>(x.p + t * x.token + (h < heads ? h : 0) * x.head);
-      float v[8] = {};
-      if (live) load8(row + c * 8, v);
-      rotate8(v, c, lanes, rope.rot_dim, rope.layout, cs, row);
-      __syncwarp();
-      if (live) store8(reinterpret_cast<T*>(y.p + t * y.token + h * y.head) + c * 8, v);
+  const int pass = 32 / lanes, c = lane & (lanes - 1), sub = lane / lanes;
+  const int slabs = (heads + slab - 1) / slab;
+  const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
+  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < tasks; task += step) {
+    const int64_t t = task / slabs;
+    const int first = (int)(task - t * slabs) * slab;
+    const int end = first + slab < heads ? first + slab : heads;
+    const unsigned char* src = x.p + t * x.token;
+    unsigned char* dst = y.p + t * y.token;
+    float2 a[8];
+    warp_angles(rope, pos[t], sign, c, cs[warp], a);
+    for (int h0 = first; h0 < end; h0 += kRowUnroll * pass) {
+      typename Chunk<T>::raw raw[kRowUnroll];
+#pragma unroll
+      for (int i = 0; i < kRowUnroll; ++i) {
+        const int h = h0 + i * pass + sub;
+        if (h < end && c < chunks) raw[i] = Chunk<T>::load(src + h * x.head + c * (8 * sizeof(T)));
+        else raw[i] = {};
+      }
+#pragma unroll
+      for (int i = 0; i < kRowUnroll; ++i) {
+        if (h0 + i * pass >= end) break;
+        const int h = h0 + i * pass + sub;
+        const bool live = h < end && c < chunks;
+        float v[8];
+        Chunk<T>::widen(raw[i], v);
+        rotate8(v, c, lanes, rope.rot_dim, rope.layout, a, live ? reinterpret_cast<const T*>(src + h * x.head) : nullptr);
+        __syncwarp();
+        if (live) store8(reinterpret_cast<T*>(dst + h * y.head) + c * 8, v);
+      }
     }
   }
 }
@@ -83,16 +97,14 @@ extern "C" lacache_status lacache_rope_apply(const lacache_rope* rope, int64_t n
   if (head_dim % 8 || head_dim > lc::kMaxHeadDim) return LACACHE_ERR_UNSUPPORTED;
   if (n == 0) return LACACHE_OK;
   if (!pos_dev || !lc::device_rows(x, dtype, &xr) || !lc::device_rows(y, dtype, &yr)) return LACACHE_ERR_INVALID_ARG;
-  const unsigned grid = (unsigned)(n < 65536 ? n : 65536);
   const int lanes = lc::lanes_for(head_dim);
+  const lc::RowPlan plan = lc::plan_rows(n, heads, lanes);
   const float sign = inverse ? -1.f : 1.f;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (dtype == LACACHE_BF16)
-    lc::rope_kernel<__nv_bfloat16><<<grid, lc::kRopeThreads, 0, st>>>(*rope, n, heads, head_dim / 8, lanes, xr, pos_dev,
-                                                                     sign, yr);
-  else if (dtype == LACACHE_F16)
-    lc::rope_kernel<__half><<<grid, lc::kRopeThreads, 0, st>>>(*rope, n, heads, head_dim / 8, lanes, xr, pos_dev, sign, yr);
-  else
-    lc::rope_kernel<float><<<grid, lc::kRopeThreads, 0, st>>>(*rope, n, heads, head_dim / 8, lanes, xr, pos_dev, sign, yr);
+  auto* kernel = dtype == LACACHE_BF16  ? lc::rope_kernel<__nv_bfloat16>
+                 : dtype == LACACHE_F16 ? lc::rope_kernel<__half>
+                                        : lc::rope_kernel<float>;
+  kernel<<<plan.blocks, lc::kRowThreads, 0, st>>>(*rope, plan.tasks, plan.slab, heads, head_dim / 8, lanes, xr, pos_dev,
+                                                   sign, yr);
   return lc::from_cuda(cudaGetLastError());
 }
