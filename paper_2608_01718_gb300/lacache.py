@@ -550,31 +550,51 @@ class LaCache:
         return lacache_last_launch(self.h)
 
 
+_DTYPES: dict = {}   # torch dtype -> lacache_dtype, filled on first use (torch is imported late)
+
+
 def _dtype(t) -> int:
     """The lacache_dtype of a tensor's elements."""
-    import torch
-    got = {torch.bfloat16: LACACHE_BF16, torch.float16: LACACHE_F16, torch.float32: LACACHE_F32}.get(t.dtype)
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: LACACHE_BF16, torch.float16: LACACHE_F16, torch.float32: LACACHE_F32})
+    got = _DTYPES.get(t.dtype)
     if got is None:
         raise ValueError(f"rows are bf16, f16 or f32, not {t.dtype}")
     return got
 
 
-def _rows(name: str, t, n: int, heads: int | None, head_dim: int, device: int, like=None) -> lacache_rows:
+def _current_stream(cuda_stream, device: int) -> int:
+    """As _stream, for the calls that decode token by token: torch's raw handle where it offers one (a microsecond less)."""
+    if cuda_stream is not None:
+        return _stream(cuda_stream)
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else _stream(None, device)
+
+
+def _rows(name: str, t, n: int, heads: int, head_dim: int, device: int, dtype) -> lacache_rows:
     """A [n x heads x head_dim] CUDA tensor (any strides, dense rows) as lacache_rows."""
-    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != head_dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} is [{n} x {'heads' if heads is None else heads} x {head_dim}], not {tuple(t.shape)}")
-    if t.stride(2) != 1 or not t.is_cuda or t.device.index != device or (like is not None and t.dtype != like):
-        raise ValueError(f"{name} has dense rows on cuda:{device}" + ("" if like is None else f" of {like}"))
-    return lacache_rows(t.data_ptr(), t.stride(0), t.stride(1))
+    if t.shape != (n, heads, head_dim):
+        raise ValueError(f"{name} is [{n} x {heads} x {head_dim}], not {tuple(t.shape)}")
+    stride = t.stride()
+    if stride[2] != 1 or t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{name} has dense rows of {dtype} on cuda:{device}")
+    return lacache_rows(t.data_ptr(), stride[0], stride[1])
 
 
 def _index(name: str, t, n: int, device: int) -> int:
     """An int32 [n] CUDA tensor's address."""
     import torch
-    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device.index != device \
-            or not t.is_cuda:
+    if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != device:
         raise ValueError(f"{name} is a dense int32 tensor of {n} on cuda:{device}")
     return t.data_ptr()
+
+
+def _three(name: str, t):
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{name} is a [tokens x heads x head_dim] CUDA tensor")
+    return t.shape
 
 
 class Rope:
@@ -597,16 +617,18 @@ class Rope:
         """x [n x heads x head_dim] rotated at ``pos`` (int32 [n]) into ``out`` (new if None; x itself for in place).
         ``inverse``: the transpose, which is the gradient."""
         import torch
+        n, heads, head_dim = _three("x", x)
+        device, dtype = x.get_device(), x.dtype
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
-        n, heads, head_dim = x.shape
-        device = x.device.index
-        rx = _rows("x", x, n, heads, head_dim, device)
-        ro = _rows("out", out, n, heads, head_dim, device, like=x.dtype)
-        _index("pos", pos, n, device)
-        with torch.cuda.device(device):
-            lacache_rope_apply(self.plan, n, heads, head_dim, _dtype(x), rx, pos, inverse, ro,
-                               _stream(cuda_stream, device))
+        args = (self.plan, n, heads, head_dim, _dtype(x), _rows("x", x, n, heads, head_dim, device, dtype),
+                _index("pos", pos, n, device), inverse, _rows("out", out, n, heads, head_dim, device, dtype),
+                _current_stream(cuda_stream, device))
+        if torch.cuda.current_device() == device:
+            lacache_rope_apply(*args)
+        else:
+            with torch.cuda.device(device):
+                lacache_rope_apply(*args)
         return out
 
 
@@ -671,46 +693,42 @@ class KVCache:
 
     def _table(self, table) -> lacache_kv_table:
         import torch
-        if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1 or table.device.index != self.device:
+        if table.dim() != 2 or table.dtype != torch.int32 or table.stride(1) != 1 or table.get_device() != self.device:
             raise ValueError(f"a table is an int32 [sequences x pages] tensor on cuda:{self.device} with dense rows")
-        return lacache_kv_table(table.data_ptr(), table.stride(0), table.shape[0], table.shape[1])
+        seqs, width = table.shape
+        return lacache_kv_table(table.data_ptr(), table.stride(0), seqs, width)
 
     def append(self, k, v, seq, pos, table, layer: int = 0, rope: Rope | None = None, rope_pos=None, q=None, q_out=None,
                cuda_stream=None):
         """Write k and v [n x kv_heads x head_dim] at positions ``pos`` of sequences ``seq`` (int32 [n]; -1 skips a token),
         k rotated by ``rope`` first. With ``q``, returns it rotated (in ``q_out`` if given)."""
-        import torch
-        n, D, dev = k.shape[0], self.cfg.head_dim, self.device
-        rk = _rows("k", k, n, self.cfg.kv_heads, D, dev)
-        rv = _rows("v", v, n, self.cfg.kv_heads, D, dev, like=k.dtype)
-        rq = ro = None
+        n, heads, D, dev, dtype = k.shape[0], self.cfg.kv_heads, self.cfg.head_dim, self.device, k.dtype
+        q_heads, rq, ro = 0, None, None
         if q is not None:
+            q_heads = _three("q", q)[1]
             if q_out is None:
+                import torch
                 q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            rq = _rows("q", q, n, None, D, dev, like=k.dtype)
-            ro = _rows("q_out", q_out, n, q.shape[1], D, dev, like=k.dtype)
-        _index("seq", seq, n, dev)
-        _index("pos", pos, n, dev)
-        if rope_pos is not None:
-            _index("rope_pos", rope_pos, n, dev)
-        lacache_kv_append(self.h, layer, self._table(table), n, seq, pos, None if rope is None else rope.plan, rope_pos,
-                          _dtype(k), rk, rv, 0 if q is None else q.shape[1], rq, ro, _stream(cuda_stream, dev))
+            rq, ro = _rows("q", q, n, q_heads, D, dev, dtype), _rows("q_out", q_out, n, q_heads, D, dev, dtype)
+        lacache_kv_append(self.h, layer, self._table(table), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
+                          None if rope is None else rope.plan,
+                          None if rope_pos is None else _index("rope_pos", rope_pos, n, dev), _dtype(k),
+                          _rows("k", k, n, heads, D, dev, dtype), _rows("v", v, n, heads, D, dev, dtype), q_heads, rq, ro,
+                          _current_stream(cuda_stream, dev))
         return q_out
 
     def read(self, seq, pos, table, layer: int = 0, dtype=None, k_out=None, v_out=None, cuda_stream=None):
         """The cached rows (k, v) of n tokens, into ``k_out`` and ``v_out`` or new tensors of ``dtype`` (bf16)."""
-        import torch
-        n, D, dev = seq.shape[0], self.cfg.head_dim, self.device
+        n, heads, D, dev = seq.shape[0], self.cfg.kv_heads, self.cfg.head_dim, self.device
         if k_out is None and v_out is None:
-            dtype = torch.bfloat16 if dtype is None else dtype
-            k_out = torch.empty(n, self.cfg.kv_heads, D, dtype=dtype, device=f"cuda:{dev}")
+            import torch
+            k_out = torch.empty(n, heads, D, dtype=torch.bfloat16 if dtype is None else dtype, device=f"cuda:{dev}")
             v_out = torch.empty_like(k_out)
         some = k_out if k_out is not None else v_out
-        rk, rv = (None if t is None else _rows(name, t, n, self.cfg.kv_heads, D, dev, like=some.dtype)
-                  for name, t in (("k_out", k_out), ("v_out", v_out)))
-        _index("seq", seq, n, dev)
-        _index("pos", pos, n, dev)
-        lacache_kv_read(self.h, layer, self._table(table), n, seq, pos, _dtype(some), rk, rv, _stream(cuda_stream, dev))
+        lacache_kv_read(self.h, layer, self._table(table), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
+                        _dtype(some), None if k_out is None else _rows("k_out", k_out, n, heads, D, dev, some.dtype),
+                        None if v_out is None else _rows("v_out", v_out, n, heads, D, dev, some.dtype),
+                        _current_stream(cuda_stream, dev))
         return k_out, v_out
 
     def attend(self, q, table, lengths, new_tokens: int = 1, layer: int = 0, starts=None, window: int = 0,
@@ -718,24 +736,22 @@ class KVCache:
         """Attention of the last ``new_tokens`` tokens of each sequence: q [sequences * new_tokens x q_heads x head_dim],
         ``lengths`` (int32) with the new tokens counted. Returns ``out``; ``lse`` (fp32 [tokens x q_heads]) is filled if
         given. ``scale`` is 1 / sqrt(head_dim) if None."""
-        import torch
-        seqs, D, dev = table.shape[0], self.cfg.head_dim, self.device
-        n = seqs * new_tokens
+        heads, D, dev, dtype = _three("q", q)[1], self.cfg.head_dim, self.device, q.dtype
+        t = self._table(table)
+        n = t.seqs * new_tokens
         if out is None:
+            import torch
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        if q.dim() != 3:
-            raise ValueError("q is [tokens x heads x head_dim]")
-        heads = q.shape[1]
-        a = lacache_attention(new_tokens, heads, window, _dtype(q), D ** -0.5 if scale is None else scale,
-                              _index("lengths", lengths, seqs, dev),
-                              None if starts is None else _index("starts", starts, seqs, dev),
-                              _rows("q", q, n, heads, D, dev), _rows("out", out, n, heads, D, dev, like=q.dtype), None)
         if lse is not None:
-            if lse.dtype != torch.float32 or tuple(lse.shape) != (n, heads) or not lse.is_contiguous() or \
-                    lse.device.index != dev:
+            import torch
+            if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
                 raise ValueError(f"lse is a dense fp32 [{n} x {heads}] tensor on cuda:{dev}")
-            a.lse_dev = lse.data_ptr()
-        lacache_kv_attend(self.h, layer, self._table(table), a, _stream(cuda_stream, dev))
+        a = lacache_attention(new_tokens, heads, window, _dtype(q), D ** -0.5 if scale is None else scale,
+                              _index("lengths", lengths, t.seqs, dev),
+                              None if starts is None else _index("starts", starts, t.seqs, dev),
+                              _rows("q", q, n, heads, D, dev, dtype), _rows("out", out, n, heads, D, dev, dtype),
+                              None if lse is None else lse.data_ptr())
+        lacache_kv_attend(self.h, layer, t, a, _current_stream(cuda_stream, dev))
         return out
 
     def sync(self) -> None:
