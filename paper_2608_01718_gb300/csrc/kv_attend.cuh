@@ -13,9 +13,10 @@
 //   S^T [16 keys x 8 rows] = K [16 x d] Q^T [d x 8],   O^T [16 dims x 8 rows] += V^T [16 dims x 16 keys] P^T [16 keys x 8]
 // The order of a contraction is free, and so is the naming of V's dimensions, so each lane takes 16 contiguous bytes of a
 // row of K or V as its share of several instructions' A operand: lane (g, t) = (lane / 4, lane % 4) owns bytes 16 t of every
-// 64 of key rows g and g + 8 of K, and of V bytes 16 g of every 128 of the rows of keys 2t, 2t+1, 2t+8 and 2t+9. Nothing is
-// shared between lanes: the copies to shared memory (cp.async) are a deep register file with an asynchronous front, without
-// bank conflicts, swizzles or barriers. P^T is the transpose of the S^T accumulator, one movmatrix for 8 x 8.
+// 64 of key rows g and g + 8 of K, and (8-bit formats) of V bytes 16 g of every 128 of the rows of keys 2t, 2t+1, 2t+8 and 2t+9. Those
+// copies to shared memory (cp.async) are a deep register file with an asynchronous front: each lane reads back what it copied
+// itself. A 16-bit V goes through shared memory in swizzled rows and comes back transposed (ldmatrix); 8-bit codes are
+// widened first and paired by byte permutes. Nothing is shared between warps: no barriers in the loop. P^T is the transpose of the S^T accumulator, one movmatrix for 8 x 8.
 //
 // Softmax. Base 2, running maximum m a row, moved only when a score exceeds it by more than 8: weights then stay below 2^8,
 // the sum is fp32, and most tiles need a vote instead of a maximum over the lanes. Weights: f16 for f16 and 8-bit caches (11
@@ -66,7 +67,7 @@ struct AttendArgs {
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
-constexpr int kMinUnits = 2;                 // a block's least part: fewer units a block cost more in joins than they gain
+constexpr int kMinUnits = 1;                 // a block's least part
 constexpr int kMaxRowTile = 32;
 constexpr int kMaxPositions = 1 << 30;      // a table's reach is cut to this
 constexpr int kMaxDevices = 64;
@@ -94,7 +95,8 @@ struct AttendConfig {
   static constexpr int kKPieces = DP * kItem / 64;                       // 16-byte pieces of a lane in a row of K
   static constexpr int kVBytes = DP * kItem >= 128 ? 16 : 8;             // bytes of a piece of V
   static constexpr int kVPieces = DP * kItem / (8 * kVBytes);
-  static constexpr int kVElems = kVBytes / kItem;                        // dimensions of a piece of V
+  static constexpr int kUnits = DP / 8 < 32 ? DP / 8 : 32;               // 16-bit V: 16-byte units of a row
+  static constexpr int kUnitRows = 32 / kUnits;                          // ... and rows that one copy of the warp covers
   static constexpr int kTileBytes = 16 * DP * kItem;                     // K (or V) of 16 keys
   static constexpr int kStageBytes = kSub * 2 * kTileBytes + (kEight ? kKeys * 8 : 0);
   static constexpr int kStages = DP == 256 && !kEight ? 3 : kStageBytes <= 4096 + 256 ? 6 : kStageBytes <= 8192 + 256 ? 3 : 3;
@@ -144,6 +146,20 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Four 8 x 8 tiles of 16-bit values from shared memory, transposed: lane l names the 16-byte row l % 8 of tile l / 8.
+__device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t& a0, uint32_t& a1, uint32_t& a2, uint32_t& a3) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3)
+               : "r"(addr)
+               : "memory");
+}
+// Where a 16-bit row of V (key j of its tile) keeps its 16-byte unit u: eight keys' units of one column lie in different
+// banks.
+template <int DP>
+__device__ __forceinline__ int v_unit(int j, int u) {
+  return j * (DP * 2) + ((u ^ (j & 7)) * 16);
 }
 
 // Four codes as f16 pairs: elements 0, 1 and 2, 3. Exact.
@@ -206,6 +222,7 @@ template <int FMT, int DP, int NT>
 __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_constant__ AttendArgs a) {
   using C = AttendConfig<FMT, DP, NT>;
   constexpr bool kBf16 = FMT == LACACHE_KV_BF16;
+  constexpr bool kQInRegs = NT * DP <= 128;   // more would spill: q is read from shared memory at its use
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float stat_m[kAttendWarps][C::kRows], stat_l[kAttendWarps][C::kRows];
   __shared__ int row_pos[C::kRows], row_lo[C::kRows];   // a row's own last and first visible position
@@ -270,8 +287,130 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
       if (raw < 0 || raw > a.max_len) atomicOr(a.status, kBadIndex);
     }
 
-    // ---- q into shared memory, in the order of the K pieces ----
     __syncthreads();   // the previous triple's readers are done
+
+    // ---- this warp's keys: KT from each unit ----
+    const int key0 = (sp.lo & ~15) + first_unit * C::kUnit + warp * C::kKeys;
+      const int32_t* table_row = a.table.pages + seq * a.table.stride;
+
+    // page ids of the stage that is issued next, read one stage ahead of their use
+    int next_page[C::kSub], next_slot[C::kSub];
+    auto look_up = [&](int i) {
+      const int key = key0 + i * C::kUnit;
+#pragma unroll
+      for (int s = 0; s < C::kSub; ++s) {
+        const int at = key + 16 * s;
+        next_page[s] = -1;
+        next_slot[s] = 0;
+        if (i < units && at < sp.hi) {
+          const int index = at / a.page_size;
+          next_slot[s] = at - index * a.page_size;
+          next_page[s] = __ldg(table_row + index);
+        }
+      }
+    };
+    auto issue = [&](int i) {
+      if (i < units) {
+        const int stage = i % C::kStages;
+        const uint32_t at = ring_addr + stage * C::kStageBytes;
+        const int key = key0 + i * C::kUnit;
+#pragma unroll
+        for (int s = 0; s < C::kSub; ++s) {
+          const int k0 = key + 16 * s;
+          int page = next_page[s];
+          if (page < 0 || page >= a.pages) {
+            if (k0 < sp.hi && lane == 0) atomicOr(a.status, kBadIndex);
+            page = -1;
+          }
+          if (lane == 0) page_ids[warp][stage][s] = page;
+          const int64_t row = ((int64_t)(page < 0 ? 0 : page) * a.kv_heads + head) * a.page_size + next_slot[s];
+          const unsigned char* kp = a.pk + row * (int64_t)(D * C::kItem);
+          const unsigned char* vp = a.pv + row * (int64_t)(D * C::kItem);
+          // a key outside [lo, hi) is not read: zeros take its place
+          auto inside = [&](int j) { return page >= 0 && k0 + j >= sp.lo && k0 + j < sp.hi; };
+          const uint32_t kd = at + s * 2 * C::kTileBytes, vd = kd + C::kTileBytes;
+          const int row_bytes = D * C::kItem;
+          const unsigned char* ksrc = kp + (int64_t)(g * row_bytes + t * 16);
+          if (D == DP && page >= 0 && k0 >= sp.lo && k0 + 16 <= sp.hi) {   // nothing to leave out: most tiles
+#pragma unroll
+            for (int c = 0; c < C::kKPieces; ++c) {
+              copy_async<16>(kd + c * 512 + lane * 16, ksrc + c * 64, true);
+              copy_async<16>(kd + (C::kKPieces + c) * 512 + lane * 16, ksrc + 8 * DP * C::kItem + c * 64, true);
+            }
+            if constexpr (C::kEight) {
+              const unsigned char* vsrc = vp + 2 * t * DP + g * C::kVBytes;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int c = 0; c < C::kVPieces; ++c)
+                  copy_async<C::kVBytes>(vd + (r * C::kVPieces + c) * (32 * C::kVBytes) + lane * C::kVBytes,
+                                         vsrc + ((r & 1) + 8 * (r >> 1)) * DP + c * 8 * C::kVBytes, true);
+              }
+            } else {
+              const unsigned char* vsrc = vp + (lane / C::kUnits) * (DP * 2) + (lane % C::kUnits) * 16;
+#pragma unroll
+              for (int i = 0; i < C::kUnits / 2; ++i)
+                copy_async<16>(vd + v_unit<DP>(i * C::kUnitRows + lane / C::kUnits, lane % C::kUnits), vsrc + i * 512, true);
+            }
+          } else {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const bool in = inside(g + 8 * r);
+#pragma unroll
+              for (int c = 0; c < C::kKPieces; ++c) {
+                const bool live = in && (c * 64 + t * 16) < row_bytes;
+                copy_async<16>(kd + (r * C::kKPieces + c) * 512 + lane * 16, live ? ksrc + 8 * r * row_bytes + c * 64 : a.pk,
+                               live);
+              }
+            }
+            if constexpr (C::kEight) {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int j = 2 * t + (r & 1) + 8 * (r >> 1);
+                const bool in = inside(j);
+#pragma unroll
+                for (int c = 0; c < C::kVPieces; ++c) {
+                  const int d = c * 8 * C::kVBytes + g * C::kVBytes;
+                  const bool live = in && d < row_bytes;
+                  copy_async<C::kVBytes>(vd + (r * C::kVPieces + c) * (32 * C::kVBytes) + lane * C::kVBytes,
+                                         live ? vp + j * row_bytes + d : a.pv, live);
+                }
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < C::kUnits / 2; ++i) {
+                const int j = i * C::kUnitRows + lane / C::kUnits, unit = lane % C::kUnits;
+                const bool live = inside(j) && unit * 16 < row_bytes;
+                copy_async<16>(vd + v_unit<DP>(j, unit), live ? vp + j * row_bytes + unit * 16 : a.pv, live);
+              }
+            }
+          }
+          if constexpr (C::kEight) {
+            // scales: lanes 0-15 those of k, 16-31 those of v
+            const int j = lane & 15;
+            const bool in = inside(j);
+            const float* src = (lane < 16 ? a.ks : a.vs) + (in ? row + j : 0);
+            copy_async<4>(at + C::kSub * 2 * C::kTileBytes + (s * 32 + lane) * 4, src, in);
+          }
+        }
+        look_up(i + 1);
+      }
+      copy_commit();
+    };
+
+    int all_hi, all_lo;   // positions that every live row sees: [all_lo, all_hi]
+    const bool rows_differ = a.new_tokens > 1;
+    float factor[NT][2];
+    uint4 qreg[kQInRegs ? NT * C::kKPieces * (C::kEight ? 2 : 1) : 1];
+    float o[C::kMTiles][NT][4];
+    float m[NT][2], l[NT][2], inv[NT][2];
+    bool split = kBf16, again = false;   // bf16 weights in two terms
+    do {
+      look_up(0);
+#pragma unroll 1
+      for (int i = 0; i < C::kStages - 1; ++i) issue(i);
+      if (!again) {
+    // ---- q into shared memory, in the order of the K pieces, while the first keys are on their way ----
     for (int r = warp; r < C::kRows; r += kAttendWarps) {
       const int row = row0 + r;
       const bool live = r < live_rows;
@@ -315,109 +454,31 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
     }
     __syncthreads();
 
-    // positions that every live row sees: [all_lo, all_hi]
-    const int all_hi = row_pos[0], all_lo = row_lo[live_rows - 1];
-    const bool rows_differ = a.new_tokens > 1;
-    float factor[NT][2];
+    all_hi = row_pos[0];
+    all_lo = row_lo[live_rows - 1];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       factor[n][0] = row_factor[n * 8 + 2 * t];
       factor[n][1] = row_factor[n * 8 + 2 * t + 1];
     }
-    uint4 qreg[NT == 1 ? C::kKPieces * (C::kEight ? 2 : 1) : 1];
-    if constexpr (NT == 1) {
+    if constexpr (kQInRegs) {
 #pragma unroll
-      for (int c = 0; c < C::kKPieces; ++c) {
-        if constexpr (C::kEight) {
-          const uint4* p = reinterpret_cast<const uint4*>(q_smem + g * C::kQStride + (c * 64 + t * 16) * 2);
-          qreg[2 * c] = p[0];
-          qreg[2 * c + 1] = p[1];
-        } else {
-          qreg[c] = *reinterpret_cast<const uint4*>(q_smem + g * C::kQStride + (c * 32 + t * 8) * 2);
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int c = 0; c < C::kKPieces; ++c) {
+          const unsigned char* q = q_smem + (n * 8 + g) * C::kQStride;
+          if constexpr (C::kEight) {
+            const uint4* p = reinterpret_cast<const uint4*>(q + (c * 64 + t * 16) * 2);
+            qreg[(n * C::kKPieces + c) * 2] = p[0];
+            qreg[(n * C::kKPieces + c) * 2 + 1] = p[1];
+          } else {
+            qreg[n * C::kKPieces + c] = *reinterpret_cast<const uint4*>(q + (c * 32 + t * 8) * 2);
+          }
         }
       }
     }
 
-    // ---- this warp's keys: KT from each unit ----
-    const int key0 = (sp.lo & ~15) + first_unit * C::kUnit + warp * C::kKeys;
-      const int32_t* table_row = a.table.pages + seq * a.table.stride;
-
-    // page ids of the stage that is issued next, read one stage ahead of their use
-    int next_page[C::kSub], next_slot[C::kSub];
-    auto look_up = [&](int i) {
-      const int key = key0 + i * C::kUnit;
-#pragma unroll
-      for (int s = 0; s < C::kSub; ++s) {
-        const int at = key + 16 * s;
-        next_page[s] = -1;
-        next_slot[s] = 0;
-        if (i < units && at < sp.hi) {
-          const int index = at / a.page_size;
-          next_slot[s] = at - index * a.page_size;
-          next_page[s] = __ldg(table_row + index);
-        }
       }
-    };
-    auto issue = [&](int i) {
-      if (i < units) {
-        const int stage = i % C::kStages;
-        const uint32_t at = ring_addr + stage * C::kStageBytes;
-        const int key = key0 + i * C::kUnit;
-#pragma unroll
-        for (int s = 0; s < C::kSub; ++s) {
-          const int k0 = key + 16 * s;
-          int page = next_page[s];
-          if (page < 0 || page >= a.pages) {
-            if (k0 < sp.hi && lane == 0) atomicOr(a.status, kBadIndex);
-            page = -1;
-          }
-          if (lane == 0) page_ids[warp][stage][s] = page;
-          const int64_t row = ((int64_t)(page < 0 ? 0 : page) * a.kv_heads + head) * a.page_size + next_slot[s];
-          const unsigned char* kp = a.pk + row * (int64_t)(D * C::kItem);
-          const unsigned char* vp = a.pv + row * (int64_t)(D * C::kItem);
-          // a key outside [lo, hi) is not read: zeros take its place
-          auto inside = [&](int j) { return page >= 0 && k0 + j >= sp.lo && k0 + j < sp.hi; };
-          const uint32_t kd = at + s * 2 * C::kTileBytes, vd = kd + C::kTileBytes;
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const int j = g + 8 * r;
-            const bool in = inside(j);
-            const unsigned char* src = kp + (int64_t)j * (D * C::kItem) + t * 16;
-#pragma unroll
-            for (int c = 0; c < C::kKPieces; ++c) {
-              const bool live = in && (c * 64 + t * 16) < D * C::kItem;
-              copy_async<16>(kd + (r * C::kKPieces + c) * 512 + lane * 16, live ? src + c * 64 : a.pk, live);
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int j = 2 * t + (r & 1) + 8 * (r >> 1);
-            const bool in = inside(j);
-            const unsigned char* src = vp + (int64_t)j * (D * C::kItem) + g * C::kVBytes;
-#pragma unroll
-            for (int c = 0; c < C::kVPieces; ++c) {
-              const bool live = in && (c * 8 * C::kVBytes + g * C::kVBytes) < D * C::kItem;
-              copy_async<C::kVBytes>(vd + (r * C::kVPieces + c) * (32 * C::kVBytes) + lane * C::kVBytes,
-                                     live ? src + c * 8 * C::kVBytes : a.pv, live);
-            }
-          }
-          if constexpr (C::kEight) {
-            // scales: lanes 0-15 those of k, 16-31 those of v
-            const int j = lane & 15;
-            const bool in = inside(j);
-            const float* src = (lane < 16 ? a.ks : a.vs) + (in ? row + j : 0);
-            copy_async<4>(at + C::kSub * 2 * C::kTileBytes + (s * 32 + lane) * 4, src, in);
-          }
-        }
-        look_up(i + 1);
-      }
-      copy_commit();
-    };
-
-    float o[C::kMTiles][NT][4];
-    float m[NT][2], l[NT][2], inv[NT][2];
-    bool split = kBf16, again = false;   // bf16 weights in two terms
-    do {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -426,10 +487,6 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
       l[n][0] = l[n][1] = 0.f;
       inv[n][0] = inv[n][1] = C::kEight ? 0x1p126f : 1.f;
     }
-    look_up(0);
-#pragma unroll
-    for (int i = 0; i < C::kStages - 1; ++i) issue(i);
-
     for (int i = 0; i < units; ++i) {
       issue(i + C::kStages - 1);
       copy_wait<C::kStages - 1>();
@@ -460,8 +517,8 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               uint4 q0, q1;
-              if constexpr (NT == 1) {
-                q0 = qreg[2 * c], q1 = qreg[2 * c + 1];
+              if constexpr (kQInRegs) {
+                q0 = qreg[(n * C::kKPieces + c) * 2], q1 = qreg[(n * C::kKPieces + c) * 2 + 1];
               } else {
                 const uint4* p = reinterpret_cast<const uint4*>(q_smem + (n * 8 + g) * C::kQStride + (c * 64 + t * 16) * 2);
                 q0 = p[0], q1 = p[1];
@@ -475,7 +532,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               uint4 q;
-              if constexpr (NT == 1) q = qreg[c];
+              if constexpr (kQInRegs) q = qreg[n * C::kKPieces + c];
               else q = *reinterpret_cast<const uint4*>(q_smem + (n * 8 + g) * C::kQStride + (c * 32 + t * 8) * 2);
               mma16816<kBf16>(s[b][n], x.x, y.x, x.y, y.y, q.x, q.y);
               mma16816<kBf16>(s[b][n], x.z, y.z, x.w, y.w, q.z, q.w);
@@ -605,74 +662,76 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
         const unsigned char* vt = st + b * 2 * C::kTileBytes + C::kTileBytes;
         // a value that is not finite at a position that only some rows see: the product would put 0 x it into the others.
         // It is taken out of the product here and added for the rows that see it.
+        constexpr uint32_t ones = kBf16 ? 0x7f80u : 0x7c00u;
         bool fix = false;
-        if (!C::kEight && some_masked && rows_differ) {
-          constexpr uint32_t ones = kBf16 ? 0x7f80u : 0x7c00u;
+        if constexpr (!C::kEight) {
+          if (some_masked && rows_differ) {
 #pragma unroll
-          for (int r = 0; r < 4 * C::kVPieces; ++r) {
-            const uint4 x = *reinterpret_cast<const uint4*>(vt + r * 512 + lane * 16);
-            const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+            for (int i = 0; i < C::kTileBytes / 512; ++i) {
+              const uint4 x = *reinterpret_cast<const uint4*>(vt + i * 512 + lane * 16);
+              const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) fix |= (xw[w] & ones) == ones || ((xw[w] >> 16) & ones) == ones;
+              for (int w = 0; w < 4; ++w) fix |= (xw[w] & ones) == ones || ((xw[w] >> 16) & ones) == ones;
+            }
+            fix = __any_sync(0xffffffffu, fix);
           }
-          fix = __any_sync(0xffffffffu, fix);
         }
-        auto clean = [&](uint32_t x) {
-          constexpr uint32_t ones = kBf16 ? 0x7f80u : 0x7c00u;
-          if ((x & ones) == ones) x &= 0xffff0000u;
-          if (((x >> 16) & ones) == ones) x &= 0x0000ffffu;
-          return x;
-        };
+        auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
-        for (int c = 0; c < C::kVPieces; ++c) {
-          uint32_t x[4][4];   // [key][word]
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            if constexpr (C::kVBytes == 16) {
-              const uint4 y = *reinterpret_cast<const uint4*>(vt + (r * C::kVPieces + c) * 512 + lane * 16);
-              x[r][0] = y.x, x[r][1] = y.y, x[r][2] = y.z, x[r][3] = y.w;
-            } else {
-              const uint2 y = *reinterpret_cast<const uint2*>(vt + (r * C::kVPieces + c) * 256 + lane * 8);
-              x[r][0] = y.x, x[r][1] = y.y;
+          for (int n = 0; n < NT; ++n) {
+            mma16816<kBf16>(o[d][n], a0, a1, a2, a3, p0[n], p1[n]);
+            if constexpr (kBf16) {
+              if (split) mma16816<true>(o[d][n], a0, a1, a2, a3, r0[n], r1[n]);
             }
           }
-          if (!C::kEight && fix) {
+        };
+        if constexpr (C::kEight) {
+#pragma unroll
+          for (int c = 0; c < C::kVPieces; ++c) {
+            uint32_t x[4][4];   // [key][word]
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-#pragma unroll
-              for (int w = 0; w < 4; ++w) x[r][w] = clean(x[r][w]);
-            }
-          }
-          auto product = [&](int d, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3) {
-            const uint32_t a0 = __byte_perm(v0, v1, 0x5410), a1 = __byte_perm(v0, v1, 0x7632);
-            const uint32_t a2 = __byte_perm(v2, v3, 0x5410), a3 = __byte_perm(v2, v3, 0x7632);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              mma16816<kBf16>(o[d][n], a0, a1, a2, a3, p0[n], p1[n]);
-              if constexpr (kBf16) {
-                if (split) mma16816<true>(o[d][n], a0, a1, a2, a3, r0[n], r1[n]);
+              if constexpr (C::kVBytes == 16) {
+                const uint4 y = *reinterpret_cast<const uint4*>(vt + (r * C::kVPieces + c) * 512 + lane * 16);
+                x[r][0] = y.x, x[r][1] = y.y, x[r][2] = y.z, x[r][3] = y.w;
+              } else {
+                const uint2 y = *reinterpret_cast<const uint2*>(vt + (r * C::kVPieces + c) * 256 + lane * 8);
+                x[r][0] = y.x, x[r][1] = y.y;
               }
             }
-          };
-          if constexpr (C::kEight) {
 #pragma unroll
             for (int w = 0; w < C::kVBytes / 4; ++w) {
               uint32_t lo[4], hi[4];
 #pragma unroll
               for (int r = 0; r < 4; ++r) widen4<FMT>(x[r][w], lo[r], hi[r]);
-              product(c * (C::kVElems / 2) + 2 * w, lo[0], lo[1], lo[2], lo[3]);
-              product(c * (C::kVElems / 2) + 2 * w + 1, hi[0], hi[1], hi[2], hi[3]);
+              const int d = c * (C::kVBytes / 2) + 2 * w;
+              product(d, __byte_perm(lo[0], lo[1], 0x5410), __byte_perm(lo[0], lo[1], 0x7632),
+                      __byte_perm(lo[2], lo[3], 0x5410), __byte_perm(lo[2], lo[3], 0x7632));
+              product(d + 1, __byte_perm(hi[0], hi[1], 0x5410), __byte_perm(hi[0], hi[1], 0x7632),
+                      __byte_perm(hi[2], hi[3], 0x5410), __byte_perm(hi[2], hi[3], 0x7632));
             }
-          } else {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) product(c * 4 + w, x[0][w], x[1][w], x[2][w], x[3][w]);
           }
-        }
-        if constexpr (!C::kEight) {
+        } else {
+          // tiles of a fragment: dims 0-7 and 8-15 of keys 0-7, then of keys 8-15
+          const uint32_t v_addr = shared_addr(vt);
+          const int j = (lane & 7) + ((lane & 16) >> 1), half = (lane >> 3) & 1;
+#pragma unroll
+          for (int d = 0; d < C::kMTiles; ++d) {
+            uint32_t a0, a1, a2, a3;
+            load_transposed(v_addr + v_unit<DP>(j, 2 * d + half), a0, a1, a2, a3);
+            if (fix) {
+              auto clean = [](uint32_t x) {
+                if ((x & ones) == ones) x &= 0xffff0000u;
+                if (((x >> 16) & ones) == ones) x &= 0x0000ffffu;
+                return x;
+              };
+              a0 = clean(a0), a1 = clean(a1), a2 = clean(a2), a3 = clean(a3);
+            }
+            product(d, a0, a1, a2, a3);
+          }
           if (fix) {
             const int k0 = key + 16 * b;
             for (int j = 0; j < 16; ++j) {
-              const int slot = (j & 1) + (j >= 8 ? 2 : 0), from = g * 4 + ((j & 7) >> 1);
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 const float w0 = __shfl_sync(0xffffffffu, j < 8 ? s[b][n][0] : s[b][n][2], (j & 7) * 4 + t);
@@ -682,12 +741,10 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
                 const bool see1 = k0 + j <= row_pos[r + 1] && k0 + j >= row_lo[r + 1];
 #pragma unroll
                 for (int d = 0; d < C::kMTiles; ++d) {
-                  const uint32_t x = *reinterpret_cast<const uint32_t*>(vt + (slot * C::kVPieces + d / 4) * 512 + from * 16 +
-                                                                        (d & 3) * 4);
-                  constexpr uint32_t ones = kBf16 ? 0x7f80u : 0x7c00u;
 #pragma unroll
                   for (int half = 0; half < 2; ++half) {
-                    const uint32_t bits = half ? x >> 16 : x & 0xffffu;
+                    const uint32_t bits =
+                        *reinterpret_cast<const uint16_t*>(vt + v_unit<DP>(j, 2 * d + half) + g * 2);
                     if ((bits & ones) != ones) continue;
                     float v;
                     if constexpr (kBf16) v = __uint_as_float(bits << 16);
@@ -741,8 +798,14 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
         const float back = C::kEight ? __frcp_rn(inv[n][h]) : 1.f;
 #pragma unroll
         for (int d = 0; d < C::kMTiles; ++d) {
-          const int at = d / (C::kVElems / 2) * (8 * C::kVElems) + g * C::kVElems + 2 * (d % (C::kVElems / 2));
-          *reinterpret_cast<float2*>(red + r * C::kOStride + at) = make_float2(o[d][n][h] * back, o[d][n][h + 2] * back);
+          if constexpr (C::kEight) {   // tile d of a lane: two neighbouring dimensions
+            constexpr int kPer = C::kVBytes / 2;
+            const int at = d / kPer * (8 * C::kVBytes) + g * C::kVBytes + 2 * (d % kPer);
+            *reinterpret_cast<float2*>(red + r * C::kOStride + at) = make_float2(o[d][n][h] * back, o[d][n][h + 2] * back);
+          } else {
+            red[r * C::kOStride + d * 16 + g] = o[d][n][h];
+            red[r * C::kOStride + d * 16 + 8 + g] = o[d][n][h + 2];
+          }
         }
       }
     }
@@ -801,22 +864,54 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
       __syncthreads();
       if (last_flag) {
         __threadfence();
+        // the blocks' maxima and sums first (the ring is free), then their sums of values with eight loads in flight
+        const int n_blocks = (int)(c_last - c_first) + 1;
+        float2* ml = reinterpret_cast<float2*>(smem);
+        auto part = [&](int i) { return a.partial + ((c_first + i) * 2 + (i == 0 ? 1 : 0)) * partial_floats(DP); };
+        for (int i = threadIdx.x; i < n_blocks * C::kRows; i += kAttendThreads)
+          ml[i] = __ldcg(reinterpret_cast<const float2*>(part(i / C::kRows) + C::kRows * DP) + i % C::kRows);
+        __syncthreads();
+        for (int r = warp; r < live_rows; r += kAttendWarps) {
+          float top = -INFINITY, sum = 0.f;
+          for (int i = lane; i < n_blocks; i += 32) top = fmaxf(top, ml[i * C::kRows + r].x);
+#pragma unroll
+          for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+          const float base = top == -INFINITY ? 0.f : top;
+          for (int i = lane; i < n_blocks; i += 32) {
+            const float2 y = ml[i * C::kRows + r];
+            const float f = exp2_fast(y.x - base);
+            sum += f * y.y;
+            ml[i * C::kRows + r].x = f;
+          }
+#pragma unroll
+          for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+          if (lane == 0) {
+            stat_m[0][r] = top;
+            stat_l[0][r] = sum;
+          }
+        }
+        __syncthreads();
         for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
           const int r = i / kQuads, quad = i % kQuads;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          float sum = 0.f, top = -INFINITY;
-          for (int64_t c = c_first; c <= c_last; ++c) {
-            const float* part = a.partial + (c * 2 + (c == c_first ? 1 : 0)) * partial_floats(DP);
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + C::kRows * DP + r * 2));
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(part + r * DP + quad * 4));
-            const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
-            const float fo = exp2_fast(top - base), fn = exp2_fast(ml.x - base);
-            acc.x = acc.x * fo + x.x * fn, acc.y = acc.y * fo + x.y * fn;
-            acc.z = acc.z * fo + x.z * fn, acc.w = acc.w * fo + x.w * fn;
-            sum = sum * fo + ml.y * fn;
-            top = now;
+          int c = 0;
+          for (; c + 8 <= n_blocks; c += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __ldcg(reinterpret_cast<const float4*>(part(c + e) + r * DP + quad * 4));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float f = ml[(c + e) * C::kRows + r].x;
+              acc.x += f * x[e].x, acc.y += f * x[e].y, acc.z += f * x[e].z, acc.w += f * x[e].w;
+            }
           }
-          write_row(r, quad, acc, sum, top);
+#pragma unroll 4
+          for (; c < n_blocks; ++c) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(part(c) + r * DP + quad * 4));
+            const float f = ml[c * C::kRows + r].x;
+            acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
+          }
+          write_row(r, quad, acc, stat_l[0][r], stat_m[0][r]);
         }
       }
     }
@@ -828,6 +923,7 @@ template <int FMT, int DP, int NT>
 cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
   using C = AttendConfig<FMT, DP, NT>;
   static_assert(C::kSmem <= 227 * 1024, "shared memory");
+
   auto* kernel = attend_kernel<FMT, DP, NT>;
   static std::atomic<int> resident[kMaxDevices];   // blocks an SM holds, by device; 0: not asked yet
   int per_sm = a.device < kMaxDevices ? resident[a.device].load(std::memory_order_relaxed) : 0;
@@ -843,6 +939,8 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
   const int64_t units = ((int64_t)a.max_len + 15) / C::kUnit + 1;
   const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units / kMinUnits + 1;
   a.parts = most < (double)per_sm * num_sms ? (int)most : per_sm * num_sms;
+  const int joinable = C::kBody / (C::kRows * 8);   // a join holds every block's maxima and sums in the ring
+  if (a.parts > joinable) a.parts = joinable;
   kernel<<<a.parts, kAttendThreads, C::kSmem, st>>>(a);
   return cudaGetLastError();
 }
