@@ -34,6 +34,13 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   a.max_len = (int)std::min<int64_t>((int64_t)table->width * c.page_size, lc::kMaxPositions);
   a.device = c.device;
   a.pages = c.pages;
+  a.page_rows = (int64_t)c.kv_heads * c.page_size;
+  a.page_bytes = a.page_rows * c.head_dim * (lc::is_quantised(c.format) ? 1 : 2);
+  // n / d = n * ceil(2^(26 + s) / d) >> (26 + s) for n < 2^26 and d <= 2^s
+  const uint32_t d = (uint32_t)c.page_size / 16;
+  a.page_shift = 26;
+  while ((1u << (a.page_shift - 26)) < d) ++a.page_shift;
+  a.page_mul = (uint32_t)((((uint64_t)1 << a.page_shift) + d - 1) / d);
   a.scale = at->scale;
   a.lengths = at->lengths_dev;
   a.starts = at->starts_dev;
@@ -46,10 +53,12 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   a.arrived = h->arrived;
   a.status = h->dev_status;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
+  cudaError_t e;
   switch (c.format) {
-    case LACACHE_KV_BF16: return lc::from_cuda(lc::launch_attend_bf16(a, h->num_sms, st));
-    case LACACHE_KV_F16: return lc::from_cuda(lc::launch_attend_f16(a, h->num_sms, st));
-    case LACACHE_KV_E4M3: return lc::from_cuda(lc::launch_attend_e4m3(a, h->num_sms, st));
-    default: return lc::from_cuda(lc::launch_attend_int8(a, h->num_sms, st));
+    case LACACHE_KV_BF16: e = lc::launch_attend_bf16(a, h->num_sms, st); break;
+    case LACACHE_KV_F16: e = lc::launch_attend_f16(a, h->num_sms, st); break;
+    case LACACHE_KV_E4M3: e = lc::launch_attend_e4m3(a, h->num_sms, st); break;
+    default: e = lc::launch_attend_int8(a, h->num_sms, st); break;
   }
+  return e == cudaErrorNotSupported ? LACACHE_ERR_UNSUPPORTED : lc::from_cuda(e);
 }

@@ -11,12 +11,15 @@
 // a tile of 8 rows wastes nothing at 8 rows, where the 64- or 128-row tiles of tcgen05 would take the scores through TMEM
 // and shared memory for no gain in a kernel that waits for HBM.
 //   S^T [16 keys x 8 rows] = K [16 x d] Q^T [d x 8],   O^T [16 dims x 8 rows] += V^T [16 dims x 16 keys] P^T [16 keys x 8]
-// The order of a contraction is free, and so is the naming of V's dimensions, so each lane takes 16 contiguous bytes of a
-// row of K or V as its share of several instructions' A operand: lane (g, t) = (lane / 4, lane % 4) owns bytes 16 t of every
-// 64 of key rows g and g + 8 of K, and (8-bit formats) of V bytes 16 g of every 128 of the rows of keys 2t, 2t+1, 2t+8 and 2t+9. Those
-// copies to shared memory (cp.async) are a deep register file with an asynchronous front: each lane reads back what it copied
-// itself. A 16-bit V goes through shared memory in swizzled rows and comes back transposed (ldmatrix); 8-bit codes are
-// widened first and paired by byte permutes. Nothing is shared between warps: no barriers in the loop. P^T is the transpose of the S^T accumulator, one movmatrix for 8 x 8.
+// The order of a contraction is free, and so is the naming of V's dimensions, so an operand's share of a lane is 16
+// contiguous bytes of a row wherever it can be: lane (g, t) = (lane / 4, lane % 4) takes bytes 16 t of every 64 of key rows g
+// and g + 8 of K, and (8-bit formats) bytes 16 g of every 128 of rows 2t, 2t+1, 2t+8 and 2t+9 of V, whose codes are paired
+// by byte permutes and widened; a 16-bit V is transposed by ldmatrix. P^T is the transpose of the S^T accumulator, one
+// movmatrix for 8 x 8.
+//
+// Copies. Each warp has a ring of its own tiles in shared memory, filled by cp.async whole lines at a time (rows of V taken
+// 32 bytes at a time, straight into the lane that uses them, halved the bandwidth of 8-bit caches), and runs it ahead of the
+// products from one triple into the next. Nothing is shared between warps: no barriers in the loop.
 //
 // Softmax. Base 2, running maximum m a row, moved only when a score exceeds it by more than 8: weights then stay below 2^8,
 // the sum is fp32, and most tiles need a vote instead of a maximum over the lanes. Weights: f16 for f16 and 8-bit caches (11
@@ -51,6 +54,10 @@ struct AttendArgs {
   int max_len;          // positions the table can name
   int device;
   int64_t pages;
+  int64_t page_rows;    // rows of a page: kv_heads x page_size ...
+  int64_t page_bytes;   // ... and their bytes
+  uint32_t page_mul;    // tile / (page_size / 16) = tile * page_mul >> page_shift, for tiles below 2^26
+  int page_shift;
   float scale;
   const int32_t* lengths;
   const int32_t* starts;
@@ -67,7 +74,6 @@ struct AttendArgs {
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
-constexpr int kMinUnits = 1;                 // a block's least part
 constexpr int kMaxRowTile = 32;
 constexpr int kMaxPositions = 1 << 30;      // a table's reach is cut to this
 constexpr int kMaxDevices = 64;
@@ -95,18 +101,18 @@ struct AttendConfig {
   static constexpr int kKPieces = DP * kItem / 64;                       // 16-byte pieces of a lane in a row of K
   static constexpr int kVBytes = DP * kItem >= 128 ? 16 : 8;             // bytes of a piece of V
   static constexpr int kVPieces = DP * kItem / (8 * kVBytes);
-  static constexpr int kUnits = DP / 8 < 32 ? DP / 8 : 32;               // 16-bit V: 16-byte units of a row
-  static constexpr int kUnitRows = 32 / kUnits;                          // ... and rows that one copy of the warp covers
+  static constexpr int kRowBytes = DP * kItem;
+  static constexpr int kUnits = kRowBytes / 16;                          // 16-byte units of a row
+  static constexpr int kCopyRows = 32 / kUnits;                          // rows that one copy of the warp covers
+  static constexpr int kCopies = 16 / kCopyRows;
   static constexpr int kTileBytes = 16 * DP * kItem;                     // K (or V) of 16 keys
   static constexpr int kStageBytes = kSub * 2 * kTileBytes + (kEight ? kKeys * 8 : 0);
-  static constexpr int kStages = DP == 256 && !kEight ? 3 : kStageBytes <= 4096 + 256 ? 6 : kStageBytes <= 8192 + 256 ? 3 : 3;
+  static constexpr int kStages = kStageBytes > 16000 ? (NT == 1 ? 3 : 2) : kStageBytes > 8000 ? 2 : 4;
   static constexpr int kMTiles = DP / 16;
   static constexpr int kQStride = DP * 2 + 64;                           // bytes of a row of q in shared memory
   static constexpr int kRing = kAttendWarps * kStages * kStageBytes;
   static constexpr int kOStride = DP + 4;                                // floats of a row of sums in the join
-  static constexpr int kJoin = kAttendWarps * kRows * kOStride * 4;
-  static constexpr int kBody = kRing > kJoin ? kRing : kJoin;            // the join reuses the ring
-  static constexpr int kSmem = kBody + kRows * kQStride;
+  static constexpr int kSmem = kRing + kRows * kQStride + kRows * kOStride * 4;
 };
 
 __device__ __forceinline__ uint32_t shared_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -124,17 +130,30 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// c (+)= A B; the first product of a sum takes zeros instead of c.
 template <bool BF16>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
   if constexpr (BF16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <bool BF16>
+__device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                               uint32_t b0, uint32_t b1) {
+  if constexpr (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // 8 x 8 of 16-bit values, one row of four lanes' registers, transposed across the warp.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -144,7 +163,7 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -152,14 +171,19 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t& a0, uint32_t& a1, uint32_t& a2, uint32_t& a3) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(a0), "=r"(a1), "=r"(a2), "=r"(a3)
-               : "r"(addr)
-               : "memory");
+               : "r"(addr));
 }
-// Where a 16-bit row of V (key j of its tile) keeps its 16-byte unit u: eight keys' units of one column lie in different
-// banks.
-template <int DP>
+// Where a tile of 16 keys keeps the 16-byte unit u of key j, so that what eight lanes read at once lies in eight different
+// bank groups: K, read as units 4c + t of keys g (lanes 4 (g & 1) + t together); a 16-bit V, read by ldmatrix as one unit of
+// eight keys; an 8-bit V, read as units g of keys 2t. Rows of 64 bytes share a 128-byte line in pairs.
+template <int ROW>
+__device__ __forceinline__ int k_unit(int j, int u) {
+  return ROW == 64 ? j * 64 + u * 16 : j * ROW + ((u ^ ((j & 1) << 2)) << 4);
+}
+template <int ROW, bool EIGHT>
 __device__ __forceinline__ int v_unit(int j, int u) {
-  return j * (DP * 2) + ((u ^ (j & 7)) * 16);
+  if (!EIGHT) return j * ROW + ((u ^ (j & 7)) << 4);
+  return ROW == 64 ? (j >> 1) * 128 + ((((j & 1) * 4 + u) ^ (j & 6)) << 4) : j * ROW + ((u ^ (j & 6)) << 4);
 }
 
 // Four codes as f16 pairs: elements 0, 1 and 2, 3. Exact.
@@ -212,10 +236,20 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_k
   return s;
 }
 
-__device__ __forceinline__ int64_t warp_sum64(int64_t x) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
+// Four dimensions of an output row (row `row` of its kv head), and with the first of them the row's lse.
+__device__ __forceinline__ void write_row(const AttendArgs& a, int seq, int head, int row, int quad, float4 acc, float sum,
+                                          float top) {
+  const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
+  const int64_t token = (int64_t)seq * a.new_tokens + tok;
+  const float f = sum == 0.f ? 0.f : 1.f / sum;   // nothing seen: zeros
+  const float4 y = sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+  if (quad * 4 < a.head_dim) {
+    uint2 w;
+    if (a.q_f16) w = make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w));
+    else w = make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
+    *reinterpret_cast<uint2*>(a.out.p + token * a.out.token + qh * a.out.head + quad * 8) = w;
+  }
+  if (quad == 0 && a.lse) a.lse[token * a.q_heads + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <int FMT, int DP, int NT>
@@ -228,29 +262,32 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
   __shared__ int row_pos[C::kRows], row_lo[C::kRows];   // a row's own last and first visible position
   __shared__ float row_factor[C::kRows];                // scale log2(e), and what the row's q was divided by
   __shared__ int page_ids[kAttendWarps][C::kStages][C::kSub];
-  __shared__ unsigned int last_flag;
+  __shared__ int pending[2][4];   // shared triples: sequence, triple, first and last block (-1: none)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int D = a.head_dim;
-  const int64_t per_seq = (int64_t)a.kv_heads * a.row_tiles;
+  const int D = a.head_dim, row_bytes = D * C::kItem;
+  const int per_seq = a.kv_heads * a.row_tiles;   // triples of a sequence
 
-  // ---- this block's part of the line of units (each warp for itself) ----
-  int64_t total = 0;
-  for (int s = lane; s < a.table.seqs; s += 32) total += span_of(a, s, C::kUnit).units;
-  total = warp_sum64(total) * per_seq;
-  int64_t parts = (total + kMinUnits - 1) / kMinUnits;
-  if (parts > a.parts) parts = a.parts;
-  const int64_t block = blockIdx.x;
+  // ---- this block's part of the line of units (each warp for itself): units [start(block), start(block + 1)) ----
+  const int first_units = lane < a.table.seqs ? span_of(a, lane, C::kUnit).units : 0;   // of the first 32 sequences
+  int total = first_units;
+  for (int s = lane + 32; s < a.table.seqs; s += 32) total += span_of(a, s, C::kUnit).units;
+  total = __reduce_add_sync(0xffffffffu, total) * per_seq;
+  const int parts = total < a.parts ? total : a.parts, block = blockIdx.x;
   if (block >= parts) return;
-  int64_t u = total * block / parts;
-  const int64_t u_end = total * (block + 1) / parts;
-  int seq = 0;
-  int64_t seq_base = 0;   // units before sequence seq
+  const int share = total / parts, longer = total - share * parts;   // the first `longer` blocks have one unit more
+  const int u = block * share + (block < longer ? block : longer);
+  auto block_of = [&](int unit) {
+    const int in_longer = longer * (share + 1);
+    return unit < in_longer ? unit / (share + 1) : longer + (unit - in_longer) / share;
+  };
+  int seq = 0, seq_base = 0;   // the sequence that unit u belongs to, and the units before it
   for (int s0 = 0; s0 < a.table.seqs; s0 += 32) {
-    const int64_t own = s0 + lane < a.table.seqs ? span_of(a, s0 + lane, C::kUnit).units * per_seq : 0;
-    int64_t upto = own;
+    const int own =
+        (s0 == 0 ? first_units : s0 + lane < a.table.seqs ? span_of(a, s0 + lane, C::kUnit).units : 0) * per_seq;
+    int upto = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += y;
     }
     const unsigned past = __ballot_sync(0xffffffffu, seq_base + upto > u);
@@ -262,186 +299,206 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
     }
     seq_base += __shfl_sync(0xffffffffu, upto, 31);
   }
+  if (threadIdx.x < 2) pending[threadIdx.x][2] = -1;   // (the first triple's q, and a barrier, come before its use)
+  constexpr int kQuads = DP / 4;
+  Span sp = span_of(a, seq, C::kUnit);
+  int triple = (u - seq_base) / sp.units, first_unit = u - seq_base - triple * sp.units;
+  int left = share + (block < longer ? 1 : 0);   // units of this block that are not done
 
   unsigned char* ring = smem + warp * C::kStages * C::kStageBytes;
-  unsigned char* q_smem = smem + C::kBody;
+  unsigned char* q_smem = smem + C::kRing;
+  float* join = reinterpret_cast<float*>(smem + C::kRing + C::kRows * C::kQStride);
   const uint32_t ring_addr = shared_addr(ring);
 
-  while (u < u_end) {
-    // ---- the triple that unit u belongs to ----
-    Span sp = span_of(a, seq, C::kUnit);
-    while (seq + 1 < a.table.seqs && u >= seq_base + sp.units * per_seq) {
-      seq_base += sp.units * per_seq;
-      sp = span_of(a, ++seq, C::kUnit);
+  // ---- the copies run ahead of the products by kStages - 1 units, from one triple into the next ----
+  struct {
+    int left, seq, triple, unit, slot;
+    Span sp;
+    int key;                      // this warp's first key of the unit
+    const int32_t* table_row;
+    const unsigned char *k, *v;   // head's part of page 0
+    int64_t scale_row;
+    int ids[C::kSub], next_ids[C::kSub];   // lane i: page ids of the batch's unit i, and of the next batch's
+    int in_batch;
+  } ahead;
+  auto page_of = [&](int at) { return (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift); };
+  auto look_up = [&](int from, int (&ids)[C::kSub]) {   // the page ids of 32 units, from the one whose first key is `from`
+#pragma unroll
+    for (int s = 0; s < C::kSub; ++s) {
+      const int64_t at = (int64_t)from + lane * C::kUnit + 16 * s;
+      ids[s] = at < ahead.sp.hi ? __ldg(ahead.table_row + page_of((int)at)) : -1;
     }
-    const int64_t in_seq = u - seq_base;
-    const int triple = (int)(in_seq / sp.units), first_unit = (int)(in_seq % sp.units);
+  };
+  auto enter_triple = [&] {
+    const int head = ahead.triple / a.row_tiles;
+    ahead.key = (ahead.sp.lo & ~15) + ahead.unit * C::kUnit + warp * C::kKeys;
+    ahead.table_row = a.table.pages + ahead.seq * a.table.stride;
+    const int64_t rows = (int64_t)head * a.page_size;
+    ahead.k = a.pk + rows * row_bytes;
+    ahead.v = a.pv + rows * row_bytes;
+    ahead.scale_row = rows;
+    ahead.in_batch = 0;
+    look_up(ahead.key, ahead.ids);
+  };
+  auto issue = [&] {
+    if (ahead.left > 0) {
+      const uint32_t at = ring_addr + ahead.slot * C::kStageBytes;
+#pragma unroll
+      for (int s = 0; s < C::kSub; ++s) {
+        const int k0 = ahead.key + 16 * s;
+        int page = __shfl_sync(0xffffffffu, ahead.ids[s], ahead.in_batch);
+        const int at_page = k0 - page_of(k0) * a.page_size;
+        if ((unsigned)page >= (unsigned)a.pages) {
+          if (k0 < ahead.sp.hi && lane == 0) atomicOr(a.status, kBadIndex);
+          page = -1;
+        }
+        if (lane == 0) page_ids[warp][ahead.slot][s] = page;
+        const int64_t offset = (page < 0 ? 0 : (int64_t)page * a.page_bytes) + (int64_t)at_page * row_bytes;
+        const unsigned char* kp = ahead.k + offset;
+        const unsigned char* vp = ahead.v + offset;
+        // a key outside [lo, hi) is not read: zeros take its place
+        auto inside = [&](int j) { return page >= 0 && k0 + j >= ahead.sp.lo && k0 + j < ahead.sp.hi; };
+        // 32 units of 16 bytes a copy, neighbouring lanes on neighbouring units: rows are requested in whole lines
+        const uint32_t kd = at + s * 2 * C::kTileBytes, vd = kd + C::kTileBytes;
+        const int unit = lane % C::kUnits, first = lane / C::kUnits;
+        if (D == DP && page >= 0 && k0 >= ahead.sp.lo && k0 + 16 <= ahead.sp.hi) {   // nothing to leave out: most tiles
+#pragma unroll
+          for (int i = 0; i < C::kCopies; ++i) {
+            const int j = i * C::kCopyRows + first;
+            copy_async<16>(kd + k_unit<C::kRowBytes>(j, unit), kp + i * 512 + lane * 16, true);
+            copy_async<16>(vd + v_unit<C::kRowBytes, C::kEight>(j, unit), vp + i * 512 + lane * 16, true);
+          }
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < C::kCopies; ++i) {
+            const int j = i * C::kCopyRows + first;
+            const bool live = inside(j) && unit * 16 < row_bytes;
+            const int from = j * row_bytes + unit * 16;
+            copy_async<16>(kd + k_unit<C::kRowBytes>(j, unit), live ? kp + from : a.pk, live);
+            copy_async<16>(vd + v_unit<C::kRowBytes, C::kEight>(j, unit), live ? vp + from : a.pv, live);
+          }
+        }
+        if constexpr (C::kEight) {
+          // scales, four keys a lane: lanes 8s to 8s + 3 those of k, 8s + 4 to 8s + 7 those of v
+          if (lane >> 3 == s) {
+            const float* src = (lane & 4 ? a.vs : a.ks);
+            copy_async<16>(at + C::kSub * 2 * C::kTileBytes + lane * 16,
+                           page >= 0 ? src + (page * a.page_rows + ahead.scale_row + at_page + (lane & 3) * 4) : src, page >= 0);
+          }
+        }
+      }
+      --ahead.left;
+      ahead.slot = ahead.slot + 1 == C::kStages ? 0 : ahead.slot + 1;
+      ahead.key += C::kUnit;
+      if (++ahead.in_batch == 16) look_up(ahead.key + 16 * C::kUnit, ahead.next_ids);
+      if (ahead.in_batch == 32) {
+        ahead.in_batch = 0;
+#pragma unroll
+        for (int s = 0; s < C::kSub; ++s) ahead.ids[s] = ahead.next_ids[s];
+      }
+      if (++ahead.unit == ahead.sp.units && ahead.left > 0) {
+        ahead.unit = 0;
+        if (++ahead.triple == per_seq) {
+          ahead.triple = 0;
+          ahead.seq = ahead.seq + 1 < a.table.seqs ? ahead.seq + 1 : ahead.seq;
+          ahead.sp = span_of(a, ahead.seq, C::kUnit);
+        }
+        enter_triple();
+      }
+    }
+    copy_commit();
+  };
+
+  // a row of q (row r of the tile that starts at row0), eight elements a lane; zeros past the live rows and dimensions
+  auto load_q = [&](int of_seq, int of_head, int of_row0, int r) {
+    const int row = of_row0 + r, tok = row / a.group;
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (row < a.rows && lane * 8 < D)
+      x = *reinterpret_cast<const uint4*>(a.q.p + ((int64_t)of_seq * a.new_tokens + tok) * a.q.token +
+                                          (int64_t)(of_head * a.group + row - tok * a.group) * a.q.head + lane * 16);
+    return x;
+  };
+  constexpr bool kQEarly = NT <= 2;   // the next triple's q is read before the join; more rows would spill
+  uint4 q_raw[kQEarly ? C::kRows / kAttendWarps : 1];
+  auto load_q_early = [&](int of_seq, int of_triple) {
+    if constexpr (kQEarly) {
+      const int of_head = of_triple / a.row_tiles;
+#pragma unroll
+      for (int k = 0; k < C::kRows / kAttendWarps; ++k)
+        q_raw[k] = load_q(of_seq, of_head, (of_triple - of_head * a.row_tiles) * C::kRows, warp + k * kAttendWarps);
+    }
+  };
+  float factor[NT][2];
+  uint4 qreg[kQInRegs ? NT * C::kKPieces * (C::kEight ? 2 : 1) : 1];
+  int all_hi = 0, all_lo = 0;   // positions that every live row sees: [all_lo, all_hi]
+  const bool rows_differ = a.new_tokens > 1;
+  bool fresh = true, redo = false;   // the copies start here; the triple's products are done again
+  bool split = kBf16;                // bf16 weights in two terms
+  int slot = 0;                      // of the unit whose products are next
+  while (left > 0) {
     const int head = triple / a.row_tiles, tile = triple % a.row_tiles;
-    const int64_t begin = u - first_unit;                         // the triple's units: [begin, begin + sp.units)
-    const int64_t left = u_end - u;
     const int units = sp.units - first_unit < left ? sp.units - first_unit : (int)left;
     const int row0 = tile * C::kRows;
     const int live_rows = a.rows - row0 < C::kRows ? a.rows - row0 : C::kRows;
-    if (threadIdx.x == 0) {
-      const int raw = a.lengths[seq];
-      if (raw < 0 || raw > a.max_len) atomicOr(a.status, kBadIndex);
+    if (fresh) {
+      if (!redo) load_q_early(seq, triple);   // before the copies, which would keep it waiting
+      copy_wait<0>();
+      __syncwarp();
+      ahead.left = left;
+      ahead.seq = seq;
+      ahead.triple = triple;
+      ahead.unit = first_unit;
+      ahead.slot = slot = 0;
+      ahead.sp = sp;
+      enter_triple();
     }
 
-    __syncthreads();   // the previous triple's readers are done
-
-    // ---- this warp's keys: KT from each unit ----
-    const int key0 = (sp.lo & ~15) + first_unit * C::kUnit + warp * C::kKeys;
-      const int32_t* table_row = a.table.pages + seq * a.table.stride;
-
-    // page ids of the stage that is issued next, read one stage ahead of their use
-    int next_page[C::kSub], next_slot[C::kSub];
-    auto look_up = [&](int i) {
-      const int key = key0 + i * C::kUnit;
-#pragma unroll
-      for (int s = 0; s < C::kSub; ++s) {
-        const int at = key + 16 * s;
-        next_page[s] = -1;
-        next_slot[s] = 0;
-        if (i < units && at < sp.hi) {
-          const int index = at / a.page_size;
-          next_slot[s] = at - index * a.page_size;
-          next_page[s] = __ldg(table_row + index);
-        }
-      }
-    };
-    auto issue = [&](int i) {
-      if (i < units) {
-        const int stage = i % C::kStages;
-        const uint32_t at = ring_addr + stage * C::kStageBytes;
-        const int key = key0 + i * C::kUnit;
-#pragma unroll
-        for (int s = 0; s < C::kSub; ++s) {
-          const int k0 = key + 16 * s;
-          int page = next_page[s];
-          if (page < 0 || page >= a.pages) {
-            if (k0 < sp.hi && lane == 0) atomicOr(a.status, kBadIndex);
-            page = -1;
-          }
-          if (lane == 0) page_ids[warp][stage][s] = page;
-          const int64_t row = ((int64_t)(page < 0 ? 0 : page) * a.kv_heads + head) * a.page_size + next_slot[s];
-          const unsigned char* kp = a.pk + row * (int64_t)(D * C::kItem);
-          const unsigned char* vp = a.pv + row * (int64_t)(D * C::kItem);
-          // a key outside [lo, hi) is not read: zeros take its place
-          auto inside = [&](int j) { return page >= 0 && k0 + j >= sp.lo && k0 + j < sp.hi; };
-          const uint32_t kd = at + s * 2 * C::kTileBytes, vd = kd + C::kTileBytes;
-          const int row_bytes = D * C::kItem;
-          const unsigned char* ksrc = kp + (int64_t)(g * row_bytes + t * 16);
-          if (D == DP && page >= 0 && k0 >= sp.lo && k0 + 16 <= sp.hi) {   // nothing to leave out: most tiles
-#pragma unroll
-            for (int c = 0; c < C::kKPieces; ++c) {
-              copy_async<16>(kd + c * 512 + lane * 16, ksrc + c * 64, true);
-              copy_async<16>(kd + (C::kKPieces + c) * 512 + lane * 16, ksrc + 8 * DP * C::kItem + c * 64, true);
-            }
-            if constexpr (C::kEight) {
-              const unsigned char* vsrc = vp + 2 * t * DP + g * C::kVBytes;
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-#pragma unroll
-                for (int c = 0; c < C::kVPieces; ++c)
-                  copy_async<C::kVBytes>(vd + (r * C::kVPieces + c) * (32 * C::kVBytes) + lane * C::kVBytes,
-                                         vsrc + ((r & 1) + 8 * (r >> 1)) * DP + c * 8 * C::kVBytes, true);
-              }
-            } else {
-              const unsigned char* vsrc = vp + (lane / C::kUnits) * (DP * 2) + (lane % C::kUnits) * 16;
-#pragma unroll
-              for (int i = 0; i < C::kUnits / 2; ++i)
-                copy_async<16>(vd + v_unit<DP>(i * C::kUnitRows + lane / C::kUnits, lane % C::kUnits), vsrc + i * 512, true);
-            }
-          } else {
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-              const bool in = inside(g + 8 * r);
-#pragma unroll
-              for (int c = 0; c < C::kKPieces; ++c) {
-                const bool live = in && (c * 64 + t * 16) < row_bytes;
-                copy_async<16>(kd + (r * C::kKPieces + c) * 512 + lane * 16, live ? ksrc + 8 * r * row_bytes + c * 64 : a.pk,
-                               live);
-              }
-            }
-            if constexpr (C::kEight) {
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int j = 2 * t + (r & 1) + 8 * (r >> 1);
-                const bool in = inside(j);
-#pragma unroll
-                for (int c = 0; c < C::kVPieces; ++c) {
-                  const int d = c * 8 * C::kVBytes + g * C::kVBytes;
-                  const bool live = in && d < row_bytes;
-                  copy_async<C::kVBytes>(vd + (r * C::kVPieces + c) * (32 * C::kVBytes) + lane * C::kVBytes,
-                                         live ? vp + j * row_bytes + d : a.pv, live);
-                }
-              }
-            } else {
-#pragma unroll
-              for (int i = 0; i < C::kUnits / 2; ++i) {
-                const int j = i * C::kUnitRows + lane / C::kUnits, unit = lane % C::kUnits;
-                const bool live = inside(j) && unit * 16 < row_bytes;
-                copy_async<16>(vd + v_unit<DP>(j, unit), live ? vp + j * row_bytes + unit * 16 : a.pv, live);
-              }
-            }
-          }
-          if constexpr (C::kEight) {
-            // scales: lanes 0-15 those of k, 16-31 those of v
-            const int j = lane & 15;
-            const bool in = inside(j);
-            const float* src = (lane < 16 ? a.ks : a.vs) + (in ? row + j : 0);
-            copy_async<4>(at + C::kSub * 2 * C::kTileBytes + (s * 32 + lane) * 4, src, in);
-          }
-        }
-        look_up(i + 1);
-      }
-      copy_commit();
-    };
-
-    int all_hi, all_lo;   // positions that every live row sees: [all_lo, all_hi]
-    const bool rows_differ = a.new_tokens > 1;
-    float factor[NT][2];
-    uint4 qreg[kQInRegs ? NT * C::kKPieces * (C::kEight ? 2 : 1) : 1];
     float o[C::kMTiles][NT][4];
     float m[NT][2], l[NT][2], inv[NT][2];
-    bool split = kBf16, again = false;   // bf16 weights in two terms
-    do {
-      look_up(0);
-#pragma unroll 1
-      for (int i = 0; i < C::kStages - 1; ++i) issue(i);
-      if (!again) {
-    // ---- q into shared memory, in the order of the K pieces, while the first keys are on their way ----
-    for (int r = warp; r < C::kRows; r += kAttendWarps) {
-      const int row = row0 + r;
-      const bool live = r < live_rows;
-      const int tok = live ? row / a.group : 0, qh = head * a.group + (live ? row % a.group : 0);
-      const unsigned char* src = a.q.p + ((int64_t)seq * a.new_tokens + tok) * a.q.token + qh * a.q.head;
-      float x[8] = {};
-      const int d0 = lane * 8;
-      const bool has = live && d0 < D;
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (has) {
-        raw = *reinterpret_cast<const uint4*>(src + d0 * 2);
-        widen8(raw, x, __nv_bfloat16());   // used for bf16 rows alone
-      }
-      float back = 1.f;
-      if (C::kEight && !a.q_f16) {
-        float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        // the power of two below top: its exponent bits alone, at most 2^126 (1 for zeros, infinities and subnormals)
-        uint32_t e = __float_as_uint(top) & 0x7f800000u;
-        if (e != 0 && e != 0x7f800000u) {
-          e = e < 0x7e800000u ? e : 0x7e800000u;
-          back = __uint_as_float(e);
-          const float down = __uint_as_float(0x7f000000u - e);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= down;
+      for (int i = 0; i < C::kMTiles; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+      inv[n][0] = inv[n][1] = C::kEight ? 0x1p126f : 1.f;
+    }
+
+    int key = (sp.lo & ~15) + first_unit * C::kUnit + warp * C::kKeys;
+    for (int i = fresh ? 1 - C::kStages : 0; i < units; ++i) {
+      issue();
+      if (i < 0) continue;   // the copies' head start
+      if (i == 0 && !redo) {
+        // ---- q into shared memory, in the order of the K pieces ----
+        if (threadIdx.x == 0) {
+          const int raw = a.lengths[seq];
+          if (raw < 0 || raw > a.max_len) atomicOr(a.status, kBadIndex);
         }
-        raw = pack8(x, __half());
-      }
+#pragma unroll
+        for (int k = 0; k < C::kRows / kAttendWarps; ++k) {
+          const int r = warp + k * kAttendWarps, row = row0 + r, d0 = lane * 8;
+          const bool live = r < live_rows;
+          const int tok = live ? row / a.group : 0;
+          uint4 raw = kQEarly ? q_raw[k] : load_q(seq, head, row0, r);
+          float back = 1.f;
+          if (C::kEight && !a.q_f16) {
+            float x[8], top = 0.f;
+            widen8(raw, x, __nv_bfloat16());
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+#pragma unroll
+            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            // the power of two below top: its exponent bits alone, at most 2^126 (1 for zeros, infinities and subnormals)
+            uint32_t e = __float_as_uint(top) & 0x7f800000u;
+            if (e != 0 && e != 0x7f800000u) {
+              e = e < 0x7e800000u ? e : 0x7e800000u;
+              back = __uint_as_float(e);
+              const float down = __uint_as_float(0x7f000000u - e);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] *= down;
+            }
+            raw = pack8(x, __half());
+          }
       if (d0 < DP) *reinterpret_cast<uint4*>(q_smem + r * C::kQStride + d0 * 2) = raw;
       if (lane == 0) {
         const int p = live ? sp.len - a.new_tokens + tok : -1;
@@ -477,23 +534,10 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
         }
       }
     }
-
       }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int i = 0; i < C::kMTiles; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
-      m[n][0] = m[n][1] = -INFINITY;
-      l[n][0] = l[n][1] = 0.f;
-      inv[n][0] = inv[n][1] = C::kEight ? 0x1p126f : 1.f;
-    }
-    for (int i = 0; i < units; ++i) {
-      issue(i + C::kStages - 1);
       copy_wait<C::kStages - 1>();
       __syncwarp();
-      const int stage = i % C::kStages;
-      const unsigned char* st = ring + stage * C::kStageBytes;
-      const int key = key0 + i * C::kUnit;
+      const unsigned char* st = ring + slot * C::kStageBytes;
 
       // scores
       float s[C::kSub][NT][4];
@@ -501,11 +545,9 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
       for (int b = 0; b < C::kSub; ++b) {
         const unsigned char* kt = st + b * 2 * C::kTileBytes;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[b][n][0] = s[b][n][1] = s[b][n][2] = s[b][n][3] = 0.f;
-#pragma unroll
         for (int c = 0; c < C::kKPieces; ++c) {
-          const uint4 x = *reinterpret_cast<const uint4*>(kt + c * 512 + lane * 16);
-          const uint4 y = *reinterpret_cast<const uint4*>(kt + (C::kKPieces + c) * 512 + lane * 16);
+          const uint4 x = *reinterpret_cast<const uint4*>(kt + k_unit<C::kRowBytes>(g, 4 * c + t));
+          const uint4 y = *reinterpret_cast<const uint4*>(kt + k_unit<C::kRowBytes>(g + 8, 4 * c + t));
           if constexpr (C::kEight) {
             const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
             uint32_t xa[8], ya[8];
@@ -523,8 +565,13 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
                 const uint4* p = reinterpret_cast<const uint4*>(q_smem + (n * 8 + g) * C::kQStride + (c * 64 + t * 16) * 2);
                 q0 = p[0], q1 = p[1];
               }
-              mma16816<false>(s[b][n], xa[0], ya[0], xa[1], ya[1], q0.x, q0.y);
-              mma16816<false>(s[b][n], xa[2], ya[2], xa[3], ya[3], q0.z, q0.w);
+              if (c == 0) {
+                mma16816_first<false>(s[b][n], xa[0], ya[0], xa[1], ya[1], q0.x, q0.y);
+                mma16816<false>(s[b][n], xa[2], ya[2], xa[3], ya[3], q0.z, q0.w);
+              } else {
+                mma16816<false>(s[b][n], xa[0], ya[0], xa[1], ya[1], q0.x, q0.y);
+                mma16816<false>(s[b][n], xa[2], ya[2], xa[3], ya[3], q0.z, q0.w);
+              }
               mma16816<false>(s[b][n], xa[4], ya[4], xa[5], ya[5], q1.x, q1.y);
               mma16816<false>(s[b][n], xa[6], ya[6], xa[7], ya[7], q1.z, q1.w);
             }
@@ -534,57 +581,78 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
               uint4 q;
               if constexpr (kQInRegs) q = qreg[n * C::kKPieces + c];
               else q = *reinterpret_cast<const uint4*>(q_smem + (n * 8 + g) * C::kQStride + (c * 32 + t * 8) * 2);
-              mma16816<kBf16>(s[b][n], x.x, y.x, x.y, y.y, q.x, q.y);
-              mma16816<kBf16>(s[b][n], x.z, y.z, x.w, y.w, q.z, q.w);
+              if (c == 0) {
+                mma16816_first<kBf16>(s[b][n], x.x, y.x, x.y, y.y, q.x, q.y);
+                mma16816<kBf16>(s[b][n], x.z, y.z, x.w, y.w, q.z, q.w);
+              } else {
+                mma16816<kBf16>(s[b][n], x.x, y.x, x.y, y.y, q.x, q.y);
+                mma16816<kBf16>(s[b][n], x.z, y.z, x.w, y.w, q.z, q.w);
+              }
             }
           }
         }
       }
 
-      // base-2 scores, masks, and whether a maximum has to move
-      float vscale[C::kSub][2];
+      // exponents (base-2 scores less the row's maximum), masks, and whether a maximum has to move
+      float x2[C::kSub][NT][4];
+      float kscale[C::kSub][2], vscale[C::kSub][2];
       bool move = false, some_masked = false;
 #pragma unroll
       for (int b = 0; b < C::kSub; ++b) {
         const int k0 = key + 16 * b;
-        float kscale[2] = {1.f, 1.f};
         if constexpr (C::kEight) {
           const float* sc = reinterpret_cast<const float*>(st + C::kSub * 2 * C::kTileBytes) + b * 32;
-          kscale[0] = sc[g], kscale[1] = sc[g + 8];
+          kscale[b][0] = sc[g], kscale[b][1] = sc[g + 8];
           vscale[b][0] = sc[16 + g], vscale[b][1] = sc[24 + g];
+        } else {
+          kscale[b][0] = kscale[b][1] = 1.f;
         }
-        const bool page_ok = page_ids[warp][stage][b] >= 0;
+        const bool page_ok = page_ids[warp][slot][b] >= 0;
         const bool masked = !page_ok || k0 < all_lo || k0 + 15 > all_hi;
         some_masked |= masked;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[b][n][e] *= factor[n][e & 1] * kscale[e >> 1];
+          for (int e = 0; e < 4; ++e)
+            x2[b][n][e] = fmaf(s[b][n][e], factor[n][e & 1] * kscale[b][e >> 1], -m[n][e & 1]);
           if (masked) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int j = k0 + g + 8 * (e >> 1), r = n * 8 + 2 * t + (e & 1);
-              if (!page_ok || j > row_pos[r] || j < row_lo[r]) s[b][n][e] = -INFINITY;
+              if (!page_ok || j > row_pos[r] || j < row_lo[r]) x2[b][n][e] = -INFINITY;
             }
           }
+          // m = -inf (nothing seen yet) gives +inf here, and NaN goes the long way too
 #pragma unroll
-          for (int e = 0; e < 4; ++e) move |= s[b][n][e] > m[n][e & 1] + 8.f;
+          for (int e = 0; e < 4; ++e) move |= !(x2[b][n][e] <= 8.f);
         }
       }
       if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
+          for (int b = 0; b < C::kSub; ++b) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (x2[b][n][e] != -INFINITY) x2[b][n][e] = s[b][n][e] * (factor[n][e & 1] * kscale[b][e >> 1]);   // the score
+          }
+#pragma unroll
           for (int h = 0; h < 2; ++h) {
             float top = m[n][h];
 #pragma unroll
-            for (int b = 0; b < C::kSub; ++b) top = fmaxf(top, fmaxf(s[b][n][h], s[b][n][h + 2]));
+            for (int b = 0; b < C::kSub; ++b) top = fmaxf(top, fmaxf(x2[b][n][h], x2[b][n][h + 2]));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
             const float f = m[n][h] == -INFINITY ? 0.f : exp2_fast(m[n][h] - top);
             m[n][h] = top;
             l[n][h] *= f;
+            const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int b = 0; b < C::kSub; ++b) {
+              x2[b][n][h] -= base;
+              x2[b][n][h + 2] -= base;
+            }
 #pragma unroll
             for (int d = 0; d < C::kMTiles; ++d) {
               o[d][n][h] *= f;
@@ -594,27 +662,32 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
         }
       }
       // weights; in 8-bit formats times v's scales, brought below 2^8 by the row's factor
-      float big = 0.f;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const float m0 = m[n][0] == -INFINITY ? 0.f : m[n][0], m1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
 #pragma unroll
         for (int b = 0; b < C::kSub; ++b) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool out = s[b][n][e] == -INFINITY;
-            const float p = exp2_fast(s[b][n][e] - ((e & 1) ? m1 : m0));
-            l[n][e & 1] += p;
-            if constexpr (C::kEight) {
-              s[b][n][e] = out ? 0.f : p * vscale[b][e >> 1];   // a masked token's scale may be NaN
-              big = fmaxf(big, s[b][n][e] * inv[n][e & 1]);
-            } else {
-              s[b][n][e] = p;
-            }
+            s[b][n][e] = exp2_fast(x2[b][n][e]);
+            l[n][e & 1] += s[b][n][e];
           }
         }
       }
       if constexpr (C::kEight) {
+        float big = 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int b = 0; b < C::kSub; ++b) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool out = some_masked && x2[b][n][e] == -INFINITY;   // its scale may be NaN
+              x2[b][n][e] = s[b][n][e];
+              s[b][n][e] = out ? 0.f : s[b][n][e] * (vscale[b][e >> 1] * inv[n][e & 1]);
+              big = fmaxf(big, s[b][n][e]);
+            }
+          }
+        }
         if (__any_sync(0xffffffffu, big > 256.f)) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -622,7 +695,8 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
             for (int h = 0; h < 2; ++h) {
               float top = 0.f;
 #pragma unroll
-              for (int b = 0; b < C::kSub; ++b) top = fmaxf(top, fmaxf(s[b][n][h], s[b][n][h + 2]));
+              for (int b = 0; b < C::kSub; ++b)
+                top = fmaxf(top, fmaxf(x2[b][n][h] * vscale[b][0], x2[b][n][h + 2] * vscale[b][1]));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -634,6 +708,11 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
                   o[d][n][h] *= f;
                   o[d][n][h + 2] *= f;
                 }
+              }
+#pragma unroll
+              for (int b = 0; b < C::kSub; ++b) {
+                if (s[b][n][h] != 0.f) s[b][n][h] = x2[b][n][h] * (vscale[b][0] * inv[n][h]);
+                if (s[b][n][h + 2] != 0.f) s[b][n][h + 2] = x2[b][n][h + 2] * (vscale[b][1] * inv[n][h]);
               }
             }
           }
@@ -648,7 +727,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
         for (int n = 0; n < NT; ++n) {
           float w[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = C::kEight ? s[b][n][e] * inv[n][e & 1] : s[b][n][e];
+          for (int e = 0; e < 4; ++e) w[e] = s[b][n][e];
           const uint32_t u0 = pack2<kBf16>(w[0], w[1]), u1 = pack2<kBf16>(w[2], w[3]);
           p0[n] = transpose8(u0);
           p1[n] = transpose8(u1);
@@ -660,20 +739,51 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
           }
         }
         const unsigned char* vt = st + b * 2 * C::kTileBytes + C::kTileBytes;
-        // a value that is not finite at a position that only some rows see: the product would put 0 x it into the others.
-        // It is taken out of the product here and added for the rows that see it.
-        constexpr uint32_t ones = kBf16 ? 0x7f80u : 0x7c00u;
-        bool fix = false;
         if constexpr (!C::kEight) {
           if (some_masked && rows_differ) {
-#pragma unroll
+            // a value that is not finite at a position that only some rows see: the product would put 0 x it into the
+            // others. It is added here for the rows that see it, and taken out of the tile.
+            constexpr uint32_t ones = kBf16 ? 0x7f80u : 0x7c00u;
+            bool fix = false;
+#pragma unroll 1
             for (int i = 0; i < C::kTileBytes / 512; ++i) {
               const uint4 x = *reinterpret_cast<const uint4*>(vt + i * 512 + lane * 16);
               const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
               for (int w = 0; w < 4; ++w) fix |= (xw[w] & ones) == ones || ((xw[w] >> 16) & ones) == ones;
             }
-            fix = __any_sync(0xffffffffu, fix);
+            if (__any_sync(0xffffffffu, fix)) {
+              const int k0 = key + 16 * b;
+#pragma unroll 1
+              for (int j = 0; j < 16; ++j) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                  const float w0 = __shfl_sync(0xffffffffu, j < 8 ? s[b][n][0] : s[b][n][2], (j & 7) * 4 + t);
+                  const float w1 = __shfl_sync(0xffffffffu, j < 8 ? s[b][n][1] : s[b][n][3], (j & 7) * 4 + t);
+                  const int r = n * 8 + 2 * t;
+                  const bool see0 = k0 + j <= row_pos[r] && k0 + j >= row_lo[r];
+                  const bool see1 = k0 + j <= row_pos[r + 1] && k0 + j >= row_lo[r + 1];
+#pragma unroll
+                  for (int d = 0; d < 2 * C::kMTiles; ++d) {
+                    const uint32_t bits = *reinterpret_cast<const uint16_t*>(vt + v_unit<C::kRowBytes, false>(j, d) + g * 2);
+                    if ((bits & ones) != ones) continue;
+                    float v;
+                    if constexpr (kBf16) v = __uint_as_float(bits << 16);
+                    else v = __half2float(__ushort_as_half((unsigned short)bits));
+                    if (see0) o[d >> 1][n][2 * (d & 1)] += w0 * v;
+                    if (see1) o[d >> 1][n][2 * (d & 1) + 1] += w1 * v;
+                  }
+                }
+              }
+              __syncwarp();
+#pragma unroll 1
+              for (int i = 0; i < C::kTileBytes / 64; ++i) {
+                uint16_t* x = reinterpret_cast<uint16_t*>(ring + slot * C::kStageBytes + b * 2 * C::kTileBytes + C::kTileBytes +
+                                                          i * 64) + lane;
+                if ((*x & ones) == ones) *x = 0;
+              }
+              __syncwarp();
+            }
           }
         }
         auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
@@ -691,24 +801,27 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
             uint32_t x[4][4];   // [key][word]
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
+              const int j = 2 * t + (r & 1) + 8 * (r >> 1);
               if constexpr (C::kVBytes == 16) {
-                const uint4 y = *reinterpret_cast<const uint4*>(vt + (r * C::kVPieces + c) * 512 + lane * 16);
+                const uint4 y = *reinterpret_cast<const uint4*>(vt + v_unit<C::kRowBytes, true>(j, 8 * c + g));
                 x[r][0] = y.x, x[r][1] = y.y, x[r][2] = y.z, x[r][3] = y.w;
               } else {
-                const uint2 y = *reinterpret_cast<const uint2*>(vt + (r * C::kVPieces + c) * 256 + lane * 8);
+                const uint2 y = *reinterpret_cast<const uint2*>(vt + v_unit<C::kRowBytes, true>(j, g >> 1) + (g & 1) * 8);
                 x[r][0] = y.x, x[r][1] = y.y;
               }
             }
 #pragma unroll
             for (int w = 0; w < C::kVBytes / 4; ++w) {
-              uint32_t lo[4], hi[4];
+              // codes of keys (2t, 2t+1) and (2t+8, 2t+9) side by side, for dimensions 0, 1 and 2, 3 of the word
+              uint32_t f[4][2];
 #pragma unroll
-              for (int r = 0; r < 4; ++r) widen4<FMT>(x[r][w], lo[r], hi[r]);
+              for (int r = 0; r < 2; ++r) {
+                widen4<FMT>(__byte_perm(x[2 * r][w], x[2 * r + 1][w], 0x5140), f[0][r], f[1][r]);
+                widen4<FMT>(__byte_perm(x[2 * r][w], x[2 * r + 1][w], 0x7362), f[2][r], f[3][r]);
+              }
               const int d = c * (C::kVBytes / 2) + 2 * w;
-              product(d, __byte_perm(lo[0], lo[1], 0x5410), __byte_perm(lo[0], lo[1], 0x7632),
-                      __byte_perm(lo[2], lo[3], 0x5410), __byte_perm(lo[2], lo[3], 0x7632));
-              product(d + 1, __byte_perm(hi[0], hi[1], 0x5410), __byte_perm(hi[0], hi[1], 0x7632),
-                      __byte_perm(hi[2], hi[3], 0x5410), __byte_perm(hi[2], hi[3], 0x7632));
+              product(d, f[0][0], f[1][0], f[0][1], f[1][1]);
+              product(d + 1, f[2][0], f[3][0], f[2][1], f[3][1]);
             }
           }
         } else {
@@ -718,49 +831,16 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
 #pragma unroll
           for (int d = 0; d < C::kMTiles; ++d) {
             uint32_t a0, a1, a2, a3;
-            load_transposed(v_addr + v_unit<DP>(j, 2 * d + half), a0, a1, a2, a3);
-            if (fix) {
-              auto clean = [](uint32_t x) {
-                if ((x & ones) == ones) x &= 0xffff0000u;
-                if (((x >> 16) & ones) == ones) x &= 0x0000ffffu;
-                return x;
-              };
-              a0 = clean(a0), a1 = clean(a1), a2 = clean(a2), a3 = clean(a3);
-            }
+            load_transposed(v_addr + v_unit<C::kRowBytes, false>(j, 2 * d + half), a0, a1, a2, a3);
             product(d, a0, a1, a2, a3);
-          }
-          if (fix) {
-            const int k0 = key + 16 * b;
-            for (int j = 0; j < 16; ++j) {
-#pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                const float w0 = __shfl_sync(0xffffffffu, j < 8 ? s[b][n][0] : s[b][n][2], (j & 7) * 4 + t);
-                const float w1 = __shfl_sync(0xffffffffu, j < 8 ? s[b][n][1] : s[b][n][3], (j & 7) * 4 + t);
-                const int r = n * 8 + 2 * t;
-                const bool see0 = k0 + j <= row_pos[r] && k0 + j >= row_lo[r];
-                const bool see1 = k0 + j <= row_pos[r + 1] && k0 + j >= row_lo[r + 1];
-#pragma unroll
-                for (int d = 0; d < C::kMTiles; ++d) {
-#pragma unroll
-                  for (int half = 0; half < 2; ++half) {
-                    const uint32_t bits =
-                        *reinterpret_cast<const uint16_t*>(vt + v_unit<DP>(j, 2 * d + half) + g * 2);
-                    if ((bits & ones) != ones) continue;
-                    float v;
-                    if constexpr (kBf16) v = __uint_as_float(bits << 16);
-                    else v = __half2float(__ushort_as_half((unsigned short)bits));
-                    if (see0) o[d][n][2 * half] += w0 * v;
-                    if (see1) o[d][n][2 * half + 1] += w1 * v;
-                  }
-                }
-              }
-            }
           }
         }
       }
       __syncwarp();   // page_ids and the ring slot are free again
+      slot = slot + 1 == C::kStages ? 0 : slot + 1;
+      key += C::kUnit;
     }
-    copy_wait<0>();
+    fresh = false;
 
     if constexpr (kBf16) {
       // an infinity of V times a weight's second term, which may be zero, gives NaN: such a triple is done again with
@@ -774,14 +854,29 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
           for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[d][n][e]) <= 3.402823466e+38f);
         }
       }
-      again = split && __any_sync(0xffffffffu, odd);
-      split = false;
+      if (split && __any_sync(0xffffffffu, odd)) {
+        split = false;
+        redo = fresh = true;
+        continue;
+      }
+      split = true;
+      redo = false;
     }
-    } while (again);
 
-    // ---- join the warps ----
-    __syncthreads();   // every warp is done with the ring
-    float* red = reinterpret_cast<float*>(smem) + warp * C::kRows * C::kOStride;
+    const int of_seq = seq, of_triple = triple, of_units = sp.units, of_base = seq_base;
+    left -= units;
+    first_unit = 0;
+    if (left > 0) {
+      if (++triple == per_seq) {
+        triple = 0;
+        seq_base += sp.units * per_seq;
+        seq = seq + 1 < a.table.seqs ? seq + 1 : seq;
+        sp = span_of(a, seq, C::kUnit);
+      }
+      load_q_early(seq, triple);
+    }
+
+    // ---- join the warps: scaled to the common maximum, added one after the other ----
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -790,132 +885,143 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
         sum += __shfl_xor_sync(0xffffffffu, sum, 4);
         sum += __shfl_xor_sync(0xffffffffu, sum, 8);
         sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-        const int r = n * 8 + 2 * t + h;
         if (g == 0) {
-          stat_m[warp][r] = m[n][h];
-          stat_l[warp][r] = sum;
-        }
-        const float back = C::kEight ? __frcp_rn(inv[n][h]) : 1.f;
-#pragma unroll
-        for (int d = 0; d < C::kMTiles; ++d) {
-          if constexpr (C::kEight) {   // tile d of a lane: two neighbouring dimensions
-            constexpr int kPer = C::kVBytes / 2;
-            const int at = d / kPer * (8 * C::kVBytes) + g * C::kVBytes + 2 * (d % kPer);
-            *reinterpret_cast<float2*>(red + r * C::kOStride + at) = make_float2(o[d][n][h] * back, o[d][n][h + 2] * back);
-          } else {
-            red[r * C::kOStride + d * 16 + g] = o[d][n][h];
-            red[r * C::kOStride + d * 16 + 8 + g] = o[d][n][h + 2];
-          }
+          stat_m[warp][n * 8 + 2 * t + h] = m[n][h];
+          stat_l[warp][n * 8 + 2 * t + h] = sum;
         }
       }
     }
     __syncthreads();
-    const bool whole = units == sp.units;
-    // the blocks that share the triple: c_first .. c_last; block i holds units [total i / parts, total (i + 1) / parts)
-    const int64_t c_first = ((begin + 1) * parts - 1) / total, c_last = ((begin + sp.units) * parts - 1) / total;
-    const float* all = reinterpret_cast<const float*>(smem);
-    constexpr int kQuads = DP / 4;
-    float* slot = a.partial + (block * 2 + (block == c_first ? 1 : 0)) * partial_floats(DP);
-    auto write_row = [&](int r, int quad, float4 acc, float sum, float top) {
-      const int row = row0 + r;
-      const int64_t tok = (int64_t)seq * a.new_tokens + row / a.group;
-      const int qh = head * a.group + row % a.group;
-      const float f = sum == 0.f ? 0.f : 1.f / sum;
-      const float4 y = sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-      unsigned char* dst = a.out.p + tok * a.out.token + qh * a.out.head;
-      if (quad * 4 < D) {
-        uint2 w;
-        if (a.q_f16) w = make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w));
-        else w = make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
-        *reinterpret_cast<uint2*>(dst + quad * 8) = w;
-      }
-      if (quad == 0 && a.lse) a.lse[tok * a.q_heads + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    auto top_of = [&](int r) {
+      return fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
     };
-    for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
-      const int r = i / kQuads, quad = i % kQuads;
-      float top = -INFINITY;
+#pragma unroll 1
+    for (int step = 0; step < kAttendWarps; ++step) {
+      if (warp == step) {
+        const bool add = step > 0;
 #pragma unroll
-      for (int w = 0; w < kAttendWarps; ++w) top = fmaxf(top, stat_m[w][r]);
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      float sum = 0.f;
-      const float base = top == -INFINITY ? 0.f : top;
+      for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int w = 0; w < kAttendWarps; ++w) {
-        const float f = exp2_fast(stat_m[w][r] - base);
-        const float4 x = *reinterpret_cast<const float4*>(all + (w * C::kRows + r) * C::kOStride + quad * 4);
-        acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
-        sum += f * stat_l[w][r];
-      }
-      if (whole) {
-        write_row(r, quad, acc, sum, top);
-      } else {
-        *reinterpret_cast<float4*>(slot + r * DP + quad * 4) = acc;
-        if (quad == 0) *reinterpret_cast<float2*>(slot + C::kRows * DP + r * 2) = make_float2(top, sum);
-      }
-    }
-    if (!whole) {
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        const unsigned int before = atomicAdd(a.arrived + c_first, 1u);
-        last_flag = before == (unsigned int)(c_last - c_first);
-        if (last_flag) a.arrived[c_first] = 0u;
-      }
-      __syncthreads();
-      if (last_flag) {
-        __threadfence();
-        // the blocks' maxima and sums first (the ring is free), then their sums of values with eight loads in flight
-        const int n_blocks = (int)(c_last - c_first) + 1;
-        float2* ml = reinterpret_cast<float2*>(smem);
-        auto part = [&](int i) { return a.partial + ((c_first + i) * 2 + (i == 0 ? 1 : 0)) * partial_floats(DP); };
-        for (int i = threadIdx.x; i < n_blocks * C::kRows; i += kAttendThreads)
-          ml[i] = __ldcg(reinterpret_cast<const float2*>(part(i / C::kRows) + C::kRows * DP) + i % C::kRows);
-        __syncthreads();
-        for (int r = warp; r < live_rows; r += kAttendWarps) {
-          float top = -INFINITY, sum = 0.f;
-          for (int i = lane; i < n_blocks; i += 32) top = fmaxf(top, ml[i * C::kRows + r].x);
+        for (int h = 0; h < 2; ++h) {
+          const int r = n * 8 + 2 * t + h;
+          const float top = top_of(r);
+          // (0 x NaN stays NaN: a row whose scores are NaN has no maximum but shows it)
+          const float f = exp2_fast(m[n][h] - (top == -INFINITY ? 0.f : top)) * (C::kEight ? __frcp_rn(inv[n][h]) : 1.f);
 #pragma unroll
-          for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-          const float base = top == -INFINITY ? 0.f : top;
-          for (int i = lane; i < n_blocks; i += 32) {
-            const float2 y = ml[i * C::kRows + r];
-            const float f = exp2_fast(y.x - base);
-            sum += f * y.y;
-            ml[i * C::kRows + r].x = f;
-          }
-#pragma unroll
-          for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-          if (lane == 0) {
-            stat_m[0][r] = top;
-            stat_l[0][r] = sum;
-          }
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
-          const int r = i / kQuads, quad = i % kQuads;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          int c = 0;
-          for (; c + 8 <= n_blocks; c += 8) {
-            float4 x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __ldcg(reinterpret_cast<const float4*>(part(c + e) + r * DP + quad * 4));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float f = ml[(c + e) * C::kRows + r].x;
-              acc.x += f * x[e].x, acc.y += f * x[e].y, acc.z += f * x[e].z, acc.w += f * x[e].w;
+          for (int d = 0; d < C::kMTiles; ++d) {
+            const float x = o[d][n][h] * f, y = o[d][n][h + 2] * f;
+            if constexpr (C::kEight) {   // tile d of a lane: two neighbouring dimensions
+              constexpr int kPer = C::kVBytes / 2;
+              float2* to = reinterpret_cast<float2*>(join + r * C::kOStride + d / kPer * (8 * C::kVBytes) + g * C::kVBytes +
+                                                     2 * (d % kPer));
+              const float2 was = add ? *to : make_float2(0.f, 0.f);
+              *to = make_float2(was.x + x, was.y + y);
+            } else {
+              float* to = join + r * C::kOStride + d * 16 + g;
+              to[0] = add ? to[0] + x : x;
+              to[8] = add ? to[8] + y : y;
             }
           }
-#pragma unroll 4
-          for (; c < n_blocks; ++c) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(part(c) + r * DP + quad * 4));
-            const float f = ml[c * C::kRows + r].x;
-            acc.x += f * x.x, acc.y += f * x.y, acc.z += f * x.z, acc.w += f * x.w;
-          }
-          write_row(r, quad, acc, stat_l[0][r], stat_m[0][r]);
         }
       }
+      }
+      __syncthreads();
     }
-    u += units;
+    const bool whole = units == of_units;
+    int c_first = block, c_last = block;   // the blocks that share the triple
+    if (!whole) {
+      const int begin = of_base + of_triple * of_units;
+      c_first = block_of(begin);
+      c_last = block_of(begin + of_units - 1);
+      if (threadIdx.x == 0) {
+        int* p = pending[block == c_first];
+        p[0] = of_seq, p[1] = of_triple, p[2] = c_first, p[3] = c_last;
+      }
+    }
+    float* mine_out = a.partial + (block * 2 + (block == c_first ? 1 : 0)) * partial_floats(DP);
+    for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
+      const int r = i / kQuads, quad = i % kQuads;
+      const float top = top_of(r), base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttendWarps; ++w) sum += exp2_fast(stat_m[w][r] - base) * stat_l[w][r];
+      const float4 acc = *reinterpret_cast<const float4*>(join + r * C::kOStride + quad * 4);
+      if (whole) {
+        write_row(a, of_seq, head, row0 + r, quad, acc, sum, top);
+      } else {
+        *reinterpret_cast<float4*>(mine_out + r * DP + quad * 4) = acc;
+        if (quad == 0) *reinterpret_cast<float2*>(mine_out + C::kRows * DP + r * 2) = make_float2(top, sum);
+      }
+    }
+  }
+
+  // ---- the triples that this block shares (the one it begins in and the one it ends in, at most): whichever block arrives
+  // last joins the blocks' sums, in their order. Only now, so that no wait for memory holds up the triples between ----
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    int* p = pending[threadIdx.x];
+    bool last = false;
+    if (p[2] >= 0) {
+      __threadfence();   // the block's partial sums, before its arrival; the others', after the last one's
+      last = atomicAdd(a.arrived + p[2], 1u) == (unsigned int)(p[3] - p[2]);
+      if (last) a.arrived[p[2]] = 0u;
+      __threadfence();
+    }
+    if (!last) p[2] = -1;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    const int c_first = pending[k][2], n_blocks = pending[k][3] - c_first + 1;
+    if (c_first < 0) continue;
+    const int of_seq = pending[k][0], head = pending[k][1] / a.row_tiles;
+    const int row0 = (pending[k][1] - head * a.row_tiles) * C::kRows;
+    const int live_rows = a.rows - row0 < C::kRows ? a.rows - row0 : C::kRows;
+    auto part = [&](int i) { return a.partial + ((int64_t)(c_first + i) * 2 + (i == 0 ? 1 : 0)) * partial_floats(DP); };
+    auto part_ml = [&](int i, int r) { return __ldcg(reinterpret_cast<const float2*>(part(i) + C::kRows * DP) + r); };
+    for (int r = warp; r < live_rows; r += kAttendWarps) {
+      float top = -INFINITY, sum = 0.f;
+      for (int i = lane; i < n_blocks; i += 32) {
+        const float2 y = part_ml(i, r);
+        const float now = fmaxf(top, y.x), base = now == -INFINITY ? 0.f : now;
+        sum = sum * exp2_fast(top - base) + exp2_fast(y.x - base) * y.y;
+        top = now;
+      }
+      float all = top;
+#pragma unroll
+      for (int x = 16; x; x >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, x));
+      sum *= exp2_fast(top - (all == -INFINITY ? 0.f : all));
+#pragma unroll
+      for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      if (lane == 0) {
+        stat_m[k][r] = all;
+        stat_l[k][r] = sum;
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
+      const int r = i / kQuads, quad = i % kQuads;
+      const float top = stat_m[k][r], base = top == -INFINITY ? 0.f : top;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = 0; c < n_blocks; c += 16) {   // sixteen loads in flight
+        float4 x[16];
+        float f[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int b = c + e < n_blocks ? c + e : n_blocks - 1;
+          x[e] = __ldcg(reinterpret_cast<const float4*>(part(b) + r * DP + quad * 4));
+          f[e] = part_ml(b, r).x;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if (c + e < n_blocks) {
+            const float w = exp2_fast(f[e] - base);
+            acc.x += w * x[e].x, acc.y += w * x[e].y, acc.z += w * x[e].z, acc.w += w * x[e].w;
+          }
+        }
+      }
+      write_row(a, of_seq, head, row0 + r, quad, acc, stat_l[k][r], top);
+    }
   }
 }
 
@@ -937,10 +1043,9 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
   a.row_tiles = (a.rows + C::kRows - 1) / C::kRows;
   // the most units the table allows, so that small calls launch few blocks
   const int64_t units = ((int64_t)a.max_len + 15) / C::kUnit + 1;
-  const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units / kMinUnits + 1;
+  const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units;
+  if (most >= 2147483648.0) return cudaErrorNotSupported;   // units are counted in 32 bits
   a.parts = most < (double)per_sm * num_sms ? (int)most : per_sm * num_sms;
-  const int joinable = C::kBody / (C::kRows * 8);   // a join holds every block's maxima and sums in the ring
-  if (a.parts > joinable) a.parts = joinable;
   kernel<<<a.parts, kAttendThreads, C::kSmem, st>>>(a);
   return cudaGetLastError();
 }
