@@ -111,8 +111,8 @@ struct AttendConfig {
   static constexpr int kMTiles = DP / 16;
   static constexpr int kQStride = DP * 2 + 64;                           // bytes of a row of q in shared memory
   static constexpr int kRing = kAttendWarps * kStages * kStageBytes;
-  static constexpr int kOStride = DP + 4;                                // floats of a row of sums in the join
-  static constexpr int kSmem = kRing + kRows * kQStride + kRows * kOStride * 4;
+  static constexpr int kOStride = DP / 4 + 8;                            // floats of a row of sums in a pass of the join
+  static constexpr int kSmem = kRing + kRows * kQStride + kAttendWarps * kRows * kOStride * 4;
 };
 
 __device__ __forceinline__ uint32_t shared_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -236,24 +236,42 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_k
   return s;
 }
 
-// Four dimensions of an output row (row `row` of its kv head), and with the first of them the row's lse.
+// Four values of an output row (row `row` of its kv head), and with the first of them the row's lse. Sums are kept in the
+// order of the accumulators: quad 4 d + p holds tile d's two values of lane group g = 2p and its two of g + 1.
+template <typename C>
 __device__ __forceinline__ void write_row(const AttendArgs& a, int seq, int head, int row, int quad, float4 acc, float sum,
                                           float top) {
   const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
   const int64_t token = (int64_t)seq * a.new_tokens + tok;
   const float f = sum == 0.f ? 0.f : 1.f / sum;   // nothing seen: zeros
   const float4 y = sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-  if (quad * 4 < a.head_dim) {
-    uint2 w;
-    if (a.q_f16) w = make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w));
-    else w = make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
-    *reinterpret_cast<uint2*>(a.out.p + token * a.out.token + qh * a.out.head + quad * 8) = w;
+  const int d = quad >> 2, g = (quad & 3) * 2;
+  int at[2];        // the first dimensions of two pairs
+  float2 pair[2];
+  if constexpr (C::kEight) {   // a lane's pair: two neighbours of its kVBytes dimensions
+    constexpr int kPer = C::kVBytes / 2;
+    at[0] = d / kPer * (8 * C::kVBytes) + g * C::kVBytes + 2 * (d % kPer);
+    at[1] = at[0] + C::kVBytes;
+    pair[0] = make_float2(y.x, y.y);
+    pair[1] = make_float2(y.z, y.w);
+  } else {                     // a lane's pair: dimensions g and g + 8 of the tile
+    at[0] = d * 16 + g;
+    at[1] = at[0] + 8;
+    pair[0] = make_float2(y.x, y.z);
+    pair[1] = make_float2(y.y, y.w);
+  }
+  unsigned char* out = a.out.p + token * a.out.token + qh * a.out.head;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (at[i] < a.head_dim)
+      *reinterpret_cast<uint32_t*>(out + at[i] * 2) =
+          a.q_f16 ? pack2<false>(pair[i].x, pair[i].y) : pack2<true>(pair[i].x, pair[i].y);
   }
   if (quad == 0 && a.lse) a.lse[token * a.q_heads + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <int FMT, int DP, int NT>
-__global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) attend_kernel(const __grid_constant__ AttendArgs a) {
   using C = AttendConfig<FMT, DP, NT>;
   constexpr bool kBf16 = FMT == LACACHE_KV_BF16;
   constexpr bool kQInRegs = NT * DP <= 128;   // more would spill: q is read from shared memory at its use
@@ -876,7 +894,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
       load_q_early(seq, triple);
     }
 
-    // ---- join the warps: scaled to the common maximum, added one after the other ----
+    // ---- join the warps, scaled to the common maximum, a quarter of the dimensions at a time ----
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -895,38 +913,6 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
     auto top_of = [&](int r) {
       return fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
     };
-#pragma unroll 1
-    for (int step = 0; step < kAttendWarps; ++step) {
-      if (warp == step) {
-        const bool add = step > 0;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = n * 8 + 2 * t + h;
-          const float top = top_of(r);
-          // (0 x NaN stays NaN: a row whose scores are NaN has no maximum but shows it)
-          const float f = exp2_fast(m[n][h] - (top == -INFINITY ? 0.f : top)) * (C::kEight ? __frcp_rn(inv[n][h]) : 1.f);
-#pragma unroll
-          for (int d = 0; d < C::kMTiles; ++d) {
-            const float x = o[d][n][h] * f, y = o[d][n][h + 2] * f;
-            if constexpr (C::kEight) {   // tile d of a lane: two neighbouring dimensions
-              constexpr int kPer = C::kVBytes / 2;
-              float2* to = reinterpret_cast<float2*>(join + r * C::kOStride + d / kPer * (8 * C::kVBytes) + g * C::kVBytes +
-                                                     2 * (d % kPer));
-              const float2 was = add ? *to : make_float2(0.f, 0.f);
-              *to = make_float2(was.x + x, was.y + y);
-            } else {
-              float* to = join + r * C::kOStride + d * 16 + g;
-              to[0] = add ? to[0] + x : x;
-              to[8] = add ? to[8] + y : y;
-            }
-          }
-        }
-      }
-      }
-      __syncthreads();
-    }
     const bool whole = units == of_units;
     int c_first = block, c_last = block;   // the blocks that share the triple
     if (!whole) {
@@ -939,19 +925,49 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
       }
     }
     float* mine_out = a.partial + (block * 2 + (block == c_first ? 1 : 0)) * partial_floats(DP);
-    for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
-      const int r = i / kQuads, quad = i % kQuads;
-      const float top = top_of(r), base = top == -INFINITY ? 0.f : top;
-      float sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kAttendWarps; ++w) sum += exp2_fast(stat_m[w][r] - base) * stat_l[w][r];
-      const float4 acc = *reinterpret_cast<const float4*>(join + r * C::kOStride + quad * 4);
-      if (whole) {
-        write_row(a, of_seq, head, row0 + r, quad, acc, sum, top);
-      } else {
-        *reinterpret_cast<float4*>(mine_out + r * DP + quad * 4) = acc;
-        if (quad == 0) *reinterpret_cast<float2*>(mine_out + C::kRows * DP + r * 2) = make_float2(top, sum);
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float top = top_of(n * 8 + 2 * t + h);
+        // (0 x NaN stays NaN: a row whose scores are NaN has no maximum but shows it)
+        m[n][h] = exp2_fast(m[n][h] - (top == -INFINITY ? 0.f : top)) * (C::kEight ? __frcp_rn(inv[n][h]) : 1.f);
       }
+    }
+    constexpr int kPart = C::kMTiles / 4, kPartQuads = kPart * 4;   // tiles, and quads of values, a pass
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float2* mine = reinterpret_cast<float2*>(join + warp * C::kRows * C::kOStride) + g;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int d = 0; d < kPart; ++d)
+            mine[(n * 8 + 2 * t + h) * (C::kOStride / 2) + d * 8] =
+                make_float2(o[c * kPart + d][n][h] * m[n][h], o[c * kPart + d][n][h + 2] * m[n][h]);
+        }
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < live_rows * kPartQuads; i += kAttendThreads) {
+        const int r = i / kPartQuads, q = i % kPartQuads, quad = c * kPartQuads + q;
+        const float top = top_of(r), base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kAttendWarps; ++w) {
+          const float4 x = *reinterpret_cast<const float4*>(join + (w * C::kRows + r) * C::kOStride + q * 4);
+          acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+          sum += exp2_fast(stat_m[w][r] - base) * stat_l[w][r];
+        }
+        if (whole) {
+          write_row<C>(a, of_seq, head, row0 + r, quad, acc, sum, top);
+        } else {
+          *reinterpret_cast<float4*>(mine_out + r * DP + quad * 4) = acc;
+          if (quad == 0) *reinterpret_cast<float2*>(mine_out + C::kRows * DP + r * 2) = make_float2(top, sum);
+        }
+      }
+      if (c < 3) __syncthreads();
     }
   }
 
@@ -1020,7 +1036,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_kernel(const __grid_con
           }
         }
       }
-      write_row(a, of_seq, head, row0 + r, quad, acc, stat_l[k][r], top);
+      write_row<C>(a, of_seq, head, row0 + r, quad, acc, stat_l[k][r], top);
     }
   }
 }
