@@ -108,6 +108,7 @@ struct AttendConfig {
   static constexpr int kTileBytes = 16 * DP * kItem;                     // K (or V) of 16 keys
   static constexpr int kStageBytes = kSub * 2 * kTileBytes + (kEight ? kKeys * 8 : 0);
   static constexpr int kStages = kStageBytes > 16000 ? (NT == 1 ? 3 : 2) : kStageBytes > 8000 ? 2 : 4;
+  static constexpr int kTripleCost = kStageBytes > 8000 ? 1 : 2;         // a triple's start and join, in units
   static constexpr int kMTiles = DP / 16;
   static constexpr int kQStride = DP * 2 + 64;                           // bytes of a row of q in shared memory
   static constexpr int kRing = kAttendWarps * kStages * kStageBytes;
@@ -236,15 +237,18 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_k
   return s;
 }
 
-// Four values of an output row (row `row` of its kv head), and with the first of them the row's lse. Sums are kept in the
-// order of the accumulators: quad 4 d + p holds tile d's two values of lane group g = 2p and its two of g + 1.
-template <typename C>
-__device__ __forceinline__ void write_row(const AttendArgs& a, int seq, int head, int row, int quad, float4 acc, float sum,
-                                          float top) {
+// Where row `row` of a kv head goes: bytes into out, and its index in lse.
+__device__ __forceinline__ int64_t out_at(const AttendArgs& a, int seq, int head, int row, int64_t* lse) {
   const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
   const int64_t token = (int64_t)seq * a.new_tokens + tok;
-  const float f = sum == 0.f ? 0.f : 1.f / sum;   // nothing seen: zeros
-  const float4 y = sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+  *lse = token * a.q_heads + qh;
+  return token * a.out.token + qh * a.out.head;
+}
+// Four values of an output row. Sums are kept in the order of the accumulators: quad 4 d + p holds tile d's two values of
+// lane group g = 2p and its two of g + 1. f is 1 / the row's sum of weights, 0 if nothing was seen.
+template <typename C>
+__device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, int quad, float4 acc, float f) {
+  const float4 y = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
   const int d = quad >> 2, g = (quad & 3) * 2;
   int at[2];        // the first dimensions of two pairs
   float2 pair[2];
@@ -260,14 +264,16 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int seq, int head
     pair[0] = make_float2(y.x, y.z);
     pair[1] = make_float2(y.y, y.w);
   }
-  unsigned char* out = a.out.p + token * a.out.token + qh * a.out.head;
+  unsigned char* out = a.out.p + at_row;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (at[i] < a.head_dim)
       *reinterpret_cast<uint32_t*>(out + at[i] * 2) =
           a.q_f16 ? pack2<false>(pair[i].x, pair[i].y) : pack2<true>(pair[i].x, pair[i].y);
   }
-  if (quad == 0 && a.lse) a.lse[token * a.q_heads + qh] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+__device__ __forceinline__ float lse_of(float top, float sum) {
+  return sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <int FMT, int DP, int NT>
@@ -279,29 +285,34 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   __shared__ float stat_m[kAttendWarps][C::kRows], stat_l[kAttendWarps][C::kRows];
   __shared__ int row_pos[C::kRows], row_lo[C::kRows];   // a row's own last and first visible position
   __shared__ float row_factor[C::kRows];                // scale log2(e), and what the row's q was divided by
+  __shared__ int64_t row_out[C::kRows];                 // where a row goes, and 1 / its sum of weights
+  __shared__ float row_inv[C::kRows];
   __shared__ int page_ids[kAttendWarps][C::kStages][C::kSub];
   __shared__ int pending[2][4];   // shared triples: sequence, triple, first and last block (-1: none)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int D = a.head_dim, row_bytes = D * C::kItem;
   const int per_seq = a.kv_heads * a.row_tiles;   // triples of a sequence
 
-  // ---- this block's part of the line of units (each warp for itself): units [start(block), start(block + 1)) ----
-  const int first_units = lane < a.table.seqs ? span_of(a, lane, C::kUnit).units : 0;   // of the first 32 sequences
+  // ---- this block's part of the line of cells (each warp for itself) ----
+  // a triple's cells: kTripleCost for its q and its join, which hold no keys, then its units
+  constexpr int kTripleCost = C::kTripleCost;
+  const int first_units = lane < a.table.seqs ? span_of(a, lane, C::kUnit).units + kTripleCost : 0;   // of 32 sequences
   int total = first_units;
-  for (int s = lane + 32; s < a.table.seqs; s += 32) total += span_of(a, s, C::kUnit).units;
+  for (int s = lane + 32; s < a.table.seqs; s += 32) total += span_of(a, s, C::kUnit).units + kTripleCost;
   total = __reduce_add_sync(0xffffffffu, total) * per_seq;
   const int parts = total < a.parts ? total : a.parts, block = blockIdx.x;
   if (block >= parts) return;
-  const int share = total / parts, longer = total - share * parts;   // the first `longer` blocks have one unit more
+  const int share = total / parts, longer = total - share * parts;   // the first `longer` blocks have one cell more
   const int u = block * share + (block < longer ? block : longer);
-  auto block_of = [&](int unit) {
+  auto block_of = [&](int cell) {
     const int in_longer = longer * (share + 1);
-    return unit < in_longer ? unit / (share + 1) : longer + (unit - in_longer) / share;
+    return cell < in_longer ? cell / (share + 1) : longer + (cell - in_longer) / share;
   };
-  int seq = 0, seq_base = 0;   // the sequence that unit u belongs to, and the units before it
+  int seq = 0, seq_base = 0;   // the sequence that cell u belongs to, and the cells before it
   for (int s0 = 0; s0 < a.table.seqs; s0 += 32) {
     const int own =
-        (s0 == 0 ? first_units : s0 + lane < a.table.seqs ? span_of(a, s0 + lane, C::kUnit).units : 0) * per_seq;
+        (s0 == 0 ? first_units : s0 + lane < a.table.seqs ? span_of(a, s0 + lane, C::kUnit).units + kTripleCost : 0) *
+        per_seq;
     int upto = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -320,8 +331,13 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   if (threadIdx.x < 2) pending[threadIdx.x][2] = -1;   // (the first triple's q, and a barrier, come before its use)
   constexpr int kQuads = DP / 4;
   Span sp = span_of(a, seq, C::kUnit);
-  int triple = (u - seq_base) / sp.units, first_unit = u - seq_base - triple * sp.units;
-  int left = share + (block < longer ? 1 : 0);   // units of this block that are not done
+  int triple = (u - seq_base) / (sp.units + kTripleCost);
+  int first_unit = u - seq_base - triple * (sp.units + kTripleCost) - kTripleCost;
+  int left = share + (block < longer ? 1 : 0);   // cells of this block that are not done
+  if (first_unit < 0) {
+    left += first_unit;
+    first_unit = 0;
+  }
 
   unsigned char* ring = smem + warp * C::kStages * C::kStageBytes;
   unsigned char* q_smem = smem + C::kRing;
@@ -414,7 +430,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
 #pragma unroll
         for (int s = 0; s < C::kSub; ++s) ahead.ids[s] = ahead.next_ids[s];
       }
-      if (++ahead.unit == ahead.sp.units && ahead.left > 0) {
+      if (++ahead.unit == ahead.sp.units && (ahead.left -= kTripleCost) > 0) {
         ahead.unit = 0;
         if (++ahead.triple == per_seq) {
           ahead.triple = 0;
@@ -883,11 +899,12 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
 
     const int of_seq = seq, of_triple = triple, of_units = sp.units, of_base = seq_base;
     left -= units;
+    if (first_unit + units == of_units) left -= kTripleCost;
     first_unit = 0;
     if (left > 0) {
       if (++triple == per_seq) {
         triple = 0;
-        seq_base += sp.units * per_seq;
+        seq_base += (sp.units + kTripleCost) * per_seq;
         seq = seq + 1 < a.table.seqs ? seq + 1 : seq;
         sp = span_of(a, seq, C::kUnit);
       }
@@ -910,13 +927,10 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       }
     }
     __syncthreads();
-    auto top_of = [&](int r) {
-      return fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
-    };
     const bool whole = units == of_units;
     int c_first = block, c_last = block;   // the blocks that share the triple
     if (!whole) {
-      const int begin = of_base + of_triple * of_units;
+      const int begin = of_base + of_triple * (of_units + kTripleCost) + kTripleCost;
       c_first = block_of(begin);
       c_last = block_of(begin + of_units - 1);
       if (threadIdx.x == 0) {
@@ -925,11 +939,28 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       }
     }
     float* mine_out = a.partial + (block * 2 + (block == c_first ? 1 : 0)) * partial_floats(DP);
+    if (threadIdx.x < live_rows) {
+      const int r = threadIdx.x;
+      const float top = fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttendWarps; ++w) sum += exp2_fast(stat_m[w][r] - base) * stat_l[w][r];
+      if (whole) {
+        int64_t at_lse;
+        row_out[r] = out_at(a, of_seq, head, row0 + r, &at_lse);
+        row_inv[r] = sum == 0.f ? 0.f : 1.f / sum;
+        if (a.lse) a.lse[at_lse] = lse_of(top, sum);
+      } else {
+        *reinterpret_cast<float2*>(mine_out + C::kRows * DP + r * 2) = make_float2(top, sum);
+      }
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float top = top_of(n * 8 + 2 * t + h);
+        const int r = n * 8 + 2 * t + h;
+        const float top = fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
         // (0 x NaN stays NaN: a row whose scores are NaN has no maximum but shows it)
         m[n][h] = exp2_fast(m[n][h] - (top == -INFINITY ? 0.f : top)) * (C::kEight ? __frcp_rn(inv[n][h]) : 1.f);
       }
@@ -951,21 +982,14 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       __syncthreads();
       for (int i = threadIdx.x; i < live_rows * kPartQuads; i += kAttendThreads) {
         const int r = i / kPartQuads, q = i % kPartQuads, quad = c * kPartQuads + q;
-        const float top = top_of(r), base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kAttendWarps; ++w) {
           const float4 x = *reinterpret_cast<const float4*>(join + (w * C::kRows + r) * C::kOStride + q * 4);
           acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
-          sum += exp2_fast(stat_m[w][r] - base) * stat_l[w][r];
         }
-        if (whole) {
-          write_row<C>(a, of_seq, head, row0 + r, quad, acc, sum, top);
-        } else {
-          *reinterpret_cast<float4*>(mine_out + r * DP + quad * 4) = acc;
-          if (quad == 0) *reinterpret_cast<float2*>(mine_out + C::kRows * DP + r * 2) = make_float2(top, sum);
-        }
+        if (whole) write_quad<C>(a, row_out[r], quad, acc, row_inv[r]);
+        else *reinterpret_cast<float4*>(mine_out + r * DP + quad * 4) = acc;
       }
       if (c < 3) __syncthreads();
     }
@@ -1010,14 +1034,17 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
 #pragma unroll
       for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
       if (lane == 0) {
-        stat_m[k][r] = all;
-        stat_l[k][r] = sum;
+        int64_t at_lse;
+        stat_m[0][r] = all;
+        row_out[r] = out_at(a, of_seq, head, row0 + r, &at_lse);
+        row_inv[r] = sum == 0.f ? 0.f : 1.f / sum;
+        if (a.lse) a.lse[at_lse] = lse_of(all, sum);
       }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
       const int r = i / kQuads, quad = i % kQuads;
-      const float top = stat_m[k][r], base = top == -INFINITY ? 0.f : top;
+      const float top = stat_m[0][r], base = top == -INFINITY ? 0.f : top;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int c = 0; c < n_blocks; c += 16) {   // sixteen loads in flight
         float4 x[16];
@@ -1036,8 +1063,9 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           }
         }
       }
-      write_row<C>(a, of_seq, head, row0 + r, quad, acc, stat_l[k][r], top);
+      write_quad<C>(a, row_out[r], quad, acc, row_inv[r]);
     }
+    __syncthreads();
   }
 }
 
@@ -1058,7 +1086,7 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
   }
   a.row_tiles = (a.rows + C::kRows - 1) / C::kRows;
   // the most units the table allows, so that small calls launch few blocks
-  const int64_t units = ((int64_t)a.max_len + 15) / C::kUnit + 1;
+  const int64_t units = ((int64_t)a.max_len + 15) / C::kUnit + 1 + C::kTripleCost;
   const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // units are counted in 32 bits
   a.parts = most < (double)per_sm * num_sms ? (int)most : per_sm * num_sms;
