@@ -296,9 +296,13 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   // ---- this block's part of the line of cells (each warp for itself) ----
   // a triple's cells: kTripleCost for its q and its join, which hold no keys, then its units
   constexpr int kTripleCost = C::kTripleCost;
-  const int first_units = lane < a.table.seqs ? span_of(a, lane, C::kUnit).units + kTripleCost : 0;   // of 32 sequences
-  int total = first_units;
-  for (int s = lane + 32; s < a.table.seqs; s += 32) total += span_of(a, s, C::kUnit).units + kTripleCost;
+  auto cells_of = [&](int s) { return s < a.table.seqs ? span_of(a, s, C::kUnit).units + kTripleCost : 0; };
+  int held[4], total = 0;   // the first 128 sequences', their loads all at once
+#pragma unroll
+  for (int i = 0; i < 4; ++i) held[i] = cells_of(32 * i + lane);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) total += held[i];
+  for (int s = lane + 128; s < a.table.seqs; s += 32) total += cells_of(s);
   total = __reduce_add_sync(0xffffffffu, total) * per_seq;
   const int parts = total < a.parts ? total : a.parts, block = blockIdx.x;
   if (block >= parts) return;
@@ -309,10 +313,10 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     return cell < in_longer ? cell / (share + 1) : longer + (cell - in_longer) / share;
   };
   int seq = 0, seq_base = 0;   // the sequence that cell u belongs to, and the cells before it
+#pragma unroll 1
   for (int s0 = 0; s0 < a.table.seqs; s0 += 32) {
-    const int own =
-        (s0 == 0 ? first_units : s0 + lane < a.table.seqs ? span_of(a, s0 + lane, C::kUnit).units + kTripleCost : 0) *
-        per_seq;
+    const int mine = s0 == 0 ? held[0] : s0 == 32 ? held[1] : s0 == 64 ? held[2] : s0 == 96 ? held[3] : cells_of(s0 + lane);
+    const int own = mine * per_seq;
     int upto = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -1010,62 +1014,119 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     if (!last) p[2] = -1;
   }
   __syncthreads();
-#pragma unroll 1
-  for (int k = 0; k < 2; ++k) {
-    const int c_first = pending[k][2], n_blocks = pending[k][3] - c_first + 1;
-    if (c_first < 0) continue;
-    const int of_seq = pending[k][0], head = pending[k][1] / a.row_tiles;
-    const int row0 = (pending[k][1] - head * a.row_tiles) * C::kRows;
-    const int live_rows = a.rows - row0 < C::kRows ? a.rows - row0 : C::kRows;
-    auto part = [&](int i) { return a.partial + ((int64_t)(c_first + i) * 2 + (i == 0 ? 1 : 0)) * partial_floats(DP); };
-    auto part_ml = [&](int i, int r) { return __ldcg(reinterpret_cast<const float2*>(part(i) + C::kRows * DP) + r); };
-    for (int r = warp; r < live_rows; r += kAttendWarps) {
-      float top = -INFINITY, sum = 0.f;
-      for (int i = lane; i < n_blocks; i += 32) {
-        const float2 y = part_ml(i, r);
-        const float now = fmaxf(top, y.x), base = now == -INFINITY ? 0.f : now;
-        sum = sum * exp2_fast(top - base) + exp2_fast(y.x - base) * y.y;
-        top = now;
-      }
-      float all = top;
+  auto part = [&](int k, int i) {   // block i's slot of shared triple k
+    return a.partial + ((int64_t)(pending[k][2] + i) * 2 + (i == 0 ? 1 : 0)) * partial_floats(DP);
+  };
+  auto part_ml = [&](int k, int i, int r) {
+    return __ldcg(reinterpret_cast<const float2*>(part(k, i) + C::kRows * DP) + r);
+  };
+  auto shared_rows = [&](int k) {
+    if (pending[k][2] < 0) return 0;
+    const int left_rows = a.rows - pending[k][1] % a.row_tiles * C::kRows;
+    return left_rows < C::kRows ? left_rows : C::kRows;
+  };
+  const int rows0 = shared_rows(0), rows1 = shared_rows(1);
+  __shared__ float joint_top[2 * C::kRows];
+  __shared__ int64_t joint_out[2 * C::kRows];
+  __shared__ float joint_inv[2 * C::kRows];
+  // the rows' common maxima and sums: eight lanes a row, eight loads in flight a lane
+  for (int x0 = 0; x0 < rows0 + rows1; x0 += kAttendThreads / 8) {
+    const int x = x0 + (threadIdx.x >> 3), sub = threadIdx.x & 7;
+    const bool live = x < rows0 + rows1;
+    const int k = x < rows0 ? 0 : 1, r = k == 0 ? x : x - rows0;
+    const int n_blocks = live ? pending[k][3] - pending[k][2] + 1 : 0;
+    float top = -INFINITY, sum = 0.f;
+    for (int c = sub; c < n_blocks; c += 64) {
+      float2 y[8];
 #pragma unroll
-      for (int x = 16; x; x >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, x));
-      sum *= exp2_fast(top - (all == -INFINITY ? 0.f : all));
+      for (int e = 0; e < 8; ++e) y[e] = c + 8 * e < n_blocks ? part_ml(k, c + 8 * e, r) : make_float2(-INFINITY, 0.f);
+      float now = top;
 #pragma unroll
-      for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-      if (lane == 0) {
-        int64_t at_lse;
-        stat_m[0][r] = all;
-        row_out[r] = out_at(a, of_seq, head, row0 + r, &at_lse);
-        row_inv[r] = sum == 0.f ? 0.f : 1.f / sum;
-        if (a.lse) a.lse[at_lse] = lse_of(all, sum);
-      }
+      for (int e = 0; e < 8; ++e) now = fmaxf(now, y[e].x);
+      const float base = now == -INFINITY ? 0.f : now;
+      sum *= exp2_fast(top - base);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += exp2_fast(y[e].x - base) * y[e].y;
+      top = now;
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < live_rows * kQuads; i += kAttendThreads) {
-      const int r = i / kQuads, quad = i % kQuads;
-      const float top = stat_m[0][r], base = top == -INFINITY ? 0.f : top;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int c = 0; c < n_blocks; c += 16) {   // sixteen loads in flight
-        float4 x[16];
-        float f[16];
+    float all = top;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int b = c + e < n_blocks ? c + e : n_blocks - 1;
-          x[e] = __ldcg(reinterpret_cast<const float4*>(part(b) + r * DP + quad * 4));
-          f[e] = part_ml(b, r).x;
-        }
+    for (int o = 4; o; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+    sum *= exp2_fast(top - (all == -INFINITY ? 0.f : all));
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (c + e < n_blocks) {
-            const float w = exp2_fast(f[e] - base);
-            acc.x += w * x[e].x, acc.y += w * x[e].y, acc.z += w * x[e].z, acc.w += w * x[e].w;
+    for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (live && sub == 0) {
+      const int head = pending[k][1] / a.row_tiles, row0 = (pending[k][1] - head * a.row_tiles) * C::kRows;
+      int64_t at_lse;
+      joint_out[x] = out_at(a, pending[k][0], head, row0 + r, &at_lse);
+      joint_top[x] = all == -INFINITY ? 0.f : all;
+      joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
+      if (a.lse) a.lse[at_lse] = lse_of(all, sum);
+    }
+  }
+  __syncthreads();
+  // sixteen loads in flight a thread: those of four values from up to four blocks, or of one value from sixteen
+  const int values = (rows0 + rows1) * kQuads;
+  const int most = max(rows0 ? pending[0][3] - pending[0][2] : 0, rows1 ? pending[1][3] - pending[1][2] : 0) + 1;
+  if (most <= 4) {
+    for (int j0 = threadIdx.x; j0 < values; j0 += 4 * kAttendThreads) {
+      float4 y[4][4];
+      float w[4][4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int j = j0 + v * kAttendThreads, x = j / kQuads, quad = j % kQuads;
+        const int k = x < rows0 ? 0 : 1, r = k == 0 ? x : x - rows0;
+        const int n_blocks = j < values ? pending[k][3] - pending[k][2] + 1 : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[v][e] = make_float4(0.f, 0.f, 0.f, 0.f);
+          w[v][e] = -INFINITY;
+          if (e < n_blocks) {
+            y[v][e] = __ldcg(reinterpret_cast<const float4*>(part(k, e) + r * DP + quad * 4));
+            w[v][e] = part_ml(k, e, r).x;
           }
         }
       }
-      write_quad<C>(a, row_out[r], quad, acc, row_inv[r]);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int j = j0 + v * kAttendThreads, x = j / kQuads;
+        if (j < values) {
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float f = exp2_fast(w[v][e] - joint_top[x]);
+            acc.x += f * y[v][e].x, acc.y += f * y[v][e].y, acc.z += f * y[v][e].z, acc.w += f * y[v][e].w;
+          }
+          write_quad<C>(a, joint_out[x], j % kQuads, acc, joint_inv[x]);
+        }
+      }
     }
-    __syncthreads();
+    return;
+  }
+  for (int j = threadIdx.x; j < values; j += kAttendThreads) {
+    const int x = j / kQuads, quad = j % kQuads;
+    const int k = x < rows0 ? 0 : 1, r = k == 0 ? x : x - rows0, n_blocks = pending[k][3] - pending[k][2] + 1;
+    const float base = joint_top[x];
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = 0; c < n_blocks; c += 16) {
+      float4 y[16];
+      float f[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if (c + e < n_blocks) {
+          y[e] = __ldcg(reinterpret_cast<const float4*>(part(k, c + e) + r * DP + quad * 4));
+          f[e] = part_ml(k, c + e, r).x;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if (c + e < n_blocks) {
+          const float w = exp2_fast(f[e] - base);
+          acc.x += w * y[e].x, acc.y += w * y[e].y, acc.z += w * y[e].z, acc.w += w * y[e].w;
+        }
+      }
+    }
+    write_quad<C>(a, joint_out[x], quad, acc, joint_inv[x]);
   }
 }
 
