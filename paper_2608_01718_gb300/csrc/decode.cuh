@@ -1,12 +1,15 @@
 // Shared by the decoding operators (rope.cu, kv_cache.cu, kv_attend.cu): rows of heads in 16-byte chunks, the rotation of a
 // chunk, the cache's formats, and the handle.
 //
-// A row of head_dim elements is held by a group of lanes, eight consecutive elements (a chunk) a lane. Groups have a power
-// of two of lanes, so that a row's maximum is a butterfly within the group; lanes past head_dim / 8 idle.
+// The row kernels hold a row of head_dim elements in a group of lanes, two chunks of eight consecutive elements a lane: the
+// two halves of its pairs in the half layout, so that a rotation needs no exchange. Groups have a power of two of lanes, so
+// that a row's maximum is a butterfly within the group; lanes past the row's chunks idle.
 #pragma once
 
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+
+#include <type_traits>
 
 #include "internal.cuh"
 
@@ -63,7 +66,8 @@ inline bool device_table(const lacache_kv_table* t, Table* out) {
 // The row kernels give a warp one token and a slab of its rows, kRowUnroll passes of 32 / lanes rows in flight. A slab is all
 // of a token's rows when the tokens alone fill the GPU; fewer tokens are cut into slabs of at least one pass.
 constexpr int kRowThreads = 128;
-constexpr int kRowUnroll = 4;
+constexpr int kRowBlocks = 8;         // blocks an SM: at most 64 registers a thread
+constexpr int kRowUnroll = 2;
 constexpr int64_t kRowWarps = 4096;   // about 27 warps an SM
 struct RowPlan {
   int slab;          // rows
@@ -82,10 +86,23 @@ inline RowPlan plan_rows(int64_t n, int rows, int lanes) {
   return p;
 }
 
-// Lanes of a group: the power of two that holds head_dim / 8 chunks.
-inline int lanes_for(int head_dim) {
+// How a rotation finds its pairs.
+enum RopeMode {
+  kRopeNone = 0,
+  kRopeHalf = 1,    // pairs (i, i + rot_dim / 2), rot_dim / 2 a multiple of 8: whole chunks pair up
+  kRopeNear = 2,    // pairs (2i, 2i + 1)
+  kRopeOdd = 3      // halves of other sizes: partners are read from memory
+};
+inline int rope_mode(const lacache_rope* r) {
+  if (!r) return kRopeNone;
+  if (r->layout == LACACHE_ROPE_INTERLEAVED) return kRopeNear;
+  return r->rot_dim % 16 ? kRopeOdd : kRopeHalf;
+}
+// Lanes of a group.
+inline int lanes_for(int head_dim, int rot_dim, int mode) {
+  const int used = mode == kRopeHalf ? rot_dim / 16 + ((head_dim - rot_dim) / 8 + 1) / 2 : (head_dim / 8 + 1) / 2;
   int n = 1;
-  while (n * 8 < head_dim) n *= 2;
+  while (n < used) n *= 2;
   return n;
 }
 
@@ -170,95 +187,137 @@ __device__ __forceinline__ float2 rope_angle(const lacache_rope& r, int i, int p
 __device__ __forceinline__ float turn_first(float x, float y, float2 a) { return __fmaf_rn(x, a.x, -__fmul_rn(y, a.y)); }
 __device__ __forceinline__ float turn_second(float x, float y, float2 a) { return __fmaf_rn(x, a.x, __fmul_rn(y, a.y)); }
 
-// A warp's angles of one token: every pair once, through shared memory, then those of this lane's chunk c into registers,
-// where they serve all heads. a[i] belongs to element 8c + i in the half layout, to pair 4c + i (i < 4) in the other.
-__device__ __forceinline__ void warp_angles(const lacache_rope& r, int pos, float sign, int c, float2* cs, float2 (&a)[8]) {
+// The chunks of lane p of a row's group: elements 8 c .. 8 c + 7.
+struct Chunks {
+  int c[2];
+  bool live[2];
+};
+template <int MODE>
+__device__ __forceinline__ Chunks chunks_of(int p, int chunks, int rot) {
+  Chunks m;
+  if (MODE == kRopeHalf) {
+    const int pairs = rot / 16;
+    m.c[0] = p < pairs ? p : 2 * p;   // past the rotated ones: rot / 8 + 2 (p - pairs)
+    m.c[1] = p < pairs ? p + pairs : 2 * p + 1;
+  } else {
+    m.c[0] = p;
+    m.c[1] = p + (chunks + 1) / 2;
+  }
+  m.live[0] = MODE == kRopeHalf ? m.c[0] < chunks : p < (chunks + 1) / 2;
+  m.live[1] = m.live[0] && m.c[1] < chunks;
+  return m;
+}
+
+// A warp's angles of one token: every pair once, through shared memory (which kRopeOdd keeps using), then this lane's into
+// registers, where they serve all heads: those of the elements of chunk 0 in the half layout, of the four pairs of each
+// chunk in the other.
+template <int MODE>
+__device__ __forceinline__ void warp_angles(const lacache_rope& r, int pos, float sign, const Chunks& m, float2* cs,
+                                            float2 (&a)[8]) {
   const int lane = threadIdx.x & 31, h = r.rot_dim >> 1;
   __syncwarp();
   for (int i = lane; i < h; i += 32) cs[i] = rope_angle(r, i, pos, sign);
   __syncwarp();
+  if constexpr (MODE != kRopeOdd) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int d = c * 8 + i;
-    const int at = r.layout == LACACHE_ROPE_INTERLEAVED ? c * 4 + i : d < h ? d : d - h;
-    a[i] = at < h ? cs[at] : make_float2(1.f, 0.f);
+    for (int i = 0; i < 8; ++i) {
+      const int at = MODE == kRopeHalf ? m.c[0] * 8 + i : m.c[i >> 2] * 4 + (i & 3);
+      a[i] = at < h ? cs[at] : make_float2(1.f, 0.f);
+    }
   }
 }
 
-// Rotates chunk c (elements 8c .. 8c+7) of the row whose chunk this lane holds in x, by the angles of warp_angles. All lanes
-// of the warp call it. In the half layout the partner of a chunk is a whole chunk of another lane of the group (`lanes`
-// wide) when rot_dim / 2 is a multiple of 8; `row` serves the other sizes, whose partners lie across chunks: the row's
-// elements in memory, still unrotated (the caller stores only after __syncwarp).
-template <typename T>
-__device__ __forceinline__ void rotate8(float (&x)[8], int c, int lanes, int rot, int layout, const float2 (&a)[8],
-                                        const T* row) {
-  const int d0 = c * 8;
-  if (layout == LACACHE_ROPE_INTERLEAVED) {
+// Rotates this lane's two chunks x0 and x1 of a row by the angles of warp_angles. kRopeOdd reads the partners from `row`, the
+// row's elements in memory, still unrotated (nullptr: no row; the caller stores only after __syncwarp).
+template <int MODE, typename T>
+__device__ __forceinline__ void rotate(float (&x0)[8], float (&x1)[8], const Chunks& m, int rot, const float2 (&a)[8],
+                                       const float2* cs, const T* row) {
+  if (MODE == kRopeHalf) {
+    if (m.c[0] * 8 >= rot) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float u = x0[i], v = x1[i];
+      x0[i] = turn_first(u, v, a[i]);
+      x1[i] = turn_second(v, u, a[i]);
+    }
+  } else if (MODE == kRopeNear) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (d0 + 2 * i < rot) {
-        const float u = x[2 * i], v = x[2 * i + 1];
-        x[2 * i] = turn_first(u, v, a[i]);
-        x[2 * i + 1] = turn_second(v, u, a[i]);
+      if (m.c[0] * 8 + 2 * i < rot) {
+        const float u = x0[2 * i], v = x0[2 * i + 1];
+        x0[2 * i] = turn_first(u, v, a[i]);
+        x0[2 * i + 1] = turn_second(v, u, a[i]);
+      }
+      if (m.c[1] * 8 + 2 * i < rot) {
+        const float u = x1[2 * i], v = x1[2 * i + 1];
+        x1[2 * i] = turn_first(u, v, a[4 + i]);
+        x1[2 * i + 1] = turn_second(v, u, a[4 + i]);
       }
     }
-    return;
-  }
-  const int h = rot >> 1;
-  float y[8];
-  if ((h & 7) == 0) {
-    const bool first = d0 < h;
-    const int src = (threadIdx.x & 31 & ~(lanes - 1)) | ((first ? c + (h >> 3) : c - (h >> 3)) & (lanes - 1));
+  } else if (MODE == kRopeOdd) {
+    const int h = rot >> 1;
+    if (!row) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, x[i], src);
-    if (d0 < rot) {
+    for (int k = 0; k < 2; ++k) {
+      float(&x)[8] = k ? x1 : x0;
+      if (!m.live[k]) continue;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = first ? turn_first(x[i], y[i], a[i]) : turn_second(x[i], y[i], a[i]);
+      for (int i = 0; i < 8; ++i) {
+        const int d = m.c[k] * 8 + i;
+        if (d < h) x[i] = turn_first(x[i], (float)row[d + h], cs[d]);
+        else if (d < rot) x[i] = turn_second(x[i], (float)row[d - h], cs[d - h]);
+      }
     }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int d = d0 + i;
-    y[i] = row && d < rot ? (float)row[d < h ? d + h : d - h] : 0.f;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int d = d0 + i;
-    if (d < rot) x[i] = d < h ? turn_first(x[i], y[i], a[i]) : turn_second(x[i], y[i], a[i]);
   }
 }
 
-// The row's scale in an 8-bit format and its codes: scale = amax / top, code = x / scale to nearest even, both IEEE
-// divisions. NaN for a row that holds an infinity or a NaN (its codes are 0).
+// The row's scale in an 8-bit format, amax / top by an IEEE division; NaN for a row that holds an infinity or a NaN (its codes
+// are 0).
 template <int FMT>
-__device__ __forceinline__ float row_scale(const float (&x)[8], int lanes) {
+__device__ __forceinline__ float row_scale(const float (&x0)[8], const float (&x1)[8], int lanes) {
+  constexpr float kInf = __builtin_huge_valf();
   float m = 0.f;
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    m = fmaxf(m, fabsf(x[i]));
-    bad |= !(fabsf(x[i]) <= 3.402823466e+38f);
+    m = fmaxf(m, fmaxf(fabsf(x0[i]), fabsf(x1[i])));
+    bad |= isnan(x0[i]) || isnan(x1[i]);
   }
-  if (bad) m = __int_as_float(0x7f800000);
+  if (bad) m = kInf;
   for (int o = lanes >> 1; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (m == __int_as_float(0x7f800000)) return __int_as_float(0x7fc00000);
-  return __fdiv_rn(m, FMT == LACACHE_KV_E4M3 ? 448.f : 127.f);
+  return m == kInf ? __int_as_float(0x7fc00000) : __fdiv_rn(m, FMT == LACACHE_KV_E4M3 ? 448.f : 127.f);
 }
+// x / scale correctly rounded, from r = 1 / scale correctly rounded: two of Markstein's corrections (P. Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): the first makes the quotient faithful,
+// the second, from an exact remainder, correctly rounded. For scales within 2^+-100, where nothing under- or overflows
+// (remainders below that belong to quotients whose code is 0).
+__device__ __forceinline__ float quotient(float x, float scale, float r) {
+  float q = __fmul_rn(x, r);
+  q = __fmaf_rn(__fmaf_rn(-q, scale, x), r, q);
+  return __fmaf_rn(__fmaf_rn(-q, scale, x), r, q);
+}
+// Codes of eight elements: x / scale (IEEE) to nearest, ties to even.
 template <int FMT>
-__device__ __forceinline__ uint2 quantise8(const float (&x)[8], float scale) {
-  uint32_t w[2] = {0, 0};
-  if (scale > 0.f) {
+__device__ __forceinline__ uint2 quantise8(const float (&x)[8], float scale, float r) {
+  if (!(scale > 0.f)) return make_uint2(0, 0);
+  float u[8];
+  const bool plain = scale > 0x1p-100f && scale < 0x1p100f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float u = __fdiv_rn(x[i], scale);
-      uint32_t code;
-      if (FMT == LACACHE_KV_E4M3) {
-        code = __nv_cvt_float_to_fp8(u, __NV_SATFINITE, __NV_E4M3);
-      } else {
-        code = (uint32_t)(int)fminf(fmaxf(rintf(u), -127.f), 127.f) & 0xffu;
-      }
-      w[i >> 2] |= code << (8 * (i & 3));
+  for (int i = 0; i < 8; ++i) u[i] = plain ? quotient(x[i], scale, r) : __fdiv_rn(x[i], scale);
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float* v = u + 4 * k;
+    if (FMT == LACACHE_KV_E4M3) {
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
+      w[k] = lo | hi << 16;
+    } else {
+      // adding 1.5 x 2^23 rounds to an integer in the low bits of the sum
+      uint32_t b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(fminf(fmaxf(v[i], -127.f), 127.f), 12582912.f));
+      w[k] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
     }
   }
   return make_uint2(w[0], w[1]);

@@ -16,7 +16,7 @@ struct AppendArgs {
   const int32_t* pos;
   const int32_t* rope_pos;
   Table table;
-  int q_heads, kv_heads, chunks, lanes, page_size, rotate, slab;
+  int q_heads, kv_heads, chunks, lanes, page_size, slab;
   int64_t tasks;
   int64_t pages;
   Rows k, v, q, q_out;
@@ -33,31 +33,17 @@ __device__ __forceinline__ int64_t cached_at(int64_t row, int chunks) {
   return row * chunks * (FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8 ? 8 : 16);
 }
 
-template <int FMT>
-__device__ __forceinline__ void store_cached(void* pool, float* scales, int64_t row, int chunks, int c, bool live, int lanes,
-                                             const float (&x)[8]) {
-  unsigned char* p = static_cast<unsigned char*>(pool) + cached_at<FMT>(row, chunks);
-  if constexpr (FMT == LACACHE_KV_BF16) {
-    if (live) store8(reinterpret_cast<__nv_bfloat16*>(p) + c * 8, x);
-  } else if constexpr (FMT == LACACHE_KV_F16) {
-    if (live) store8(reinterpret_cast<__half*>(p) + c * 8, x);
-  } else {
-    const float scale = row_scale<FMT>(x, lanes);
-    if (live) {
-      reinterpret_cast<uint2*>(p)[c] = quantise8<FMT>(x, scale);
-      if (c == 0) scales[row] = scale;
-    }
-  }
-}
-
 // A warp takes a token and a slab of its rows: q, then k, then v.
-template <typename T, int FMT>
-__global__ void __launch_bounds__(kRowThreads)
+template <typename T, int FMT, int MODE>
+__global__ void __launch_bounds__(kRowThreads, 5)   // its quotients take more registers than the other row kernels
     append_kernel(const __grid_constant__ lacache_rope rope, const __grid_constant__ AppendArgs a) {
+  using Stored = typename std::conditional<FMT == LACACHE_KV_F16, __half, __nv_bfloat16>::type;
+  constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
   __shared__ float2 cs[kRowThreads / 32][kMaxHeadDim / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int pass = 32 / a.lanes, c = lane & (a.lanes - 1), sub = lane / a.lanes;
-  const int rows = a.q_heads + 2 * a.kv_heads, slabs = (rows + a.slab - 1) / a.slab;
+  const int pass = 32 / a.lanes, sub = lane / a.lanes;
+  const Chunks m = chunks_of<MODE>(lane & (a.lanes - 1), a.chunks, rope.rot_dim);
+  const int kv = a.q_heads + a.kv_heads, rows = kv + a.kv_heads, slabs = (rows + a.slab - 1) / a.slab;
   const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
   for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.tasks; task += step) {
     const int64_t t = task / slabs;
@@ -67,40 +53,51 @@ __global__ void __launch_bounds__(kRowThreads)
         slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages, lane == 0 ? a.status : nullptr);
     if (place < 0) continue;
     float2 angle[8];
-    if (a.rotate) warp_angles(rope, a.rope_pos[t], 1.f, c, cs[warp], angle);
+    if (MODE != kRopeNone) warp_angles<MODE>(rope, a.rope_pos[t], 1.f, m, cs[warp], angle);
     for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
-      typename Chunk<T>::raw raw[kRowUnroll];
+      typename Chunk<T>::raw raw[kRowUnroll][2];
       const unsigned char* src[kRowUnroll];
 #pragma unroll
       for (int i = 0; i < kRowUnroll; ++i) {
         const int r = r0 + i * pass + sub;
-        const Rows& from = r < a.q_heads ? a.q : r < a.q_heads + a.kv_heads ? a.k : a.v;
-        const int h = r < a.q_heads ? r : r < a.q_heads + a.kv_heads ? r - a.q_heads : r - a.q_heads - a.kv_heads;
-        src[i] = from.p + t * from.token + h * from.head;
-        if (r < end && c < a.chunks) raw[i] = Chunk<T>::load(src[i] + c * (8 * sizeof(T)));
-        else raw[i] = {};
+        src[i] = r < a.q_heads ? a.q.p + t * a.q.token + r * a.q.head
+                 : r < kv      ? a.k.p + t * a.k.token + (r - a.q_heads) * a.k.head
+                               : a.v.p + t * a.v.token + (r - kv) * a.v.head;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          raw[i][k] = {};
+          if (r < end && m.live[k]) raw[i][k] = Chunk<T>::load(src[i] + m.c[k] * (8 * (int)sizeof(T)));
+        }
       }
 #pragma unroll
       for (int i = 0; i < kRowUnroll; ++i) {
-        if (r0 + i * pass >= end) break;
-        const int r = r0 + i * pass + sub;
-        const bool live = r < end && c < a.chunks, is_q = r < a.q_heads, is_v = r >= a.q_heads + a.kv_heads;
-        float x[8];
-        Chunk<T>::widen(raw[i], x);
-        // every lane takes part in the exchange; rows of v keep their own elements
-        if (a.rotate && r0 + i * pass < a.q_heads + a.kv_heads) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = x[e];
-          rotate8(y, c, a.lanes, rope.rot_dim, rope.layout, angle, live ? reinterpret_cast<const T*>(src[i]) : nullptr);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = is_v ? x[e] : y[e];
+        const int at = r0 + i * pass, r = at + sub;
+        if (at >= end) break;
+        float x0[8], x1[8];
+        Chunk<T>::widen(raw[i][0], x0);
+        Chunk<T>::widen(raw[i][1], x1);
+        if (MODE != kRopeNone) {
+          if (r < kv) rotate<MODE>(x0, x1, m, rope.rot_dim, angle, cs[warp], r < end ? reinterpret_cast<const T*>(src[i]) : nullptr);
+          if (MODE == kRopeOdd) __syncwarp();
         }
-        __syncwarp();
-        if (live && is_q) store8(reinterpret_cast<T*>(a.q_out.p + t * a.q_out.token + r * a.q_out.head) + c * 8, x);
-        if (r0 + (i + 1) * pass > a.q_heads) {   // a pass with rows of k or v: its lanes share their rows' maxima
-          const int64_t at = place + (int64_t)(is_q ? 0 : is_v ? r - a.q_heads - a.kv_heads : r - a.q_heads) * a.page_size;
-          store_cached<FMT>(is_v ? a.pv : a.pk, is_v ? a.vs : a.ks, at, a.chunks, c, live && !is_q, a.lanes, x);
+        const bool live[2] = {r < end && m.live[0], r < end && m.live[1]};
+        if (r < a.q_heads) {
+          T* to = reinterpret_cast<T*>(a.q_out.p + t * a.q_out.token + r * a.q_out.head);
+          if (live[0]) store8(to + m.c[0] * 8, x0);
+          if (live[1]) store8(to + m.c[1] * 8, x1);
+        }
+        if (at + pass <= a.q_heads) continue;   // no row of k or v in this pass
+        const bool is_v = r >= kv, cached = r >= a.q_heads;
+        const int64_t row = place + (int64_t)(is_v ? r - kv : cached ? r - a.q_heads : 0) * a.page_size;
+        unsigned char* to = static_cast<unsigned char*>(is_v ? a.pv : a.pk) + cached_at<FMT>(row, a.chunks);
+        if constexpr (kEight) {
+          const float scale = row_scale<FMT>(x0, x1, a.lanes), inv = __frcp_rn(scale);
+          if (cached && live[0]) reinterpret_cast<uint2*>(to)[m.c[0]] = quantise8<FMT>(x0, scale, inv);
+          if (cached && live[1]) reinterpret_cast<uint2*>(to)[m.c[1]] = quantise8<FMT>(x1, scale, inv);
+          if (cached && live[0] && m.c[0] == 0) (is_v ? a.vs : a.ks)[row] = scale;
+        } else {
+          if (cached && live[0]) store8(reinterpret_cast<Stored*>(to) + m.c[0] * 8, x0);
+          if (cached && live[1]) store8(reinterpret_cast<Stored*>(to) + m.c[1] * 8, x1);
         }
       }
     }
@@ -124,11 +121,12 @@ struct ReadArgs {
 
 // As append_kernel: a warp takes a token and a slab of its rows, k, then v.
 template <typename T, int FMT>
-__global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant__ ReadArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) read_kernel(const __grid_constant__ ReadArgs a) {
   using Stored = typename std::conditional<FMT == LACACHE_KV_F16, __half, __nv_bfloat16>::type;
   constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int pass = 32 / a.lanes, c = lane & (a.lanes - 1), sub = lane / a.lanes;
+  const int pass = 32 / a.lanes, sub = lane / a.lanes;
+  const Chunks m = chunks_of<kRopeNone>(lane & (a.lanes - 1), a.chunks, 0);
   const int rows = 2 * a.kv_heads, slabs = (rows + a.slab - 1) / a.slab;
   const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
   for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.tasks; task += step) {
@@ -139,44 +137,55 @@ __global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant
         slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages, lane == 0 ? a.status : nullptr);
     if (place < 0) continue;
     for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
-      typename std::conditional<kEight, uint2, uint4>::type raw[kRowUnroll];
+      typename std::conditional<kEight, uint2, uint4>::type raw[kRowUnroll][2];
       float scale[kRowUnroll];
 #pragma unroll
       for (int i = 0; i < kRowUnroll; ++i) {
         const int r = r0 + i * pass + sub;
         const bool is_v = r >= a.kv_heads;
-        if (r >= end || c >= a.chunks || !(is_v ? a.v.p : a.k.p)) continue;
+        if (r >= end || !m.live[0] || !(is_v ? a.v.p : a.k.p)) continue;
         const int64_t at = place + (int64_t)(is_v ? r - a.kv_heads : r) * a.page_size;
         const unsigned char* p = static_cast<const unsigned char*>(is_v ? a.pv : a.pk) + cached_at<FMT>(at, a.chunks);
-        if constexpr (kEight) {
-          raw[i] = reinterpret_cast<const uint2*>(p)[c];
-          scale[i] = (is_v ? a.vs : a.ks)[at];
-        } else {
-          raw[i] = reinterpret_cast<const uint4*>(p)[c];
-        }
+        const auto* from = reinterpret_cast<const typename std::conditional<kEight, uint2, uint4>::type*>(p);
+        raw[i][0] = from[m.c[0]];
+        if (m.live[1]) raw[i][1] = from[m.c[1]];
+        if constexpr (kEight) scale[i] = (is_v ? a.vs : a.ks)[at];
       }
 #pragma unroll
       for (int i = 0; i < kRowUnroll; ++i) {
         const int r = r0 + i * pass + sub;
         const bool is_v = r >= a.kv_heads;
         const Rows& dst = is_v ? a.v : a.k;
-        if (r >= end || c >= a.chunks || !dst.p) continue;
-        float x[8];
-        if constexpr (kEight) dequantise8<FMT>(raw[i], scale[i], x);
-        else widen8(raw[i], x, Stored());
-        store8(reinterpret_cast<T*>(dst.p + t * dst.token + (is_v ? r - a.kv_heads : r) * dst.head) + c * 8, x);
+        if (r >= end || !dst.p) continue;
+        T* to = reinterpret_cast<T*>(dst.p + t * dst.token + (is_v ? r - a.kv_heads : r) * dst.head);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (!m.live[k]) continue;
+          float x[8];
+          if constexpr (kEight) dequantise8<FMT>(raw[i][k], scale[i], x);
+          else widen8(raw[i][k], x, Stored());
+          store8(to + m.c[k] * 8, x);
+        }
       }
     }
   }
 }
 
+template <typename T, int FMT>
+void launch_append_mode(int mode, const lacache_rope& rope, const AppendArgs& a, unsigned grid, cudaStream_t st) {
+  auto* kernel = mode == kRopeNone   ? append_kernel<T, FMT, kRopeNone>
+                 : mode == kRopeHalf ? append_kernel<T, FMT, kRopeHalf>
+                 : mode == kRopeNear ? append_kernel<T, FMT, kRopeNear>
+                                     : append_kernel<T, FMT, kRopeOdd>;
+  kernel<<<grid, kRowThreads, 0, st>>>(rope, a);
+}
 template <typename T>
-void launch_append(int format, const lacache_rope& rope, const AppendArgs& a, unsigned grid, cudaStream_t st) {
+void launch_append(int format, int mode, const lacache_rope& rope, const AppendArgs& a, unsigned grid, cudaStream_t st) {
   switch (format) {
-    case LACACHE_KV_BF16: append_kernel<T, LACACHE_KV_BF16><<<grid, kRowThreads, 0, st>>>(rope, a); break;
-    case LACACHE_KV_F16: append_kernel<T, LACACHE_KV_F16><<<grid, kRowThreads, 0, st>>>(rope, a); break;
-    case LACACHE_KV_E4M3: append_kernel<T, LACACHE_KV_E4M3><<<grid, kRowThreads, 0, st>>>(rope, a); break;
-    default: append_kernel<T, LACACHE_KV_INT8><<<grid, kRowThreads, 0, st>>>(rope, a); break;
+    case LACACHE_KV_BF16: launch_append_mode<T, LACACHE_KV_BF16>(mode, rope, a, grid, st); break;
+    case LACACHE_KV_F16: launch_append_mode<T, LACACHE_KV_F16>(mode, rope, a, grid, st); break;
+    case LACACHE_KV_E4M3: launch_append_mode<T, LACACHE_KV_E4M3>(mode, rope, a, grid, st); break;
+    default: launch_append_mode<T, LACACHE_KV_INT8>(mode, rope, a, grid, st); break;
   }
 }
 template <typename T>
@@ -291,10 +300,10 @@ extern "C" lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, cons
   a.q_heads = q ? q_heads : 0;
   a.kv_heads = h->cfg.kv_heads;
   a.chunks = h->cfg.head_dim / 8;
-  a.lanes = lc::lanes_for(h->cfg.head_dim);
   a.page_size = h->cfg.page_size;
   a.pages = h->cfg.pages;
-  a.rotate = rope ? 1 : 0;
+  const int mode = lc::rope_mode(rope);
+  a.lanes = lc::lanes_for(h->cfg.head_dim, rope ? rope->rot_dim : 0, mode);
   a.pk = pool.k;
   a.pv = pool.v;
   a.ks = pool.k_scale;
@@ -307,9 +316,9 @@ extern "C" lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, cons
   a.tasks = rp.tasks;
   const unsigned grid = rp.blocks;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  if (dtype == LACACHE_BF16) lc::launch_append<__nv_bfloat16>(h->cfg.format, plan, a, grid, st);
-  else if (dtype == LACACHE_F16) lc::launch_append<__half>(h->cfg.format, plan, a, grid, st);
-  else lc::launch_append<float>(h->cfg.format, plan, a, grid, st);
+  if (dtype == LACACHE_BF16) lc::launch_append<__nv_bfloat16>(h->cfg.format, mode, plan, a, grid, st);
+  else if (dtype == LACACHE_F16) lc::launch_append<__half>(h->cfg.format, mode, plan, a, grid, st);
+  else lc::launch_append<float>(h->cfg.format, mode, plan, a, grid, st);
   return lc::from_cuda(cudaGetLastError());
 }
 
@@ -331,7 +340,7 @@ extern "C" lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const 
   a.pos = pos_dev;
   a.kv_heads = h->cfg.kv_heads;
   a.chunks = h->cfg.head_dim / 8;
-  a.lanes = lc::lanes_for(h->cfg.head_dim);
+  a.lanes = lc::lanes_for(h->cfg.head_dim, 0, lc::kRopeNone);
   a.page_size = h->cfg.page_size;
   a.pages = h->cfg.pages;
   a.pk = pool.k;

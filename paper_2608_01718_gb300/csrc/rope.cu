@@ -9,13 +9,14 @@
 namespace lc {
 namespace {
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads)
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks)
     rope_kernel(const __grid_constant__ lacache_rope rope, int64_t tasks, int slab, int heads, int chunks, int lanes, Rows x,
                 const int32_t* __restrict__ pos, float sign, Rows y) {
   __shared__ float2 cs[kRowThreads / 32][kMaxHeadDim / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int pass = 32 / lanes, c = lane & (lanes - 1), sub = lane / lanes;
+  const int pass = 32 / lanes, sub = lane / lanes;
+  const Chunks m = chunks_of<MODE>(lane & (lanes - 1), chunks, rope.rot_dim);
   const int slabs = (heads + slab - 1) / slab;
   const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
   for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < tasks; task += step) {
@@ -25,28 +26,41 @@ __global__ void __launch_bounds__(kRowThreads)
     const unsigned char* src = x.p + t * x.token;
     unsigned char* dst = y.p + t * y.token;
     float2 a[8];
-    warp_angles(rope, pos[t], sign, c, cs[warp], a);
+    warp_angles<MODE>(rope, pos[t], sign, m, cs[warp], a);
     for (int h0 = first; h0 < end; h0 += kRowUnroll * pass) {
-      typename Chunk<T>::raw raw[kRowUnroll];
+      typename Chunk<T>::raw raw[kRowUnroll][2];
 #pragma unroll
       for (int i = 0; i < kRowUnroll; ++i) {
         const int h = h0 + i * pass + sub;
-        if (h < end && c < chunks) raw[i] = Chunk<T>::load(src + h * x.head + c * (8 * sizeof(T)));
-        else raw[i] = {};
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          if (h < end && m.live[k]) raw[i][k] = Chunk<T>::load(src + h * x.head + m.c[k] * (8 * (int)sizeof(T)));
       }
 #pragma unroll
       for (int i = 0; i < kRowUnroll; ++i) {
-        if (h0 + i * pass >= end) break;
         const int h = h0 + i * pass + sub;
-        const bool live = h < end && c < chunks;
-        float v[8];
-        Chunk<T>::widen(raw[i], v);
-        rotate8(v, c, lanes, rope.rot_dim, rope.layout, a, live ? reinterpret_cast<const T*>(src + h * x.head) : nullptr);
-        __syncwarp();
-        if (live) store8(reinterpret_cast<T*>(dst + h * y.head) + c * 8, v);
+        float v0[8], v1[8];
+        Chunk<T>::widen(raw[i][0], v0);
+        Chunk<T>::widen(raw[i][1], v1);
+        rotate<MODE>(v0, v1, m, rope.rot_dim, a, cs[warp], h < end ? reinterpret_cast<const T*>(src + h * x.head) : nullptr);
+        if (MODE == kRopeOdd) __syncwarp();
+        T* to = reinterpret_cast<T*>(dst + h * y.head);
+        if (h < end && m.live[0]) store8(to + m.c[0] * 8, v0);
+        if (h < end && m.live[1]) store8(to + m.c[1] * 8, v1);
       }
     }
   }
+}
+
+template <typename T>
+void launch_rope(int mode, const lacache_rope& rope, int64_t n, int heads, int head_dim, const Rows& x, const int32_t* pos,
+                 float sign, const Rows& y, cudaStream_t st) {
+  const int lanes = lanes_for(head_dim, rope.rot_dim, mode);
+  const RowPlan plan = plan_rows(n, heads, lanes);
+  auto* kernel = mode == kRopeHalf   ? rope_kernel<T, kRopeHalf>
+                 : mode == kRopeNear ? rope_kernel<T, kRopeNear>
+                                     : rope_kernel<T, kRopeOdd>;
+  kernel<<<plan.blocks, kRowThreads, 0, st>>>(rope, plan.tasks, plan.slab, heads, head_dim / 8, lanes, x, pos, sign, y);
 }
 
 }  // namespace
@@ -97,14 +111,11 @@ extern "C" lacache_status lacache_rope_apply(const lacache_rope* rope, int64_t n
   if (head_dim % 8 || head_dim > lc::kMaxHeadDim) return LACACHE_ERR_UNSUPPORTED;
   if (n == 0) return LACACHE_OK;
   if (!pos_dev || !lc::device_rows(x, dtype, &xr) || !lc::device_rows(y, dtype, &yr)) return LACACHE_ERR_INVALID_ARG;
-  const int lanes = lc::lanes_for(head_dim);
-  const lc::RowPlan plan = lc::plan_rows(n, heads, lanes);
   const float sign = inverse ? -1.f : 1.f;
+  const int mode = lc::rope_mode(rope);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  auto* kernel = dtype == LACACHE_BF16  ? lc::rope_kernel<__nv_bfloat16>
-                 : dtype == LACACHE_F16 ? lc::rope_kernel<__half>
-                                        : lc::rope_kernel<float>;
-  kernel<<<plan.blocks, lc::kRowThreads, 0, st>>>(*rope, plan.tasks, plan.slab, heads, head_dim / 8, lanes, xr, pos_dev,
-                                                   sign, yr);
+  if (dtype == LACACHE_BF16) lc::launch_rope<__nv_bfloat16>(mode, *rope, n, heads, head_dim, xr, pos_dev, sign, yr, st);
+  else if (dtype == LACACHE_F16) lc::launch_rope<__half>(mode, *rope, n, heads, head_dim, xr, pos_dev, sign, yr, st);
+  else lc::launch_rope<float>(mode, *rope, n, heads, head_dim, xr, pos_dev, sign, yr, st);
   return lc::from_cuda(cudaGetLastError());
 }
