@@ -37,18 +37,21 @@ constexpr int kMaxNewTokens = 512;
 struct Rows {   // lacache_rows on the device
   unsigned char* p;
   int64_t token;   // bytes
-  int64_t head;
+  int head16;      // 16-byte units
+  __device__ __forceinline__ unsigned char* at(int64_t t, int h) const { return p + t * token + (int64_t)h * head16 * 16; }
 };
 
 inline int dtype_bytes(int dtype) { return dtype == LACACHE_F32 ? 4 : 2; }
 inline bool known_dtype(int dtype) { return dtype == LACACHE_BF16 || dtype == LACACHE_F32 || dtype == LACACHE_F16; }
 inline bool is_quantised(int format) { return format == LACACHE_KV_E4M3 || format == LACACHE_KV_INT8; }
 
-// *r as device rows; false if its address or strides are not multiples of 16 bytes.
+// *r as device rows; false if its address or strides are not multiples of 16 bytes (or its heads lie 32 GB apart).
 inline bool device_rows(const lacache_rows* r, int dtype, Rows* out) {
   const int64_t b = dtype_bytes(dtype);
   if (!r || !r->data || !aligned16(r->data) || (r->token_stride * b) % 16 || (r->head_stride * b) % 16) return false;
-  *out = Rows{static_cast<unsigned char*>(r->data), r->token_stride * b, r->head_stride * b};
+  const int64_t head16 = r->head_stride * b / 16;
+  if (head16 > INT32_MAX || head16 < INT32_MIN) return false;
+  *out = Rows{static_cast<unsigned char*>(r->data), r->token_stride * b, (int)head16};
   return true;
 }
 
@@ -63,26 +66,36 @@ inline bool device_table(const lacache_kv_table* t, Table* out) {
   return true;
 }
 
-// The row kernels give a warp one token and a slab of its rows, kRowUnroll passes of 32 / lanes rows in flight. A slab is all
-// of a token's rows when the tokens alone fill the GPU; fewer tokens are cut into slabs of at least one pass.
+// The row kernels give a warp a group of tokens and a slab of their rows, kRowUnroll passes of 32 / lanes rows in flight. Few
+// tokens are cut into slabs of at least one pass, until the warps fill the GPU; of many, a warp of the cache's kernels takes
+// up to kRowGroup, whose places its lanes look up at once (write of 12,001 tokens of 48 rows: one 68.6 us, four 63.4; read
+// of 60,000 of 16 rows: one 69.0 us, two 64.4, four 63.1). Beyond that there are more blocks than the GPU holds.
 constexpr int kRowThreads = 128;
-constexpr int kRowBlocks = 8;         // blocks an SM: at most 64 registers a thread
 constexpr int kRowUnroll = 2;
-constexpr int64_t kRowWarps = 4096;   // about 27 warps an SM
+constexpr int kRowGroup = 4;
+constexpr int kSms = 152;
 struct RowPlan {
-  int slab;          // rows
-  int64_t tasks;     // tokens x slabs, one a warp
-  unsigned blocks;
+  int64_t n;         // tokens
+  int rows, slab;    // of a token, and of a task
+  int slabs, group;  // slabs of a token, tokens of a task
+  int64_t tasks;
 };
-inline RowPlan plan_rows(int64_t n, int rows, int lanes) {
+// `blocks`: blocks of the kernel an SM holds. `most`: tokens of a group. *grid: the launch's blocks.
+inline RowPlan plan_rows(int64_t n, int rows, int lanes, int blocks, int most, unsigned* grid) {
+  const int64_t resident = (int64_t)kSms * blocks * (kRowThreads / 32);
   const int pass = 32 / lanes, passes = (rows + pass - 1) / pass;
-  int64_t slabs = (kRowWarps + n - 1) / n;
-  if (slabs > passes) slabs = passes;
+  int64_t slabs = resident / n, group = (n + resident - 1) / resident;
+  slabs = slabs < 1 ? 1 : slabs > passes ? passes : slabs;
+  group = group > most ? most : group;
   RowPlan p;
+  p.n = n;
+  p.rows = rows;
   p.slab = (int)((passes + slabs - 1) / slabs) * pass;
-  p.tasks = n * ((rows + p.slab - 1) / p.slab);
-  const int64_t blocks = (p.tasks + kRowThreads / 32 - 1) / (kRowThreads / 32);
-  p.blocks = (unsigned)(blocks < (1 << 30) ? blocks : 1 << 30);
+  p.slabs = (rows + p.slab - 1) / p.slab;
+  p.group = (int)group;
+  p.tasks = (n + group - 1) / group * p.slabs;
+  const int64_t want = (p.tasks + kRowThreads / 32 - 1) / (kRowThreads / 32);
+  *grid = (unsigned)(want < (1 << 30) ? want : 1 << 30);
   return p;
 }
 
@@ -90,12 +103,12 @@ inline RowPlan plan_rows(int64_t n, int rows, int lanes) {
 enum RopeMode {
   kRopeNone = 0,
   kRopeHalf = 1,    // pairs (i, i + rot_dim / 2), rot_dim / 2 a multiple of 8: whole chunks pair up
-  kRopeNear = 2,    // pairs (2i, 2i + 1)
-  kRopeOdd = 3      // halves of other sizes: partners are read from memory
+  kRopeNear = 2,    // pairs (2i, 2i + 1), rot_dim a multiple of 8
+  kRopeOdd = 3      // either, of other sizes: partners are read from memory
 };
 inline int rope_mode(const lacache_rope* r) {
   if (!r) return kRopeNone;
-  if (r->layout == LACACHE_ROPE_INTERLEAVED) return kRopeNear;
+  if (r->layout == LACACHE_ROPE_INTERLEAVED) return r->rot_dim % 8 ? kRopeOdd : kRopeNear;
   return r->rot_dim % 16 ? kRopeOdd : kRopeHalf;
 }
 // Lanes of a group.
@@ -230,8 +243,8 @@ __device__ __forceinline__ void warp_angles(const lacache_rope& r, int pos, floa
 // Rotates this lane's two chunks x0 and x1 of a row by the angles of warp_angles. kRopeOdd reads the partners from `row`, the
 // row's elements in memory, still unrotated (nullptr: no row; the caller stores only after __syncwarp).
 template <int MODE, typename T>
-__device__ __forceinline__ void rotate(float (&x0)[8], float (&x1)[8], const Chunks& m, int rot, const float2 (&a)[8],
-                                       const float2* cs, const T* row) {
+__device__ __forceinline__ void rotate(float (&x0)[8], float (&x1)[8], const Chunks& m, int rot, int layout,
+                                       const float2 (&a)[8], const float2* cs, const T* row) {
   if (MODE == kRopeHalf) {
     if (m.c[0] * 8 >= rot) return;
 #pragma unroll
@@ -242,20 +255,20 @@ __device__ __forceinline__ void rotate(float (&x0)[8], float (&x1)[8], const Chu
     }
   } else if (MODE == kRopeNear) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (m.c[0] * 8 + 2 * i < rot) {
-        const float u = x0[2 * i], v = x0[2 * i + 1];
-        x0[2 * i] = turn_first(u, v, a[i]);
-        x0[2 * i + 1] = turn_second(v, u, a[i]);
-      }
-      if (m.c[1] * 8 + 2 * i < rot) {
-        const float u = x1[2 * i], v = x1[2 * i + 1];
-        x1[2 * i] = turn_first(u, v, a[4 + i]);
-        x1[2 * i + 1] = turn_second(v, u, a[4 + i]);
+    for (int k = 0; k < 2; ++k) {
+      float(&x)[8] = k ? x1 : x0;
+      if (m.c[k] * 8 < rot) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float u = x[2 * i], v = x[2 * i + 1];
+          x[2 * i] = turn_first(u, v, a[4 * k + i]);
+          x[2 * i + 1] = turn_second(v, u, a[4 * k + i]);
+        }
       }
     }
   } else if (MODE == kRopeOdd) {
     const int h = rot >> 1;
+    const bool near = layout == LACACHE_ROPE_INTERLEAVED;
     if (!row) return;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -264,8 +277,11 @@ __device__ __forceinline__ void rotate(float (&x0)[8], float (&x1)[8], const Chu
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int d = m.c[k] * 8 + i;
-        if (d < h) x[i] = turn_first(x[i], (float)row[d + h], cs[d]);
-        else if (d < rot) x[i] = turn_second(x[i], (float)row[d - h], cs[d - h]);
+        if (d >= rot) continue;
+        const bool first = near ? !(d & 1) : d < h;
+        const float y = (float)row[near ? d ^ 1 : first ? d + h : d - h];
+        const float2 angle = cs[near ? d >> 1 : first ? d : d - h];
+        x[i] = first ? turn_first(x[i], y, angle) : turn_second(x[i], y, angle);
       }
     }
   }
@@ -275,17 +291,13 @@ __device__ __forceinline__ void rotate(float (&x0)[8], float (&x1)[8], const Chu
 // are 0).
 template <int FMT>
 __device__ __forceinline__ float row_scale(const float (&x0)[8], const float (&x1)[8], int lanes) {
-  constexpr float kInf = __builtin_huge_valf();
-  float m = 0.f;
-  bool bad = false;
+  // magnitudes order as their bits do, infinity and NaN above the finite ones
+  uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    m = fmaxf(m, fmaxf(fabsf(x0[i]), fabsf(x1[i])));
-    bad |= isnan(x0[i]) || isnan(x1[i]);
-  }
-  if (bad) m = kInf;
-  for (int o = lanes >> 1; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  return m == kInf ? __int_as_float(0x7fc00000) : __fdiv_rn(m, FMT == LACACHE_KV_E4M3 ? 448.f : 127.f);
+  for (int i = 0; i < 8; ++i) m = max(max(m, __float_as_uint(x0[i]) & 0x7fffffffu), __float_as_uint(x1[i]) & 0x7fffffffu);
+  for (int o = lanes >> 1; o; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+  return m >= 0x7f800000u ? __int_as_float(0x7fc00000)
+                          : __fdiv_rn(__uint_as_float(m), FMT == LACACHE_KV_E4M3 ? 448.f : 127.f);
 }
 // x / scale correctly rounded, from r = 1 / scale correctly rounded: two of Markstein's corrections (P. Markstein,
 // "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): the first makes the quotient faithful,
@@ -304,6 +316,11 @@ __device__ __forceinline__ uint2 quantise8(const float (&x)[8], float scale, flo
   const bool plain = scale > 0x1p-100f && scale < 0x1p100f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) u[i] = plain ? quotient(x[i], scale, r) : __fdiv_rn(x[i], scale);
+  // (a plain quotient is at most top, but for a rounding; a subnormal scale may be too small for its row)
+  if (FMT == LACACHE_KV_INT8 && !plain) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = fminf(fmaxf(u[i], -127.f), 127.f);
+  }
   uint32_t w[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -316,22 +333,37 @@ __device__ __forceinline__ uint2 quantise8(const float (&x)[8], float scale, flo
       // adding 1.5 x 2^23 rounds to an integer in the low bits of the sum
       uint32_t b[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(fminf(fmaxf(v[i], -127.f), 127.f), 12582912.f));
+      for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(v[i], 12582912.f));
       w[k] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
     }
   }
   return make_uint2(w[0], w[1]);
 }
+// Four codes as f16 pairs: elements 0, 1 and 2, 3. Exact.
+template <int FMT>
+__device__ __forceinline__ void widen4(uint32_t u, uint32_t& lo, uint32_t& hi) {
+  if constexpr (FMT == LACACHE_KV_E4M3) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(u));
+  } else {
+    // 0x6400 | (code + 128) is 1024 + code + 128 as f16
+    const uint32_t x = u ^ 0x80808080u;
+    const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+    const __half2 bias = __float2half2_rn(1152.f);
+    const __half2 p = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), q = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
+    lo = *reinterpret_cast<const uint32_t*>(&p);
+    hi = *reinterpret_cast<const uint32_t*>(&q);
+  }
+}
 template <int FMT>
 __device__ __forceinline__ void dequantise8(uint2 u, float scale, float (&x)[8]) {
+  uint32_t w[4];
+  widen4<FMT>(u.x, w[0], w[1]);
+  widen4<FMT>(u.y, w[2], w[3]);
+  widen8(make_uint4(w[0], w[1], w[2], w[3]), x, __half());
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t code = ((i < 4 ? u.x : u.y) >> (8 * (i & 3))) & 0xffu;
-    if (FMT == LACACHE_KV_E4M3)
-      x[i] = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3))) * scale;
-    else
-      x[i] = (float)(int)(int8_t)code * scale;
-  }
+  for (int i = 0; i < 8; ++i) x[i] *= scale;
 }
 
 // The cache row index (page * heads + head) * page_size + slot of a token, without the head: page * heads * page_size + slot,

@@ -187,24 +187,6 @@ __device__ __forceinline__ int v_unit(int j, int u) {
   return ROW == 64 ? (j >> 1) * 128 + ((((j & 1) * 4 + u) ^ (j & 6)) << 4) : j * ROW + ((u ^ (j & 6)) << 4);
 }
 
-// Four codes as f16 pairs: elements 0, 1 and 2, 3. Exact.
-template <int FMT>
-__device__ __forceinline__ void widen4(uint32_t u, uint32_t& lo, uint32_t& hi) {
-  if constexpr (FMT == LACACHE_KV_E4M3) {
-    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-        : "=r"(lo), "=r"(hi)
-        : "r"(u));
-  } else {
-    // 0x6400 | (code + 128) is 1024 + code + 128 as f16
-    const uint32_t x = u ^ 0x80808080u;
-    const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
-    const __half2 bias = __float2half2_rn(1152.f);
-    const __half2 p = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), q = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
-    lo = *reinterpret_cast<const uint32_t*>(&p);
-    hi = *reinterpret_cast<const uint32_t*>(&q);
-  }
-}
-
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float x, float y) {
   if constexpr (BF16) {
@@ -242,7 +224,7 @@ __device__ __forceinline__ int64_t out_at(const AttendArgs& a, int seq, int head
   const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
   const int64_t token = (int64_t)seq * a.new_tokens + tok;
   *lse = token * a.q_heads + qh;
-  return token * a.out.token + qh * a.out.head;
+  return a.out.at(token, qh) - a.out.p;
 }
 // Four values of an output row. Sums are kept in the order of the accumulators: quad 4 d + p holds tile d's two values of
 // lane group g = 2p and its two of g + 1. f is 1 / the row's sum of weights, 0 if nothing was seen.
@@ -452,8 +434,8 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     const int row = of_row0 + r, tok = row / a.group;
     uint4 x = make_uint4(0, 0, 0, 0);
     if (row < a.rows && lane * 8 < D)
-      x = *reinterpret_cast<const uint4*>(a.q.p + ((int64_t)of_seq * a.new_tokens + tok) * a.q.token +
-                                          (int64_t)(of_head * a.group + row - tok * a.group) * a.q.head + lane * 16);
+      x = *reinterpret_cast<const uint4*>(
+          a.q.at((int64_t)of_seq * a.new_tokens + tok, of_head * a.group + row - tok * a.group) + lane * 16);
     return x;
   };
   constexpr bool kQEarly = NT <= 2;   // the next triple's q is read before the join; more rows would spill

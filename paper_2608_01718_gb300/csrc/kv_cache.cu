@@ -1,8 +1,8 @@
 // The paged key-value cache: the handle, the write of new tokens (rotation, quantisation and placement in one pass), and
 // reading cached tokens back.
 //
-// Both kernels are bound by memory: every input row is read once and every cached row written once (or the reverse). A warp
-// takes a token, finds its place and its angles once, and runs over its rows.
+// Both kernels are bound by memory: every input row is read once and every cached row written once (or the reverse). For each
+// of its tokens a warp finds the place and the angles once, and runs over the rows.
 #include <new>
 #include <type_traits>
 
@@ -11,93 +11,111 @@
 namespace lc {
 namespace {
 
+// Blocks an SM (append_kernel's quotients take more registers).
+constexpr int kAppendBlocks = 5, kReadBlocks = 8;
+
 struct AppendArgs {
+  RowPlan plan;
   const int32_t* seq;
   const int32_t* pos;
   const int32_t* rope_pos;
   Table table;
-  int q_heads, kv_heads, chunks, lanes, page_size, slab;
-  int64_t tasks;
+  int q_heads, kv_heads, chunks, lanes, page_size;
+  int64_t head_bytes;   // a head's rows of a page
   int64_t pages;
   Rows k, v, q, q_out;
-  void* pk;
-  void* pv;
+  unsigned char* pk;
+  unsigned char* pv;
   float* ks;
   float* vs;
   unsigned int* status;
 };
 
-// Element (0, head, slot) of a cached row, as bytes from the pool's start.
+// The place of cached row `row`, in bytes from the pool's start.
 template <int FMT>
 __device__ __forceinline__ int64_t cached_at(int64_t row, int chunks) {
   return row * chunks * (FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8 ? 8 : 16);
 }
 
-// A warp takes a token and a slab of its rows: q, then k, then v.
+// A token's rows: q, then k, then v. The tokens' places are looked up by the warp's lanes at once.
 template <typename T, int FMT, int MODE>
-__global__ void __launch_bounds__(kRowThreads, 5)   // its quotients take more registers than the other row kernels
+__global__ void __launch_bounds__(kRowThreads, kAppendBlocks)
     append_kernel(const __grid_constant__ lacache_rope rope, const __grid_constant__ AppendArgs a) {
   using Stored = typename std::conditional<FMT == LACACHE_KV_F16, __half, __nv_bfloat16>::type;
   constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
   __shared__ float2 cs[kRowThreads / 32][kMaxHeadDim / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int pass = 32 / a.lanes, sub = lane / a.lanes;
+  const int pass = 32 / a.lanes, sub = lane / a.lanes, kv = a.q_heads + a.kv_heads;
   const Chunks m = chunks_of<MODE>(lane & (a.lanes - 1), a.chunks, rope.rot_dim);
-  const int kv = a.q_heads + a.kv_heads, rows = kv + a.kv_heads, slabs = (rows + a.slab - 1) / a.slab;
   const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
-  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.tasks; task += step) {
-    const int64_t t = task / slabs;
-    const int first = (int)(task - t * slabs) * a.slab;
-    const int end = first + a.slab < rows ? first + a.slab : rows;
-    const int64_t place =
-        slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages, lane == 0 ? a.status : nullptr);
-    if (place < 0) continue;
-    float2 angle[8];
-    if (MODE != kRopeNone) warp_angles<MODE>(rope, a.rope_pos[t], 1.f, m, cs[warp], angle);
-    for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
-      typename Chunk<T>::raw raw[kRowUnroll][2];
-      const unsigned char* src[kRowUnroll];
+  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.plan.tasks; task += step) {
+    const int64_t first_token = task / a.plan.slabs * a.plan.group;
+    const int first = (int)(task % a.plan.slabs) * a.plan.slab;
+    const int end = first + a.plan.slab < a.plan.rows ? first + a.plan.slab : a.plan.rows;
+    const int tokens = a.plan.n - first_token < a.plan.group ? (int)(a.plan.n - first_token) : a.plan.group;
+    int64_t own_place = -1;
+    int own_pos = 0;
+    if (lane < tokens) {
+      const int64_t t = first_token + lane;
+      if (MODE != kRopeNone) own_pos = a.rope_pos[t];
+      own_place = slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages, a.status);
+    }
+    for (int g = 0; g < tokens; ++g) {
+      const int64_t t = first_token + g, place = __shfl_sync(0xffffffffu, own_place, g);
+      if (place < 0) continue;
+      float2 angle[8];
+      if (MODE != kRopeNone) warp_angles<MODE>(rope, __shfl_sync(0xffffffffu, own_pos, g), 1.f, m, cs[warp], angle);
+      // where row r would lie if q, k and v each began at row 0
+      const unsigned char* from_q = a.q.at(t, 0);
+      const unsigned char* from_k = a.k.at(t, -a.q_heads);
+      const unsigned char* from_v = a.v.at(t, -kv);
+      const int64_t at_k = cached_at<FMT>(place, a.chunks);
+      for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
+        typename Chunk<T>::raw raw[kRowUnroll][2];
+        const unsigned char* src[kRowUnroll];
 #pragma unroll
-      for (int i = 0; i < kRowUnroll; ++i) {
-        const int r = r0 + i * pass + sub;
-        src[i] = r < a.q_heads ? a.q.p + t * a.q.token + r * a.q.head
-                 : r < kv      ? a.k.p + t * a.k.token + (r - a.q_heads) * a.k.head
-                               : a.v.p + t * a.v.token + (r - kv) * a.v.head;
+        for (int i = 0; i < kRowUnroll; ++i) {
+          const int r = r0 + i * pass + sub;
+          src[i] = (r < a.q_heads ? from_q : r < kv ? from_k : from_v) +
+                   (int64_t)r * (r < a.q_heads ? a.q.head16 : r < kv ? a.k.head16 : a.v.head16) * 16;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          raw[i][k] = {};
-          if (r < end && m.live[k]) raw[i][k] = Chunk<T>::load(src[i] + m.c[k] * (8 * (int)sizeof(T)));
+          for (int k = 0; k < 2; ++k) {
+            raw[i][k] = {};
+            if (r < end && m.live[k]) raw[i][k] = Chunk<T>::load(src[i] + m.c[k] * (8 * (int)sizeof(T)));
+          }
         }
-      }
 #pragma unroll
-      for (int i = 0; i < kRowUnroll; ++i) {
-        const int at = r0 + i * pass, r = at + sub;
-        if (at >= end) break;
-        float x0[8], x1[8];
-        Chunk<T>::widen(raw[i][0], x0);
-        Chunk<T>::widen(raw[i][1], x1);
-        if (MODE != kRopeNone) {
-          if (r < kv) rotate<MODE>(x0, x1, m, rope.rot_dim, angle, cs[warp], r < end ? reinterpret_cast<const T*>(src[i]) : nullptr);
-          if (MODE == kRopeOdd) __syncwarp();
-        }
-        const bool live[2] = {r < end && m.live[0], r < end && m.live[1]};
-        if (r < a.q_heads) {
-          T* to = reinterpret_cast<T*>(a.q_out.p + t * a.q_out.token + r * a.q_out.head);
-          if (live[0]) store8(to + m.c[0] * 8, x0);
-          if (live[1]) store8(to + m.c[1] * 8, x1);
-        }
-        if (at + pass <= a.q_heads) continue;   // no row of k or v in this pass
-        const bool is_v = r >= kv, cached = r >= a.q_heads;
-        const int64_t row = place + (int64_t)(is_v ? r - kv : cached ? r - a.q_heads : 0) * a.page_size;
-        unsigned char* to = static_cast<unsigned char*>(is_v ? a.pv : a.pk) + cached_at<FMT>(row, a.chunks);
-        if constexpr (kEight) {
-          const float scale = row_scale<FMT>(x0, x1, a.lanes), inv = __frcp_rn(scale);
-          if (cached && live[0]) reinterpret_cast<uint2*>(to)[m.c[0]] = quantise8<FMT>(x0, scale, inv);
-          if (cached && live[1]) reinterpret_cast<uint2*>(to)[m.c[1]] = quantise8<FMT>(x1, scale, inv);
-          if (cached && live[0] && m.c[0] == 0) (is_v ? a.vs : a.ks)[row] = scale;
-        } else {
-          if (cached && live[0]) store8(reinterpret_cast<Stored*>(to) + m.c[0] * 8, x0);
-          if (cached && live[1]) store8(reinterpret_cast<Stored*>(to) + m.c[1] * 8, x1);
+        for (int i = 0; i < kRowUnroll; ++i) {
+          const int at = r0 + i * pass, r = at + sub;
+          if (at >= end) break;
+          float x0[8], x1[8];
+          Chunk<T>::widen(raw[i][0], x0);
+          Chunk<T>::widen(raw[i][1], x1);
+          if (MODE != kRopeNone) {
+            if (r < kv)
+              rotate<MODE>(x0, x1, m, rope.rot_dim, rope.layout, angle, cs[warp],
+                           r < end ? reinterpret_cast<const T*>(src[i]) : nullptr);
+            if (MODE == kRopeOdd) __syncwarp();
+          }
+          const bool live[2] = {r < end && m.live[0], r < end && m.live[1]};
+          if (r < a.q_heads) {
+            T* to = reinterpret_cast<T*>(a.q_out.at(t, r));
+            if (live[0]) store8(to + m.c[0] * 8, x0);
+            if (live[1]) store8(to + m.c[1] * 8, x1);
+          }
+          if (at + pass <= a.q_heads) continue;   // no row of k or v in this pass
+          const bool is_v = r >= kv, cached = r >= a.q_heads;
+          const int h = is_v ? r - kv : cached ? r - a.q_heads : 0;
+          unsigned char* to = (is_v ? a.pv : a.pk) + at_k + h * a.head_bytes;
+          if constexpr (kEight) {
+            const float scale = row_scale<FMT>(x0, x1, a.lanes), inv = __frcp_rn(scale);
+            if (cached && live[0]) reinterpret_cast<uint2*>(to)[m.c[0]] = quantise8<FMT>(x0, scale, inv);
+            if (cached && live[1]) reinterpret_cast<uint2*>(to)[m.c[1]] = quantise8<FMT>(x1, scale, inv);
+            if (cached && live[0] && m.c[0] == 0) (is_v ? a.vs : a.ks)[place + (int64_t)h * a.page_size] = scale;
+          } else {
+            if (cached && live[0]) store8(reinterpret_cast<Stored*>(to) + m.c[0] * 8, x0);
+            if (cached && live[1]) store8(reinterpret_cast<Stored*>(to) + m.c[1] * 8, x1);
+          }
         }
       }
     }
@@ -105,66 +123,70 @@ __global__ void __launch_bounds__(kRowThreads, 5)   // its quotients take more r
 }
 
 struct ReadArgs {
+  RowPlan plan;
   const int32_t* seq;
   const int32_t* pos;
   Table table;
-  int kv_heads, chunks, lanes, page_size, slab;
-  int64_t tasks;
+  int kv_heads, chunks, lanes, page_size;
   int64_t pages;
   Rows k, v;   // p == nullptr: not wanted
-  const void* pk;
-  const void* pv;
+  const unsigned char* pk;
+  const unsigned char* pv;
   const float* ks;
   const float* vs;
   unsigned int* status;
 };
 
-// As append_kernel: a warp takes a token and a slab of its rows, k, then v.
+// A token's rows: k, then v.
 template <typename T, int FMT>
-__global__ void __launch_bounds__(kRowThreads, kRowBlocks) read_kernel(const __grid_constant__ ReadArgs a) {
+__global__ void __launch_bounds__(kRowThreads, kReadBlocks) read_kernel(const __grid_constant__ ReadArgs a) {
   using Stored = typename std::conditional<FMT == LACACHE_KV_F16, __half, __nv_bfloat16>::type;
   constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
+  using Raw = typename std::conditional<kEight, uint2, uint4>::type;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int pass = 32 / a.lanes, sub = lane / a.lanes;
   const Chunks m = chunks_of<kRopeNone>(lane & (a.lanes - 1), a.chunks, 0);
-  const int rows = 2 * a.kv_heads, slabs = (rows + a.slab - 1) / a.slab;
   const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
-  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.tasks; task += step) {
-    const int64_t t = task / slabs;
-    const int first = (int)(task - t * slabs) * a.slab;
-    const int end = first + a.slab < rows ? first + a.slab : rows;
-    const int64_t place =
-        slot_row(a.table, a.seq[t], a.pos[t], a.kv_heads, a.page_size, a.pages, lane == 0 ? a.status : nullptr);
-    if (place < 0) continue;
-    for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
-      typename std::conditional<kEight, uint2, uint4>::type raw[kRowUnroll][2];
-      float scale[kRowUnroll];
+  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < a.plan.tasks; task += step) {
+    const int64_t first_token = task / a.plan.slabs * a.plan.group;
+    const int first = (int)(task % a.plan.slabs) * a.plan.slab;
+    const int end = first + a.plan.slab < a.plan.rows ? first + a.plan.slab : a.plan.rows;
+    const int tokens = a.plan.n - first_token < a.plan.group ? (int)(a.plan.n - first_token) : a.plan.group;
+    int64_t own_place = -1;
+    if (lane < tokens)
+      own_place = slot_row(a.table, a.seq[first_token + lane], a.pos[first_token + lane], a.kv_heads, a.page_size, a.pages,
+                           a.status);
+    for (int g = 0; g < tokens; ++g) {
+      const int64_t t = first_token + g, place = __shfl_sync(0xffffffffu, own_place, g);
+      if (place < 0) continue;
+      for (int r0 = first; r0 < end; r0 += kRowUnroll * pass) {
+        Raw raw[kRowUnroll][2];
+        float scale[kRowUnroll];
 #pragma unroll
-      for (int i = 0; i < kRowUnroll; ++i) {
-        const int r = r0 + i * pass + sub;
-        const bool is_v = r >= a.kv_heads;
-        if (r >= end || !m.live[0] || !(is_v ? a.v.p : a.k.p)) continue;
-        const int64_t at = place + (int64_t)(is_v ? r - a.kv_heads : r) * a.page_size;
-        const unsigned char* p = static_cast<const unsigned char*>(is_v ? a.pv : a.pk) + cached_at<FMT>(at, a.chunks);
-        const auto* from = reinterpret_cast<const typename std::conditional<kEight, uint2, uint4>::type*>(p);
-        raw[i][0] = from[m.c[0]];
-        if (m.live[1]) raw[i][1] = from[m.c[1]];
-        if constexpr (kEight) scale[i] = (is_v ? a.vs : a.ks)[at];
-      }
+        for (int i = 0; i < kRowUnroll; ++i) {
+          const int r = r0 + i * pass + sub;
+          const bool is_v = r >= a.kv_heads;
+          if (r >= end || !m.live[0] || !(is_v ? a.v.p : a.k.p)) continue;
+          const int64_t at = place + (int64_t)(is_v ? r - a.kv_heads : r) * a.page_size;
+          const Raw* from = reinterpret_cast<const Raw*>((is_v ? a.pv : a.pk) + cached_at<FMT>(at, a.chunks));
+          raw[i][0] = from[m.c[0]];
+          if (m.live[1]) raw[i][1] = from[m.c[1]];
+          if constexpr (kEight) scale[i] = (is_v ? a.vs : a.ks)[at];
+        }
 #pragma unroll
-      for (int i = 0; i < kRowUnroll; ++i) {
-        const int r = r0 + i * pass + sub;
-        const bool is_v = r >= a.kv_heads;
-        const Rows& dst = is_v ? a.v : a.k;
-        if (r >= end || !dst.p) continue;
-        T* to = reinterpret_cast<T*>(dst.p + t * dst.token + (is_v ? r - a.kv_heads : r) * dst.head);
+        for (int i = 0; i < kRowUnroll; ++i) {
+          const int r = r0 + i * pass + sub;
+          const bool is_v = r >= a.kv_heads;
+          if (r >= end || !(is_v ? a.v.p : a.k.p)) continue;
+          T* to = reinterpret_cast<T*>(is_v ? a.v.at(t, r - a.kv_heads) : a.k.at(t, r));
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (!m.live[k]) continue;
-          float x[8];
-          if constexpr (kEight) dequantise8<FMT>(raw[i][k], scale[i], x);
-          else widen8(raw[i][k], x, Stored());
-          store8(to + m.c[k] * 8, x);
+          for (int k = 0; k < 2; ++k) {
+            if (!m.live[k]) continue;
+            float x[8];
+            if constexpr (kEight) dequantise8<FMT>(raw[i][k], scale[i], x);
+            else widen8(raw[i][k], x, Stored());
+            store8(to + m.c[k] * 8, x);
+          }
         }
       }
     }
@@ -302,19 +324,18 @@ extern "C" lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, cons
   a.chunks = h->cfg.head_dim / 8;
   a.page_size = h->cfg.page_size;
   a.pages = h->cfg.pages;
+  a.head_bytes = (int64_t)h->cfg.page_size * h->cfg.head_dim * (lc::is_quantised(h->cfg.format) ? 1 : 2);
   const int mode = lc::rope_mode(rope);
   a.lanes = lc::lanes_for(h->cfg.head_dim, rope ? rope->rot_dim : 0, mode);
-  a.pk = pool.k;
-  a.pv = pool.v;
+  a.pk = static_cast<unsigned char*>(pool.k);
+  a.pv = static_cast<unsigned char*>(pool.v);
   a.ks = pool.k_scale;
   a.vs = pool.v_scale;
   a.status = h->dev_status;
   static const lacache_rope none = {};
   const lacache_rope& plan = rope ? *rope : none;
-  const lc::RowPlan rp = lc::plan_rows(n, a.q_heads + 2 * a.kv_heads, a.lanes);
-  a.slab = rp.slab;
-  a.tasks = rp.tasks;
-  const unsigned grid = rp.blocks;
+  unsigned grid;
+  a.plan = lc::plan_rows(n, a.q_heads + 2 * a.kv_heads, a.lanes, lc::kAppendBlocks, lc::kRowGroup, &grid);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   if (dtype == LACACHE_BF16) lc::launch_append<__nv_bfloat16>(h->cfg.format, mode, plan, a, grid, st);
   else if (dtype == LACACHE_F16) lc::launch_append<__half>(h->cfg.format, mode, plan, a, grid, st);
@@ -343,15 +364,13 @@ extern "C" lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const 
   a.lanes = lc::lanes_for(h->cfg.head_dim, 0, lc::kRopeNone);
   a.page_size = h->cfg.page_size;
   a.pages = h->cfg.pages;
-  a.pk = pool.k;
-  a.pv = pool.v;
+  a.pk = static_cast<unsigned char*>(pool.k);
+  a.pv = static_cast<unsigned char*>(pool.v);
   a.ks = pool.k_scale;
   a.vs = pool.v_scale;
   a.status = h->dev_status;
-  const lc::RowPlan rp = lc::plan_rows(n, 2 * a.kv_heads, a.lanes);
-  a.slab = rp.slab;
-  a.tasks = rp.tasks;
-  const unsigned grid = rp.blocks;
+  unsigned grid;
+  a.plan = lc::plan_rows(n, 2 * a.kv_heads, a.lanes, lc::kReadBlocks, lc::kRowGroup, &grid);
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   if (dtype == LACACHE_BF16) lc::launch_read<__nv_bfloat16>(h->cfg.format, a, grid, st);
   else if (dtype == LACACHE_F16) lc::launch_read<__half>(h->cfg.format, a, grid, st);

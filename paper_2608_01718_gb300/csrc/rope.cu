@@ -1,7 +1,7 @@
 // Rotary positions of rows of heads, and their gradient (the rotation by the negated angles).
 //
-// Bound by memory: each element is read and written once. A warp takes a token, computes its angles once, holds those of its
-// lanes' chunks in registers, and runs over the heads. The plan (rotations as fractions of 2^64 a position) is a kernel argument.
+// Bound by memory: each element is read and written once. For each of its tokens a warp computes the angles once, holds those
+// of its lanes' chunks in registers, and runs over the heads. The plan (rotations as fractions of 2^64 a position) is a kernel argument.
 #include <math.h>
 
 #include "decode.cuh"
@@ -9,45 +9,53 @@
 namespace lc {
 namespace {
 
+// Blocks an SM, and passes in flight: four of 16-bit rows (16,384 x 32 x 128 of bf16: two, at eight blocks an SM, 48 us; four
+// 43.6); two where a lane's rows or partners take twice the registers.
+constexpr int kRopeBlocks = 5;
+
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kRowThreads, kRowBlocks)
-    rope_kernel(const __grid_constant__ lacache_rope rope, int64_t tasks, int slab, int heads, int chunks, int lanes, Rows x,
-                const int32_t* __restrict__ pos, float sign, Rows y) {
+__global__ void __launch_bounds__(kRowThreads, kRopeBlocks)
+    rope_kernel(const __grid_constant__ lacache_rope rope, const __grid_constant__ RowPlan plan, int chunks, int lanes,
+                const __grid_constant__ Rows x, const int32_t* __restrict__ pos, float sign, const __grid_constant__ Rows y) {
+  constexpr int kUnroll = sizeof(T) == 4 || MODE == kRopeOdd ? 2 : 4;
   __shared__ float2 cs[kRowThreads / 32][kMaxHeadDim / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int pass = 32 / lanes, sub = lane / lanes;
   const Chunks m = chunks_of<MODE>(lane & (lanes - 1), chunks, rope.rot_dim);
-  const int slabs = (heads + slab - 1) / slab;
   const int64_t step = (int64_t)gridDim.x * (kRowThreads / 32);
-  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < tasks; task += step) {
-    const int64_t t = task / slabs;
-    const int first = (int)(task - t * slabs) * slab;
-    const int end = first + slab < heads ? first + slab : heads;
-    const unsigned char* src = x.p + t * x.token;
-    unsigned char* dst = y.p + t * y.token;
+  for (int64_t task = blockIdx.x * (int64_t)(kRowThreads / 32) + warp; task < plan.tasks; task += step) {
+    const int64_t t = task / plan.slabs;
+    const int first = (int)(task - t * plan.slabs) * plan.slab;
+    const int end = first + plan.slab < plan.rows ? first + plan.slab : plan.rows;
+    const unsigned char* src = x.at(t, first + sub);
+    unsigned char* dst = y.at(t, first + sub);
+    const int64_t src_step = (int64_t)pass * x.head16 * 16, dst_step = (int64_t)pass * y.head16 * 16;
     float2 a[8];
     warp_angles<MODE>(rope, pos[t], sign, m, cs[warp], a);
-    for (int h0 = first; h0 < end; h0 += kRowUnroll * pass) {
-      typename Chunk<T>::raw raw[kRowUnroll][2];
+    for (int h = first + sub; h - sub < end; h += kUnroll * pass) {
+      typename Chunk<T>::raw raw[kUnroll][2];
 #pragma unroll
-      for (int i = 0; i < kRowUnroll; ++i) {
-        const int h = h0 + i * pass + sub;
+      for (int i = 0; i < kUnroll; ++i) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          if (h < end && m.live[k]) raw[i][k] = Chunk<T>::load(src + h * x.head + m.c[k] * (8 * (int)sizeof(T)));
+          if (h + i * pass < end && m.live[k])
+            raw[i][k] = Chunk<T>::load(src + i * src_step + m.c[k] * (8 * (int)sizeof(T)));
       }
 #pragma unroll
-      for (int i = 0; i < kRowUnroll; ++i) {
-        const int h = h0 + i * pass + sub;
+      for (int i = 0; i < kUnroll; ++i) {
+        const bool live = h + i * pass < end;
         float v0[8], v1[8];
         Chunk<T>::widen(raw[i][0], v0);
         Chunk<T>::widen(raw[i][1], v1);
-        rotate<MODE>(v0, v1, m, rope.rot_dim, a, cs[warp], h < end ? reinterpret_cast<const T*>(src + h * x.head) : nullptr);
+        rotate<MODE>(v0, v1, m, rope.rot_dim, rope.layout, a, cs[warp],
+                     live ? reinterpret_cast<const T*>(src + i * src_step) : nullptr);
         if (MODE == kRopeOdd) __syncwarp();
-        T* to = reinterpret_cast<T*>(dst + h * y.head);
-        if (h < end && m.live[0]) store8(to + m.c[0] * 8, v0);
-        if (h < end && m.live[1]) store8(to + m.c[1] * 8, v1);
+        T* to = reinterpret_cast<T*>(dst + i * dst_step);
+        if (live && m.live[0]) store8(to + m.c[0] * 8, v0);
+        if (live && m.live[1]) store8(to + m.c[1] * 8, v1);
       }
+      src += kUnroll * src_step;
+      dst += kUnroll * dst_step;
     }
   }
 }
@@ -56,11 +64,12 @@ template <typename T>
 void launch_rope(int mode, const lacache_rope& rope, int64_t n, int heads, int head_dim, const Rows& x, const int32_t* pos,
                  float sign, const Rows& y, cudaStream_t st) {
   const int lanes = lanes_for(head_dim, rope.rot_dim, mode);
-  const RowPlan plan = plan_rows(n, heads, lanes);
+  unsigned grid;
+  const RowPlan plan = plan_rows(n, heads, lanes, kRopeBlocks, 1, &grid);
   auto* kernel = mode == kRopeHalf   ? rope_kernel<T, kRopeHalf>
                  : mode == kRopeNear ? rope_kernel<T, kRopeNear>
                                      : rope_kernel<T, kRopeOdd>;
-  kernel<<<plan.blocks, kRowThreads, 0, st>>>(rope, plan.tasks, plan.slab, heads, head_dim / 8, lanes, x, pos, sign, y);
+  kernel<<<grid, kRowThreads, 0, st>>>(rope, plan, head_dim / 8, lanes, x, pos, sign, y);
 }
 
 }  // namespace
