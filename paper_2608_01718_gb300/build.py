@@ -26,7 +26,8 @@ PEAKS_SOURCE = "peaks.cu"
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "stage1_stream.cu", "stage1_tensor.cu", "stage2.cu", "noalloc.cu", "calibrate.cu", "lsh.cu",
            "lsh_tc.cu", "speculative.cu", "shards.cu", "rope.cu", "kv_cache.cu",
-           "kv_attend.cu", "kv_attend_bf16.cu", "kv_attend_f16.cu", "kv_attend_e4m3.cu", "kv_attend_int8.cu"]
+           "kv_attend.cu", "kv_attend_bf16.cu", "kv_attend_f16.cu", "kv_attend_e4m3.cu", "kv_attend_int8.cu",
+           "kv_attend_tc.cu"]
 
 
 def nvcc() -> str:

@@ -25,12 +25,13 @@ struct lacache_kv {
   float* vs;
   float* partial;            // the attention's partial sums, two slots a block
   unsigned int* arrived;     // its counters, one a block (each launch leaves them zero)
-  unsigned int* dev_status;  // kBadIndex once a kernel met an index outside its range
+  unsigned int* dev_status;  // kBadIndex: a kernel met an index outside its range; kAttendTimeout: a bounded wait ran out
 };
 
 namespace lc {
 
-constexpr unsigned int kBadIndex = 1u;
+// Bits of a cache's status word.
+constexpr unsigned int kBadIndex = 1u, kAttendTimeout = 2u;
 constexpr int kMaxHeadDim = LACACHE_MAX_HEAD_DIM;
 constexpr int kMaxNewTokens = 512;
 

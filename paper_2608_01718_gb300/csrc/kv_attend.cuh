@@ -53,6 +53,7 @@ struct AttendArgs {
   int parts;            // blocks the units may be split over (at most the grid)
   int max_len;          // positions the table can name
   int device;
+  int tile_rows, padded;   // the tcgen05 kernel: rows of a tile, and floats of a row of a partial slot
   int64_t pages;
   int64_t page_rows;    // rows of a page: kv_heads x page_size ...
   int64_t page_bytes;   // ... and their bytes
@@ -87,6 +88,9 @@ cudaError_t launch_attend_bf16(const AttendArgs& a, int num_sms, cudaStream_t st
 cudaError_t launch_attend_f16(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
+// The tcgen05 kernel for many rows (kv_attend_tc.cu): 16-bit caches with heads of up to 128.
+constexpr int kTcRows = 32;   // from more rows than this
+cudaError_t launch_attend_tc(const AttendArgs& a, bool bf16, int num_sms, cudaStream_t st);
 
 namespace {
 

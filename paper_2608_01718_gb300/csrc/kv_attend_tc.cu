@@ -1,0 +1,697 @@
+// Attention over a 16-bit cache for many rows a kv head (a window of drafts under verification times a group of heads):
+// the products on tcgen05.
+//
+// From some tens of rows on, 4 x rows flops a cached element are more than the warp-level tensor instruction sustains at the
+// rate of HBM, and a tile of 32 rows reads the cache several times. Here a tile is 128 rows of q:
+//   S [128 rows x 128 keys] = Q [128 x d] K^T,   O [128 x d] += P [128 x 128 keys] V
+// with S, P and O in TMEM and q, K and V in shared memory. A thread of the softmax owns a row: its maximum, sum, masks and
+// rescaling need no other thread. At 128 rows and d = 128 a tile of keys takes 0.3 us of tensor time and about as much of
+// exponentials against 1.5 us for its 64 KB at an SM's share of HBM, so the kernel is bound by reading the cache.
+//
+// One block an SM, warp-specialised:
+//   warps 5-7 (loaders): the tiles of K and V, in turn, into a ring of six 32 KB slots in the 128-byte swizzle layout, by
+//     cp.async (whole 16-byte units of rows found through the page table; masked and missing positions are zeros), and with
+//     a triple's first tile its q;
+//   warp 4 (MMA): S of tile j into one of two accumulators, then O += P V of tile j - 1;
+//   warps 0-3 (softmax, a row a thread): S from TMEM, base-2 softmax with a maximum that moves only by more than 2^8 (as in
+//     kv_attend.cuh), weights to TMEM as the A operand of the second product; for a bf16 cache in two terms, which the
+//     product sums (one would add an error as large as the output's rounding).
+// K is the first product's B operand as stored (K-major); V, as stored, the second's with its dimensions contiguous
+// (MN-major), so neither is transposed. Work is cut and joined as in kv_attend.cuh, in units of 128 keys.
+//
+// An output that is not finite is computed again key by key: a masked key's value times a zero weight, or an infinity times
+// a weight's second term, may have made it so.
+//
+// Every wait is bounded (about a second): past it the block records a timeout, its roles stop, copies and products in flight
+// are drained, TMEM is freed and the block ends; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
+#include "kv_attend.cuh"
+#include "tcgen05.cuh"
+
+namespace lc {
+namespace {
+
+constexpr int kTile = 128;                   // rows of q, and keys, a tile
+constexpr int kSlots = 6;
+constexpr int kAhead = 4;                    // slots whose copies are in flight
+constexpr int kBlockBytes = kTile * 128;     // 64 elements of 128 rows
+constexpr int kSlotBytes = 2 * kBlockBytes;
+constexpr int kMmaWarp = 4;
+constexpr int kLoaders = 96;                 // (eight warps in all: 255 registers a thread)
+constexpr int kThreads = 128 + 32 + kLoaders;
+constexpr int kCost = 2;                     // a triple's start and end, in units
+constexpr uint32_t kS = 0, kO = 256, kP = 384;   // TMEM columns: two S, O, P (two terms of 64)
+
+struct Tail {
+  uint64_t full[kSlots], empty[kSlots];      // a slot's copies have landed; its products are done
+  uint64_t s_full[2], s_empty[2];            // an S is complete; has been read
+  uint64_t p_full, pv_done;                  // the weights are stored; their product is done
+  uint64_t q_empty, o_empty;                 // q has been used for the last time; O has been read
+  uint64_t drain;
+  uint32_t tmem;
+  uint32_t abort_flag;
+  uint32_t bad[16];                          // a unit's 16-key tiles whose page id is no page (by unit modulo 16)
+  int pending[2][4];                         // shared triples, as in kv_attend.cuh
+};
+constexpr int kSmem = 1024 + kSlotBytes + kSlots * kSlotBytes + (int)sizeof(Tail);
+static_assert(kSmem <= 227 * 1024, "shared memory");
+
+// Where 16-byte unit u of row r lies in a tile of 128 rows: blocks of 64 elements, 128-byte swizzle.
+__device__ __forceinline__ uint32_t unit_at(int r, int u) {
+  return (uint32_t)((u >> 3) * kBlockBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4));
+}
+
+// An MN-major operand in the 128-byte swizzle layout: 64 elements a row of 128 B, 8 rows 1024 B apart along K (stride byte
+// offset), blocks of 64 elements kBlockBytes apart along N (leading byte offset).
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
+  uint64_t desc = (uint64_t)((addr >> 4) & 0x3FFFu);
+  desc |= (uint64_t)(kBlockBytes >> 4) << 16;
+  desc |= (uint64_t)(1024 >> 4) << 32;
+  desc |= (uint64_t)1 << 46;
+  desc |= (uint64_t)2 << 61;
+  return desc;
+}
+// D += A B with A in shared memory, and with A in TMEM (lane = row, two elements a column).
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// This block's part of the line of cells: triples in order, each with its first unit and how many units are the block's.
+struct Walk {
+  int seq, seq_base, triple, first_unit, left;   // left: cells, this triple's units first
+  int per_seq;
+  Span sp;
+  __device__ __forceinline__ int units() const { return min(sp.units - first_unit, left); }
+  __device__ __forceinline__ bool done() const { return left <= 0; }
+  __device__ __forceinline__ void next(const AttendArgs& a) {
+    const int n = units();
+    left -= n;
+    if (first_unit + n == sp.units) left -= kCost;
+    first_unit = 0;
+    if (left > 0 && ++triple == per_seq) {
+      triple = 0;
+      seq_base += (sp.units + kCost) * per_seq;
+      seq = min(seq + 1, a.table.seqs - 1);
+      sp = span_of(a, seq, kTile);
+    }
+  }
+};
+struct Line {
+  int share, longer;
+  __device__ __forceinline__ int block_of(int cell) const {
+    const int in_longer = longer * (share + 1);
+    return cell < in_longer ? cell / (share + 1) : longer + (cell - in_longer) / share;
+  }
+};
+// By a whole warp. false: this block has no part.
+__device__ bool start_walk(const AttendArgs& a, Walk& w, Line& line) {
+  const int lane = threadIdx.x & 31, block = blockIdx.x;
+  w.per_seq = a.kv_heads * a.row_tiles;
+  int total = 0;
+  for (int s = lane; s < a.table.seqs; s += 32) total += span_of(a, s, kTile).units + kCost;
+  total = __reduce_add_sync(0xffffffffu, total) * w.per_seq;
+  const int parts = min(total, a.parts);
+  if (block >= parts) return false;
+  line.share = total / parts;
+  line.longer = total - line.share * parts;
+  const int u = block * line.share + min(block, line.longer);
+  w.seq = w.seq_base = 0;
+  for (int s0 = 0; s0 < a.table.seqs; s0 += 32) {
+    const int own = s0 + lane < a.table.seqs ? (span_of(a, s0 + lane, kTile).units + kCost) * w.per_seq : 0;
+    int upto = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, w.seq_base + upto > u);
+    if (past) {
+      const int l0 = __ffs(past) - 1;
+      w.seq = s0 + l0;
+      w.seq_base += __shfl_sync(0xffffffffu, upto - own, l0);
+      break;
+    }
+    w.seq_base += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  w.sp = span_of(a, w.seq, kTile);
+  w.triple = (u - w.seq_base) / (w.sp.units + kCost);
+  w.first_unit = u - w.seq_base - w.triple * (w.sp.units + kCost) - kCost;
+  w.left = line.share + (block < line.longer ? 1 : 0);
+  if (w.first_unit < 0) {
+    w.left += w.first_unit;
+    w.first_unit = 0;
+  }
+  return true;
+}
+
+// Four neighbouring dimensions of an output row.
+__device__ __forceinline__ void write4(const AttendArgs& a, int64_t at_row, int d, float4 y) {
+  *reinterpret_cast<uint2*>(a.out.p + at_row + d * 2) =
+      a.q_f16 ? make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w)) : make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
+}
+
+// One row of one block's keys [from, to), key by key, by a warp: lane i holds dimensions 4 i .. 4 i + 3.
+template <bool BF16>
+__device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, int tok, int qh, int from, int to, float4* acc,
+                                      float* top, float* sum) {
+  const int lane = threadIdx.x & 31, D = a.head_dim;
+  const bool has = lane * 4 < D;
+  auto load4 = [&](const unsigned char* p) {
+    if (!has) return make_float4(0.f, 0.f, 0.f, 0.f);
+    const uint2 u = *reinterpret_cast<const uint2*>(p + lane * 8);
+    if (BF16)
+      return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                         __uint_as_float(u.y & 0xffff0000u));
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
+    return make_float4(x.x, x.y, y.x, y.y);
+  };
+  const float4 q = load4(a.q.at((int64_t)seq * a.new_tokens + tok, qh));
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int j = from; j < to; ++j) {
+    const int index = (int)(((uint64_t)(uint32_t)(j >> 4) * a.page_mul) >> a.page_shift);
+    const int page = a.table.pages[seq * a.table.stride + index];
+    if ((unsigned)page >= (unsigned)a.pages) continue;
+    const int64_t row = page * a.page_rows + (int64_t)head * a.page_size + (j - index * a.page_size);
+    const float4 k = load4(a.pk + row * D * 2), v = load4(a.pv + row * D * 2);
+    float dot = has ? q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w : 0.f;
+#pragma unroll
+    for (int x = 16; x; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
+    const float s = dot * (a.scale * 1.4426950408889634f);
+    const float now = fmaxf(m, s), base = now == -INFINITY ? 0.f : now;
+    const float f = exp2_fast(m - base), p = exp2_fast(s - base);
+    l = l * f + p;
+    o.x = o.x * f + p * v.x, o.y = o.y * f + p * v.y, o.z = o.z * f + p * v.z, o.w = o.w * f + p * v.w;
+    m = now;
+  }
+  *acc = o;
+  *top = m;
+  *sum = l;
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  unsigned char* gbase = smem_raw + (base - raw);
+  const uint32_t q_smem = base, ring = base + kSlotBytes;
+  Tail& t = *reinterpret_cast<Tail*>(gbase + kSlotBytes + kSlots * kSlotBytes);
+  volatile uint32_t* abort_flag = &t.abort_flag;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int D = a.head_dim, row_bytes = D * 2, units_row = D / 8;
+  const int slot_floats = kTile * (a.padded + 2);   // of a.partial
+
+  Walk walk;
+  Line line;
+  if (!start_walk(a, walk, line)) return;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(smem_u32(&t.full[s]), kLoaders);
+      mbar_init(smem_u32(&t.empty[s]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&t.s_full[b]), 1);
+      mbar_init(smem_u32(&t.s_empty[b]), 128);
+    }
+    mbar_init(smem_u32(&t.p_full), 128);
+    mbar_init(smem_u32(&t.pv_done), 1);
+    mbar_init(smem_u32(&t.q_empty), 1);
+    mbar_init(smem_u32(&t.o_empty), 128);
+    mbar_init(smem_u32(&t.drain), 1);
+    t.abort_flag = 0;
+    t.pending[0][2] = t.pending[1][2] = -1;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc<false>(smem_u32(&t.tmem), 512);
+    tmem_relinquish<false>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = t.tmem;
+  auto fail = [&] {
+    *abort_flag = 1u;
+    atomicOr(a.status, kAttendTimeout);
+  };
+  auto wait = [&](uint64_t& bar, uint32_t parity) {   // false (and the block stops) past the bound
+    if (mbar_wait(smem_u32(&bar), parity, abort_flag)) return true;
+    if (!*abort_flag) fail();
+    return false;
+  };
+
+  if (warp > kMmaWarp) {
+    // ---- loaders ----
+    const int me = threadIdx.x - 160;
+    int n = 0, sent = 0;   // slots begun, and handed over
+    int triples = 0, units = 0;
+    bool ok = true;
+    auto hand_over = [&](int upto) {   // slots whose copies have landed
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      for (; sent < upto; ++sent) mbar_arrive(smem_u32(&t.full[sent % kSlots]));
+    };
+    for (; ok && !walk.done(); walk.next(a), ++triples) {
+      const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
+      const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
+      const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
+      const unsigned char* head_k = a.pk + (int64_t)head * a.page_size * row_bytes;
+      const unsigned char* head_v = a.pv + (int64_t)head * a.page_size * row_bytes;
+      int key = (walk.sp.lo & ~15) + walk.first_unit * kTile;
+      // lane i < 8: the page id of a unit's 16-key tile i, one unit ahead
+      auto look_up = [&](int from) {
+        const int at = from + (lane & 7) * 16;
+        return at < walk.sp.hi ? __ldg(table_row + (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift)) : -1;
+      };
+      int ids = look_up(key);
+      for (int i = 0; ok && i < count; ++i, key += kTile, ++units) {
+        const int next_ids = i + 1 < count ? look_up(key + kTile) : -1;
+        const bool wrong = key + (lane & 7) * 16 < walk.sp.hi && (unsigned)ids >= (unsigned)a.pages;
+        const unsigned bad = __ballot_sync(0xffffffffu, wrong) & 0xffu;
+        if (bad && me == 0) atomicOr(a.status, kBadIndex);
+        if (me == 0) t.bad[units & 15] = bad;
+        const int live_keys = walk.sp.hi - key, dead_keys = walk.sp.lo - key;   // keys [dead, live) of the tile are read
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv, ++n) {
+          if (n >= kSlots) ok = wait(t.empty[n % kSlots], (n / kSlots - 1) & 1);
+          if (!__all_sync(0xffffffffu, ok)) {
+            ok = false;
+            break;
+          }
+          if (kv == 0 && i == 0) {
+            // q of the triple, once its predecessor's last product with q is done (which needs all the copies so far)
+            if (triples) {
+              copy_wait<0>();
+              hand_over(n);
+              ok = wait(t.q_empty, (triples - 1) & 1);
+            }
+            if (!__all_sync(0xffffffffu, ok)) {
+              ok = false;
+              break;
+            }
+            for (int x = me; x < kTile * units_row; x += kLoaders) {
+              const int r = x / units_row, u = x - r * units_row, row = row0 + r, tok = row / a.group;
+              const bool in = r < live;
+              copy_async<16>(q_smem + unit_at(r, u),
+                             in ? a.q.at((int64_t)walk.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) + u * 16
+                                : a.pk, in);
+            }
+          }
+          const uint32_t dst = ring + (n % kSlots) * kSlotBytes;
+          const unsigned char* from = kv ? head_v : head_k;
+          for (int x = me; x < kTile * units_row; x += kLoaders) {
+            const int j = units_row == 16 ? x >> 4 : x / units_row, u = x - j * units_row;
+            const int page = __shfl_sync(0xffffffffu, ids, j >> 4);   // (warps run this loop whole)
+            const int at = key + (j & ~15);
+            const int slot = at - (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift) * a.page_size + (j & 15);
+            const bool in = j >= dead_keys && j < live_keys && (unsigned)page < (unsigned)a.pages;
+            copy_async<16>(dst + unit_at(j, u), in ? from + page * a.page_bytes + (int64_t)slot * row_bytes + u * 16 : a.pk, in);
+          }
+          copy_commit();
+          copy_wait<kAhead>();
+          if (n >= kAhead) hand_over(n - kAhead + 1);
+        }
+        ids = next_ids;
+      }
+    }
+    copy_wait<0>();
+    if (ok) hand_over(n);
+  } else if (warp == kMmaWarp) {
+    // ---- MMA ----
+    const uint32_t type = BF16 ? (1u << 7) | (1u << 10) : 0u;
+    const uint32_t qk = (1u << 4) | type | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    const uint32_t pv = (1u << 4) | type | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    const uint64_t q_desc = smem_desc(q_smem);
+    int j = 0, triples = 0;    // tiles and triples begun
+    bool ok = true;
+    // O (+)= P V of tile k
+    auto second = [&](int k, bool first_of_triple, int of_triple) {
+      const int v_slot = (2 * k + 1) % kSlots;
+      ok = wait(t.full[v_slot], ((2 * k + 1) / kSlots) & 1) && wait(t.p_full, k & 1) &&
+           (!first_of_triple || of_triple == 0 || wait(t.o_empty, (of_triple - 1) & 1));
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      tc_fence_after();
+      const uint32_t v = ring + v_slot * kSlotBytes;
+      if (elect_one()) {
+#pragma unroll 1
+        for (int kk = 0; kk < kTile / 16; ++kk) {
+          const uint64_t v_desc = smem_desc_mn(v + kk * 2048);
+          mma_ts(tmem + kO, tmem + kP + kk * 8, v_desc, pv, first_of_triple && kk == 0 ? 0u : 1u);
+          if (BF16) mma_ts(tmem + kO, tmem + kP + 64 + kk * 8, v_desc, pv, 1u);
+        }
+        mma_commit<false>(smem_u32(&t.empty[v_slot]), 0);
+        mma_commit<false>(smem_u32(&t.pv_done), 0);
+      }
+      __syncwarp();
+    };
+    for (; ok && !walk.done(); walk.next(a), ++triples) {
+      const int count = walk.units();
+      for (int i = 0; ok && i < count; ++i, ++j) {
+        const int k_slot = (2 * j) % kSlots;
+        ok = wait(t.full[k_slot], ((2 * j) / kSlots) & 1) && (j < 2 || wait(t.s_empty[j & 1], ((j >> 1) - 1) & 1));
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t k_desc = smem_desc(ring + k_slot * kSlotBytes);
+        if (elect_one()) {
+#pragma unroll 1
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t at = (uint64_t)((kk >> 2) * (kBlockBytes >> 4) + (kk & 3) * 2);
+            mma_ss(tmem + kS + (j & 1) * kTile, q_desc + at, k_desc + at, qk, kk ? 1u : 0u);
+          }
+          mma_commit<false>(smem_u32(&t.empty[k_slot]), 0);
+          mma_commit<false>(smem_u32(&t.s_full[j & 1]), 0);
+          if (i + 1 == count) mma_commit<false>(smem_u32(&t.q_empty), 0);
+        }
+        __syncwarp();
+        if (i > 0) second(j - 1, i == 1, triples);
+        if (ok && i + 1 == count) second(j, i == 0, triples);
+      }
+    }
+  } else {
+    // ---- softmax: a row a thread ----
+    const uint32_t lanes = tmem + ((uint32_t)warp << 21);   // this warp's 32 lanes
+    int j = 0;
+    bool ok = true;
+    for (; ok && !walk.done(); walk.next(a)) {
+      const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
+      const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
+      const int r = threadIdx.x, tok = (row0 + r) / a.group;
+      const bool mine = r < live, some = warp * 32 < live;
+      const int pos = mine ? walk.sp.len - a.new_tokens + tok : INT_MAX;
+      int lo = INT_MIN;
+      if (mine) {
+        lo = a.starts ? a.starts[walk.seq] : 0;
+        if (a.window > 0 && pos - a.window + 1 > lo) lo = pos - a.window + 1;
+      }
+      const float factor = a.scale * 1.4426950408889634f;
+      float m = -INFINITY, l = 0.f;
+      const int key_begin = (walk.sp.lo & ~15) + walk.first_unit * kTile;
+      if (threadIdx.x == 0) {
+        const int raw_len = a.lengths[walk.seq];
+        if (raw_len < 0 || raw_len > a.max_len) atomicOr(a.status, kBadIndex);
+      }
+      for (int i = 0; ok && i < count; ++i, ++j) {
+        const int key = key_begin + i * kTile;
+        ok = wait(t.s_full[j & 1], (j >> 1) & 1);
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        if (some) {
+          tc_fence_after();
+          uint32_t u[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32_issue(lanes + kS + (j & 1) * kTile + c * 32, u[c]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32_wait(u[c]);
+          tc_fence_before();
+          mbar_arrive(smem_u32(&t.s_empty[j & 1]));
+          float (&x)[4][32] = reinterpret_cast<float(&)[4][32]>(u);
+          const uint32_t bad = t.bad[j & 15];
+          const bool whole = bad == 0 && key >= lo && key + kTile - 1 <= pos;
+          bool move = false;
+          const bool masked = !__all_sync(0xffffffffu, whole);
+          // scores; masked ones -inf
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[c][e] *= factor;
+          }
+          if (masked) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const int at = key + c * 32 + e;
+                if (at > pos || at < lo || (bad >> (c * 2 + e / 16) & 1)) x[c][e] = -INFINITY;
+              }
+            }
+          }
+          float top = m;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) top = fmaxf(top, x[c][e]);
+          }
+          move = top > m + 8.f;   // (from nothing seen, m = -inf: any finite score)
+          if (m == -INFINITY) move = top != -INFINITY;
+          const float f = move ? exp2_fast(m - top) : 1.f;
+          if (move) {
+            l *= f;
+            m = top;
+          }
+          const float shift = m == -INFINITY ? 0.f : m;
+          // weights, their sum, and their terms
+          float sum[4] = {};
+          uint32_t hi[2][32], lo_term[BF16 ? 2 : 1][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float p0 = exp2_fast(x[c][e] - shift), p1 = exp2_fast(x[c][e + 1] - shift);
+              sum[c] += p0 + p1;
+              const uint32_t h = pack2<BF16>(p0, p1);
+              hi[c >> 1][(c & 1) * 16 + e / 2] = h;
+              if constexpr (BF16)
+                lo_term[c >> 1][(c & 1) * 16 + e / 2] =
+                    pack2<true>(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+            }
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          // the last product has used P, and O may be scaled
+          if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
+          if (!__all_sync(0xffffffffu, ok)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (i > 0 && __any_sync(0xffffffffu, move)) {
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              uint32_t o[32];
+              tmem_ld32_issue(lanes + kO + c, o);
+              tmem_ld32_wait(o);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st32(lanes + kO + c, o);
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            tmem_st32(lanes + kP + c * 32, hi[c]);
+            if constexpr (BF16) tmem_st32(lanes + kP + 64 + c * 32, lo_term[c]);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+        } else {
+          mbar_arrive(smem_u32(&t.s_empty[j & 1]));   // rows past the tile's: their weights are never used
+          if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
+          if (!__all_sync(0xffffffffu, ok)) {
+            ok = false;
+            break;
+          }
+        }
+        mbar_arrive(smem_u32(&t.p_full));
+      }
+      if (!ok) break;
+      // ---- the triple's end: O of this block's keys ----
+      ok = wait(t.pv_done, (j - 1) & 1);
+      if (!__all_sync(0xffffffffu, ok)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const bool whole = count == walk.sp.units;
+      int c_first = blockIdx.x, c_last = blockIdx.x;
+      if (!whole) {
+        const int begin = walk.seq_base + walk.triple * (walk.sp.units + kCost) + kCost;
+        c_first = line.block_of(begin);
+        c_last = line.block_of(begin + walk.sp.units - 1);
+        if (threadIdx.x == 0) {
+          int* p = t.pending[(int)blockIdx.x == c_first];
+          p[0] = walk.seq, p[1] = walk.triple, p[2] = c_first, p[3] = c_last;
+        }
+      }
+      float* slot = a.partial + ((int64_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * slot_floats;
+      if (some) {
+        int64_t at_lse = 0, at_row = 0;
+        if (mine) at_row = out_at(a, walk.seq, head, row0 + r, &at_lse);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bool odd = false;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          float o[32];
+          tmem_ld32(lanes + kO + c, o);
+          const int dims = min(32, D - c);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) odd |= e < dims && !(fabsf(o[e]) <= 3.402823466e+38f);
+          if (mine) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              if (e < dims) {
+                if (whole) write4(a, at_row, c + e, inv == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                               : make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv));
+                else *reinterpret_cast<float4*>(slot + r * a.padded + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              }
+            }
+          }
+        }
+        if (mine) {
+          if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, l);
+          else if (a.lse) a.lse[at_lse] = lse_of(m, l);
+        }
+        // rows that are not finite, again
+        const int key_end = min(key_begin + count * kTile, walk.sp.hi);
+        for (unsigned rows = __ballot_sync(0xffffffffu, mine && odd); rows; rows &= rows - 1) {
+          const int src = __ffs(rows) - 1;
+          const int rr = warp * 32 + src, its_tok = (row0 + rr) / a.group, its_qh = head * a.group + row0 + rr - its_tok * a.group;
+          const int its_pos = __shfl_sync(0xffffffffu, pos, src), its_lo = __shfl_sync(0xffffffffu, lo, src);
+          float4 acc;
+          float top, sum;
+          slow_row<BF16>(a, walk.seq, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1), &acc, &top, &sum);
+          int64_t its_lse;
+          const int64_t its_row = out_at(a, walk.seq, head, row0 + rr, &its_lse);
+          if (lane * 4 < D) {
+            if (whole) {
+              const float g = sum == 0.f ? 0.f : 1.f / sum;
+              write4(a, its_row, lane * 4, sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                      : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g));
+            } else {
+              *reinterpret_cast<float4*>(slot + rr * a.padded + lane * 4) = acc;
+            }
+          }
+          if (lane == 0) {
+            if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + rr * 2) = make_float2(top, sum);
+            else if (a.lse) a.lse[its_lse] = lse_of(top, sum);
+          }
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(smem_u32(&t.o_empty));
+    }
+  }
+
+  // ---- nothing in flight: every product is done (the loaders have waited for their copies); TMEM is freed ----
+  if (warp == kMmaWarp) {
+    if (elect_one()) mma_commit<false>(smem_u32(&t.drain), 0);
+    __syncwarp();
+    mbar_wait(smem_u32(&t.drain), 0, nullptr);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc<false>(tmem, 512);
+  if (*abort_flag) return;
+
+  // ---- shared triples: whichever block arrives last joins the blocks' sums, in their order ----
+  if (threadIdx.x < 2) {
+    int* p = t.pending[threadIdx.x];
+    bool last = false;
+    if (p[2] >= 0) {
+      __threadfence();
+      last = atomicAdd(a.arrived + p[2], 1u) == (unsigned int)(p[3] - p[2]);
+      if (last) a.arrived[p[2]] = 0u;
+      __threadfence();
+    }
+    if (!last) p[2] = -1;
+  }
+  __syncthreads();
+  float* joint_top = reinterpret_cast<float*>(gbase);   // [2][kTile] each, in q's place
+  float* joint_inv = joint_top + 2 * kTile;
+  int64_t* joint_out = reinterpret_cast<int64_t*>(joint_inv + 2 * kTile);
+  auto part = [&](int k, int i) { return a.partial + ((int64_t)(t.pending[k][2] + i) * 2 + (i == 0 ? 1 : 0)) * slot_floats; };
+  auto part_ml = [&](int k, int i, int r) { return __ldcg(reinterpret_cast<const float2*>(part(k, i) + kTile * a.padded) + r); };
+  auto rows_of = [&](int k) {
+    return t.pending[k][2] < 0 ? 0 : min(a.rows - t.pending[k][1] % a.row_tiles * a.tile_rows, a.tile_rows);
+  };
+  const int rows0 = rows_of(0), rows1 = rows_of(1);
+  for (int x = threadIdx.x; x < rows0 + rows1; x += kThreads) {
+    const int k = x < rows0 ? 0 : 1, r = k == 0 ? x : x - rows0, blocks = t.pending[k][3] - t.pending[k][2] + 1;
+    float top = -INFINITY, sum = 0.f;
+    for (int c = 0; c < blocks; c += 8) {
+      float2 y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = c + e < blocks ? part_ml(k, c + e, r) : make_float2(-INFINITY, 0.f);
+      float now = top;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) now = fmaxf(now, y[e].x);
+      const float to = now == -INFINITY ? 0.f : now;
+      sum *= exp2_fast(top - to);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += exp2_fast(y[e].x - to) * y[e].y;
+      top = now;
+    }
+    const int head = t.pending[k][1] / a.row_tiles, row0 = (t.pending[k][1] - head * a.row_tiles) * a.tile_rows;
+    int64_t at_lse;
+    joint_out[x] = out_at(a, t.pending[k][0], head, row0 + r, &at_lse);
+    joint_top[x] = top == -INFINITY ? 0.f : top;
+    joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
+    if (a.lse) a.lse[at_lse] = lse_of(top, sum);
+  }
+  __syncthreads();
+  const int quads = D / 4;
+  for (int j = threadIdx.x; j < (rows0 + rows1) * quads; j += kThreads) {
+    const int x = j / quads, quad = j - x * quads;
+    const int k = x < rows0 ? 0 : 1, r = k == 0 ? x : x - rows0, blocks = t.pending[k][3] - t.pending[k][2] + 1;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = 0; c < blocks; c += 8) {
+      float4 y[8];
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (c + e < blocks) {
+          y[e] = __ldcg(reinterpret_cast<const float4*>(part(k, c + e) + r * a.padded + quad * 4));
+          f[e] = part_ml(k, c + e, r).x;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (c + e < blocks) {
+          const float w = exp2_fast(f[e] - joint_top[x]);
+          acc.x += w * y[e].x, acc.y += w * y[e].y, acc.z += w * y[e].z, acc.w += w * y[e].w;
+        }
+      }
+    }
+    const float g = joint_inv[x];
+    write4(a, joint_out[x], quad * 4, g == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g));
+  }
+}
+
+template <bool BF16>
+cudaError_t launch_tc(AttendArgs a, int num_sms, cudaStream_t st) {
+  auto* kernel = attend_tc_kernel<BF16>;
+  static std::atomic<bool> ready[kMaxDevices];
+  if (a.device >= kMaxDevices || !ready[a.device].load(std::memory_order_relaxed)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    if (a.device < kMaxDevices) ready[a.device].store(true, std::memory_order_relaxed);
+  }
+  a.row_tiles = (a.rows + kTile - 1) / kTile;
+  a.tile_rows = (a.rows + a.row_tiles - 1) / a.row_tiles;
+  a.padded = padded_dim(a.head_dim);
+  const int64_t units = ((int64_t)a.max_len + 15) / kTile + 1 + kCost;
+  const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units;
+  if (most >= 2147483648.0) return cudaErrorNotSupported;   // cells are counted in 32 bits
+  a.parts = most < (double)num_sms ? (int)most : num_sms;
+  kernel<<<a.parts, kThreads, kSmem, st>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(const AttendArgs& a, bool bf16, int num_sms, cudaStream_t st) {
+  return bf16 ? launch_tc<true>(a, num_sms, st) : launch_tc<false>(a, num_sms, st);
+}
+
+}  // namespace lc

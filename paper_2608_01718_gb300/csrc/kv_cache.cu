@@ -387,6 +387,8 @@ extern "C" lacache_status lacache_kv_sync(lacache_kv_t* h) {
       cudaMemcpy(&word, h->dev_status, 4, cudaMemcpyDeviceToHost) != cudaSuccess)
     return LACACHE_ERR_CUDA;
   if (!word) return LACACHE_OK;
-  if (cudaMemset(h->dev_status, 0, 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) return LACACHE_ERR_CUDA;
-  return LACACHE_ERR_INVALID_ARG;
+  // (a call that timed out may have left the attention's counters, which lie before the word, in between)
+  const size_t bytes = (unsigned char*)(h->dev_status + 1) - (unsigned char*)h->arrived;
+  if (cudaMemset(h->arrived, 0, bytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) return LACACHE_ERR_CUDA;
+  return word & lc::kAttendTimeout ? LACACHE_ERR_DEVICE_TIMEOUT : LACACHE_ERR_INVALID_ARG;
 }
