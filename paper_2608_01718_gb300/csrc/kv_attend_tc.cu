@@ -10,10 +10,9 @@
 //
 // One block an SM, warp-specialised:
 //   warps 5-7 (loaders): the tiles of K and V, in turn, into a ring of six 32 KB slots in the 128-byte swizzle layout, by
-//     cp.async (whole 16-byte units of rows found through the page table; masked and missing positions are zeros), and with
-//     a triple's first tile its q;
+//     cp.async (whole 16-byte units of rows found through the page table; masked and missing positions are zeros);
 //   warp 4 (MMA): S of tile j into one of two accumulators, then O += P V of tile j - 1;
-//   warps 0-3 (softmax, a row a thread): S from TMEM, base-2 softmax with a maximum that moves only by more than 2^8 (as in
+//   warps 0-3 (softmax, a row a thread): a triple's q into shared memory; S from TMEM, base-2 softmax with a maximum that moves only by more than 2^8 (as in
 //     kv_attend.cuh), weights to TMEM as the A operand of the second product; for a bf16 cache in two terms, which the
 //     product sums (one would add an error as large as the output's rounding).
 // K is the first product's B operand as stored (K-major); V, as stored, the second's with its dimensions contiguous
@@ -45,7 +44,7 @@ struct Tail {
   uint64_t full[kSlots], empty[kSlots];      // a slot's copies have landed; its products are done
   uint64_t s_full[2], s_empty[2];            // an S is complete; has been read
   uint64_t p_full, pv_done;                  // the weights are stored; their product is done
-  uint64_t q_empty, o_empty;                 // q has been used for the last time; O has been read
+  uint64_t q_full, o_empty;                  // a triple's q is there; its O has been read
   uint64_t drain;
   uint32_t tmem;
   uint32_t abort_flag;
@@ -84,6 +83,17 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
       "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+
+// Whether the phase of the given parity is complete, without waiting.
+__device__ __forceinline__ bool test_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 
 // This block's part of the line of cells: triples in order, each with its first unit and how many units are the block's.
@@ -160,6 +170,13 @@ __device__ __forceinline__ void write4(const AttendArgs& a, int64_t at_row, int 
       a.q_f16 ? make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w)) : make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
 }
 
+// Eight, times g (0: zeros, whatever they are).
+__device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int d, float4 x, float4 y, float g) {
+  if (g == 0.f) x = y = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float v[8] = {x.x * g, x.y * g, x.z * g, x.w * g, y.x * g, y.y * g, y.z * g, y.w * g};
+  *reinterpret_cast<uint4*>(a.out.p + at_row + d * 2) = a.q_f16 ? pack8(v, __half()) : pack8(v, __nv_bfloat16());
+}
+
 // One row of one block's keys [from, to), key by key, by a warp: lane i holds dimensions 4 i .. 4 i + 3.
 template <bool BF16>
 __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, int tok, int qh, int from, int to, float4* acc,
@@ -225,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     }
     mbar_init(smem_u32(&t.p_full), 128);
     mbar_init(smem_u32(&t.pv_done), 1);
-    mbar_init(smem_u32(&t.q_empty), 1);
+    mbar_init(smem_u32(&t.q_full), 128);
     mbar_init(smem_u32(&t.o_empty), 128);
     mbar_init(smem_u32(&t.drain), 1);
     t.abort_flag = 0;
@@ -254,15 +271,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     // ---- loaders ----
     const int me = threadIdx.x - 160;
     int n = 0, sent = 0;   // slots begun, and handed over
-    int triples = 0, units = 0;
+    int units = 0;
     bool ok = true;
+    const int unit_mul = 65536 / units_row + 1;   // z / units_row = z * unit_mul >> 16 for z < 256
+    // where the lane's units of a 16-key tile lie, in heads of 128 and 64: copies i and i + 4 lie 8 rows apart
+    uint32_t place[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      place[i] = units_row == 16 ? unit_at(2 * i + (lane >> 4), lane & 15) : unit_at(4 * i + (lane >> 3), lane & 7);
     auto hand_over = [&](int upto) {   // slots whose copies have landed
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       for (; sent < upto; ++sent) mbar_arrive(smem_u32(&t.full[sent % kSlots]));
     };
-    for (; ok && !walk.done(); walk.next(a), ++triples) {
-      const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
-      const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
+    for (; ok && !walk.done(); walk.next(a)) {
+      const int head = walk.triple / a.row_tiles, count = walk.units();
       const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
       const unsigned char* head_k = a.pk + (int64_t)head * a.page_size * row_bytes;
       const unsigned char* head_v = a.pv + (int64_t)head * a.page_size * row_bytes;
@@ -282,43 +304,56 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         const int live_keys = walk.sp.hi - key, dead_keys = walk.sp.lo - key;   // keys [dead, live) of the tile are read
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv, ++n) {
-          if (n >= kSlots) ok = wait(t.empty[n % kSlots], (n / kSlots - 1) & 1);
+          if (n >= kSlots) {
+            // while the slot is in use there is nothing to copy: what has landed is handed over at once
+            const uint32_t bar = smem_u32(&t.empty[n % kSlots]), parity = (n / kSlots - 1) & 1;
+            bool free = __all_sync(0xffffffffu, test_wait(bar, parity));
+            if (!free) copy_wait<3>(), hand_over(n - 3), free = __all_sync(0xffffffffu, test_wait(bar, parity));
+            if (!free) copy_wait<2>(), hand_over(n - 2), free = __all_sync(0xffffffffu, test_wait(bar, parity));
+            if (!free) copy_wait<1>(), hand_over(n - 1), free = __all_sync(0xffffffffu, test_wait(bar, parity));
+            if (!free) copy_wait<0>(), hand_over(n);
+            ok = wait(t.empty[n % kSlots], parity);
+          }
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
           }
-          if (kv == 0 && i == 0) {
-            // q of the triple, once its predecessor's last product with q is done (which needs all the copies so far)
-            if (triples) {
-              copy_wait<0>();
-              hand_over(n);
-              ok = wait(t.q_empty, (triples - 1) & 1);
-            }
-            if (!__all_sync(0xffffffffu, ok)) {
-              ok = false;
-              break;
-            }
-            for (int x = me; x < kTile * units_row; x += kLoaders) {
-              const int r = x / units_row, u = x - r * units_row, row = row0 + r, tok = row / a.group;
-              const bool in = r < live;
-              copy_async<16>(q_smem + unit_at(r, u),
-                             in ? a.q.at((int64_t)walk.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) + u * 16
-                                : a.pk, in);
-            }
-          }
+          // a warp takes a page's 16 keys at a time, the three in turn
           const uint32_t dst = ring + (n % kSlots) * kSlotBytes;
           const unsigned char* from = kv ? head_v : head_k;
-          for (int x = me; x < kTile * units_row; x += kLoaders) {
-            const int j = units_row == 16 ? x >> 4 : x / units_row, u = x - j * units_row;
-            const int page = __shfl_sync(0xffffffffu, ids, j >> 4);   // (warps run this loop whole)
-            const int at = key + (j & ~15);
-            const int slot = at - (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift) * a.page_size + (j & 15);
-            const bool in = j >= dead_keys && j < live_keys && (unsigned)page < (unsigned)a.pages;
-            copy_async<16>(dst + unit_at(j, u), in ? from + page * a.page_bytes + (int64_t)slot * row_bytes + u * 16 : a.pk, in);
+          const int first = ((me >> 5) + n) % 3;
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            const int tile = first + 3 * k, at = key + tile * 16, j0 = tile * 16;
+            if (tile >= 8) break;
+            const int page = __shfl_sync(0xffffffffu, ids, tile);
+            const int slot = at - (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift) * a.page_size;
+            const bool there = (unsigned)page < (unsigned)a.pages;
+            const unsigned char* src = from + (there ? page * a.page_bytes : 0) + (int64_t)slot * row_bytes;
+            const bool inside = there && j0 >= dead_keys && j0 + 16 <= live_keys;
+            const uint32_t to = dst + j0 * 128;
+            if (inside && units_row == 16) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) copy_async<16>(to + place[i & 3] + (i >> 2) * 1024, src + lane * 16 + i * 512, true);
+            } else if (inside && units_row == 8) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) copy_async<16>(to + place[i], src + lane * 16 + i * 512, true);
+            } else {
+              for (int z = lane; z < 16 * units_row; z += 32) {
+                const int j = (z * unit_mul) >> 16;
+                const bool in = there && j0 + j >= dead_keys && j0 + j < live_keys;
+                copy_async<16>(dst + unit_at(j0 + j, z - j * units_row), in ? src + z * 16 : a.pk, in);
+              }
+            }
           }
           copy_commit();
-          copy_wait<kAhead>();
-          if (n >= kAhead) hand_over(n - kAhead + 1);
+          if (n < kSlots) {   // the block's first slots, while the memory is idle: two in flight behind the one handed over
+            copy_wait<2>();
+            if (n >= 2) hand_over(n - 1);
+          } else {
+            copy_wait<kAhead>();
+            hand_over(n - kAhead + 1);
+          }
         }
         ids = next_ids;
       }
@@ -358,7 +393,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       const int count = walk.units();
       for (int i = 0; ok && i < count; ++i, ++j) {
         const int k_slot = (2 * j) % kSlots;
-        ok = wait(t.full[k_slot], ((2 * j) / kSlots) & 1) && (j < 2 || wait(t.s_empty[j & 1], ((j >> 1) - 1) & 1));
+        ok = (i > 0 || wait(t.q_full, triples & 1)) && wait(t.full[k_slot], ((2 * j) / kSlots) & 1) &&
+             (j < 2 || wait(t.s_empty[j & 1], ((j >> 1) - 1) & 1));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
@@ -371,7 +407,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           }
           mma_commit<false>(smem_u32(&t.empty[k_slot]), 0);
           mma_commit<false>(smem_u32(&t.s_full[j & 1]), 0);
-          if (i + 1 == count) mma_commit<false>(smem_u32(&t.q_empty), 0);
         }
         __syncwarp();
         if (i > 0) second(j - 1, i == 1, triples);
@@ -383,6 +418,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     const uint32_t lanes = tmem + ((uint32_t)warp << 21);   // this warp's 32 lanes
     int j = 0;
     bool ok = true;
+    // a triple's q into shared memory: begun behind the previous one's last weights, handed over behind its end
+    auto load_q = [&](const Walk& w) {
+      const int head = w.triple / a.row_tiles, row0 = (w.triple - head * a.row_tiles) * a.tile_rows;
+      const int live = min(a.rows - row0, a.tile_rows);
+      const int unit_mul = 65536 / units_row + 1;   // x / units_row = x * unit_mul >> 16 for x < 2048
+#pragma unroll 4
+      for (int x = threadIdx.x; x < kTile * units_row; x += 128) {
+        const int r = (x * unit_mul) >> 16, u = x - r * units_row, row = row0 + r, tok = row / a.group;
+        const bool in = r < live;
+        copy_async<16>(q_smem + unit_at(r, u),
+                       in ? a.q.at((int64_t)w.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) + u * 16 : a.pk, in);
+      }
+      copy_commit();
+    };
+    auto hand_over_q = [&] {
+      copy_wait<0>();
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive(smem_u32(&t.q_full));
+    };
+    load_q(walk);
+    hand_over_q();
     for (; ok && !walk.done(); walk.next(a)) {
       const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
       const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
@@ -419,33 +475,41 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           mbar_arrive(smem_u32(&t.s_empty[j & 1]));
           float (&x)[4][32] = reinterpret_cast<float(&)[4][32]>(u);
           const uint32_t bad = t.bad[j & 15];
-          const bool whole = bad == 0 && key >= lo && key + kTile - 1 <= pos;
-          bool move = false;
-          const bool masked = !__all_sync(0xffffffffu, whole);
-          // scores; masked ones -inf
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[c][e] *= factor;
-          }
-          if (masked) {
+          float by = factor;
+          if (!(factor > 0.f)) {   // scores that the maximum of the products does not order
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const int at = key + c * 32 + e;
-                if (at > pos || at < lo || (bad >> (c * 2 + e / 16) & 1)) x[c][e] = -INFINITY;
+              for (int e = 0; e < 32; ++e) x[c][e] *= factor;
+            }
+            by = 1.f;
+          }
+          if (!__all_sync(0xffffffffu, bad == 0 && key >= lo && key + kTile - 1 <= pos)) {
+            const int first = lo < key ? 0 : lo - key, last = pos >= key + kTile ? kTile : pos - key;   // columns seen
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (c * 32 + e < first || c * 32 + e > last) x[c][e] = -INFINITY;
+            }
+            if (bad) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  if (bad >> (c * 2 + e / 16) & 1) x[c][e] = -INFINITY;
               }
             }
           }
-          float top = m;
+          float tops[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
+            tops[c] = x[c][0];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) top = fmaxf(top, x[c][e]);
+            for (int e = 1; e < 32; ++e) tops[c] = fmaxf(tops[c], x[c][e]);
           }
-          move = top > m + 8.f;   // (from nothing seen, m = -inf: any finite score)
-          if (m == -INFINITY) move = top != -INFINITY;
+          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * by;
+          const bool move = m == -INFINITY ? top > -INFINITY : top > m + 8.f;
           const float f = move ? exp2_fast(m - top) : 1.f;
           if (move) {
             l *= f;
@@ -459,8 +523,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           for (int c = 0; c < 4; ++c) {
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float p0 = exp2_fast(x[c][e] - shift), p1 = exp2_fast(x[c][e + 1] - shift);
-              sum[c] += p0 + p1;
+              const float p0 = exp2_fast(fmaf(x[c][e], by, -shift)), p1 = exp2_fast(fmaf(x[c][e + 1], by, -shift));
+              sum[e / 2 & 3] += p0 + p1;
               const uint32_t h = pack2<BF16>(p0, p1);
               hi[c >> 1][(c & 1) * 16 + e / 2] = h;
               if constexpr (BF16)
@@ -505,6 +569,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         mbar_arrive(smem_u32(&t.p_full));
       }
       if (!ok) break;
+      // every product with this q is done (the last S was complete): the next one's takes its place
+      Walk next = walk;
+      next.next(a);
+      const bool more = !next.done();
+      if (more) load_q(next);
       // ---- the triple's end: O of this block's keys ----
       ok = wait(t.pv_done, (j - 1) & 1);
       if (!__all_sync(0xffffffffu, ok)) {
@@ -538,11 +607,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           for (int e = 0; e < 32; ++e) odd |= e < dims && !(fabsf(o[e]) <= 3.402823466e+38f);
           if (mine) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
+            for (int e = 0; e < 32; e += 8) {
               if (e < dims) {
-                if (whole) write4(a, at_row, c + e, inv == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                                               : make_float4(o[e] * inv, o[e + 1] * inv, o[e + 2] * inv, o[e + 3] * inv));
-                else *reinterpret_cast<float4*>(slot + r * a.padded + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                const float4 y0 = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                const float4 y1 = make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);
+                if (whole) {
+                  write8(a, at_row, c + e, y0, y1, inv);
+                } else {
+                  reinterpret_cast<float4*>(slot)[(c + e) / 4 * kTile + r] = y0;
+                  reinterpret_cast<float4*>(slot)[((c + e) / 4 + 1) * kTile + r] = y1;
+                }
               }
             }
           }
@@ -568,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               write4(a, its_row, lane * 4, sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
                                                       : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g));
             } else {
-              *reinterpret_cast<float4*>(slot + rr * a.padded + lane * 4) = acc;
+              reinterpret_cast<float4*>(slot)[lane * kTile + rr] = acc;
             }
           }
           if (lane == 0) {
@@ -579,6 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       }
       tc_fence_before();
       mbar_arrive(smem_u32(&t.o_empty));
+      if (more) hand_over_q();
     }
   }
 
@@ -640,31 +715,46 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     if (a.lse) a.lse[at_lse] = lse_of(top, sum);
   }
   __syncthreads();
-  const int quads = D / 4;
-  for (int j = threadIdx.x; j < (rows0 + rows1) * quads; j += kThreads) {
-    const int x = j / quads, quad = j - x * quads;
-    const int k = x < rows0 ? 0 : 1, r = k == 0 ? x : x - rows0, blocks = t.pending[k][3] - t.pending[k][2] + 1;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = 0; c < blocks; c += 8) {
-      float4 y[8];
-      float f[8];
+  // a row's eight dimensions at a time, four times, from two blocks: sixteen loads in flight; neighbouring threads on
+  // neighbouring rows
+  const int r = threadIdx.x & (kTile - 1);
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    const int rows = k ? rows1 : rows0, x = k ? rows0 + r : r;
+    if (r >= rows) continue;
+    const int blocks = t.pending[k][3] - t.pending[k][2] + 1;
+    const float base_top = joint_top[x], g = joint_inv[x];
+#pragma unroll 1
+    for (int q0 = (threadIdx.x >> 7) * 8; q0 < D / 4; q0 += 2 * 8) {   // eight quads: 32 dimensions
+      float4 acc[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (c + e < blocks) {
-          y[e] = __ldcg(reinterpret_cast<const float4*>(part(k, c + e) + r * a.padded + quad * 4));
-          f[e] = part_ml(k, c + e, r).x;
+      for (int v = 0; v < 8; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+      for (int c = 0; c < blocks; c += 2) {
+        float4 y[2][8];
+        float w[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bool in = c + e < blocks;
+          const float4* from = reinterpret_cast<const float4*>(part(k, in ? c + e : 0));
+          w[e] = in ? part_ml(k, c + e, r).x : -INFINITY;
+#pragma unroll
+          for (int v = 0; v < 8; ++v)
+            y[e][v] = in && q0 + v < D / 4 ? __ldcg(from + (q0 + v) * kTile + r) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float f = exp2_fast(w[e] - base_top);
+#pragma unroll
+          for (int v = 0; v < 8; ++v)
+            acc[v].x += f * y[e][v].x, acc[v].y += f * y[e][v].y, acc[v].z += f * y[e][v].z, acc[v].w += f * y[e][v].w;
         }
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (c + e < blocks) {
-          const float w = exp2_fast(f[e] - joint_top[x]);
-          acc.x += w * y[e].x, acc.y += w * y[e].y, acc.z += w * y[e].z, acc.w += w * y[e].w;
-        }
+      for (int v = 0; v < 8; v += 2) {
+        if (q0 + v < D / 4) write8(a, joint_out[x], (q0 + v) * 4, acc[v], acc[v + 1], g);
       }
     }
-    const float g = joint_inv[x];
-    write4(a, joint_out[x], quad * 4, g == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g));
   }
 }
 
