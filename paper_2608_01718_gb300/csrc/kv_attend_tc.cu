@@ -4,15 +4,15 @@
 // From some tens of rows on, 4 x rows flops a cached element are more than the warp-level tensor instruction sustains at the
 // rate of HBM, and a tile of 32 rows reads the cache several times. Here a tile is 128 rows of q:
 //   S [128 rows x 128 keys] = Q [128 x d] K^T,   O [128 x d] += P [128 x 128 keys] V
-// with S, P and O in TMEM and q, K and V in shared memory. A thread of the softmax owns a row: its maximum, sum, masks and
-// rescaling need no other thread. At 128 rows and d = 128 a tile of keys takes 0.3 us of tensor time and about as much of
+// with S, P and O in TMEM and q, K and V in shared memory. Two threads of the softmax own a row, half of a tile's keys each,
+// and share no more than its maximum. At 128 rows and d = 128 a tile of keys takes 0.3 us of tensor time and about as much of
 // exponentials against 1.5 us for its 64 KB at an SM's share of HBM, so the kernel is bound by reading the cache.
 //
 // One block an SM, warp-specialised:
-//   warps 5-7 (loaders): the tiles of K and V, in turn, into a ring of six 32 KB slots in the 128-byte swizzle layout, by
+//   warps 9-11 (loaders): the tiles of K and V, in turn, into a ring of six 32 KB slots in the 128-byte swizzle layout, by
 //     cp.async (whole 16-byte units of rows found through the page table; masked and missing positions are zeros);
-//   warp 4 (MMA): S of tile j into one of two accumulators, then O += P V of tile j - 1;
-//   warps 0-3 (softmax, a row a thread): a triple's q into shared memory; S from TMEM, base-2 softmax with a maximum that moves only by more than 2^8 (as in
+//   warp 8 (MMA): S of tile j into one of two accumulators, then O += P V of tile j - 1;
+//   warps 0-7 (softmax, two threads a row): a triple's q into shared memory; S from TMEM, base-2 softmax with a maximum that moves only by more than 2^8 (as in
 //     kv_attend.cuh), weights to TMEM as the A operand of the second product; for a bf16 cache in two terms, which the
 //     product sums (one would add an error as large as the output's rounding).
 // K is the first product's B operand as stored (K-major); V, as stored, the second's with its dimensions contiguous
@@ -34,10 +34,11 @@ constexpr int kSlots = 6;
 constexpr int kAhead = 4;                    // slots whose copies are in flight
 constexpr int kBlockBytes = kTile * 128;     // 64 elements of 128 rows
 constexpr int kSlotBytes = 2 * kBlockBytes;
-constexpr int kMmaWarp = 4;
-constexpr int kLoaders = 96;                 // (eight warps in all: 255 registers a thread)
-constexpr int kThreads = 128 + 32 + kLoaders;
-constexpr int kCost = 2;                     // a triple's start and end, in units
+constexpr int kSoftmax = 256;                // threads: two a row, half of the keys each
+constexpr int kMmaWarp = 8;
+constexpr int kLoaders = 96;                 // (twelve warps in all: 168 registers a thread)
+constexpr int kThreads = kSoftmax + 32 + kLoaders;
+constexpr int kCost = 3;                     // a triple's start and end, in units
 constexpr uint32_t kS = 0, kO = 256, kP = 384;   // TMEM columns: two S, O, P (two terms of 64)
 
 struct Tail {
@@ -48,10 +49,13 @@ struct Tail {
   uint64_t drain;
   uint32_t tmem;
   uint32_t abort_flag;
+  uint64_t pair;                             // the two threads of every row have left their part
+  float given[2][2][kTile];                  // what they leave, in turn and by half: the row's largest product, or at a
+                                             // triple's end its sum of weights (NaN: not finite)
   uint32_t bad[16];                          // a unit's 16-key tiles whose page id is no page (by unit modulo 16)
   int pending[2][4];                         // shared triples, as in kv_attend.cuh
 };
-constexpr int kSmem = 1024 + kSlotBytes + kSlots * kSlotBytes + (int)sizeof(Tail);
+constexpr int kSmem = kSlotBytes + kSlots * kSlotBytes + (int)sizeof(Tail);
 static_assert(kSmem <= 227 * 1024, "shared memory");
 
 // Where 16-byte unit u of row r lies in a tile of 128 rows: blocks of 64 elements, 128-byte swizzle.
@@ -218,9 +222,12 @@ __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, in
 
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a) {
-  extern __shared__ unsigned char smem_raw[];
-  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  unsigned char* gbase = smem_raw + (base - raw);
+  extern __shared__ __align__(1024) unsigned char gbase[];
+  const uint32_t base = smem_u32(gbase);
+  if (base & 1023u) {   // the swizzled tiles start on 1024 bytes (dynamic shared memory does, with none of the static kind)
+    if (threadIdx.x == 0) atomicOr(a.status, kAttendTimeout);
+    return;
+  }
   const uint32_t q_smem = base, ring = base + kSlotBytes;
   Tail& t = *reinterpret_cast<Tail*>(gbase + kSlotBytes + kSlots * kSlotBytes);
   volatile uint32_t* abort_flag = &t.abort_flag;
@@ -238,12 +245,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(smem_u32(&t.s_full[b]), 1);
-      mbar_init(smem_u32(&t.s_empty[b]), 128);
+      mbar_init(smem_u32(&t.s_empty[b]), kSoftmax);
     }
-    mbar_init(smem_u32(&t.p_full), 128);
+    mbar_init(smem_u32(&t.p_full), kSoftmax);
+    mbar_init(smem_u32(&t.pair), kSoftmax);
     mbar_init(smem_u32(&t.pv_done), 1);
-    mbar_init(smem_u32(&t.q_full), 128);
-    mbar_init(smem_u32(&t.o_empty), 128);
+    mbar_init(smem_u32(&t.q_full), kSoftmax);
+    mbar_init(smem_u32(&t.o_empty), kSoftmax);
     mbar_init(smem_u32(&t.drain), 1);
     t.abort_flag = 0;
     t.pending[0][2] = t.pending[1][2] = -1;
@@ -262,14 +270,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     atomicOr(a.status, kAttendTimeout);
   };
   auto wait = [&](uint64_t& bar, uint32_t parity) {   // false (and the block stops) past the bound
-    if (mbar_wait(smem_u32(&bar), parity, abort_flag)) return true;
+    if (mbar_wait_inline(smem_u32(&bar), parity, abort_flag)) return true;
     if (!*abort_flag) fail();
     return false;
   };
 
   if (warp > kMmaWarp) {
     // ---- loaders ----
-    const int me = threadIdx.x - 160;
+    const int me = threadIdx.x - kSoftmax - 32;
     int n = 0, sent = 0;   // slots begun, and handed over
     int units = 0;
     bool ok = true;
@@ -414,9 +422,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       }
     }
   } else {
-    // ---- softmax: a row a thread ----
-    const uint32_t lanes = tmem + ((uint32_t)warp << 21);   // this warp's 32 lanes
+    // ---- softmax: two threads a row ----
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);   // this warp's 32 lanes
+    const int half = warp >> 2;
     int j = 0;
+    uint32_t pairs = 0;
     bool ok = true;
     // a triple's q into shared memory: begun behind the previous one's last weights, handed over behind its end
     auto load_q = [&](const Walk& w) {
@@ -424,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       const int live = min(a.rows - row0, a.tile_rows);
       const int unit_mul = 65536 / units_row + 1;   // x / units_row = x * unit_mul >> 16 for x < 2048
 #pragma unroll 4
-      for (int x = threadIdx.x; x < kTile * units_row; x += 128) {
+      for (int x = threadIdx.x; x < kTile * units_row; x += kSoftmax) {
         const int r = (x * unit_mul) >> 16, u = x - r * units_row, row = row0 + r, tok = row / a.group;
         const bool in = r < live;
         copy_async<16>(q_smem + unit_at(r, u),
@@ -442,8 +452,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     for (; ok && !walk.done(); walk.next(a)) {
       const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
       const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
-      const int r = threadIdx.x, tok = (row0 + r) / a.group;
-      const bool mine = r < live, some = warp * 32 < live;
+      const int r = threadIdx.x & (kTile - 1), tok = (row0 + r) / a.group;
+      const bool mine = r < live, some = (warp & 3) * 32 < live;
       const int pos = mine ? walk.sp.len - a.new_tokens + tok : INT_MAX;
       int lo = INT_MIN;
       if (mine) {
@@ -466,49 +476,59 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
         if (some) {
           tc_fence_after();
-          uint32_t u[4][32];
+          uint32_t u[2][32];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32_issue(lanes + kS + (j & 1) * kTile + c * 32, u[c]);
+          for (int c = 0; c < 2; ++c) tmem_ld32_issue(lanes + kS + (j & 1) * kTile + half * 64 + c * 32, u[c]);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32_wait(u[c]);
+          for (int c = 0; c < 2; ++c) tmem_ld32_wait(u[c]);
           tc_fence_before();
           mbar_arrive(smem_u32(&t.s_empty[j & 1]));
-          float (&x)[4][32] = reinterpret_cast<float(&)[4][32]>(u);
+          float (&x)[2][32] = reinterpret_cast<float(&)[2][32]>(u);
           const uint32_t bad = t.bad[j & 15];
           float by = factor;
           if (!(factor > 0.f)) {   // scores that the maximum of the products does not order
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[c][e] *= factor;
             }
             by = 1.f;
           }
           if (!__all_sync(0xffffffffu, bad == 0 && key >= lo && key + kTile - 1 <= pos)) {
-            const int first = lo < key ? 0 : lo - key, last = pos >= key + kTile ? kTile : pos - key;   // columns seen
+            const int at = key + half * 64;
+            const int first = lo < at ? 0 : lo - at, last = pos >= at + 64 ? 64 : pos - at;   // columns seen
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
                 if (c * 32 + e < first || c * 32 + e > last) x[c][e] = -INFINITY;
             }
             if (bad) {
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
+              for (int c = 0; c < 2; ++c) {
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
-                  if (bad >> (c * 2 + e / 16) & 1) x[c][e] = -INFINITY;
+                  if (bad >> (half * 4 + c * 2 + e / 16) & 1) x[c][e] = -INFINITY;
               }
             }
           }
-          float tops[4];
+          float tops[2];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             tops[c] = x[c][0];
 #pragma unroll
             for (int e = 1; e < 32; ++e) tops[c] = fmaxf(tops[c], x[c][e]);
           }
-          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * by;
+          // both halves of the row move its maximum, or neither
+          const float own = fmaxf(tops[0], tops[1]);
+          t.given[pairs & 1][half][r] = own;
+          mbar_arrive(smem_u32(&t.pair));
+          ok = wait(t.pair, pairs & 1);
+          if (!__all_sync(0xffffffffu, ok)) {
+            ok = false;
+            break;
+          }
+          const float top = fmaxf(own, t.given[pairs++ & 1][half ^ 1][r]) * by;
           const bool move = m == -INFINITY ? top > -INFINITY : top > m + 8.f;
           const float f = move ? exp2_fast(m - top) : 1.f;
           if (move) {
@@ -518,17 +538,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           const float shift = m == -INFINITY ? 0.f : m;
           // weights, their sum, and their terms
           float sum[4] = {};
-          uint32_t hi[2][32], lo_term[BF16 ? 2 : 1][32];
+          uint32_t hi[32], lo_term[BF16 ? 32 : 1];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
               const float p0 = exp2_fast(fmaf(x[c][e], by, -shift)), p1 = exp2_fast(fmaf(x[c][e + 1], by, -shift));
               sum[e / 2 & 3] += p0 + p1;
               const uint32_t h = pack2<BF16>(p0, p1);
-              hi[c >> 1][(c & 1) * 16 + e / 2] = h;
+              hi[c * 16 + e / 2] = h;
               if constexpr (BF16)
-                lo_term[c >> 1][(c & 1) * 16 + e / 2] =
+                lo_term[c * 16 + e / 2] =
                     pack2<true>(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
             }
           }
@@ -542,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           tc_fence_after();
           if (i > 0 && __any_sync(0xffffffffu, move)) {
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
+            for (int c = half * 32; c < D; c += 64) {
               uint32_t o[32];
               tmem_ld32_issue(lanes + kO + c, o);
               tmem_ld32_wait(o);
@@ -551,15 +571,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               tmem_st32(lanes + kO + c, o);
             }
           }
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            tmem_st32(lanes + kP + c * 32, hi[c]);
-            if constexpr (BF16) tmem_st32(lanes + kP + 64 + c * 32, lo_term[c]);
-          }
+          tmem_st32(lanes + kP + half * 32, hi);
+          if constexpr (BF16) tmem_st32(lanes + kP + 64 + half * 32, lo_term);
           tmem_wait_st();
           tc_fence_before();
         } else {
           mbar_arrive(smem_u32(&t.s_empty[j & 1]));   // rows past the tile's: their weights are never used
+          mbar_arrive(smem_u32(&t.pair));
+          ++pairs;
           if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
@@ -593,41 +612,61 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
       }
       float* slot = a.partial + ((int64_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * slot_floats;
-      if (some) {
+      if (!some) {
+        mbar_arrive(smem_u32(&t.pair));
+        ++pairs;
+      } else {
+        // this half's dimensions: 32 of every 64
+        float o[2][32];
+        bool odd = false;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int d0 = half * 32 + c * 64;
+          if (d0 < D) {
+            tmem_ld32(lanes + kO + d0, o[c]);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) odd |= d0 + e < D && !(fabsf(o[c][e]) <= 3.402823466e+38f);
+          }
+        }
+        t.given[pairs & 1][half][r] = odd ? __int_as_float(0x7fc00000) : l;
+        mbar_arrive(smem_u32(&t.pair));
+        ok = wait(t.pair, pairs & 1);
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        const float total = t.given[pairs & 1][0][r] + t.given[pairs & 1][1][r];
+        ++pairs;
+        odd = !(total <= 3.402823466e+38f);   // a row that is not finite in either half is done again, by the first
         int64_t at_lse = 0, at_row = 0;
         if (mine) at_row = out_at(a, walk.seq, head, row0 + r, &at_lse);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        bool odd = false;
-#pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          float o[32];
-          tmem_ld32(lanes + kO + c, o);
-          const int dims = min(32, D - c);
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        if (mine && !odd) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) odd |= e < dims && !(fabsf(o[e]) <= 3.402823466e+38f);
-          if (mine) {
+          for (int c = 0; c < 2; ++c) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
-              if (e < dims) {
-                const float4 y0 = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                const float4 y1 = make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);
+              const int d = half * 32 + c * 64 + e;
+              if (d < D) {
+                const float4 y0 = make_float4(o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]);
+                const float4 y1 = make_float4(o[c][e + 4], o[c][e + 5], o[c][e + 6], o[c][e + 7]);
                 if (whole) {
-                  write8(a, at_row, c + e, y0, y1, inv);
+                  write8(a, at_row, d, y0, y1, inv);
                 } else {
-                  reinterpret_cast<float4*>(slot)[(c + e) / 4 * kTile + r] = y0;
-                  reinterpret_cast<float4*>(slot)[((c + e) / 4 + 1) * kTile + r] = y1;
+                  reinterpret_cast<float4*>(slot)[d / 4 * kTile + r] = y0;
+                  reinterpret_cast<float4*>(slot)[(d / 4 + 1) * kTile + r] = y1;
                 }
               }
             }
           }
-        }
-        if (mine) {
-          if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, l);
-          else if (a.lse) a.lse[at_lse] = lse_of(m, l);
+          if (half == 0) {
+            if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, total);
+            else if (a.lse) a.lse[at_lse] = lse_of(m, total);
+          }
         }
         // rows that are not finite, again
         const int key_end = min(key_begin + count * kTile, walk.sp.hi);
-        for (unsigned rows = __ballot_sync(0xffffffffu, mine && odd); rows; rows &= rows - 1) {
+        for (unsigned rows = half ? 0u : __ballot_sync(0xffffffffu, mine && odd); rows; rows &= rows - 1) {
           const int src = __ffs(rows) - 1;
           const int rr = warp * 32 + src, its_tok = (row0 + rr) / a.group, its_qh = head * a.group + row0 + rr - its_tok * a.group;
           const int its_pos = __shfl_sync(0xffffffffu, pos, src), its_lo = __shfl_sync(0xffffffffu, lo, src);
@@ -661,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   if (warp == kMmaWarp) {
     if (elect_one()) mma_commit<false>(smem_u32(&t.drain), 0);
     __syncwarp();
-    mbar_wait(smem_u32(&t.drain), 0, nullptr);
+    mbar_wait_inline(smem_u32(&t.drain), 0, nullptr);
   }
   tc_fence_before();
   __syncthreads();
@@ -715,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     if (a.lse) a.lse[at_lse] = lse_of(top, sum);
   }
   __syncthreads();
-  // a row's eight dimensions at a time, four times, from two blocks: sixteen loads in flight; neighbouring threads on
+  // eight quads of a row at a time from two blocks: sixteen loads in flight; neighbouring threads on
   // neighbouring rows
   const int r = threadIdx.x & (kTile - 1);
 #pragma unroll 1
@@ -725,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     const int blocks = t.pending[k][3] - t.pending[k][2] + 1;
     const float base_top = joint_top[x], g = joint_inv[x];
 #pragma unroll 1
-    for (int q0 = (threadIdx.x >> 7) * 8; q0 < D / 4; q0 += 2 * 8) {   // eight quads: 32 dimensions
+    for (int q0 = (threadIdx.x >> 7) * 8; q0 < D / 4; q0 += kThreads / kTile * 8) {   // eight quads: 32 dimensions
       float4 acc[8];
 #pragma unroll
       for (int v = 0; v < 8; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
