@@ -54,8 +54,8 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   a.status = h->dev_status;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e;
-  if (!lc::is_quantised(c.format) && c.head_dim <= 128 && a.rows > lc::kTcRows) {
-    e = lc::launch_attend_tc(a, c.format == LACACHE_KV_BF16, h->num_sms, st);
+  if (c.head_dim <= 128 && a.rows > lc::kTcRows) {
+    e = lc::launch_attend_tc(a, c.format, h->num_sms, st);
   } else switch (c.format) {
     case LACACHE_KV_BF16: e = lc::launch_attend_bf16(a, h->num_sms, st); break;
     case LACACHE_KV_F16: e = lc::launch_attend_f16(a, h->num_sms, st); break;

@@ -88,9 +88,9 @@ cudaError_t launch_attend_bf16(const AttendArgs& a, int num_sms, cudaStream_t st
 cudaError_t launch_attend_f16(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
-// The tcgen05 kernel for many rows (kv_attend_tc.cu): 16-bit caches with heads of up to 128.
+// The tcgen05 kernel for many rows (kv_attend_tc.cu): heads of up to 128.
 constexpr int kTcRows = 32;   // from more rows than this
-cudaError_t launch_attend_tc(const AttendArgs& a, bool bf16, int num_sms, cudaStream_t st);
+cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
 
 namespace {
 
@@ -112,7 +112,7 @@ struct AttendConfig {
   static constexpr int kTileBytes = 16 * DP * kItem;                     // K (or V) of 16 keys
   static constexpr int kStageBytes = kSub * 2 * kTileBytes + (kEight ? kKeys * 8 : 0);
   static constexpr int kStages = kStageBytes > 16000 ? (NT == 1 ? 3 : 2) : kStageBytes > 8000 ? 2 : 4;
-  static constexpr int kTripleCost = kStageBytes > 8000 ? 1 : 2;         // a triple's start and join, in units
+  static constexpr int kTripleCost = kStageBytes > 8000 ? (NT == 4 ? 3 : NT) : 2;         // a triple's start and join, in units
   static constexpr int kMTiles = DP / 16;
   static constexpr int kQStride = DP * 2 + 64;                           // bytes of a row of q in shared memory
   static constexpr int kRing = kAttendWarps * kStages * kStageBytes;
@@ -442,14 +442,27 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           a.q.at((int64_t)of_seq * a.new_tokens + tok, of_head * a.group + row - tok * a.group) + lane * 16);
     return x;
   };
-  constexpr bool kQEarly = NT <= 2;   // the next triple's q is read before the join; more rows would spill
+  // the next triple's q is read ahead of the join: into registers, or where more rows would spill, by cp.async into its place
+  // in shared memory, once every warp is done with the last
+  constexpr bool kQEarly = NT <= 2;
   uint4 q_raw[kQEarly ? C::kRows / kAttendWarps : 1];
   auto load_q_early = [&](int of_seq, int of_triple) {
+    const int of_head = of_triple / a.row_tiles, of_row0 = (of_triple - of_head * a.row_tiles) * C::kRows;
     if constexpr (kQEarly) {
-      const int of_head = of_triple / a.row_tiles;
 #pragma unroll
       for (int k = 0; k < C::kRows / kAttendWarps; ++k)
-        q_raw[k] = load_q(of_seq, of_head, (of_triple - of_head * a.row_tiles) * C::kRows, warp + k * kAttendWarps);
+        q_raw[k] = load_q(of_seq, of_head, of_row0, warp + k * kAttendWarps);
+    } else {
+#pragma unroll
+      for (int k = 0; k < C::kRows / kAttendWarps; ++k) {
+        const int r = warp + k * kAttendWarps, row = of_row0 + r, tok = row / a.group;
+        const bool in = row < a.rows && lane * 8 < D;
+        if (lane * 8 < DP)
+          copy_async<16>(shared_addr(q_smem + r * C::kQStride + lane * 16),
+                         in ? a.q.at((int64_t)of_seq * a.new_tokens + tok, of_head * a.group + row - tok * a.group) + lane * 16
+                            : a.pk, in);
+      }
+      copy_commit();
     }
   };
   float factor[NT][2];
@@ -494,6 +507,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       if (i < 0) continue;   // the copies' head start
       if (i == 0 && !redo) {
         // ---- q into shared memory, in the order of the K pieces ----
+        if constexpr (!kQEarly) copy_wait<1>();   // all but the newest copies: q's lie before them
         if (threadIdx.x == 0) {
           const int raw = a.lengths[seq];
           if (raw < 0 || raw > a.max_len) atomicOr(a.status, kBadIndex);
@@ -503,7 +517,9 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           const int r = warp + k * kAttendWarps, row = row0 + r, d0 = lane * 8;
           const bool live = r < live_rows;
           const int tok = live ? row / a.group : 0;
-          uint4 raw = kQEarly ? q_raw[k] : load_q(seq, head, row0, r);
+          uint4 raw = make_uint4(0, 0, 0, 0);
+          if (kQEarly) raw = q_raw[k];
+          else if (d0 < DP) raw = *reinterpret_cast<const uint4*>(q_smem + r * C::kQStride + d0 * 2);
           float back = 1.f;
           if (C::kEight && !a.q_f16) {
             float x[8], top = 0.f;
@@ -898,7 +914,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
         seq = seq + 1 < a.table.seqs ? seq + 1 : seq;
         sp = span_of(a, seq, C::kUnit);
       }
-      load_q_early(seq, triple);
+      if constexpr (kQEarly) load_q_early(seq, triple);
     }
 
     // ---- join the warps, scaled to the common maximum, a quarter of the dimensions at a time ----
@@ -917,6 +933,9 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       }
     }
     __syncthreads();
+    if constexpr (!kQEarly) {
+      if (left > 0) load_q_early(seq, triple);
+    }
     const bool whole = units == of_units;
     int c_first = block, c_last = block;   // the blocks that share the triple
     if (!whole) {

@@ -30,8 +30,9 @@ namespace lc {
 namespace {
 
 constexpr int kTile = 128;                   // rows of q, and keys, a tile
-constexpr int kSlots = 6;
-constexpr int kAhead = 4;                    // slots whose copies are in flight
+constexpr int kAhead = 4;                    // 16-bit caches: slots whose copies are in flight
+constexpr int kStages = 3;                   // 8-bit caches: tiles of codes in flight
+constexpr int kStageBytes = kTile * 128;
 constexpr int kBlockBytes = kTile * 128;     // 64 elements of 128 rows
 constexpr int kSlotBytes = 2 * kBlockBytes;
 constexpr int kSoftmax = 256;                // threads: two a row, half of the keys each
@@ -41,22 +42,34 @@ constexpr int kThreads = kSoftmax + 32 + kLoaders;
 constexpr int kCost = 3;                     // a triple's start and end, in units
 constexpr uint32_t kS = 0, kO = 256, kP = 384;   // TMEM columns: two S, O, P (two terms of 64)
 
-struct Tail {
-  uint64_t full[kSlots], empty[kSlots];      // a slot's copies have landed; its products are done
-  uint64_t s_full[2], s_empty[2];            // an S is complete; has been read
-  uint64_t p_full, pv_done;                  // the weights are stored; their product is done
-  uint64_t q_full, o_empty;                  // a triple's q is there; its O has been read
-  uint64_t drain;
-  uint32_t tmem;
-  uint32_t abort_flag;
-  uint64_t pair;                             // the two threads of every row have left their part
-  float given[2][2][kTile];                  // what they leave, in turn and by half: the row's largest product, or at a
-                                             // triple's end its sum of weights (NaN: not finite)
-  uint32_t bad[16];                          // a unit's 16-key tiles whose page id is no page (by unit modulo 16)
-  int pending[2][4];                         // shared triples, as in kv_attend.cuh
+// Cache format and q's type. An 8-bit cache's keys are widened to q's type and its values to bf16, both exact.
+template <int FMT, bool QF16>
+struct Tc {
+  static constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
+  static constexpr bool kSplit = FMT != LACACHE_KV_F16;    // bf16 weights, in two terms
+  static constexpr int kSlots = kEight ? 4 : 6;
+  struct Tail {
+    uint64_t full[6], empty[6];                // a slot's tile is there; its products are done
+    uint64_t s_full[2], s_empty[2];            // an S is complete; has been read
+    uint64_t p_full, pv_done;                  // the weights are stored; their product is done
+    uint64_t q_full, o_empty;                  // a triple's q is there; its O has been read
+    uint64_t pair;                             // the two threads of every row have left their part
+    uint64_t drain;
+    float given[2][2][kTile];                  // what they leave, in turn and by half: the row's largest product, or at a
+                                               // triple's end its sum of weights (NaN: not finite)
+    uint32_t tmem;
+    uint32_t abort_flag;
+    uint32_t bad[16];                          // a unit's 16-key tiles whose page id is no page (by unit modulo 16)
+    int pending[2][4];                         // shared triples, as in kv_attend.cuh
+    // 8-bit caches: a unit's scales of K, then of V (by unit modulo 8)
+    alignas(16) float scales[kEight ? 8 * 2 * kTile : 4];   // read four at a time
+  };
+  static constexpr int kRing = kSlotBytes, kStage = kRing + kSlots * kSlotBytes;   // offsets in shared memory, after q
+  static constexpr int kTail = kStage + (kEight ? kStages * kStageBytes : 0);
+  static constexpr int kSmem = kTail + (int)sizeof(Tail);
+  static_assert(kSmem <= 227 * 1024, "shared memory");
+  static_assert(kTail % 16 == 0 && alignof(Tail) == 16, "the scales' alignment");
 };
-constexpr int kSmem = kSlotBytes + kSlots * kSlotBytes + (int)sizeof(Tail);
-static_assert(kSmem <= 227 * 1024, "shared memory");
 
 // Where 16-byte unit u of row r lies in a tile of 128 rows: blocks of 64 elements, 128-byte swizzle.
 __device__ __forceinline__ uint32_t unit_at(int r, int u) {
@@ -182,19 +195,33 @@ __device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int 
 }
 
 // One row of one block's keys [from, to), key by key, by a warp: lane i holds dimensions 4 i .. 4 i + 3.
-template <bool BF16>
+template <int FMT, bool QF16>
 __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, int tok, int qh, int from, int to, float4* acc,
                                       float* top, float* sum) {
+  using T = Tc<FMT, QF16>;
   const int lane = threadIdx.x & 31, D = a.head_dim;
   const bool has = lane * 4 < D;
-  auto load4 = [&](const unsigned char* p) {
-    if (!has) return make_float4(0.f, 0.f, 0.f, 0.f);
-    const uint2 u = *reinterpret_cast<const uint2*>(p + lane * 8);
-    if (BF16)
+  auto four = [](uint2 u, bool f16) {
+    if (!f16)
       return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                          __uint_as_float(u.y & 0xffff0000u));
     const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
     return make_float4(x.x, x.y, y.x, y.y);
+  };
+  auto load4 = [&](const unsigned char* p) {
+    return has ? four(*reinterpret_cast<const uint2*>(p + lane * 8), QF16) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  auto cached4 = [&](const unsigned char* pool, const float* scales, int64_t row) {
+    if (!has) return make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (T::kEight) {
+      uint2 u;
+      widen4<FMT>(*reinterpret_cast<const uint32_t*>(pool + row * D + lane * 4), u.x, u.y);
+      const float4 x = four(u, true);
+      const float f = scales[row];
+      return make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+    } else {
+      return four(*reinterpret_cast<const uint2*>(pool + row * D * 2 + lane * 8), FMT == LACACHE_KV_F16);
+    }
   };
   const float4 q = load4(a.q.at((int64_t)seq * a.new_tokens + tok, qh));
   float m = -INFINITY, l = 0.f;
@@ -204,7 +231,7 @@ __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, in
     const int page = a.table.pages[seq * a.table.stride + index];
     if ((unsigned)page >= (unsigned)a.pages) continue;
     const int64_t row = page * a.page_rows + (int64_t)head * a.page_size + (j - index * a.page_size);
-    const float4 k = load4(a.pk + row * D * 2), v = load4(a.pv + row * D * 2);
+    const float4 k = cached4(a.pk, a.ks, row), v = cached4(a.pv, a.vs, row);
     float dot = has ? q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w : 0.f;
 #pragma unroll
     for (int x = 16; x; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
@@ -220,19 +247,24 @@ __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, in
   *sum = l;
 }
 
-template <bool BF16>
+template <int FMT, bool QF16>
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a) {
+  using T = Tc<FMT, QF16>;
+  using Tail = typename T::Tail;
+  constexpr bool kSplit = T::kSplit;
+  constexpr int kSlots = T::kSlots;
   extern __shared__ __align__(1024) unsigned char gbase[];
   const uint32_t base = smem_u32(gbase);
   if (base & 1023u) {   // the swizzled tiles start on 1024 bytes (dynamic shared memory does, with none of the static kind)
     if (threadIdx.x == 0) atomicOr(a.status, kAttendTimeout);
     return;
   }
-  const uint32_t q_smem = base, ring = base + kSlotBytes;
-  Tail& t = *reinterpret_cast<Tail*>(gbase + kSlotBytes + kSlots * kSlotBytes);
+  const uint32_t q_smem = base, ring = base + T::kRing;
+  Tail& t = *reinterpret_cast<Tail*>(gbase + T::kTail);
   volatile uint32_t* abort_flag = &t.abort_flag;
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int D = a.head_dim, row_bytes = D * 2, units_row = D / 8;
+  const int D = a.head_dim, units_row = D / 8;                    // 16-byte units of a row in shared memory
+  const int row_bytes = T::kEight ? D : D * 2;                    // of the cache
   const int slot_floats = kTile * (a.padded + 2);   // of a.partial
 
   Walk walk;
@@ -281,6 +313,102 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     int n = 0, sent = 0;   // slots begun, and handed over
     int units = 0;
     bool ok = true;
+    if constexpr (T::kEight) {
+      // codes by cp.async into a stage, each lane its own pieces; kStages tiles later the lane widens them into a slot
+      const int pieces = D / 16, piece_mul = 65536 / pieces + 1, tile_pieces = 16 * pieces;   // of a row; of 16 keys
+      auto widen_tile = [&](int k) {
+        if (k >= kSlots) ok = wait(t.empty[k % kSlots], (k / kSlots - 1) & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) return;
+        const unsigned char* from = gbase + T::kStage + (k % kStages) * kStageBytes;
+        const uint32_t dst = ring + (k % kSlots) * kSlotBytes;
+        const bool as_f16 = QF16 && !(k & 1);
+#pragma unroll 1
+        for (int tile = ((me >> 5) + k) % 3; tile < 8; tile += 3) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int z = lane + 32 * i, j = (z * piece_mul) >> 16, u = z - j * pieces;
+            if (z >= tile_pieces) break;
+            const uint4 codes = *reinterpret_cast<const uint4*>(from + tile * 2048 + z * 16);
+            const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+            uint32_t h[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) widen4<FMT>(w[e], h[2 * e], h[2 * e + 1]);
+            if (!as_f16) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
+                h[e] = pack2<true>(f.x, f.y);
+              }
+            }
+            const int row = tile * 16 + j;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at(row, 2 * u)), "r"(h[0]), "r"(h[1]),
+                         "r"(h[2]), "r"(h[3])
+                         : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at(row, 2 * u + 1)), "r"(h[4]),
+                         "r"(h[5]), "r"(h[6]), "r"(h[7])
+                         : "memory");
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(smem_u32(&t.full[k % kSlots]));
+      };
+      for (; ok && !walk.done(); walk.next(a)) {
+        const int head = walk.triple / a.row_tiles, count = walk.units();
+        const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
+        const int64_t head_row = (int64_t)head * a.page_size;
+        int key = (walk.sp.lo & ~15) + walk.first_unit * kTile;
+        auto look_up = [&](int from) {
+          const int at = from + (lane & 7) * 16;
+          return at < walk.sp.hi ? __ldg(table_row + (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift)) : -1;
+        };
+        int ids = look_up(key);
+        for (int i = 0; ok && i < count; ++i, key += kTile, ++units) {
+          const int next_ids = i + 1 < count ? look_up(key + kTile) : -1;
+          const bool wrong = key + (lane & 7) * 16 < walk.sp.hi && (unsigned)ids >= (unsigned)a.pages;
+          const unsigned bad = __ballot_sync(0xffffffffu, wrong) & 0xffu;
+          if (bad && me == 0) atomicOr(a.status, kBadIndex);
+          if (me == 0) t.bad[units & 15] = bad;
+          const int live_keys = walk.sp.hi - key, dead_keys = walk.sp.lo - key;
+#pragma unroll 1
+          for (int kv = 0; kv < 2 && ok; ++kv, ++n) {
+            // (the stage was widened kStages tiles ago by the same lanes)
+            const uint32_t to = base + T::kStage + (n % kStages) * kStageBytes;
+            const unsigned char* pool = kv ? a.pv : a.pk;
+#pragma unroll 1
+            for (int tile = ((me >> 5) + n) % 3; tile < 8; tile += 3) {
+              const int page = __shfl_sync(0xffffffffu, ids, tile), at = key + tile * 16, j0 = tile * 16;
+              const int slot = at - (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift) * a.page_size;
+              const bool there = (unsigned)page < (unsigned)a.pages;
+              const int64_t row = there ? page * a.page_rows + head_row + slot : 0;
+              const unsigned char* src = pool + row * row_bytes;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const int z = lane + 32 * x, j = j0 + ((z * piece_mul) >> 16);
+                const bool in = there && j >= dead_keys && j < live_keys;
+                if (z < tile_pieces) copy_async<16>(to + tile * 2048 + z * 16, in ? src + z * 16 : a.pk, in);
+              }
+              if (kv == 0) {   // with K, the scales of both: the softmax wants them before V has to be there
+                const int j = lane & 15;
+                const bool in = there && j0 + j >= dead_keys && j0 + j < live_keys;
+                const float* scales = lane < 16 ? a.ks : a.vs;
+                copy_async<4>(smem_u32(&t.scales[((units & 7) * 2 + (lane >> 4)) * kTile + j0 + j]), in ? scales + row + j : scales,
+                              in);
+              }
+            }
+            copy_commit();
+            if (n >= kStages - 1) {
+              copy_wait<kStages - 1>();
+              widen_tile(n - (kStages - 1));
+            }
+          }
+          ids = next_ids;
+        }
+      }
+      copy_wait<0>();
+      for (int k = max(n - (kStages - 1), 0); ok && k < n; ++k) widen_tile(k);
+      walk.left = 0;   // nothing is left for the 16-bit caches' loop below
+    }
     const int unit_mul = 65536 / units_row + 1;   // z / units_row = z * unit_mul >> 16 for z < 256
     // where the lane's units of a 16-key tile lie, in heads of 128 and 64: copies i and i + 4 lie 8 rows apart
     uint32_t place[4];
@@ -367,12 +495,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       }
     }
     copy_wait<0>();
-    if (ok) hand_over(n);
+    if (!T::kEight && ok) hand_over(n);   // (8-bit tiles were handed over as they were widened)
   } else if (warp == kMmaWarp) {
     // ---- MMA ----
-    const uint32_t type = BF16 ? (1u << 7) | (1u << 10) : 0u;
-    const uint32_t qk = (1u << 4) | type | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
-    const uint32_t pv = (1u << 4) | type | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    const uint32_t bf16 = (1u << 7) | (1u << 10);   // both operands' type; f16 is 0
+    const uint32_t qk = (1u << 4) | (QF16 ? 0u : bf16) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    const uint32_t pv = (1u << 4) | (kSplit ? bf16 : 0u) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
     const uint64_t q_desc = smem_desc(q_smem);
     int j = 0, triples = 0;    // tiles and triples begun
     bool ok = true;
@@ -390,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         for (int kk = 0; kk < kTile / 16; ++kk) {
           const uint64_t v_desc = smem_desc_mn(v + kk * 2048);
           mma_ts(tmem + kO, tmem + kP + kk * 8, v_desc, pv, first_of_triple && kk == 0 ? 0u : 1u);
-          if (BF16) mma_ts(tmem + kO, tmem + kP + 64 + kk * 8, v_desc, pv, 1u);
+          if (kSplit) mma_ts(tmem + kO, tmem + kP + 64 + kk * 8, v_desc, pv, 1u);
         }
         mma_commit<false>(smem_u32(&t.empty[v_slot]), 0);
         mma_commit<false>(smem_u32(&t.pv_done), 0);
@@ -485,6 +613,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           mbar_arrive(smem_u32(&t.s_empty[j & 1]));
           float (&x)[2][32] = reinterpret_cast<float(&)[2][32]>(u);
           const uint32_t bad = t.bad[j & 15];
+          if constexpr (T::kEight) {
+            const float4* ks = reinterpret_cast<const float4*>(t.scales + (j & 7) * 2 * kTile + half * 64);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float4 k4 = ks[e];
+              float* y = x[e >> 3] + (e & 7) * 4;
+              y[0] *= k4.x, y[1] *= k4.y, y[2] *= k4.z, y[3] *= k4.w;
+            }
+          }
           float by = factor;
           if (!(factor > 0.f)) {   // scores that the maximum of the products does not order
 #pragma unroll
@@ -538,16 +675,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           const float shift = m == -INFINITY ? 0.f : m;
           // weights, their sum, and their terms
           float sum[4] = {};
-          uint32_t hi[32], lo_term[BF16 ? 32 : 1];
+          uint32_t hi[32], lo_term[kSplit ? 32 : 1];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float p0 = exp2_fast(fmaf(x[c][e], by, -shift)), p1 = exp2_fast(fmaf(x[c][e + 1], by, -shift));
+              float p0 = exp2_fast(fmaf(x[c][e], by, -shift)), p1 = exp2_fast(fmaf(x[c][e + 1], by, -shift));
               sum[e / 2 & 3] += p0 + p1;
-              const uint32_t h = pack2<BF16>(p0, p1);
+              if constexpr (T::kEight) {   // (a token that this row does not see but whose scale is NaN: the row is done again)
+                const float2 vs = *reinterpret_cast<const float2*>(t.scales + ((j & 7) * 2 + 1) * kTile + half * 64 + c * 32 + e);
+                p0 *= vs.x;
+                p1 *= vs.y;
+              }
+              const uint32_t h = pack2<kSplit>(p0, p1);
               hi[c * 16 + e / 2] = h;
-              if constexpr (BF16)
+              if constexpr (kSplit)
                 lo_term[c * 16 + e / 2] =
                     pack2<true>(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
             }
@@ -572,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             }
           }
           tmem_st32(lanes + kP + half * 32, hi);
-          if constexpr (BF16) tmem_st32(lanes + kP + 64 + half * 32, lo_term);
+          if constexpr (kSplit) tmem_st32(lanes + kP + 64 + half * 32, lo_term);
           tmem_wait_st();
           tc_fence_before();
         } else {
@@ -672,7 +814,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           const int its_pos = __shfl_sync(0xffffffffu, pos, src), its_lo = __shfl_sync(0xffffffffu, lo, src);
           float4 acc;
           float top, sum;
-          slow_row<BF16>(a, walk.seq, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1), &acc, &top, &sum);
+          slow_row<FMT, QF16>(a, walk.seq, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1), &acc, &top, &sum);
           int64_t its_lse;
           const int64_t its_row = out_at(a, walk.seq, head, row0 + rr, &its_lse);
           if (lane * 4 < D) {
@@ -797,9 +939,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   }
 }
 
-template <bool BF16>
+template <int FMT, bool QF16>
 cudaError_t launch_tc(AttendArgs a, int num_sms, cudaStream_t st) {
-  auto* kernel = attend_tc_kernel<BF16>;
+  constexpr int kSmem = Tc<FMT, QF16>::kSmem;
+  auto* kernel = attend_tc_kernel<FMT, QF16>;
   static std::atomic<bool> ready[kMaxDevices];
   if (a.device >= kMaxDevices || !ready[a.device].load(std::memory_order_relaxed)) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
@@ -819,8 +962,15 @@ cudaError_t launch_tc(AttendArgs a, int num_sms, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_attend_tc(const AttendArgs& a, bool bf16, int num_sms, cudaStream_t st) {
-  return bf16 ? launch_tc<true>(a, num_sms, st) : launch_tc<false>(a, num_sms, st);
+cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st) {
+  switch (format) {
+    case LACACHE_KV_BF16: return launch_tc<LACACHE_KV_BF16, false>(a, num_sms, st);
+    case LACACHE_KV_F16: return launch_tc<LACACHE_KV_F16, true>(a, num_sms, st);
+    case LACACHE_KV_E4M3:
+      return a.q_f16 ? launch_tc<LACACHE_KV_E4M3, true>(a, num_sms, st) : launch_tc<LACACHE_KV_E4M3, false>(a, num_sms, st);
+    default:
+      return a.q_f16 ? launch_tc<LACACHE_KV_INT8, true>(a, num_sms, st) : launch_tc<LACACHE_KV_INT8, false>(a, num_sms, st);
+  }
 }
 
 }  // namespace lc
