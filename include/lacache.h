@@ -509,7 +509,7 @@ lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const lacache_kv_
  * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read the lengths and tables anew. */
 typedef struct {
   int32_t new_tokens;
-  int32_t q_heads; /* a multiple of kv_heads */
+  int32_t q_heads; /* a multiple of kv_heads, at most 65536 */
   int32_t window;  /* 0: none */
   int32_t dtype;
   float scale;

@@ -34,6 +34,7 @@ namespace lc {
 constexpr unsigned int kBadIndex = 1u, kAttendTimeout = 2u;
 constexpr int kMaxHeadDim = LACACHE_MAX_HEAD_DIM;
 constexpr int kMaxNewTokens = 512;
+constexpr int kMaxQHeads = 1 << 16;
 
 struct Rows {   // lacache_rows on the device
   unsigned char* p;

@@ -14,7 +14,7 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   if (at->new_tokens < 1 || at->q_heads < 1 || at->q_heads % c.kv_heads || at->window < 0 || !isfinite(at->scale) ||
       (at->dtype != LACACHE_BF16 && at->dtype != LACACHE_F16))
     return LACACHE_ERR_INVALID_ARG;
-  if (at->new_tokens > lc::kMaxNewTokens || (c.format == LACACHE_KV_BF16 && at->dtype != LACACHE_BF16) ||
+  if (at->new_tokens > lc::kMaxNewTokens || at->q_heads > lc::kMaxQHeads || (c.format == LACACHE_KV_BF16 && at->dtype != LACACHE_BF16) ||
       (c.format == LACACHE_KV_F16 && at->dtype != LACACHE_F16))
     return LACACHE_ERR_UNSUPPORTED;
   if (table->seqs == 0) return LACACHE_OK;
@@ -54,7 +54,7 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   a.status = h->dev_status;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e;
-  if (c.head_dim <= 128 && a.rows > lc::kTcRows) {
+  if (lc::takes_tc(a.rows, a.group, c.head_dim, lc::is_quantised(c.format))) {
     e = lc::launch_attend_tc(a, c.format, h->num_sms, st);
   } else switch (c.format) {
     case LACACHE_KV_BF16: e = lc::launch_attend_bf16(a, h->num_sms, st); break;

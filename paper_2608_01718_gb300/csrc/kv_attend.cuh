@@ -53,7 +53,9 @@ struct AttendArgs {
   int parts;            // blocks the units may be split over (at most the grid)
   int max_len;          // positions the table can name
   int device;
-  int tile_rows, padded;   // the tcgen05 kernel: rows of a tile, and floats of a row of a partial slot
+  // the tcgen05 kernel: rows of a tile, floats of a row of a partial slot, and ceil(2^32 / group)
+  int tile_rows, padded;
+  uint32_t group_mul;
   int64_t pages;
   int64_t page_rows;    // rows of a page: kv_heads x page_size ...
   int64_t page_bytes;   // ... and their bytes
@@ -89,7 +91,13 @@ cudaError_t launch_attend_f16(const AttendArgs& a, int num_sms, cudaStream_t st)
 cudaError_t launch_attend_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
 // The tcgen05 kernel for many rows (kv_attend_tc.cu): heads of up to 128.
-constexpr int kTcRows = 32;   // from more rows than this
+// From how many rows: measured for 4 kv heads (us, warp-level / tcgen05)
+//   bf16, d = 128: 32 x 2,000 tokens, 24 rows 46 / 54, 32 49 / 55, 40 (past the warp-level kernel's tile) 77 / 56
+//   bf16, d = 64: 24 rows 32 / 47, 32 34 / 47
+//   e4m3, d = 128: 16 rows 32 / 61, 24 63 / 61, 32 67 / 61; 2 x 1,000 tokens: 16 15 / 20, 24 26 / 20; d = 64: 32 rows 44 / 51
+inline bool takes_tc(int rows, int group, int head_dim, bool eight) {   // (group: its products with rows fit in 32 bits)
+  return head_dim <= 128 && group <= 2048 && rows > (eight && head_dim > 64 ? 16 : kMaxRowTile);
+}
 cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
 
 namespace {

@@ -39,7 +39,7 @@ constexpr int kSoftmax = 256;                // threads: two a row, half of the 
 constexpr int kMmaWarp = 8;
 constexpr int kLoaders = 96;                 // (twelve warps in all: 168 registers a thread)
 constexpr int kThreads = kSoftmax + 32 + kLoaders;
-constexpr int kCost = 3;                     // a triple's start and end, in units
+constexpr int kCost = 4;                     // a triple's start and end, in units
 constexpr uint32_t kS = 0, kO = 256, kP = 384;   // TMEM columns: two S, O, P (two terms of 64)
 
 // Cache format and q's type. An 8-bit cache's keys are widened to q's type and its values to bf16, both exact.
@@ -267,6 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   const int row_bytes = T::kEight ? D : D * 2;                    // of the cache
   const int slot_floats = kTile * (a.padded + 2);   // of a.partial
 
+  auto by_group = [&](int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_mul); };   // row / group
   Walk walk;
   Line line;
   if (!start_walk(a, walk, line)) return;
@@ -556,14 +557,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     int j = 0;
     uint32_t pairs = 0;
     bool ok = true;
-    // a triple's q into shared memory: begun behind the previous one's last weights, handed over behind its end
+    // a triple's q into shared memory, and its hand-over once it is there
     auto load_q = [&](const Walk& w) {
       const int head = w.triple / a.row_tiles, row0 = (w.triple - head * a.row_tiles) * a.tile_rows;
       const int live = min(a.rows - row0, a.tile_rows);
       const int unit_mul = 65536 / units_row + 1;   // x / units_row = x * unit_mul >> 16 for x < 2048
 #pragma unroll 4
       for (int x = threadIdx.x; x < kTile * units_row; x += kSoftmax) {
-        const int r = (x * unit_mul) >> 16, u = x - r * units_row, row = row0 + r, tok = row / a.group;
+        const int r = (x * unit_mul) >> 16, u = x - r * units_row, row = row0 + r, tok = by_group(row);
         const bool in = r < live;
         copy_async<16>(q_smem + unit_at(r, u),
                        in ? a.q.at((int64_t)w.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) + u * 16 : a.pk, in);
@@ -580,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     for (; ok && !walk.done(); walk.next(a)) {
       const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
       const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
-      const int r = threadIdx.x & (kTile - 1), tok = (row0 + r) / a.group;
+      const int r = threadIdx.x & (kTile - 1), tok = by_group(row0 + r);
       const bool mine = r < live, some = (warp & 3) * 32 < live;
       const int pos = mine ? walk.sp.len - a.new_tokens + tok : INT_MAX;
       int lo = INT_MIN;
@@ -719,9 +720,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           tc_fence_before();
         } else {
           mbar_arrive(smem_u32(&t.s_empty[j & 1]));   // rows past the tile's: their weights are never used
+          // (they wait for the pairs too: two arrivals of theirs in one phase would end it without another thread's)
           mbar_arrive(smem_u32(&t.pair));
-          ++pairs;
-          if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
+          ok = wait(t.pair, pairs++ & 1);
+          if (ok && j > 0) ok = wait(t.pv_done, (j - 1) & 1);
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
@@ -730,7 +732,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         mbar_arrive(smem_u32(&t.p_full));
       }
       if (!ok) break;
-      // every product with this q is done (the last S was complete): the next one's takes its place
+      // with the last S of a triple complete, every product with its q is done: the next one's takes its place, while the
+      // last product with V runs
       Walk next = walk;
       next.next(a);
       const bool more = !next.done();
@@ -742,6 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         break;
       }
       tc_fence_after();
+      if (more) hand_over_q();
       const bool whole = count == walk.sp.units;
       int c_first = blockIdx.x, c_last = blockIdx.x;
       if (!whole) {
@@ -756,7 +760,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       float* slot = a.partial + ((int64_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * slot_floats;
       if (!some) {
         mbar_arrive(smem_u32(&t.pair));
-        ++pairs;
+        ok = wait(t.pair, pairs++ & 1);
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
       } else {
         // this half's dimensions: 32 of every 64
         float o[2][32];
@@ -810,7 +818,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         const int key_end = min(key_begin + count * kTile, walk.sp.hi);
         for (unsigned rows = half ? 0u : __ballot_sync(0xffffffffu, mine && odd); rows; rows &= rows - 1) {
           const int src = __ffs(rows) - 1;
-          const int rr = warp * 32 + src, its_tok = (row0 + rr) / a.group, its_qh = head * a.group + row0 + rr - its_tok * a.group;
+          const int rr = warp * 32 + src, its_tok = by_group(row0 + rr), its_qh = head * a.group + row0 + rr - its_tok * a.group;
           const int its_pos = __shfl_sync(0xffffffffu, pos, src), its_lo = __shfl_sync(0xffffffffu, lo, src);
           float4 acc;
           float top, sum;
@@ -834,7 +842,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       }
       tc_fence_before();
       mbar_arrive(smem_u32(&t.o_empty));
-      if (more) hand_over_q();
     }
   }
 
@@ -952,6 +959,7 @@ cudaError_t launch_tc(AttendArgs a, int num_sms, cudaStream_t st) {
   a.row_tiles = (a.rows + kTile - 1) / kTile;
   a.tile_rows = (a.rows + a.row_tiles - 1) / a.row_tiles;
   a.padded = padded_dim(a.head_dim);
+  a.group_mul = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);   // exact for rows x group < 2^32
   const int64_t units = ((int64_t)a.max_len + 15) / kTile + 1 + kCost;
   const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // cells are counted in 32 bits
