@@ -21,8 +21,10 @@
 // 32 bytes at a time, straight into the lane that uses them, halved the bandwidth of 8-bit caches), and runs it ahead of the
 // products from one triple into the next. Nothing is shared between warps: no barriers in the loop.
 //
-// Softmax. Base 2, running maximum m a row, moved only when a score exceeds it by more than 8: weights then stay below 2^8,
-// the sum is fp32, and most tiles need a vote instead of a maximum over the lanes. Weights: f16 for f16 and 8-bit caches (11
+// Softmax. Base 2, with a reference m a row: 7 below the largest score so far when it is set, and moved only when a score
+// exceeds it by more than 15. Weights then stay below 2^15, the sum is fp32, and most tiles need a vote instead of a maximum
+// over the lanes. (f16 weights have their full 11 bits down to 2^-21 of the largest that way; with a reference at the
+// maximum, keys of small weight and large values lost some of theirs.) Weights: f16 for f16 and 8-bit caches (11
 // bits); on a bf16 cache, whose products need bf16 weights of 8 bits, a weight is split in two bf16 terms (16 bits), as
 // one alone would add an error as large as the output's own rounding.
 //
@@ -78,6 +80,7 @@ struct AttendArgs {
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
 constexpr int kMaxRowTile = 32;
+constexpr float kBelow = 7.f, kHeadroom = 15.f;   // a row's reference below its maximum, and scores above it, in powers of two
 constexpr int kMaxPositions = 1 << 30;      // a table's reach is cut to this
 constexpr int kMaxDevices = 64;
 
@@ -506,7 +509,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       for (int i = 0; i < C::kMTiles; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
       m[n][0] = m[n][1] = -INFINITY;
       l[n][0] = l[n][1] = 0.f;
-      inv[n][0] = inv[n][1] = C::kEight ? 0x1p126f : 1.f;
+      inv[n][0] = inv[n][1] = C::kEight ? 0x1p120f : 1.f;
     }
 
     int key = (sp.lo & ~15) + first_unit * C::kUnit + warp * C::kKeys;
@@ -672,7 +675,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           }
           // m = -inf (nothing seen yet) gives +inf here, and NaN goes the long way too
 #pragma unroll
-          for (int e = 0; e < 4; ++e) move |= !(x2[b][n][e] <= 8.f);
+          for (int e = 0; e < 4; ++e) move |= !(x2[b][n][e] <= kHeadroom);
         }
       }
       if (__any_sync(0xffffffffu, move)) {
@@ -686,12 +689,13 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            float top = m[n][h];
+            float top = -INFINITY;
 #pragma unroll
             for (int b = 0; b < C::kSub; ++b) top = fmaxf(top, fmaxf(x2[b][n][h], x2[b][n][h + 2]));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            top = fmaxf(m[n][h], top - kBelow);
             const float f = m[n][h] == -INFINITY ? 0.f : exp2_fast(m[n][h] - top);
             m[n][h] = top;
             l[n][h] *= f;
@@ -709,7 +713,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           }
         }
       }
-      // weights; in 8-bit formats times v's scales, brought below 2^8 by the row's factor
+      // weights; in 8-bit formats times v's scales, brought below 2^15 by the row's factor
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -736,7 +740,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             }
           }
         }
-        if (__any_sync(0xffffffffu, big > 256.f)) {
+        if (__any_sync(0xffffffffu, big > 32768.f)) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -748,8 +752,8 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-              if (top * inv[n][h] > 1.f) {
-                const float now = __frcp_rn(top), f = now / inv[n][h];
+              if (top * inv[n][h] > 128.f) {
+                const float now = 128.f * __frcp_rn(top), f = now / inv[n][h];
                 inv[n][h] = now;
 #pragma unroll
                 for (int d = 0; d < C::kMTiles; ++d) {

@@ -12,7 +12,7 @@
 //   warps 9-11 (loaders): the tiles of K and V, in turn, into a ring of six 32 KB slots in the 128-byte swizzle layout, by
 //     cp.async (whole 16-byte units of rows found through the page table; masked and missing positions are zeros);
 //   warp 8 (MMA): S of tile j into one of two accumulators, then O += P V of tile j - 1;
-//   warps 0-7 (softmax, two threads a row): a triple's q into shared memory; S from TMEM, base-2 softmax with a maximum that moves only by more than 2^8 (as in
+//   warps 0-7 (softmax, two threads a row): a triple's q into shared memory; S from TMEM, base-2 softmax by a reference that seldom moves (as in
 //     kv_attend.cuh), weights to TMEM as the A operand of the second product; for a bf16 cache in two terms, which the
 //     product sums (one would add an error as large as the output's rounding).
 // K is the first product's B operand as stored (K-major); V, as stored, the second's with its dimensions contiguous
@@ -667,11 +667,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             break;
           }
           const float top = fmaxf(own, t.given[pairs++ & 1][half ^ 1][r]) * by;
-          const bool move = m == -INFINITY ? top > -INFINITY : top > m + 8.f;
-          const float f = move ? exp2_fast(m - top) : 1.f;
+          const bool move = m == -INFINITY ? top > -INFINITY : top > m + kHeadroom;
+          const float f = move ? exp2_fast(m - (top - kBelow)) : 1.f;
           if (move) {
             l *= f;
-            m = top;
+            m = top - kBelow;
           }
           const float shift = m == -INFINITY ? 0.f : m;
           // weights, their sum, and their terms
