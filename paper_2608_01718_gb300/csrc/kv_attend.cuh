@@ -1174,14 +1174,17 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
 
 template <int FMT>
 cudaError_t launch_format(const AttendArgs& a, int num_sms, cudaStream_t st) {
-  const int dp = padded_dim(a.head_dim), nt = a.rows <= 8 ? 1 : a.rows <= 16 || dp == 256 ? 2 : 4;
+  // tiles of 32 rows where takes_tc leaves more than 16 to this kernel (and, at d = 256, registers would spill)
+  constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
+  const int dp = padded_dim(a.head_dim), nt = a.rows <= 8 ? 1 : a.rows <= 16 || dp == 256 || (kEight && dp == 128) ? 2 : 4;
   switch (dp * 8 + nt) {
     case 64 * 8 + 1: return launch_one<FMT, 64, 1>(a, num_sms, st);
     case 64 * 8 + 2: return launch_one<FMT, 64, 2>(a, num_sms, st);
     case 64 * 8 + 4: return launch_one<FMT, 64, 4>(a, num_sms, st);
     case 128 * 8 + 1: return launch_one<FMT, 128, 1>(a, num_sms, st);
     case 128 * 8 + 2: return launch_one<FMT, 128, 2>(a, num_sms, st);
-    case 128 * 8 + 4: return launch_one<FMT, 128, 4>(a, num_sms, st);
+    case 128 * 8 + 4:
+      if constexpr (!kEight) return launch_one<FMT, 128, 4>(a, num_sms, st);
     case 256 * 8 + 1: return launch_one<FMT, 256, 1>(a, num_sms, st);
     default: return launch_one<FMT, 256, 2>(a, num_sms, st);
   }

@@ -30,7 +30,6 @@ namespace lc {
 namespace {
 
 constexpr int kTile = 128;                   // rows of q, and keys, a tile
-constexpr int kAhead = 4;                    // 16-bit caches: slots whose copies are in flight
 constexpr int kStages = 3;                   // 8-bit caches: tiles of codes in flight
 constexpr int kStageBytes = kTile * 128;
 constexpr int kBlockBytes = kTile * 128;     // 64 elements of 128 rows
@@ -53,7 +52,7 @@ struct Tc {
     uint64_t s_full[2], s_empty[2];            // an S is complete; has been read
     uint64_t p_full, pv_done;                  // the weights are stored; their product is done
     uint64_t q_full, o_empty;                  // a triple's q is there; its O has been read
-    uint64_t pair;                             // the two threads of every row have left their part
+    uint64_t pair[4];                          // the two threads of every row of 32 have left their part
     uint64_t drain;
     float given[2][2][kTile];                  // what they leave, in turn and by half: the row's largest product, or at a
                                                // triple's end its sum of weights (NaN: not finite)
@@ -102,15 +101,40 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       : "memory");
 }
 
-// Whether the phase of the given parity is complete, without waiting.
-__device__ __forceinline__ bool test_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
-  return ok != 0;
+}
+
+// Two fp32 at a time: the instruction that bounds the softmax is its issue.
+__device__ __forceinline__ float2 fma_two(float2 x, float2 y, float2 z) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<uint64_t*>(&x)), "l"(*reinterpret_cast<uint64_t*>(&y)), "l"(*reinterpret_cast<uint64_t*>(&z)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 add_two(float2 x, float2 y) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t*>(&x)), "l"(*reinterpret_cast<uint64_t*>(&y)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float max_three(float x, float y, float z) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
+  return d;
+}
+// An arrival of this thread's, once all of its copies so far have landed.
+__device__ __forceinline__ void copies_arrive(uint64_t& bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bar)) : "memory");
+}
+// One arrival for a warp, after what all of its lanes did.
+__device__ __forceinline__ void warp_arrive(uint64_t& bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&bar));
 }
 
 // This block's part of the line of cells: triples in order, each with its first unit and how many units are the block's.
@@ -273,18 +297,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   if (!start_walk(a, walk, line)) return;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(smem_u32(&t.full[s]), kLoaders);
+      mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders / 32 : kLoaders);
       mbar_init(smem_u32(&t.empty[s]), 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(smem_u32(&t.s_full[b]), 1);
-      mbar_init(smem_u32(&t.s_empty[b]), kSoftmax);
+      mbar_init(smem_u32(&t.s_empty[b]), kSoftmax / 32);
     }
-    mbar_init(smem_u32(&t.p_full), kSoftmax);
-    mbar_init(smem_u32(&t.pair), kSoftmax);
+    mbar_init(smem_u32(&t.p_full), kSoftmax / 32);
+    for (int b = 0; b < 4; ++b) mbar_init(smem_u32(&t.pair[b]), 2);
     mbar_init(smem_u32(&t.pv_done), 1);
-    mbar_init(smem_u32(&t.q_full), kSoftmax);
-    mbar_init(smem_u32(&t.o_empty), kSoftmax);
+    mbar_init(smem_u32(&t.q_full), kSoftmax / 32);
+    mbar_init(smem_u32(&t.o_empty), kSoftmax / 32);
     mbar_init(smem_u32(&t.drain), 1);
     t.abort_flag = 0;
     t.pending[0][2] = t.pending[1][2] = -1;
@@ -311,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   if (warp > kMmaWarp) {
     // ---- loaders ----
     const int me = threadIdx.x - kSoftmax - 32;
-    int n = 0, sent = 0;   // slots begun, and handed over
+    int n = 0;   // slots begun
     int units = 0;
     bool ok = true;
     if constexpr (T::kEight) {
@@ -326,12 +350,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         const bool as_f16 = QF16 && !(k & 1);
 #pragma unroll 1
         for (int tile = ((me >> 5) + k) % 3; tile < 8; tile += 3) {
+          uint4 codes[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (lane + 32 * i < tile_pieces) codes[i] = *reinterpret_cast<const uint4*>(from + tile * 2048 + (lane + 32 * i) * 16);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int z = lane + 32 * i, j = (z * piece_mul) >> 16, u = z - j * pieces;
-            if (z >= tile_pieces) break;
-            const uint4 codes = *reinterpret_cast<const uint4*>(from + tile * 2048 + z * 16);
-            const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+            const uint32_t w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
             uint32_t h[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) widen4<FMT>(w[e], h[2 * e], h[2 * e + 1]);
@@ -343,16 +369,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               }
             }
             const int row = tile * 16 + j;
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at(row, 2 * u)), "r"(h[0]), "r"(h[1]),
-                         "r"(h[2]), "r"(h[3])
-                         : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at(row, 2 * u + 1)), "r"(h[4]),
-                         "r"(h[5]), "r"(h[6]), "r"(h[7])
-                         : "memory");
+            if (z < tile_pieces) {
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at(row, 2 * u)), "r"(h[0]), "r"(h[1]),
+                           "r"(h[2]), "r"(h[3])
+                           : "memory");
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at(row, 2 * u + 1)), "r"(h[4]),
+                           "r"(h[5]), "r"(h[6]), "r"(h[7])
+                           : "memory");
+            }
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(smem_u32(&t.full[k % kSlots]));
+        warp_arrive(t.full[k % kSlots]);
       };
       for (; ok && !walk.done(); walk.next(a)) {
         const int head = walk.triple / a.row_tiles, count = walk.units();
@@ -416,10 +444,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       place[i] = units_row == 16 ? unit_at(2 * i + (lane >> 4), lane & 15) : unit_at(4 * i + (lane >> 3), lane & 7);
-    auto hand_over = [&](int upto) {   // slots whose copies have landed
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      for (; sent < upto; ++sent) mbar_arrive(smem_u32(&t.full[sent % kSlots]));
-    };
     for (; ok && !walk.done(); walk.next(a)) {
       const int head = walk.triple / a.row_tiles, count = walk.units();
       const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
@@ -441,16 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         const int live_keys = walk.sp.hi - key, dead_keys = walk.sp.lo - key;   // keys [dead, live) of the tile are read
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv, ++n) {
-          if (n >= kSlots) {
-            // while the slot is in use there is nothing to copy: what has landed is handed over at once
-            const uint32_t bar = smem_u32(&t.empty[n % kSlots]), parity = (n / kSlots - 1) & 1;
-            bool free = __all_sync(0xffffffffu, test_wait(bar, parity));
-            if (!free) copy_wait<3>(), hand_over(n - 3), free = __all_sync(0xffffffffu, test_wait(bar, parity));
-            if (!free) copy_wait<2>(), hand_over(n - 2), free = __all_sync(0xffffffffu, test_wait(bar, parity));
-            if (!free) copy_wait<1>(), hand_over(n - 1), free = __all_sync(0xffffffffu, test_wait(bar, parity));
-            if (!free) copy_wait<0>(), hand_over(n);
-            ok = wait(t.empty[n % kSlots], parity);
-          }
+          if (n >= kSlots) ok = wait(t.empty[n % kSlots], (n / kSlots - 1) & 1);
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
@@ -483,20 +498,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               }
             }
           }
-          copy_commit();
-          if (n < kSlots) {   // the block's first slots, while the memory is idle: two in flight behind the one handed over
-            copy_wait<2>();
-            if (n >= 2) hand_over(n - 1);
-          } else {
-            copy_wait<kAhead>();
-            hand_over(n - kAhead + 1);
-          }
+          copies_arrive(t.full[n % kSlots]);
         }
         ids = next_ids;
       }
     }
     copy_wait<0>();
-    if (!T::kEight && ok) hand_over(n);   // (8-bit tiles were handed over as they were widened)
   } else if (warp == kMmaWarp) {
     // ---- MMA ----
     const uint32_t bf16 = (1u << 7) | (1u << 10);   // both operands' type; f16 is 0
@@ -512,6 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
            (!first_of_triple || of_triple == 0 || wait(t.o_empty, (of_triple - 1) & 1));
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
+      if (!T::kEight) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the copies' writes)
       tc_fence_after();
       const uint32_t v = ring + v_slot * kSlotBytes;
       if (elect_one()) {
@@ -534,6 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
              (j < 2 || wait(t.s_empty[j & 1], ((j >> 1) - 1) & 1));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
+        if (!T::kEight) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_after();
         const uint64_t k_desc = smem_desc(ring + k_slot * kSlotBytes);
         if (elect_one()) {
@@ -574,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     auto hand_over_q = [&] {
       copy_wait<0>();
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(smem_u32(&t.q_full));
+      warp_arrive(t.q_full);
     };
     load_q(walk);
     hand_over_q();
@@ -611,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll
           for (int c = 0; c < 2; ++c) tmem_ld32_wait(u[c]);
           tc_fence_before();
-          mbar_arrive(smem_u32(&t.s_empty[j & 1]));
+          warp_arrive(t.s_empty[j & 1]);
           float (&x)[2][32] = reinterpret_cast<float(&)[2][32]>(u);
           const uint32_t bad = t.bad[j & 15];
           if constexpr (T::kEight) {
@@ -653,15 +662,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           float tops[2];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            tops[c] = x[c][0];
+            tops[c] = fmaxf(x[c][0], x[c][31]);
 #pragma unroll
-            for (int e = 1; e < 32; ++e) tops[c] = fmaxf(tops[c], x[c][e]);
+            for (int e = 1; e < 31; e += 2) tops[c] = max_three(tops[c], x[c][e], x[c][e + 1]);
           }
           // both halves of the row move its maximum, or neither
           const float own = fmaxf(tops[0], tops[1]);
           t.given[pairs & 1][half][r] = own;
-          mbar_arrive(smem_u32(&t.pair));
-          ok = wait(t.pair, pairs & 1);
+          warp_arrive(t.pair[warp & 3]);
+          ok = wait(t.pair[warp & 3], pairs & 1);
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
@@ -675,61 +684,63 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           }
           const float shift = m == -INFINITY ? 0.f : m;
           // weights, their sum, and their terms
-          float sum[4] = {};
-          uint32_t hi[32], lo_term[kSplit ? 32 : 1];
+          float2 sum[2] = {};
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
+            uint32_t hi[16], lo_term[kSplit ? 16 : 1];
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              float p0 = exp2_fast(fmaf(x[c][e], by, -shift)), p1 = exp2_fast(fmaf(x[c][e + 1], by, -shift));
-              sum[e / 2 & 3] += p0 + p1;
+              const float2 y = fma_two(make_float2(x[c][e], x[c][e + 1]), make_float2(by, by), make_float2(-shift, -shift));
+              float2 p = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+              sum[e / 2 & 1] = add_two(sum[e / 2 & 1], p);
               if constexpr (T::kEight) {   // (a token that this row does not see but whose scale is NaN: the row is done again)
                 const float2 vs = *reinterpret_cast<const float2*>(t.scales + ((j & 7) * 2 + 1) * kTile + half * 64 + c * 32 + e);
-                p0 *= vs.x;
-                p1 *= vs.y;
+                p.x *= vs.x;
+                p.y *= vs.y;
               }
-              const uint32_t h = pack2<kSplit>(p0, p1);
-              hi[c * 16 + e / 2] = h;
-              if constexpr (kSplit)
-                lo_term[c * 16 + e / 2] =
-                    pack2<true>(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+              const uint32_t h = pack2<kSplit>(p.x, p.y);
+              hi[e / 2] = h;
+              if constexpr (kSplit) {
+                const float2 rest = fma_two(make_float2(__uint_as_float(h << 16), __uint_as_float(h & 0xffff0000u)),
+                                            make_float2(-1.f, -1.f), p);
+                lo_term[e / 2] = pack2<true>(rest.x, rest.y);
+              }
             }
+            if (c == 0) {   // the last product has used P, and O may be scaled
+              if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
+              if (!__all_sync(0xffffffffu, ok)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+              if (i > 0 && __any_sync(0xffffffffu, move)) {
+#pragma unroll 1
+                for (int d = half * 32; d < D; d += 64) {
+                  uint32_t o[32];
+                  tmem_ld32_issue(lanes + kO + d, o);
+                  tmem_ld32_wait(o);
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                  tmem_st32(lanes + kO + d, o);
+                }
+              }
+            }
+            tmem_st16(lanes + kP + half * 32 + c * 16, hi);
+            if constexpr (kSplit) tmem_st16(lanes + kP + 64 + half * 32 + c * 16, lo_term);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          // the last product has used P, and O may be scaled
+          if (!ok) break;
+          l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+          tmem_wait_st();
+          tc_fence_before();
+        } else {
+          warp_arrive(t.s_empty[j & 1]);   // rows past the tile's: their weights are never used
           if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
             break;
           }
-          tc_fence_after();
-          if (i > 0 && __any_sync(0xffffffffu, move)) {
-#pragma unroll 1
-            for (int c = half * 32; c < D; c += 64) {
-              uint32_t o[32];
-              tmem_ld32_issue(lanes + kO + c, o);
-              tmem_ld32_wait(o);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st32(lanes + kO + c, o);
-            }
-          }
-          tmem_st32(lanes + kP + half * 32, hi);
-          if constexpr (kSplit) tmem_st32(lanes + kP + 64 + half * 32, lo_term);
-          tmem_wait_st();
-          tc_fence_before();
-        } else {
-          mbar_arrive(smem_u32(&t.s_empty[j & 1]));   // rows past the tile's: their weights are never used
-          // (they wait for the pairs too: two arrivals of theirs in one phase would end it without another thread's)
-          mbar_arrive(smem_u32(&t.pair));
-          ok = wait(t.pair, pairs++ & 1);
-          if (ok && j > 0) ok = wait(t.pv_done, (j - 1) & 1);
-          if (!__all_sync(0xffffffffu, ok)) {
-            ok = false;
-            break;
-          }
         }
-        mbar_arrive(smem_u32(&t.p_full));
+        warp_arrive(t.p_full);
       }
       if (!ok) break;
       // with the last S of a triple complete, every product with its q is done: the next one's takes its place, while the
@@ -758,14 +769,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
       }
       float* slot = a.partial + ((int64_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * slot_floats;
-      if (!some) {
-        mbar_arrive(smem_u32(&t.pair));
-        ok = wait(t.pair, pairs++ & 1);
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
-        }
-      } else {
+      if (some) {
         // this half's dimensions: 32 of every 64
         float o[2][32];
         bool odd = false;
@@ -779,8 +783,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           }
         }
         t.given[pairs & 1][half][r] = odd ? __int_as_float(0x7fc00000) : l;
-        mbar_arrive(smem_u32(&t.pair));
-        ok = wait(t.pair, pairs & 1);
+        warp_arrive(t.pair[warp & 3]);
+        ok = wait(t.pair[warp & 3], pairs & 1);
         if (!__all_sync(0xffffffffu, ok)) {
           ok = false;
           break;
@@ -841,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
       }
       tc_fence_before();
-      mbar_arrive(smem_u32(&t.o_empty));
+      warp_arrive(t.o_empty);
     }
   }
 
