@@ -72,19 +72,19 @@ struct AttendArgs {
   const unsigned char* pv;
   const float* ks;
   const float* vs;
-  float* partial;       // two slots a block: [kMaxRowTile rows x DP] sums, then (m, l) a row
+  float* partial;       // two slots a block: [rows of a tile x DP] sums, then (m, l) a row
   unsigned int* arrived;   // blocks that have left their part of the triple that begins in this block; zero between launches
   unsigned int* status;
 };
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
-constexpr int kMaxRowTile = 32;
 constexpr float kBelow = 7.f, kHeadroom = 15.f;   // a row's reference below its maximum, and scores above it, in powers of two
 constexpr int kMaxPositions = 1 << 30;      // a table's reach is cut to this
 constexpr int kMaxDevices = 64;
 
-// Floats of one partial slot, for the largest row tile at a padded head dimension.
+// Floats of one partial slot, for the largest row tile at a padded head dimension. (kMaxBlocksPerSm x 2 slots an SM of up to
+// 32 rows, or 2 of the tcgen05 kernel's 128.)
 constexpr int64_t partial_floats(int padded) { return (int64_t)(padded == 256 ? 16 : 32) * (padded + 2); }
 constexpr int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
@@ -94,12 +94,15 @@ cudaError_t launch_attend_f16(const AttendArgs& a, int num_sms, cudaStream_t st)
 cudaError_t launch_attend_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
 // The tcgen05 kernel for many rows (kv_attend_tc.cu): heads of up to 128.
-// From how many rows: measured for 4 kv heads (us, warp-level / tcgen05)
-//   bf16, d = 128: 32 x 2,000 tokens, 24 rows 46 / 54, 32 49 / 55, 40 (past the warp-level kernel's tile) 77 / 56
-//   bf16, d = 64: 24 rows 32 / 47, 32 34 / 47
-//   e4m3, d = 128: 16 rows 32 / 61, 24 63 / 61, 32 67 / 61; 2 x 1,000 tokens: 16 15 / 20, 24 26 / 20; d = 64: 32 rows 44 / 51
-inline bool takes_tc(int rows, int group, int head_dim, bool eight) {   // (group: its products with rows fit in 32 bits)
-  return head_dim <= 128 && group <= 2048 && rows > (eight && head_dim > 64 ? 16 : kMaxRowTile);
+// From how many rows: measured for 4 kv heads (us, warp-level / tcgen05), at 20 and at 32 rows
+//                   32 x 2,000 tokens   2 x 1,000   4 x 30,000   64 x 100     32 x 2,000   2 x 1,000   4 x 30,000   64 x 100
+//   bf16, d = 128      46 / 47          21 / 18     79 / 71      17 / 19      50 / 47      26 / 18     94 / 69      18 / 19
+//   f16,  d = 128      42 / 40          21 / 16     73 / 63      16 / 16      46 / 40      26 / 16     87 / 62      18 / 16
+//   bf16, d = 64       32 / 37          16 / 14     49 / 57      12 / 17      34 / 37      18 / 14     56 / 57      13 / 17
+//   e4m3, d = 64       39 / 51          18 / 16     54 / 81      14 / 20      42 / 51      20 / 16     62 / 81      15 / 20
+// and up to 16 rows (one tile of the warp-level kernel) its: bf16, d = 128, 15 rows 34 / 49, 16 / 19, 63 / 75, 13 / 19.
+inline bool takes_tc(int rows, int group, int head_dim) {   // (group: its products with rows fit in 32 bits)
+  return head_dim <= 128 && group <= 2048 && rows > (head_dim > 64 ? 16 : 32);
 }
 cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
 
@@ -1174,17 +1177,14 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
 
 template <int FMT>
 cudaError_t launch_format(const AttendArgs& a, int num_sms, cudaStream_t st) {
-  // tiles of 32 rows where takes_tc leaves more than 16 to this kernel (and, at d = 256, registers would spill)
-  constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
-  const int dp = padded_dim(a.head_dim), nt = a.rows <= 8 ? 1 : a.rows <= 16 || dp == 256 || (kEight && dp == 128) ? 2 : 4;
+  // tiles of 32 rows where takes_tc leaves so many to this kernel
+  const int dp = padded_dim(a.head_dim), nt = a.rows <= 8 ? 1 : a.rows <= 16 || dp > 64 ? 2 : 4;
   switch (dp * 8 + nt) {
     case 64 * 8 + 1: return launch_one<FMT, 64, 1>(a, num_sms, st);
     case 64 * 8 + 2: return launch_one<FMT, 64, 2>(a, num_sms, st);
     case 64 * 8 + 4: return launch_one<FMT, 64, 4>(a, num_sms, st);
     case 128 * 8 + 1: return launch_one<FMT, 128, 1>(a, num_sms, st);
     case 128 * 8 + 2: return launch_one<FMT, 128, 2>(a, num_sms, st);
-    case 128 * 8 + 4:
-      if constexpr (!kEight) return launch_one<FMT, 128, 4>(a, num_sms, st);
     case 256 * 8 + 1: return launch_one<FMT, 256, 1>(a, num_sms, st);
     default: return launch_one<FMT, 256, 2>(a, num_sms, st);
   }

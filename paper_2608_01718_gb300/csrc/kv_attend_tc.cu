@@ -379,7 +379,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             }
           }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         warp_arrive(t.full[k % kSlots]);
       };
       for (; ok && !walk.done(); walk.next(a)) {
@@ -519,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
            (!first_of_triple || of_triple == 0 || wait(t.o_empty, (of_triple - 1) & 1));
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
-      if (!T::kEight) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the copies' writes)
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the loaders' writes)
       tc_fence_after();
       const uint32_t v = ring + v_slot * kSlotBytes;
       if (elect_one()) {
@@ -542,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
              (j < 2 || wait(t.s_empty[j & 1], ((j >> 1) - 1) & 1));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        if (!T::kEight) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_after();
         const uint64_t k_desc = smem_desc(ring + k_slot * kSlotBytes);
         if (elect_one()) {
