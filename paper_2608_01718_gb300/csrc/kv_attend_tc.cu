@@ -292,9 +292,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   const int slot_floats = kTile * (a.padded + 2);   // of a.partial
 
   auto by_group = [&](int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_mul); };   // row / group
-  Walk walk;
-  Line line;
-  if (!start_walk(a, walk, line)) return;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders / 32 : kLoaders);
@@ -314,6 +311,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     t.pending[0][2] = t.pending[1][2] = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  Walk walk;
+  Line line;
+  if (!start_walk(a, walk, line)) return;
   if (warp == kMmaWarp) {
     tmem_alloc<false>(smem_u32(&t.tmem), 512);
     tmem_relinquish<false>();
@@ -749,7 +749,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       const bool more = !next.done();
       if (more) load_q(next);
       // ---- the triple's end: O of this block's keys ----
-      ok = wait(t.pv_done, (j - 1) & 1);
+      float total = 0.f;
+      if (some) {   // the row's sum of weights from both halves, while the last product runs
+        t.given[pairs & 1][half][r] = l;
+        warp_arrive(t.pair[warp & 3]);
+        ok = wait(t.pair[warp & 3], pairs & 1);
+        total = t.given[pairs & 1][0][r] + t.given[pairs & 1][1][r];
+        ++pairs;
+      }
+      ok = ok && wait(t.pv_done, (j - 1) & 1);
       if (!__all_sync(0xffffffffu, ok)) {
         ok = false;
         break;
@@ -769,40 +777,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       }
       float* slot = a.partial + ((int64_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * slot_floats;
       if (some) {
-        // this half's dimensions: 32 of every 64
-        float o[2][32];
-        bool odd = false;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int d0 = half * 32 + c * 64;
-          if (d0 < D) {
-            tmem_ld32(lanes + kO + d0, o[c]);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) odd |= d0 + e < D && !(fabsf(o[c][e]) <= 3.402823466e+38f);
-          }
-        }
-        t.given[pairs & 1][half][r] = odd ? __int_as_float(0x7fc00000) : l;
-        warp_arrive(t.pair[warp & 3]);
-        ok = wait(t.pair[warp & 3], pairs & 1);
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
-        }
-        const float total = t.given[pairs & 1][0][r] + t.given[pairs & 1][1][r];
-        ++pairs;
-        odd = !(total <= 3.402823466e+38f);   // a row that is not finite in either half is done again, by the first
         int64_t at_lse = 0, at_row = 0;
         if (mine) at_row = out_at(a, walk.seq, head, row0 + r, &at_lse);
         const float inv = total == 0.f ? 0.f : 1.f / total;
-        if (mine && !odd) {
+        // this half's dimensions: 32 of every 64 (rolled: code that runs once a triple waits for its fetch)
+        float2 zero = make_float2(0.f, 0.f);   // NaN after a product that is not finite
+#pragma unroll 1
+        for (int d0 = half * 32; d0 < D; d0 += 64) {
+          float o[32];
+          tmem_ld32(lanes + kO + d0, o);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
+          for (int e = 0; e < 32; e += 8) {
+            const int d = d0 + e;
+            if (d < D) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              const int d = half * 32 + c * 64 + e;
-              if (d < D) {
-                const float4 y0 = make_float4(o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]);
-                const float4 y1 = make_float4(o[c][e + 4], o[c][e + 5], o[c][e + 6], o[c][e + 7]);
+              for (int x = 0; x < 8; x += 2) zero = fma_two(make_float2(o[e + x], o[e + x + 1]), make_float2(0.f, 0.f), zero);
+              if (mine) {
+                const float4 y0 = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                const float4 y1 = make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);
                 if (whole) {
                   write8(a, at_row, d, y0, y1, inv);
                 } else {
@@ -812,11 +804,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
               }
             }
           }
-          if (half == 0) {
-            if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, total);
-            else if (a.lse) a.lse[at_lse] = lse_of(m, total);
-          }
         }
+        if (mine && half == 0) {
+          if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, total);
+          else if (a.lse) a.lse[at_lse] = lse_of(m, total);
+        }
+        // a row that is not finite in either half is done again, by the first, past what both have written
+        t.given[pairs & 1][half][r] = zero.x + zero.y;
+        warp_arrive(t.pair[warp & 3]);
+        ok = wait(t.pair[warp & 3], pairs & 1);
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          break;
+        }
+        const bool odd = !(t.given[pairs & 1][0][r] + t.given[pairs & 1][1][r] == 0.f && total <= 3.402823466e+38f);
+        ++pairs;
         // rows that are not finite, again
         const int key_end = min(key_begin + count * kTile, walk.sp.hi);
         for (unsigned rows = half ? 0u : __ballot_sync(0xffffffffu, mine && odd); rows; rows &= rows - 1) {
@@ -906,45 +908,41 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     if (a.lse) a.lse[at_lse] = lse_of(top, sum);
   }
   __syncthreads();
-  // eight quads of a row at a time from two blocks: sixteen loads in flight; neighbouring threads on
+  // a thread joins 16 dimensions of a row at a time, from four blocks: sixteen loads in flight; neighbouring threads on
   // neighbouring rows
-  const int r = threadIdx.x & (kTile - 1);
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {
-    const int rows = k ? rows1 : rows0, x = k ? rows0 + r : r;
-    if (r >= rows) continue;
+    const int rows = k ? rows1 : rows0, x0 = k ? rows0 : 0;
     const int blocks = t.pending[k][3] - t.pending[k][2] + 1;
-    const float base_top = joint_top[x], g = joint_inv[x];
 #pragma unroll 1
-    for (int q0 = (threadIdx.x >> 7) * 8; q0 < D / 4; q0 += kThreads / kTile * 8) {   // eight quads: 32 dimensions
-      float4 acc[8];
+    for (int item = threadIdx.x; item < rows * (D / 16); item += kThreads) {
+      const int q0 = item / rows * 4, r = item - q0 / 4 * rows;
+      const float base_top = joint_top[x0 + r], g = joint_inv[x0 + r];
+      float4 acc[4];
 #pragma unroll
-      for (int v = 0; v < 8; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int v = 0; v < 4; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-      for (int c = 0; c < blocks; c += 2) {
-        float4 y[2][8];
-        float w[2];
+      for (int c = 0; c < blocks; c += 4) {
+        float4 y[4][4];
+        float w[4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < 4; ++e) {
           const bool in = c + e < blocks;
           const float4* from = reinterpret_cast<const float4*>(part(k, in ? c + e : 0));
           w[e] = in ? part_ml(k, c + e, r).x : -INFINITY;
 #pragma unroll
-          for (int v = 0; v < 8; ++v)
-            y[e][v] = in && q0 + v < D / 4 ? __ldcg(from + (q0 + v) * kTile + r) : make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int v = 0; v < 4; ++v) y[e][v] = in ? __ldcg(from + (q0 + v) * kTile + r) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < 4; ++e) {
           const float f = exp2_fast(w[e] - base_top);
 #pragma unroll
-          for (int v = 0; v < 8; ++v)
+          for (int v = 0; v < 4; ++v)
             acc[v].x += f * y[e][v].x, acc[v].y += f * y[e][v].y, acc[v].z += f * y[e][v].z, acc[v].w += f * y[e][v].w;
         }
       }
 #pragma unroll
-      for (int v = 0; v < 8; v += 2) {
-        if (q0 + v < D / 4) write8(a, joint_out[x], (q0 + v) * 4, acc[v], acc[v + 1], g);
-      }
+      for (int v = 0; v < 4; v += 2) write8(a, joint_out[x0 + r], (q0 + v) * 4, acc[v], acc[v + 1], g);
     }
   }
 }
