@@ -30,7 +30,7 @@ namespace lc {
 namespace {
 
 constexpr int kTile = 128;                   // rows of q, and keys, a tile
-constexpr int kStages = 3;                   // 8-bit caches: tiles of codes in flight
+constexpr int kStages = 3;                   // 8-bit caches: tiles of codes in flight (five measured 2% slower)
 constexpr int kStageBytes = kTile * 128;
 constexpr int kBlockBytes = kTile * 128;     // 64 elements of 128 rows
 constexpr int kSlotBytes = 2 * kBlockBytes;
@@ -39,17 +39,18 @@ constexpr int kMmaWarp = 8;
 constexpr int kLoaders = 96;                 // (twelve warps in all: 168 registers a thread)
 constexpr int kThreads = kSoftmax + 32 + kLoaders;
 constexpr int kCost = 4;                     // a triple's start and end, in units
-constexpr uint32_t kS = 0, kO = 256, kP = 384;   // TMEM columns: two S, O, P (two terms of 64)
+constexpr uint32_t kS = 0, kO = 256, kQ = 384;   // TMEM columns: two S, O, q (two elements a column)
+constexpr uint32_t kLow = 32;                    // where the weights' second terms lie behind the first, a half of the keys
 
 // Cache format and q's type. An 8-bit cache's keys are widened to q's type and its values to bf16, both exact.
 template <int FMT, bool QF16>
 struct Tc {
   static constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
   static constexpr bool kSplit = FMT != LACACHE_KV_F16;    // bf16 weights, in two terms
-  static constexpr int kSlots = kEight ? 4 : 6;
+  static constexpr int kSlots = kEight ? 4 : 7;
   struct Tail {
-    uint64_t full[6], empty[6];                // a slot's tile is there; its products are done
-    uint64_t s_full[2], s_empty[2];            // an S is complete; has been read
+    uint64_t full[7], empty[7];                // a slot's tile is there; its products are done
+    uint64_t s_full[2];                        // an S is complete
     uint64_t p_full, pv_done;                  // the weights are stored; their product is done
     uint64_t q_full, o_empty;                  // a triple's q is there; its O has been read
     uint64_t pair[4];                          // the two threads of every row of 32 have left their part
@@ -63,7 +64,7 @@ struct Tc {
     // 8-bit caches: a unit's scales of K, then of V (by unit modulo 8)
     alignas(16) float scales[kEight ? 8 * 2 * kTile : 4];   // read four at a time
   };
-  static constexpr int kRing = kSlotBytes, kStage = kRing + kSlots * kSlotBytes;   // offsets in shared memory, after q
+  static constexpr int kStage = kSlots * kSlotBytes;       // offsets in shared memory, after the slots
   static constexpr int kTail = kStage + (kEight ? kStages * kStageBytes : 0);
   static constexpr int kSmem = kTail + (int)sizeof(Tail);
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -85,14 +86,7 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
   desc |= (uint64_t)2 << 61;
   return desc;
 }
-// D += A B with A in shared memory, and with A in TMEM (lane = row, two elements a column).
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
+// D += A B with A in TMEM (lane = row, two elements a column).
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -283,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     if (threadIdx.x == 0) atomicOr(a.status, kAttendTimeout);
     return;
   }
-  const uint32_t q_smem = base, ring = base + T::kRing;
+  const uint32_t ring = base;
   Tail& t = *reinterpret_cast<Tail*>(gbase + T::kTail);
   volatile uint32_t* abort_flag = &t.abort_flag;
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -297,10 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders / 32 : kLoaders);
       mbar_init(smem_u32(&t.empty[s]), 1);
     }
-    for (int b = 0; b < 2; ++b) {
-      mbar_init(smem_u32(&t.s_full[b]), 1);
-      mbar_init(smem_u32(&t.s_empty[b]), kSoftmax / 32);
-    }
+    for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&t.s_full[b]), 1);
     mbar_init(smem_u32(&t.p_full), kSoftmax / 32);
     for (int b = 0; b < 4; ++b) mbar_init(smem_u32(&t.pair[b]), 2);
     mbar_init(smem_u32(&t.pv_done), 1);
@@ -349,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         const uint32_t dst = ring + (k % kSlots) * kSlotBytes;
         const bool as_f16 = QF16 && !(k & 1);
 #pragma unroll 1
-        for (int tile = ((me >> 5) + k) % 3; tile < 8; tile += 3) {
+        for (int tile = ((me >> 5) + k % kStages) % 3; tile < 8; tile += 3) {
           uint4 codes[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -400,11 +391,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           const int live_keys = walk.sp.hi - key, dead_keys = walk.sp.lo - key;
 #pragma unroll 1
           for (int kv = 0; kv < 2 && ok; ++kv, ++n) {
-            // (the stage was widened kStages tiles ago by the same lanes)
+            // (the stage was widened kStages tiles ago, each part by the lanes that fill it now: warps share it out by stage)
             const uint32_t to = base + T::kStage + (n % kStages) * kStageBytes;
             const unsigned char* pool = kv ? a.pv : a.pk;
 #pragma unroll 1
-            for (int tile = ((me >> 5) + n) % 3; tile < 8; tile += 3) {
+            for (int tile = ((me >> 5) + n % kStages) % 3; tile < 8; tile += 3) {
               const int page = __shfl_sync(0xffffffffu, ids, tile), at = key + tile * 16, j0 = tile * 16;
               const int slot = at - (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift) * a.page_size;
               const bool there = (unsigned)page < (unsigned)a.pages;
@@ -508,13 +499,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     const uint32_t bf16 = (1u << 7) | (1u << 10);   // both operands' type; f16 is 0
     const uint32_t qk = (1u << 4) | (QF16 ? 0u : bf16) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
     const uint32_t pv = (1u << 4) | (kSplit ? bf16 : 0u) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
-    const uint64_t q_desc = smem_desc(q_smem);
     int j = 0, triples = 0;    // tiles and triples begun
+    int done = 0;              // products with V that have been waited for
     bool ok = true;
+    auto wait_second = [&](int upto) {   // (before the next one is begun, as each phase has to be seen)
+      for (; ok && done <= upto; ++done) ok = wait(t.pv_done, done & 1);
+    };
     // O (+)= P V of tile k
     auto second = [&](int k, bool first_of_triple, int of_triple) {
       const int v_slot = (2 * k + 1) % kSlots;
-      ok = wait(t.full[v_slot], ((2 * k + 1) / kSlots) & 1) && wait(t.p_full, k & 1) &&
+      wait_second(k - 1);
+      ok = ok && wait(t.full[v_slot], ((2 * k + 1) / kSlots) & 1) && wait(t.p_full, k & 1) &&
            (!first_of_triple || of_triple == 0 || wait(t.o_empty, (of_triple - 1) & 1));
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
@@ -525,8 +520,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll 1
         for (int kk = 0; kk < kTile / 16; ++kk) {
           const uint64_t v_desc = smem_desc_mn(v + kk * 2048);
-          mma_ts(tmem + kO, tmem + kP + kk * 8, v_desc, pv, first_of_triple && kk == 0 ? 0u : 1u);
-          if (kSplit) mma_ts(tmem + kO, tmem + kP + 64 + kk * 8, v_desc, pv, 1u);
+          const uint32_t p = tmem + kS + (k & 1) * kTile + (kk >> 2) * 64 + (kk & 3) * 8;
+          mma_ts(tmem + kO, p, v_desc, pv, first_of_triple && kk == 0 ? 0u : 1u);
+          if (kSplit) mma_ts(tmem + kO, p + kLow, v_desc, pv, 1u);
         }
         mma_commit<false>(smem_u32(&t.empty[v_slot]), 0);
         mma_commit<false>(smem_u32(&t.pv_done), 0);
@@ -537,8 +533,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       const int count = walk.units();
       for (int i = 0; ok && i < count; ++i, ++j) {
         const int k_slot = (2 * j) % kSlots;
-        ok = (i > 0 || wait(t.q_full, triples & 1)) && wait(t.full[k_slot], ((2 * j) / kSlots) & 1) &&
-             (j < 2 || wait(t.s_empty[j & 1], ((j >> 1) - 1) & 1));
+        wait_second(j - 2);   // the weights of tile j - 2 lie where S of tile j goes
+        ok = ok && (i > 0 || wait(t.q_full, triples & 1)) && wait(t.full[k_slot], ((2 * j) / kSlots) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -548,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll 1
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint64_t at = (uint64_t)((kk >> 2) * (kBlockBytes >> 4) + (kk & 3) * 2);
-            mma_ss(tmem + kS + (j & 1) * kTile, q_desc + at, k_desc + at, qk, kk ? 1u : 0u);
+            mma_ts(tmem + kS + (j & 1) * kTile, tmem + kQ + kk * 8, k_desc + at, qk, kk ? 1u : 0u);
           }
           mma_commit<false>(smem_u32(&t.empty[k_slot]), 0);
           mma_commit<false>(smem_u32(&t.s_full[j & 1]), 0);
@@ -565,23 +561,25 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     int j = 0;
     uint32_t pairs = 0;
     bool ok = true;
-    // a triple's q into shared memory, and its hand-over once it is there
+    // a triple's q: this thread's 64 dimensions of its row, into registers, and from there to TMEM
+    uint32_t q_row[32];
     auto load_q = [&](const Walk& w) {
       const int head = w.triple / a.row_tiles, row0 = (w.triple - head * a.row_tiles) * a.tile_rows;
       const int live = min(a.rows - row0, a.tile_rows);
-      const int unit_mul = 65536 / units_row + 1;   // x / units_row = x * unit_mul >> 16 for x < 2048
-#pragma unroll 4
-      for (int x = threadIdx.x; x < kTile * units_row; x += kSoftmax) {
-        const int r = (x * unit_mul) >> 16, u = x - r * units_row, row = row0 + r, tok = by_group(row);
-        const bool in = r < live;
-        copy_async<16>(q_smem + unit_at(r, u),
-                       in ? a.q.at((int64_t)w.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) + u * 16 : a.pk, in);
+      const int r = threadIdx.x & (kTile - 1), row = row0 + r, tok = by_group(row);
+      const uint4* from = reinterpret_cast<const uint4*>(
+          r < live ? a.q.at((int64_t)w.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) : nullptr);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int u = half * 8 + i;
+        const uint4 x = r < live && u < units_row ? from[u] : make_uint4(0, 0, 0, 0);
+        q_row[4 * i] = x.x, q_row[4 * i + 1] = x.y, q_row[4 * i + 2] = x.z, q_row[4 * i + 3] = x.w;
       }
-      copy_commit();
     };
     auto hand_over_q = [&] {
-      copy_wait<0>();
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      if (half * 64 < D) tmem_st32(lanes + kQ + half * 32, q_row);
+      tmem_wait_st();
+      tc_fence_before();
       warp_arrive(t.q_full);
     };
     load_q(walk);
@@ -618,8 +616,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           for (int c = 0; c < 2; ++c) tmem_ld32_issue(lanes + kS + (j & 1) * kTile + half * 64 + c * 32, u[c]);
 #pragma unroll
           for (int c = 0; c < 2; ++c) tmem_ld32_wait(u[c]);
-          tc_fence_before();
-          warp_arrive(t.s_empty[j & 1]);
           float (&x)[2][32] = reinterpret_cast<float(&)[2][32]>(u);
           const uint32_t bad = t.bad[j & 15];
           if constexpr (T::kEight) {
@@ -705,34 +701,30 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
                 lo_term[e / 2] = pack2<true>(rest.x, rest.y);
               }
             }
-            if (c == 0) {   // the last product has used P, and O may be scaled
-              if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
-              if (!__all_sync(0xffffffffu, ok)) {
-                ok = false;
-                break;
-              }
-              tc_fence_after();
-              if (i > 0 && __any_sync(0xffffffffu, move)) {
-#pragma unroll 1
-                for (int d = half * 32; d < D; d += 64) {
-                  uint32_t o[32];
-                  tmem_ld32_issue(lanes + kO + d, o);
-                  tmem_ld32_wait(o);
-#pragma unroll
-                  for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                  tmem_st32(lanes + kO + d, o);
-                }
-              }
-            }
-            tmem_st16(lanes + kP + half * 32 + c * 16, hi);
-            if constexpr (kSplit) tmem_st16(lanes + kP + 64 + half * 32 + c * 16, lo_term);
+            tmem_st16(lanes + kS + (j & 1) * kTile + half * 64 + c * 16, hi);
+            if constexpr (kSplit) tmem_st16(lanes + kS + (j & 1) * kTile + half * 64 + kLow + c * 16, lo_term);
           }
-          if (!ok) break;
           l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+          if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);   // O may be scaled
+          if (!__all_sync(0xffffffffu, ok)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (i > 0 && __any_sync(0xffffffffu, move)) {
+#pragma unroll 1
+            for (int d = half * 32; d < D; d += 64) {
+              uint32_t o[32];
+              tmem_ld32_issue(lanes + kO + d, o);
+              tmem_ld32_wait(o);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st32(lanes + kO + d, o);
+            }
+          }
           tmem_wait_st();
           tc_fence_before();
-        } else {
-          warp_arrive(t.s_empty[j & 1]);   // rows past the tile's: their weights are never used
+        } else {   // rows past the tile's: their weights are never used
           if (j > 0) ok = wait(t.pv_done, (j - 1) & 1);
           if (!__all_sync(0xffffffffu, ok)) {
             ok = false;
