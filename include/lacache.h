@@ -523,7 +523,8 @@ lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_k
                                  const lacache_attention* a, void* cuda_stream);
 
 /* Synchronize the handle's device and report what its kernels found since the previous call: LACACHE_ERR_INVALID_ARG for
- * an index outside its range (see lacache_kv_table). */
+ * an index outside its range (see lacache_kv_table), or LACACHE_ERR_DEVICE_TIMEOUT if an attention gave up waiting within
+ * the GPU (its outputs are then undefined). */
 lacache_status lacache_kv_sync(lacache_kv_t* h);
 
 #ifdef __cplusplus

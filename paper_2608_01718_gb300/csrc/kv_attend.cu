@@ -54,7 +54,7 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   a.status = h->dev_status;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e;
-  if (lc::takes_tc(a.rows, a.group, c.head_dim)) {
+  if (lc::takes_tc(a.rows, a.group, c.head_dim, lc::is_quantised(c.format))) {
     e = lc::launch_attend_tc(a, c.format, h->num_sms, st);
   } else switch (c.format) {
     case LACACHE_KV_BF16: e = lc::launch_attend_bf16(a, h->num_sms, st); break;

@@ -3,9 +3,15 @@
 //
 //   s_j = scale <q, k_j>,  out = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m)   over the visible j
 //
-// A kv head's K and V are read once for all rows that share it: the q heads of its group times the new tokens. With up to
-// 32 rows that is 4 x rows flops a cached element, so the kernel is bound by reading the cache, and every choice below is
-// about keeping enough loads in flight with little work a byte.
+// A kv head's K and V are read once for all rows that share it: the q heads of its group times the new tokens. This kernel
+// is for few rows (takes_tc below has the rule): 4 x rows flops a cached element, so it is bound by reading the cache, and
+// every choice below is about keeping enough loads in flight with little work a byte.
+//
+// Measured (bf16 q, 32 q heads on 8, d = 128, lse written; 6.69 TB/s is a plain copy's rate here): 200,003 tokens of one
+// sequence 129 us, 6.4 TB/s; 32 sequences of 0 to 4,096 50 us, 5.5 TB/s, of which some 8 us are start and joins; e4m3, 64 of 500
+// to 16,384 185 us, 6.2 TB/s. One sequence of 100 tokens (8 heads, d = 64): 5.8 us, a launch, two dependent loads to the
+// first K, and a join. d = 256 with 16 rows (int8, a window of 1,024, 48 sequences): 42 us, 2.4 TB/s: there 255 registers
+// leave two warps a scheduler and widening and products are 25,000 instructions an SM quarter, issued in 35% of the cycles.
 //
 // Products. Both run on the warp-level tensor instruction m16n8k16, with keys (or dimensions) as M and the rows of q as N:
 // a tile of 8 rows wastes nothing at 8 rows, where the 64- or 128-row tiles of tcgen05 would take the scores through TMEM
@@ -94,15 +100,13 @@ cudaError_t launch_attend_f16(const AttendArgs& a, int num_sms, cudaStream_t st)
 cudaError_t launch_attend_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
 // The tcgen05 kernel for many rows (kv_attend_tc.cu): heads of up to 128.
-// From how many rows: measured for 4 kv heads (us, warp-level / tcgen05), at 20 and at 32 rows
-//                   32 x 2,000 tokens   2 x 1,000   4 x 30,000   64 x 100     32 x 2,000   2 x 1,000   4 x 30,000   64 x 100
-//   bf16, d = 128      46 / 47          21 / 18     79 / 71      17 / 19      50 / 47      26 / 18     94 / 69      18 / 19
-//   f16,  d = 128      42 / 40          21 / 16     73 / 63      16 / 16      46 / 40      26 / 16     87 / 62      18 / 16
-//   bf16, d = 64       32 / 37          16 / 14     49 / 57      12 / 17      34 / 37      18 / 14     56 / 57      13 / 17
-//   e4m3, d = 64       39 / 51          18 / 16     54 / 81      14 / 20      42 / 51      20 / 16     62 / 81      15 / 20
-// and up to 16 rows (one tile of the warp-level kernel) its: bf16, d = 128, 15 rows 34 / 49, 16 / 19, 63 / 75, 13 / 19.
-inline bool takes_tc(int rows, int group, int head_dim) {   // (group: its products with rows fit in 32 bits)
-  return head_dim <= 128 && group <= 2048 && rows > (head_dim > 64 ? 16 : 32);
+// From how many rows: measured for 4 kv heads (us, this kernel / tcgen05) over 32 x 2,000 tokens, 2 x 1,000, 4 x 30,000, 64 x 100
+//   bf16, d = 128   16 rows 34 / 36, 16 / 12, 61 / 55, 13 / 15     20 rows 46 / 37, 21 / 12, 79 / 56, 17 / 16
+//   bf16, d = 64    16 rows 23 / 30, 12 / 11, 37 / 50, 10 / 14     20 rows 32 / 30, 16 / 11, 47 / 50, 12 / 14
+//   e4m3, d = 128   16 rows 30 / 51, 15 / 14, 52 / 83, 11 / 18     24 rows 63 / 51, 26 / 14 (a second tile of 16)
+//   e4m3, d = 64    20 rows 39 / 49, 18 / 13, 54 / 77, 14 / 17     32 rows 42 / 49, 20 / 13, 61 / 77, 15 / 17
+inline bool takes_tc(int rows, int group, int head_dim, bool eight) {   // (group: its products with rows fit in 32 bits)
+  return head_dim <= 128 && group <= 2048 && rows > (eight && head_dim <= 64 ? 32 : 16);
 }
 cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
 
@@ -126,7 +130,7 @@ struct AttendConfig {
   static constexpr int kTileBytes = 16 * DP * kItem;                     // K (or V) of 16 keys
   static constexpr int kStageBytes = kSub * 2 * kTileBytes + (kEight ? kKeys * 8 : 0);
   static constexpr int kStages = kStageBytes > 16000 ? (NT == 1 ? 3 : 2) : kStageBytes > 8000 ? 2 : 4;
-  static constexpr int kTripleCost = kStageBytes > 8000 ? (NT == 4 ? 3 : NT) : 2;         // a triple's start and join, in units
+  static constexpr int kTripleCost = kStageBytes > 8000 ? NT : 2;         // a triple's start and join, in units
   static constexpr int kMTiles = DP / 16;
   static constexpr int kQStride = DP * 2 + 64;                           // bytes of a row of q in shared memory
   static constexpr int kRing = kAttendWarps * kStages * kStageBytes;
@@ -1178,11 +1182,14 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
 template <int FMT>
 cudaError_t launch_format(const AttendArgs& a, int num_sms, cudaStream_t st) {
   // tiles of 32 rows where takes_tc leaves so many to this kernel
-  const int dp = padded_dim(a.head_dim), nt = a.rows <= 8 ? 1 : a.rows <= 16 || dp > 64 ? 2 : 4;
+  constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
+  const int dp = padded_dim(a.head_dim), nt = a.rows <= 8 ? 1 : a.rows <= 16 || dp > 64 || !kEight ? 2 : 4;
+  if constexpr (kEight) {
+    if (nt == 4) return launch_one<FMT, 64, 4>(a, num_sms, st);
+  }
   switch (dp * 8 + nt) {
     case 64 * 8 + 1: return launch_one<FMT, 64, 1>(a, num_sms, st);
     case 64 * 8 + 2: return launch_one<FMT, 64, 2>(a, num_sms, st);
-    case 64 * 8 + 4: return launch_one<FMT, 64, 4>(a, num_sms, st);
     case 128 * 8 + 1: return launch_one<FMT, 128, 1>(a, num_sms, st);
     case 128 * 8 + 2: return launch_one<FMT, 128, 2>(a, num_sms, st);
     case 256 * 8 + 1: return launch_one<FMT, 256, 1>(a, num_sms, st);

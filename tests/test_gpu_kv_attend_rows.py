@@ -1,5 +1,5 @@
 """Attention of many rows a kv head (a window of drafts times a group of heads) against the fp64 oracle: the kernel that takes
-more than 32 rows, or more than 16 over an 8-bit cache with heads past 64."""
+more than 16 rows, or more than 32 over an 8-bit cache with heads of up to 64."""
 import numpy as np
 import pytest
 import torch
