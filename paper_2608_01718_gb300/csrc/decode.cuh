@@ -289,54 +289,94 @@ __device__ __forceinline__ void rotate(float (&x0)[8], float (&x1)[8], const Chu
   }
 }
 
+// Two fp32 at a time (kernels here that wait for memory least are bound by their instructions' issue), and the largest
+// magnitude of three (NaN if one is).
+__device__ __forceinline__ uint64_t bits_of(float2 x) { return (uint64_t)__float_as_uint(x.y) << 32 | __float_as_uint(x.x); }
+__device__ __forceinline__ float2 pair_of(uint64_t u) {
+  return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
+}
+__device__ __forceinline__ float2 fma_two(float2 x, float2 y, float2 z) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits_of(x)), "l"(bits_of(y)), "l"(bits_of(z)));
+  return pair_of(d);
+}
+__device__ __forceinline__ float2 mul_two(float2 x, float2 y) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(x)), "l"(bits_of(y)));
+  return pair_of(d);
+}
+__device__ __forceinline__ float2 add_two(float2 x, float2 y) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(x)), "l"(bits_of(y)));
+  return pair_of(d);
+}
+__device__ __forceinline__ float largest(float x, float y, float z) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
+  return d;
+}
+
 // The row's scale in an 8-bit format, amax / top by an IEEE division; NaN for a row that holds an infinity or a NaN (its codes
 // are 0).
 template <int FMT>
 __device__ __forceinline__ float row_scale(const float (&x0)[8], const float (&x1)[8], int lanes) {
-  // magnitudes order as their bits do, infinity and NaN above the finite ones
-  uint32_t m = 0;
+  float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(max(m, __float_as_uint(x0[i]) & 0x7fffffffu), __float_as_uint(x1[i]) & 0x7fffffffu);
-  for (int o = lanes >> 1; o; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-  return m >= 0x7f800000u ? __int_as_float(0x7fc00000)
-                          : __fdiv_rn(__uint_as_float(m), FMT == LACACHE_KV_E4M3 ? 448.f : 127.f);
+  for (int i = 0; i < 8; ++i) m = largest(m, x0[i], x1[i]);
+  for (int o = lanes >> 1; o; o >>= 1) {
+    const float y = __shfl_xor_sync(0xffffffffu, m, o);
+    m = largest(m, y, y);
+  }
+  return m < INFINITY ? __fdiv_rn(m, FMT == LACACHE_KV_E4M3 ? 448.f : 127.f) : __int_as_float(0x7fc00000);
 }
 // x / scale correctly rounded, from r = 1 / scale correctly rounded: two of Markstein's corrections (P. Markstein,
 // "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): the first makes the quotient faithful,
 // the second, from an exact remainder, correctly rounded. For scales within 2^+-100, where nothing under- or overflows
 // (remainders below that belong to quotients whose code is 0).
-__device__ __forceinline__ float quotient(float x, float scale, float r) {
-  float q = __fmul_rn(x, r);
-  q = __fmaf_rn(__fmaf_rn(-q, scale, x), r, q);
-  return __fmaf_rn(__fmaf_rn(-q, scale, x), r, q);
+__device__ __forceinline__ float2 quotients(float2 x, float scale, float r) {
+  const float2 s = make_float2(-scale, -scale), t = make_float2(r, r);
+  float2 q = mul_two(x, t);
+  q = fma_two(fma_two(q, s, x), t, q);
+  return fma_two(fma_two(q, s, x), t, q);
+}
+// The same for other scales. (A quotient of a plain scale is at most top, but for a rounding; a subnormal scale may be too
+// small for its row.)
+template <int FMT>
+__device__ __noinline__ void far_quotients(float (&u)[8], float scale) {
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) {
+    u[i] = __fdiv_rn(u[i], scale);
+    if (FMT == LACACHE_KV_INT8) u[i] = fminf(fmaxf(u[i], -127.f), 127.f);
+  }
 }
 // Codes of eight elements: x / scale (IEEE) to nearest, ties to even.
 template <int FMT>
 __device__ __forceinline__ uint2 quantise8(const float (&x)[8], float scale, float r) {
   if (!(scale > 0.f)) return make_uint2(0, 0);
-  float u[8];
-  const bool plain = scale > 0x1p-100f && scale < 0x1p100f;
+  float2 u[4];
+  if (scale > 0x1p-100f && scale < 0x1p100f) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) u[i] = plain ? quotient(x[i], scale, r) : __fdiv_rn(x[i], scale);
-  // (a plain quotient is at most top, but for a rounding; a subnormal scale may be too small for its row)
-  if (FMT == LACACHE_KV_INT8 && !plain) {
+    for (int i = 0; i < 4; ++i) u[i] = quotients(make_float2(x[2 * i], x[2 * i + 1]), scale, r);
+  } else {
+    float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = fminf(fmaxf(u[i], -127.f), 127.f);
+    for (int i = 0; i < 8; ++i) y[i] = x[i];
+    far_quotients<FMT>(y, scale);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = make_float2(y[2 * i], y[2 * i + 1]);
   }
   uint32_t w[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const float* v = u + 4 * k;
     if (FMT == LACACHE_KV_E4M3) {
-      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
-      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(u[2 * k], __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(u[2 * k + 1], __NV_SATFINITE, __NV_E4M3);
       w[k] = lo | hi << 16;
     } else {
       // adding 1.5 x 2^23 rounds to an integer in the low bits of the sum
-      uint32_t b[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(__fadd_rn(v[i], 12582912.f));
-      w[k] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+      const float2 big = make_float2(12582912.f, 12582912.f), a = add_two(u[2 * k], big), b = add_two(u[2 * k + 1], big);
+      w[k] = __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
+                         __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
     }
   }
   return make_uint2(w[0], w[1]);

@@ -110,19 +110,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 
-// Two fp32 at a time: the instruction that bounds the softmax is its issue.
-__device__ __forceinline__ float2 fma_two(float2 x, float2 y, float2 z) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(d)
-      : "l"(*reinterpret_cast<uint64_t*>(&x)), "l"(*reinterpret_cast<uint64_t*>(&y)), "l"(*reinterpret_cast<uint64_t*>(&z)));
-  return *reinterpret_cast<float2*>(&d);
-}
-__device__ __forceinline__ float2 add_two(float2 x, float2 y) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t*>(&x)), "l"(*reinterpret_cast<uint64_t*>(&y)));
-  return *reinterpret_cast<float2*>(&d);
-}
 __device__ __forceinline__ float max_three(float x, float y, float z) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
