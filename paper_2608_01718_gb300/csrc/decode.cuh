@@ -70,8 +70,8 @@ inline bool device_table(const lacache_kv_table* t, Table* out) {
 
 // The row kernels give a warp a group of tokens and a slab of their rows, kRowUnroll passes of 32 / lanes rows in flight. Few
 // tokens are cut into slabs of at least one pass, until the warps fill the GPU; of many, a warp of the cache's kernels takes
-// up to kRowGroup, whose places its lanes look up at once (write of 12,001 tokens of 48 rows: one 68.6 us, four 63.4; read
-// of 60,000 of 16 rows: one 69.0 us, two 64.4, four 63.1). Beyond that there are more blocks than the GPU holds.
+// up to kRowGroup, whose places its lanes look up at once (write of 12,001 tokens of 48 rows: one 57.1 us, two 54.4, four
+// 52.4; read of 60,000 of 16 rows: one 69.7, two 65.1, four 63.9, eight 72.8). Beyond that there are more blocks than the GPU holds.
 constexpr int kRowThreads = 128;
 constexpr int kRowUnroll = 2;
 constexpr int kRowGroup = 4;
