@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   auto by_group = [&](int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_mul); };   // row / group
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders / 32 : kLoaders);
+      mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders / 32 : kLoaders + 1);
       mbar_init(smem_u32(&t.empty[s]), 1);
     }
     for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&t.s_full[b]), 1);
@@ -483,6 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             }
           }
           copies_arrive(t.full[n % kSlots]);
+          if (me == 0) mbar_arrive(smem_u32(&t.full[n % kSlots]));   // for t.bad, which no copy writes
         }
         ids = next_ids;
       }

@@ -550,14 +550,21 @@ class LaCache:
         return lacache_last_launch(self.h)
 
 
-_DTYPES: dict = {}   # torch dtype -> lacache_dtype, filled on first use (torch is imported late)
+# What the calls that decode token by token need of torch, which is imported late: a call's every look-up of it would be a
+# tenth of the call.
+_DTYPES: dict = {}   # torch dtype -> lacache_dtype
+_INT32 = _RAW_STREAM = None
+
+
+def _bind_torch() -> None:
+    global _INT32, _RAW_STREAM
+    import torch
+    _DTYPES.update({torch.bfloat16: LACACHE_BF16, torch.float16: LACACHE_F16, torch.float32: LACACHE_F32})
+    _INT32, _RAW_STREAM = torch.int32, getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _dtype(t) -> int:
     """The lacache_dtype of a tensor's elements."""
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.bfloat16: LACACHE_BF16, torch.float16: LACACHE_F16, torch.float32: LACACHE_F32})
     got = _DTYPES.get(t.dtype)
     if got is None:
         raise ValueError(f"rows are bf16, f16 or f32, not {t.dtype}")
@@ -566,11 +573,9 @@ def _dtype(t) -> int:
 
 def _current_stream(cuda_stream, device: int) -> int:
     """As _stream, for the calls that decode token by token: torch's raw handle where it offers one (a microsecond less)."""
-    if cuda_stream is not None:
-        return _stream(cuda_stream)
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw is not None else _stream(None, device)
+    if cuda_stream is None and _RAW_STREAM is not None:
+        return _RAW_STREAM(device)
+    return _stream(cuda_stream, device)
 
 
 def _rows(name: str, t, n: int, heads: int, head_dim: int, device: int, dtype) -> lacache_rows:
@@ -585,8 +590,7 @@ def _rows(name: str, t, n: int, heads: int, head_dim: int, device: int, dtype) -
 
 def _index(name: str, t, n: int, device: int) -> int:
     """An int32 [n] CUDA tensor's address."""
-    import torch
-    if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != device:
+    if t.dtype != _INT32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != device:
         raise ValueError(f"{name} is a dense int32 tensor of {n} on cuda:{device}")
     return t.data_ptr()
 
@@ -610,15 +614,16 @@ class Rope:
                  "banded": LACACHE_ROPE_BANDED}
         if scaling not in modes:
             raise ValueError(f"scaling is one of {list(modes)}, not {scaling!r}")
+        _bind_torch()
         self.plan = lacache_rope_init(rot_dim, LACACHE_ROPE_INTERLEAVED if interleaved else LACACHE_ROPE_HALF, base,
                                       modes[scaling], factor, original_len, low_turns, high_turns, amplitude)
 
     def apply(self, x, pos, inverse: bool = False, out=None, cuda_stream=None):
         """x [n x heads x head_dim] rotated at ``pos`` (int32 [n]) into ``out`` (new if None; x itself for in place).
         ``inverse``: the transpose, which is the gradient."""
-        import torch
         n, heads, head_dim = _three("x", x)
         device, dtype = x.get_device(), x.dtype
+        import torch
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
         args = (self.plan, n, heads, head_dim, _dtype(x), _rows("x", x, n, heads, head_dim, device, dtype),
@@ -655,7 +660,8 @@ class KVCache:
             raise ValueError(f"format is one of {list(self.FORMATS)}, not {format!r}")
         self.cfg = lacache_kv_config(layers, kv_heads, head_dim, page_size, pages, self.FORMATS[format], device)
         self.format, self.device = format, device
-        self.h = lacache_kv_create(self.cfg)
+        _bind_torch()
+        self.h, self._lib = lacache_kv_create(self.cfg), load()
 
     def close(self) -> None:
         if self.h:
@@ -692,8 +698,7 @@ class KVCache:
         return out
 
     def _table(self, table) -> lacache_kv_table:
-        import torch
-        if table.dim() != 2 or table.dtype != torch.int32 or table.stride(1) != 1 or table.get_device() != self.device:
+        if table.dim() != 2 or table.dtype != _INT32 or table.stride(1) != 1 or table.get_device() != self.device:
             raise ValueError(f"a table is an int32 [sequences x pages] tensor on cuda:{self.device} with dense rows")
         seqs, width = table.shape
         return lacache_kv_table(table.data_ptr(), table.stride(0), seqs, width)
@@ -710,11 +715,13 @@ class KVCache:
                 import torch
                 q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
             rq, ro = _rows("q", q, n, q_heads, D, dev, dtype), _rows("q_out", q_out, n, q_heads, D, dev, dtype)
-        lacache_kv_append(self.h, layer, self._table(table), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
-                          None if rope is None else rope.plan,
-                          None if rope_pos is None else _index("rope_pos", rope_pos, n, dev), _dtype(k),
-                          _rows("k", k, n, heads, D, dev, dtype), _rows("v", v, n, heads, D, dev, dtype), q_heads, rq, ro,
-                          _current_stream(cuda_stream, dev))
+        t, rk, rv = self._table(table), _rows("k", k, n, heads, D, dev, dtype), _rows("v", v, n, heads, D, dev, dtype)
+        at = ctypes.addressof
+        _check("lacache_kv_append", self._lib.lacache_kv_append(
+            self.h, layer, at(t), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
+            None if rope is None else at(rope.plan), None if rope_pos is None else _index("rope_pos", rope_pos, n, dev),
+            _dtype(k), at(rk), at(rv), q_heads, None if rq is None else at(rq), None if ro is None else at(ro),
+            _current_stream(cuda_stream, dev)))
         return q_out
 
     def read(self, seq, pos, table, layer: int = 0, dtype=None, k_out=None, v_out=None, cuda_stream=None):
@@ -751,7 +758,8 @@ class KVCache:
                               None if starts is None else _index("starts", starts, t.seqs, dev),
                               _rows("q", q, n, heads, D, dev, dtype), _rows("out", out, n, heads, D, dev, dtype),
                               None if lse is None else lse.data_ptr())
-        lacache_kv_attend(self.h, layer, t, a, _current_stream(cuda_stream, dev))
+        _check("lacache_kv_attend", self._lib.lacache_kv_attend(self.h, layer, ctypes.addressof(t), ctypes.addressof(a),
+                                                                _current_stream(cuda_stream, dev)))
         return out
 
     def sync(self) -> None:
