@@ -403,12 +403,24 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
         // 32 units of 16 bytes a copy, neighbouring lanes on neighbouring units: rows are requested in whole lines
         const uint32_t kd = at + s * 2 * C::kTileBytes, vd = kd + C::kTileBytes;
         const int unit = lane % C::kUnits, first = lane / C::kUnits;
-        if (D == DP && page >= 0 && k0 >= ahead.sp.lo && k0 + 16 <= ahead.sp.hi) {   // nothing to leave out: most tiles
+        // (most tiles: no key to leave out. With D == DP's constants apart d = 256 is 4% faster; without the second form, heads
+        // of 192 were 176 us instead of 124 over 64 x 4,000 tokens, 4 rows, bf16)
+        const bool full = page >= 0 && k0 >= ahead.sp.lo && k0 + 16 <= ahead.sp.hi;
+        if (full && D == DP) {
 #pragma unroll
           for (int i = 0; i < C::kCopies; ++i) {
             const int j = i * C::kCopyRows + first;
             copy_async<16>(kd + k_unit<C::kRowBytes>(j, unit), kp + i * 512 + lane * 16, true);
             copy_async<16>(vd + v_unit<C::kRowBytes, C::kEight>(j, unit), vp + i * 512 + lane * 16, true);
+          }
+        } else if (full) {
+          const bool live = unit * 16 < row_bytes;                        // (past the row's end: zeros)
+          const int from = first * row_bytes + unit * 16, step = C::kCopyRows * row_bytes;
+#pragma unroll
+          for (int i = 0; i < C::kCopies; ++i) {
+            const int j = i * C::kCopyRows + first;
+            copy_async<16>(kd + k_unit<C::kRowBytes>(j, unit), kp + from + i * step, live);
+            copy_async<16>(vd + v_unit<C::kRowBytes, C::kEight>(j, unit), vp + from + i * step, live);
           }
         } else {
 #pragma unroll 1
