@@ -498,9 +498,8 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   float factor[NT][2];
   uint4 qreg[kQInRegs ? NT * C::kKPieces * (C::kEight ? 2 : 1) : 1];
   int all_hi = 0, all_lo = 0;   // positions that every live row sees: [all_lo, all_hi]
-  const bool rows_differ = a.new_tokens > 1;
-  bool fresh = true, redo = false;   // the copies start here; the triple's products are done again
-  bool split = kBf16;                // bf16 weights in two terms
+  bool fresh = true;                 // the copies start here
+  bool careful = false;              // the triple's products are done again, V's values that are not finite apart
   int slot = 0;                      // of the unit whose products are next
   while (left > 0) {
     const int head = triple / a.row_tiles, tile = triple % a.row_tiles;
@@ -508,7 +507,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     const int row0 = tile * C::kRows;
     const int live_rows = a.rows - row0 < C::kRows ? a.rows - row0 : C::kRows;
     if (fresh) {
-      if (!redo) load_q_early(seq, triple);   // before the copies, which would keep it waiting
+      if (!careful) load_q_early(seq, triple);   // before the copies, which would keep it waiting
       copy_wait<0>();
       __syncwarp();
       ahead.left = left;
@@ -535,7 +534,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     for (int i = fresh ? 1 - C::kStages : 0; i < units; ++i) {
       issue();
       if (i < 0) continue;   // the copies' head start
-      if (i == 0 && !redo) {
+      if (i == 0 && !careful) {
         // ---- q into shared memory, in the order of the K pieces ----
         if constexpr (!kQEarly) copy_wait<1>();   // all but the newest copies: q's lie before them
         if (threadIdx.x == 0) {
@@ -811,9 +810,9 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
         }
         const unsigned char* vt = st + b * 2 * C::kTileBytes + C::kTileBytes;
         if constexpr (!C::kEight) {
-          if (some_masked && rows_differ) {
-            // a value that is not finite at a position that only some rows see: the product would put 0 x it into the
-            // others. It is added here for the rows that see it, and taken out of the tile.
+          if (careful) {
+            // a value that is not finite: a product would put 0 x it into the rows that do not see it, and into those whose
+            // weight has a term that is 0. It is added here for the rows that see it, and taken out of the tile.
             constexpr uint32_t ones = kBf16 ? 0x7f80u : 0x7c00u;
             bool fix = false;
 #pragma unroll 1
@@ -861,9 +860,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             mma16816<kBf16>(o[d][n], a0, a1, a2, a3, p0[n], p1[n]);
-            if constexpr (kBf16) {
-              if (split) mma16816<true>(o[d][n], a0, a1, a2, a3, r0[n], r1[n]);
-            }
+            if constexpr (kBf16) mma16816<true>(o[d][n], a0, a1, a2, a3, r0[n], r1[n]);
           }
         };
         if constexpr (C::kEight) {
@@ -913,25 +910,25 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     }
     fresh = false;
 
-    if constexpr (kBf16) {
-      // an infinity of V times a weight's second term, which may be zero, gives NaN: such a triple is done again with
-      // weights of one term
+    if constexpr (!C::kEight) {
+      // an output that is not finite: a value of V may have reached rows that do not see it, or met a weight's term that is
+      // 0. This warp's part of the triple is done again, such values apart (and again only once: they may be seen)
       bool odd = false;
 #pragma unroll
-      for (int d = 0; d < C::kMTiles; ++d) {
+      for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int e = 0; e < 4; ++e) {
+          bool some = false;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[d][n][e]) <= 3.402823466e+38f);
+          for (int d = 0; d < C::kMTiles; ++d) some |= !(fabsf(o[d][n][e]) <= 3.402823466e+38f);
+          odd |= some && n * 8 + 2 * t + (e & 1) < live_rows;
         }
       }
-      if (split && __any_sync(0xffffffffu, odd)) {
-        split = false;
-        redo = fresh = true;
+      if (!careful && __any_sync(0xffffffffu, odd)) {
+        careful = fresh = true;
         continue;
       }
-      split = true;
-      redo = false;
+      careful = false;
     }
 
     const int of_seq = seq, of_triple = triple, of_units = sp.units, of_base = seq_base;

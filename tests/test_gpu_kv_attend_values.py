@@ -1,0 +1,87 @@
+"""Attention over values that are not finite, very large, or of very different magnitudes, against the fp64 oracle: what only
+some rows see, what a weight rounded to fewer bits would lose, and what an unnormalised sum would."""
+import numpy as np
+import pytest
+import torch
+
+from kv_cases import Filled, TORCH, bounds
+from oracle import decode
+from paper_2608_01718_gb300 import build
+from paper_2608_01718_gb300 import lacache as L
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a CUDA device")
+    build.build()
+    L.load()
+
+
+def rows_along_first(scores, head_dim, dtype):
+    """Rows whose product with (1, 0, 0, ...) is `scores` [n x heads]; their other elements are small and random."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    s = torch.as_tensor(scores, dtype=torch.float32, device="cuda")
+    x = torch.randn(*s.shape, head_dim, generator=gen, device="cuda") / 64
+    x[..., 0] = s
+    return x.to(dtype)
+
+
+def first(n, heads, head_dim, dtype):
+    q = torch.zeros(n, heads, head_dim, device="cuda", dtype=dtype)
+    q[..., 0] = 1
+    return q
+
+
+# rows a kv head: eight, nine to sixteen, and the many-row kernel's
+ROWS = [(1, 4), (3, 4), (9, 4)]
+
+
+@pytest.mark.parametrize("new,group", ROWS)
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_an_infinity_under_a_weight_that_f16_rounds_to_zero(new, group, head_dim):
+    # its weight is 2^-43 of the largest: below f16's range, but not zero, so the output is an infinity and not 0 x inf
+    c = Filled("f16", [290], 1, head_dim, seed=20)
+    scores = torch.zeros(290, 1)
+    scores[5] = -30.0
+    v = c.v_rows.clone()
+    v[5, 0, 3], v[5, 0, 9] = float("inf"), -float("inf")
+    c.kv.append(rows_along_first(scores, head_dim, torch.float16), v, c.seq, c.pos, c.table)
+    out = c.kv.attend(first(new, group, head_dim, torch.float16), c.table, c.len_dev, new_tokens=new, scale=1.0)
+    c.kv.sync()
+    assert (out[..., 3] == float("inf")).all() and (out[..., 9] == -float("inf")).all()
+    rest = [d for d in range(head_dim) if d not in (3, 9)]
+    k, vv = c.values()
+    vv[0][5, 0, [3, 9]] = 0.0
+    q = first(new, group, head_dim, torch.float64).cpu().numpy()
+    want, lse, mass, span = decode.attend(q, k, vv, c.lengths, new, 1.0)
+    tol, _ = bounds(want, mass, span, lse, q, k, 1.0, "f16")
+    assert np.all((np.abs(out.double().cpu().numpy() - want) <= tol)[..., rest])
+
+
+@pytest.mark.parametrize("new,group", ROWS)
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_weights_keep_their_bits_beside_an_infinity(new, group, head_dim):
+    """bf16: one dimension of one value is an infinity; the other dimensions are as exact as without it. A weight's two bf16
+    terms leave 2^-18 of it, the scores' error delta (kv_cases.bounds) 4 delta; the output rounds to within 2^-8 of itself."""
+    c = Filled("bf16", [290], 1, head_dim, seed=21)
+    v = c.v_rows.clone()
+    v[100, 0, 3] = float("inf")
+    c.kv.append(c.k_rows, v, c.seq, c.pos, c.table)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    q = torch.randn(new, group, head_dim, generator=gen, device="cuda").bfloat16()
+    out = c.kv.attend(q, c.table, c.len_dev, new_tokens=new, scale=head_dim ** -0.5)
+    c.kv.sync()
+    assert (out[..., 3] == float("inf")).all()
+    k, vv = c.values()
+    vv[0][100, 0, 3] = 0.0
+    hq = q.double().cpu().numpy()
+    want, lse, mass, span = decode.attend(hq, k, vv, c.lengths, new, head_dim ** -0.5)
+    delta = 2.0 ** -19 * span
+    tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -17 + 4 * delta)[..., None] * mass
+    rest = [d for d in range(head_dim) if d != 3]
+    assert np.all((np.abs(out.double().cpu().numpy() - want) <= tol)[..., rest])
