@@ -856,6 +856,47 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             }
           }
         }
+        if constexpr (FMT == LACACHE_KV_E4M3) {
+          if (careful) {
+            // the same for codes that are no numbers (the only ones of the format that are not finite)
+            unsigned char* codes = ring + slot * C::kStageBytes + b * 2 * C::kTileBytes + C::kTileBytes;
+            auto no_numbers = [](uint32_t x) { return __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu); };
+            bool fix = false;
+#pragma unroll 1
+            for (int i = 0; i < C::kTileBytes / 128; ++i) fix |= no_numbers(reinterpret_cast<const uint32_t*>(codes)[i * 32 + lane]) != 0;
+            if (__any_sync(0xffffffffu, fix)) {
+              const int k0 = key + 16 * b;
+#pragma unroll 1
+              for (int j = 0; j < 16; ++j) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                  const int r = n * 8 + 2 * t;
+                  const bool see0 = k0 + j <= row_pos[r] && k0 + j >= row_lo[r];
+                  const bool see1 = k0 + j <= row_pos[r + 1] && k0 + j >= row_lo[r + 1];
+#pragma unroll
+                  for (int d = 0; d < C::kMTiles; ++d) {   // as write_quad: tile d's two codes of this lane group's bytes
+                    constexpr int kPer = C::kVBytes / 2;
+                    const int at = C::kVBytes == 16 ? v_unit<C::kRowBytes, true>(j, 8 * (d / kPer) + g) + 2 * (d % kPer)
+                                                    : v_unit<C::kRowBytes, true>(j, g >> 1) + (g & 1) * 8 + 2 * d;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                      if ((codes[at + x] & 0x7f) != 0x7f) continue;
+                      if (see0) o[d][n][2 * x] = NAN;
+                      if (see1) o[d][n][2 * x + 1] = NAN;
+                    }
+                  }
+                }
+              }
+              __syncwarp();
+#pragma unroll 1
+              for (int i = 0; i < C::kTileBytes / 128; ++i) {
+                uint32_t& x = reinterpret_cast<uint32_t*>(codes)[i * 32 + lane];
+                x &= ~no_numbers(x);
+              }
+              __syncwarp();
+            }
+          }
+        }
         auto product = [&](int d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
@@ -910,7 +951,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     }
     fresh = false;
 
-    if constexpr (!C::kEight) {
+    if constexpr (FMT != LACACHE_KV_INT8) {
       // an output that is not finite: a value of V may have reached rows that do not see it, or met a weight's term that is
       // 0. This warp's part of the triple is done again, such values apart (and again only once: they may be seen)
       bool odd = false;

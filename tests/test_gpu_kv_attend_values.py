@@ -85,3 +85,36 @@ def test_weights_keep_their_bits_beside_an_infinity(new, group, head_dim):
     tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -17 + 4 * delta)[..., None] * mass
     rest = [d for d in range(head_dim) if d != 3]
     assert np.all((np.abs(out.double().cpu().numpy() - want) <= tol)[..., rest])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,group", [(2, 1), (4, 2), (4, 4), (8, 4), (9, 4)])
+@pytest.mark.parametrize("head_dim", [48, 64, 80, 128, 256])
+def test_codes_that_are_no_numbers_stay_in_the_rows_that_see_them(dtype, new, group, head_dim):
+    """e4m3: NaN codes in V (0x7f and 0xff; a pool filled by a page copy or another quantiser may hold them) of the last two
+    tokens, in dimensions of their own. A row shows NaN where it sees the token and nowhere else."""
+    c = Filled("e4m3", [150, new + 1], 2, head_dim, seed=22)
+    bad = {1: [0, 17, head_dim - 1], 2: [5, 30, head_dim - 10]}      # tokens from the end: dimensions
+    pool = c.kv.pool()["v"].view(torch.uint8)
+    seen = np.zeros((2 * new, 2 * group, head_dim), dtype=bool)
+    for s, n in enumerate(c.lengths):
+        for back, dims in bad.items():
+            p = n - back
+            for i, d in enumerate(dims):
+                pool[int(c.host_table[s, p // 16]), :, p % 16, d] = 0x7f if i % 2 else 0xff
+                for t in range(new):
+                    if n - new + t >= p:
+                        seen[s * new + t, :, d] = True
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    q = torch.randn(2 * new, 2 * group, head_dim, generator=gen, device="cuda").to(TORCH[dtype])
+    out = c.kv.attend(q, c.table, c.len_dev, new_tokens=new)
+    c.kv.sync()
+    got = out.double().cpu().numpy()
+    k, v = c.values()
+    v = [np.nan_to_num(x, nan=0.0) for x in v]
+    hq = q.double().cpu().numpy()
+    want, lse, mass, span = decode.attend(hq, k, v, c.lengths, new, head_dim ** -0.5)
+    tol, _ = bounds(want, mass, span, lse, hq, k, head_dim ** -0.5, dtype)
+    assert np.array_equal(np.isnan(got), seen)
+    assert np.all((np.abs(got - want) <= tol)[~seen])
