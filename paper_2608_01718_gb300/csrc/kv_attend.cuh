@@ -36,7 +36,7 @@
 //
 // 8-bit rows. Codes become f16 exactly. q of a bf16 type is scaled to f16 by a power of two that brings its row's largest
 // magnitude to [1, 2): exact for elements within 2^-14 of that. The scales multiply the scores (k) and the weights (v);
-// the weights times scales are brought into f16's range by a factor a row, kept like the maximum.
+// the weights times scales are brought into f16's range by a factor a row, kept like the maximum and raised when that moves.
 //
 // Work. All (sequence, kv head, tile of rows) triples, each of its length in units of 4 warps x KT keys, form one line of
 // units; block i of P takes the i-th of P equal parts, whatever the lengths. Within a unit each warp has KT keys of its
@@ -714,9 +714,16 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
             top = fmaxf(m[n][h], top - kBelow);
-            const float f = m[n][h] == -INFINITY ? 0.f : exp2_fast(m[n][h] - top);
-            m[n][h] = top;
+            float f = m[n][h] == -INFINITY ? 0.f : exp2_fast(m[n][h] - top);
             l[n][h] *= f;
+            if constexpr (C::kEight) {
+              // what the factor was made for counts f times as much from here on: the factor rises by 1 / f (to its first
+              // value at most), which leaves the sums as they are, so that weights are held relative to what still counts
+              const float up = fminf(inv[n][h] * exp2_fast(top - m[n][h]), 0x1p120f);   // (from -inf, or to NaN: that value)
+              f = f == 0.f ? 0.f : fminf(f * __fdividef(up, inv[n][h]), 1.f);
+              inv[n][h] = up;
+            }
+            m[n][h] = top;
             const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
             for (int b = 0; b < C::kSub; ++b) {

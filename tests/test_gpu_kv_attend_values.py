@@ -118,3 +118,31 @@ def test_codes_that_are_no_numbers_stay_in_the_rows_that_see_them(dtype, new, gr
     tol, _ = bounds(want, mass, span, lse, hq, k, head_dim ** -0.5, dtype)
     assert np.array_equal(np.isnan(got), seen)
     assert np.all((np.abs(got - want) <= tol)[~seen])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("new,group", [(1, 1), (2, 4), (3, 4), (9, 4)])
+@pytest.mark.parametrize("head_dim", [64, 128, 256])
+@pytest.mark.parametrize("gap", [20.0, 60.0, 95.0])
+def test_large_values_of_small_weight_before_small_values_of_large_weight(fmt, new, group, head_dim, gap):
+    """8-bit caches, whose scales multiply the weights: the first token's value is 2^40 times the others' (at 20 nats 2^12), the
+    last ones' scores are `gap` nats above its, the rest's far below both. The late tokens decide the output. Enough
+    sequences that a block has whole ones, so that a warp meets both."""
+    c = Filled(fmt, [300], 8, head_dim, seed=23)
+    scores = torch.full((300, 8), -gap - 90.0)
+    scores[0] = -gap
+    scores[-76 - new:] = torch.linspace(-1, 0, 76 + new).unsqueeze(1)
+    v = c.v_rows.clone()
+    v[0] *= 2.0 ** (40 if gap > 20 else 12)
+    c.kv.append(rows_along_first(scores, head_dim, torch.bfloat16), v, c.seq, c.pos, c.table)
+    seqs = 128                                       # of one table row each, all the same
+    q = first(seqs * new, 8 * group, head_dim, torch.bfloat16)
+    table, lengths = c.table.expand(seqs, -1), c.len_dev.expand(seqs).contiguous()
+    out = c.kv.attend(q, table, lengths, new_tokens=new, scale=1.0)
+    c.kv.sync()
+    k, vv = c.values()
+    hq = q[:new].double().cpu().numpy()
+    want, lse, mass, span = decode.attend(hq, k, vv, [300], new, 1.0)
+    tol, _ = bounds(want, mass, span, lse, hq, k, 1.0, "bf16")
+    got = out.view(seqs, new, -1, head_dim).double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= tol), float((np.abs(got - want) / tol).max())
