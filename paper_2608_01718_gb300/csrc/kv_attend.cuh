@@ -86,6 +86,7 @@ struct AttendArgs {
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
 constexpr float kBelow = 7.f, kHeadroom = 15.f;   // a row's reference below its maximum, and scores above it, in powers of two
+constexpr float kFar = 0x1p110f, kToEnd = 0x1p18f;   // sums past kFar (times kToEnd: infinite) are done again, weights at most 1
 constexpr int kMaxPositions = 1 << 30;      // a table's reach is cut to this
 constexpr int kMaxDevices = 64;
 
@@ -696,7 +697,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           for (int e = 0; e < 4; ++e) move |= !(x2[b][n][e] <= kHeadroom);
         }
       }
-      if (__any_sync(0xffffffffu, move)) {
+      if (__any_sync(0xffffffffu, move) || careful) {   // (careful: weights of at most 1, so that sums stay in range)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -713,7 +714,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-            top = fmaxf(m[n][h], top - kBelow);
+            top = fmaxf(m[n][h], careful ? top : top - kBelow);
             float f = m[n][h] == -INFINITY ? 0.f : exp2_fast(m[n][h] - top);
             l[n][h] *= f;
             if constexpr (C::kEight) {
@@ -777,6 +778,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+              top = fminf(top, 3.402823466e+38f);
               if (top * inv[n][h] > 128.f) {
                 const float now = 128.f * __frcp_rn(top), f = now / inv[n][h];
                 inv[n][h] = now;
@@ -958,17 +960,21 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     }
     fresh = false;
 
-    if constexpr (FMT != LACACHE_KV_INT8) {
-      // an output that is not finite: a value of V may have reached rows that do not see it, or met a weight's term that is
-      // 0. This warp's part of the triple is done again, such values apart (and again only once: they may be seen)
+    // an output that is not finite: a value of V may have reached rows that do not see it, or met a weight's term that is 0,
+    // or the weights, which may exceed 1, brought a sum to the end of fp32's range (or its join would). This warp's part of the
+    // triple is done again, values that are not finite apart and the weights at most 1 (once: the values may be seen)
+    {
       bool odd = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          bool some = false;
+          // (8-bit: codes below 2^9 times weights below 2^15, of 2^30 keys at most, over the factor)
+          bool some = C::kEight && inv[n][e & 1] < 0x1p54f / kFar;
+          if constexpr (FMT != LACACHE_KV_INT8) {
 #pragma unroll
-          for (int d = 0; d < C::kMTiles; ++d) some |= !(fabsf(o[d][n][e]) <= 3.402823466e+38f);
+            for (int d = 0; d < C::kMTiles; ++d) some |= !(fabsf(o[d][n][e]) <= kFar);
+          }
           odd |= some && n * 8 + 2 * t + (e & 1) < live_rows;
         }
       }

@@ -25,8 +25,8 @@
 // With the loads left out a unit takes 1.6 us (1.0 of tensor time in bf16), with the softmax left out 1.9: no one part
 // bounds the kernel, their overlap within a ring of seven slots does.
 //
-// An output that is not finite is computed again key by key: a masked key's value times a zero weight, or an infinity times
-// a weight's second term, may have made it so.
+// An output that is not finite, or near the end of fp32's range, is computed again key by key with weights of at most 1: a
+// masked key's value times a zero weight, an infinity times a weight's second term, or weights above 1 may have made it so.
 //
 // Every wait is bounded (about a second): past it the block records a timeout, its roles stop, copies and products in flight
 // are drained, TMEM is freed and the block ends; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
@@ -779,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         if (mine) at_row = out_at(a, walk.seq, head, row0 + r, &at_lse);
         const float inv = total == 0.f ? 0.f : 1.f / total;
         // this half's dimensions: 32 of every 64 (rolled: code that runs once a triple waits for its fetch)
-        float2 zero = make_float2(0.f, 0.f);   // NaN after a product that is not finite
+        float2 zero = make_float2(0.f, 0.f);   // NaN after a product that is not finite, or past kFar
 #pragma unroll 1
         for (int d0 = half * 32; d0 < D; d0 += 64) {
           float o[32];
@@ -789,7 +789,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
             const int d = d0 + e;
             if (d < D) {
 #pragma unroll
-              for (int x = 0; x < 8; x += 2) zero = fma_two(make_float2(o[e + x], o[e + x + 1]), make_float2(0.f, 0.f), zero);
+              for (int x = 0; x < 8; x += 2) {
+                const float2 y = mul_two(make_float2(o[e + x], o[e + x + 1]), make_float2(kToEnd, kToEnd));
+                zero = fma_two(y, make_float2(0.f, 0.f), zero);
+              }
               if (mine) {
                 const float4 y0 = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 const float4 y1 = make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);

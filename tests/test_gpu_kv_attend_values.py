@@ -146,3 +146,36 @@ def test_large_values_of_small_weight_before_small_values_of_large_weight(fmt, n
     tol, _ = bounds(want, mass, span, lse, hq, k, 1.0, "bf16")
     got = out.view(seqs, new, -1, head_dim).double().cpu().numpy()
     assert np.all(np.abs(got - want) <= tol), float((np.abs(got - want) / tol).max())
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("new,group", [(1, 1), (1, 4), (3, 4), (9, 4)])
+@pytest.mark.parametrize("head_dim", [64, 128, 256])
+def test_values_near_the_largest_float(fmt, new, group, head_dim):
+    """V of 2^119 and scores that rise: weights taken relative to less than the largest would bring the sums past fp32's range
+    (290 of them by their softmax weights stay within it)."""
+    c = Filled(fmt, [290], 2, head_dim, seed=24)
+    scores = torch.linspace(-9, 0, 290).unsqueeze(1).expand(-1, 2)
+    v = (c.v_rows.float().clamp(-1, 1) * 2.0 ** 119).to(torch.bfloat16)
+    c.kv.append(rows_along_first(scores, head_dim, torch.bfloat16), v, c.seq, c.pos, c.table)
+    q = first(new, 2 * group, head_dim, torch.bfloat16)
+    out = c.kv.attend(q, c.table, c.len_dev, new_tokens=new, scale=1.0)
+    c.kv.sync()
+    k, vv = c.values()
+    hq = q.double().cpu().numpy()
+    want, lse, mass, span = decode.attend(hq, k, vv, c.lengths, new, 1.0)
+    tol, _ = bounds(want, mass, span, lse, hq, k, 1.0, "bf16")
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all() and np.all(np.abs(got - want) <= tol)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("new,group", [(1, 4), (3, 4), (9, 4)])
+def test_partial_sums_whose_join_would_leave_the_range(fmt, new, group):
+    # equal weights, one value everywhere: every part's sum is finite, and the parts' total is not
+    c = Filled(fmt, [384], 2, 64, seed=25)
+    v = torch.full_like(c.v_rows, 2.0 ** 113)
+    c.kv.append(rows_along_first(torch.zeros(384, 2), 64, torch.bfloat16), v, c.seq, c.pos, c.table)
+    out = c.kv.attend(first(new, 2 * group, 64, torch.bfloat16), c.table, c.len_dev, new_tokens=new, scale=1.0)
+    c.kv.sync()
+    assert ((out.double() / 2.0 ** 113 - 1).abs() <= 2.0 ** -8).all()
