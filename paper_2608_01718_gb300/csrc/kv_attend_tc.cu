@@ -28,7 +28,7 @@
 // An output that is not finite, or near the end of fp32's range, is computed again key by key with weights of at most 1: a
 // masked key's value times a zero weight, an infinity times a weight's second term, or weights above 1 may have made it so.
 //
-// Every wait is bounded (about a second): past it the block records a timeout, its roles stop, copies and products in flight
+// Every wait is bounded (about a second, renewed while a row is computed again): past it the block records a timeout, its roles stop, copies and products in flight
 // are drained, TMEM is freed and the block ends; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
 #include "kv_attend.cuh"
 #include "tcgen05.cuh"
@@ -62,6 +62,7 @@ struct Tc {
     uint64_t q_full, o_empty;                  // a triple's q is there; its O has been read
     uint64_t pair[4];                          // the two threads of every row of 32 have left their part
     uint64_t drain;
+    long long progress;                        // clock64() of a warp at work on a row key by key: the waits' second counts from it
     float given[2][2][kTile];                  // what they leave, in turn and by half: the row's largest product; at a
                                                // triple's end its sum of weights, then 0 or NaN (an output not finite)
     uint32_t tmem;
@@ -206,10 +207,11 @@ __device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int 
   *reinterpret_cast<uint4*>(a.out.p + at_row + d * 2) = a.q_f16 ? pack8(v, __half()) : pack8(v, __nv_bfloat16());
 }
 
-// One row of one block's keys [from, to), key by key, by a warp: lane i holds dimensions 4 i .. 4 i + 3.
+// One row of one block's keys [from, to), by a warp, four keys at a time: lane i holds dimensions 4 i .. 4 i + 3. It may take
+// longer than a wait's bound, so it tells the waits that it goes on.
 template <int FMT, bool QF16>
-__device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, int tok, int qh, int from, int to, float4* acc,
-                                      float* top, float* sum) {
+__device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, int tok, int qh, int from, int to,
+                                      volatile long long* progress, float4* acc, float* top, float* sum) {
   using T = Tc<FMT, QF16>;
   const int lane = threadIdx.x & 31, D = a.head_dim;
   const bool has = lane * 4 < D;
@@ -220,11 +222,7 @@ __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, in
     const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
     return make_float4(x.x, x.y, y.x, y.y);
   };
-  auto load4 = [&](const unsigned char* p) {
-    return has ? four(*reinterpret_cast<const uint2*>(p + lane * 8), QF16) : make_float4(0.f, 0.f, 0.f, 0.f);
-  };
   auto cached4 = [&](const unsigned char* pool, const float* scales, int64_t row) {
-    if (!has) return make_float4(0.f, 0.f, 0.f, 0.f);
     if constexpr (T::kEight) {
       uint2 u;
       widen4<FMT>(*reinterpret_cast<const uint32_t*>(pool + row * D + lane * 4), u.x, u.y);
@@ -235,23 +233,45 @@ __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, in
       return four(*reinterpret_cast<const uint2*>(pool + row * D * 2 + lane * 8), FMT == LACACHE_KV_F16);
     }
   };
-  const float4 q = load4(a.q.at((int64_t)seq * a.new_tokens + tok, qh));
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  const unsigned char* q_row = a.q.at((int64_t)seq * a.new_tokens + tok, qh);
+  const float4 q = has ? four(*reinterpret_cast<const uint2*>(q_row + lane * 8), QF16) : zero;
   float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j = from; j < to; ++j) {
+  float4 o = zero;
+  for (int j = from & ~3; j < to; j += 4) {
+    if (lane == 0) *progress = clock64();
     const int index = (int)(((uint64_t)(uint32_t)(j >> 4) * a.page_mul) >> a.page_shift);
     const int page = a.table.pages[seq * a.table.stride + index];
     if ((unsigned)page >= (unsigned)a.pages) continue;
     const int64_t row = page * a.page_rows + (int64_t)head * a.page_size + (j - index * a.page_size);
-    const float4 k = cached4(a.pk, a.ks, row), v = cached4(a.pv, a.vs, row);
-    float dot = has ? q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w : 0.f;
+    float4 k[4], v[4];
+    float s[4];
 #pragma unroll
-    for (int x = 16; x; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
-    const float s = dot * (a.scale * 1.4426950408889634f);
-    const float now = fmaxf(m, s), base = now == -INFINITY ? 0.f : now;
-    const float f = exp2_fast(m - base), p = exp2_fast(s - base);
-    l = l * f + p;
-    o.x = o.x * f + p * v.x, o.y = o.y * f + p * v.y, o.z = o.z * f + p * v.z, o.w = o.w * f + p * v.w;
+    for (int e = 0; e < 4; ++e) {
+      const bool in = has && j + e >= from && j + e < to;
+      k[e] = in ? cached4(a.pk, a.ks, row + e) : zero;
+      v[e] = in ? cached4(a.pv, a.vs, row + e) : zero;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] = has ? q.x * k[e].x + q.y * k[e].y + q.z * k[e].z + q.w * k[e].w : 0.f;
+#pragma unroll
+    for (int x = 16; x; x >>= 1) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += __shfl_xor_sync(0xffffffffu, s[e], x);
+    }
+    float now = m;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[e] = j + e >= from && j + e < to ? s[e] * (a.scale * 1.4426950408889634f) : -INFINITY;
+      now = fmaxf(now, s[e]);
+    }
+    const float base = now == -INFINITY ? 0.f : now, f = exp2_fast(m - base);
+    l *= f, o.x *= f, o.y *= f, o.z *= f, o.w *= f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float p = exp2_fast(s[e] - base);
+      l += p, o.x += p * v[e].x, o.y += p * v[e].y, o.z += p * v[e].z, o.w += p * v[e].w;
+    }
     m = now;
   }
   *acc = o;
@@ -274,6 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   const uint32_t ring = base;
   Tail& t = *reinterpret_cast<Tail*>(gbase + T::kTail);
   volatile uint32_t* abort_flag = &t.abort_flag;
+  volatile long long* progress = &t.progress;
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int D = a.head_dim, units_row = D / 8;                    // 16-byte units of a row in shared memory
   const int row_bytes = T::kEight ? D : D * 2;                    // of the cache
@@ -292,6 +313,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     mbar_init(smem_u32(&t.q_full), kSoftmax / 32);
     mbar_init(smem_u32(&t.o_empty), kSoftmax / 32);
     mbar_init(smem_u32(&t.drain), 1);
+    t.progress = 0;
     t.abort_flag = 0;
     t.pending[0][2] = t.pending[1][2] = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -312,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     atomicOr(a.status, kAttendTimeout);
   };
   auto wait = [&](uint64_t& bar, uint32_t parity) {   // false (and the block stops) past the bound
-    if (mbar_wait_inline(smem_u32(&bar), parity, abort_flag)) return true;
+    if (mbar_wait_inline(smem_u32(&bar), parity, abort_flag, progress)) return true;
     if (!*abort_flag) fail();
     return false;
   };
@@ -810,7 +832,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, total);
           else if (a.lse) a.lse[at_lse] = lse_of(m, total);
         }
-        // a row that is not finite in either half is done again, by the first, past what both have written
+        // a row that is not finite in either half is done again, past what both have written; not where its sum of weights
+        // is NaN: then a score that it sees is (masked ones are -infinity), and NaN is its result
         t.given[pairs & 1][half][r] = zero.x + zero.y;
         warp_arrive(t.pair[warp & 3]);
         ok = wait(t.pair[warp & 3], pairs & 1);
@@ -818,17 +841,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           ok = false;
           break;
         }
-        const bool odd = !(t.given[pairs & 1][0][r] + t.given[pairs & 1][1][r] == 0.f && total <= 3.402823466e+38f);
+        const bool odd = !(t.given[pairs & 1][0][r] + t.given[pairs & 1][1][r] == 0.f) && total <= 3.402823466e+38f;
         ++pairs;
-        // rows that are not finite, again
+        // rows that are not finite, again: every second one by the other half's warp
         const int key_end = min(key_begin + count * kTile, walk.sp.hi);
-        for (unsigned rows = half ? 0u : __ballot_sync(0xffffffffu, mine && odd); rows; rows &= rows - 1) {
+        for (unsigned rows = __ballot_sync(0xffffffffu, mine && odd) & (half ? 0xaaaaaaaau : 0x55555555u); rows; rows &= rows - 1) {
           const int src = __ffs(rows) - 1;
-          const int rr = warp * 32 + src, its_tok = by_group(row0 + rr), its_qh = head * a.group + row0 + rr - its_tok * a.group;
+          const int rr = (warp & 3) * 32 + src, its_tok = by_group(row0 + rr), its_qh = head * a.group + row0 + rr - its_tok * a.group;
           const int its_pos = __shfl_sync(0xffffffffu, pos, src), its_lo = __shfl_sync(0xffffffffu, lo, src);
           float4 acc;
           float top, sum;
-          slow_row<FMT, QF16>(a, walk.seq, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1), &acc, &top, &sum);
+          slow_row<FMT, QF16>(a, walk.seq, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1),
+                               progress, &acc, &top, &sum);
           int64_t its_lse;
           const int64_t its_row = out_at(a, walk.seq, head, row0 + rr, &its_lse);
           if (lane * 4 < D) {

@@ -179,3 +179,44 @@ def test_partial_sums_whose_join_would_leave_the_range(fmt, new, group):
     out = c.kv.attend(first(new, 2 * group, 64, torch.bfloat16), c.table, c.len_dev, new_tokens=new, scale=1.0)
     c.kv.sync()
     assert ((out.double() / 2.0 ** 113 - 1).abs() <= 2.0 ** -8).all()
+
+
+@pytest.mark.parametrize("where,n", [("k", 300_000), ("v", 1_200_000)])
+def test_a_long_sequence_that_is_not_finite_leaves_the_others_alone(where, n):
+    """Many rows: outputs that are not finite are computed again key by key, which over 1,200,000 keys takes longer than the bound of
+    the kernel's waits. That is no timeout, and the sequences that share the blocks are as without it."""
+    new, D, page, seqs = 32, 16, 64, 200
+    used = -(-n // page)
+    kv = L.KVCache(1, D, 2 * used, page, "bf16")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(26)
+    pool = kv.pool()
+    for name in "kv":
+        half = torch.randn(used, 1, page, D, generator=gen, device="cuda").bfloat16()
+        pool[name][:used] = half
+        pool[name][used:] = half
+    if where == "k":
+        pool["k"][used, 0, 5, 2] = float("nan")                  # sequence 1's token 5
+    else:
+        pool["v"][used, 0, 5, 3], pool["v"][used, 0, 7, 5] = float("inf"), float("nan")
+    table = torch.arange(used, dtype=torch.int32, device="cuda").repeat(seqs, 1)
+    table[1] += used
+    q = torch.randn(new, 1, D, generator=gen, device="cuda").bfloat16()
+    lengths = torch.full((seqs,), n, dtype=torch.int32, device="cuda")
+    lse = torch.empty(seqs * new, 1, device="cuda")
+    out = kv.attend(q.repeat(seqs, 1, 1), table, lengths, new_tokens=new, lse=lse).view(seqs, new, 1, D)
+    kv.sync()
+    rows = [pool[name][:used].transpose(1, 2).reshape(-1, 1, D)[:n].double().cpu().numpy() for name in "kv"]
+    hq = q.double().cpu().numpy()
+    want, want_lse, mass, span = decode.attend(hq, rows[:1], rows[1:], [n], new, D ** -0.5)
+    tol, tol_lse = bounds(want, mass, span, want_lse, hq, rows[:1], D ** -0.5, "bf16")
+    got, got_lse = out.double().cpu().numpy(), lse.view(seqs, new, 1).double().cpu().numpy()
+    healthy = [s for s in range(seqs) if s != 1]
+    assert np.all(np.abs(got[healthy] - want) <= tol) and np.all(np.abs(got_lse[healthy] - want_lse) <= tol_lse)
+    if where == "k":
+        assert np.isnan(got[1]).all() and np.isnan(got_lse[1]).all()
+    else:
+        rest = [d for d in range(D) if d not in (3, 5)]
+        assert np.isposinf(got[1, ..., 3]).all() and np.isnan(got[1, ..., 5]).all()
+        assert np.all((np.abs(got[1] - want) <= tol)[..., rest]) and np.all(np.abs(got_lse[1] - want_lse) <= tol_lse)
+    kv.close()
