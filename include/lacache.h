@@ -524,8 +524,14 @@ lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_k
 
 /* Synchronize the handle's device and report what its kernels found since the previous call: LACACHE_ERR_INVALID_ARG for
  * an index outside its range (see lacache_kv_table), or LACACHE_ERR_DEVICE_TIMEOUT if an attention gave up waiting within
- * the GPU (its outputs are then undefined). */
+ * the GPU (that call's outputs are then undefined; later calls are not affected). */
 lacache_status lacache_kv_sync(lacache_kv_t* h);
+
+/* Test support for failure detection: the next `attends` calls of lacache_kv_attend that have many rows (more than 16 a kv
+ * head, 32 over 8-bit caches with heads of up to 64; heads of up to 128) make the block that holds the first keys withhold its loads. The
+ * bounded waits for them (about a second) run out, the block records the timeout, frees what it holds and ends, and
+ * lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT. Nothing faults, and the context stays usable. 0 cancels. */
+lacache_status lacache_kv_inject_stall(lacache_kv_t* h, int32_t attends);
 
 #ifdef __cplusplus
 }

@@ -25,6 +25,7 @@ struct lacache_kv {
   float* vs;
   float* partial;            // the attention's partial sums, two slots a block
   unsigned int* arrived;     // its counters, one a block (each launch leaves them zero)
+  int inject_stall;          // attentions of many rows left that withhold a load (failure-detection tests)
   unsigned int* dev_status;  // kBadIndex: a kernel met an index outside its range; kAttendTimeout: a bounded wait ran out
 };
 

@@ -55,6 +55,10 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e;
   if (lc::takes_tc(a.rows, a.group, c.head_dim, lc::is_quantised(c.format))) {
+    if (h->inject_stall > 0) {
+      a.inject_stall = 1;
+      --h->inject_stall;
+    }
     e = lc::launch_attend_tc(a, c.format, h->num_sms, st);
   } else switch (c.format) {
     case LACACHE_KV_BF16: e = lc::launch_attend_bf16(a, h->num_sms, st); break;

@@ -61,6 +61,7 @@ struct AttendArgs {
   int parts;            // blocks the units may be split over (at most the grid)
   int max_len;          // positions the table can name
   int device;
+  int inject_stall;     // test support: the tcgen05 kernel's block with the first unit withholds its loads: waits run out
   // the tcgen05 kernel: rows of a tile, floats of a row of a partial slot, and ceil(2^32 / group)
   int tile_rows, padded;
   uint32_t group_mul;

@@ -29,7 +29,7 @@
 // masked key's value times a zero weight, an infinity times a weight's second term, or weights above 1 may have made it so.
 //
 // Every wait is bounded (about a second, renewed while a row is computed again): past it the block records a timeout, its roles stop, copies and products in flight
-// are drained, TMEM is freed and the block ends; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
+// are drained, TMEM is freed and the block ends, after it has arrived where it shares triples; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
 #include "kv_attend.cuh"
 #include "tcgen05.cuh"
 
@@ -345,6 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     int n = 0;   // slots begun
     int units = 0;
     bool ok = true;
+    if (a.inject_stall && walk.seq_base + walk.triple + walk.first_unit == 0) walk.left = 0;
     if constexpr (T::kEight) {
       // codes by cp.async into a stage, each lane its own pieces; kStages tiles later the lane widens them into a slot
       const int pieces = D / 16, piece_mul = 65536 / pieces + 1, tile_pieces = 16 * pieces;   // of a row; of 16 keys
@@ -885,7 +886,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   __syncthreads();
   tc_fence_after();
   if (warp == kMmaWarp) tmem_dealloc<false>(tmem, 512);
-  if (*abort_flag) return;
+  if (*abort_flag) {   // it still arrives where it shares a triple: the counters are zero when the launch ends
+    if (warp == 0) {
+      start_walk(a, walk, line);
+      for (; !walk.done(); walk.next(a)) {
+        if (walk.units() == walk.sp.units) continue;
+        const int begin = walk.seq_base + walk.triple * (walk.sp.units + kCost) + kCost;
+        const int c_first = line.block_of(begin), c_last = line.block_of(begin + walk.sp.units - 1);
+        if (lane == 0 && atomicAdd(a.arrived + c_first, 1u) == (unsigned int)(c_last - c_first)) a.arrived[c_first] = 0u;
+      }
+    }
+    return;
+  }
 
   // ---- shared triples: whichever block arrives last joins the blocks' sums, in their order ----
   if (threadIdx.x < 2) {

@@ -399,6 +399,12 @@ extern "C" lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const 
   return lc::from_cuda(cudaGetLastError());
 }
 
+extern "C" lacache_status lacache_kv_inject_stall(lacache_kv_t* h, int32_t attends) {
+  if (!h || attends < 0) return LACACHE_ERR_INVALID_ARG;
+  h->inject_stall = attends;
+  return LACACHE_OK;
+}
+
 extern "C" lacache_status lacache_kv_sync(lacache_kv_t* h) {
   lc::NvtxRange nvtx("lacache_kv_sync");
   if (!h) return LACACHE_ERR_INVALID_ARG;
@@ -408,8 +414,6 @@ extern "C" lacache_status lacache_kv_sync(lacache_kv_t* h) {
       cudaMemcpy(&word, h->dev_status, 4, cudaMemcpyDeviceToHost) != cudaSuccess)
     return LACACHE_ERR_CUDA;
   if (!word) return LACACHE_OK;
-  // (a call that timed out may have left the attention's counters, which lie before the word, in between)
-  const size_t bytes = (unsigned char*)(h->dev_status + 1) - (unsigned char*)h->arrived;
-  if (cudaMemset(h->arrived, 0, bytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) return LACACHE_ERR_CUDA;
+  if (cudaMemset(h->dev_status, 0, 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) return LACACHE_ERR_CUDA;
   return word & lc::kAttendTimeout ? LACACHE_ERR_DEVICE_TIMEOUT : LACACHE_ERR_INVALID_ARG;
 }

@@ -35,7 +35,7 @@ EXPORTS = ["lacache_create", "lacache_create_ensemble", "lacache_destroy", "laca
            "lacache_calibrate_workspace_bytes", "lacache_verify_draft", "lacache_lookup_noalloc",
            "lacache_merge_shards", "lacache_get_stats", "lacache_save", "lacache_load", "lacache_get_config",
            "lacache_rope_init", "lacache_rope_apply", "lacache_kv_create", "lacache_kv_destroy", "lacache_kv_get_pool",
-           "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_sync",
+           "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_sync", "lacache_kv_inject_stall",
            "lacache_status_string"]
 
 
@@ -161,6 +161,7 @@ def load() -> ctypes.CDLL:
         "lacache_kv_read": ([vp, i32, vp, i64, vp, vp, i32, vp, vp, vp], i32),
         "lacache_kv_attend": ([vp, i32, vp, vp, vp], i32),
         "lacache_kv_sync": ([vp], i32),
+        "lacache_kv_inject_stall": ([vp, i32], i32),
         "lacache_status_string": ([i32], ctypes.c_char_p),
     }
     for name, (args, res) in sig.items():
@@ -446,6 +447,10 @@ def lacache_kv_attend(h: int, layer: int, table: lacache_kv_table, attention: la
 
 def lacache_kv_sync(h: int) -> None:
     _check("lacache_kv_sync", load().lacache_kv_sync(h))
+
+
+def lacache_kv_inject_stall(h: int, attends: int) -> None:
+    _check("lacache_kv_inject_stall", load().lacache_kv_inject_stall(h, attends))
 
 
 def alloc_result(batch: int, top_c: int, device, candidates: bool = True, pinned: bool = False,
