@@ -18,7 +18,8 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
       (c.format == LACACHE_KV_F16 && at->dtype != LACACHE_F16))
     return LACACHE_ERR_UNSUPPORTED;
   if (table->seqs == 0) return LACACHE_OK;
-  if (!at->lengths_dev || !lc::device_rows(&at->q, at->dtype, &a.q) || !lc::device_rows(&at->out, at->dtype, &a.out))
+  if (!at->lengths_dev || !lc::device_rows(&at->q, at->dtype, &a.q) || !lc::device_rows(&at->out, at->dtype, &a.out) ||
+      at->out.data == at->q.data)
     return LACACHE_ERR_INVALID_ARG;
   lc::DeviceGuard guard(c.device);
   if (!guard.ok()) return LACACHE_ERR_CUDA;

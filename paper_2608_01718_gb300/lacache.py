@@ -747,7 +747,7 @@ class KVCache:
                scale: float | None = None, out=None, lse=None, cuda_stream=None):
         """Attention of the last ``new_tokens`` tokens of each sequence: q [sequences * new_tokens x q_heads x head_dim],
         ``lengths`` (int32) with the new tokens counted. Returns ``out``; ``lse`` (fp32 [tokens x q_heads]) is filled if
-        given. ``scale`` is 1 / sqrt(head_dim) if None."""
+        given. ``scale`` is 1 / sqrt(head_dim) if None. ``out`` does not overlap ``q``."""
         heads, D, dev, dtype = _three("q", q)[1], self.cfg.head_dim, self.device, q.dtype
         t = self._table(table)
         n = t.seqs * new_tokens
