@@ -664,7 +664,7 @@ class KVCache:
         if format not in self.FORMATS:
             raise ValueError(f"format is one of {list(self.FORMATS)}, not {format!r}")
         self.cfg = lacache_kv_config(layers, kv_heads, head_dim, page_size, pages, self.FORMATS[format], device)
-        self.format, self.device = format, device
+        self.format, self.device, self.layers = format, device, layers
         _bind_torch()
         self.h, self._lib = lacache_kv_create(self.cfg), load()
 
@@ -685,11 +685,16 @@ class KVCache:
         except Exception:
             pass
 
+    def _layer(self, layer: int) -> int:   # (ctypes would drop the bits past 32)
+        if not 0 <= layer < self.layers:
+            raise ValueError(f"layer is 0 to {self.layers - 1}, not {layer}")
+        return layer
+
     def pool(self, layer: int = 0) -> dict:
         """A layer's arrays as tensors on the handle's own memory (valid until close): k and v
         [pages x kv_heads x page_size x head_dim] and, in 8-bit formats, their fp32 scales ks and vs."""
         import torch
-        c, p = self.cfg, lacache_kv_get_pool(self.h, layer)
+        c, p = self.cfg, lacache_kv_get_pool(self.h, self._layer(layer))
         rows = (c.pages, c.kv_heads, c.page_size)
         typestr, dtype = {"bf16": ("<i2", torch.bfloat16), "f16": ("<f2", torch.float16),
                           "e4m3": ("|u1", torch.float8_e4m3fn), "int8": ("|i1", torch.int8)}[self.format]
@@ -723,7 +728,7 @@ class KVCache:
         t, rk, rv = self._table(table), _rows("k", k, n, heads, D, dev, dtype), _rows("v", v, n, heads, D, dev, dtype)
         at = ctypes.addressof
         _check("lacache_kv_append", self._lib.lacache_kv_append(
-            self.h, layer, at(t), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
+            self.h, self._layer(layer), at(t), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
             None if rope is None else at(rope.plan), None if rope_pos is None else _index("rope_pos", rope_pos, n, dev),
             _dtype(k), at(rk), at(rv), q_heads, None if rq is None else at(rq), None if ro is None else at(ro),
             _current_stream(cuda_stream, dev)))
@@ -737,7 +742,7 @@ class KVCache:
             k_out = torch.empty(n, heads, D, dtype=torch.bfloat16 if dtype is None else dtype, device=f"cuda:{dev}")
             v_out = torch.empty_like(k_out)
         some = k_out if k_out is not None else v_out
-        lacache_kv_read(self.h, layer, self._table(table), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
+        lacache_kv_read(self.h, self._layer(layer), self._table(table), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
                         _dtype(some), None if k_out is None else _rows("k_out", k_out, n, heads, D, dev, some.dtype),
                         None if v_out is None else _rows("v_out", v_out, n, heads, D, dev, some.dtype),
                         _current_stream(cuda_stream, dev))
@@ -758,12 +763,16 @@ class KVCache:
             import torch
             if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
                 raise ValueError(f"lse is a dense fp32 [{n} x {heads}] tensor on cuda:{dev}")
+        if not 0 <= window < 1 << 31:
+            if window < 0:
+                raise ValueError(f"window is a number of positions, or 0 for none, not {window}")
+            window = 0   # no position lies further back
         a = lacache_attention(new_tokens, heads, window, _dtype(q), D ** -0.5 if scale is None else scale,
                               _index("lengths", lengths, t.seqs, dev),
                               None if starts is None else _index("starts", starts, t.seqs, dev),
                               _rows("q", q, n, heads, D, dev, dtype), _rows("out", out, n, heads, D, dev, dtype),
                               None if lse is None else lse.data_ptr())
-        _check("lacache_kv_attend", self._lib.lacache_kv_attend(self.h, layer, ctypes.addressof(t), ctypes.addressof(a),
+        _check("lacache_kv_attend", self._lib.lacache_kv_attend(self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a),
                                                                 _current_stream(cuda_stream, dev)))
         return out
 

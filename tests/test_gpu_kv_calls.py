@@ -27,3 +27,26 @@ def test_outputs_over_the_queries_are_refused():
             c.kv.attend(q, c.table, c.len_dev, new_tokens=new, out=q)
         assert e.value.status == L.LACACHE_ERR_INVALID_ARG and torch.equal(q, kept)
     c.kv.sync()
+
+
+def test_numbers_past_32_bits_are_refused_or_mean_what_they_say():
+    # a window of 2^32 + 5 is no window of 5
+    c = Filled("bf16", [40], 1, 64, seed=35)
+    q = torch.randn(1, 1, 64, device="cuda").bfloat16()
+    want = c.kv.attend(q, c.table, c.len_dev)
+    for window in ((1 << 32) + 5, 1 << 31, 1 << 62):
+        assert torch.equal(c.kv.attend(q, c.table, c.len_dev, window=window), want)
+    for window in (-1, -(1 << 32) + 5):
+        with pytest.raises((ValueError, L.LacacheError)):
+            c.kv.attend(q, c.table, c.len_dev, window=window)
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for layer in (1 << 32, -(1 << 32)):
+        with pytest.raises((ValueError, L.LacacheError)):
+            c.kv.attend(q, c.table, c.len_dev, layer=layer)
+        with pytest.raises((ValueError, L.LacacheError)):
+            c.kv.append(q, q, one, one, c.table, layer=layer)
+        with pytest.raises((ValueError, L.LacacheError)):
+            c.kv.read(one, one, c.table, layer=layer)
+        with pytest.raises((ValueError, L.LacacheError)):
+            c.kv.pool(layer)
+    c.kv.sync()
