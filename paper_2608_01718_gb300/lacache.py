@@ -6,6 +6,7 @@ if the library has not been built, loading it raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -194,6 +195,17 @@ def _stream(cuda_stream, device: int | None = None):
         return cuda_stream if isinstance(cuda_stream, int) else cuda_stream.cuda_stream
     import torch
     return torch.cuda.current_stream(device).cuda_stream
+
+
+def _results_on(cuda_stream, device):
+    """Where a call's results are allocated: from the memory of the stream that the call runs on. (A block of another stream's
+    may still be in use there by work that was queued before the block was freed.)"""
+    if cuda_stream is None:
+        return contextlib.nullcontext()
+    import torch
+    if isinstance(cuda_stream, int):   # 0 is the default stream
+        cuda_stream = torch.cuda.ExternalStream(cuda_stream, device) if cuda_stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(cuda_stream)
 
 
 def make_config(d: int, k: int, capacity: int, tau_c: float, tau_a: float, top_c: int, *, max_batch: int,
@@ -534,7 +546,8 @@ class LaCache:
     def lookup(self, q_emb, q_prefix, q_ids, out: dict | None = None, candidates: bool = True,
                cuda_stream=None) -> dict:
         if out is None:
-            out = alloc_result(q_emb.shape[0], self.cfg.top_c, q_emb.device, candidates, models=self.models)
+            with _results_on(cuda_stream, self.device):
+                out = alloc_result(q_emb.shape[0], self.cfg.top_c, q_emb.device, candidates, models=self.models)
         lacache_lookup(self.h, q_emb, q_prefix, q_ids, out, cuda_stream)
         return out
 
@@ -581,6 +594,15 @@ def _current_stream(cuda_stream, device: int) -> int:
     if cuda_stream is None and _RAW_STREAM is not None:
         return _RAW_STREAM(device)
     return _stream(cuda_stream, device)
+
+
+def _new_like(x, cuda_stream, device: int):
+    """A dense tensor of x's shape and type for the results of a call on cuda_stream."""
+    import torch
+    if cuda_stream is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    with _results_on(cuda_stream, device):
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def _rows(name: str, t, n: int, heads: int, head_dim: int, device: int, dtype) -> lacache_rows:
@@ -630,7 +652,7 @@ class Rope:
         device, dtype = x.get_device(), x.dtype
         import torch
         if out is None:
-            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            out = _new_like(x, cuda_stream, device)
         args = (self.plan, n, heads, head_dim, _dtype(x), _rows("x", x, n, heads, head_dim, device, dtype),
                 _index("pos", pos, n, device), inverse, _rows("out", out, n, heads, head_dim, device, dtype),
                 _current_stream(cuda_stream, device))
@@ -654,7 +676,9 @@ class KVCache:
     """A paged key-value cache (lacache_kv_t) with its calls. ``format``: "bf16", "f16", "e4m3" or "int8".
 
     Tables are int32 [sequences x pages] CUDA tensors, lengths and positions int32 vectors, rows [tokens x heads x head_dim]
-    tensors with dense rows. Calls run on torch's current stream of the cache's device unless given another."""
+    tensors with dense rows. Calls run on torch's current stream of the cache's device unless given another (and then allocate
+    the results that they are not given from its memory). A cache's calls share scratch: issue them on one stream, or order the
+    streams by events."""
 
     FORMATS = {"bf16": LACACHE_KV_BF16, "f16": LACACHE_KV_F16, "e4m3": LACACHE_KV_E4M3, "int8": LACACHE_KV_INT8}
 
@@ -722,8 +746,7 @@ class KVCache:
         if q is not None:
             q_heads = _three("q", q)[1]
             if q_out is None:
-                import torch
-                q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                q_out = _new_like(q, cuda_stream, dev)
             rq, ro = _rows("q", q, n, q_heads, D, dev, dtype), _rows("q_out", q_out, n, q_heads, D, dev, dtype)
         t, rk, rv = self._table(table), _rows("k", k, n, heads, D, dev, dtype), _rows("v", v, n, heads, D, dev, dtype)
         at = ctypes.addressof
@@ -739,8 +762,9 @@ class KVCache:
         n, heads, D, dev = seq.shape[0], self.cfg.kv_heads, self.cfg.head_dim, self.device
         if k_out is None and v_out is None:
             import torch
-            k_out = torch.empty(n, heads, D, dtype=torch.bfloat16 if dtype is None else dtype, device=f"cuda:{dev}")
-            v_out = torch.empty_like(k_out)
+            with _results_on(cuda_stream, dev):
+                k_out = torch.empty(n, heads, D, dtype=torch.bfloat16 if dtype is None else dtype, device=f"cuda:{dev}")
+                v_out = torch.empty_like(k_out)
         some = k_out if k_out is not None else v_out
         lacache_kv_read(self.h, self._layer(layer), self._table(table), n, _index("seq", seq, n, dev), _index("pos", pos, n, dev),
                         _dtype(some), None if k_out is None else _rows("k_out", k_out, n, heads, D, dev, some.dtype),
@@ -757,8 +781,7 @@ class KVCache:
         t = self._table(table)
         n = t.seqs * new_tokens
         if out is None:
-            import torch
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            out = _new_like(q, cuda_stream, dev)
         if lse is not None:
             import torch
             if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:

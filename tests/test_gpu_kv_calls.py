@@ -50,3 +50,66 @@ def test_numbers_past_32_bits_are_refused_or_mean_what_they_say():
         with pytest.raises((ValueError, L.LacacheError)):
             c.kv.pool(layer)
     c.kv.sync()
+
+
+class Slow:
+    """Work for the current stream that takes some ten milliseconds."""
+
+    def __init__(self):
+        self.x = torch.randn(4096, 4096, device="cuda")
+
+    def __call__(self):
+        for _ in range(20):
+            self.x @ self.x
+
+
+@pytest.mark.parametrize("call", ["rotate", "append", "read", "attend"])
+def test_results_made_on_another_stream_take_no_memory_of_this_one(call):
+    """A call on a given stream allocates its result from that stream's memory: a block that was freed while the current stream still
+    works on it must not be written from the other."""
+    c = Filled("bf16", [500] * 8, 32, 64, seed=36)           # results of 16 MB: a block of memory of their own
+    x = torch.randn(4000, 32, 64, device="cuda").bfloat16()
+    rope, at = L.Rope(64), torch.arange(4000, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    slow = Slow()
+
+    def run(stream):
+        if call == "rotate":
+            return rope.apply(x, at, cuda_stream=stream)
+        if call == "append":
+            return c.kv.append(x, x, c.seq, c.pos, c.table, q=x, cuda_stream=stream)
+        if call == "read":
+            return c.kv.read(c.seq, c.pos, c.table, cuda_stream=stream)[0]
+        return c.kv.attend(x, c.table, c.len_dev, new_tokens=500, cuda_stream=stream)
+
+    for stream in (side, side.cuda_stream):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        old = torch.full((4000, 32, 64), 3.0, device="cuda", dtype=torch.bfloat16)
+        kept = torch.empty_like(old)
+        torch.cuda.synchronize()
+        slow()
+        kept.copy_(old)              # queued behind the slow work
+        where = old.data_ptr()
+        del old
+        got = run(stream)
+        assert got.data_ptr() != where
+        torch.cuda.synchronize()
+        assert float(kept.float().min()) == 3.0 == float(kept.float().max())
+        assert torch.equal(got, run(None))
+    c.kv.sync()
+
+
+def test_a_lookup_on_another_stream_allocates_there():
+    x = torch.nn.functional.normalize(torch.randn(4, 64, device="cuda"), dim=-1).bfloat16()
+    ids = torch.zeros(4, 8, dtype=torch.int32, device="cuda")
+    with L.LaCache(d=64, k=8, capacity=64, tau_c=0.9, tau_a=0.8, top_c=2, max_batch=4) as cache:
+        cache.insert(x, x, ids)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        for stream, handle in ((side, side.cuda_stream), (side.cuda_stream, side.cuda_stream), (0, 0), (None, 0)):
+            out = cache.lookup(x, x, ids, cuda_stream=stream)
+            torch.cuda.synchronize()
+            at = out["entry_id"].data_ptr()
+            (where,) = [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]]
+            assert where == handle and out["entry_id"].tolist() == [0, 1, 2, 3]
