@@ -571,12 +571,28 @@ class LaCache:
 # What the calls that decode token by token need of torch, which is imported late: a call's every look-up of it would be a
 # tenth of the call.
 _DTYPES: dict = {}   # torch dtype -> lacache_dtype
-_INT32 = _RAW_STREAM = None
+_INT32 = _RAW_STREAM = _Rotation = None
 
 
 def _bind_torch() -> None:
-    global _INT32, _RAW_STREAM
+    global _INT32, _RAW_STREAM, _Rotation
+    if _Rotation is not None:
+        return
     import torch
+
+    class _Rotation(torch.autograd.Function):
+        """Rope.apply for autograd: linear, its gradient the inverse at the same positions."""
+
+        @staticmethod
+        def forward(ctx, x, pos, rope, inverse, cuda_stream):
+            ctx.save_for_backward(pos)
+            ctx.rope, ctx.inverse = rope, inverse
+            return rope.apply(x, pos, inverse, cuda_stream=cuda_stream)
+
+        @staticmethod
+        def backward(ctx, grad):
+            return ctx.rope.apply(grad.contiguous(), ctx.saved_tensors[0], not ctx.inverse), None, None, None, None
+
     _DTYPES.update({torch.bfloat16: LACACHE_BF16, torch.float16: LACACHE_F16, torch.float32: LACACHE_F32})
     _INT32, _RAW_STREAM = torch.int32, getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -647,10 +663,14 @@ class Rope:
 
     def apply(self, x, pos, inverse: bool = False, out=None, cuda_stream=None):
         """x [n x heads x head_dim] rotated at ``pos`` (int32 [n]) into ``out`` (new if None; x itself for in place).
-        ``inverse``: the transpose, which is the gradient."""
+        ``inverse``: the transpose, which is the gradient; autograd takes it, where there is no ``out``."""
         n, heads, head_dim = _three("x", x)
         device, dtype = x.get_device(), x.dtype
         import torch
+        if (x.requires_grad or out is not None and out.requires_grad) and torch.is_grad_enabled():
+            if out is not None:
+                raise ValueError("autograd does not follow a rotation into a given out: use torch.no_grad(), or no out")
+            return _Rotation.apply(x, pos, self, inverse, cuda_stream)
         if out is None:
             out = _new_like(x, cuda_stream, device)
         args = (self.plan, n, heads, head_dim, _dtype(x), _rows("x", x, n, heads, head_dim, device, dtype),
@@ -678,7 +698,7 @@ class KVCache:
     Tables are int32 [sequences x pages] CUDA tensors, lengths and positions int32 vectors, rows [tokens x heads x head_dim]
     tensors with dense rows. Calls run on torch's current stream of the cache's device unless given another (and then allocate
     the results that they are not given from its memory). A cache's calls share scratch: issue them on one stream, or order the
-    streams by events."""
+    streams by events. Autograd does not follow them."""
 
     FORMATS = {"bf16": LACACHE_KV_BF16, "f16": LACACHE_KV_F16, "e4m3": LACACHE_KV_E4M3, "int8": LACACHE_KV_INT8}
 

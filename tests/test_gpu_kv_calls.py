@@ -113,3 +113,41 @@ def test_a_lookup_on_another_stream_allocates_there():
             at = out["entry_id"].data_ptr()
             (where,) = [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]]
             assert where == handle and out["entry_id"].tolist() == [0, 1, 2, 3]
+
+
+def test_autograd_goes_through_the_rotation():
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    pos = torch.arange(100, 107, dtype=torch.int32, device="cuda")
+    for rope in (L.Rope(32, interleaved=True, amplitude=1.5), L.Rope(48), L.Rope(20)):
+        for inverse in (False, True):
+            x, g = (torch.randn(7, 3, 64, generator=gen, device="cuda") for _ in range(2))
+            x.requires_grad_(True)
+            y = rope.apply(x, pos, inverse=inverse)
+            with torch.no_grad():
+                plain = rope.apply(x, pos, inverse=inverse)
+                want = rope.apply(g, pos, inverse=not inverse)
+            assert y.requires_grad and not plain.requires_grad and torch.equal(y, plain)
+            (got,) = torch.autograd.grad(y, x, g)
+            assert torch.equal(got, want)
+            # against differences: f(x) = <g, y> is linear
+            d = torch.randn(7, 3, 64, generator=gen, device="cuda")
+            with torch.no_grad():
+                up, down = ((g.double() * rope.apply(x + e * 0.5 * d, pos, inverse=inverse).double()).sum() for e in (1, -1))
+            assert abs(float(up - down) - float((got.double() * d.double()).sum())) < 1e-4
+
+
+def test_autograd_of_shared_and_strided_rows():
+    # a gradient that autograd expands (a sum's: strides of zero), and a leaf that is used twice
+    rope, pos = L.Rope(64), torch.arange(5, dtype=torch.int32, device="cuda")
+    x = torch.randn(5, 2, 64, device="cuda").bfloat16().requires_grad_(True)
+    (rope.apply(x, pos).float().sum() + rope.apply(x, pos, inverse=True).float().sum()).backward()
+    ones = torch.ones(5, 2, 64, device="cuda").bfloat16()
+    want = rope.apply(ones, pos, inverse=True).float() + rope.apply(ones, pos).float()
+    assert torch.allclose(x.grad.float(), want, atol=2 ** -6)
+    stored = torch.empty(5, 2, 64, device="cuda").bfloat16()
+    for out in (stored, x):          # autograd cannot follow a given output
+        with pytest.raises(ValueError):
+            rope.apply(x, pos, out=out)
+    with torch.no_grad():
+        rope.apply(x, pos, out=stored)
