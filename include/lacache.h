@@ -418,7 +418,7 @@ typedef struct {
 
 /* Fill *out. rot_dim is even, 2..LACACHE_MAX_HEAD_DIM (for LACACHE_ROPE_BASE at least 4); base > 1; factor > 0 (ignored by
  * LACACHE_ROPE_PLAIN); original_len > 0 and low_turns < high_turns for LACACHE_ROPE_BANDED (ignored otherwise); amplitude is
- * finite (1 for none). */
+ * finite (1 for none). Arguments whose frequencies are not finite are LACACHE_ERR_INVALID_ARG. */
 lacache_status lacache_rope_init(int32_t rot_dim, int32_t layout, double base, int32_t scaling, double factor,
                                  double original_len, double low_turns, double high_turns, float amplitude,
                                  lacache_rope* out);

@@ -87,14 +87,14 @@ extern "C" lacache_status lacache_rope_init(int32_t rot_dim, int32_t layout, dou
   if (scaling == LACACHE_ROPE_BASE && rot_dim < 4) return LACACHE_ERR_INVALID_ARG;
   if (scaling == LACACHE_ROPE_BANDED &&
       (!(original_len > 0.0) || !isfinite(original_len) || !(low_turns < high_turns) || !isfinite(low_turns) ||
-       !isfinite(high_turns)))
+       !isfinite(high_turns) || !isfinite(high_turns - low_turns)))
     return LACACHE_ERR_INVALID_ARG;
   lacache_rope r = {};
   r.rot_dim = rot_dim;
   r.layout = layout;
   r.amplitude = amplitude;
   if (scaling == LACACHE_ROPE_BASE) base *= pow(factor, (double)rot_dim / (rot_dim - 2));
-  if (!isfinite(base)) return LACACHE_ERR_INVALID_ARG;
+  if (!(base > 0.0) || !isfinite(base)) return LACACHE_ERR_INVALID_ARG;
   const double two_pi = 6.283185307179586476925;
   for (int i = 0; i < rot_dim / 2; ++i) {
     double turns = pow(base, -2.0 * i / rot_dim) / two_pi;   // a position
@@ -104,6 +104,7 @@ extern "C" lacache_status lacache_rope_init(int32_t rot_dim, int32_t layout, dou
       g = g < 0.0 ? 0.0 : g > 1.0 ? 1.0 : g;
       turns = (1.0 - g) * turns / factor + g * turns;
     }
+    if (!isfinite(turns)) return LACACHE_ERR_INVALID_ARG;
     const double phase = ldexp(turns - floor(turns), 64);   // in [0, 2^64]
     r.turn[i] = phase >= 18446744073709551616.0 ? 0u : (uint64_t)phase;
   }
