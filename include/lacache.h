@@ -426,8 +426,8 @@ lacache_status lacache_rope_init(int32_t rot_dim, int32_t layout, double base, i
 /* Rotate n tokens of `heads` heads from *x into *y (the same array, for in place, or one that does not overlap it), in
  * `dtype` (bf16, f16 or f32; the arithmetic is fp32). pos_dev[i] is token i's position, any int32. inverse != 0 applies the
  * transpose of the rotation (angles negated, the same amplitude): the gradient of the call with inverse == 0. head_dim is a
- * multiple of 8, rope->rot_dim..LACACHE_MAX_HEAD_DIM. n = 0 does nothing. Runs on the current device, asynchronously on
- * cuda_stream. */
+ * multiple of 8, rope->rot_dim..LACACHE_MAX_HEAD_DIM; heads is at most 2^30. n = 0 does nothing. Runs on the current device,
+ * asynchronously on cuda_stream. */
 lacache_status lacache_rope_apply(const lacache_rope* rope, int64_t n, int32_t heads, int32_t head_dim, int32_t dtype,
                                   const lacache_rows* x, const int32_t* pos_dev, int32_t inverse, const lacache_rows* y,
                                   void* cuda_stream);
@@ -483,7 +483,7 @@ typedef struct {
  * padding). No two of a call may name the same slot. k and v are [n x kv_heads] rows in `dtype` (bf16, f16 or f32),
  * converted to the cache's format. With rope != NULL, k is rotated first, by rope_pos_dev[i] (NULL: pos_dev[i]); if
  * q != NULL, its [n x q_heads] rows are rotated the same way into *q_out (same dtype; in place or not overlapping; skipped
- * tokens' rows are not written). rope == NULL copies q. n = 0 does nothing. Asynchronous on cuda_stream; may be captured
+ * tokens' rows are not written; q_heads at most 2^30). rope == NULL copies q. n = 0 does nothing. Asynchronous on cuda_stream; may be captured
  * into a CUDA graph. */
 lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table, int64_t n,
                                  const int32_t* seq_dev, const int32_t* pos_dev, const lacache_rope* rope,

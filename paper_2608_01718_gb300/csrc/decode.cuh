@@ -36,6 +36,7 @@ constexpr unsigned int kBadIndex = 1u, kAttendTimeout = 2u;
 constexpr int kMaxHeadDim = LACACHE_MAX_HEAD_DIM;
 constexpr int kMaxNewTokens = 512;
 constexpr int kMaxQHeads = 1 << 16;
+constexpr int kMaxRowHeads = 1 << 30;   // of a rotation or a write: a token's rows, and some passes more, are counted in 32 bits
 
 struct Rows {   // lacache_rows on the device
   unsigned char* p;

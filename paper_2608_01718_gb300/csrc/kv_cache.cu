@@ -330,6 +330,7 @@ extern "C" lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, cons
       !lc::device_table(table, &a.table))
     return LACACHE_ERR_INVALID_ARG;
   if (rope && (rope->rot_dim < 2 || rope->rot_dim % 2 || rope->rot_dim > h->cfg.head_dim)) return LACACHE_ERR_INVALID_ARG;
+  if (q && q_heads > lc::kMaxRowHeads) return LACACHE_ERR_UNSUPPORTED;
   if (n == 0) return LACACHE_OK;
   if (!seq_dev || !pos_dev || !lc::device_rows(k, dtype, &a.k) || !lc::device_rows(v, dtype, &a.v))
     return LACACHE_ERR_INVALID_ARG;

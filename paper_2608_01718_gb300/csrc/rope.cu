@@ -119,7 +119,7 @@ extern "C" lacache_status lacache_rope_apply(const lacache_rope* rope, int64_t n
   lc::Rows xr, yr;
   if (!rope || n < 0 || heads < 1 || head_dim < 1 || !lc::known_dtype(dtype)) return LACACHE_ERR_INVALID_ARG;
   if (rope->rot_dim < 2 || rope->rot_dim % 2 || rope->rot_dim > head_dim) return LACACHE_ERR_INVALID_ARG;
-  if (head_dim % 8 || head_dim > lc::kMaxHeadDim) return LACACHE_ERR_UNSUPPORTED;
+  if (head_dim % 8 || head_dim > lc::kMaxHeadDim || heads > lc::kMaxRowHeads) return LACACHE_ERR_UNSUPPORTED;
   if (n == 0) return LACACHE_OK;
   if (!pos_dev || !lc::device_rows(x, dtype, &xr) || !lc::device_rows(y, dtype, &yr)) return LACACHE_ERR_INVALID_ARG;
   const float sign = inverse ? -1.f : 1.f;

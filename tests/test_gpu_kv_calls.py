@@ -1,4 +1,6 @@
-"""The decoding calls' arguments: what is refused, strides and numbers at the edges, streams and gradients."""
+"""The decoding calls' arguments: what is refused, numbers at the edges, streams and gradients."""
+import ctypes
+
 import pytest
 import torch
 
@@ -151,3 +153,15 @@ def test_autograd_of_shared_and_strided_rows():
             rope.apply(x, pos, out=out)
     with torch.no_grad():
         rope.apply(x, pos, out=stored)
+
+
+def test_counts_of_query_heads_past_32_bits():
+    c = Filled("bf16", [16], 1, 64, seed=37)
+    lib, ref = L.load(), ctypes.addressof
+    rows = L.lacache_rows(c.k_rows.data_ptr(), 64, 64)
+    table = L.lacache_kv_table(c.table.data_ptr(), c.table.stride(0), 1, c.table.shape[1])
+    for heads, n, want in (((1 << 31) - 1, 16, L.LACACHE_ERR_UNSUPPORTED), ((1 << 30) + 1, 16, L.LACACHE_ERR_UNSUPPORTED),
+                           (1 << 30, 0, L.LACACHE_OK)):
+        assert lib.lacache_kv_append(c.kv.h, 0, ref(table), n, c.seq.data_ptr(), c.pos.data_ptr(), None, None, L.LACACHE_BF16,
+                                     ref(rows), ref(rows), heads, ref(rows), ref(rows), None) == want
+    c.kv.sync()
