@@ -407,7 +407,8 @@ typedef enum {
                               (1 - g) w_i / factor + g w_i with g = (r_i - low_turns) / (high_turns - low_turns) */
 } lacache_rope_scaling;
 /* A rotation's plan, filled by lacache_rope_init on the host and passed by value to the kernels: no device memory. turn[i]
- * is w_i / 2 pi as a fraction of 2^64, so that position * turn[i] modulo 2^64 is the exact phase at every position. */
+ * is w_i / 2 pi as a fraction of 2^64 (computed in double), and position * turn[i] modulo 2^64 the phase, without a rounding of
+ * its own: 2^-35 of a turn from the phase of the exact w_i at position 10^6, 2^-24 at 2^31. */
 typedef struct {
   int32_t rot_dim;
   int32_t layout;
@@ -483,8 +484,8 @@ typedef struct {
  * padding). No two of a call may name the same slot. k and v are [n x kv_heads] rows in `dtype` (bf16, f16 or f32),
  * converted to the cache's format. With rope != NULL, k is rotated first, by rope_pos_dev[i] (NULL: pos_dev[i]); if
  * q != NULL, its [n x q_heads] rows are rotated the same way into *q_out (same dtype; in place or not overlapping; skipped
- * tokens' rows are not written; q_heads at most 2^30). rope == NULL copies q. n = 0 does nothing. Asynchronous on cuda_stream; may be captured
- * into a CUDA graph. */
+ * tokens' rows are not written; q_heads at most 2^30). rope == NULL copies q. n = 0 does nothing. Asynchronous on
+ * cuda_stream; may be captured into a CUDA graph. */
 lacache_status lacache_kv_append(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table, int64_t n,
                                  const int32_t* seq_dev, const int32_t* pos_dev, const lacache_rope* rope,
                                  const int32_t* rope_pos_dev, int32_t dtype, const lacache_rows* k,
@@ -530,9 +531,9 @@ lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_k
 lacache_status lacache_kv_sync(lacache_kv_t* h);
 
 /* Test support for failure detection: the next `attends` calls of lacache_kv_attend that have many rows (more than 16 a kv
- * head, 32 over 8-bit caches with heads of up to 64; heads of up to 128) make the block that holds the first keys withhold its loads. The
- * bounded waits for them (about a second) run out, the block records the timeout, frees what it holds and ends, and
- * lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT. Nothing faults, and the context stays usable. 0 cancels. */
+ * head, 32 over 8-bit caches with heads of up to 64; heads of up to 128) make the block that holds the first keys withhold
+ * its loads. The bounded waits for them (about a second) run out, the block records the timeout, frees what it holds and
+ * ends, and lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT. Nothing faults, and the context stays usable. 0 cancels. */
 lacache_status lacache_kv_inject_stall(lacache_kv_t* h, int32_t attends);
 
 #ifdef __cplusplus

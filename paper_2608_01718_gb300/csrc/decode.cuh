@@ -190,8 +190,9 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-// cos and sin, times the amplitude, of pair i at `pos`, the sine times `sign` (-1 for the inverse). The phase position * turn is exact modulo a turn; its upper 32 bits
-// are the fraction of a turn in [-1/2, 1/2), to 2^-33, at every position.
+// cos and sin, times the amplitude, of pair i at `pos`, the sine times `sign` (-1 for the inverse). position * turn is exact
+// modulo a turn, so the phase is as good as the turn that is stored (a double's 53 bits: position * 2^-55 of a turn or so, 2^-35
+// at position 10^6 and 2^-24 at 2^31). Its upper 32 bits are the fraction of a turn in [-1/2, 1/2), cut to 2^-32.
 __device__ __forceinline__ float2 rope_angle(const lacache_rope& r, int i, int pos, float sign) {
   const uint64_t phase = r.turn[i] * (uint64_t)(int64_t)pos;
   const float half_turns = (float)(int32_t)(uint32_t)(phase >> 32) * 4.656612873077393e-10f;   // 2^-31: in half turns

@@ -8,10 +8,10 @@
 // every choice below is about keeping enough loads in flight with little work a byte.
 //
 // Measured (bf16 q, 32 q heads on 8, d = 128, lse written; 6.69 TB/s is a plain copy's rate here): 200,003 tokens of one
-// sequence 129 us, 6.4 TB/s; 32 sequences of 0 to 4,096 50 us, 5.5 TB/s, of which some 8 us are start and joins; e4m3, 64 of 500
+// sequence 131 us, 6.3 TB/s; 32 sequences of 0 to 4,096 50 us, 5.5 TB/s, of which some 8 us are start and joins; e4m3, 64 of 500
 // to 16,384 185 us, 6.2 TB/s. One sequence of 100 tokens (8 heads, d = 64): 5.8 us, a launch, two dependent loads to the
-// first K, and a join. d = 256 with 16 rows (int8, a window of 1,024, 48 sequences): 42 us, 2.4 TB/s: there 255 registers
-// leave two warps a scheduler and widening and products are 25,000 instructions an SM quarter, issued in 35% of the cycles.
+// first K, and a join. d = 256 with 16 rows (int8, a window of 1,024, 48 sequences): 44 us, 2.3 TB/s: there 255 registers
+// leave two warps a scheduler and widening and products are 26,000 instructions an SM quarter, issued in 34% of the cycles.
 //
 // Products. Both run on the warp-level tensor instruction m16n8k16, with keys (or dimensions) as M and the rows of q as N:
 // a tile of 8 rows wastes nothing at 8 rows, where the 64- or 128-row tiles of tcgen05 would take the scores through TMEM
@@ -33,6 +33,10 @@
 // maximum, keys of small weight and large values lost some of theirs.) Weights: f16 for f16 and 8-bit caches (11
 // bits); on a bf16 cache, whose products need bf16 weights of 8 bits, a weight is split in two bf16 terms (16 bits), as
 // one alone would add an error as large as the output's own rounding.
+//
+// Sums that are not finite, or past 2^110. A warp that finds one at a triple's end does its part of it again with weights of at
+// most 1, and with V's values that are no finite numbers taken out of the tiles and multiplied in fp32 for the rows that see
+// them: so none reaches a row by a weight of zero, or meets a weight's term that was rounded to zero.
 //
 // 8-bit rows. Codes become f16 exactly. q of a bf16 type is scaled to f16 by a power of two that brings its row's largest
 // magnitude to [1, 2): exact for elements within 2^-14 of that. The scales multiply the scores (k) and the weights (v);
@@ -102,11 +106,21 @@ cudaError_t launch_attend_f16(const AttendArgs& a, int num_sms, cudaStream_t st)
 cudaError_t launch_attend_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_attend_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
 // The tcgen05 kernel for many rows (kv_attend_tc.cu): heads of up to 128.
-// From how many rows: measured for 4 kv heads (us, this kernel / tcgen05) over 32 x 2,000 tokens, 2 x 1,000, 4 x 30,000, 64 x 100
-//   bf16, d = 128   16 rows 34 / 36, 16 / 12, 61 / 55, 13 / 15     20 rows 46 / 37, 21 / 12, 79 / 56, 17 / 16
-//   bf16, d = 64    16 rows 23 / 30, 12 / 11, 37 / 50, 10 / 14     20 rows 32 / 30, 16 / 11, 47 / 50, 12 / 14
-//   e4m3, d = 128   16 rows 30 / 51, 15 / 14, 52 / 83, 11 / 18     24 rows 63 / 51, 26 / 14 (a second tile of 16)
-//   e4m3, d = 64    20 rows 39 / 49, 18 / 13, 54 / 77, 14 / 17     32 rows 42 / 49, 20 / 13, 61 / 77, 15 / 17
+// From how many rows: us of this kernel / tcgen05 over 32 x 2,000 tokens, 2 x 1,000, 4 x 30,000, 64 x 100
+//   4 kv heads, bf16, d = 128   16 rows 34 / 37, 14 / 12, 64 / 55, 12 / 16     20 rows 43 / 37, 16 / 12, 86 / 56, 18 / 16
+//               bf16, d = 64    16 rows 23 / 31, 12 / 11, 36 / 50, 9 / 14      20 rows 31 / 31, 11 / 11, 48 / 50, 14 / 14
+//               e4m3, d = 128   16 rows 32 / 51, 16 / 14, 51 / 82, 12 / 18     20 rows 46 / 51, 15 / 14, 68 / 82, 20 / 18
+//               e4m3, d = 64    20 rows 43 / 49, 18 / 13, 57 / 77, 15 / 17     32 rows 46 / 49, 20 / 13, 65 / 77, 16 / 17
+//   8 kv heads, bf16, d = 128   16 rows 54 / 63, 16 / 13, 91 / 94, 19 / 26     20 rows 91 / 63, 15 / 13, 156 / 95, 31 / 26
+//               bf16, d = 64    16 rows 34 / 58, 12 / 12, 52 / 86, 15 / 23     20 rows 53 / 58, 13 / 12, 81 / 87, 24 / 23
+//               e4m3, d = 128   16 rows 48 / 92, 16 / 16, 73 / 149, 20 / 30    20 rows 79 / 92, 18 / 16, 115 / 149, 35 / 30
+//               e4m3, d = 64    20 rows 66 / 87, 19 / 15, 85 / 143, 27 / 27    32 rows 69 / 87, 21 / 15, 90 / 143, 28 / 27
+//   1 kv head,  bf16, d = 128   16 rows 17 / 18, 13 / 12, 58 / 26, 12 / 11     20 rows 23 / 18, 14 / 12, 36 / 27, 12 / 11
+//               e4m3, d = 128   16 rows 19 / 24, 15 / 14, 35 / 34, 12 / 12     20 rows 22 / 24, 16 / 14, 38 / 35, 11 / 12
+// f16 is as bf16, int8 as e4m3 with tcgen05 some 10% slower; 24 and 32 rows as 20, which are tiles of 16 twice (of 32 over
+// 8-bit heads of 64). Where the rule takes the slower one: 17 to 32 rows over long 8-bit caches at d = 128 (by 10 to 30%, int8
+// by up to 47%; short ones are faster so, and weights keep 16 bits instead of 11), 20 rows over 8 heads of 64 in bf16 (by 8%),
+// and 16 rows over long caches of few heads at d = 128 in 16 bits (64 for 55, with one head 58 for 26).
 inline bool takes_tc(int rows, int group, int head_dim, bool eight) {   // (group: its products with rows fit in 32 bits)
   return head_dim <= 128 && group <= 2048 && rows > (eight && head_dim <= 64 ? 32 : 16);
 }
@@ -570,41 +584,41 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             }
             raw = pack8(x, __half());
           }
-      if (d0 < DP) *reinterpret_cast<uint4*>(q_smem + r * C::kQStride + d0 * 2) = raw;
-      if (lane == 0) {
-        const int p = live ? sp.len - a.new_tokens + tok : -1;
-        int lo = a.starts ? a.starts[seq] : 0;
-        if (a.window > 0 && p - a.window + 1 > lo) lo = p - a.window + 1;
-        row_pos[r] = p;
-        row_lo[r] = lo;
-        row_factor[r] = a.scale * 1.4426950408889634f * back;
-      }
-    }
-    __syncthreads();
-
-    all_hi = row_pos[0];
-    all_lo = row_lo[live_rows - 1];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      factor[n][0] = row_factor[n * 8 + 2 * t];
-      factor[n][1] = row_factor[n * 8 + 2 * t + 1];
-    }
-    if constexpr (kQInRegs) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int c = 0; c < C::kKPieces; ++c) {
-          const unsigned char* q = q_smem + (n * 8 + g) * C::kQStride;
-          if constexpr (C::kEight) {
-            const uint4* p = reinterpret_cast<const uint4*>(q + (c * 64 + t * 16) * 2);
-            qreg[(n * C::kKPieces + c) * 2] = p[0];
-            qreg[(n * C::kKPieces + c) * 2 + 1] = p[1];
-          } else {
-            qreg[n * C::kKPieces + c] = *reinterpret_cast<const uint4*>(q + (c * 32 + t * 8) * 2);
+          if (d0 < DP) *reinterpret_cast<uint4*>(q_smem + r * C::kQStride + d0 * 2) = raw;
+          if (lane == 0) {
+            const int p = live ? sp.len - a.new_tokens + tok : -1;
+            int lo = a.starts ? a.starts[seq] : 0;
+            if (a.window > 0 && p - a.window + 1 > lo) lo = p - a.window + 1;
+            row_pos[r] = p;
+            row_lo[r] = lo;
+            row_factor[r] = a.scale * 1.4426950408889634f * back;
           }
         }
-      }
-    }
+        __syncthreads();
+
+        all_hi = row_pos[0];
+        all_lo = row_lo[live_rows - 1];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          factor[n][0] = row_factor[n * 8 + 2 * t];
+          factor[n][1] = row_factor[n * 8 + 2 * t + 1];
+        }
+        if constexpr (kQInRegs) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int c = 0; c < C::kKPieces; ++c) {
+              const unsigned char* q = q_smem + (n * 8 + g) * C::kQStride;
+              if constexpr (C::kEight) {
+                const uint4* p = reinterpret_cast<const uint4*>(q + (c * 64 + t * 16) * 2);
+                qreg[(n * C::kKPieces + c) * 2] = p[0];
+                qreg[(n * C::kKPieces + c) * 2 + 1] = p[1];
+              } else {
+                qreg[n * C::kKPieces + c] = *reinterpret_cast<const uint4*>(q + (c * 32 + t * 8) * 2);
+              }
+            }
+          }
+        }
       }
       copy_wait<C::kStages - 1>();
       __syncwarp();
@@ -873,7 +887,8 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             auto no_numbers = [](uint32_t x) { return __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu); };
             bool fix = false;
 #pragma unroll 1
-            for (int i = 0; i < C::kTileBytes / 128; ++i) fix |= no_numbers(reinterpret_cast<const uint32_t*>(codes)[i * 32 + lane]) != 0;
+            for (int i = 0; i < C::kTileBytes / 128; ++i)
+              fix |= no_numbers(reinterpret_cast<const uint32_t*>(codes)[i * 32 + lane]) != 0;
             if (__any_sync(0xffffffffu, fix)) {
               const int k0 = key + 16 * b;
 #pragma unroll 1

@@ -19,17 +19,19 @@
 // K is the first product's B operand as stored (K-major); V, as stored, the second's with its dimensions contiguous
 // (MN-major), so neither is transposed. Work is cut and joined as in kv_attend.cuh, in units of 128 keys.
 //
-// Measured (32 q heads on 4, d = 128): bf16, 16 sequences of 300 to 3,000 tokens, 17 new ones (136 rows, two tiles) 34.5 us, of
+// Measured (32 q heads on 4, d = 128): bf16, 16 sequences of 300 to 3,000 tokens, 17 new ones (136 rows, two tiles) 35.5 us, of
 // which 5 us until the first S, 2 a unit of 64 KB, 2.5 for a triple's end and up to 6 for joins; 4 sequences of 30,000 tokens
-// and 36 rows 57 us (4.3 TB/s), 136 rows 99 us; f16 56 and 96, e4m3 93 and 170 (widening: three warps, 32,000 codes a unit).
+// and 36 rows 57 us (4.3 TB/s), 136 rows 99 us; f16 56 and 96, e4m3 92 and 169, int8 104 and 192 (widening: three warps, 32,000
+// codes a unit). Of 200,000 keys, 32 rows that are not finite take 235 ms more (below).
 // With the loads left out a unit takes 1.6 us (1.0 of tensor time in bf16), with the softmax left out 1.9: no one part
 // bounds the kernel, their overlap within a ring of seven slots does.
 //
 // An output that is not finite, or near the end of fp32's range, is computed again key by key with weights of at most 1: a
 // masked key's value times a zero weight, an infinity times a weight's second term, or weights above 1 may have made it so.
 //
-// Every wait is bounded (about a second, renewed while a row is computed again): past it the block records a timeout, its roles stop, copies and products in flight
-// are drained, TMEM is freed and the block ends, after it has arrived where it shares triples; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
+// Every wait is bounded (about a second, renewed while a row is computed again): past it the block records a timeout, its roles
+// stop, copies and products in flight are drained, TMEM is freed and the block ends, after it has arrived where it shares
+// triples; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
 #include "kv_attend.cuh"
 #include "tcgen05.cuh"
 

@@ -5,9 +5,11 @@
 // of its tokens a warp finds the place and the angles once, and runs over the rows.
 //
 // Measured (bf16 rows, 32 q heads, 8 of k and v, d = 128): 12,001 tokens written to an e4m3 cache, half of each head rotated,
-// 52 us, 5.2 TB/s; all rotated 58; to a bf16 cache 54, 5.4 TB/s. A loop for q's rows of its own is 6% faster for the e4m3
-// cache than one for all rows (3% slower for the bf16 one); four rows in flight instead of two spill. 60,000 tokens of int8
-// read as f16: 64 us, 5.9 TB/s. Of 32 tokens written and 333 read: 4.3 and 2.9 us, a launch and two dependent loads.
+// interleaved, 52 us, 5.2 TB/s; all rotated, in the half layout 57 and interleaved 54; the same to an int8 cache; to a bf16 cache
+// 54 (half layout, all rotated), 5.4 TB/s. A loop for q's rows of its own is 6% faster for the e4m3 cache than one for all rows
+// (3% slower for the bf16 one). Of 16-bit rows, the rotated kernels of whole chunks spill 36 to 48 bytes a thread (half layout)
+// and 16 to 20 (interleaved) at the cap of 96 registers; with four rows in flight instead of two 150 to 580. 60,000 tokens of
+// int8 read as f16: 64 us, 5.9 TB/s. Of 32 tokens written and 333 read: 4.3 and 2.9 us, a launch and two dependent loads.
 #include <new>
 #include <type_traits>
 

@@ -815,8 +815,8 @@ class KVCache:
                               None if starts is None else _index("starts", starts, t.seqs, dev),
                               _rows("q", q, n, heads, D, dev, dtype), _rows("out", out, n, heads, D, dev, dtype),
                               None if lse is None else lse.data_ptr())
-        _check("lacache_kv_attend", self._lib.lacache_kv_attend(self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a),
-                                                                _current_stream(cuda_stream, dev)))
+        _check("lacache_kv_attend", self._lib.lacache_kv_attend(
+            self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a), _current_stream(cuda_stream, dev)))
         return out
 
     def sync(self) -> None:
