@@ -220,3 +220,55 @@ def test_a_long_sequence_that_is_not_finite_leaves_the_others_alone(where, n):
         assert np.isposinf(got[1, ..., 3]).all() and np.isnan(got[1, ..., 5]).all()
         assert np.all((np.abs(got[1] - want) <= tol)[..., rest]) and np.all(np.abs(got_lse[1] - want_lse) <= tol_lse)
     kv.close()
+
+
+@pytest.mark.parametrize("fmt,dtype", [("bf16", "bf16"), ("f16", "f16"), ("e4m3", "bf16"), ("int8", "f16")])
+@pytest.mark.parametrize("new,group", [(1, 3), (3, 2), (4, 4), (7, 4), (10, 12)])
+@pytest.mark.parametrize("head_dim,window", [(64, 0), (80, 37), (128, 150), (256, 0)])
+def test_scattered_values_that_are_not_finite(fmt, dtype, new, group, head_dim, window):
+    """Infinities and NaN here and there in V, and NaN in K, of many ragged sequences, most of which are finite: every output is what the
+    oracle's is, finite, infinite or NaN. (8-bit caches: NaN codes of e4m3, NaN scales of both.)"""
+    rng = np.random.default_rng(new * 1000 + head_dim + window)
+    lengths = [int(n) for n in rng.integers(0, 260, 30)] + [1500, new, new + 1]
+    c = Filled(fmt, lengths, 2, head_dim, seed=27)
+    pool = c.kv.pool()
+    bad = {"bf16": [np.inf, -np.inf, np.nan], "f16": [np.inf, -np.inf, np.nan]}.get(fmt, [])
+    for s in range(0, len(lengths), 2):
+        for _ in range(int(rng.integers(1, 6))):
+            n = lengths[s]
+            if n == 0:
+                continue
+            p = int(rng.integers(max(0, n - 2 * new), n)) if rng.random() < 0.6 else int(rng.integers(0, n))
+            page, at, h, d = int(c.host_table[s, p // c.page]), p % c.page, int(rng.integers(0, 2)), int(rng.integers(0, head_dim))
+            kind = rng.random()
+            if kind < 0.15:                                                    # K: the whole row for those who see it
+                if fmt in ("bf16", "f16"):
+                    pool["k"][page, h, at, d] = float("nan")
+                else:
+                    pool["ks"][page, h, at] = float("nan")
+            elif fmt in ("bf16", "f16"):
+                pool["v"][page, h, at, d] = float(bad[int(rng.integers(0, 3))])
+            elif fmt == "e4m3" and kind < 0.8:
+                pool["v"].view(torch.uint8)[page, h, at, d] = 0x7f
+            else:
+                pool["vs"][page, h, at] = float("nan")
+    starts = [int(rng.integers(0, n + 1)) if rng.random() < 0.3 else 0 for n in lengths]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(28)
+    q = torch.randn(len(lengths) * new, 2 * group, head_dim, generator=gen, device="cuda").to(TORCH[dtype])
+    out = c.kv.attend(q, c.table, c.len_dev, new_tokens=new, window=window,
+                      starts=torch.tensor(starts, dtype=torch.int32, device="cuda"))
+    c.kv.sync()
+    k, v = c.values()
+    hq = q.double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want, _, _, _ = decode.attend(hq, k, v, lengths, new, head_dim ** -0.5, starts, window)
+        got = out.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.isnan(want).any()
+        assert np.array_equal(np.isposinf(got), np.isposinf(want)) and np.array_equal(np.isneginf(got), np.isneginf(want))
+        # what is finite, against the same without them
+        k, v = [[np.nan_to_num(x, nan=0.0, posinf=0.0, neginf=0.0) for x in rows] for rows in (k, v)]
+        clean, lse, mass, span = decode.attend(hq, k, v, lengths, new, head_dim ** -0.5, starts, window)
+        tol, _ = bounds(clean, mass, span, lse, hq, k, head_dim ** -0.5, dtype)
+        fine = np.isfinite(want)
+        assert np.all((np.abs(got - want) <= tol)[fine])
