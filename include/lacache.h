@@ -336,6 +336,32 @@ size_t lacache_calibrate_workspace_bytes(void);
 lacache_status lacache_verify_draft(int32_t B, int32_t k, const float* p_target_dev, const float* p_draft_dev,
                                     const uint8_t* status_dev, int32_t* accepted_dev, void* cuda_stream);
 
+/* Probabilities of next tokens: a device array of [queries x positions x vocab] fp32 with any query and position strides;
+ * a row's elements are dense. */
+typedef struct {
+  const float* data_dev;
+  int64_t seq_stride;   /* elements */
+  int64_t token_stride; /* elements */
+} lacache_probs;
+
+/* The same for drafts that were drawn at random, or are to be followed by a drawn token: verification from given random
+ * numbers, whose accepted drafts and next token are together distributed as the target model's own tokens. Query b has up to
+ * k drafts drafts_dev[b * k + t] (0 <= k <= 256; an id outside [0, vocab), such as -1, ends the window there),
+ * p_target [B x (k + 1)] rows, p_draft [B x k] rows, and u_dev [B x (k + 1)] numbers in [0, 1).
+ *  - Draft x at t is accepted while u_t * p_draft(x) < p_target(x) (as real numbers); the first that is not ends the window
+ *    and is refused. accepted_dev[b] = the number n of accepted drafts.
+ *  - token_dev[b] is drawn at position n: the first i with C_i > u_k * C_vocab, where C_i sums w_0 .. w_i, and
+ *    w = max(p_target - p_draft, 0) after a refusal, w = p_target otherwise (the window's end, or a refusal whose w is all
+ *    zeros). A NaN or negative weight counts as none; a row without any weight gives -1. The last token of any weight is taken
+ *    if none qualifies (u_k >= 1). C is summed to within 2^-40 of itself.
+ *  - p_draft == NULL: the drafts were not drawn (the draft model's likeliest tokens, or any others): p_draft(x) = 1.
+ *  - status_dev as above: served queries get -1 for both. Rows are probabilities: finite, and not negative.
+ * vocab is at most 2^30. Asynchronous on cuda_stream; may be captured into a CUDA graph. */
+lacache_status lacache_verify_sample(int32_t B, int32_t k, int32_t vocab, const lacache_probs* p_target,
+                                     const lacache_probs* p_draft, const int32_t* drafts_dev, const float* u_dev,
+                                     const uint8_t* status_dev, int32_t* accepted_dev, int32_t* token_dev,
+                                     void* cuda_stream);
+
 /* Static description of a status code. */
 const char* lacache_status_string(lacache_status s);
 

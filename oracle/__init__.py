@@ -13,11 +13,11 @@ from .lookup import (CHECK_BOTH, CHECK_EMB, CHECK_TOKENS, HIT, MISS_KEY, REJECT,
 from .serve import ServeLoop
 from .calibrate import calibrate, nearest_rank, pair_similarities
 from .lsh import LshKeyCheck, hamming, lookup_lsh, projections, signatures
-from .speculative import accepted_prefix
+from .speculative import accepted_prefix, verify_sample
 from .shards import merge as merge_shards
 from . import decode
 
 __all__ = ["round_to_bf16", "widen", "CHECK_BOTH", "CHECK_EMB", "CHECK_TOKENS", "HIT", "MISS_KEY", "REJECT",
            "KeyCheck", "Params", "Result", "Store", "decide", "lookahead", "lookup", "passes", "ServeLoop",
            "calibrate", "nearest_rank", "pair_similarities", "LshKeyCheck", "hamming", "lookup_lsh", "projections", "signatures",
-           "accepted_prefix", "merge_shards", "decode"]
+           "accepted_prefix", "verify_sample", "merge_shards", "decode"]

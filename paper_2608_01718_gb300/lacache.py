@@ -33,7 +33,7 @@ EXPORTS = ["lacache_create", "lacache_create_ensemble", "lacache_destroy", "laca
            "lacache_lookup_host", "lacache_lookup_host_async", "lacache_append_misses", "lacache_read_rows",
            "lacache_size", "lacache_sync", "lacache_last_launch", "lacache_stage_timing", "lacache_stage_times",
            "lacache_inject_stall", "lacache_enable_lsh", "lacache_read_signatures", "lacache_calibrate",
-           "lacache_calibrate_workspace_bytes", "lacache_verify_draft", "lacache_lookup_noalloc",
+           "lacache_calibrate_workspace_bytes", "lacache_verify_draft", "lacache_verify_sample", "lacache_lookup_noalloc",
            "lacache_merge_shards", "lacache_get_stats", "lacache_save", "lacache_load", "lacache_get_config",
            "lacache_rope_init", "lacache_rope_apply", "lacache_kv_create", "lacache_kv_destroy", "lacache_kv_get_pool",
            "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_sync", "lacache_kv_inject_stall",
@@ -68,6 +68,10 @@ class lacache_shard_result(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in
                 ("cand_id", "cand_score", "cand_prefix_score", "cand_matches", "cand_pass", "cand_prefix_scores",
                  "key_score", "n_cand")] + [("id_base", ctypes.c_int64)]
+
+
+class lacache_probs(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
 
 
 class lacache_rows(ctypes.Structure):
@@ -144,6 +148,7 @@ def load() -> ctypes.CDLL:
         "lacache_calibrate": ([i64, i32, vp, vp, ctypes.c_double, ctypes.c_float, vp, vp, vp, vp], i32),
         "lacache_calibrate_workspace_bytes": ([], ctypes.c_size_t),
         "lacache_verify_draft": ([i32, i32, vp, vp, vp, vp, vp], i32),
+        "lacache_verify_sample": ([i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp], i32),
         "lacache_lookup_noalloc": ([ctypes.POINTER(lacache_config), i64, vp, vp, vp, i32, vp, vp, vp,
                                     ctypes.POINTER(lacache_result), vp], i32),
         "lacache_get_stats": ([vp, ctypes.POINTER(lacache_stats), i32], i32),
@@ -384,6 +389,43 @@ def lacache_verify_draft(p_target, p_draft, status, accepted, cuda_stream=None) 
     B, k = int(p_target.shape[0]), int(p_target.shape[1])
     _check("lacache_verify_draft", load().lacache_verify_draft(B, k, _ptr(p_target), _ptr(p_draft), _ptr(status),
                                                                _ptr(accepted), _stream(cuda_stream)))
+
+
+def _dense(name: str, t, shape: tuple, dtype, device: int) -> int:
+    """A dense CUDA tensor's address."""
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name} is a dense {dtype} tensor of {list(shape)} on cuda:{device}")
+    return t.data_ptr()
+
+
+def lacache_verify_sample(p_target, p_draft, drafts, u, accepted, token, status=None, cuda_stream=None) -> None:
+    """Accepted drafts and the next token per query, from the random numbers ``u`` (fp32 [B x k + 1] in [0, 1)).
+
+    ``p_target`` [B x k + 1 x vocab] and ``p_draft`` [B x k x vocab] are fp32 probabilities (any strides, dense rows);
+    ``p_draft`` is None for drafts that were not drawn. ``drafts`` int32 [B x k] (-1 ends a window), ``accepted`` and ``token``
+    int32 [B]; -1 in both for served queries (``status``)."""
+    import torch
+    if p_target.dim() != 3 or not p_target.is_cuda:
+        raise ValueError("p_target is a [queries x drafts + 1 x vocab] CUDA tensor")
+    B, rows, vocab = p_target.shape
+    k, device = rows - 1, p_target.get_device()
+
+    def probs(name, t, n):
+        if t.shape != (B, n, vocab) or t.dtype != torch.float32 or t.get_device() != device or (t.stride(2) != 1 and vocab > 1):
+            raise ValueError(f"{name} is a [{B} x {n} x {vocab}] fp32 tensor with dense rows on cuda:{device}")
+        return lacache_probs(t.data_ptr(), t.stride(0), t.stride(1))
+
+    pt, pd = probs("p_target", p_target, rows), None if p_draft is None else probs("p_draft", p_draft, k)
+    args = (B, k, vocab, ctypes.addressof(pt), _address(pd), _dense("drafts", drafts, (B, k), torch.int32, device),
+            _dense("u", u, (B, rows), torch.float32, device),
+            None if status is None else _dense("status", status, (B,), torch.uint8, device),
+            _dense("accepted", accepted, (B,), torch.int32, device), _dense("token", token, (B,), torch.int32, device),
+            _stream(cuda_stream, device))
+    if torch.cuda.current_device() == device:
+        _check("lacache_verify_sample", load().lacache_verify_sample(*args))
+    else:
+        with torch.cuda.device(device):
+            _check("lacache_verify_sample", load().lacache_verify_sample(*args))
 
 
 def lacache_lookup_noalloc(cfg: lacache_config, key, prefix, ids, q_emb, q_prefix, q_ids, out: dict,
