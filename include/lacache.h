@@ -551,6 +551,59 @@ typedef struct {
 lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table,
                                  const lacache_attention* a, void* cuda_stream);
 
+/* Attention weights of cached tokens: a device array of [seqs x kv_heads x width] fp32 with any sequence and head strides; a
+ * row's elements, one a position, are dense. */
+typedef struct {
+  float* data_dev;
+  int64_t seq_stride;  /* elements */
+  int64_t head_stride; /* elements */
+  int32_t width;       /* positions a row */
+} lacache_weights;
+
+/* The attention weight that every cached token got from the last new_tokens tokens of its sequence, added to its weight from
+ * before. For a kv head, position j and the queries r that see it (all q heads of its group, all new tokens, the mask of
+ * lacache_kv_attend with the same arguments),
+ *     out_j = decay * past_j + sum_r exp(scale * <q_r, k_j> - lse_r)
+ * with lse as that call wrote it; a query with lse = -inf has seen nothing and adds nothing. The new tokens' own positions
+ * start from 0, whatever past holds there, as everything does if past.data_dev is NULL. Positions from lengths_dev[s] on are
+ * not written. out may be past (the same address and strides), or must not overlap it; past.width is at least out.width. A length past
+ * out.width is reported as an index outside its range (and cut). What a masked position holds never reaches another's weight.
+ * decay is finite; the rest is as for lacache_kv_attend. Asynchronous on cuda_stream; may be captured into a CUDA graph. */
+typedef struct {
+  int32_t new_tokens;
+  int32_t q_heads;
+  int32_t window;
+  int32_t dtype;
+  float scale;
+  float decay;
+  const int32_t* lengths_dev;
+  const int32_t* starts_dev;
+  lacache_rows q;
+  const float* lse_dev; /* [seqs * new_tokens x q_heads] */
+  lacache_weights past;
+  lacache_weights out;
+} lacache_weighing;
+lacache_status lacache_kv_weigh(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table, const lacache_weighing* w,
+                                void* cuda_stream);
+
+/* Eviction by weight: of every sequence and kv head, the tokens that have gathered the most attention are copied, in order, to
+ * the pages of another table. Of the positions starts_dev[s] (NULL: 0) <= j < lengths_dev[s], the last `recent` are kept, and
+ * of the others those of the largest weight, `keep` in all (all of them, if there are no more); of equal weights the earlier
+ * positions, a NaN counting as the least of all. The i-th kept token of head h goes to position i of sequence s in *to, its K, V
+ * and scales as they are. Heads keep different tokens; all have new_lengths_dev[s] = min(keep, positions) of them.
+ *   kept_dev          [seqs x kv_heads x keep] int32: the kept tokens' positions, ascending, then -1
+ *   new_lengths_dev   [seqs] int32
+ *   new_weights       their weights (positions from new_lengths_dev[s] on are not written; data_dev may be NULL)
+ * The tokens carry the rotary positions that they were written with: pass append's rope_pos for those that follow. *to names
+ * as many sequences and holds keep tokens at least; its pages are none that the sequences of *table use, in this layer (or the
+ * result is undefined). Slots behind a sequence's last are left as they were. A length past weights->width, and table entries
+ * outside their range, are reported by lacache_kv_sync (a length is cut, a token without a page is not copied). 1 <= keep,
+ * 0 <= recent <= keep; new_weights->width is at least keep. Asynchronous on cuda_stream; may be captured into a CUDA graph. */
+lacache_status lacache_kv_evict(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table, const int32_t* lengths_dev,
+                                const int32_t* starts_dev, const lacache_weights* weights, int32_t keep, int32_t recent,
+                                const lacache_kv_table* to, int32_t* kept_dev, int32_t* new_lengths_dev,
+                                const lacache_weights* new_weights, void* cuda_stream);
+
 /* Synchronize the handle's device and report what its kernels found since the previous call: LACACHE_ERR_INVALID_ARG for
  * an index outside its range (see lacache_kv_table), or LACACHE_ERR_DEVICE_TIMEOUT if an attention gave up waiting within
  * the GPU (that call's outputs are then undefined; later calls are not affected). */

@@ -1,5 +1,5 @@
-"""Oracle of the decoding operators (test infrastructure only): rotary positions, the cache's 8-bit rows and the attention of
-new tokens over cached ones, in fp64 numpy from their definitions.
+"""Oracle of the decoding operators (test infrastructure only): rotary positions, the attention of new tokens over cached ones,
+the weights that cached tokens gather and eviction by them, in fp64 numpy from their definitions.
 """
 from __future__ import annotations
 
@@ -58,3 +58,50 @@ def attend(q, k, v, lengths, new_tokens: int, scale: float, starts=None, window:
                 lse[r, h] = score.max() + math.log(w.sum())
                 span[r, h] = (np.abs(kk) @ np.abs(q[r, h])).max() * abs(scale)
     return out, lse, mass, span
+
+
+def weigh(q, k, lengths, new_tokens: int, scale: float, lse, past=None, decay: float = 1.0, starts=None, window: int = 0):
+    """q [seqs * T x heads x d], lse [seqs * T x heads]; k and past: per sequence [tokens x kv_heads x d] and [kv_heads x tokens].
+    Returns per sequence the weights [kv_heads x tokens], and the same sums with each query's share times
+    its largest sum of |q k| * scale, and times |lse|, for error bounds."""
+    got = []
+    for s, length in enumerate(lengths):
+        kv_heads, heads = k[s].shape[1], q.shape[1]
+        w, by_span, by_lse = (np.zeros((kv_heads, length)) for _ in range(3))
+        if past is not None:
+            w[:, :max(0, length - new_tokens)] = decay * np.asarray(past[s], np.float64)[:, :max(0, length - new_tokens)]
+        for t in range(new_tokens):
+            p = length - new_tokens + t
+            lo = max(0, 0 if starts is None else int(starts[s]), p - window + 1 if window else 0)
+            if p < lo:
+                continue
+            r = s * new_tokens + t
+            for h in range(heads):
+                if lse[r, h] == -np.inf:
+                    continue
+                g = h // (heads // kv_heads)
+                kk = k[s][lo:p + 1, g]
+                share = np.exp(kk @ q[r, h] * scale - lse[r, h])
+                w[g, lo:p + 1] += share
+                by_span[g, lo:p + 1] += share * (np.abs(kk) @ np.abs(q[r, h])).max() * abs(scale)
+                by_lse[g, lo:p + 1] += share * abs(lse[r, h])
+        got.append((w, by_span, by_lse))
+    return got
+
+
+def evict(weights, lengths, keep: int, recent: int, starts=None):
+    """weights: per sequence [kv_heads x tokens]. Per sequence and head the kept positions, ascending."""
+    kept = []
+    for s, length in enumerate(lengths):
+        start = min(length, max(0, 0 if starts is None else int(starts[s])))
+        rows = []
+        for w in np.asarray(weights[s], np.float64):
+            held = list(range(start, length))
+            if len(held) <= keep:
+                rows.append(held)
+                continue
+            last = held[len(held) - recent:]
+            rest = sorted(held[:len(held) - recent], key=lambda j: (np.isnan(w[j]), 0.0 if np.isnan(w[j]) else -w[j], j))
+            rows.append(sorted(rest[:keep - recent] + last))
+        kept.append(rows)
+    return kept

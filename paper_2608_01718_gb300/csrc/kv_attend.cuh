@@ -125,6 +125,9 @@ inline bool takes_tc(int rows, int group, int head_dim, bool eight) {   // (grou
   return head_dim <= 128 && group <= 2048 && rows > (eight && head_dim <= 64 ? 32 : 16);
 }
 cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
+lacache_status attend_args(lacache_kv_t* h, int layer, const lacache_kv_table* table, int new_tokens, int q_heads, int window,
+                           int dtype, float scale, const int32_t* lengths, const int32_t* starts, const lacache_rows* q,
+                           AttendArgs* out);
 
 namespace {
 

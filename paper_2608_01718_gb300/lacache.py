@@ -36,7 +36,7 @@ EXPORTS = ["lacache_create", "lacache_create_ensemble", "lacache_destroy", "laca
            "lacache_calibrate_workspace_bytes", "lacache_verify_draft", "lacache_verify_sample", "lacache_lookup_noalloc",
            "lacache_merge_shards", "lacache_get_stats", "lacache_save", "lacache_load", "lacache_get_config",
            "lacache_rope_init", "lacache_rope_apply", "lacache_kv_create", "lacache_kv_destroy", "lacache_kv_get_pool",
-           "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_sync", "lacache_kv_inject_stall",
+           "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_weigh", "lacache_kv_evict", "lacache_kv_sync", "lacache_kv_inject_stall",
            "lacache_status_string"]
 
 
@@ -105,6 +105,18 @@ class lacache_attention(ctypes.Structure):
                 ("lse_dev", ctypes.c_void_p)]
 
 
+class lacache_weights(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("width", ctypes.c_int32)]
+
+
+class lacache_weighing(ctypes.Structure):
+    _fields_ = [("new_tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("decay", ctypes.c_float),
+                ("lengths_dev", ctypes.c_void_p), ("starts_dev", ctypes.c_void_p), ("q", lacache_rows),
+                ("lse_dev", ctypes.c_void_p), ("past", lacache_weights), ("out", lacache_weights)]
+
+
 class LacacheError(RuntimeError):
     def __init__(self, call: str, status: int):
         super().__init__(f"{call}: {status_string(status)} ({status})")
@@ -166,6 +178,8 @@ def load() -> ctypes.CDLL:
         "lacache_kv_append": ([vp, i32, vp, i64, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp], i32),
         "lacache_kv_read": ([vp, i32, vp, i64, vp, vp, i32, vp, vp, vp], i32),
         "lacache_kv_attend": ([vp, i32, vp, vp, vp], i32),
+        "lacache_kv_weigh": ([vp, i32, vp, vp, vp], i32),
+        "lacache_kv_evict": ([vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp], i32),
         "lacache_kv_sync": ([vp], i32),
         "lacache_kv_inject_stall": ([vp, i32], i32),
         "lacache_status_string": ([i32], ctypes.c_char_p),
@@ -499,6 +513,20 @@ def lacache_kv_attend(h: int, layer: int, table: lacache_kv_table, attention: la
                                                          _stream(cuda_stream)))
 
 
+def lacache_kv_weigh(h: int, layer: int, table: lacache_kv_table, weighing: lacache_weighing, cuda_stream=None) -> None:
+    """Attention weights of the cached tokens, added to those from before."""
+    _check("lacache_kv_weigh", load().lacache_kv_weigh(h, layer, _address(table), _address(weighing), _stream(cuda_stream)))
+
+
+def lacache_kv_evict(h: int, layer: int, table: lacache_kv_table, lengths, starts, weights: lacache_weights, keep: int,
+                     recent: int, to: lacache_kv_table, kept, new_lengths, new_weights: lacache_weights | None,
+                     cuda_stream=None) -> None:
+    """The tokens of the largest weights, copied in order to the pages of another table."""
+    _check("lacache_kv_evict", load().lacache_kv_evict(
+        h, layer, _address(table), _ptr(lengths), _ptr(starts), _address(weights), keep, recent, _address(to), _ptr(kept),
+        _ptr(new_lengths), _address(new_weights), _stream(cuda_stream)))
+
+
 def lacache_kv_sync(h: int) -> None:
     _check("lacache_kv_sync", load().lacache_kv_sync(h))
 
@@ -793,6 +821,11 @@ class KVCache:
             out["ks"], out["vs"] = view(p.k_scale, rows, "<f4"), view(p.v_scale, rows, "<f4")
         return out
 
+    def _window(self, window: int) -> int:
+        if window < 0:
+            raise ValueError(f"window is a number of positions, or 0 for none, not {window}")
+        return window if window < 1 << 31 else 0   # no position lies further back
+
     def _table(self, table) -> lacache_kv_table:
         if table.dim() != 2 or table.dtype != _INT32 or table.stride(1) != 1 or table.get_device() != self.device:
             raise ValueError(f"a table is an int32 [sequences x pages] tensor on cuda:{self.device} with dense rows")
@@ -848,11 +881,7 @@ class KVCache:
             import torch
             if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
                 raise ValueError(f"lse is a dense fp32 [{n} x {heads}] tensor on cuda:{dev}")
-        if not 0 <= window < 1 << 31:
-            if window < 0:
-                raise ValueError(f"window is a number of positions, or 0 for none, not {window}")
-            window = 0   # no position lies further back
-        a = lacache_attention(new_tokens, heads, window, _dtype(q), D ** -0.5 if scale is None else scale,
+        a = lacache_attention(new_tokens, heads, self._window(window), _dtype(q), D ** -0.5 if scale is None else scale,
                               _index("lengths", lengths, t.seqs, dev),
                               None if starts is None else _index("starts", starts, t.seqs, dev),
                               _rows("q", q, n, heads, D, dev, dtype), _rows("out", out, n, heads, D, dev, dtype),
@@ -860,6 +889,69 @@ class KVCache:
         _check("lacache_kv_attend", self._lib.lacache_kv_attend(
             self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a), _current_stream(cuda_stream, dev)))
         return out
+
+    def _weights(self, name: str, t, seqs: int, least: int = 1) -> lacache_weights:
+        import torch
+        if (t.dim() != 3 or t.shape[:2] != (seqs, self.cfg.kv_heads) or t.dtype != torch.float32 or t.shape[2] < least or
+                (t.stride(2) != 1 and t.shape[2] > 1) or t.get_device() != self.device):
+            raise ValueError(f"{name} is a [{seqs} x {self.cfg.kv_heads} x positions] fp32 tensor of {least} positions or more, "
+                             f"its rows dense, on cuda:{self.device}")
+        return lacache_weights(t.data_ptr(), t.stride(0), t.stride(1), min(t.shape[2], (1 << 31) - 1))
+
+    def weigh(self, q, table, lengths, lse, weights=None, decay: float = 1.0, out=None, new_tokens: int = 1, layer: int = 0,
+              starts=None, window: int = 0, scale: float | None = None, cuda_stream=None):
+        """The attention weight that every cached token got from the last ``new_tokens`` tokens of its sequence (``q`` and the
+        masks as for attend, ``lse`` from it), by kv head, plus ``decay`` times its weight from before: ``out``
+        [sequences x kv_heads x positions] fp32. The new tokens' own positions start from 0. ``out`` is ``weights`` itself if
+        None, or, without weights, a new tensor of zeros as wide as the table."""
+        heads, D, dev = _three("q", q)[1], self.cfg.head_dim, self.device
+        t = self._table(table)
+        n = t.seqs * new_tokens
+        if out is None:
+            out = weights
+        if out is None:
+            import torch
+            with _results_on(cuda_stream, dev):
+                out = torch.zeros(t.seqs, self.cfg.kv_heads, t.width * self.cfg.page_size, device=f"cuda:{dev}")
+        to = self._weights("out", out, t.seqs)
+        past = lacache_weights() if weights is None else self._weights("weights", weights, t.seqs, out.shape[2])
+        if lse.dtype != out.dtype or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
+            raise ValueError(f"lse is a dense fp32 [{n} x {heads}] tensor on cuda:{dev}")
+        w = lacache_weighing(new_tokens, heads, self._window(window), _dtype(q), D ** -0.5 if scale is None else scale, decay,
+                             _index("lengths", lengths, t.seqs, dev),
+                             None if starts is None else _index("starts", starts, t.seqs, dev),
+                             _rows("q", q, n, heads, D, dev, q.dtype), lse.data_ptr(), past, to)
+        _check("lacache_kv_weigh", self._lib.lacache_kv_weigh(
+            self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(w), _current_stream(cuda_stream, dev)))
+        return out
+
+    def evict(self, table, lengths, weights, keep: int, to, recent: int = 0, layer: int = 0, starts=None, kept=None,
+              new_lengths=None, new_weights=None, cuda_stream=None):
+        """Of every sequence and kv head, the last ``recent`` tokens and those of the largest ``weights``, ``keep`` in all, copied in
+        order to the pages of the table ``to`` (which the sequences of ``table`` do not use). Returns ``new_lengths`` (int32
+        [sequences]), ``kept`` (int32 [sequences x kv_heads x keep]: their positions, then -1) and ``new_weights``
+        [sequences x kv_heads x keep]. The tokens keep the rotary positions that they were written with."""
+        import torch
+        t, target, H, dev = self._table(table), self._table(to), self.cfg.kv_heads, self.device
+        if not 1 <= keep < 1 << 31 or not 0 <= recent <= keep:
+            raise ValueError(f"keep is 1 or more and recent 0 to keep, not {keep} and {recent}")
+        with _results_on(cuda_stream, dev):
+            kw = {"device": f"cuda:{dev}"}
+            if kept is None:
+                kept = torch.empty(t.seqs, H, keep, dtype=torch.int32, **kw)
+            if new_lengths is None:
+                new_lengths = torch.empty(t.seqs, dtype=torch.int32, **kw)
+            if new_weights is None:
+                new_weights = torch.zeros(t.seqs, H, keep, **kw)
+        if kept.dtype != _INT32 or kept.shape != (t.seqs, H, keep) or not kept.is_contiguous() or kept.get_device() != dev:
+            raise ValueError(f"kept is a dense int32 [{t.seqs} x {H} x {keep}] tensor on cuda:{dev}")
+        w, nw = self._weights("weights", weights, t.seqs), self._weights("new_weights", new_weights, t.seqs, keep)
+        _check("lacache_kv_evict", self._lib.lacache_kv_evict(
+            self.h, self._layer(layer), ctypes.addressof(t), _index("lengths", lengths, t.seqs, dev),
+            None if starts is None else _index("starts", starts, t.seqs, dev), ctypes.addressof(w), keep, recent,
+            ctypes.addressof(target), kept.data_ptr(), _index("new_lengths", new_lengths, t.seqs, dev), ctypes.addressof(nw),
+            _current_stream(cuda_stream, dev)))
+        return new_lengths, kept, new_weights
 
     def sync(self) -> None:
         lacache_kv_sync(self.h)
