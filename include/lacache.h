@@ -551,6 +551,27 @@ typedef struct {
 lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table,
                                  const lacache_attention* a, void* cuda_stream);
 
+/* The same attention for sequences that have their first positions in common (a system prompt, a document), which are then read
+ * once for all. Sequences bounds_dev[g] .. bounds_dev[g + 1] - 1 are group g (bounds rise within [0, seqs]; NULL: one group of
+ * all sequences; a sequence may be in none), and the first lengths_dev[g] positions of all of them hold the same tokens: the
+ * pages are read from the first of them, whatever the others' rows of the table name there. Lengths, starts, windows and the
+ * outputs are as for lacache_kv_attend, and mean whole sequences, the common positions counted in; a sequence may end within
+ * them. The result is that of lacache_kv_attend but for roundings. Bounds that do not rise, and lengths past the table, are reported
+ * by lacache_kv_sync (without groups, and with the lengths cut).
+ * The workspace is device memory, 16-byte aligned, of lacache_kv_attend_shared_workspace_bytes(h, seqs, groups, new_tokens,
+ * q_heads) (0 for arguments outside their ranges); calls that may overlap, those of two captured graphs among them, have one each.
+ * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read bounds, lengths and tables anew. */
+typedef struct {
+  int32_t groups;            /* at least 1 */
+  const int32_t* bounds_dev; /* [groups + 1] */
+  const int32_t* lengths_dev;/* [groups] */
+} lacache_shared;
+size_t lacache_kv_attend_shared_workspace_bytes(const lacache_kv_t* h, int32_t seqs, int32_t groups, int32_t new_tokens,
+                                                int32_t q_heads);
+lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table,
+                                        const lacache_attention* a, const lacache_shared* shared, void* workspace_dev,
+                                        size_t workspace_bytes, void* cuda_stream);
+
 /* Attention weights of cached tokens: a device array of [seqs x kv_heads x width] fp32 with any sequence and head strides; a
  * row's elements, one a position, are dense. */
 typedef struct {

@@ -86,7 +86,17 @@ struct AttendArgs {
   float* partial;       // two slots a block: [rows of a tile x DP] sums, then (m, l) a row
   unsigned int* arrived;   // blocks that have left their part of the triple that begins in this block; zero between launches
   unsigned int* status;
+  // a call over groups of sequences that have their first positions in common (kv_shared.cu), in two passes
+  int groups;
+  const int4* spans;      // of each group: the first common position that is seen, one past the last, first sequence, sequences
+  const int32_t* joined;  // whether a sequence has a common part
+  float* common;          // that part's outputs, [tokens x q_heads x head_dim] ...
+  float* common_lse;      // ... and base-2 lse
 };
+
+// The kernels' forms: attention of its own; over what groups of sequences have in common, where a group takes a sequence's place
+// and has the rows of all of its sequences; and over what each sequence has of its own, joined with the other.
+constexpr int kWhole = 0, kCommon = 1, kOwn = 2;
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
@@ -125,6 +135,17 @@ inline bool takes_tc(int rows, int group, int head_dim, bool eight) {   // (grou
   return head_dim <= 128 && group <= 2048 && rows > (eight && head_dim <= 64 ? 32 : 16);
 }
 cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
+// The two kernels' passes over sequences that have their first positions in common (kv_shared*.cu).
+cudaError_t launch_common_bf16(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_common_f16(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_common_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_common_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_common_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
+cudaError_t launch_own_bf16(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_own_f16(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_own_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_own_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_own_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
 lacache_status attend_args(lacache_kv_t* h, int layer, const lacache_kv_table* table, int new_tokens, int q_heads, int window,
                            int dtype, float scale, const int32_t* lengths, const int32_t* starts, const lacache_rows* q,
                            AttendArgs* out);
@@ -203,11 +224,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 // Four 8 x 8 tiles of 16-bit values from shared memory, transposed: lane l names the 16-byte row l % 8 of tile l / 8.
 __device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t& a0, uint32_t& a1, uint32_t& a2, uint32_t& a3) {
@@ -243,9 +259,30 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 // see at most, [lo, hi), and its units.
 struct Span {
   int len, lo, hi, units;
+  int first, rows, tiles;   // kCommon: the group's first sequence, its rows a kv head, their tiles
 };
-__device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_keys) {
+template <int FORM = kWhole>
+__device__ __forceinline__ int seqs_of(const AttendArgs& a) { return FORM == kCommon ? a.groups : a.table.seqs; }
+template <int FORM>
+__device__ __forceinline__ int rows_of(const AttendArgs& a, const Span& s) { return FORM == kCommon ? s.rows : a.rows; }
+template <int FORM>
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, const Span& s) { return FORM == kCommon ? s.tiles : a.row_tiles; }
+template <int FORM>   // the row of the table, and of which sequence the rows' first token is
+__device__ __forceinline__ int first_of(int seq, const Span& s) { return FORM == kCommon ? s.first : seq; }
+template <int FORM = kWhole>
+__device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_keys, int tile_rows = 0) {
   Span s;
+  if constexpr (FORM == kCommon) {
+    const int4 x = a.spans[seq];
+    s.lo = x.x;
+    s.len = s.hi = x.y;
+    s.first = x.z;
+    s.rows = x.w * a.rows;
+    s.tiles = s.rows ? (s.rows + tile_rows - 1) / tile_rows : 1;
+    const int common = s.hi - (s.lo & ~15);
+    s.units = common <= 0 ? 1 : (common + unit_keys - 1) / unit_keys;
+    return s;
+  }
   int len = a.lengths[seq];
   len = len < 0 ? 0 : len > a.max_len ? a.max_len : len;
   const int first = len - a.new_tokens;   // the first row's position
@@ -255,22 +292,75 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_k
   s.len = len;
   s.lo = lo;
   s.hi = len;
-  const int keys = len - (lo & ~15);
+  if (FORM == kOwn && lo >= len) s.lo = s.hi = len & ~15;   // nothing of its own: no page is looked up
+  const int keys = s.hi - (s.lo & ~15);
   s.units = keys <= 0 ? 1 : (keys + unit_keys - 1) / unit_keys;   // an empty sequence has rows to write
   return s;
 }
 
-// Where row `row` of a kv head goes: bytes into out, and its index in lse.
-__device__ __forceinline__ int64_t out_at(const AttendArgs& a, int seq, int head, int row, int64_t* lse) {
+// The last and the first position that token tok of a triple sees.
+template <int FORM>
+__device__ __forceinline__ int2 seen_by(const AttendArgs& a, int seq, const Span& sp, int tok) {
+  int of = seq, pos;
+  if constexpr (FORM == kCommon) {
+    const int i = tok / a.new_tokens;
+    of = sp.first + i;
+    const int len = a.lengths[of];
+    pos = (len < 0 ? 0 : len > a.max_len ? a.max_len : len) - a.new_tokens + (tok - i * a.new_tokens);
+  } else {
+    pos = sp.len - a.new_tokens + tok;
+  }
+  int lo = a.starts ? a.starts[of] : 0;
+  if (a.window > 0 && pos - a.window + 1 > lo) lo = pos - a.window + 1;
+  if (FORM == kCommon && pos > sp.hi - 1) pos = sp.hi - 1;
+  return make_int2(pos, lo);
+}
+
+// Where row `row` of a kv head goes: bytes into out, and its index in lse. (kCommon: into the common part's outputs.)
+template <int FORM = kWhole>
+__device__ __forceinline__ int64_t out_at(const AttendArgs& a, int first, int head, int row, int64_t* lse) {
   const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
-  const int64_t token = (int64_t)seq * a.new_tokens + tok;
+  const int64_t token = (int64_t)first * a.new_tokens + tok;
   *lse = token * a.q_heads + qh;
+  if (FORM == kCommon) return *lse * a.head_dim * 4;
   return a.out.at(token, qh) - a.out.p;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// A row's end: its sums' factor, kOwn's weight of the common part's output, and its lse (written). `joined`: it has a common part.
+struct End {
+  float f, common;
+};
+template <int FORM>
+__device__ __forceinline__ End end_of(const AttendArgs& a, float top, float sum, int64_t lse, bool joined, bool write = true) {
+  End x = {sum == 0.f ? 0.f : 1.f / sum, 0.f};
+  if constexpr (FORM == kCommon) {
+    if (write) a.common_lse[lse] = sum == 0.f ? -INFINITY : top + log2f(sum);
+  } else {
+    float l = sum == 0.f ? -INFINITY : top + log2f(sum);
+    if (FORM == kOwn && joined) {
+      const float other = a.common_lse[lse], most = fmaxf(l, other);
+      if (most > -INFINITY || l != l || other != other) {
+        const float mine = exp2_fast(l - most), its = exp2_fast(other - most), both = mine + its;
+        x.common = its / both;
+        // (not 0 where anything was seen: a value that is not finite shows however little it counts)
+        if (sum != 0.f) x.f = fmaxf(x.f * (mine / both), 0x1p-126f);
+        if (mine != mine || both != both) x.f = NAN;
+        l = most + log2f(both);
+      }
+    }
+    if (write && a.lse) a.lse[lse] = l * 0.6931471805599453f;
+  }
+  return x;
 }
 // Four values of an output row. Sums are kept in the order of the accumulators: quad 4 d + p holds tile d's two values of
 // lane group g = 2p and its two of g + 1. f is 1 / the row's sum of weights, 0 if nothing was seen.
-template <typename C>
-__device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, int quad, float4 acc, float f) {
+template <typename C, int FORM = kWhole>
+__device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, int quad, float4 acc, float f, float of_common = 0.f,
+                                           int64_t lse = 0, bool joined = false) {
   const float4 y = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
   const int d = quad >> 2, g = (quad & 3) * 2;
   int at[2];        // the first dimensions of two pairs
@@ -287,6 +377,22 @@ __device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, 
     pair[0] = make_float2(y.x, y.z);
     pair[1] = make_float2(y.y, y.w);
   }
+  if constexpr (FORM == kCommon) {
+    float* out = a.common + at_row / 4;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (at[i] < a.head_dim) *reinterpret_cast<float2*>(out + at[i]) = pair[i];
+    return;
+  }
+  if (FORM == kOwn && joined) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (at[i] >= a.head_dim) continue;
+      const float2 c = *reinterpret_cast<const float2*>(a.common + lse * a.head_dim + at[i]);
+      pair[i].x += of_common * c.x;
+      pair[i].y += of_common * c.y;
+    }
+  }
   unsigned char* out = a.out.p + at_row;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -299,7 +405,7 @@ __device__ __forceinline__ float lse_of(float top, float sum) {
   return sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
-template <int FMT, int DP, int NT>
+template <int FMT, int DP, int NT, int FORM = kWhole>
 __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) attend_kernel(const __grid_constant__ AttendArgs a) {
   using C = AttendConfig<FMT, DP, NT>;
   constexpr bool kBf16 = FMT == LACACHE_KV_BF16;
@@ -310,22 +416,33 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   __shared__ float row_factor[C::kRows];                // scale log2(e), and what the row's q was divided by
   __shared__ int64_t row_out[C::kRows];                 // where a row goes, and 1 / its sum of weights
   __shared__ float row_inv[C::kRows];
+  __shared__ float row_common[FORM == kOwn ? C::kRows : 1];   // kOwn: the common part's weight, and the row's index in lse
+  __shared__ int64_t row_lse[FORM == kOwn ? C::kRows : 1];
   __shared__ int page_ids[kAttendWarps][C::kStages][C::kSub];
-  __shared__ int pending[2][4];   // shared triples: sequence, triple, first and last block (-1: none)
+  __shared__ int pending[2][6];   // shared triples: sequence, triple, first and last block (-1: none), rows and tiles (kCommon)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int D = a.head_dim, row_bytes = D * C::kItem;
-  const int per_seq = a.kv_heads * a.row_tiles;   // triples of a sequence
+  const int per_whole = a.kv_heads * a.row_tiles;
+  auto triples_of = [&](const Span& s) { return FORM == kCommon ? a.kv_heads * s.tiles : per_whole; };   // of a sequence
+  const int seqs = seqs_of<FORM>(a);
+  auto span = [&](int s) { return span_of<FORM>(a, s, C::kUnit, C::kRows); };
 
   // ---- this block's part of the line of cells (each warp for itself) ----
   // a triple's cells: kTripleCost for its q and its join, which hold no keys, then its units
   constexpr int kTripleCost = C::kTripleCost;
-  auto cells_of = [&](int s) { return s < a.table.seqs ? span_of(a, s, C::kUnit).units + kTripleCost : 0; };
+  // (a sequence's: of one of its triples, or, where their number differs, of all)
+  auto cells_of = [&](int s) {
+    if (s >= seqs) return 0;
+    const Span x = span(s);
+    return (x.units + kTripleCost) * (FORM == kCommon ? triples_of(x) : 1);
+  };
+  const int per_seq = FORM == kCommon ? 1 : per_whole;
   int held[4], total = 0;   // the first 128 sequences', their loads all at once
 #pragma unroll
   for (int i = 0; i < 4; ++i) held[i] = cells_of(32 * i + lane);
 #pragma unroll
   for (int i = 0; i < 4; ++i) total += held[i];
-  for (int s = lane + 128; s < a.table.seqs; s += 32) total += cells_of(s);
+  for (int s = lane + 128; s < seqs; s += 32) total += cells_of(s);
   total = __reduce_add_sync(0xffffffffu, total) * per_seq;
   const int parts = total < a.parts ? total : a.parts, block = blockIdx.x;
   if (block >= parts) return;
@@ -337,7 +454,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   };
   int seq = 0, seq_base = 0;   // the sequence that cell u belongs to, and the cells before it
 #pragma unroll 1
-  for (int s0 = 0; s0 < a.table.seqs; s0 += 32) {
+  for (int s0 = 0; s0 < seqs; s0 += 32) {
     const int mine = s0 == 0 ? held[0] : s0 == 32 ? held[1] : s0 == 64 ? held[2] : s0 == 96 ? held[3] : cells_of(s0 + lane);
     const int own = mine * per_seq;
     int upto = own;
@@ -357,7 +474,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   }
   if (threadIdx.x < 2) pending[threadIdx.x][2] = -1;   // (the first triple's q, and a barrier, come before its use)
   constexpr int kQuads = DP / 4;
-  Span sp = span_of(a, seq, C::kUnit);
+  Span sp = span(seq);
   int triple = (u - seq_base) / (sp.units + kTripleCost);
   int first_unit = u - seq_base - triple * (sp.units + kTripleCost) - kTripleCost;
   int left = share + (block < longer ? 1 : 0);   // cells of this block that are not done
@@ -391,9 +508,9 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
     }
   };
   auto enter_triple = [&] {
-    const int head = ahead.triple / a.row_tiles;
+    const int head = ahead.triple / tiles_of<FORM>(a, ahead.sp);
     ahead.key = (ahead.sp.lo & ~15) + ahead.unit * C::kUnit + warp * C::kKeys;
-    ahead.table_row = a.table.pages + ahead.seq * a.table.stride;
+    ahead.table_row = a.table.pages + first_of<FORM>(ahead.seq, ahead.sp) * a.table.stride;
     const int64_t rows = (int64_t)head * a.page_size;
     ahead.k = a.pk + rows * row_bytes;
     ahead.v = a.pv + rows * row_bytes;
@@ -471,10 +588,10 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       }
       if (++ahead.unit == ahead.sp.units && (ahead.left -= kTripleCost) > 0) {
         ahead.unit = 0;
-        if (++ahead.triple == per_seq) {
+        if (++ahead.triple == triples_of(ahead.sp)) {
           ahead.triple = 0;
-          ahead.seq = ahead.seq + 1 < a.table.seqs ? ahead.seq + 1 : ahead.seq;
-          ahead.sp = span_of(a, ahead.seq, C::kUnit);
+          ahead.seq = ahead.seq + 1 < seqs ? ahead.seq + 1 : ahead.seq;
+          ahead.sp = span(ahead.seq);
         }
         enter_triple();
       }
@@ -483,10 +600,10 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   };
 
   // a row of q (row r of the tile that starts at row0), eight elements a lane; zeros past the live rows and dimensions
-  auto load_q = [&](int of_seq, int of_head, int of_row0, int r) {
+  auto load_q = [&](int of_seq, int of_head, int of_row0, int r) {   // (of_seq: the sequence of the rows' first token)
     const int row = of_row0 + r, tok = row / a.group;
     uint4 x = make_uint4(0, 0, 0, 0);
-    if (row < a.rows && lane * 8 < D)
+    if (row < rows_of<FORM>(a, sp) && lane * 8 < D)
       x = *reinterpret_cast<const uint4*>(
           a.q.at((int64_t)of_seq * a.new_tokens + tok, of_head * a.group + row - tok * a.group) + lane * 16);
     return x;
@@ -495,8 +612,9 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   // in shared memory, once every warp is done with the last
   constexpr bool kQEarly = NT <= 2;
   uint4 q_raw[kQEarly ? C::kRows / kAttendWarps : 1];
-  auto load_q_early = [&](int of_seq, int of_triple) {
-    const int of_head = of_triple / a.row_tiles, of_row0 = (of_triple - of_head * a.row_tiles) * C::kRows;
+  auto load_q_early = [&](int seq_now, int of_triple) {   // (sp is that sequence's)
+    const int of_seq = first_of<FORM>(seq_now, sp), tiles = tiles_of<FORM>(a, sp);
+    const int of_head = of_triple / tiles, of_row0 = (of_triple - of_head * tiles) * C::kRows;
     if constexpr (kQEarly) {
 #pragma unroll
       for (int k = 0; k < C::kRows / kAttendWarps; ++k)
@@ -505,7 +623,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
 #pragma unroll
       for (int k = 0; k < C::kRows / kAttendWarps; ++k) {
         const int r = warp + k * kAttendWarps, row = of_row0 + r, tok = row / a.group;
-        const bool in = row < a.rows && lane * 8 < D;
+        const bool in = row < rows_of<FORM>(a, sp) && lane * 8 < D;
         if (lane * 8 < DP)
           copy_async<16>(shared_addr(q_smem + r * C::kQStride + lane * 16),
                          in ? a.q.at((int64_t)of_seq * a.new_tokens + tok, of_head * a.group + row - tok * a.group) + lane * 16
@@ -521,10 +639,10 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   bool careful = false;              // the triple's products are done again, V's values that are not finite apart
   int slot = 0;                      // of the unit whose products are next
   while (left > 0) {
-    const int head = triple / a.row_tiles, tile = triple % a.row_tiles;
+    const int head = triple / tiles_of<FORM>(a, sp), tile = triple % tiles_of<FORM>(a, sp);
     const int units = sp.units - first_unit < left ? sp.units - first_unit : (int)left;
     const int row0 = tile * C::kRows;
-    const int live_rows = a.rows - row0 < C::kRows ? a.rows - row0 : C::kRows;
+    const int all_rows = rows_of<FORM>(a, sp), live_rows = all_rows - row0 < C::kRows ? all_rows - row0 : C::kRows;
     if (fresh) {
       if (!careful) load_q_early(seq, triple);   // before the copies, which would keep it waiting
       copy_wait<0>();
@@ -556,7 +674,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       if (i == 0 && !careful) {
         // ---- q into shared memory, in the order of the K pieces ----
         if constexpr (!kQEarly) copy_wait<1>();   // all but the newest copies: q's lie before them
-        if (threadIdx.x == 0) {
+        if (FORM != kCommon && threadIdx.x == 0) {
           const int raw = a.lengths[seq];
           if (raw < 0 || raw > a.max_len) atomicOr(a.status, kBadIndex);
         }
@@ -589,18 +707,31 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           }
           if (d0 < DP) *reinterpret_cast<uint4*>(q_smem + r * C::kQStride + d0 * 2) = raw;
           if (lane == 0) {
-            const int p = live ? sp.len - a.new_tokens + tok : -1;
-            int lo = a.starts ? a.starts[seq] : 0;
-            if (a.window > 0 && p - a.window + 1 > lo) lo = p - a.window + 1;
-            row_pos[r] = p;
-            row_lo[r] = lo;
+            if constexpr (FORM == kCommon) {
+              const int2 seen = live ? seen_by<FORM>(a, seq, sp, tok) : make_int2(-1, 0);
+              row_pos[r] = seen.x;
+              row_lo[r] = seen.y;
+            } else {
+              const int p = live ? sp.len - a.new_tokens + tok : -1;
+              int lo = a.starts ? a.starts[seq] : 0;
+              if (a.window > 0 && p - a.window + 1 > lo) lo = p - a.window + 1;
+              row_pos[r] = p;
+              row_lo[r] = lo;
+            }
             row_factor[r] = a.scale * 1.4426950408889634f * back;
           }
         }
         __syncthreads();
 
-        all_hi = row_pos[0];
-        all_lo = row_lo[live_rows - 1];
+        if constexpr (FORM == kCommon) {   // rows of several sequences: in no order
+          all_hi = lane < live_rows ? row_pos[lane] : INT_MAX;
+          all_lo = lane < live_rows ? row_lo[lane] : INT_MIN;
+          all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+          all_lo = __reduce_max_sync(0xffffffffu, all_lo);
+        } else {
+          all_hi = row_pos[0];
+          all_lo = row_lo[live_rows - 1];
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           factor[n][0] = row_factor[n * 8 + 2 * t];
@@ -1004,16 +1135,18 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       careful = false;
     }
 
-    const int of_seq = seq, of_triple = triple, of_units = sp.units, of_base = seq_base;
+    const int of_seq = first_of<FORM>(seq, sp), of_triple = triple, of_units = sp.units, of_base = seq_base;
+    const int of_rows = rows_of<FORM>(a, sp), of_tiles = tiles_of<FORM>(a, sp);
+    const bool joined = FORM == kOwn && a.joined[seq];
     left -= units;
     if (first_unit + units == of_units) left -= kTripleCost;
     first_unit = 0;
     if (left > 0) {
-      if (++triple == per_seq) {
+      if (++triple == triples_of(sp)) {
         triple = 0;
-        seq_base += (sp.units + kTripleCost) * per_seq;
-        seq = seq + 1 < a.table.seqs ? seq + 1 : seq;
-        sp = span_of(a, seq, C::kUnit);
+        seq_base += (sp.units + kTripleCost) * triples_of(sp);
+        seq = seq + 1 < seqs ? seq + 1 : seq;
+        sp = span(seq);
       }
       if constexpr (kQEarly) load_q_early(seq, triple);
     }
@@ -1046,6 +1179,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       if (threadIdx.x == 0) {
         int* p = pending[block == c_first];
         p[0] = of_seq, p[1] = of_triple, p[2] = c_first, p[3] = c_last;
+        if (FORM == kCommon) p[4] = of_rows, p[5] = of_tiles;
       }
     }
     float* mine_out = a.partial + (block * 2 + (block == c_first ? 1 : 0)) * partial_floats(DP);
@@ -1058,9 +1192,18 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       for (int w = 0; w < kAttendWarps; ++w) sum += exp2_fast(stat_m[w][r] - base) * stat_l[w][r];
       if (whole) {
         int64_t at_lse;
-        row_out[r] = out_at(a, of_seq, head, row0 + r, &at_lse);
-        row_inv[r] = sum == 0.f ? 0.f : 1.f / sum;
-        if (a.lse) a.lse[at_lse] = lse_of(top, sum);
+        row_out[r] = out_at<FORM>(a, of_seq, head, row0 + r, &at_lse);
+        if constexpr (FORM == kWhole) {
+          row_inv[r] = sum == 0.f ? 0.f : 1.f / sum;
+          if (a.lse) a.lse[at_lse] = lse_of(top, sum);
+        } else {
+          const End end = end_of<FORM>(a, top, sum, at_lse, joined);
+          row_inv[r] = end.f;
+          if constexpr (FORM == kOwn) {
+            row_common[r] = end.common;
+            row_lse[r] = at_lse;
+          }
+        }
       } else {
         *reinterpret_cast<float2*>(mine_out + C::kRows * DP + r * 2) = make_float2(top, sum);
       }
@@ -1098,7 +1241,10 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           const float4 x = *reinterpret_cast<const float4*>(join + (w * C::kRows + r) * C::kOStride + q * 4);
           acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
         }
-        if (whole) write_quad<C>(a, row_out[r], quad, acc, row_inv[r]);
+        if (whole) {
+          if constexpr (FORM == kOwn) write_quad<C, FORM>(a, row_out[r], quad, acc, row_inv[r], row_common[r], row_lse[r], joined);
+          else write_quad<C, FORM>(a, row_out[r], quad, acc, row_inv[r]);
+        }
         else *reinterpret_cast<float4*>(mine_out + r * DP + quad * 4) = acc;
       }
       if (c < 3) __syncthreads();
@@ -1128,13 +1274,16 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   };
   auto shared_rows = [&](int k) {
     if (pending[k][2] < 0) return 0;
-    const int left_rows = a.rows - pending[k][1] % a.row_tiles * C::kRows;
+    const int tiles = FORM == kCommon ? pending[k][5] : a.row_tiles;
+    const int left_rows = (FORM == kCommon ? pending[k][4] : a.rows) - pending[k][1] % tiles * C::kRows;
     return left_rows < C::kRows ? left_rows : C::kRows;
   };
   const int rows0 = shared_rows(0), rows1 = shared_rows(1);
   __shared__ float joint_top[2 * C::kRows];
   __shared__ int64_t joint_out[2 * C::kRows];
   __shared__ float joint_inv[2 * C::kRows];
+  __shared__ float joint_common[FORM == kOwn ? 2 * C::kRows : 1];
+  __shared__ int64_t joint_lse[FORM == kOwn ? 2 * C::kRows : 1];
   // the rows' common maxima and sums: eight lanes a row, eight loads in flight a lane
   for (int x0 = 0; x0 < rows0 + rows1; x0 += kAttendThreads / 8) {
     const int x = x0 + (threadIdx.x >> 3), sub = threadIdx.x & 7;
@@ -1162,16 +1311,32 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
 #pragma unroll
     for (int o = 4; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (live && sub == 0) {
-      const int head = pending[k][1] / a.row_tiles, row0 = (pending[k][1] - head * a.row_tiles) * C::kRows;
+      const int tiles = FORM == kCommon ? pending[k][5] : a.row_tiles;
+      const int head = pending[k][1] / tiles, row0 = (pending[k][1] - head * tiles) * C::kRows;
       int64_t at_lse;
-      joint_out[x] = out_at(a, pending[k][0], head, row0 + r, &at_lse);
+      joint_out[x] = out_at<FORM>(a, pending[k][0], head, row0 + r, &at_lse);
       joint_top[x] = all == -INFINITY ? 0.f : all;
-      joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
-      if (a.lse) a.lse[at_lse] = lse_of(all, sum);
+      if constexpr (FORM == kWhole) {
+        joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
+        if (a.lse) a.lse[at_lse] = lse_of(all, sum);
+      } else {
+        const End end = end_of<FORM>(a, all, sum, at_lse, FORM == kOwn && a.joined[pending[k][0]]);
+        joint_inv[x] = end.f;
+        if constexpr (FORM == kOwn) {
+          joint_common[x] = end.common;
+          joint_lse[x] = at_lse;
+        }
+      }
     }
   }
   __syncthreads();
   // sixteen loads in flight a thread: those of four values from up to four blocks, or of one value from sixteen
+  auto write_joint = [&](int x, int quad, float4 acc) {
+    if constexpr (FORM == kOwn)
+      write_quad<C, FORM>(a, joint_out[x], quad, acc, joint_inv[x], joint_common[x], joint_lse[x],
+                          a.joined[pending[x < rows0 ? 0 : 1][0]]);
+    else write_quad<C, FORM>(a, joint_out[x], quad, acc, joint_inv[x]);
+  };
   const int values = (rows0 + rows1) * kQuads;
   const int most = max(rows0 ? pending[0][3] - pending[0][2] : 0, rows1 ? pending[1][3] - pending[1][2] : 0) + 1;
   if (most <= 4) {
@@ -1203,7 +1368,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             const float f = exp2_fast(w[v][e] - joint_top[x]);
             acc.x += f * y[v][e].x, acc.y += f * y[v][e].y, acc.z += f * y[v][e].z, acc.w += f * y[v][e].w;
           }
-          write_quad<C>(a, joint_out[x], j % kQuads, acc, joint_inv[x]);
+          write_joint(x, j % kQuads, acc);
         }
       }
     }
@@ -1232,16 +1397,16 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
         }
       }
     }
-    write_quad<C>(a, joint_out[x], quad, acc, joint_inv[x]);
+    write_joint(x, quad, acc);
   }
 }
 
-template <int FMT, int DP, int NT>
+template <int FMT, int DP, int NT, int FORM = kWhole>
 cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
   using C = AttendConfig<FMT, DP, NT>;
   static_assert(C::kSmem <= 227 * 1024, "shared memory");
 
-  auto* kernel = attend_kernel<FMT, DP, NT>;
+  auto* kernel = attend_kernel<FMT, DP, NT, FORM>;
   static std::atomic<int> resident[kMaxDevices];   // blocks an SM holds, by device; 0: not asked yet
   int per_sm = a.device < kMaxDevices ? resident[a.device].load(std::memory_order_relaxed) : 0;
   if (per_sm == 0) {
@@ -1254,28 +1419,30 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
   a.row_tiles = (a.rows + C::kRows - 1) / C::kRows;
   // the most units the table allows, so that small calls launch few blocks
   const int64_t units = ((int64_t)a.max_len + 15) / C::kUnit + 1 + C::kTripleCost;
-  const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units;
+  const double tiles = FORM == kCommon ? (double)a.table.seqs * a.rows / C::kRows + a.groups : (double)a.table.seqs * a.row_tiles;
+  const double most = tiles * a.kv_heads * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // units are counted in 32 bits
   a.parts = most < (double)per_sm * num_sms ? (int)most : per_sm * num_sms;
   kernel<<<a.parts, kAttendThreads, C::kSmem, st>>>(a);
   return cudaGetLastError();
 }
 
-template <int FMT>
+template <int FMT, int FORM = kWhole>
 cudaError_t launch_format(const AttendArgs& a, int num_sms, cudaStream_t st) {
   // tiles of 32 rows where takes_tc leaves so many to this kernel
   constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
-  const int dp = padded_dim(a.head_dim), nt = a.rows <= 8 ? 1 : a.rows <= 16 || dp > 64 || !kEight ? 2 : 4;
+  const int64_t rows = FORM == kCommon ? (int64_t)a.rows * a.table.seqs / a.groups : a.rows;   // (of a group, on average)
+  const int dp = padded_dim(a.head_dim), nt = rows <= 8 ? 1 : rows <= 16 || dp > 64 || !kEight ? 2 : 4;
   if constexpr (kEight) {
-    if (nt == 4) return launch_one<FMT, 64, 4>(a, num_sms, st);
+    if (nt == 4) return launch_one<FMT, 64, 4, FORM>(a, num_sms, st);
   }
   switch (dp * 8 + nt) {
-    case 64 * 8 + 1: return launch_one<FMT, 64, 1>(a, num_sms, st);
-    case 64 * 8 + 2: return launch_one<FMT, 64, 2>(a, num_sms, st);
-    case 128 * 8 + 1: return launch_one<FMT, 128, 1>(a, num_sms, st);
-    case 128 * 8 + 2: return launch_one<FMT, 128, 2>(a, num_sms, st);
-    case 256 * 8 + 1: return launch_one<FMT, 256, 1>(a, num_sms, st);
-    default: return launch_one<FMT, 256, 2>(a, num_sms, st);
+    case 64 * 8 + 1: return launch_one<FMT, 64, 1, FORM>(a, num_sms, st);
+    case 64 * 8 + 2: return launch_one<FMT, 64, 2, FORM>(a, num_sms, st);
+    case 128 * 8 + 1: return launch_one<FMT, 128, 1, FORM>(a, num_sms, st);
+    case 128 * 8 + 2: return launch_one<FMT, 128, 2, FORM>(a, num_sms, st);
+    case 256 * 8 + 1: return launch_one<FMT, 256, 1, FORM>(a, num_sms, st);
+    default: return launch_one<FMT, 256, 2, FORM>(a, num_sms, st);
   }
 }
 

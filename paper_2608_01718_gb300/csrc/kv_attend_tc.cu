@@ -70,7 +70,7 @@ struct Tc {
     uint32_t tmem;
     uint32_t abort_flag;
     uint32_t bad[16];                          // a unit's 16-key tiles whose page id is no page (by unit modulo 16)
-    int pending[2][4];                         // shared triples, as in kv_attend.cuh
+    int pending[2][6];                         // shared triples, as in kv_attend.cuh
     // 8-bit caches: a unit's scales of K, then of V (by unit modulo 8)
     alignas(16) float scales[kEight ? 8 * 2 * kTile : 4];   // read four at a time
   };
@@ -129,10 +129,12 @@ __device__ __forceinline__ void warp_arrive(uint64_t& bar) {
 }
 
 // This block's part of the line of cells: triples in order, each with its first unit and how many units are the block's.
+template <int FORM>
 struct Walk {
   int seq, seq_base, triple, first_unit, left;   // left: cells, this triple's units first
-  int per_seq;
+  int per_whole;
   Span sp;
+  __device__ __forceinline__ int per_seq(const AttendArgs& a) const { return FORM == kCommon ? a.kv_heads * sp.tiles : per_whole; }
   __device__ __forceinline__ int units() const { return min(sp.units - first_unit, left); }
   __device__ __forceinline__ bool done() const { return left <= 0; }
   __device__ __forceinline__ void next(const AttendArgs& a) {
@@ -140,11 +142,11 @@ struct Walk {
     left -= n;
     if (first_unit + n == sp.units) left -= kCost;
     first_unit = 0;
-    if (left > 0 && ++triple == per_seq) {
+    if (left > 0 && ++triple == per_seq(a)) {
       triple = 0;
-      seq_base += (sp.units + kCost) * per_seq;
-      seq = min(seq + 1, a.table.seqs - 1);
-      sp = span_of(a, seq, kTile);
+      seq_base += (sp.units + kCost) * per_seq(a);
+      seq = min(seq + 1, seqs_of<FORM>(a) - 1);
+      sp = span_of<FORM>(a, seq, kTile, kTile);
     }
   }
 };
@@ -156,20 +158,26 @@ struct Line {
   }
 };
 // By a whole warp. false: this block has no part.
-__device__ bool start_walk(const AttendArgs& a, Walk& w, Line& line) {
-  const int lane = threadIdx.x & 31, block = blockIdx.x;
-  w.per_seq = a.kv_heads * a.row_tiles;
+template <int FORM>
+__device__ bool start_walk(const AttendArgs& a, Walk<FORM>& w, Line& line) {
+  const int lane = threadIdx.x & 31, block = blockIdx.x, seqs = seqs_of<FORM>(a);
+  w.per_whole = a.kv_heads * a.row_tiles;
+  auto cells_of = [&](int s) {   // of one of the sequence's triples, or, where their number differs, of all
+    const Span x = span_of<FORM>(a, s, kTile, kTile);
+    return (x.units + kCost) * (FORM == kCommon ? a.kv_heads * x.tiles : 1);
+  };
+  const int times = FORM == kCommon ? 1 : w.per_whole;
   int total = 0;
-  for (int s = lane; s < a.table.seqs; s += 32) total += span_of(a, s, kTile).units + kCost;
-  total = __reduce_add_sync(0xffffffffu, total) * w.per_seq;
+  for (int s = lane; s < seqs; s += 32) total += cells_of(s);
+  total = __reduce_add_sync(0xffffffffu, total) * times;
   const int parts = min(total, a.parts);
   if (block >= parts) return false;
   line.share = total / parts;
   line.longer = total - line.share * parts;
   const int u = block * line.share + min(block, line.longer);
   w.seq = w.seq_base = 0;
-  for (int s0 = 0; s0 < a.table.seqs; s0 += 32) {
-    const int own = s0 + lane < a.table.seqs ? (span_of(a, s0 + lane, kTile).units + kCost) * w.per_seq : 0;
+  for (int s0 = 0; s0 < seqs; s0 += 32) {
+    const int own = s0 + lane < seqs ? cells_of(s0 + lane) * times : 0;
     int upto = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -185,7 +193,7 @@ __device__ bool start_walk(const AttendArgs& a, Walk& w, Line& line) {
     }
     w.seq_base += __shfl_sync(0xffffffffu, upto, 31);
   }
-  w.sp = span_of(a, w.seq, kTile);
+  w.sp = span_of<FORM>(a, w.seq, kTile, kTile);
   w.triple = (u - w.seq_base) / (w.sp.units + kCost);
   w.first_unit = u - w.seq_base - w.triple * (w.sp.units + kCost) - kCost;
   w.left = line.share + (block < line.longer ? 1 : 0);
@@ -196,15 +204,38 @@ __device__ bool start_walk(const AttendArgs& a, Walk& w, Line& line) {
   return true;
 }
 
+// The common part's output, in a row of kOwn.
+struct Other {
+  float weight;
+  int64_t lse;
+  bool joined;
+};
+__device__ __forceinline__ void add_common(const AttendArgs& a, const Other& o, int d, float4& y) {
+  const float4 c = *reinterpret_cast<const float4*>(a.common + o.lse * a.head_dim + d);
+  y.x += o.weight * c.x, y.y += o.weight * c.y, y.z += o.weight * c.z, y.w += o.weight * c.w;
+}
 // Four neighbouring dimensions of an output row.
-__device__ __forceinline__ void write4(const AttendArgs& a, int64_t at_row, int d, float4 y) {
+template <int FORM>
+__device__ __forceinline__ void write4(const AttendArgs& a, int64_t at_row, int d, float4 y, const Other& o) {
+  if constexpr (FORM == kCommon) {
+    *reinterpret_cast<float4*>(a.common + at_row / 4 + d) = y;
+    return;
+  }
+  if (FORM == kOwn && o.joined) add_common(a, o, d, y);
   *reinterpret_cast<uint2*>(a.out.p + at_row + d * 2) =
       a.q_f16 ? make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w)) : make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
 }
 
 // Eight, times g (0: zeros, whatever they are).
-__device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int d, float4 x, float4 y, float g) {
+template <int FORM>
+__device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int d, float4 x, float4 y, float g, const Other& o) {
   if (g == 0.f) x = y = make_float4(0.f, 0.f, 0.f, 0.f);
+  if constexpr (FORM != kWhole) {
+    x = make_float4(x.x * g, x.y * g, x.z * g, x.w * g), y = make_float4(y.x * g, y.y * g, y.z * g, y.w * g);
+    write4<FORM>(a, at_row, d, x, o);
+    write4<FORM>(a, at_row, d + 4, y, o);
+    return;
+  }
   const float v[8] = {x.x * g, x.y * g, x.z * g, x.w * g, y.x * g, y.y * g, y.z * g, y.w * g};
   *reinterpret_cast<uint4*>(a.out.p + at_row + d * 2) = a.q_f16 ? pack8(v, __half()) : pack8(v, __nv_bfloat16());
 }
@@ -212,7 +243,7 @@ __device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int 
 // One row of one block's keys [from, to), by a warp, four keys at a time: lane i holds dimensions 4 i .. 4 i + 3. It may take
 // longer than a wait's bound, so it tells the waits that it goes on.
 template <int FMT, bool QF16>
-__device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, int tok, int qh, int from, int to,
+__device__ __noinline__ void slow_row(const AttendArgs& a, int first, int head, int tok, int qh, int from, int to,
                                       volatile long long* progress, float4* acc, float* top, float* sum) {
   using T = Tc<FMT, QF16>;
   const int lane = threadIdx.x & 31, D = a.head_dim;
@@ -236,14 +267,14 @@ __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, in
     }
   };
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-  const unsigned char* q_row = a.q.at((int64_t)seq * a.new_tokens + tok, qh);
+  const unsigned char* q_row = a.q.at((int64_t)first * a.new_tokens + tok, qh);
   const float4 q = has ? four(*reinterpret_cast<const uint2*>(q_row + lane * 8), QF16) : zero;
   float m = -INFINITY, l = 0.f;
   float4 o = zero;
   for (int j = from & ~3; j < to; j += 4) {
     if (lane == 0) *progress = clock64();
     const int index = (int)(((uint64_t)(uint32_t)(j >> 4) * a.page_mul) >> a.page_shift);
-    const int page = a.table.pages[seq * a.table.stride + index];
+    const int page = a.table.pages[first * a.table.stride + index];
     if ((unsigned)page >= (unsigned)a.pages) continue;
     const int64_t row = page * a.page_rows + (int64_t)head * a.page_size + (j - index * a.page_size);
     float4 k[4], v[4];
@@ -281,7 +312,7 @@ __device__ __noinline__ void slow_row(const AttendArgs& a, int seq, int head, in
   *sum = l;
 }
 
-template <int FMT, bool QF16>
+template <int FMT, bool QF16, int FORM = kWhole>
 __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a) {
   using T = Tc<FMT, QF16>;
   using Tail = typename T::Tail;
@@ -302,7 +333,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   const int row_bytes = T::kEight ? D : D * 2;                    // of the cache
   const int slot_floats = kTile * (a.padded + 2);   // of a.partial
 
-  auto by_group = [&](int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_mul); };   // row / group
+  auto by_group = [&](int row) {   // row / group (a group of sequences may have rows past the multiplication's range)
+    return FORM == kCommon ? row / a.group : a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_mul);
+  };
+  auto tiles_of = [&](const Walk<FORM>& w) { return FORM == kCommon ? w.sp.tiles : a.row_tiles; };
+  auto live_of = [&](const Walk<FORM>& w, int row0) {
+    return FORM == kCommon ? min(w.sp.rows - row0, kTile) : min(a.rows - row0, a.tile_rows);
+  };
+  const int tile_rows = FORM == kCommon ? kTile : a.tile_rows;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders / 32 : kLoaders + 1);
@@ -320,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     t.pending[0][2] = t.pending[1][2] = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  Walk walk;
+  Walk<FORM> walk;
   Line line;
   if (!start_walk(a, walk, line)) return;
   if (warp == kMmaWarp) {
@@ -392,8 +430,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         warp_arrive(t.full[k % kSlots]);
       };
       for (; ok && !walk.done(); walk.next(a)) {
-        const int head = walk.triple / a.row_tiles, count = walk.units();
-        const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
+        const int head = walk.triple / tiles_of(walk), count = walk.units();
+        const int32_t* table_row = a.table.pages + first_of<FORM>(walk.seq, walk.sp) * a.table.stride;
         const int64_t head_row = (int64_t)head * a.page_size;
         int key = (walk.sp.lo & ~15) + walk.first_unit * kTile;
         auto look_up = [&](int from) {
@@ -457,8 +495,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < 4; ++i) place[i] = unit_at((wide ? 2 : 4) * i + own_row, own_unit);
     for (; ok && !walk.done(); walk.next(a)) {
-      const int head = walk.triple / a.row_tiles, count = walk.units();
-      const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
+      const int head = walk.triple / tiles_of(walk), count = walk.units();
+      const int32_t* table_row = a.table.pages + first_of<FORM>(walk.seq, walk.sp) * a.table.stride;
       const unsigned char* head_k = a.pk + (int64_t)head * a.page_size * row_bytes;
       const unsigned char* head_v = a.pv + (int64_t)head * a.page_size * row_bytes;
       int key = (walk.sp.lo & ~15) + walk.first_unit * kTile;
@@ -594,12 +632,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     bool ok = true;
     // a triple's q: this thread's 64 dimensions of its row, into registers, and from there to TMEM
     uint32_t q_row[32];
-    auto load_q = [&](const Walk& w) {
-      const int head = w.triple / a.row_tiles, row0 = (w.triple - head * a.row_tiles) * a.tile_rows;
-      const int live = min(a.rows - row0, a.tile_rows);
+    auto load_q = [&](const Walk<FORM>& w) {
+      const int head = w.triple / tiles_of(w), row0 = (w.triple - head * tiles_of(w)) * tile_rows;
+      const int live = live_of(w, row0);
       const int r = threadIdx.x & (kTile - 1), row = row0 + r, tok = by_group(row);
       const uint4* from = reinterpret_cast<const uint4*>(
-          r < live ? a.q.at((int64_t)w.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) : nullptr);
+          r < live ? a.q.at((int64_t)first_of<FORM>(w.seq, w.sp) * a.new_tokens + tok, head * a.group + row - tok * a.group)
+                   : nullptr);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int u = half * 8 + i;
@@ -616,20 +655,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     load_q(walk);
     hand_over_q();
     for (; ok && !walk.done(); walk.next(a)) {
-      const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
-      const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
+      const int head = walk.triple / tiles_of(walk), row0 = (walk.triple - head * tiles_of(walk)) * tile_rows;
+      const int live = live_of(walk, row0), count = walk.units(), first = first_of<FORM>(walk.seq, walk.sp);
       const int r = threadIdx.x & (kTile - 1), tok = by_group(row0 + r);
       const bool mine = r < live, some = (warp & 3) * 32 < live;
-      const int pos = mine ? walk.sp.len - a.new_tokens + tok : INT_MAX;
-      int lo = INT_MIN;
-      if (mine) {
-        lo = a.starts ? a.starts[walk.seq] : 0;
-        if (a.window > 0 && pos - a.window + 1 > lo) lo = pos - a.window + 1;
+      int pos, lo = INT_MIN;
+      if constexpr (FORM == kCommon) {
+        pos = INT_MAX;
+        if (mine) {
+          const int2 seen = seen_by<FORM>(a, walk.seq, walk.sp, tok);
+          pos = seen.x, lo = seen.y;
+        }
+      } else {
+        pos = mine ? walk.sp.len - a.new_tokens + tok : INT_MAX;
+        if (mine) {
+          lo = a.starts ? a.starts[walk.seq] : 0;
+          if (a.window > 0 && pos - a.window + 1 > lo) lo = pos - a.window + 1;
+        }
       }
       const float factor = a.scale * 1.4426950408889634f;
       float m = -INFINITY, l = 0.f;
       const int key_begin = (walk.sp.lo & ~15) + walk.first_unit * kTile;
-      if (threadIdx.x == 0) {
+      if (FORM != kCommon && threadIdx.x == 0) {
         const int raw_len = a.lengths[walk.seq];
         if (raw_len < 0 || raw_len > a.max_len) atomicOr(a.status, kBadIndex);
       }
@@ -767,7 +814,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       if (!ok) break;
       // with the last S of a triple complete, every product with its q is done: the next one's takes its place, while the
       // last product with V runs
-      Walk next = walk;
+      Walk<FORM> next = walk;
       next.next(a);
       const bool more = !next.done();
       if (more) load_q(next);
@@ -795,14 +842,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         c_last = line.block_of(begin + walk.sp.units - 1);
         if (threadIdx.x == 0) {
           int* p = t.pending[(int)blockIdx.x == c_first];
-          p[0] = walk.seq, p[1] = walk.triple, p[2] = c_first, p[3] = c_last;
+          p[0] = first, p[1] = walk.triple, p[2] = c_first, p[3] = c_last;
+          if (FORM == kCommon) p[4] = walk.sp.rows, p[5] = walk.sp.tiles;
         }
       }
       float* slot = a.partial + ((int64_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * slot_floats;
       if (some) {
         int64_t at_lse = 0, at_row = 0;
-        if (mine) at_row = out_at(a, walk.seq, head, row0 + r, &at_lse);
-        const float inv = total == 0.f ? 0.f : 1.f / total;
+        if (mine) at_row = out_at<FORM>(a, first, head, row0 + r, &at_lse);
+        float inv = total == 0.f ? 0.f : 1.f / total;
+        Other other = {0.f, at_lse, FORM == kOwn && a.joined[walk.seq]};
+        if (FORM == kOwn && whole && mine) {   // (lse is written below)
+          const End end = end_of<FORM>(a, m, total, at_lse, other.joined, false);
+          inv = end.f;
+          other.weight = end.common;
+        }
         // this half's dimensions: 32 of every 64 (rolled: code that runs once a triple waits for its fetch)
         float2 zero = make_float2(0.f, 0.f);   // NaN after a product that is not finite, or past kFar
 #pragma unroll 1
@@ -822,7 +876,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
                 const float4 y0 = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 const float4 y1 = make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);
                 if (whole) {
-                  write8(a, at_row, d, y0, y1, inv);
+                  write8<FORM>(a, at_row, d, y0, y1, inv, other);
                 } else {
                   reinterpret_cast<float4*>(slot)[d / 4 * kTile + r] = y0;
                   reinterpret_cast<float4*>(slot)[(d / 4 + 1) * kTile + r] = y1;
@@ -833,6 +887,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
         if (mine && half == 0) {
           if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, total);
+          else if (FORM != kWhole) end_of<FORM>(a, m, total, at_lse, other.joined);
           else if (a.lse) a.lse[at_lse] = lse_of(m, total);
         }
         // a row that is not finite in either half is done again, past what both have written; not where its sum of weights
@@ -854,21 +909,28 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           const int its_pos = __shfl_sync(0xffffffffu, pos, src), its_lo = __shfl_sync(0xffffffffu, lo, src);
           float4 acc;
           float top, sum;
-          slow_row<FMT, QF16>(a, walk.seq, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1),
+          slow_row<FMT, QF16>(a, first, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1),
                                progress, &acc, &top, &sum);
           int64_t its_lse;
-          const int64_t its_row = out_at(a, walk.seq, head, row0 + rr, &its_lse);
+          const int64_t its_row = out_at<FORM>(a, first, head, row0 + rr, &its_lse);
+          float g = sum == 0.f ? 0.f : 1.f / sum;
+          Other its = {0.f, its_lse, other.joined};
+          if (FORM == kOwn && whole) {
+            const End end = end_of<FORM>(a, top, sum, its_lse, its.joined, false);
+            g = end.f;
+            its.weight = end.common;
+          }
           if (lane * 4 < D) {
             if (whole) {
-              const float g = sum == 0.f ? 0.f : 1.f / sum;
-              write4(a, its_row, lane * 4, sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                                      : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g));
+              write4<FORM>(a, its_row, lane * 4, sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                            : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g), its);
             } else {
               reinterpret_cast<float4*>(slot)[lane * kTile + rr] = acc;
             }
           }
           if (lane == 0) {
             if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + rr * 2) = make_float2(top, sum);
+            else if (FORM != kWhole) end_of<FORM>(a, top, sum, its_lse, its.joined);
             else if (a.lse) a.lse[its_lse] = lse_of(top, sum);
           }
         }
@@ -917,10 +979,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   float* joint_top = reinterpret_cast<float*>(gbase);   // [2][kTile] each, in q's place
   float* joint_inv = joint_top + 2 * kTile;
   int64_t* joint_out = reinterpret_cast<int64_t*>(joint_inv + 2 * kTile);
+  int64_t* joint_lse = joint_out + 2 * kTile;   // kOwn: its index in lse, and the common part's weight
+  float* joint_common = reinterpret_cast<float*>(joint_lse + 2 * kTile);
   auto part = [&](int k, int i) { return a.partial + ((int64_t)(t.pending[k][2] + i) * 2 + (i == 0 ? 1 : 0)) * slot_floats; };
   auto part_ml = [&](int k, int i, int r) { return __ldcg(reinterpret_cast<const float2*>(part(k, i) + kTile * a.padded) + r); };
   auto rows_of = [&](int k) {
-    return t.pending[k][2] < 0 ? 0 : min(a.rows - t.pending[k][1] % a.row_tiles * a.tile_rows, a.tile_rows);
+    const int tiles = FORM == kCommon ? t.pending[k][5] : a.row_tiles, rows = FORM == kCommon ? t.pending[k][4] : a.rows;
+    return t.pending[k][2] < 0 ? 0 : min(rows - t.pending[k][1] % tiles * tile_rows, tile_rows);
   };
   const int rows0 = rows_of(0), rows1 = rows_of(1);
   for (int x = threadIdx.x; x < rows0 + rows1; x += kThreads) {
@@ -939,12 +1004,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       for (int e = 0; e < 8; ++e) sum += exp2_fast(y[e].x - to) * y[e].y;
       top = now;
     }
-    const int head = t.pending[k][1] / a.row_tiles, row0 = (t.pending[k][1] - head * a.row_tiles) * a.tile_rows;
+    const int tiles = FORM == kCommon ? t.pending[k][5] : a.row_tiles;
+    const int head = t.pending[k][1] / tiles, row0 = (t.pending[k][1] - head * tiles) * tile_rows;
     int64_t at_lse;
-    joint_out[x] = out_at(a, t.pending[k][0], head, row0 + r, &at_lse);
+    joint_out[x] = out_at<FORM>(a, t.pending[k][0], head, row0 + r, &at_lse);
     joint_top[x] = top == -INFINITY ? 0.f : top;
-    joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
-    if (a.lse) a.lse[at_lse] = lse_of(top, sum);
+    if constexpr (FORM == kWhole) {
+      joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
+      if (a.lse) a.lse[at_lse] = lse_of(top, sum);
+    } else {
+      const End end = end_of<FORM>(a, top, sum, at_lse, FORM == kOwn && a.joined[t.pending[k][0]]);
+      joint_inv[x] = end.f;
+      joint_common[x] = end.common;
+      joint_lse[x] = at_lse;
+    }
   }
   __syncthreads();
   // a thread joins 16 dimensions of a row at a time, from four blocks: sixteen loads in flight; neighbouring threads on
@@ -981,15 +1054,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
       }
 #pragma unroll
-      for (int v = 0; v < 4; v += 2) write8(a, joint_out[x0 + r], (q0 + v) * 4, acc[v], acc[v + 1], g);
+      for (int v = 0; v < 4; v += 2) {
+        Other other = {0.f, 0, false};
+        if constexpr (FORM == kOwn)
+          other = Other{joint_common[x0 + r], joint_lse[x0 + r], a.joined[t.pending[k][0]] != 0};
+        write8<FORM>(a, joint_out[x0 + r], (q0 + v) * 4, acc[v], acc[v + 1], g, other);
+      }
     }
   }
 }
 
-template <int FMT, bool QF16>
+template <int FMT, bool QF16, int FORM>
 cudaError_t launch_tc(AttendArgs a, int num_sms, cudaStream_t st) {
   constexpr int kSmem = Tc<FMT, QF16>::kSmem;
-  auto* kernel = attend_tc_kernel<FMT, QF16>;
+  auto* kernel = attend_tc_kernel<FMT, QF16, FORM>;
   static std::atomic<bool> ready[kMaxDevices];
   if (a.device >= kMaxDevices || !ready[a.device].load(std::memory_order_relaxed)) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
@@ -1001,24 +1079,35 @@ cudaError_t launch_tc(AttendArgs a, int num_sms, cudaStream_t st) {
   a.padded = padded_dim(a.head_dim);
   a.group_mul = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);   // exact for rows x group < 2^32
   const int64_t units = ((int64_t)a.max_len + 15) / kTile + 1 + kCost;
-  const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units;
+  const double tiles = FORM == kCommon ? (double)a.table.seqs * a.rows / kTile + a.groups : (double)a.table.seqs * a.row_tiles;
+  const double most = tiles * a.kv_heads * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // cells are counted in 32 bits
   a.parts = most < (double)num_sms ? (int)most : num_sms;
   kernel<<<a.parts, kThreads, kSmem, st>>>(a);
   return cudaGetLastError();
 }
 
+template <int FORM>
+cudaError_t launch_tc_form(const AttendArgs& a, int format, int num_sms, cudaStream_t st) {
+  switch (format) {
+    case LACACHE_KV_BF16: return launch_tc<LACACHE_KV_BF16, false, FORM>(a, num_sms, st);
+    case LACACHE_KV_F16: return launch_tc<LACACHE_KV_F16, true, FORM>(a, num_sms, st);
+    case LACACHE_KV_E4M3:
+      return a.q_f16 ? launch_tc<LACACHE_KV_E4M3, true, FORM>(a, num_sms, st) : launch_tc<LACACHE_KV_E4M3, false, FORM>(a, num_sms, st);
+    default:
+      return a.q_f16 ? launch_tc<LACACHE_KV_INT8, true, FORM>(a, num_sms, st) : launch_tc<LACACHE_KV_INT8, false, FORM>(a, num_sms, st);
+  }
+}
+
 }  // namespace
 
-cudaError_t launch_attend_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st) {
-  switch (format) {
-    case LACACHE_KV_BF16: return launch_tc<LACACHE_KV_BF16, false>(a, num_sms, st);
-    case LACACHE_KV_F16: return launch_tc<LACACHE_KV_F16, true>(a, num_sms, st);
-    case LACACHE_KV_E4M3:
-      return a.q_f16 ? launch_tc<LACACHE_KV_E4M3, true>(a, num_sms, st) : launch_tc<LACACHE_KV_E4M3, false>(a, num_sms, st);
-    default:
-      return a.q_f16 ? launch_tc<LACACHE_KV_INT8, true>(a, num_sms, st) : launch_tc<LACACHE_KV_INT8, false>(a, num_sms, st);
-  }
+// (kv_shared_tc_*.cu compile this file for the kernel's other forms)
+#ifndef LC_TC_FORM
+#define LC_TC_FORM kWhole
+#define LC_TC_LAUNCH launch_attend_tc
+#endif
+cudaError_t LC_TC_LAUNCH(const AttendArgs& a, int format, int num_sms, cudaStream_t st) {
+  return launch_tc_form<LC_TC_FORM>(a, format, num_sms, st);
 }
 
 }  // namespace lc

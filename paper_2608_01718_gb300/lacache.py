@@ -36,7 +36,8 @@ EXPORTS = ["lacache_create", "lacache_create_ensemble", "lacache_destroy", "laca
            "lacache_calibrate_workspace_bytes", "lacache_verify_draft", "lacache_verify_sample", "lacache_lookup_noalloc",
            "lacache_merge_shards", "lacache_get_stats", "lacache_save", "lacache_load", "lacache_get_config",
            "lacache_rope_init", "lacache_rope_apply", "lacache_kv_create", "lacache_kv_destroy", "lacache_kv_get_pool",
-           "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_weigh", "lacache_kv_evict", "lacache_kv_sync", "lacache_kv_inject_stall",
+           "lacache_kv_append", "lacache_kv_read", "lacache_kv_attend", "lacache_kv_attend_shared",
+           "lacache_kv_attend_shared_workspace_bytes", "lacache_kv_weigh", "lacache_kv_evict", "lacache_kv_sync", "lacache_kv_inject_stall",
            "lacache_status_string"]
 
 
@@ -103,6 +104,10 @@ class lacache_attention(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("lengths_dev", ctypes.c_void_p),
                 ("starts_dev", ctypes.c_void_p), ("q", lacache_rows), ("out", lacache_rows),
                 ("lse_dev", ctypes.c_void_p)]
+
+
+class lacache_shared(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int32), ("bounds_dev", ctypes.c_void_p), ("lengths_dev", ctypes.c_void_p)]
 
 
 class lacache_weights(ctypes.Structure):
@@ -178,6 +183,8 @@ def load() -> ctypes.CDLL:
         "lacache_kv_append": ([vp, i32, vp, i64, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp], i32),
         "lacache_kv_read": ([vp, i32, vp, i64, vp, vp, i32, vp, vp, vp], i32),
         "lacache_kv_attend": ([vp, i32, vp, vp, vp], i32),
+        "lacache_kv_attend_shared": ([vp, i32, vp, vp, vp, vp, ctypes.c_size_t, vp], i32),
+        "lacache_kv_attend_shared_workspace_bytes": ([vp, i32, i32, i32, i32], ctypes.c_size_t),
         "lacache_kv_weigh": ([vp, i32, vp, vp, vp], i32),
         "lacache_kv_evict": ([vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp], i32),
         "lacache_kv_sync": ([vp], i32),
@@ -511,6 +518,17 @@ def lacache_kv_attend(h: int, layer: int, table: lacache_kv_table, attention: la
     """Attention of the last new tokens of every sequence over its cached tokens."""
     _check("lacache_kv_attend", load().lacache_kv_attend(h, layer, _address(table), _address(attention),
                                                          _stream(cuda_stream)))
+
+
+def lacache_kv_attend_shared_workspace_bytes(h: int, seqs: int, groups: int, new_tokens: int, q_heads: int) -> int:
+    return int(load().lacache_kv_attend_shared_workspace_bytes(h, seqs, groups, new_tokens, q_heads))
+
+
+def lacache_kv_attend_shared(h: int, layer: int, table: lacache_kv_table, attention: lacache_attention, shared: lacache_shared,
+                             workspace, workspace_bytes: int, cuda_stream=None) -> None:
+    """Attention of new tokens where groups of sequences have their first positions in common."""
+    _check("lacache_kv_attend_shared", load().lacache_kv_attend_shared(
+        h, layer, _address(table), _address(attention), _address(shared), _ptr(workspace), workspace_bytes, _stream(cuda_stream)))
 
 
 def lacache_kv_weigh(h: int, layer: int, table: lacache_kv_table, weighing: lacache_weighing, cuda_stream=None) -> None:
@@ -872,6 +890,12 @@ class KVCache:
         """Attention of the last ``new_tokens`` tokens of each sequence: q [sequences * new_tokens x q_heads x head_dim],
         ``lengths`` (int32) with the new tokens counted. Returns ``out``; ``lse`` (fp32 [tokens x q_heads]) is filled if
         given. ``scale`` is 1 / sqrt(head_dim) if None. ``out`` does not overlap ``q``."""
+        t, a, out = self._attention(q, table, lengths, new_tokens, starts, window, scale, out, lse, cuda_stream)
+        _check("lacache_kv_attend", self._lib.lacache_kv_attend(
+            self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a), _current_stream(cuda_stream, self.device)))
+        return out
+
+    def _attention(self, q, table, lengths, new_tokens, starts, window, scale, out, lse, cuda_stream):
         heads, D, dev, dtype = _three("q", q)[1], self.cfg.head_dim, self.device, q.dtype
         t = self._table(table)
         n = t.seqs * new_tokens
@@ -881,13 +905,33 @@ class KVCache:
             import torch
             if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
                 raise ValueError(f"lse is a dense fp32 [{n} x {heads}] tensor on cuda:{dev}")
-        a = lacache_attention(new_tokens, heads, self._window(window), _dtype(q), D ** -0.5 if scale is None else scale,
-                              _index("lengths", lengths, t.seqs, dev),
-                              None if starts is None else _index("starts", starts, t.seqs, dev),
-                              _rows("q", q, n, heads, D, dev, dtype), _rows("out", out, n, heads, D, dev, dtype),
-                              None if lse is None else lse.data_ptr())
-        _check("lacache_kv_attend", self._lib.lacache_kv_attend(
-            self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a), _current_stream(cuda_stream, dev)))
+        return t, lacache_attention(new_tokens, heads, self._window(window), _dtype(q), D ** -0.5 if scale is None else scale,
+                                    _index("lengths", lengths, t.seqs, dev),
+                                    None if starts is None else _index("starts", starts, t.seqs, dev),
+                                    _rows("q", q, n, heads, D, dev, dtype), _rows("out", out, n, heads, D, dev, dtype),
+                                    None if lse is None else lse.data_ptr()), out
+
+    def attend_shared(self, q, table, lengths, shared, bounds=None, new_tokens: int = 1, layer: int = 0, starts=None,
+                      window: int = 0, scale: float | None = None, out=None, lse=None, cuda_stream=None):
+        """attend for sequences that have their first positions in common, which are read once for all: the first ``shared[g]``
+        positions (int32 [groups]) of the sequences ``bounds[g]`` to ``bounds[g + 1] - 1`` (int32 [groups + 1]; None: one group of
+        all), from the pages of the first of them. ``lengths`` count whole sequences. Everything else, and the result, as attend."""
+        import torch
+        dev = self.device
+        t, a, out = self._attention(q, table, lengths, new_tokens, starts, window, scale, out, lse, cuda_stream)
+        groups = shared.shape[0]
+        if groups < 1:
+            raise ValueError("shared has a length a group, one at least")
+        if bounds is None and groups != 1:
+            raise ValueError(f"{groups} groups have {groups + 1} bounds")
+        common = lacache_shared(groups, None if bounds is None else _index("bounds", bounds, groups + 1, dev),
+                                _index("shared", shared, groups, dev))
+        size = self._lib.lacache_kv_attend_shared_workspace_bytes(self.h, t.seqs, groups, new_tokens, a.q_heads)
+        with _results_on(cuda_stream, dev):
+            workspace = torch.empty(size, dtype=torch.uint8, device=f"cuda:{dev}")
+        _check("lacache_kv_attend_shared", self._lib.lacache_kv_attend_shared(
+            self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a), ctypes.addressof(common), workspace.data_ptr(),
+            size, _current_stream(cuda_stream, dev)))
         return out
 
     def _weights(self, name: str, t, seqs: int, least: int = 1) -> lacache_weights:
