@@ -27,7 +27,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["api.cu", "stage1_stream.cu", "stage1_tensor.cu", "stage2.cu", "noalloc.cu", "calibrate.cu", "lsh.cu",
            "lsh_tc.cu", "speculative.cu", "shards.cu", "rope.cu", "kv_cache.cu",
            "kv_attend.cu", "kv_attend_bf16.cu", "kv_attend_f16.cu", "kv_attend_e4m3.cu", "kv_attend_int8.cu",
-           "kv_attend_tc.cu", "kv_weigh.cu", "kv_evict.cu",
+           "kv_attend_tc.cu", "kv_weigh.cu", "kv_weigh_tc.cu", "kv_evict.cu",
            "kv_shared.cu", "kv_shared_bf16.cu", "kv_shared_f16.cu", "kv_shared_e4m3.cu", "kv_shared_int8.cu",
            "kv_shared_tc_common.cu", "kv_shared_tc_own.cu"]
 
@@ -62,7 +62,7 @@ def build(verbose: bool = False, force: bool = False) -> str:
 
 def _build_locked(verbose: bool, force: bool) -> str:
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    deps = srcs + [os.path.join(CSRC, h) for h in ("internal.cuh", "tcgen05.cuh", "decode.cuh", "kv_attend.cuh")]
+    deps = srcs + [os.path.join(CSRC, h) for h in ("internal.cuh", "tcgen05.cuh", "decode.cuh", "kv_attend.cuh", "kv_weigh.cuh")]
     deps += [os.path.join(INCLUDE, "lacache.h"), __file__]
     peaks_src = os.path.join(CSRC, PEAKS_SOURCE)
     lib_ok = os.path.exists(LIB) and os.path.getmtime(LIB) >= max(os.path.getmtime(p) for p in deps)

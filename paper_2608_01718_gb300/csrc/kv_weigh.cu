@@ -1,280 +1,331 @@
-// The attention weight that cached tokens get from new ones, added to what they got before:
-//
-//   w_j <- decay w_j + sum over the rows r that see j of e^(s_rj - lse_r),   s_rj = scale <q_r, k_j>
-//
-// for every kv head, over the rows that share it (its group of q heads times the new tokens), from the lse that the attention of
-// the same rows wrote. K is read once. Each key belongs to one warp, which adds its rows in order: no atomics, no joins.
+// The attention weight of cached tokens: the kernel for few rows a kv head, and the C entry.
 //
 // Products are the warp-level tensor instruction's, S^T [16 keys x 8 rows] = K Q^T, with the naming of a row's dimensions chosen
-// so that a lane's share of K is 16 contiguous bytes (as in kv_attend.cuh). K goes from memory straight into the registers that
-// the products read, 64 contiguous bytes of each row an instruction, and stays there for all rows, whose q is staged in shared
-// memory, kChunk rows at a time. 8-bit codes are widened to f16 exactly; q of bf16 over an 8-bit cache is scaled to f16 by a power of
-// two a row (exact for elements within 2^-14 of the row's largest). Scores, weights and sums are fp32.
+// so that a lane's share of K is 16 contiguous bytes, as in kv_attend.cuh. 8-bit codes are widened to f16 exactly; q of bf16 over
+// an 8-bit cache is scaled to f16 by a power of two a row (exact for elements within 2^-14 of the row's largest).
+//
+// Bound by reading K: every warp, for itself, has a ring of its own tiles of 16 or 32 keys in shared memory, filled by cp.async
+// whole lines at a time (with the keys' scales and past weights), and takes an equal part of the line of units (sequences, their
+// heads, their keys), whatever the lengths. q stays in registers; nothing is shared between warps.
 #include <algorithm>
 
-#include "kv_attend.cuh"
+#include "kv_weigh.cuh"
 
 namespace lc {
 namespace {
 
-struct WeighArgs {
-  AttendArgs a;   // (lse is read; out, the partial sums and the counters are not used)
-  float decay;
-  const float* past;
-  int64_t past_seq, past_head;
-  float* out;
-  int64_t out_seq, out_head;
-};
+constexpr int kFewRows = 16;   // a kv head
+constexpr int kWeighWarps = 4, kWeighThreads = kWeighWarps * 32;
 
-constexpr int kWeighWarps = 8, kWeighThreads = kWeighWarps * 32;
-constexpr int kChunk = 64;   // rows of q staged at a time
-
-template <int FMT, int DP>
+template <int FMT, int DP, int NT>
 struct WeighConfig {
-  static constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
-  static constexpr int kTiles = DP <= 128 ? 2 : 1;             // tiles of 16 keys a warp: 64 registers of operands
-  static constexpr int kKeys = 16 * kTiles;
-  static constexpr int kUnit = kWeighWarps * kKeys;
-  static constexpr int kPieces = DP * (kEight ? 1 : 2) / 64;   // of a lane, 16 bytes each, in a row of K
+  using C = AttendConfig<FMT, DP, NT>;
+  static constexpr bool kEight = C::kEight;
+  static constexpr int kSub = C::kSub, kKeys = C::kKeys, kTileBytes = C::kTileBytes, kRowBytes = C::kRowBytes;
+  static constexpr int kPieces = C::kKPieces;                         // 16-byte pieces of a lane in a row of K
   static constexpr int kSteps = DP / 16;
-  static constexpr int kQStride = DP * 2 + (kEight ? 16 : 64); // of a row of q: what eight lanes read lies in eight bank groups
+  static constexpr int kScales = kSub * kTileBytes;                   // offsets in a stage
+  static constexpr int kPast = kScales + (kEight ? kKeys * 4 : 0);
+  static constexpr int kStageBytes = kPast + kKeys * 4;
+  static constexpr int kStages = kSub * kTileBytes > 4096 ? 2 : kSub * kTileBytes > 2048 ? 4 : 7;
+  static constexpr int kRing = kStages * kStageBytes;                 // of a warp
+  static constexpr int kSmem = kWeighWarps * kRing;
+  static constexpr int kBlocks = NT == 4 ? 2 : 3;
 };
 
-__device__ __forceinline__ int weigh_length(const AttendArgs& a, int seq) {
-  const int len = a.lengths[seq];
-  return len < 0 ? 0 : len > a.max_len ? a.max_len : len;
-}
-
-template <int FMT, int DP>
-__global__ void __launch_bounds__(kWeighThreads, 2) weigh_kernel(const __grid_constant__ WeighArgs w) {
-  using C = WeighConfig<FMT, DP>;
+template <int FMT, int DP, int NT>
+__global__ void __launch_bounds__(kWeighThreads, WeighConfig<FMT, DP, NT>::kBlocks) weigh_kernel(const __grid_constant__ WeighArgs w) {
+  using W = WeighConfig<FMT, DP, NT>;
+  using C = typename W::C;
   constexpr bool kBf16 = FMT == LACACHE_KV_BF16;
+  extern __shared__ __align__(128) unsigned char smem[];
   const AttendArgs& a = w.a;
-  __shared__ __align__(16) unsigned char q_smem[kChunk * C::kQStride];
-  __shared__ __align__(8) float row_lse[kChunk], row_factor[kChunk];   // lse log2(e), and scale log2(e) times what q was divided by
-  __shared__ int row_pos[kChunk], row_lo[kChunk];                      // a row's last and first visible position
-  __shared__ int4 tile_span[kChunk / 8];                               // of eight rows: least and largest last, least and largest first
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int D = a.head_dim, row_bytes = D * (C::kEight ? 1 : 2);
+  const int D = a.head_dim, row_bytes = D * C::kItem;
 
-  // ---- this block's part of the line of units: sequences, their heads, their keys ----
-  int total = 0;
-  for (int s = lane; s < a.table.seqs; s += 32) total += (weigh_length(a, s) + C::kUnit - 1) / C::kUnit;
-  total = __reduce_add_sync(0xffffffffu, total) * a.kv_heads;
-  const int share = total / gridDim.x, longer = total - share * gridDim.x, block = blockIdx.x;
-  int left = share + (block < longer ? 1 : 0);
-  const int u = block * share + min(block, longer);
-  if (threadIdx.x == 0) {
-    for (int s = block; s < a.table.seqs; s += gridDim.x)
-      if (a.lengths[s] < 0 || a.lengths[s] > a.max_len) atomicOr(a.status, kBadIndex);
-  }
-  if (left == 0) return;
-  int seq = 0, seq_base = 0;
-  for (int s0 = 0; s0 < a.table.seqs; s0 += 32) {
-    const int own = s0 + lane < a.table.seqs ? (weigh_length(a, s0 + lane) + C::kUnit - 1) / C::kUnit * a.kv_heads : 0;
-    int upto = own;
+  weigh_check(a);
+  // where the products are, and where the copies are, kStages - 1 units ahead
+  WeighPlace<W::kKeys> at;
+  const int mine = weigh_start<W::kKeys>(a, blockIdx.x + warp * gridDim.x, gridDim.x * kWeighWarps, at);
+  if (mine == 0) return;
+  WeighPlace<W::kKeys> ahead = at;
+
+  unsigned char* ring = smem + warp * W::kRing;
+  const uint32_t ring_addr = shared_addr(ring);
+  auto page_of = [&](int k) { return (int)(((uint64_t)(uint32_t)(k >> 4) * a.page_mul) >> a.page_shift); };
+  int ids[W::kSub], next_ids[W::kSub], in_batch = 0;   // lane i: page ids of the batch's unit i, and of the next batch's
+  int ahead_left = mine, ahead_slot = 0, first_seen = 0;
+  const int32_t* table_row;
+  const unsigned char* head_k;
+  const float* past;
+  int64_t head_row;
+  uint32_t bad_slots = 0;   // bit slot * kSub + s: that tile has no page
+  auto look_up = [&](int from, int (&to)[W::kSub]) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
+    for (int s = 0; s < W::kSub; ++s) {
+      const int64_t k = (int64_t)from + lane * W::kKeys + 16 * s;
+      to[s] = k < ahead.len ? __ldg(table_row + page_of((int)k)) : -1;
     }
-    const unsigned past = __ballot_sync(0xffffffffu, seq_base + upto > u);
-    if (past) {
-      const int l0 = __ffs(past) - 1;
-      seq = s0 + l0;
-      seq_base += __shfl_sync(0xffffffffu, upto - own, l0);
-      break;
+  };
+  auto enter = [&] {
+    table_row = a.table.pages + ahead.seq * a.table.stride;
+    head_row = (int64_t)ahead.head * a.page_size;
+    head_k = a.pk + head_row * row_bytes;
+    past = w.past ? w.past + ahead.seq * w.past_seq + ahead.head * w.past_head : nullptr;
+    const Span sp = span_of(a, ahead.seq, W::kKeys);
+    first_seen = sp.lo;
+    in_batch = 0;
+    look_up(ahead.unit * W::kKeys, ids);
+  };
+  enter();
+  auto issue = [&] {
+    if (ahead_left > 0) {
+      const uint32_t to = ring_addr + ahead_slot * W::kStageBytes;
+      const int key = ahead.unit * W::kKeys;
+#pragma unroll
+      for (int s = 0; s < W::kSub; ++s) {
+        const int k0 = key + 16 * s;
+        const int page = __shfl_sync(0xffffffffu, ids[s], in_batch);
+        const bool there = (unsigned)page < (unsigned)a.pages;
+        if (!there && k0 < ahead.len && lane == 0) atomicOr(a.status, kBadIndex);
+        const uint32_t bit = 1u << (ahead_slot * W::kSub + s);
+        bad_slots = there ? bad_slots & ~bit : bad_slots | bit;
+        if (!there || k0 + 16 <= first_seen) continue;   // (not seen by any row: what the stage holds is not looked at)
+        const int slot = k0 - page_of(k0) * a.page_size;
+        const unsigned char* from = head_k + page * a.page_bytes + (int64_t)slot * row_bytes;
+        const uint32_t kd = to + s * W::kTileBytes;
+        const int unit = lane % C::kUnits, first = lane / C::kUnits;
+        if (D == DP) {
+#pragma unroll
+          for (int i = 0; i < C::kCopies; ++i)
+            copy_async<16>(kd + k_unit<W::kRowBytes>(i * C::kCopyRows + first, unit), from + i * 512 + lane * 16, true);
+        } else {
+          const bool live = unit * 16 < row_bytes;   // (past the row's end: zeros)
+#pragma unroll
+          for (int i = 0; i < C::kCopies; ++i) {
+            const int j = i * C::kCopyRows + first;
+            copy_async<16>(kd + k_unit<W::kRowBytes>(j, unit), from + (live ? j * row_bytes + unit * 16 : 0), live);
+          }
+        }
+        if constexpr (W::kEight) {   // four scales a lane
+          if (lane >> 2 == s)
+            copy_async<16>(to + W::kScales + lane * 16, a.ks + page * a.page_rows + head_row + slot + (lane & 3) * 4, true);
+        }
+      }
+      const int own = key + lane;
+      if (past && lane < W::kKeys) {
+        const bool live = own < ahead.len - a.new_tokens;
+        copy_async<4>(to + W::kPast + lane * 4, live ? past + own : past, live);
+      }
+      --ahead_left;
+      ahead_slot = ahead_slot + 1 == W::kStages ? 0 : ahead_slot + 1;
+      if (++in_batch == 16) look_up((ahead.unit + 1 + 16) * W::kKeys, next_ids);
+      if (in_batch == 32) {
+        in_batch = 0;
+#pragma unroll
+        for (int s = 0; s < W::kSub; ++s) ids[s] = next_ids[s];
+      }
+      if (ahead_left > 0 && ahead.next(a)) enter();
     }
-    seq_base += __shfl_sync(0xffffffffu, upto, 31);
-  }
-  int len = weigh_length(a, seq), units = (len + C::kUnit - 1) / C::kUnit;
-  int head = (u - seq_base) / units, unit = (u - seq_base) - head * units;
+    copy_commit();
+  };
 
-  // q of rows [row0, row0 + kChunk) of this sequence and head; by the whole block, between barriers
-  auto stage = [&](int row0) {
-#pragma unroll 1
-    for (int r = warp; r < kChunk; r += kWeighWarps) {
-      const int row = row0 + r, d0 = lane * 8;
-      const bool live = row < a.rows;
-      if (!live && row - r % 8 >= a.rows) break;   // a tile without a row is not looked at
-      const int tok = live ? row / a.group : 0, qh = head * a.group + row - tok * a.group;
-      const int64_t token = (int64_t)seq * a.new_tokens + tok;
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (live && d0 < D) raw = *reinterpret_cast<const uint4*>(a.q.at(token, qh) + d0 * 2);
+  // ---- a triple's rows ----
+  uint4 q[NT][W::kSteps / 2];
+  float lse[NT][2], factor[NT][2];    // of rows 8 n + 2 t and the next: times log2(e); scale log2(e) times what q was divided by
+  int pos[NT][2], lo[NT][2];          // their last and first visible position
+  int min_pos = 0, max_lo = 0, max_pos = -1;
+  auto load_rows = [&] {
+    const int64_t token0 = (int64_t)at.seq * a.new_tokens;
+    int least = INT_MAX, most = -1, latest = INT_MIN;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      {
+        const int row = n * 8 + g, tok = row / a.group;
+        const bool live = row < a.rows;
+        const unsigned char* from = live ? a.q.at(token0 + tok, at.head * a.group + row - tok * a.group) : nullptr;
+#pragma unroll
+        for (int j = 0; j < W::kSteps / 2; ++j) {
+          const int byte = W::kEight ? 128 * (j >> 1) + 32 * t + 16 * (j & 1) : 64 * j + 16 * t;
+          q[n][j] = live && byte < D * 2 ? *reinterpret_cast<const uint4*>(from + byte) : make_uint4(0, 0, 0, 0);
+        }
+      }
       float back = 1.f;
-      if (C::kEight && !a.q_f16) {
-        float x[8], top = 0.f;
-        widen8(raw, x, __nv_bfloat16());
+      if (W::kEight && !a.q_f16) {
+        float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+        for (int j = 0; j < W::kSteps / 2; ++j) {
+          float x[8];
+          widen8(q[n][j], x, __nv_bfloat16());
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // the power of two below top (1 for zeros, infinities and subnormals)
         uint32_t e = __float_as_uint(top) & 0x7f800000u;
+        float down = 1.f;
         if (e != 0 && e != 0x7f800000u) {
           e = e < 0x7e800000u ? e : 0x7e800000u;
           back = __uint_as_float(e);
-          const float down = __uint_as_float(0x7f000000u - e);
+          down = __uint_as_float(0x7f000000u - e);
+        }
+#pragma unroll
+        for (int j = 0; j < W::kSteps / 2; ++j) {
+          float x[8];
+          widen8(q[n][j], x, __nv_bfloat16());
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] *= down;
-        }
-        raw = pack8(x, __half());
-      }
-      if (d0 < DP) *reinterpret_cast<uint4*>(q_smem + r * C::kQStride + d0 * 2) = raw;
-      if (lane == 0) {
-        const float lse = live ? w.a.lse[token * a.q_heads + qh] : -INFINITY;
-        int p = live ? len - a.new_tokens + tok : -1, lo = a.starts ? a.starts[seq] : 0;
-        if (a.window > 0 && p - a.window + 1 > lo) lo = p - a.window + 1;
-        if (lse == -INFINITY) p = -1;   // a row that sees nothing (and those past the last)
-        row_lse[r] = lse * 1.4426950408889634f;
-        row_factor[r] = a.scale * 1.4426950408889634f * back;
-        row_pos[r] = p;
-        row_lo[r] = lo;
-      }
-    }
-    __syncthreads();
-    if (threadIdx.x < kChunk / 8 && row0 + (int)threadIdx.x * 8 < a.rows) {
-      int4 x = make_int4(INT_MAX, -1, INT_MAX, INT_MIN);
-      for (int r = threadIdx.x * 8; r < (int)threadIdx.x * 8 + 8; ++r) {
-        x.x = min(x.x, row_pos[r]), x.y = max(x.y, row_pos[r]);
-        x.z = min(x.z, row_lo[r]), x.w = max(x.w, row_lo[r]);
-      }
-      tile_span[threadIdx.x] = x;
-    }
-    __syncthreads();
-  };
-
-  bool staged = false;
-  for (; left > 0; --left) {
-    const int key0 = unit * C::kUnit + warp * C::kKeys;
-    const int64_t head_row = (int64_t)head * a.page_size;
-    // ---- K: from memory into the products' operands ----
-    uint32_t x[C::kTiles][C::kSteps][4];
-    float kscale[C::kTiles][2];
-    bool there[C::kTiles];
-#pragma unroll
-    for (int b = 0; b < C::kTiles; ++b) {
-      const int k0 = key0 + 16 * b;
-      const int index = (int)(((uint64_t)(uint32_t)(k0 >> 4) * a.page_mul) >> a.page_shift);
-      const int page = k0 < len ? __ldg(a.table.pages + seq * a.table.stride + index) : -1;
-      there[b] = (unsigned)page < (unsigned)a.pages;
-      if (k0 < len && !there[b] && lane == 0) atomicOr(a.status, kBadIndex);
-      const int64_t row = there[b] ? page * a.page_rows + head_row + (k0 - index * a.page_size) : 0;
-      const unsigned char* from = a.pk + (row + g) * row_bytes + t * 16;
-#pragma unroll
-      for (int c = 0; c < C::kPieces; ++c) {
-        const bool in = there[b] && 64 * c + 16 * t < row_bytes;
-        const uint4 y = in ? __ldg(reinterpret_cast<const uint4*>(from + 64 * c)) : make_uint4(0, 0, 0, 0);
-        const uint4 z = in ? __ldg(reinterpret_cast<const uint4*>(from + 8 * row_bytes + 64 * c)) : make_uint4(0, 0, 0, 0);
-        if constexpr (C::kEight) {
-          const uint32_t yw[4] = {y.x, y.y, y.z, y.w}, zw[4] = {z.x, z.y, z.z, z.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            widen4<FMT>(yw[i], x[b][4 * c + i][0], x[b][4 * c + i][2]);
-            widen4<FMT>(zw[i], x[b][4 * c + i][1], x[b][4 * c + i][3]);
-          }
-        } else {
-          x[b][2 * c][0] = y.x, x[b][2 * c][1] = z.x, x[b][2 * c][2] = y.y, x[b][2 * c][3] = z.y;
-          x[b][2 * c + 1][0] = y.z, x[b][2 * c + 1][1] = z.z, x[b][2 * c + 1][2] = y.w, x[b][2 * c + 1][3] = z.w;
+          q[n][j] = pack8(x, __half());
         }
       }
-      kscale[b][0] = kscale[b][1] = 1.f;
-      if (C::kEight && there[b]) kscale[b][0] = a.ks[row + g], kscale[b][1] = a.ks[row + g + 8];
-    }
-    // the key that this lane writes, and its weight so far
-    const int own = key0 + (C::kTiles == 2 ? 8 * t : 8 * (t & 1)) + g;
-    const bool writes = own < len && (C::kTiles == 2 || t < 2);
-    float before = 0.f;
-    if (writes && w.past && own < len - a.new_tokens) before = w.decay * w.past[seq * w.past_seq + head * w.past_head + own];
-
-    float sum[C::kTiles][2] = {};
-    for (int row0 = 0; row0 < a.rows; row0 += kChunk) {
-      if (!staged || a.rows > kChunk) {
-        __syncthreads();   // everyone is done with the last chunk
-        stage(row0);
-        staged = true;
-      }
-      const int tiles = (min(a.rows - row0, kChunk) + 7) / 8;
-      for (int n = 0; n < tiles; ++n) {
-        const int4 span = tile_span[n];
-        if (key0 > span.y || key0 + C::kKeys - 1 < span.z) continue;   // keys that none of these rows sees
-        float s[C::kTiles][4];
-#pragma unroll
-        for (int j = 0; j < C::kSteps / 2; ++j) {
-          const uint4 q = *reinterpret_cast<const uint4*>(
-              q_smem + (n * 8 + g) * C::kQStride + (C::kEight ? 128 * (j >> 1) + 32 * t + 16 * (j & 1) : 64 * j + 16 * t));
-#pragma unroll
-          for (int b = 0; b < C::kTiles; ++b) {
-            const uint32_t(&y)[4] = x[b][2 * j], (&z)[4] = x[b][2 * j + 1];
-            if (j == 0) mma16816_first<kBf16>(s[b], y[0], y[1], y[2], y[3], q.x, q.y);
-            else mma16816<kBf16>(s[b], y[0], y[1], y[2], y[3], q.x, q.y);
-            mma16816<kBf16>(s[b], z[0], z[1], z[2], z[3], q.z, q.w);
-          }
-        }
-        const int r = n * 8 + 2 * t;
-        const float2 lse = *reinterpret_cast<const float2*>(row_lse + r), f = *reinterpret_cast<const float2*>(row_factor + r);
-#pragma unroll
-        for (int b = 0; b < C::kTiles; ++b) {
-          float p[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            p[e] = exp2_fast(fmaf(s[b][e], (e & 1 ? f.y : f.x) * kscale[b][e >> 1], e & 1 ? -lse.y : -lse.x));
-          const int k0 = key0 + 16 * b;
-          if (!there[b] || k0 < span.w || k0 + 15 > span.x) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int j = k0 + g + 8 * (e >> 1), rr = r + (e & 1);
-              if (!there[b] || j > row_pos[rr] || j < row_lo[rr]) p[e] = 0.f;
-            }
-          }
-          sum[b][0] += p[0] + p[1];
-          sum[b][1] += p[2] + p[3];
-        }
-      }
-    }
-    // over the lanes that hold the other rows; then a key a lane
-#pragma unroll
-    for (int b = 0; b < C::kTiles; ++b) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        sum[b][e] += __shfl_xor_sync(0xffffffffu, sum[b][e], 1);
-        sum[b][e] += __shfl_xor_sync(0xffffffffu, sum[b][e], 2);
+        const int r = 2 * t + e, row = n * 8 + r, tok = row / a.group;
+        const bool live = row < a.rows;
+        const float x = live ? w.a.lse[(token0 + tok) * a.q_heads + at.head * a.group + row - tok * a.group] : -INFINITY;
+        int p = at.len - a.new_tokens + tok, first = a.starts ? a.starts[at.seq] : 0;
+        if (a.window > 0 && p - a.window + 1 > first) first = p - a.window + 1;
+        if (x == -INFINITY) p = -1;   // a row that sees nothing (and those past the last)
+        lse[n][e] = x * 1.4426950408889634f;
+        factor[n][e] = a.scale * 1.4426950408889634f * __shfl_sync(0xffffffffu, back, r * 4);
+        pos[n][e] = p;
+        lo[n][e] = first;
+        least = min(least, p), most = max(most, p), latest = max(latest, first);
       }
     }
-    const float low = t & 1 ? sum[0][1] : sum[0][0], high = t & 1 ? sum[C::kTiles - 1][1] : sum[C::kTiles - 1][0];
-    const float got = t & 2 ? high : low;
-    if (writes) w.out[seq * w.out_seq + head * w.out_head + own] = before + got;
+    min_pos = __reduce_min_sync(0xffffffffu, least);
+    max_pos = __reduce_max_sync(0xffffffffu, most);
+    max_lo = __reduce_max_sync(0xffffffffu, latest);
+  };
 
-    if (++unit == units && left > 1) {
-      unit = 0;
-      staged = false;
-      if (++head == a.kv_heads) {
-        head = 0;
-        do len = weigh_length(a, ++seq);
-        while (len == 0 && seq + 1 < a.table.seqs);
-        units = (len + C::kUnit - 1) / C::kUnit;
-      }
+  int slot = 0;
+  bool fresh = true;
+  int seen_from = 0;
+  for (int i = 1 - W::kStages; i < mine; ++i) {
+    issue();
+    if (i < 0) continue;   // the copies' head start
+    if (fresh) {
+      load_rows();
+      seen_from = span_of(a, at.seq, W::kKeys).lo;
+      fresh = false;
     }
+    copy_wait<W::kStages - 1>();
+    __syncwarp();
+    const unsigned char* st = ring + slot * W::kStageBytes;
+    const int key = at.unit * W::kKeys;
+    float got = 0.f;
+#pragma unroll
+    for (int b = 0; b < W::kSub; ++b) {
+      const int k0 = key + 16 * b;
+      float sum0 = 0.f, sum1 = 0.f;
+      if (k0 <= max_pos && k0 + 16 > seen_from && !(bad_slots >> (slot * W::kSub + b) & 1)) {
+        const unsigned char* kt = st + b * W::kTileBytes;
+        float s[NT][4];
+#pragma unroll
+        for (int c = 0; c < W::kPieces; ++c) {
+          const uint4 x = *reinterpret_cast<const uint4*>(kt + k_unit<W::kRowBytes>(g, 4 * c + t));
+          const uint4 y = *reinterpret_cast<const uint4*>(kt + k_unit<W::kRowBytes>(g + 8, 4 * c + t));
+          if constexpr (W::kEight) {
+            const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+            uint32_t xa[8], ya[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              widen4<FMT>(xw[e], xa[2 * e], xa[2 * e + 1]);
+              widen4<FMT>(yw[e], ya[2 * e], ya[2 * e + 1]);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const uint4 q0 = q[n][2 * c], q1 = q[n][2 * c + 1];
+              if (c == 0) mma16816_first<false>(s[n], xa[0], ya[0], xa[1], ya[1], q0.x, q0.y);
+              else mma16816<false>(s[n], xa[0], ya[0], xa[1], ya[1], q0.x, q0.y);
+              mma16816<false>(s[n], xa[2], ya[2], xa[3], ya[3], q0.z, q0.w);
+              mma16816<false>(s[n], xa[4], ya[4], xa[5], ya[5], q1.x, q1.y);
+              mma16816<false>(s[n], xa[6], ya[6], xa[7], ya[7], q1.z, q1.w);
+            }
+          } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const uint4 qn = q[n][c];
+              if (c == 0) mma16816_first<kBf16>(s[n], x.x, y.x, x.y, y.y, qn.x, qn.y);
+              else mma16816<kBf16>(s[n], x.x, y.x, x.y, y.y, qn.x, qn.y);
+              mma16816<kBf16>(s[n], x.z, y.z, x.w, y.w, qn.z, qn.w);
+            }
+          }
+        }
+        float scale0 = 1.f, scale1 = 1.f;
+        if constexpr (W::kEight) {
+          const float* sc = reinterpret_cast<const float*>(st + W::kScales) + b * 16;
+          scale0 = sc[g], scale1 = sc[g + 8];
+        }
+        const bool masked = k0 < max_lo || k0 + 15 > min_pos;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = exp2_fast(fmaf(s[n][e], factor[n][e & 1] * (e < 2 ? scale0 : scale1), -lse[n][e & 1]));
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int j = k0 + g + 8 * (e >> 1);
+              if (j > pos[n][e & 1] || j < lo[n][e & 1]) p[e] = 0.f;
+            }
+          }
+          sum0 += p[0] + p[1];
+          sum1 += p[2] + p[3];
+        }
+      }
+      // over the lanes that hold the other rows; then a key a lane: lane l the unit's key l
+      sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1);
+      sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1);
+      sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);
+      sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
+      const float from0 = __shfl_sync(0xffffffffu, sum0, (lane & 7) * 4), from1 = __shfl_sync(0xffffffffu, sum1, (lane & 7) * 4);
+      if (lane >> 4 == b) got = lane & 8 ? from1 : from0;
+    }
+    const int own = key + lane;
+    if (lane < W::kKeys && own < at.len) {
+      const float before = w.past ? w.decay * reinterpret_cast<const float*>(st + W::kPast)[lane] : 0.f;
+      w.out[at.seq * w.out_seq + at.head * w.out_head + own] = own < at.len - a.new_tokens ? before + got : got;
+    }
+    __syncwarp();   // the slot is free again
+    slot = slot + 1 == W::kStages ? 0 : slot + 1;
+    if (i + 1 < mine && at.next(a)) fresh = true;
   }
 }
 
-template <int FMT, int DP>
+template <int FMT, int DP, int NT>
 cudaError_t launch_weigh_one(const WeighArgs& w, int num_sms, cudaStream_t st) {
-  using C = WeighConfig<FMT, DP>;
-  const int64_t units = ((int64_t)w.a.max_len + C::kUnit - 1) / C::kUnit;
+  using W = WeighConfig<FMT, DP, NT>;
+  static_assert(W::kSmem <= 227 * 1024 && W::kStages * W::kSub <= 32, "shared memory, and a bit a tile");
+  auto* kernel = weigh_kernel<FMT, DP, NT>;
+  static std::atomic<int> resident[kMaxDevices];   // blocks an SM holds, by device; 0: not asked yet
+  int per_sm = w.a.device < kMaxDevices ? resident[w.a.device].load(std::memory_order_relaxed) : 0;
+  if (per_sm == 0) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, W::kSmem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kWeighThreads, W::kSmem);
+    if (e != cudaSuccess) return e;
+    per_sm = per_sm < 1 ? 1 : per_sm;
+    if (w.a.device < kMaxDevices) resident[w.a.device].store(per_sm, std::memory_order_relaxed);
+  }
+  const int64_t units = ((int64_t)w.a.max_len + W::kKeys - 1) / W::kKeys;
   const double most = (double)w.a.table.seqs * w.a.kv_heads * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // units are counted in 32 bits
-  const int blocks = most < 2.0 * num_sms ? (int)most : 2 * num_sms;
-  weigh_kernel<FMT, DP><<<blocks, kWeighThreads, 0, st>>>(w);
+  const int blocks = most < (double)per_sm * num_sms ? (int)most : per_sm * num_sms;
+  kernel<<<blocks, kWeighThreads, W::kSmem, st>>>(w);
   return cudaGetLastError();
+}
+template <int FMT, int NT>
+cudaError_t launch_weigh_rows(const WeighArgs& w, int num_sms, cudaStream_t st) {
+  switch (padded_dim(w.a.head_dim)) {
+    case 64: return launch_weigh_one<FMT, 64, NT>(w, num_sms, st);
+    case 128: return launch_weigh_one<FMT, 128, NT>(w, num_sms, st);
+    default: return launch_weigh_one<FMT, 256, NT>(w, num_sms, st);
+  }
 }
 template <int FMT>
 cudaError_t launch_weigh(const WeighArgs& w, int num_sms, cudaStream_t st) {
-  switch (padded_dim(w.a.head_dim)) {
-    case 64: return launch_weigh_one<FMT, 64>(w, num_sms, st);
-    case 128: return launch_weigh_one<FMT, 128>(w, num_sms, st);
-    default: return launch_weigh_one<FMT, 256>(w, num_sms, st);
-  }
+  return w.a.rows <= 8 ? launch_weigh_rows<FMT, 1>(w, num_sms, st) : launch_weigh_rows<FMT, 2>(w, num_sms, st);
 }
 
 }  // namespace
@@ -303,7 +354,13 @@ extern "C" lacache_status lacache_kv_weigh(lacache_kv_t* h, int32_t layer, const
   w.out_head = in->out.head_stride;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
   cudaError_t e;
-  switch (h->cfg.format) {
+  if (w.a.rows > lc::kFewRows) {
+    if (h->inject_stall > 0) {
+      w.a.inject_stall = 1;
+      --h->inject_stall;
+    }
+    e = lc::launch_weigh_tc(w, h->cfg.format, h->num_sms, st);
+  } else switch (h->cfg.format) {
     case LACACHE_KV_BF16: e = lc::launch_weigh<LACACHE_KV_BF16>(w, h->num_sms, st); break;
     case LACACHE_KV_F16: e = lc::launch_weigh<LACACHE_KV_F16>(w, h->num_sms, st); break;
     case LACACHE_KV_E4M3: e = lc::launch_weigh<LACACHE_KV_E4M3>(w, h->num_sms, st); break;

@@ -237,6 +237,42 @@ def test_another_stream_and_layers():
         assert torch.allclose(got[s, :, :n] + past[s, :, :n], want[s, :, :n], rtol=2 ** -22, atol=2 ** -22)
 
 
+def test_a_wait_that_runs_out_is_reported():
+    c = Filled("bf16", [400, 90], 2, 64, seed=14)
+    q, lse = queries(c, "bf16", 8, 9), torch.empty(18, 8, device="cuda")
+    c.kv.attend(q, c.table, c.len_dev, new_tokens=9, lse=lse)
+    want = c.kv.weigh(q, c.table, c.len_dev, lse, new_tokens=9)
+    L.load().lacache_kv_inject_stall(c.kv.h, 1)
+    c.kv.weigh(q, c.table, c.len_dev, lse, new_tokens=9)
+    with pytest.raises(L.LacacheError) as e:
+        c.kv.sync()
+    assert e.value.status == L.LACACHE_ERR_DEVICE_TIMEOUT
+    assert torch.equal(c.kv.weigh(q, c.table, c.len_dev, lse, new_tokens=9), want)
+    c.kv.sync()
+
+
+@pytest.mark.parametrize("head_dim", [256, 144])
+def test_a_wait_that_runs_out_in_wide_heads(head_dim):
+    c = Filled("f16", [400, 90], 1, head_dim, seed=15)
+    q, lse = queries(c, "f16", 8, 9), torch.zeros(18, 8, device="cuda")
+    L.load().lacache_kv_inject_stall(c.kv.h, 1)
+    c.kv.weigh(q, c.table, c.len_dev, lse, new_tokens=9)
+    with pytest.raises(L.LacacheError) as e:
+        c.kv.sync()
+    assert e.value.status == L.LACACHE_ERR_DEVICE_TIMEOUT
+    check(c, "f16", 8, 9)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("head_dim", [48, 64, 80, 128, 144, 256])
+@pytest.mark.parametrize("group,new", [(3, 6), (1, 33), (7, 15), (2, 97)])
+def test_rows_of_every_tile(fmt, dtype, head_dim, group, new):
+    """From 18 to 200 rows a kv head: tiles that are full, and not."""
+    c = Filled(fmt, [530, 128, 1, 0, 255, 257, new, new + 1], 2, head_dim, 16, seed=head_dim + new)
+    check(c, dtype, 2 * group, new)
+    check(c, dtype, 2 * group, new, window=100, starts=[0, 3, 0, 0, 200, 100, 5, 0], decay=0.5)
+
+
 def test_refusals():
     c = Filled("bf16", [40], 2, 64, seed=13)
     q, lse = queries(c, "bf16", 4, 1), torch.zeros(1, 4, device="cuda")
