@@ -120,6 +120,18 @@ def test_long_sequences():
     check(c, to, random_weights(c, 6), 5000, 100)
 
 
+def test_more_positions_than_shared_memory_holds():
+    c, to = filled("bf16", [450_001, 9], 1, 16, 128, 700, seed=12)
+    check(c, to, random_weights(c, 12), 700, 100)
+    check(c, to, random_weights(c, 13, levels=40), 700, 0)
+
+
+@pytest.mark.parametrize("kv_heads,lengths", [(3, [9000] * 40), (1, [5000, 4097, 12_288, 2048]), (8, [20_000, 11])])
+def test_clusters_of_every_size(kv_heads, lengths):
+    c, to = filled("bf16", lengths, kv_heads, 16, 64, 900, seed=13)
+    check(c, to, random_weights(c, 14, levels=1000), 900, 77)
+
+
 def test_strided_weights_and_layers():
     c, to = filled("bf16", [100, 44], 2, 64, 16, 30, seed=7, layers=2, layer=1)
     w = random_weights(c, 7, wide=9)
