@@ -62,7 +62,8 @@ def build(verbose: bool = False, force: bool = False) -> str:
 
 def _build_locked(verbose: bool, force: bool) -> str:
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    deps = srcs + [os.path.join(CSRC, h) for h in ("internal.cuh", "tcgen05.cuh", "decode.cuh", "kv_attend.cuh", "kv_weigh.cuh")]
+    deps = srcs + [os.path.join(CSRC, h) for h in ("internal.cuh", "tcgen05.cuh", "decode.cuh", "kv_attend.cuh", "kv_weigh.cuh",
+                                                     "kv_tc.cuh")]
     deps += [os.path.join(INCLUDE, "lacache.h"), __file__]
     peaks_src = os.path.join(CSRC, PEAKS_SOURCE)
     lib_ok = os.path.exists(LIB) and os.path.getmtime(LIB) >= max(os.path.getmtime(p) for p in deps)

@@ -86,17 +86,20 @@ struct AttendArgs {
   float* partial;       // two slots a block: [rows of a tile x DP] sums, then (m, l) a row
   unsigned int* arrived;   // blocks that have left their part of the triple that begins in this block; zero between launches
   unsigned int* status;
-  // a call over groups of sequences that have their first positions in common (kv_shared.cu), in two passes
+  // a pass of a call over groups of sequences that have their first positions in common (kv_shared.cu)
   int groups;
   const int4* spans;      // of each group: the first common position that is seen, one past the last, first sequence, sequences
-  const int32_t* joined;  // whether a sequence has a common part
-  float* common;          // that part's outputs, [tokens x q_heads x head_dim] ...
-  float* common_lse;      // ... and base-2 lse
+  int* line;              // kCommon on tcgen05: cells a block has, blocks that have one more, the cells before each group
+  int slot_rows;          // ... and rows of a slot of partial sums
+  float* part;            // the pass's outputs, [tokens x q_heads x head_dim] ...
+  float* part_lse;        // ... and base-2 lse
 };
 
-// The kernels' forms: attention of its own; over what groups of sequences have in common, where a group takes a sequence's place
-// and has the rows of all of its sequences; and over what each sequence has of its own, joined with the other.
+// The kernels' forms: a whole attention; the pass over what groups of sequences have in common, where a group takes a sequence's
+// place and has the rows of all of its sequences; and the pass over what each sequence has of its own. The passes leave their
+// outputs in fp32, to be joined.
 constexpr int kWhole = 0, kCommon = 1, kOwn = 2;
+constexpr int kCommonRows = 256, kCommonKeys = 128, kCommonCost = 4;   // kCommon on tcgen05: a block's rows, and the line's units
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;
@@ -140,7 +143,7 @@ cudaError_t launch_common_bf16(const AttendArgs& a, int num_sms, cudaStream_t st
 cudaError_t launch_common_f16(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_common_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_common_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
-cudaError_t launch_common_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
+cudaError_t launch_common_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);   // heads of up to 128
 cudaError_t launch_own_bf16(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_own_f16(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_own_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
@@ -224,6 +227,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // Four 8 x 8 tiles of 16-bit values from shared memory, transposed: lane l names the 16-byte row l % 8 of tile l / 8.
 __device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t& a0, uint32_t& a1, uint32_t& a2, uint32_t& a3) {
@@ -269,11 +277,15 @@ template <int FORM>
 __device__ __forceinline__ int tiles_of(const AttendArgs& a, const Span& s) { return FORM == kCommon ? s.tiles : a.row_tiles; }
 template <int FORM>   // the row of the table, and of which sequence the rows' first token is
 __device__ __forceinline__ int first_of(int seq, const Span& s) { return FORM == kCommon ? s.first : seq; }
+template <int FORM>   // (kOwn: written as the spans are)
+__device__ __forceinline__ int start_of(const AttendArgs& a, int seq) {
+  return !a.starts ? 0 : FORM == kOwn ? __ldcg(a.starts + seq) : a.starts[seq];
+}
 template <int FORM = kWhole>
 __device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_keys, int tile_rows = 0) {
   Span s;
   if constexpr (FORM == kCommon) {
-    const int4 x = a.spans[seq];
+    const int4 x = __ldcg(a.spans + seq);   // (written by a kernel that this one may have started beside)
     s.lo = x.x;
     s.len = s.hi = x.y;
     s.first = x.z;
@@ -286,7 +298,7 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int seq, int unit_k
   int len = a.lengths[seq];
   len = len < 0 ? 0 : len > a.max_len ? a.max_len : len;
   const int first = len - a.new_tokens;   // the first row's position
-  int lo = a.starts ? a.starts[seq] : 0;
+  int lo = start_of<FORM>(a, seq);
   if (a.window > 0 && first - a.window + 1 > lo) lo = first - a.window + 1;   // window < 2^31, first >= -512: no overflow
   lo = lo < 0 ? 0 : lo > len ? len : lo;
   s.len = len;
@@ -310,57 +322,25 @@ __device__ __forceinline__ int2 seen_by(const AttendArgs& a, int seq, const Span
   } else {
     pos = sp.len - a.new_tokens + tok;
   }
-  int lo = a.starts ? a.starts[of] : 0;
+  int lo = start_of<FORM>(a, of);
   if (a.window > 0 && pos - a.window + 1 > lo) lo = pos - a.window + 1;
   if (FORM == kCommon && pos > sp.hi - 1) pos = sp.hi - 1;
   return make_int2(pos, lo);
 }
 
-// Where row `row` of a kv head goes: bytes into out, and its index in lse. (kCommon: into the common part's outputs.)
+// Where row `row` of a kv head goes: bytes into out (of a pass: into part), and its index in lse.
 template <int FORM = kWhole>
 __device__ __forceinline__ int64_t out_at(const AttendArgs& a, int first, int head, int row, int64_t* lse) {
   const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
   const int64_t token = (int64_t)first * a.new_tokens + tok;
   *lse = token * a.q_heads + qh;
-  if (FORM == kCommon) return *lse * a.head_dim * 4;
+  if (FORM != kWhole) return *lse * a.head_dim * 4;
   return a.out.at(token, qh) - a.out.p;
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// A row's end: its sums' factor, kOwn's weight of the common part's output, and its lse (written). `joined`: it has a common part.
-struct End {
-  float f, common;
-};
-template <int FORM>
-__device__ __forceinline__ End end_of(const AttendArgs& a, float top, float sum, int64_t lse, bool joined, bool write = true) {
-  End x = {sum == 0.f ? 0.f : 1.f / sum, 0.f};
-  if constexpr (FORM == kCommon) {
-    if (write) a.common_lse[lse] = sum == 0.f ? -INFINITY : top + log2f(sum);
-  } else {
-    float l = sum == 0.f ? -INFINITY : top + log2f(sum);
-    if (FORM == kOwn && joined) {
-      const float other = a.common_lse[lse], most = fmaxf(l, other);
-      if (most > -INFINITY || l != l || other != other) {
-        const float mine = exp2_fast(l - most), its = exp2_fast(other - most), both = mine + its;
-        x.common = its / both;
-        // (not 0 where anything was seen: a value that is not finite shows however little it counts)
-        if (sum != 0.f) x.f = fmaxf(x.f * (mine / both), 0x1p-126f);
-        if (mine != mine || both != both) x.f = NAN;
-        l = most + log2f(both);
-      }
-    }
-    if (write && a.lse) a.lse[lse] = l * 0.6931471805599453f;
-  }
-  return x;
 }
 // Four values of an output row. Sums are kept in the order of the accumulators: quad 4 d + p holds tile d's two values of
 // lane group g = 2p and its two of g + 1. f is 1 / the row's sum of weights, 0 if nothing was seen.
 template <typename C, int FORM = kWhole>
-__device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, int quad, float4 acc, float f, float of_common = 0.f,
-                                           int64_t lse = 0, bool joined = false) {
+__device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, int quad, float4 acc, float f) {
   const float4 y = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
   const int d = quad >> 2, g = (quad & 3) * 2;
   int at[2];        // the first dimensions of two pairs
@@ -377,21 +357,12 @@ __device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, 
     pair[0] = make_float2(y.x, y.z);
     pair[1] = make_float2(y.y, y.w);
   }
-  if constexpr (FORM == kCommon) {
-    float* out = a.common + at_row / 4;
+  if constexpr (FORM != kWhole) {
+    float* out = a.part + at_row / 4;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (at[i] < a.head_dim) *reinterpret_cast<float2*>(out + at[i]) = pair[i];
     return;
-  }
-  if (FORM == kOwn && joined) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (at[i] >= a.head_dim) continue;
-      const float2 c = *reinterpret_cast<const float2*>(a.common + lse * a.head_dim + at[i]);
-      pair[i].x += of_common * c.x;
-      pair[i].y += of_common * c.y;
-    }
   }
   unsigned char* out = a.out.p + at_row;
 #pragma unroll
@@ -403,6 +374,21 @@ __device__ __forceinline__ void write_quad(const AttendArgs& a, int64_t at_row, 
 }
 __device__ __forceinline__ float lse_of(float top, float sum) {
   return sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+template <int FORM>
+__device__ __forceinline__ void write_lse(const AttendArgs& a, int64_t at, float top, float sum) {
+  if (FORM != kWhole) a.part_lse[at] = sum == 0.f ? -INFINITY : top + log2f(sum);
+  else if (a.lse) a.lse[at] = lse_of(top, sum);
+}
+
+// The kernels of a call over groups are launched as soon as the one before has begun (programmatic dependent launch), and wait for
+// its end here.
+template <int FORM>
+__device__ __forceinline__ void pass_begins() {
+  if (FORM != kWhole) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
 }
 
 template <int FMT, int DP, int NT, int FORM = kWhole>
@@ -416,11 +402,10 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   __shared__ float row_factor[C::kRows];                // scale log2(e), and what the row's q was divided by
   __shared__ int64_t row_out[C::kRows];                 // where a row goes, and 1 / its sum of weights
   __shared__ float row_inv[C::kRows];
-  __shared__ float row_common[FORM == kOwn ? C::kRows : 1];   // kOwn: the common part's weight, and the row's index in lse
-  __shared__ int64_t row_lse[FORM == kOwn ? C::kRows : 1];
   __shared__ int page_ids[kAttendWarps][C::kStages][C::kSub];
   __shared__ int pending[2][6];   // shared triples: sequence, triple, first and last block (-1: none), rows and tiles (kCommon)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  pass_begins<FORM>();
   const int D = a.head_dim, row_bytes = D * C::kItem;
   const int per_whole = a.kv_heads * a.row_tiles;
   auto triples_of = [&](const Span& s) { return FORM == kCommon ? a.kv_heads * s.tiles : per_whole; };   // of a sequence
@@ -713,7 +698,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
               row_lo[r] = seen.y;
             } else {
               const int p = live ? sp.len - a.new_tokens + tok : -1;
-              int lo = a.starts ? a.starts[seq] : 0;
+              int lo = start_of<FORM>(a, seq);
               if (a.window > 0 && p - a.window + 1 > lo) lo = p - a.window + 1;
               row_pos[r] = p;
               row_lo[r] = lo;
@@ -1137,7 +1122,6 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
 
     const int of_seq = first_of<FORM>(seq, sp), of_triple = triple, of_units = sp.units, of_base = seq_base;
     const int of_rows = rows_of<FORM>(a, sp), of_tiles = tiles_of<FORM>(a, sp);
-    const bool joined = FORM == kOwn && a.joined[seq];
     left -= units;
     if (first_unit + units == of_units) left -= kTripleCost;
     first_unit = 0;
@@ -1193,17 +1177,8 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       if (whole) {
         int64_t at_lse;
         row_out[r] = out_at<FORM>(a, of_seq, head, row0 + r, &at_lse);
-        if constexpr (FORM == kWhole) {
-          row_inv[r] = sum == 0.f ? 0.f : 1.f / sum;
-          if (a.lse) a.lse[at_lse] = lse_of(top, sum);
-        } else {
-          const End end = end_of<FORM>(a, top, sum, at_lse, joined);
-          row_inv[r] = end.f;
-          if constexpr (FORM == kOwn) {
-            row_common[r] = end.common;
-            row_lse[r] = at_lse;
-          }
-        }
+        row_inv[r] = sum == 0.f ? 0.f : 1.f / sum;
+        write_lse<FORM>(a, at_lse, top, sum);
       } else {
         *reinterpret_cast<float2*>(mine_out + C::kRows * DP + r * 2) = make_float2(top, sum);
       }
@@ -1241,10 +1216,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
           const float4 x = *reinterpret_cast<const float4*>(join + (w * C::kRows + r) * C::kOStride + q * 4);
           acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
         }
-        if (whole) {
-          if constexpr (FORM == kOwn) write_quad<C, FORM>(a, row_out[r], quad, acc, row_inv[r], row_common[r], row_lse[r], joined);
-          else write_quad<C, FORM>(a, row_out[r], quad, acc, row_inv[r]);
-        }
+        if (whole) write_quad<C, FORM>(a, row_out[r], quad, acc, row_inv[r]);
         else *reinterpret_cast<float4*>(mine_out + r * DP + quad * 4) = acc;
       }
       if (c < 3) __syncthreads();
@@ -1282,8 +1254,6 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
   __shared__ float joint_top[2 * C::kRows];
   __shared__ int64_t joint_out[2 * C::kRows];
   __shared__ float joint_inv[2 * C::kRows];
-  __shared__ float joint_common[FORM == kOwn ? 2 * C::kRows : 1];
-  __shared__ int64_t joint_lse[FORM == kOwn ? 2 * C::kRows : 1];
   // the rows' common maxima and sums: eight lanes a row, eight loads in flight a lane
   for (int x0 = 0; x0 < rows0 + rows1; x0 += kAttendThreads / 8) {
     const int x = x0 + (threadIdx.x >> 3), sub = threadIdx.x & 7;
@@ -1316,27 +1286,12 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
       int64_t at_lse;
       joint_out[x] = out_at<FORM>(a, pending[k][0], head, row0 + r, &at_lse);
       joint_top[x] = all == -INFINITY ? 0.f : all;
-      if constexpr (FORM == kWhole) {
-        joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
-        if (a.lse) a.lse[at_lse] = lse_of(all, sum);
-      } else {
-        const End end = end_of<FORM>(a, all, sum, at_lse, FORM == kOwn && a.joined[pending[k][0]]);
-        joint_inv[x] = end.f;
-        if constexpr (FORM == kOwn) {
-          joint_common[x] = end.common;
-          joint_lse[x] = at_lse;
-        }
-      }
+      joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
+      write_lse<FORM>(a, at_lse, all, sum);
     }
   }
   __syncthreads();
   // sixteen loads in flight a thread: those of four values from up to four blocks, or of one value from sixteen
-  auto write_joint = [&](int x, int quad, float4 acc) {
-    if constexpr (FORM == kOwn)
-      write_quad<C, FORM>(a, joint_out[x], quad, acc, joint_inv[x], joint_common[x], joint_lse[x],
-                          a.joined[pending[x < rows0 ? 0 : 1][0]]);
-    else write_quad<C, FORM>(a, joint_out[x], quad, acc, joint_inv[x]);
-  };
   const int values = (rows0 + rows1) * kQuads;
   const int most = max(rows0 ? pending[0][3] - pending[0][2] : 0, rows1 ? pending[1][3] - pending[1][2] : 0) + 1;
   if (most <= 4) {
@@ -1368,7 +1323,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
             const float f = exp2_fast(w[v][e] - joint_top[x]);
             acc.x += f * y[v][e].x, acc.y += f * y[v][e].y, acc.z += f * y[v][e].z, acc.w += f * y[v][e].w;
           }
-          write_joint(x, j % kQuads, acc);
+          write_quad<C, FORM>(a, joint_out[x], j % kQuads, acc, joint_inv[x]);
         }
       }
     }
@@ -1397,8 +1352,27 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 && DP <= 128 ? 3 : 1) 
         }
       }
     }
-    write_joint(x, quad, acc);
+    write_quad<C, FORM>(a, joint_out[x], quad, acc, joint_inv[x]);
   }
+}
+
+template <int FORM>
+cudaError_t launch_form(void (*kernel)(AttendArgs), int blocks, int threads, int smem, const AttendArgs& a, cudaStream_t st) {
+  if (FORM == kWhole) {
+    kernel<<<blocks, threads, smem, st>>>(a);
+    return cudaGetLastError();
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <int FMT, int DP, int NT, int FORM = kWhole>
@@ -1423,8 +1397,7 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
   const double most = tiles * a.kv_heads * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // units are counted in 32 bits
   a.parts = most < (double)per_sm * num_sms ? (int)most : per_sm * num_sms;
-  kernel<<<a.parts, kAttendThreads, C::kSmem, st>>>(a);
-  return cudaGetLastError();
+  return launch_form<FORM>(kernel, a.parts, kAttendThreads, C::kSmem, a, st);
 }
 
 template <int FMT, int FORM = kWhole>

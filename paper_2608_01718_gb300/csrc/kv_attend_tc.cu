@@ -32,16 +32,13 @@
 // Every wait is bounded (about a second, renewed while a row is computed again): past it the block records a timeout, its roles
 // stop, copies and products in flight are drained, TMEM is freed and the block ends, after it has arrived where it shares
 // triples; lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT.
-#include "kv_attend.cuh"
-#include "tcgen05.cuh"
+#include "kv_tc.cuh"
 
 namespace lc {
 namespace {
 
-constexpr int kTile = 128;                   // rows of q, and keys, a tile
 constexpr int kStages = 3;                   // 8-bit caches: tiles of codes in flight (five measured 2% slower)
 constexpr int kStageBytes = kTile * 128;
-constexpr int kBlockBytes = kTile * 128;     // 64 elements of 128 rows
 constexpr int kSlotBytes = 2 * kBlockBytes;
 constexpr int kSoftmax = 256;                // threads: two a row, half of the keys each
 constexpr int kMmaWarp = 8;
@@ -70,7 +67,7 @@ struct Tc {
     uint32_t tmem;
     uint32_t abort_flag;
     uint32_t bad[16];                          // a unit's 16-key tiles whose page id is no page (by unit modulo 16)
-    int pending[2][6];                         // shared triples, as in kv_attend.cuh
+    int pending[2][4];                         // shared triples, as in kv_attend.cuh
     // 8-bit caches: a unit's scales of K, then of V (by unit modulo 8)
     alignas(16) float scales[kEight ? 8 * 2 * kTile : 4];   // read four at a time
   };
@@ -81,235 +78,22 @@ struct Tc {
   static_assert(kTail % 16 == 0 && alignof(Tail) == 16, "the scales' alignment");
 };
 
-// Where 16-byte unit u of row r lies in a tile of 128 rows: blocks of 64 elements, 128-byte swizzle.
-__device__ __forceinline__ uint32_t unit_at(int r, int u) {
-  return (uint32_t)((u >> 3) * kBlockBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4));
-}
-
-// An MN-major operand in the 128-byte swizzle layout: 64 elements a row of 128 B, 8 rows 1024 B apart along K (stride byte
-// offset), blocks of 64 elements kBlockBytes apart along N (leading byte offset).
-__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr) {
-  uint64_t desc = (uint64_t)((addr >> 4) & 0x3FFFu);
-  desc |= (uint64_t)(kBlockBytes >> 4) << 16;
-  desc |= (uint64_t)(1024 >> 4) << 32;
-  desc |= (uint64_t)1 << 46;
-  desc |= (uint64_t)2 << 61;
-  return desc;
-}
-// D += A B with A in TMEM (lane = row, two elements a column).
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-
-__device__ __forceinline__ float max_three(float x, float y, float z) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
-  return d;
-}
-// An arrival of this thread's, once all of its copies so far have landed.
-__device__ __forceinline__ void copies_arrive(uint64_t& bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bar)) : "memory");
-}
-// One arrival for a warp, after what all of its lanes did.
-__device__ __forceinline__ void warp_arrive(uint64_t& bar) {
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&bar));
-}
-
-// This block's part of the line of cells: triples in order, each with its first unit and how many units are the block's.
-template <int FORM>
-struct Walk {
-  int seq, seq_base, triple, first_unit, left;   // left: cells, this triple's units first
-  int per_whole;
-  Span sp;
-  __device__ __forceinline__ int per_seq(const AttendArgs& a) const { return FORM == kCommon ? a.kv_heads * sp.tiles : per_whole; }
-  __device__ __forceinline__ int units() const { return min(sp.units - first_unit, left); }
-  __device__ __forceinline__ bool done() const { return left <= 0; }
-  __device__ __forceinline__ void next(const AttendArgs& a) {
-    const int n = units();
-    left -= n;
-    if (first_unit + n == sp.units) left -= kCost;
-    first_unit = 0;
-    if (left > 0 && ++triple == per_seq(a)) {
-      triple = 0;
-      seq_base += (sp.units + kCost) * per_seq(a);
-      seq = min(seq + 1, seqs_of<FORM>(a) - 1);
-      sp = span_of<FORM>(a, seq, kTile, kTile);
-    }
-  }
-};
-struct Line {
-  int share, longer;
-  __device__ __forceinline__ int block_of(int cell) const {
-    const int in_longer = longer * (share + 1);
-    return cell < in_longer ? cell / (share + 1) : longer + (cell - in_longer) / share;
-  }
-};
-// By a whole warp. false: this block has no part.
-template <int FORM>
-__device__ bool start_walk(const AttendArgs& a, Walk<FORM>& w, Line& line) {
-  const int lane = threadIdx.x & 31, block = blockIdx.x, seqs = seqs_of<FORM>(a);
-  w.per_whole = a.kv_heads * a.row_tiles;
-  auto cells_of = [&](int s) {   // of one of the sequence's triples, or, where their number differs, of all
-    const Span x = span_of<FORM>(a, s, kTile, kTile);
-    return (x.units + kCost) * (FORM == kCommon ? a.kv_heads * x.tiles : 1);
-  };
-  const int times = FORM == kCommon ? 1 : w.per_whole;
-  int total = 0;
-  for (int s = lane; s < seqs; s += 32) total += cells_of(s);
-  total = __reduce_add_sync(0xffffffffu, total) * times;
-  const int parts = min(total, a.parts);
-  if (block >= parts) return false;
-  line.share = total / parts;
-  line.longer = total - line.share * parts;
-  const int u = block * line.share + min(block, line.longer);
-  w.seq = w.seq_base = 0;
-  for (int s0 = 0; s0 < seqs; s0 += 32) {
-    const int own = s0 + lane < seqs ? cells_of(s0 + lane) * times : 0;
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
-    }
-    const unsigned past = __ballot_sync(0xffffffffu, w.seq_base + upto > u);
-    if (past) {
-      const int l0 = __ffs(past) - 1;
-      w.seq = s0 + l0;
-      w.seq_base += __shfl_sync(0xffffffffu, upto - own, l0);
-      break;
-    }
-    w.seq_base += __shfl_sync(0xffffffffu, upto, 31);
-  }
-  w.sp = span_of<FORM>(a, w.seq, kTile, kTile);
-  w.triple = (u - w.seq_base) / (w.sp.units + kCost);
-  w.first_unit = u - w.seq_base - w.triple * (w.sp.units + kCost) - kCost;
-  w.left = line.share + (block < line.longer ? 1 : 0);
-  if (w.first_unit < 0) {
-    w.left += w.first_unit;
-    w.first_unit = 0;
-  }
-  return true;
-}
-
-// The common part's output, in a row of kOwn.
-struct Other {
-  float weight;
-  int64_t lse;
-  bool joined;
-};
-__device__ __forceinline__ void add_common(const AttendArgs& a, const Other& o, int d, float4& y) {
-  const float4 c = *reinterpret_cast<const float4*>(a.common + o.lse * a.head_dim + d);
-  y.x += o.weight * c.x, y.y += o.weight * c.y, y.z += o.weight * c.z, y.w += o.weight * c.w;
-}
 // Four neighbouring dimensions of an output row.
 template <int FORM>
-__device__ __forceinline__ void write4(const AttendArgs& a, int64_t at_row, int d, float4 y, const Other& o) {
-  if constexpr (FORM == kCommon) {
-    *reinterpret_cast<float4*>(a.common + at_row / 4 + d) = y;
-    return;
-  }
-  if (FORM == kOwn && o.joined) add_common(a, o, d, y);
-  *reinterpret_cast<uint2*>(a.out.p + at_row + d * 2) =
-      a.q_f16 ? make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w)) : make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
+__device__ __forceinline__ void write4(const AttendArgs& a, int64_t at_row, int d, float4 y) {
+  if constexpr (FORM != kWhole) *reinterpret_cast<float4*>(a.part + at_row / 4 + d) = y;
+  else
+    *reinterpret_cast<uint2*>(a.out.p + at_row + d * 2) =
+        a.q_f16 ? make_uint2(pack2<false>(y.x, y.y), pack2<false>(y.z, y.w)) : make_uint2(pack2<true>(y.x, y.y), pack2<true>(y.z, y.w));
 }
 
 // Eight, times g (0: zeros, whatever they are).
 template <int FORM>
-__device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int d, float4 x, float4 y, float g, const Other& o) {
+__device__ __forceinline__ void write8(const AttendArgs& a, int64_t at_row, int d, float4 x, float4 y, float g) {
   if (g == 0.f) x = y = make_float4(0.f, 0.f, 0.f, 0.f);
-  if constexpr (FORM != kWhole) {
-    x = make_float4(x.x * g, x.y * g, x.z * g, x.w * g), y = make_float4(y.x * g, y.y * g, y.z * g, y.w * g);
-    write4<FORM>(a, at_row, d, x, o);
-    write4<FORM>(a, at_row, d + 4, y, o);
-    return;
-  }
   const float v[8] = {x.x * g, x.y * g, x.z * g, x.w * g, y.x * g, y.y * g, y.z * g, y.w * g};
-  *reinterpret_cast<uint4*>(a.out.p + at_row + d * 2) = a.q_f16 ? pack8(v, __half()) : pack8(v, __nv_bfloat16());
-}
-
-// One row of one block's keys [from, to), by a warp, four keys at a time: lane i holds dimensions 4 i .. 4 i + 3. It may take
-// longer than a wait's bound, so it tells the waits that it goes on.
-template <int FMT, bool QF16>
-__device__ __noinline__ void slow_row(const AttendArgs& a, int first, int head, int tok, int qh, int from, int to,
-                                      volatile long long* progress, float4* acc, float* top, float* sum) {
-  using T = Tc<FMT, QF16>;
-  const int lane = threadIdx.x & 31, D = a.head_dim;
-  const bool has = lane * 4 < D;
-  auto four = [](uint2 u, bool f16) {
-    if (!f16)
-      return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                         __uint_as_float(u.y & 0xffff0000u));
-    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&u.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&u.y));
-    return make_float4(x.x, x.y, y.x, y.y);
-  };
-  auto cached4 = [&](const unsigned char* pool, const float* scales, int64_t row) {
-    if constexpr (T::kEight) {
-      uint2 u;
-      widen4<FMT>(*reinterpret_cast<const uint32_t*>(pool + row * D + lane * 4), u.x, u.y);
-      const float4 x = four(u, true);
-      const float f = scales[row];
-      return make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
-    } else {
-      return four(*reinterpret_cast<const uint2*>(pool + row * D * 2 + lane * 8), FMT == LACACHE_KV_F16);
-    }
-  };
-  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-  const unsigned char* q_row = a.q.at((int64_t)first * a.new_tokens + tok, qh);
-  const float4 q = has ? four(*reinterpret_cast<const uint2*>(q_row + lane * 8), QF16) : zero;
-  float m = -INFINITY, l = 0.f;
-  float4 o = zero;
-  for (int j = from & ~3; j < to; j += 4) {
-    if (lane == 0) *progress = clock64();
-    const int index = (int)(((uint64_t)(uint32_t)(j >> 4) * a.page_mul) >> a.page_shift);
-    const int page = a.table.pages[first * a.table.stride + index];
-    if ((unsigned)page >= (unsigned)a.pages) continue;
-    const int64_t row = page * a.page_rows + (int64_t)head * a.page_size + (j - index * a.page_size);
-    float4 k[4], v[4];
-    float s[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool in = has && j + e >= from && j + e < to;
-      k[e] = in ? cached4(a.pk, a.ks, row + e) : zero;
-      v[e] = in ? cached4(a.pv, a.vs, row + e) : zero;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] = has ? q.x * k[e].x + q.y * k[e].y + q.z * k[e].z + q.w * k[e].w : 0.f;
-#pragma unroll
-    for (int x = 16; x; x >>= 1) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += __shfl_xor_sync(0xffffffffu, s[e], x);
-    }
-    float now = m;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      s[e] = j + e >= from && j + e < to ? s[e] * (a.scale * 1.4426950408889634f) : -INFINITY;
-      now = fmaxf(now, s[e]);
-    }
-    const float base = now == -INFINITY ? 0.f : now, f = exp2_fast(m - base);
-    l *= f, o.x *= f, o.y *= f, o.z *= f, o.w *= f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float p = exp2_fast(s[e] - base);
-      l += p, o.x += p * v[e].x, o.y += p * v[e].y, o.z += p * v[e].z, o.w += p * v[e].w;
-    }
-    m = now;
-  }
-  *acc = o;
-  *top = m;
-  *sum = l;
+  if constexpr (FORM != kWhole) store8(a.part + at_row / 4 + d, v);
+  else *reinterpret_cast<uint4*>(a.out.p + at_row + d * 2) = a.q_f16 ? pack8(v, __half()) : pack8(v, __nv_bfloat16());
 }
 
 template <int FMT, bool QF16, int FORM = kWhole>
@@ -325,6 +109,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     return;
   }
   const uint32_t ring = base;
+  pass_begins<FORM>();
   Tail& t = *reinterpret_cast<Tail*>(gbase + T::kTail);
   volatile uint32_t* abort_flag = &t.abort_flag;
   volatile long long* progress = &t.progress;
@@ -333,14 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   const int row_bytes = T::kEight ? D : D * 2;                    // of the cache
   const int slot_floats = kTile * (a.padded + 2);   // of a.partial
 
-  auto by_group = [&](int row) {   // row / group (a group of sequences may have rows past the multiplication's range)
-    return FORM == kCommon ? row / a.group : a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_mul);
-  };
-  auto tiles_of = [&](const Walk<FORM>& w) { return FORM == kCommon ? w.sp.tiles : a.row_tiles; };
-  auto live_of = [&](const Walk<FORM>& w, int row0) {
-    return FORM == kCommon ? min(w.sp.rows - row0, kTile) : min(a.rows - row0, a.tile_rows);
-  };
-  const int tile_rows = FORM == kCommon ? kTile : a.tile_rows;
+  auto by_group = [&](int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_mul); };   // row / group
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders / 32 : kLoaders + 1);
@@ -358,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     t.pending[0][2] = t.pending[1][2] = -1;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  Walk<FORM> walk;
+  Walk<FORM, kCost, kTile> walk;
   Line line;
   if (!start_walk(a, walk, line)) return;
   if (warp == kMmaWarp) {
@@ -430,8 +208,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         warp_arrive(t.full[k % kSlots]);
       };
       for (; ok && !walk.done(); walk.next(a)) {
-        const int head = walk.triple / tiles_of(walk), count = walk.units();
-        const int32_t* table_row = a.table.pages + first_of<FORM>(walk.seq, walk.sp) * a.table.stride;
+        const int head = walk.triple / a.row_tiles, count = walk.units();
+        const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
         const int64_t head_row = (int64_t)head * a.page_size;
         int key = (walk.sp.lo & ~15) + walk.first_unit * kTile;
         auto look_up = [&](int from) {
@@ -495,8 +273,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
 #pragma unroll
     for (int i = 0; i < 4; ++i) place[i] = unit_at((wide ? 2 : 4) * i + own_row, own_unit);
     for (; ok && !walk.done(); walk.next(a)) {
-      const int head = walk.triple / tiles_of(walk), count = walk.units();
-      const int32_t* table_row = a.table.pages + first_of<FORM>(walk.seq, walk.sp) * a.table.stride;
+      const int head = walk.triple / a.row_tiles, count = walk.units();
+      const int32_t* table_row = a.table.pages + walk.seq * a.table.stride;
       const unsigned char* head_k = a.pk + (int64_t)head * a.page_size * row_bytes;
       const unsigned char* head_v = a.pv + (int64_t)head * a.page_size * row_bytes;
       int key = (walk.sp.lo & ~15) + walk.first_unit * kTile;
@@ -632,13 +410,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     bool ok = true;
     // a triple's q: this thread's 64 dimensions of its row, into registers, and from there to TMEM
     uint32_t q_row[32];
-    auto load_q = [&](const Walk<FORM>& w) {
-      const int head = w.triple / tiles_of(w), row0 = (w.triple - head * tiles_of(w)) * tile_rows;
-      const int live = live_of(w, row0);
+    auto load_q = [&](const Walk<FORM, kCost, kTile>& w) {
+      const int head = w.triple / a.row_tiles, row0 = (w.triple - head * a.row_tiles) * a.tile_rows;
+      const int live = min(a.rows - row0, a.tile_rows);
       const int r = threadIdx.x & (kTile - 1), row = row0 + r, tok = by_group(row);
       const uint4* from = reinterpret_cast<const uint4*>(
-          r < live ? a.q.at((int64_t)first_of<FORM>(w.seq, w.sp) * a.new_tokens + tok, head * a.group + row - tok * a.group)
-                   : nullptr);
+          r < live ? a.q.at((int64_t)w.seq * a.new_tokens + tok, head * a.group + row - tok * a.group) : nullptr);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int u = half * 8 + i;
@@ -655,28 +432,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
     load_q(walk);
     hand_over_q();
     for (; ok && !walk.done(); walk.next(a)) {
-      const int head = walk.triple / tiles_of(walk), row0 = (walk.triple - head * tiles_of(walk)) * tile_rows;
-      const int live = live_of(walk, row0), count = walk.units(), first = first_of<FORM>(walk.seq, walk.sp);
+      const int head = walk.triple / a.row_tiles, row0 = (walk.triple - head * a.row_tiles) * a.tile_rows;
+      const int live = min(a.rows - row0, a.tile_rows), count = walk.units();
       const int r = threadIdx.x & (kTile - 1), tok = by_group(row0 + r);
       const bool mine = r < live, some = (warp & 3) * 32 < live;
-      int pos, lo = INT_MIN;
-      if constexpr (FORM == kCommon) {
-        pos = INT_MAX;
-        if (mine) {
-          const int2 seen = seen_by<FORM>(a, walk.seq, walk.sp, tok);
-          pos = seen.x, lo = seen.y;
-        }
-      } else {
-        pos = mine ? walk.sp.len - a.new_tokens + tok : INT_MAX;
-        if (mine) {
-          lo = a.starts ? a.starts[walk.seq] : 0;
-          if (a.window > 0 && pos - a.window + 1 > lo) lo = pos - a.window + 1;
-        }
+      const int pos = mine ? walk.sp.len - a.new_tokens + tok : INT_MAX;
+      int lo = INT_MIN;
+      if (mine) {
+        lo = start_of<FORM>(a, walk.seq);
+        if (a.window > 0 && pos - a.window + 1 > lo) lo = pos - a.window + 1;
       }
       const float factor = a.scale * 1.4426950408889634f;
       float m = -INFINITY, l = 0.f;
       const int key_begin = (walk.sp.lo & ~15) + walk.first_unit * kTile;
-      if (FORM != kCommon && threadIdx.x == 0) {
+      if (threadIdx.x == 0) {
         const int raw_len = a.lengths[walk.seq];
         if (raw_len < 0 || raw_len > a.max_len) atomicOr(a.status, kBadIndex);
       }
@@ -814,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       if (!ok) break;
       // with the last S of a triple complete, every product with its q is done: the next one's takes its place, while the
       // last product with V runs
-      Walk<FORM> next = walk;
+      Walk<FORM, kCost, kTile> next = walk;
       next.next(a);
       const bool more = !next.done();
       if (more) load_q(next);
@@ -842,21 +611,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         c_last = line.block_of(begin + walk.sp.units - 1);
         if (threadIdx.x == 0) {
           int* p = t.pending[(int)blockIdx.x == c_first];
-          p[0] = first, p[1] = walk.triple, p[2] = c_first, p[3] = c_last;
-          if (FORM == kCommon) p[4] = walk.sp.rows, p[5] = walk.sp.tiles;
+          p[0] = walk.seq, p[1] = walk.triple, p[2] = c_first, p[3] = c_last;
         }
       }
       float* slot = a.partial + ((int64_t)blockIdx.x * 2 + ((int)blockIdx.x == c_first ? 1 : 0)) * slot_floats;
       if (some) {
         int64_t at_lse = 0, at_row = 0;
-        if (mine) at_row = out_at<FORM>(a, first, head, row0 + r, &at_lse);
-        float inv = total == 0.f ? 0.f : 1.f / total;
-        Other other = {0.f, at_lse, FORM == kOwn && a.joined[walk.seq]};
-        if (FORM == kOwn && whole && mine) {   // (lse is written below)
-          const End end = end_of<FORM>(a, m, total, at_lse, other.joined, false);
-          inv = end.f;
-          other.weight = end.common;
-        }
+        if (mine) at_row = out_at<FORM>(a, walk.seq, head, row0 + r, &at_lse);
+        const float inv = total == 0.f ? 0.f : 1.f / total;
         // this half's dimensions: 32 of every 64 (rolled: code that runs once a triple waits for its fetch)
         float2 zero = make_float2(0.f, 0.f);   // NaN after a product that is not finite, or past kFar
 #pragma unroll 1
@@ -876,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
                 const float4 y0 = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                 const float4 y1 = make_float4(o[e + 4], o[e + 5], o[e + 6], o[e + 7]);
                 if (whole) {
-                  write8<FORM>(a, at_row, d, y0, y1, inv, other);
+                  write8<FORM>(a, at_row, d, y0, y1, inv);
                 } else {
                   reinterpret_cast<float4*>(slot)[d / 4 * kTile + r] = y0;
                   reinterpret_cast<float4*>(slot)[(d / 4 + 1) * kTile + r] = y1;
@@ -887,8 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
         }
         if (mine && half == 0) {
           if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + r * 2) = make_float2(m, total);
-          else if (FORM != kWhole) end_of<FORM>(a, m, total, at_lse, other.joined);
-          else if (a.lse) a.lse[at_lse] = lse_of(m, total);
+          else write_lse<FORM>(a, at_lse, m, total);
         }
         // a row that is not finite in either half is done again, past what both have written; not where its sum of weights
         // is NaN: then a score that it sees is (masked ones are -infinity), and NaN is its result
@@ -909,29 +670,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
           const int its_pos = __shfl_sync(0xffffffffu, pos, src), its_lo = __shfl_sync(0xffffffffu, lo, src);
           float4 acc;
           float top, sum;
-          slow_row<FMT, QF16>(a, first, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1),
+          slow_row<FMT, QF16>(a, walk.seq, head, its_tok, its_qh, max(max(key_begin, its_lo), 0), min(key_end, its_pos + 1),
                                progress, &acc, &top, &sum);
           int64_t its_lse;
-          const int64_t its_row = out_at<FORM>(a, first, head, row0 + rr, &its_lse);
-          float g = sum == 0.f ? 0.f : 1.f / sum;
-          Other its = {0.f, its_lse, other.joined};
-          if (FORM == kOwn && whole) {
-            const End end = end_of<FORM>(a, top, sum, its_lse, its.joined, false);
-            g = end.f;
-            its.weight = end.common;
-          }
+          const int64_t its_row = out_at<FORM>(a, walk.seq, head, row0 + rr, &its_lse);
           if (lane * 4 < D) {
             if (whole) {
+              const float g = sum == 0.f ? 0.f : 1.f / sum;
               write4<FORM>(a, its_row, lane * 4, sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                                                            : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g), its);
+                                                            : make_float4(acc.x * g, acc.y * g, acc.z * g, acc.w * g));
             } else {
               reinterpret_cast<float4*>(slot)[lane * kTile + rr] = acc;
             }
           }
           if (lane == 0) {
             if (!whole) *reinterpret_cast<float2*>(slot + kTile * a.padded + rr * 2) = make_float2(top, sum);
-            else if (FORM != kWhole) end_of<FORM>(a, top, sum, its_lse, its.joined);
-            else if (a.lse) a.lse[its_lse] = lse_of(top, sum);
+            else write_lse<FORM>(a, its_lse, top, sum);
           }
         }
       }
@@ -979,13 +733,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   float* joint_top = reinterpret_cast<float*>(gbase);   // [2][kTile] each, in q's place
   float* joint_inv = joint_top + 2 * kTile;
   int64_t* joint_out = reinterpret_cast<int64_t*>(joint_inv + 2 * kTile);
-  int64_t* joint_lse = joint_out + 2 * kTile;   // kOwn: its index in lse, and the common part's weight
-  float* joint_common = reinterpret_cast<float*>(joint_lse + 2 * kTile);
   auto part = [&](int k, int i) { return a.partial + ((int64_t)(t.pending[k][2] + i) * 2 + (i == 0 ? 1 : 0)) * slot_floats; };
   auto part_ml = [&](int k, int i, int r) { return __ldcg(reinterpret_cast<const float2*>(part(k, i) + kTile * a.padded) + r); };
   auto rows_of = [&](int k) {
-    const int tiles = FORM == kCommon ? t.pending[k][5] : a.row_tiles, rows = FORM == kCommon ? t.pending[k][4] : a.rows;
-    return t.pending[k][2] < 0 ? 0 : min(rows - t.pending[k][1] % tiles * tile_rows, tile_rows);
+    return t.pending[k][2] < 0 ? 0 : min(a.rows - t.pending[k][1] % a.row_tiles * a.tile_rows, a.tile_rows);
   };
   const int rows0 = rows_of(0), rows1 = rows_of(1);
   for (int x = threadIdx.x; x < rows0 + rows1; x += kThreads) {
@@ -1004,20 +755,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       for (int e = 0; e < 8; ++e) sum += exp2_fast(y[e].x - to) * y[e].y;
       top = now;
     }
-    const int tiles = FORM == kCommon ? t.pending[k][5] : a.row_tiles;
-    const int head = t.pending[k][1] / tiles, row0 = (t.pending[k][1] - head * tiles) * tile_rows;
+    const int head = t.pending[k][1] / a.row_tiles, row0 = (t.pending[k][1] - head * a.row_tiles) * a.tile_rows;
     int64_t at_lse;
     joint_out[x] = out_at<FORM>(a, t.pending[k][0], head, row0 + r, &at_lse);
     joint_top[x] = top == -INFINITY ? 0.f : top;
-    if constexpr (FORM == kWhole) {
-      joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
-      if (a.lse) a.lse[at_lse] = lse_of(top, sum);
-    } else {
-      const End end = end_of<FORM>(a, top, sum, at_lse, FORM == kOwn && a.joined[t.pending[k][0]]);
-      joint_inv[x] = end.f;
-      joint_common[x] = end.common;
-      joint_lse[x] = at_lse;
-    }
+    joint_inv[x] = sum == 0.f ? 0.f : 1.f / sum;
+    write_lse<FORM>(a, at_lse, top, sum);
   }
   __syncthreads();
   // a thread joins 16 dimensions of a row at a time, from four blocks: sixteen loads in flight; neighbouring threads on
@@ -1055,10 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
       }
 #pragma unroll
       for (int v = 0; v < 4; v += 2) {
-        Other other = {0.f, 0, false};
-        if constexpr (FORM == kOwn)
-          other = Other{joint_common[x0 + r], joint_lse[x0 + r], a.joined[t.pending[k][0]] != 0};
-        write8<FORM>(a, joint_out[x0 + r], (q0 + v) * 4, acc[v], acc[v + 1], g, other);
+        write8<FORM>(a, joint_out[x0 + r], (q0 + v) * 4, acc[v], acc[v + 1], g);
       }
     }
   }
@@ -1079,12 +819,10 @@ cudaError_t launch_tc(AttendArgs a, int num_sms, cudaStream_t st) {
   a.padded = padded_dim(a.head_dim);
   a.group_mul = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);   // exact for rows x group < 2^32
   const int64_t units = ((int64_t)a.max_len + 15) / kTile + 1 + kCost;
-  const double tiles = FORM == kCommon ? (double)a.table.seqs * a.rows / kTile + a.groups : (double)a.table.seqs * a.row_tiles;
-  const double most = tiles * a.kv_heads * (double)units;
+  const double most = (double)a.table.seqs * a.kv_heads * a.row_tiles * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // cells are counted in 32 bits
   a.parts = most < (double)num_sms ? (int)most : num_sms;
-  kernel<<<a.parts, kThreads, kSmem, st>>>(a);
-  return cudaGetLastError();
+  return launch_form<FORM>(kernel, a.parts, kThreads, kSmem, a, st);
 }
 
 template <int FORM>

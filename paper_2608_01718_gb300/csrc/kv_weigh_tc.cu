@@ -16,8 +16,8 @@
 // Bound by the exponentials, one a score. Every wait is bounded (about a second): past it the block records a timeout, its roles
 // stop, copies and products in flight are drained, TMEM is freed and the block ends; lacache_kv_sync reports
 // LACACHE_ERR_DEVICE_TIMEOUT.
+#include "kv_tc.cuh"
 #include "kv_weigh.cuh"
-#include "tcgen05.cuh"
 
 namespace lc {
 namespace {
@@ -56,9 +56,9 @@ struct Weigh {
   static constexpr uint32_t kColumns = DP == 256 ? 128 : 512;    // of TMEM, 2 x kBlocks x kRows of them used
 };
 
-// Where 16-byte unit u of row r lies in an operand of ROWS rows: blocks of 64 elements, 128-byte swizzle.
+// unit_at in an operand of ROWS rows.
 template <int ROWS>
-__device__ __forceinline__ uint32_t unit_at(int r, int u) {
+__device__ __forceinline__ uint32_t unit_of(int r, int u) {
   return (uint32_t)((u >> 3) * (ROWS * 128) + r * 128 + (((u & 7) ^ (r & 7)) << 4));
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -67,13 +67,6 @@ __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint3
       "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
-}
-__device__ __forceinline__ void copies_arrive(uint64_t& bar) {   // once all of this thread's copies so far have landed
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bar)) : "memory");
-}
-__device__ __forceinline__ void warp_arrive(uint64_t& bar) {     // once, after what all of the warp's lanes did
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&bar));
 }
 
 // The tiles of rows that see any of the keys [key, key + KEYS): [first, end).
@@ -206,10 +199,10 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
               const int r = tile * 16 + j;   // of the unit
               const uint32_t dst = base + set * W::kSetBytes + (r >> 7) * (128 * DP * 2);
               if (unit8 < D / 16) {
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at<128>(r & 127, 2 * unit8)), "r"(h[0]),
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_of<128>(r & 127, 2 * unit8)), "r"(h[0]),
                              "r"(h[1]), "r"(h[2]), "r"(h[3])
                              : "memory");
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_at<128>(r & 127, 2 * unit8 + 1)), "r"(h[4]),
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + unit_of<128>(r & 127, 2 * unit8 + 1)), "r"(h[4]),
                              "r"(h[5]), "r"(h[6]), "r"(h[7])
                              : "memory");
               }
@@ -225,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
             const int j0 = (tile & 7) * 16 + own_row;
             if (in_row) {
 #pragma unroll
-              for (int i = 0; i < 16; i += kEachCopy) copy_async<16>(dst + unit_at<128>(j0 + i, own_unit), src + i * (D * 2), true);
+              for (int i = 0; i < 16; i += kEachCopy) copy_async<16>(dst + unit_of<128>(j0 + i, own_unit), src + i * (D * 2), true);
             }
           }
         }
@@ -262,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       for (int i = 0; i < kOwn; i += kEachCopy) {
         const unsigned char* src = reinterpret_cast<const unsigned char*>(
             __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(from), i + own_row));
-        if (src && in_row) copy_async<16>(dst + unit_at<W::kRows>(me * kOwn + i + own_row, own_unit), src + own_unit * 16, true);
+        if (src && in_row) copy_async<16>(dst + unit_of<W::kRows>(me * kOwn + i + own_row, own_unit), src + own_unit * 16, true);
       }
       copies_arrive(t.q_full[slot]);
       int pos = p.len - a.new_tokens + tok, lo = a.starts ? a.starts[p.seq] : 0;
