@@ -553,11 +553,12 @@ lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_k
 
 /* The same attention for sequences that have their first positions in common (a system prompt, a document), which are then read
  * once for all. Sequences bounds_dev[g] .. bounds_dev[g + 1] - 1 are group g (bounds rise within [0, seqs]; NULL: one group of
- * all sequences; a sequence may be in none), and the first lengths_dev[g] positions of all of them hold the same tokens: the
- * pages are read from the first of them, whatever the others' rows of the table name there. Lengths, starts, windows and the
- * outputs are as for lacache_kv_attend, and mean whole sequences, the common positions counted in; a sequence may end within
- * them. The result is that of lacache_kv_attend but for roundings. Bounds that do not rise, and lengths past the table, are reported
- * by lacache_kv_sync (without groups, and with the lengths cut).
+ * all sequences; a sequence may be in none), and the first lengths_dev[g] positions of all of them hold the same tokens, in the
+ * same pages or in copies: they are read from the pages of the first of them. Lengths, starts, windows and the outputs are as for
+ * lacache_kv_attend, and mean whole sequences, the common positions counted in; a sequence may end within them. The result is
+ * that of lacache_kv_attend but for roundings. Bounds that do not rise, and lengths past the table, are reported by
+ * lacache_kv_sync (and the call runs without groups, or with the lengths cut). Where the table can name no more than 64 MB of K
+ * and V in all, every sequence is read for itself, and the groups are not looked at.
  * The workspace is device memory, 16-byte aligned, of lacache_kv_attend_shared_workspace_bytes(h, seqs, groups, new_tokens,
  * q_heads) (0 for arguments outside their ranges); calls that may overlap, those of two captured graphs among them, have one each.
  * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read bounds, lengths and tables anew. */

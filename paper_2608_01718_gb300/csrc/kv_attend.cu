@@ -53,6 +53,25 @@ lacache_status attend_args(lacache_kv_t* h, int layer, const lacache_kv_table* t
   return LACACHE_OK;
 }
 
+// An attention with its outputs, by the kernel that its sizes call for.
+lacache_status launch_whole(lacache_kv_t* h, AttendArgs& a, cudaStream_t st) {
+  const lacache_kv_config& c = h->cfg;
+  cudaError_t e;
+  if (takes_tc(a.rows, a.group, c.head_dim, is_quantised(c.format))) {
+    if (h->inject_stall > 0) {
+      a.inject_stall = 1;
+      --h->inject_stall;
+    }
+    e = launch_attend_tc(a, c.format, h->num_sms, st);
+  } else switch (c.format) {
+    case LACACHE_KV_BF16: e = launch_attend_bf16(a, h->num_sms, st); break;
+    case LACACHE_KV_F16: e = launch_attend_f16(a, h->num_sms, st); break;
+    case LACACHE_KV_E4M3: e = launch_attend_e4m3(a, h->num_sms, st); break;
+    default: e = launch_attend_int8(a, h->num_sms, st); break;
+  }
+  return e == cudaErrorNotSupported ? LACACHE_ERR_UNSUPPORTED : from_cuda(e);
+}
+
 }  // namespace lc
 
 extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table,
@@ -68,19 +87,5 @@ extern "C" lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, cons
   lc::DeviceGuard guard(c.device);
   if (!guard.ok()) return LACACHE_ERR_CUDA;
   a.lse = at->lse_dev;
-  const cudaStream_t st = (cudaStream_t)cuda_stream;
-  cudaError_t e;
-  if (lc::takes_tc(a.rows, a.group, c.head_dim, lc::is_quantised(c.format))) {
-    if (h->inject_stall > 0) {
-      a.inject_stall = 1;
-      --h->inject_stall;
-    }
-    e = lc::launch_attend_tc(a, c.format, h->num_sms, st);
-  } else switch (c.format) {
-    case LACACHE_KV_BF16: e = lc::launch_attend_bf16(a, h->num_sms, st); break;
-    case LACACHE_KV_F16: e = lc::launch_attend_f16(a, h->num_sms, st); break;
-    case LACACHE_KV_E4M3: e = lc::launch_attend_e4m3(a, h->num_sms, st); break;
-    default: e = lc::launch_attend_int8(a, h->num_sms, st); break;
-  }
-  return e == cudaErrorNotSupported ? LACACHE_ERR_UNSUPPORTED : lc::from_cuda(e);
+  return lc::launch_whole(h, a, (cudaStream_t)cuda_stream);
 }

@@ -149,6 +149,7 @@ cudaError_t launch_own_f16(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_own_e4m3(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_own_int8(const AttendArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_own_tc(const AttendArgs& a, int format, int num_sms, cudaStream_t st);
+lacache_status launch_whole(lacache_kv_t* h, AttendArgs& a, cudaStream_t st);
 lacache_status attend_args(lacache_kv_t* h, int layer, const lacache_kv_table* table, int new_tokens, int q_heads, int window,
                            int dtype, float scale, const int32_t* lengths, const int32_t* starts, const lacache_rows* q,
                            AttendArgs* out);

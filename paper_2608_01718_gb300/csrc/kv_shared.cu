@@ -75,9 +75,9 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_const
   if (threadIdx.x == 0) a.spans[g] = make_int4(min(s_lo, s_hi), s_hi, first, common > 0 ? end - first : 0);
 }
 
-// ---- the join: a warp a row ----
+// ---- the join ----
 struct Join {
-  int64_t rows;             // tokens x q heads
+  int64_t rows;             // of a kv head: tokens x group
   int new_tokens, q_heads, group, head_dim, q_f16;
   int cut;                  // the common part was cut into partial sums (by kv_shared_tc_common.cu)
   int slot_rows;
@@ -92,119 +92,94 @@ struct Join {
   Rows out;
   float* lse;
 };
-constexpr int kJoinThreads = 128;
+constexpr int kJoinWarps = 8;
+constexpr double kSmall = 64e6;   // bytes of K and V
 
-__device__ __forceinline__ float4 scaled(float4 x, float f) { return make_float4(x.x * f, x.y * f, x.z * f, x.w * f); }
-__device__ __forceinline__ void add_scaled(float4& x, float4 y, float f) {
-  x.x += y.x * f, x.y += y.y * f, x.z += y.z * f, x.w += y.w * f;
-}
-
-// WIDE: heads past 128, two values of four a lane.
-template <bool WIDE>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Join a) {
-  constexpr int kValues = WIDE ? 2 : 1;
-  const int lane = threadIdx.x & 31, D = a.head_dim;
-  const int64_t x = blockIdx.x * (int64_t)(kJoinThreads / 32) + (threadIdx.x >> 5);
+// 32 rows of a kv head a block, a row a lane; each warp four of the dimensions. The common part is one row, in
+// the order of the outputs (not cut) or with four dimensions of neighbouring rows side by side, or partial sums, a block's each, in
+// that order too.
+__global__ void __launch_bounds__(kJoinWarps * 32, 4) join_kernel(const __grid_constant__ Join a) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.head_dim, head = blockIdx.y;
+  const int64_t row = blockIdx.x * (int64_t)32 + lane;   // of the kv head
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (x >= a.rows) return;
-  const int64_t token = x / a.q_heads;
-  const int qh = (int)(x - token * a.q_heads), seq = (int)(token / a.new_tokens);
-  const int g = __ldcg(a.group_of + seq);
-  auto four = [&](const float* row, int v) {
-    const int d = lane * 4 + v * 128;
-    return d < D ? __ldcg(reinterpret_cast<const float4*>(row + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
-  };
-  float4 own[kValues], common[kValues];
-#pragma unroll
-  for (int v = 0; v < kValues; ++v) {
-    own[v] = four(a.own + x * D, v);
-    common[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const bool mine = row < a.rows;
+  const int64_t token = mine ? row / a.group : 0;
+  const int qh = head * a.group + (int)(row - row / a.group * a.group), seq = (int)(token / a.new_tokens);
+  const int64_t x = token * a.q_heads + qh;              // in the outputs' order
+  const int g = mine ? __ldcg(a.group_of + seq) : 0;
+  float l = mine ? __ldcg(a.own_lse + x) : -INFINITY;    // base 2
+  // where the common part is
+  int c_first = 0, c_last = 0, r = 0;
+  float other = -INFINITY, top = -INFINITY, sum = 0.f;
+  if (g > 0 && a.cut) {
+    const int4 span = __ldcg(a.spans + g - 1);
+    const int share = __ldcg(a.line), longer = __ldcg(a.line + 1), base = __ldcg(a.line + 1 + g);
+    const int in_group = (int)(row - (int64_t)span.z * a.new_tokens * a.group);
+    const int tiles = (span.w * a.new_tokens * a.group + kCommonRows - 1) / kCommonRows;
+    const int keys = span.y - (span.x & ~15), units = keys <= 0 ? 1 : (keys + kCommonKeys - 1) / kCommonKeys;
+    const int begin = base + (head * tiles + in_group / kCommonRows) * (units + kCommonCost) + kCommonCost;
+    const int in_longer = longer * (share + 1);
+    auto block_of = [&](int cell) { return cell < in_longer ? cell / (share + 1) : longer + (cell - in_longer) / share; };
+    c_first = block_of(begin);
+    c_last = block_of(begin + units - 1);
+    r = in_group % kCommonRows;
   }
-  float l = __ldcg(a.own_lse + x);   // base 2
-  if (g > 0) {
-    // the common part: one row, or a block's partial sums each
-    float other = -INFINITY;
-    int c_first = 0, c_last = 0, r = 0;
-    if (a.cut) {
-      const int4 span = __ldcg(a.spans + g - 1);
-      const int share = __ldcg(a.line), longer = __ldcg(a.line + 1), base = __ldcg(a.line + 1 + g);
-      const int row = ((int)(token - (int64_t)span.z * a.new_tokens)) * a.group + qh % a.group;
-      const int tiles = (span.w * a.new_tokens * a.group + kCommonRows - 1) / kCommonRows;
-      const int keys = span.y - (span.x & ~15), units = keys <= 0 ? 1 : (keys + kCommonKeys - 1) / kCommonKeys;
-      const int begin = base + (qh / a.group * tiles + row / kCommonRows) * (units + kCommonCost) + kCommonCost;
-      const int in_longer = longer * (share + 1);
-      auto block_of = [&](int cell) { return cell < in_longer ? cell / (share + 1) : longer + (cell - in_longer) / share; };
-      c_first = block_of(begin);
-      c_last = block_of(begin + units - 1);
-      r = row % kCommonRows;
-    }
-    if (c_first == c_last) {
-      other = __ldcg(a.common_lse + x);
+  const int64_t slot = (int64_t)a.slot_rows * (D + 2);
+  auto part = [&](int c) { return a.partial + ((int64_t)c * 2 + (c == c_first ? 1 : 0)) * slot; };
+  const bool parts = c_first < c_last;
+  const int d = (blockIdx.z * kJoinWarps + warp) * 4, d_in = d < D ? d : 0;   // (warps past the row's end compute, and write nothing)
+  const float4 y = mine ? __ldcg(reinterpret_cast<const float4*>(a.own + x * D + d_in)) : make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [](float4& to, float4 v, float f) { to.x += v.x * f, to.y += v.y * f, to.z += v.z * f, to.w += v.w * f; };
+  if (parts) {
+    constexpr int kLoads = 6;   // in flight, of each kind
+    for (int c0 = c_first; c0 <= c_last; c0 += kLoads) {
+      float2 ml[kLoads];
+      float4 v[kLoads];
 #pragma unroll
-      for (int v = 0; v < kValues; ++v) common[v] = four(a.common + x * D, v);
-    } else {
-      const int64_t slot = (int64_t)a.slot_rows * (D + 2);
-      auto part = [&](int c) { return a.partial + ((int64_t)c * 2 + (c == c_first ? 1 : 0)) * slot; };
-      auto end = [&](int c) { return __ldcg(reinterpret_cast<const float2*>(part(c) + (int64_t)a.slot_rows * D) + r); };   // (m, l)
-      float top = -INFINITY, sum = 0.f;
-      for (int c0 = c_first; c0 <= c_last; c0 += 32) {   // (at most an SM a block)
-        const float2 y = c0 + lane <= c_last ? end(c0 + lane) : make_float2(-INFINITY, 0.f);
-        float most = y.x;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        const float now = fmaxf(top, most), to = now == -INFINITY ? 0.f : now, was = exp2_fast(top - to), w = exp2_fast(y.x - to);
-        float add = w * y.y;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) add += __shfl_xor_sync(0xffffffffu, add, o);
-        sum = sum * was + add;
-#pragma unroll
-        for (int v = 0; v < kValues; ++v) common[v] = scaled(common[v], was);
-        const int n = min(c_last - c0 + 1, 32);
-        for (int e0 = 0; e0 < n; e0 += 8) {   // eight loads in flight
-          float4 z[8][kValues];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-#pragma unroll
-            for (int v = 0; v < kValues; ++v)
-              z[e][v] = e0 + e < n ? four(part(c0 + e0 + e) + (int64_t)r * D, v) : make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float f = __shfl_sync(0xffffffffu, w, (e0 + e) & 31);
-            if (e0 + e < n) {
-#pragma unroll
-              for (int v = 0; v < kValues; ++v) add_scaled(common[v], z[e][v], f);
-            }
-          }
-        }
-        top = now;
+      for (int e = 0; e < kLoads; ++e) {
+        const float* from = part(min(c0 + e, c_last));
+        ml[e] = __ldcg(reinterpret_cast<const float2*>(from + (int64_t)a.slot_rows * D) + r);
+        v[e] = __ldcg(reinterpret_cast<const float4*>(from) + (int64_t)(d_in / 4) * a.slot_rows + r);
       }
-      other = sum == 0.f ? -INFINITY : top + log2f(sum);
+      float now = top;
 #pragma unroll
-      for (int v = 0; v < kValues; ++v)
-        common[v] = sum == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : scaled(common[v], 1.f / sum);
+      for (int e = 0; e < kLoads; ++e) now = fmaxf(now, ml[e].x);
+      const float to = now == -INFINITY ? 0.f : now, f = exp2_fast(top - to);
+      sum *= f;
+      z = make_float4(z.x * f, z.y * f, z.z * f, z.w * f);
+#pragma unroll
+      for (int e = 0; e < kLoads; ++e) {
+        if (c0 + e > c_last) continue;
+        const float w = exp2_fast(ml[e].x - to);
+        sum += w * ml[e].y;
+        add(z, v[e], w);
+      }
+      top = now;
     }
-    // both: their shares of the sum of weights (NaN, where a row sees a score that is, stays)
+    other = sum == 0.f ? -INFINITY : top + log2f(sum);
+  } else if (g > 0) {
+    other = __ldcg(a.common_lse + x);
+    z = a.cut ? __ldcg(reinterpret_cast<const float4*>(a.common) + ((int64_t)head * (D / 4) + d_in / 4) * a.rows + row)
+              : __ldcg(reinterpret_cast<const float4*>(a.common + x * D + d_in));
+  }
+  if (!mine) return;
+  // both: their shares of the sum of weights (NaN, where a row sees a score that is, stays)
+  float4 out4 = y;
+  if (g > 0) {
     const float most = fmaxf(l, other);
     if (most > -INFINITY || l != l || other != other) {
-      const float mine = exp2_fast(l - most), its = exp2_fast(other - most), both = mine + its;
-#pragma unroll
-      for (int v = 0; v < kValues; ++v) {
-        own[v] = scaled(own[v], mine / both);
-        add_scaled(own[v], common[v], its / both);
-      }
+      const float own = exp2_fast(l - most), its = exp2_fast(other - most), both = own + its, f = own / both;
+      out4 = make_float4(y.x * f, y.y * f, y.z * f, y.w * f);
+      if (!parts || sum != 0.f) add(out4, z, parts ? its / both / sum : its / both);
       l = most + log2f(both);
     }
   }
-  unsigned char* out = a.out.at(token, qh);
-#pragma unroll
-  for (int v = 0; v < kValues; ++v) {
-    const int d = lane * 4 + v * 128;
-    if (d < D)
-      *reinterpret_cast<uint2*>(out + d * 2) = a.q_f16 ? make_uint2(pack2<false>(own[v].x, own[v].y), pack2<false>(own[v].z, own[v].w))
-                                                       : make_uint2(pack2<true>(own[v].x, own[v].y), pack2<true>(own[v].z, own[v].w));
-  }
-  if (lane == 0 && a.lse) a.lse[x] = l * 0.6931471805599453f;
+  if (d < D)
+    *reinterpret_cast<uint2*>(a.out.at(token, qh) + d * 2) =
+        a.q_f16 ? make_uint2(pack2<false>(out4.x, out4.y), pack2<false>(out4.z, out4.w))
+                : make_uint2(pack2<true>(out4.x, out4.y), pack2<true>(out4.z, out4.w));
+  if (d == 0 && a.lse) a.lse[x] = l * 0.6931471805599453f;
 }
 
 struct Workspace {
@@ -278,6 +253,15 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
   lc::DeviceGuard guard(c.device);
   if (!guard.ok()) return LACACHE_ERR_CUDA;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
+  const bool eight = lc::is_quantised(c.format);
+  // What the table can name at most, read for every sequence, against four kernels: two sequences of 340 tokens of 8 heads (d = 64,
+  // bf16, 1.4 MB) take 6.5 us so and 19.6 in parts. 64 MB are some 12 us more.
+  const double bytes = 2.0 * table->seqs * a.max_len * c.kv_heads * c.head_dim * (eight ? 1 : 2);
+  if (bytes <= lc::kSmall) {
+    a.out = j.out;
+    a.lse = at->lse_dev;
+    return lc::launch_whole(h, a, st);
+  }
   unsigned char* ws = static_cast<unsigned char*>(workspace_dev);
   auto floats = [&](size_t at_byte) { return reinterpret_cast<float*>(ws + at_byte); };
   auto ints = [&](size_t at_byte) { return reinterpret_cast<int32_t*>(ws + at_byte); };
@@ -297,7 +281,6 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
   g.status = a.status;
   lc::group_kernel<<<shared->groups, lc::kGroupThreads, 0, st>>>(g);
   cudaError_t e = cudaGetLastError();
-  const bool eight = lc::is_quantised(c.format);
   // the sequences' own positions
   lc::AttendArgs own = a;
   own.starts = g.own_starts;
@@ -326,7 +309,7 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
     e = lc::launch_common(a, c.format, h->num_sms, st);
   }
   if (e != cudaSuccess) return e == cudaErrorNotSupported ? LACACHE_ERR_UNSUPPORTED : LACACHE_ERR_CUDA;
-  j.rows = (int64_t)table->seqs * a.new_tokens * a.q_heads;
+  j.rows = (int64_t)table->seqs * a.rows;
   j.new_tokens = a.new_tokens;
   j.q_heads = a.q_heads;
   j.group = a.group;
@@ -343,16 +326,14 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
   j.common_lse = a.part_lse;
   j.partial = a.partial;
   j.lse = at->lse_dev;
-  const int64_t blocks = (j.rows + lc::kJoinThreads / 32 - 1) / (lc::kJoinThreads / 32);
-  if (blocks > INT32_MAX) return LACACHE_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(lc::kJoinThreads);
+  cfg.gridDim = dim3((unsigned)((j.rows + 31) / 32), (unsigned)c.kv_heads, (unsigned)((c.head_dim / 4 + lc::kJoinWarps - 1) / lc::kJoinWarps));
+  cfg.blockDim = dim3(lc::kJoinWarps * 32);
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return lc::from_cuda(cudaLaunchKernelEx(&cfg, c.head_dim > 128 ? lc::join_kernel<true> : lc::join_kernel<false>, j));
+  return lc::from_cuda(cudaLaunchKernelEx(&cfg, lc::join_kernel, j));
 }

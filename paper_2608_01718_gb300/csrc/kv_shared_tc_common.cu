@@ -8,11 +8,10 @@
 // S of 128 columns and two O of up to 128 fill it).
 //
 // One block an SM, warp-specialised:
-//   warps 9-15 (loaders): the tiles of K and V, in turn, into a ring of slots in the 128-byte swizzle layout: 16-bit rows by
+//   warps 10 and 11, or to 15 (loaders): the tiles of K and V, in turn, into a ring of slots in the 128-byte swizzle layout: 16-bit rows by
 //     cp.async (found through the page table; positions past the common ones are zeros), 8-bit codes through registers, a slot
 //     ahead, widened exactly (keys to q's type, values to bf16), with their scales beside them;
-//   warp 8 (MMA): S of the second tile of rows, O of the first, S of the first one unit ahead, O of the second, each as soon as
-//     what it needs is there;
+//   warps 8 and 9 (MMA), a tile of rows each: S of a unit, then O += P V as soon as its weights are there;
 //   warps 0-7 (softmax, a thread a row): a triple's q into shared memory; base-2 softmax by a reference that seldom moves, the
 //     scores read from TMEM twice (for the maximum, and for the weights, which overwrite them 32 keys at a time); for f16 caches
 //     weights in f16, else in two bf16 terms, as in kv_attend_tc.cu, whose treatment of values that are not finite is used too.
@@ -30,27 +29,29 @@ namespace {
 constexpr int kRows = kCommonRows;           // of q a block
 static_assert(kRows == 2 * kTile && kCommonKeys == kTile, "two tiles of rows");
 constexpr int kSoftmax = 256;                // threads: one a row
-constexpr int kMmaWarp = 8;
-constexpr int kLoaders = 7;                  // warps
-constexpr int kThreads = kSoftmax + 32 + 32 * kLoaders;
+constexpr int kMmaWarp = 8;                  // and 9: one a tile of rows
 constexpr int kCost = kCommonCost;           // a triple's start and end, in units
 
 template <int FMT, bool QF16, int DP>
 struct Common {
   static constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
   static constexpr bool kSplit = FMT != LACACHE_KV_F16;    // bf16 weights, in two terms
+  static constexpr int kLoaders = 6;                       // warps
+  static constexpr int kThreads = kSoftmax + 64 + 32 * kLoaders;
   static constexpr int kSlotBytes = kTile * DP * 2;
   static constexpr int kSlots = DP == 64 ? 8 : kEight ? 4 : 5;
   struct Tail {
     uint64_t full[8], empty[8];                // a slot's tile is there; its products are done
     uint64_t q_full[2], s_full[2], p_full[2];  // of each tile of rows: a triple's q is there; an S is complete; its weights are stored
     uint64_t pv_done[2], o_empty[2];           // their product is done; a triple's O has been read
+    uint64_t turn[2];                          // a tile of rows may make its weights: the other has
     uint64_t drain;
     long long progress;                        // clock64() of a warp at work on a row key by key: the waits' second counts from it
     uint32_t tmem;
     uint32_t abort_flag;
     uint32_t bad[16];                          // a unit's 16-key tiles whose page id is no page (by unit modulo 16)
-    alignas(16) float scales[kEight ? 8 * 2 * kTile : 4];   // 8-bit caches: a unit's scales of K, then of V (by unit modulo 8)
+    alignas(16) float scales[kEight ? 8 * 2 * kTile : 4];   // 8-bit caches: a unit's scales of K times scale log2(e), then of V (by
+                                                            // unit modulo 8)
   };
   static constexpr int kQ = kSlots * kSlotBytes;           // offsets in shared memory
   static constexpr int kTail = kQ + 2 * kSlotBytes;
@@ -68,12 +69,12 @@ __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint3
 }
 
 template <int FMT, bool QF16, int DP>
-__global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_kernel(const __grid_constant__ AttendArgs a) {
   using T = Common<FMT, QF16, DP>;
   using Tail = typename T::Tail;
   using Place = Walk<kCommon, kCost, kRows>;
   constexpr bool kSplit = T::kSplit;
-  constexpr int kSlots = T::kSlots;
+  constexpr int kSlots = T::kSlots, kLoaders = T::kLoaders;
   extern __shared__ __align__(1024) unsigned char gbase[];
   const uint32_t base = smem_u32(gbase);
   // (launched beside the pass over the sequences' own positions, once all of its blocks know that the groups are known)
@@ -91,16 +92,17 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(smem_u32(&t.full[s]), T::kEight ? kLoaders : 32 * kLoaders + 1);
-      mbar_init(smem_u32(&t.empty[s]), 1);
+      mbar_init(smem_u32(&t.empty[s]), 2);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(smem_u32(&t.q_full[b]), 4);
+      mbar_init(smem_u32(&t.q_full[b]), kSoftmax / 2);
       mbar_init(smem_u32(&t.s_full[b]), 1);
       mbar_init(smem_u32(&t.p_full[b]), 4);
       mbar_init(smem_u32(&t.pv_done[b]), 1);
       mbar_init(smem_u32(&t.o_empty[b]), 4);
+      mbar_init(smem_u32(&t.turn[b]), 4);
     }
-    mbar_init(smem_u32(&t.drain), 1);
+    mbar_init(smem_u32(&t.drain), 2);
     t.progress = 0;
     t.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -148,9 +150,9 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
   auto has_two = [&](const Place& w) { return w.sp.rows - row0_of(w) > kTile; };
   auto page_index = [&](int at) { return (int)(((uint64_t)(uint32_t)(at >> 4) * a.page_mul) >> a.page_shift); };
 
-  if (warp > kMmaWarp) {
+  if (warp > kMmaWarp + 1) {
     // ---- loaders ----
-    const int me = warp - kMmaWarp - 1;
+    const int me = warp - kMmaWarp - 2;
     bool ok = true;
     if (a.inject_stall && walk.seq_base + walk.triple + walk.first_unit == 0) walk.left = 0;
     // the units of this block, one after another, with the page ids of each (lane i < 8: of its i-th 16 keys), and of the next
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
       }
     };
     if constexpr (T::kEight) {
-      // a warp's 16-key tiles of a slot (the n-th): one, or two in every seventh; their codes are loaded a slot ahead
+      // a warp's one or two 16-key tiles of a slot (the n-th); their codes are loaded a slot ahead
       constexpr int kLanes = DP / 16, kRowsLoad = 32 / kLanes, kLoads = 16 / kRowsLoad;   // lanes a row; rows a load; loads a tile
       const int unit = lane % kLanes, row = lane / kLanes;
       struct Codes {
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
           }
           const int j = first + (lane & 15);
           const bool in = there && !is_v && j >= u.w.sp.lo && j < u.w.sp.hi;
-          c.scale[e] = in ? __ldg((lane < 16 ? a.ks : a.vs) + from + (lane & 15)) : 0.f;
+          c.scale[e] = in ? __ldg((lane < 16 ? a.ks : a.vs) + from + (lane & 15)) * (lane < 16 ? a.scale * 1.4426950408889634f : 1.f) : 0.f;
         }
       };
       auto store = [&](int n, const Codes& c) {
@@ -255,18 +257,22 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
           }
         }
       };
-      Codes now, next;
-      if (!at.done) load(at, 0, now);
-      for (int n = 0; ok && !at.done; ++n) {
-        if (me == 0 && !(n & 1)) note_bad(n / 2);
-        if (n & 1) step(at);
-        if (!at.done) load(at, n + 1, next);
+      auto finish = [&](int n, const Codes& c) {
         if (n >= kSlots) ok = wait(t.empty[n % kSlots], (n / kSlots - 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        store(n, now);
+        if (!ok) return;
+        store(n, c);
         warp_arrive(t.full[n % kSlots]);
-        now = next;
+      };
+      Codes of_k, of_v;
+      if (!at.done) load(at, 0, of_k);
+      for (int n = 0; ok && !at.done; n += 2) {
+        if (me == 0) note_bad(n / 2);
+        load(at, n + 1, of_v);
+        finish(n, of_k);
+        step(at);
+        if (!at.done) load(at, n + 2, of_k);
+        if (ok) finish(n + 1, of_v);
       }
     } else {
       const int row_bytes = D * 2;
@@ -305,110 +311,91 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
       }
     }
     copy_wait<0>();
-  } else if (warp == kMmaWarp) {
-    // ---- MMA ----
+  } else if (warp >= kMmaWarp) {
+    // ---- MMA: a warp a tile of rows ----
+    const int b = warp - kMmaWarp;
     const uint32_t bf16 = (1u << 7) | (1u << 10);   // both operands' type; f16 is 0
     const uint32_t qk = (1u << 4) | (QF16 ? 0u : bf16) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
     const uint32_t pv = (1u << 4) | (kSplit ? bf16 : 0u) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
-    struct Unit {
-      bool there, first, two;
-    };
-    int left_in_triple = 0;
-    bool two = false;
-    auto fetch = [&] {   // the next unit of the walk
-      Unit u = {false, false, two};
-      if (left_in_triple == 0) {
-        if (walk.done()) return u;
-        left_in_triple = walk.units();
-        u.two = two = has_two(walk);
-        u.first = true;
-        walk.next(a);
-      }
-      --left_in_triple;
-      u.there = true;
-      return u;
-    };
+    const uint32_t s_to = tmem + T::kS + b * kTile, o_to = tmem + T::kO + b * kTile;
     bool ok = true;
-    int units[2] = {0, 0}, triples[2] = {0, 0};   // of a tile of rows: S issued, and triples begun
-    // S of tile of rows b, unit j of the block
-    auto first_product = [&](int b, int j, const Unit& u, bool last_use) {
-      const int slot = (2 * j) % kSlots, k = units[b];
-      ok = ok && (k == 0 || wait(t.pv_done[b], (k - 1) & 1)) && (!u.first || wait(t.q_full[b], triples[b] & 1)) &&
-           wait(t.full[slot], ((2 * j) / kSlots) & 1);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the loaders' and the softmax's writes)
-      tc_fence_after();
-      const uint64_t q_desc = smem_desc(base + T::kQ + b * T::kSlotBytes), k_desc = smem_desc(base + slot * T::kSlotBytes);
-      if (elect_one()) {
-#pragma unroll 1
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint64_t at = (uint64_t)((kk >> 2) * (kBlockBytes >> 4) + (kk & 3) * 2);
-          mma_ss(tmem + T::kS + b * kTile, q_desc + at, k_desc + at, qk, kk ? 1u : 0u);
-        }
-        if (last_use) mma_commit<false>(smem_u32(&t.empty[slot]), 0);
-        mma_commit<false>(smem_u32(&t.s_full[b]), 0);
+    int j = 0, k = 0, triples = 0;   // units of the block, units and triples of this tile of rows
+    for (; ok && !walk.done(); walk.next(a)) {
+      const int count = walk.units();
+      const bool two = has_two(walk);
+      if (b == 1 && !two) {
+        j += count;
+        continue;
       }
-      __syncwarp();
-      ++units[b];
-      if (u.first) ++triples[b];
-    };
-    // O (+)= P V of tile of rows b, unit j of the block (the k-th of the tile of rows)
-    auto second_product = [&](int b, int j, int k, const Unit& u, int triple, bool last_use) {
-      const int slot = (2 * j + 1) % kSlots;
-      ok = ok && wait(t.full[slot], ((2 * j + 1) / kSlots) & 1) && wait(t.p_full[b], k & 1) &&
-           (!u.first || triple == 0 || wait(t.o_empty[b], (triple - 1) & 1));
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      tc_fence_after();
-      const uint32_t v = base + slot * T::kSlotBytes;
-      if (elect_one()) {
-#pragma unroll 1
-        for (int kk = 0; kk < kTile / 16; ++kk) {
-          const uint64_t v_desc = smem_desc_mn(v + kk * 2048);
-          const uint32_t p = tmem + T::kS + b * kTile + (kk >> 1) * 32 + (kk & 1) * 8;
-          mma_ts(tmem + T::kO + b * kTile, p, v_desc, pv, u.first && kk == 0 ? 0u : 1u);
-          if (kSplit) mma_ts(tmem + T::kO + b * kTile, p + 16, v_desc, pv, 1u);
+      for (int i = 0; ok && i < count; ++i, ++j, ++k) {
+        // S, once the product with its last weights, which lie there, is done
+        const int k_slot = (2 * j) % kSlots, v_slot = (2 * j + 1) % kSlots;
+        ok = (k == 0 || wait(t.pv_done[b], (k - 1) & 1)) && (i > 0 || wait(t.q_full[b], triples & 1)) &&
+             wait(t.full[k_slot], ((2 * j) / kSlots) & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the loaders' and the softmax's writes)
+        tc_fence_after();
+        const uint64_t q_desc = smem_desc(base + T::kQ + b * T::kSlotBytes), k_desc = smem_desc(base + k_slot * T::kSlotBytes);
+        if (elect_one()) {
+          // (unrolled, all under one election: 56 to 78 cycles a product of 128 x 128 x 16, 64 of them the tensor core's; rolled 92,
+          // an election each 143)
+#pragma unroll
+          for (int kk = 0; kk < DP / 16; ++kk) {
+            const uint64_t at = (uint64_t)((kk >> 2) * (kBlockBytes >> 4) + (kk & 3) * 2);
+            if (kk < D / 16) mma_ss(s_to, q_desc + at, k_desc + at, qk, kk ? 1u : 0u);
+          }
+          mma_commit<false>(smem_u32(&t.s_full[b]), 0);
+          mma_commit<false>(smem_u32(&t.empty[k_slot]), 0);
+          if (!two) mma_commit<false>(smem_u32(&t.empty[k_slot]), 0);   // (for the other tile, which is empty)
         }
-        if (last_use) mma_commit<false>(smem_u32(&t.empty[slot]), 0);
-        mma_commit<false>(smem_u32(&t.pv_done[b]), 0);
+        __syncwarp();
+        // O (+)= P V
+        ok = wait(t.full[v_slot], ((2 * j + 1) / kSlots) & 1) && (i > 0 || triples == 0 || wait(t.o_empty[b], (triples - 1) & 1)) &&
+             wait(t.p_full[b], k & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tc_fence_after();
+        const uint64_t v_desc = smem_desc_mn(base + v_slot * T::kSlotBytes);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk) {
+            const uint32_t p = s_to + (kk >> 1) * 32 + (kk & 1) * 8;
+            mma_ts(o_to, p, v_desc + kk * (2048 >> 4), pv, kk || i ? 1u : 0u);
+            if (kSplit) mma_ts(o_to, p + 16, v_desc + kk * (2048 >> 4), pv, 1u);
+          }
+          mma_commit<false>(smem_u32(&t.pv_done[b]), 0);
+          mma_commit<false>(smem_u32(&t.empty[v_slot]), 0);
+          if (!two) mma_commit<false>(smem_u32(&t.empty[v_slot]), 0);
+        }
+        __syncwarp();
       }
-      __syncwarp();
-    };
-    Unit now = fetch();
-    if (now.there) first_product(0, 0, now, !now.two);
-    for (int j = 0; ok && now.there; ++j) {
-      const Unit next = fetch();
-      const int k0 = units[0] - 1, triple0 = triples[0] - 1;
-      if (now.two) first_product(1, j, now, true);
-      const int k1 = units[1] - 1, triple1 = triples[1] - 1;
-      if (ok) second_product(0, j, k0, now, triple0, !now.two);
-      if (ok && next.there) first_product(0, j + 1, next, !next.two);
-      if (ok && now.two) second_product(1, j, k1, now, triple1, true);
-      now = next;
+      ++triples;
     }
   } else {
     // ---- softmax: a thread a row ----
     const int b = warp >> 2, r = threadIdx.x & (kTile - 1);
     const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);   // this warp's 32 lanes
     const uint32_t s_at = lanes + T::kS + b * kTile, o_at = lanes + T::kO + b * kTile;
-    int j = 0, k = 0;   // units of the block, and of this tile of rows
+    int j = 0, k = 0, turns = 0;   // units of the block, of this tile of rows, and of those with two
     bool ok = true;
-    // the triple's q: this thread's row
+    // the triple's q: 32 rows a warp, whole rows at a time
     auto hand_over_q = [&](const Place& w) {
-      const int head = w.triple / w.sp.tiles, row = row0_of(w) + b * kTile + r, tok = row / a.group;
-      const bool live = row < w.sp.rows;
-      const uint4* from = reinterpret_cast<const uint4*>(
-          live ? a.q.at((int64_t)w.sp.first * a.new_tokens + tok, head * a.group + row - tok * a.group) : nullptr);
+      constexpr int kLanes = DP / 8, kRowsCopy = 32 / kLanes;
+      const int r0 = (warp & 3) * 32, its = row0_of(w) + b * kTile + r0 + lane, tok = its / a.group, head = w.triple / w.sp.tiles;
+      const unsigned char* from =
+          its < w.sp.rows ? a.q.at((int64_t)w.sp.first * a.new_tokens + tok, head * a.group + its - tok * a.group) : nullptr;
+      const int unit = lane % kLanes;
       const uint32_t to = base + T::kQ + b * T::kSlotBytes;
-#pragma unroll 4
-      for (int u = 0; u < units_row; ++u) {
-        const uint4 x = live ? from[u] : make_uint4(0, 0, 0, 0);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + unit_at(r, u)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w)
-                     : "memory");
+#pragma unroll
+      for (int i = 0; i < 32; i += kRowsCopy) {
+        const int row = i + lane / kLanes;
+        const unsigned char* src = reinterpret_cast<const unsigned char*>(
+            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(from), row));
+        if (unit < units_row) copy_async<16>(to + unit_at(r0 + row, unit), src ? src + unit * 16 : a.pk, src != nullptr);   // (no row: zeros)
       }
-      warp_arrive(t.q_full[b]);
+      copies_arrive(t.q_full[b]);
     };
     auto takes_part = [&](const Place& w) { return b == 0 || has_two(w); };
     if (takes_part(walk)) hand_over_q(walk);
@@ -421,6 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
         continue;
       }
       if (!handed) hand_over_q(walk);   // (the triple before had no rows here)
+      const bool two = has_two(walk);
       const int head = walk.triple / walk.sp.tiles, row = row0_of(walk) + b * kTile + r, tok = row / a.group;
       const bool mine = row < walk.sp.rows, some = row - lane < walk.sp.rows;
       int pos = INT_MAX, lo = INT_MIN;
@@ -429,34 +417,31 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
         pos = seen.x, lo = seen.y;
       }
       const float factor = a.scale * 1.4426950408889634f;
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f, seen_top = -INFINITY;   // (of the unit before)
       for (int i = 0; i < count; ++i, ++j, ++k) {
         const int key = key_begin + i * kTile;
-        ok = wait(t.s_full[b], k & 1);
+        // the tiles make their weights in turn, so that the products of one run beside the other's softmax
+        ok = wait(t.s_full[b], k & 1) && (!two || (b == 0 && turns == 0) || wait(t.turn[b], (b ? turns : turns - 1) & 1));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (some) {
           tc_fence_after();
           const uint32_t bad = t.bad[j & 15];
-          const bool ordered = factor > 0.f, masked = !__all_sync(0xffffffffu, bad == 0 && key >= lo && key + kTile - 1 <= pos);
-          const float* k_scale = t.scales + (j & 7) * 2 * kTile;
-          // 32 scores (times the factor, where the products' order is not theirs), -infinity where not seen
-          auto scores = [&](int c, float (&x)[32]) {
-            uint32_t(&u)[32] = reinterpret_cast<uint32_t(&)[32]>(x);
+          const bool masked = !__all_sync(0xffffffffu, bad == 0 && key >= lo && key + kTile - 1 <= pos);
+          const float* scales = t.scales + (j & 7) * 2 * kTile;
+          // 32 scores less `shift`, -infinity where not seen
+          auto scores = [&](int c, uint32_t (&u)[32], float shift) {
+            float (&x)[32] = reinterpret_cast<float(&)[32]>(u);
             tmem_ld32_issue(s_at + c * 32, u);
             tmem_ld32_wait(u);
-            if constexpr (T::kEight) {
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 k4 = *reinterpret_cast<const float4*>(k_scale + c * 32 + e);
-                const float2 p = mul_two(make_float2(x[e], x[e + 1]), make_float2(k4.x, k4.y));
-                const float2 q = mul_two(make_float2(x[e + 2], x[e + 3]), make_float2(k4.z, k4.w));
-                x[e] = p.x, x[e + 1] = p.y, x[e + 2] = q.x, x[e + 3] = q.y;
-              }
-            }
-            if (!ordered) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) x[e] *= factor;
+            for (int e = 0; e < 32; e += 4) {
+              float4 by = make_float4(factor, factor, factor, factor);
+              if constexpr (T::kEight) by = *reinterpret_cast<const float4*>(scales + c * 32 + e);   // (times the factor)
+              const float2 less = make_float2(-shift, -shift);
+              const float2 p = fma_two(make_float2(x[e], x[e + 1]), make_float2(by.x, by.y), less);
+              const float2 q = fma_two(make_float2(x[e + 2], x[e + 3]), make_float2(by.z, by.w), less);
+              x[e] = p.x, x[e + 1] = p.y, x[e + 2] = q.x, x[e + 3] = q.y;
             }
             if (masked) {
               const int at = key + c * 32;
@@ -466,63 +451,82 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
                 if (e < first || e > last || (bad >> (c * 2 + e / 16) & 1)) x[e] = -INFINITY;
             }
           };
-          const float by = ordered ? factor : 1.f;
-          float top = -INFINITY;
+          // The reference. bf16 weights have fp32's range, so only a triple's first unit needs its maximum before its weights: a
+          // later one's moves the reference for the units after it (and what overflows all the same is not finite: done again).
+          // f16 weights need each unit's.
+          auto move_to = [&](float top) {
+            const bool move = m == -INFINITY ? top > -INFINITY : top > m + kHeadroom;
+            if (i > 0 && __any_sync(0xffffffffu, move)) {
+              const float f = move ? exp2_fast(m - (top - kBelow)) : 1.f;
+              l *= f;
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            float x[32];
-            scores(c, x);
+              for (int d = 0; d < D; d += 32) {   // (the last product into O is done: this S was begun after it)
+                uint32_t o[32];
+                tmem_ld32_issue(o_at + d, o);
+                tmem_ld32_wait(o);
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) top = max_three(top, x[e], x[e + 1]);
-          }
-          top *= by;
-          const bool move = m == -INFINITY ? top > -INFINITY : top > m + kHeadroom;
-          const float f = move ? exp2_fast(m - (top - kBelow)) : 1.f;
-          if (move) {
-            l *= f;
-            m = top - kBelow;
-          }
-          if (i > 0 && __any_sync(0xffffffffu, move)) {   // (the last product into O is done: this S was begun after it)
-#pragma unroll 1
-            for (int d = 0; d < D; d += 32) {
-              uint32_t o[32];
-              tmem_ld32_issue(o_at + d, o);
-              tmem_ld32_wait(o);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st32(o_at + d, o);
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tmem_st32(o_at + d, o);
+              }
             }
+            if (move) m = top - kBelow;
+          };
+          if (i == 0 || !kSplit) {
+            float top = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              uint32_t u[32];
+              scores(c, u, 0.f);
+              const float (&x)[32] = reinterpret_cast<const float(&)[32]>(u);
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) top = max_three(top, x[e], x[e + 1]);
+            }
+            move_to(top);
+          } else {
+            move_to(seen_top);
           }
           const float shift = m == -INFINITY ? 0.f : m;
           float2 sum[2] = {};
+          float tops[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
           for (int c = 0; c < 4; ++c) {
-            float x[32];
-            scores(c, x);
+            uint32_t u[32];
+            scores(c, u, shift);
+            const float (&y)[32] = reinterpret_cast<const float(&)[32]>(u);
             uint32_t hi[16], lo_term[kSplit ? 16 : 1];
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              const float2 y = fma_two(make_float2(x[e], x[e + 1]), make_float2(by, by), make_float2(-shift, -shift));
-              float2 p = make_float2(exp2_fast(y.x), exp2_fast(y.y));
-              sum[e / 2 & 1] = add_two(sum[e / 2 & 1], p);
-              if constexpr (T::kEight)   // (a token that this row does not see but whose scale is NaN: the row is done again)
-                p = mul_two(p, *reinterpret_cast<const float2*>(k_scale + kTile + c * 32 + e));
-              const uint32_t h = pack2<kSplit>(p.x, p.y);
-              hi[e / 2] = h;
-              if constexpr (kSplit) {
-                const float2 rest = fma_two(make_float2(__uint_as_float(h << 16), __uint_as_float(h & 0xffff0000u)),
-                                            make_float2(-1.f, -1.f), p);
-                lo_term[e / 2] = pack2<true>(rest.x, rest.y);
+            for (int e = 0; e < 32; e += 4) {
+              float4 vs;
+              if constexpr (T::kEight) vs = *reinterpret_cast<const float4*>(scales + kTile + c * 32 + e);
+#pragma unroll
+              for (int x = 0; x < 4; x += 2) {
+                if (kSplit) tops[x / 2] = max_three(tops[x / 2], y[e + x], y[e + x + 1]);
+                float2 p = make_float2(exp2_fast(y[e + x]), exp2_fast(y[e + x + 1]));
+                sum[x / 2] = add_two(sum[x / 2], p);
+                if constexpr (T::kEight)   // (a token that this row does not see but whose scale is NaN: the row is done again)
+                  p = mul_two(p, x ? make_float2(vs.z, vs.w) : make_float2(vs.x, vs.y));
+                const uint32_t h = pack2<kSplit>(p.x, p.y);
+                hi[(e + x) / 2] = h;
+                if constexpr (kSplit) {
+                  const float2 rest = fma_two(make_float2(__uint_as_float(h << 16), __uint_as_float(h & 0xffff0000u)),
+                                              make_float2(-1.f, -1.f), p);
+                  lo_term[(e + x) / 2] = pack2<true>(rest.x, rest.y);
+                }
               }
             }
             tmem_st16(s_at + c * 32, hi);
             if constexpr (kSplit) tmem_st16(s_at + c * 32 + 16, lo_term);
           }
+          seen_top = fmaxf(tops[0], tops[1]) + shift;
           l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
           tmem_wait_st();
           tc_fence_before();
         }
         warp_arrive(t.p_full[b]);
+        if (two) {
+          warp_arrive(t.turn[b ^ 1]);
+          ++turns;
+        }
       }
       if (!ok) break;
       // with the last S of a triple complete every product with its q is done: the next one's takes its place, while the last
@@ -543,7 +547,10 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
       if (some) {
         int64_t at_lse = 0;
         if (mine) out_at<kCommon>(a, walk.sp.first, head, row, &at_lse);
-        float* to = whole ? a.part + at_lse * D : slot + (int64_t)(b * kTile + r) * D;
+        // four dimensions of neighbouring rows side by side: of all rows of a kv head, or of the slot's
+        const int64_t stride = whole ? (int64_t)a.table.seqs * a.rows : a.slot_rows;
+        float4* to = whole ? reinterpret_cast<float4*>(a.part) + head * (D / 4) * stride + (int64_t)walk.sp.first * a.rows + row
+                           : reinterpret_cast<float4*>(slot) + b * kTile + r;
         const float g = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
         float2 zero = make_float2(0.f, 0.f);   // NaN after a product that is not finite, or past kFar
 #pragma unroll 1
@@ -561,7 +568,10 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
                 v[x] = g == 0.f ? 0.f : o[e + x] * g;
                 v[x + 1] = g == 0.f ? 0.f : o[e + x + 1] * g;
               }
-              if (mine) store8(to + d0 + e, v);
+              if (mine) {
+                to[(d0 + e) / 4 * stride] = make_float4(v[0], v[1], v[2], v[3]);
+                to[((d0 + e) / 4 + 1) * stride] = make_float4(v[4], v[5], v[6], v[7]);
+              }
             }
           }
         }
@@ -585,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
           const int at_row = b * kTile + r - lane + src;
           const float s = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
           if (lane * 4 < D)
-            *reinterpret_cast<float4*>((whole ? a.part + its_lse * D : slot + (int64_t)at_row * D) + lane * 4) =
+            to[src - lane + lane * stride] =
                 s == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * s, acc.y * s, acc.z * s, acc.w * s);
           if (lane == 0) write_end(at_row, its_lse, top, sum);
         }
@@ -593,10 +603,11 @@ __global__ void __launch_bounds__(kThreads, 1) common_kernel(const __grid_consta
       tc_fence_before();
       warp_arrive(t.o_empty[b]);
     }
+    copy_wait<0>();
   }
 
   // ---- nothing in flight: every product is done (the loaders have waited for their copies); TMEM is freed ----
-  if (warp == kMmaWarp) {
+  if (warp == kMmaWarp || warp == kMmaWarp + 1) {
     if (elect_one()) mma_commit<false>(smem_u32(&t.drain), 0);
     __syncwarp();
     mbar_wait_inline(smem_u32(&t.drain), 0, nullptr);
@@ -622,7 +633,7 @@ cudaError_t launch_heads(AttendArgs a, int num_sms, cudaStream_t st) {
   const double tiles = (double)a.table.seqs * a.rows / kRows + a.groups, most = tiles * a.kv_heads * (double)units;
   if (most >= 2147483648.0) return cudaErrorNotSupported;   // cells are counted in 32 bits
   a.parts = most < (double)num_sms ? (int)most : num_sms;
-  return launch_form<kCommon>(kernel, a.parts, kThreads, kSmem, a, st);
+  return launch_form<kCommon>(kernel, a.parts, Common<FMT, QF16, DP>::kThreads, kSmem, a, st);
 }
 template <int FMT, bool QF16>
 cudaError_t launch_type(const AttendArgs& a, int num_sms, cudaStream_t st) {

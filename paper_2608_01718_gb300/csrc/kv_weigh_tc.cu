@@ -307,14 +307,15 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
         const uint32_t idesc = (1u << 4) | type | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
         const uint64_t q_desc = smem_desc(base + W::kQ + slot * W::kTileBytes);
         const uint64_t k_desc = smem_desc(base + (units & 1) * W::kSetBytes);
+        const uint32_t s_to = tmem + buffer * W::kBlocks * W::kRows;
         if (elect_one()) {
-#pragma unroll 1
+#pragma unroll
           for (int b = 0; b < W::kBlocks; ++b) {
-#pragma unroll 1
-            for (int kk = 0; kk < D / 16; ++kk)
-              mma_ss(tmem + (buffer * W::kBlocks + b) * W::kRows,
-                     k_desc + (uint64_t)((b * 128 * DP * 2 + (kk >> 2) * (128 * 128)) / 16 + (kk & 3) * 2),
-                     q_desc + (uint64_t)((kk >> 2) * (W::kRows * 128) / 16 + (kk & 3) * 2), idesc, kk ? 1u : 0u);
+#pragma unroll
+            for (int kk = 0; kk < DP / 16; ++kk)
+              if (kk < D / 16)
+                mma_ss(s_to + b * W::kRows, k_desc + (uint64_t)((b * 128 * DP * 2 + (kk >> 2) * (128 * 128)) / 16 + (kk & 3) * 2),
+                       q_desc + (uint64_t)((kk >> 2) * (W::kRows * 128) / 16 + (kk & 3) * 2), idesc, kk ? 1u : 0u);
           }
           mma_commit<false>(smem_u32(&t.q_empty[slot]), 0);
           mma_commit<false>(smem_u32(&t.s_full[buffer]), 0);

@@ -24,14 +24,14 @@ def ints(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
 
-def filled(fmt, groups, kv_heads, head_dim, page=16, seed=0, alone=(), poison_rows=True, **kw):
-    """groups: (common positions, [lengths of its sequences, whole]); `alone`: lengths of sequences of no group, after them. Only the
-    first sequence of a group names the pages of the common positions; the others' rows name no pages there."""
+def filled(fmt, groups, kv_heads, head_dim, page=16, seed=0, alone=(), small=False, **kw):
+    """groups: (common positions, [lengths of its sequences, whole]); `alone`: lengths of sequences of no group, after them. A table
+    as wide as one that serves long sequences too (unless `small`), or the call would read each sequence for itself."""
     lengths = [n for _, ns in groups for n in ns] + list(alone)
     c = Filled(fmt, lengths, kv_heads, head_dim, page, seed=seed, **kw)
     c.bounds = np.cumsum([0] + [len(ns) for _, ns in groups]).tolist()
     c.common = [p for p, _ in groups]
-    pool, seen = c.kv.pool(c.layer), c.host_table.copy()
+    pool = c.kv.pool(c.layer)
     for g, (p, ns) in enumerate(groups):
         first = c.bounds[g]
         if not ns or lengths[first] < min(p, max(ns)):
@@ -39,17 +39,17 @@ def filled(fmt, groups, kv_heads, head_dim, page=16, seed=0, alone=(), poison_ro
             continue
         for s in range(first + 1, c.bounds[g + 1]):
             full, rest = min(p, lengths[s]) // page, min(p, lengths[s]) % page
-            c.host_table[s, :full] = seen[s, :full] = c.host_table[first, :full]
-            if poison_rows:
-                seen[s, :full] = -7
+            c.host_table[s, :full] = c.host_table[first, :full]
             if rest:      # the page that the common part ends in is the sequence's own, with a copy
                 a, b = int(c.host_table[first, full]), int(c.host_table[s, full])
                 for t in pool.values():
                     x = t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t
                     x[b, :, :rest] = x[a, :, :rest].clone()
-                if lengths[s] <= p and poison_rows:
-                    c.host_table[s, full], seen[s, full] = a, -7
-    c.table = torch.from_numpy(seen).cuda()
+    row = 2 * kv_heads * head_dim * (1 if fmt in ("e4m3", "int8") else 2)
+    width = c.host_table.shape[1] if small else max(c.host_table.shape[1], 80_000_000 // (row * page * len(lengths)) + 1)
+    wide = np.full((len(lengths), width), 1 << 29, dtype=np.int32)
+    wide[:, :c.host_table.shape[1]] = c.host_table
+    c.table = torch.from_numpy(wide).cuda()
     return c
 
 
@@ -156,7 +156,7 @@ def test_values_that_are_not_finite_keep_to_the_rows_that_see_them(fmt, q_heads,
 
 
 def test_bad_groups_are_reported():
-    c = filled("bf16", [(100, [120, 130, 140, 125])], 1, 64, seed=11, poison_rows=False)
+    c = filled("bf16", [(100, [120, 130, 140, 125])], 1, 64, seed=11)
     q = queries(c, "bf16", 4, 1)
     want = c.kv.attend(q, c.table, c.len_dev)
     for bounds in ([0, 5], [-1, 4], [3, 1], [0, 3, 2, 4]):
@@ -168,7 +168,7 @@ def test_bad_groups_are_reported():
     c.kv.attend_shared(q, c.table, c.len_dev, ints([-5]))
     with pytest.raises(L.LacacheError):
         c.kv.sync()
-    c.kv.attend_shared(q, c.table, c.len_dev, ints([1 << 30]))     # past the table: cut; nothing is left of any sequence's own
+    c.kv.attend_shared(q, c.table, c.len_dev, ints([(1 << 31) - 1]))   # past the table: cut; nothing is left of any sequence's own
     with pytest.raises(L.LacacheError):
         c.kv.sync()
     table = c.table.clone()
@@ -178,6 +178,17 @@ def test_bad_groups_are_reported():
         c.kv.sync()
     c.kv.attend_shared(q, c.table, c.len_dev, ints([100]))
     c.kv.sync()
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS[:3])
+def test_small_calls_are_the_ordinary_attention(fmt, dtype):
+    c = filled(fmt, [(100, [120, 130, 99, 125]), (20, [21])], 2, 64, seed=16, small=True)
+    for new in (1, 9):
+        out, lse = check(c, dtype, 4, new, window=70)
+        q = queries(c, dtype, 4, new)
+        want_lse = torch.empty_like(lse)
+        want = c.kv.attend(q, c.table, c.len_dev, new_tokens=new, window=70, lse=want_lse)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
 def test_strided_rows():
