@@ -559,16 +559,17 @@ lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_k
  * that of lacache_kv_attend but for roundings. Bounds that do not rise, and lengths past the table, are reported by
  * lacache_kv_sync (and the call runs without groups, or with the lengths cut). Where the table can name no more than 64 MB of K
  * and V in all, every sequence is read for itself, and the groups are not looked at.
- * The workspace is device memory, 16-byte aligned, of lacache_kv_attend_shared_workspace_bytes(h, seqs, groups, new_tokens,
- * q_heads) (0 for arguments outside their ranges); calls that may overlap, those of two captured graphs among them, have one each.
+ * The workspace is device memory, 16-byte aligned, of lacache_kv_attend_shared_workspace_bytes(h, table, groups, new_tokens,
+ * q_heads) (0 for such a small call, and for arguments outside their ranges; of the table, seqs and width are looked at); calls
+ * that may overlap, those of two captured graphs among them, have one each.
  * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read bounds, lengths and tables anew. */
 typedef struct {
   int32_t groups;            /* at least 1 */
   const int32_t* bounds_dev; /* [groups + 1] */
   const int32_t* lengths_dev;/* [groups] */
 } lacache_shared;
-size_t lacache_kv_attend_shared_workspace_bytes(const lacache_kv_t* h, int32_t seqs, int32_t groups, int32_t new_tokens,
-                                                int32_t q_heads);
+size_t lacache_kv_attend_shared_workspace_bytes(const lacache_kv_t* h, const lacache_kv_table* table, int32_t groups,
+                                                int32_t new_tokens, int32_t q_heads);
 lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table,
                                         const lacache_attention* a, const lacache_shared* shared, void* workspace_dev,
                                         size_t workspace_bytes, void* cuda_stream);

@@ -226,11 +226,23 @@ cudaError_t launch_own(const AttendArgs& a, int format, int num_sms, cudaStream_
 }  // namespace
 }  // namespace lc
 
-extern "C" size_t lacache_kv_attend_shared_workspace_bytes(const lacache_kv_t* h, int32_t seqs, int32_t groups,
+namespace lc {
+namespace {
+// What the table can name at most, read for every sequence, against four kernels: two sequences of 340 tokens of 8 heads (d = 64,
+// bf16, 1.4 MB) take 8 us so and 19.6 in parts. 64 MB are some 12 us more.
+bool is_small(const lacache_kv_config& c, const lacache_kv_table& t) {
+  const double reach = std::min<double>((double)t.width * c.page_size, kMaxPositions);
+  return 2.0 * t.seqs * reach * c.kv_heads * c.head_dim * (is_quantised(c.format) ? 1 : 2) <= kSmall;
+}
+}  // namespace
+}  // namespace lc
+
+extern "C" size_t lacache_kv_attend_shared_workspace_bytes(const lacache_kv_t* h, const lacache_kv_table* table, int32_t groups,
                                                            int32_t new_tokens, int32_t q_heads) {
-  if (!h || seqs < 0 || groups < 0 || new_tokens < 1 || q_heads < 1) return 0;
+  if (!h || !table || table->seqs < 0 || table->width < 1 || groups < 1 || new_tokens < 1 || q_heads < 1) return 0;
   const lacache_kv_config& c = h->cfg;
-  return lc::workspace_of(seqs, groups, new_tokens, q_heads, c.kv_heads, c.head_dim, c.head_dim <= 128 ? h->num_sms : 0).bytes;
+  if (lc::is_small(c, *table)) return 0;
+  return lc::workspace_of(table->seqs, groups, new_tokens, q_heads, c.kv_heads, c.head_dim, c.head_dim <= 128 ? h->num_sms : 0).bytes;
 }
 
 extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table,
@@ -245,23 +257,21 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
   const lacache_kv_config& c = h->cfg;
   const lc::Workspace w = lc::workspace_of(table->seqs, shared->groups, at->new_tokens, at->q_heads, c.kv_heads, c.head_dim,
                                            c.head_dim <= 128 ? h->num_sms : 0);
+  const bool small = lc::is_small(c, *table);
   lc::Join j = {};
-  if (!lc::device_rows(&at->out, at->dtype, &j.out) || at->out.data == at->q.data || !shared->lengths_dev || !workspace_dev ||
-      !lc::aligned16(workspace_dev) || workspace_bytes < w.bytes)
+  if (!lc::device_rows(&at->out, at->dtype, &j.out) || at->out.data == at->q.data || !shared->lengths_dev ||
+      (!small && (!workspace_dev || !lc::aligned16(workspace_dev) || workspace_bytes < w.bytes)))
     return LACACHE_ERR_INVALID_ARG;
   if ((double)table->seqs * a.rows >= 2147483648.0) return LACACHE_ERR_UNSUPPORTED;   // a group's rows are counted in 32 bits
   lc::DeviceGuard guard(c.device);
   if (!guard.ok()) return LACACHE_ERR_CUDA;
   const cudaStream_t st = (cudaStream_t)cuda_stream;
-  const bool eight = lc::is_quantised(c.format);
-  // What the table can name at most, read for every sequence, against four kernels: two sequences of 340 tokens of 8 heads (d = 64,
-  // bf16, 1.4 MB) take 6.5 us so and 19.6 in parts. 64 MB are some 12 us more.
-  const double bytes = 2.0 * table->seqs * a.max_len * c.kv_heads * c.head_dim * (eight ? 1 : 2);
-  if (bytes <= lc::kSmall) {
+  if (small) {
     a.out = j.out;
     a.lse = at->lse_dev;
     return lc::launch_whole(h, a, st);
   }
+  const bool eight = lc::is_quantised(c.format);
   unsigned char* ws = static_cast<unsigned char*>(workspace_dev);
   auto floats = [&](size_t at_byte) { return reinterpret_cast<float*>(ws + at_byte); };
   auto ints = [&](size_t at_byte) { return reinterpret_cast<int32_t*>(ws + at_byte); };

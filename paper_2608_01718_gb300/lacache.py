@@ -184,7 +184,7 @@ def load() -> ctypes.CDLL:
         "lacache_kv_read": ([vp, i32, vp, i64, vp, vp, i32, vp, vp, vp], i32),
         "lacache_kv_attend": ([vp, i32, vp, vp, vp], i32),
         "lacache_kv_attend_shared": ([vp, i32, vp, vp, vp, vp, ctypes.c_size_t, vp], i32),
-        "lacache_kv_attend_shared_workspace_bytes": ([vp, i32, i32, i32, i32], ctypes.c_size_t),
+        "lacache_kv_attend_shared_workspace_bytes": ([vp, vp, i32, i32, i32], ctypes.c_size_t),
         "lacache_kv_weigh": ([vp, i32, vp, vp, vp], i32),
         "lacache_kv_evict": ([vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp], i32),
         "lacache_kv_sync": ([vp], i32),
@@ -425,27 +425,28 @@ def lacache_verify_sample(p_target, p_draft, drafts, u, accepted, token, status=
     ``p_target`` [B x k + 1 x vocab] and ``p_draft`` [B x k x vocab] are fp32 probabilities (any strides, dense rows);
     ``p_draft`` is None for drafts that were not drawn. ``drafts`` int32 [B x k] (-1 ends a window), ``accepted`` and ``token``
     int32 [B]; -1 in both for served queries (``status``)."""
-    import torch
+    _bind_torch()
     if p_target.dim() != 3 or not p_target.is_cuda:
         raise ValueError("p_target is a [queries x drafts + 1 x vocab] CUDA tensor")
     B, rows, vocab = p_target.shape
     k, device = rows - 1, p_target.get_device()
 
     def probs(name, t, n):
-        if t.shape != (B, n, vocab) or t.dtype != torch.float32 or t.get_device() != device or (t.stride(2) != 1 and vocab > 1):
+        stride = t.stride()
+        if t.shape != (B, n, vocab) or t.dtype != _F32 or t.get_device() != device or (stride[2] != 1 and vocab > 1):
             raise ValueError(f"{name} is a [{B} x {n} x {vocab}] fp32 tensor with dense rows on cuda:{device}")
-        return lacache_probs(t.data_ptr(), t.stride(0), t.stride(1))
+        return lacache_probs(t.data_ptr(), stride[0], stride[1])
 
     pt, pd = probs("p_target", p_target, rows), None if p_draft is None else probs("p_draft", p_draft, k)
-    args = (B, k, vocab, ctypes.addressof(pt), _address(pd), _dense("drafts", drafts, (B, k), torch.int32, device),
-            _dense("u", u, (B, rows), torch.float32, device),
-            None if status is None else _dense("status", status, (B,), torch.uint8, device),
-            _dense("accepted", accepted, (B,), torch.int32, device), _dense("token", token, (B,), torch.int32, device),
-            _stream(cuda_stream, device))
-    if torch.cuda.current_device() == device:
+    args = (B, k, vocab, ctypes.addressof(pt), _address(pd), _dense("drafts", drafts, (B, k), _INT32, device),
+            _dense("u", u, (B, rows), _F32, device),
+            None if status is None else _dense("status", status, (B,), _torch.uint8, device),
+            _dense("accepted", accepted, (B,), _INT32, device), _dense("token", token, (B,), _INT32, device),
+            _current_stream(cuda_stream, device))
+    if _torch.cuda.current_device() == device:
         _check("lacache_verify_sample", load().lacache_verify_sample(*args))
     else:
-        with torch.cuda.device(device):
+        with _torch.cuda.device(device):
             _check("lacache_verify_sample", load().lacache_verify_sample(*args))
 
 
@@ -520,8 +521,8 @@ def lacache_kv_attend(h: int, layer: int, table: lacache_kv_table, attention: la
                                                          _stream(cuda_stream)))
 
 
-def lacache_kv_attend_shared_workspace_bytes(h: int, seqs: int, groups: int, new_tokens: int, q_heads: int) -> int:
-    return int(load().lacache_kv_attend_shared_workspace_bytes(h, seqs, groups, new_tokens, q_heads))
+def lacache_kv_attend_shared_workspace_bytes(h: int, table: lacache_kv_table, groups: int, new_tokens: int, q_heads: int) -> int:
+    return int(load().lacache_kv_attend_shared_workspace_bytes(h, _address(table), groups, new_tokens, q_heads))
 
 
 def lacache_kv_attend_shared(h: int, layer: int, table: lacache_kv_table, attention: lacache_attention, shared: lacache_shared,
@@ -659,11 +660,11 @@ class LaCache:
 # What the calls that decode token by token need of torch, which is imported late: a call's every look-up of it would be a
 # tenth of the call.
 _DTYPES: dict = {}   # torch dtype -> lacache_dtype
-_INT32 = _RAW_STREAM = _Rotation = None
+_INT32 = _F32 = _RAW_STREAM = _Rotation = _torch = None
 
 
 def _bind_torch() -> None:
-    global _INT32, _RAW_STREAM, _Rotation
+    global _INT32, _F32, _RAW_STREAM, _Rotation, _torch
     if _Rotation is not None:
         return
     import torch
@@ -682,7 +683,7 @@ def _bind_torch() -> None:
             return ctx.rope.apply(grad.contiguous(), ctx.saved_tensors[0], not ctx.inverse), None, None, None, None
 
     _DTYPES.update({torch.bfloat16: LACACHE_BF16, torch.float16: LACACHE_F16, torch.float32: LACACHE_F32})
-    _INT32, _RAW_STREAM = torch.int32, getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _torch, _INT32, _F32, _RAW_STREAM = torch, torch.int32, torch.float32, getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _dtype(t) -> int:
@@ -799,6 +800,7 @@ class KVCache:
         self.format, self.device, self.layers = format, device, layers
         _bind_torch()
         self.h, self._lib = lacache_kv_create(self.cfg), load()
+        self._torch_device = _torch.device("cuda", device)
 
     def close(self) -> None:
         if self.h:
@@ -902,8 +904,7 @@ class KVCache:
         if out is None:
             out = _new_like(q, cuda_stream, dev)
         if lse is not None:
-            import torch
-            if lse.dtype != torch.float32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
+            if lse.dtype != _F32 or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
                 raise ValueError(f"lse is a dense fp32 [{n} x {heads}] tensor on cuda:{dev}")
         return t, lacache_attention(new_tokens, heads, self._window(window), _dtype(q), D ** -0.5 if scale is None else scale,
                                     _index("lengths", lengths, t.seqs, dev),
@@ -916,7 +917,6 @@ class KVCache:
         """attend for sequences that have their first positions in common, which are read once for all: the first ``shared[g]``
         positions (int32 [groups]) of the sequences ``bounds[g]`` to ``bounds[g + 1] - 1`` (int32 [groups + 1]; None: one group of
         all), from the pages of the first of them. ``lengths`` count whole sequences. Everything else, and the result, as attend."""
-        import torch
         dev = self.device
         t, a, out = self._attention(q, table, lengths, new_tokens, starts, window, scale, out, lse, cuda_stream)
         groups = shared.shape[0]
@@ -926,21 +926,30 @@ class KVCache:
             raise ValueError(f"{groups} groups have {groups + 1} bounds")
         common = lacache_shared(groups, None if bounds is None else _index("bounds", bounds, groups + 1, dev),
                                 _index("shared", shared, groups, dev))
-        size = self._lib.lacache_kv_attend_shared_workspace_bytes(self.h, t.seqs, groups, new_tokens, a.q_heads)
-        with _results_on(cuda_stream, dev):
-            workspace = torch.empty(size, dtype=torch.uint8, device=f"cuda:{dev}")
+        at, workspace = ctypes.addressof, None
+        size = self._lib.lacache_kv_attend_shared_workspace_bytes(self.h, at(t), groups, new_tokens, a.q_heads)
+        if size:
+            workspace = self._new((size,), _torch.uint8, cuda_stream)
         _check("lacache_kv_attend_shared", self._lib.lacache_kv_attend_shared(
-            self.h, self._layer(layer), ctypes.addressof(t), ctypes.addressof(a), ctypes.addressof(common), workspace.data_ptr(),
-            size, _current_stream(cuda_stream, dev)))
+            self.h, self._layer(layer), at(t), at(a), at(common), None if workspace is None else workspace.data_ptr(), size,
+            _current_stream(cuda_stream, dev)))
         return out
 
+    def _new(self, shape, dtype, cuda_stream, zero: bool = False):
+        """A tensor for a call on cuda_stream."""
+        make = _torch.zeros if zero else _torch.empty
+        if cuda_stream is None:
+            return make(shape, dtype=dtype, device=self._torch_device)
+        with _results_on(cuda_stream, self.device):
+            return make(shape, dtype=dtype, device=self._torch_device)
+
     def _weights(self, name: str, t, seqs: int, least: int = 1) -> lacache_weights:
-        import torch
-        if (t.dim() != 3 or t.shape[:2] != (seqs, self.cfg.kv_heads) or t.dtype != torch.float32 or t.shape[2] < least or
-                (t.stride(2) != 1 and t.shape[2] > 1) or t.get_device() != self.device):
+        shape, stride = t.shape, t.stride()
+        if (len(shape) != 3 or shape[0] != seqs or shape[1] != self.cfg.kv_heads or t.dtype != _F32 or shape[2] < least or
+                (stride[2] != 1 and shape[2] > 1) or t.get_device() != self.device):
             raise ValueError(f"{name} is a [{seqs} x {self.cfg.kv_heads} x positions] fp32 tensor of {least} positions or more, "
                              f"its rows dense, on cuda:{self.device}")
-        return lacache_weights(t.data_ptr(), t.stride(0), t.stride(1), min(t.shape[2], (1 << 31) - 1))
+        return lacache_weights(t.data_ptr(), stride[0], stride[1], min(shape[2], (1 << 31) - 1))
 
     def weigh(self, q, table, lengths, lse, weights=None, decay: float = 1.0, out=None, new_tokens: int = 1, layer: int = 0,
               starts=None, window: int = 0, scale: float | None = None, cuda_stream=None):
@@ -954,9 +963,7 @@ class KVCache:
         if out is None:
             out = weights
         if out is None:
-            import torch
-            with _results_on(cuda_stream, dev):
-                out = torch.zeros(t.seqs, self.cfg.kv_heads, t.width * self.cfg.page_size, device=f"cuda:{dev}")
+            out = self._new((t.seqs, self.cfg.kv_heads, t.width * self.cfg.page_size), _F32, cuda_stream, zero=True)
         to = self._weights("out", out, t.seqs)
         past = lacache_weights() if weights is None else self._weights("weights", weights, t.seqs, out.shape[2])
         if lse.dtype != out.dtype or lse.shape != (n, heads) or not lse.is_contiguous() or lse.get_device() != dev:
@@ -975,26 +982,23 @@ class KVCache:
         order to the pages of the table ``to`` (which the sequences of ``table`` do not use). Returns ``new_lengths`` (int32
         [sequences]), ``kept`` (int32 [sequences x kv_heads x keep]: their positions, then -1) and ``new_weights``
         [sequences x kv_heads x keep]. The tokens keep the rotary positions that they were written with."""
-        import torch
         t, target, H, dev = self._table(table), self._table(to), self.cfg.kv_heads, self.device
         if not 1 <= keep < 1 << 31 or not 0 <= recent <= keep:
             raise ValueError(f"keep is 1 or more and recent 0 to keep, not {keep} and {recent}")
-        with _results_on(cuda_stream, dev):
-            kw = {"device": f"cuda:{dev}"}
-            if kept is None:
-                kept = torch.empty(t.seqs, H, keep, dtype=torch.int32, **kw)
-            if new_lengths is None:
-                new_lengths = torch.empty(t.seqs, dtype=torch.int32, **kw)
-            if new_weights is None:
-                new_weights = torch.zeros(t.seqs, H, keep, **kw)
-        if kept.dtype != _INT32 or kept.shape != (t.seqs, H, keep) or not kept.is_contiguous() or kept.get_device() != dev:
+        if kept is None:
+            kept = self._new((t.seqs, H, keep), _INT32, cuda_stream)
+        elif kept.dtype != _INT32 or kept.shape != (t.seqs, H, keep) or not kept.is_contiguous() or kept.get_device() != dev:
             raise ValueError(f"kept is a dense int32 [{t.seqs} x {H} x {keep}] tensor on cuda:{dev}")
+        if new_lengths is None:
+            new_lengths = self._new((t.seqs,), _INT32, cuda_stream)
+        if new_weights is None:
+            new_weights = self._new((t.seqs, H, keep), _F32, cuda_stream, zero=True)
         w, nw = self._weights("weights", weights, t.seqs), self._weights("new_weights", new_weights, t.seqs, keep)
+        at = ctypes.addressof
         _check("lacache_kv_evict", self._lib.lacache_kv_evict(
-            self.h, self._layer(layer), ctypes.addressof(t), _index("lengths", lengths, t.seqs, dev),
-            None if starts is None else _index("starts", starts, t.seqs, dev), ctypes.addressof(w), keep, recent,
-            ctypes.addressof(target), kept.data_ptr(), _index("new_lengths", new_lengths, t.seqs, dev), ctypes.addressof(nw),
-            _current_stream(cuda_stream, dev)))
+            self.h, self._layer(layer), at(t), _index("lengths", lengths, t.seqs, dev),
+            None if starts is None else _index("starts", starts, t.seqs, dev), at(w), keep, recent, at(target), kept.data_ptr(),
+            _index("new_lengths", new_lengths, t.seqs, dev), at(nw), _current_stream(cuda_stream, dev)))
         return new_lengths, kept, new_weights
 
     def sync(self) -> None:

@@ -265,7 +265,8 @@ def test_refusals():
     assert c.kv.attend_shared(q[:0], c.table[:0], c.len_dev[:0], common).shape == (0, 4, 64)
     t, a, out = c.kv._attention(q, c.table, c.len_dev, 1, None, 0, None, None, None, None)
     lib, at = L.load(), ctypes.addressof
-    size = L.lacache_kv_attend_shared_workspace_bytes(c.kv.h, 2, 1, 1, 4)
+    size = L.lacache_kv_attend_shared_workspace_bytes(c.kv.h, t, 1, 1, 4)
+    assert size > 0 and L.lacache_kv_attend_shared_workspace_bytes(c.kv.h, L.lacache_kv_table(None, 0, 2, 9), 1, 1, 4) == 0
     ws = torch.empty(size + 16, dtype=torch.uint8, device="cuda")
     groups = L.lacache_shared(1, None, common.data_ptr())
 
@@ -276,6 +277,6 @@ def test_refusals():
     for bad in (dict(p=None), dict(p=ws.data_ptr() + 8), dict(n=size - 1), dict(shared=L.lacache_shared(0, None, common.data_ptr())),
                 dict(shared=L.lacache_shared(2, None, common.data_ptr())), dict(shared=L.lacache_shared(1, None, None))):
         assert call(**bad) == L.LACACHE_ERR_INVALID_ARG, bad
-    for bad in ((-1, 1, 1, 4), (2, -1, 1, 4), (2, 1, 0, 4), (2, 1, 1, 0)):
+    for bad in ((None, 1, 1, 4), (L.lacache_kv_table(None, 0, -1, 1 << 20), 1, 1, 4), (t, 0, 1, 4), (t, 1, 0, 4), (t, 1, 1, 0)):
         assert L.lacache_kv_attend_shared_workspace_bytes(c.kv.h, *bad) == 0
     c.kv.sync()
