@@ -322,8 +322,13 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
     int j = 0, k = 0, triples = 0;   // units of the block, units and triples of this tile of rows
     for (; ok && !walk.done(); walk.next(a)) {
       const int count = walk.units();
-      const bool two = has_two(walk);
-      if (b == 1 && !two) {
+      if (b == 1 && !has_two(walk)) {   // (one by one: a wait for a slot's later phase would take an earlier one of its parity for it)
+        for (int i = 0; ok && i < 2 * count; ++i) {
+          const int n = 2 * j + i, slot = n % kSlots;
+          ok = wait(t.full[slot], (n / kSlots) & 1);
+          ok = __all_sync(0xffffffffu, ok);
+          if (ok) warp_arrive(t.empty[slot]);
+        }
         j += count;
         continue;
       }
@@ -347,7 +352,6 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
           }
           mma_commit<false>(smem_u32(&t.s_full[b]), 0);
           mma_commit<false>(smem_u32(&t.empty[k_slot]), 0);
-          if (!two) mma_commit<false>(smem_u32(&t.empty[k_slot]), 0);   // (for the other tile, which is empty)
         }
         __syncwarp();
         // O (+)= P V
@@ -367,7 +371,6 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
           }
           mma_commit<false>(smem_u32(&t.pv_done[b]), 0);
           mma_commit<false>(smem_u32(&t.empty[v_slot]), 0);
-          if (!two) mma_commit<false>(smem_u32(&t.empty[v_slot]), 0);
         }
         __syncwarp();
       }
@@ -451,9 +454,9 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
                 if (e < first || e > last || (bad >> (c * 2 + e / 16) & 1)) x[e] = -INFINITY;
             }
           };
-          // The reference. bf16 weights have fp32's range, so only a triple's first unit needs its maximum before its weights: a
-          // later one's moves the reference for the units after it (and what overflows all the same is not finite: done again).
-          // f16 weights need each unit's.
+          // The reference. bf16 weights have fp32's range, so only the first unit that a row sees needs its maximum before its
+          // weights: a later one's moves the reference for the units after it (and what overflows all the same is not finite:
+          // done again). f16 weights need each unit's.
           auto move_to = [&](float top) {
             const bool move = m == -INFINITY ? top > -INFINITY : top > m + kHeadroom;
             if (i > 0 && __any_sync(0xffffffffu, move)) {
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
             }
             if (move) m = top - kBelow;
           };
-          if (i == 0 || !kSplit) {
+          if (!kSplit || __any_sync(0xffffffffu, mine && m == -INFINITY && lo <= key + kTile - 1 && pos >= key)) {
             float top = -INFINITY;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
@@ -482,7 +485,7 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
               for (int e = 0; e < 32; e += 2) top = max_three(top, x[e], x[e + 1]);
             }
             move_to(top);
-          } else {
+          } else if (i > 0) {
             move_to(seen_top);
           }
           const float shift = m == -INFINITY ? 0.f : m;

@@ -129,6 +129,25 @@ def test_groups_of_one_and_many_groups():
     check(c, "f16", 4, none_bounds=True)
 
 
+@pytest.mark.parametrize("fmt,head_dim", [("bf16", 80), ("e4m3", 64), ("f16", 128)])
+def test_blocks_with_one_and_two_tiles_of_rows(fmt, head_dim):
+    """Groups of 100 and of 140 rows a kv head in turn: a block has units of one tile of rows, then units of two."""
+    groups = [(700 - i, [701 + (i * 7 + s) % 40 for s in range(5 if i % 2 else 7)]) for i in range(20)]
+    c = filled(fmt, groups, 8, head_dim, seed=17)
+    check(c, fmt if fmt == "f16" else "bf16", 32, 5)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS[:3])
+def test_rows_that_see_nothing_of_their_first_units(fmt, dtype):
+    """Windows and starts that begin some hundred positions into a block's keys, and rows that see nothing at all."""
+    groups = [(900 - 9 * i, [901 + (i * 7 + s * 29) % 60 for s in range(9)] + [0, 500]) for i in range(12)]
+    starts = [(s * 97) % 1000 for s in range(12 * 11)]
+    c = filled(fmt, groups, 4, 64, seed=18)
+    check(c, dtype, 16, 3, window=333)
+    check(c, dtype, 16, 3, starts=starts)
+    check(c, dtype, 16, 3, starts=starts, window=450, scale=-0.25)
+
+
 def test_own_parts_of_a_draft_window():
     c = filled("bf16", [(500, [517, 600, 530, 560])], 2, 128, seed=8)
     check(c, "bf16", 8, 17)                                   # the own part on tcgen05 too
