@@ -49,10 +49,14 @@ __global__ void __launch_bounds__(kVerifyWarps * 32)
 // of the calls; in fp64 alone, the differences and sums of a row of 10^5 take longer than reading it.
 //
 // A cluster of 1 to 8 blocks a query, each warp a run of consecutive tokens, with sixteen loads in flight a lane. The runs'
-// sums are exchanged through the cluster's shared memory; the block that holds the border adds its run again in fp64, a few
-// consecutive tokens a thread.
+// sums are exchanged through the cluster's shared memory; the block that holds the border adds its run again, a part a warp, and
+// one warp looks for the token in that part. fp64 takes 16 cycles of an SM an instruction, so one warp a block takes those steps:
+// by all warps they were a third of the time. 64 queries of 16 drafts and 100,003 tokens, two rows of one position read: 18.2 us
+// (2.8 TB/s); one query of 32,000 tokens 8.5 us, the latency of the chain from the drafts to the token. What bounds both is that
+// chain: with twice or half the loads in flight the times are the same.
 constexpr int kSampleThreads = 256, kSampleWarps = kSampleThreads / 32, kMaxCluster = 8;
 constexpr int kSampleUnroll = 8;
+constexpr int kSampleWalk = 64;   // of a part, walked 32 tokens at a time; a longer one is cut further first (196 tokens: 18.2 us so, 19.9 walked)
 constexpr int kMaxVocab = 1 << 30, kSampleResident = 152 * 8;
 
 struct Probs {
@@ -83,6 +87,17 @@ __device__ __forceinline__ void add_difference(Twofold& a, float x, float y) {
   a.sum = s;
   a.rest = __fadd_rn(a.rest, __fadd_rn(s_err, d_err));
 }
+__device__ __forceinline__ Twofold plus(Twofold a, Twofold b) {
+  const float s = __fadd_rn(a.sum, b.sum), c = __fsub_rn(s, a.sum);
+  const float s_err = __fadd_rn(__fsub_rn(a.sum, __fsub_rn(s, c)), __fsub_rn(b.sum, c));
+  return Twofold{s, __fadd_rn(__fadd_rn(a.rest, b.rest), s_err)};
+}
+__device__ __forceinline__ Twofold warp_sum(Twofold x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    x = plus(x, Twofold{__shfl_xor_sync(0xffffffffu, x.sum, o), __shfl_xor_sync(0xffffffffu, x.rest, o)});
+  return x;
+}
 __device__ __forceinline__ double inclusive_sum(double x) {   // over the warp's lanes
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -91,12 +106,23 @@ __device__ __forceinline__ double inclusive_sum(double x) {   // over the warp's
   }
   return x;
 }
+// Of the warp's lanes, in order: the first that the cumulative weight `upto` exceeds `target` in, else (u at or above 1, sums that
+// are not finite, or that end below those of the level above by their last bits) the last that has any weight, else -1. `base`: the
+// weight before the first lane, then before that one.
+__device__ __forceinline__ int border_lane(double own, double upto, double target, double& base) {
+  const unsigned past = __ballot_sync(0xffffffffu, own > 0.0 && upto > target), some = __ballot_sync(0xffffffffu, own > 0.0);
+  const int at = past ? __ffs(past) - 1 : 31 - __clz(some);
+  const double before = __shfl_sync(0xffffffffu, upto, at > 0 ? at - 1 : 0);
+  if (at > 0) base = before;
+  return at;
+}
 
 __global__ void __launch_bounds__(kSampleThreads) verify_sample_kernel(const __grid_constant__ SampleArgs a) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
-  __shared__ double run_sum[kSampleWarps], all_sum[kSampleWarps * kMaxCluster], warp_sum[kSampleWarps];
-  __shared__ int first_past, last_some;
+  __shared__ alignas(16) Twofold run_sum[kSampleWarps];
+  __shared__ Twofold part_sum[kSampleWarps];
+  __shared__ int s_n, s_refused, s_run;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t b = blockIdx.x / a.blocks;
   const int rank = blockIdx.x - (int)b * a.blocks, runs = a.blocks * kSampleWarps;
@@ -104,114 +130,128 @@ __global__ void __launch_bounds__(kSampleThreads) verify_sample_kernel(const __g
     if (rank == 0 && threadIdx.x == 0) a.accepted[b] = a.token[b] = -1;
     return;
   }
-  // how many drafts are accepted, and which one, if any, was refused: every warp for itself
-  int n = a.k, refused = -1;
-  for (int base = 0; base < a.k; base += 32) {
-    const int t = base + lane;
-    int x = -1;
-    bool go = false;
-    if (t < a.k) {
-      x = a.drafts[b * a.k + t];
-      if (x < 0 || x >= a.vocab) {
-        x = -1;
-      } else {
-        const float p = a.target.data[b * a.target.seq + t * a.target.token + x];
-        const float q = a.draft.data ? a.draft.data[b * a.draft.seq + t * a.draft.token + x] : 1.f;
-        go = (double)a.u[b * (a.k + 1) + t] * (double)q < (double)p;
+  const double u = a.u[b * (a.k + 1) + a.k];
+  // how many drafts are accepted, and which one, if any, was refused
+  if (warp == 0) {
+    int n = a.k, refused = -1;
+    for (int base = 0; base < a.k; base += 32) {
+      const int t = base + lane;
+      int x = -1;
+      bool go = false;
+      if (t < a.k) {
+        x = a.drafts[b * a.k + t];
+        if (x < 0 || x >= a.vocab) {
+          x = -1;
+        } else {
+          const float p = a.target.data[b * a.target.seq + t * a.target.token + x];
+          const float q = a.draft.data ? a.draft.data[b * a.draft.seq + t * a.draft.token + x] : 1.f;
+          go = (double)a.u[b * (a.k + 1) + t] * (double)q < (double)p;
+        }
+      }
+      const unsigned stop = __ballot_sync(0xffffffffu, t < a.k && !go);
+      if (stop) {
+        n = base + __ffs(stop) - 1;
+        refused = __shfl_sync(0xffffffffu, x, __ffs(stop) - 1);
+        break;
       }
     }
-    const unsigned stop = __ballot_sync(0xffffffffu, t < a.k && !go);
-    if (stop) {
-      n = base + __ffs(stop) - 1;
-      refused = __shfl_sync(0xffffffffu, x, __ffs(stop) - 1);
-      break;
-    }
+    if (lane == 0) s_n = n, s_refused = refused;
   }
+  __syncthreads();
+  const int n = s_n, refused = s_refused;
   const float* p = a.target.data + b * a.target.seq + n * a.target.token;
-  const double u = a.u[b * (a.k + 1) + a.k];
-  int token = -1;
   // a second time with p alone where p - q leaves no weight
   for (int attempt = refused >= 0 ? 0 : 1; attempt < 2; ++attempt) {
     const float* q = attempt == 0 && a.draft.data ? a.draft.data + b * a.draft.seq + n * a.draft.token : nullptr;
     const int one = attempt == 0 && !a.draft.data ? refused : -1;   // where q is 1, if it has no row
     auto less = [&](int i) { return q ? q[i] : i == one ? 1.f : 0.f; };
-    const int first = (int)min((int64_t)(rank * kSampleWarps + warp) * a.run, (int64_t)a.vocab);
-    const int end = (int)min((int64_t)first + a.run, (int64_t)a.vocab);
-    Twofold sum = {0.f, 0.f};
-    for (int i0 = first + lane; i0 < end; i0 += 32 * kSampleUnroll) {
-      float x[kSampleUnroll], y[kSampleUnroll];
+    // tokens i, i + step, ... before `end`
+    auto add_up = [&](int i0, int end, int step) {
+      Twofold sum = {0.f, 0.f};
+      for (; i0 < end; i0 += step * kSampleUnroll) {
+        float x[kSampleUnroll], y[kSampleUnroll];
 #pragma unroll
-      for (int e = 0; e < kSampleUnroll; ++e) {
-        const int i = i0 + 32 * e;
-        x[e] = i < end ? p[i] : 0.f;
-        y[e] = i < end ? less(i) : 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < kSampleUnroll; ++e)
-        if (x[e] > y[e]) add_difference(sum, x[e], y[e]);
-    }
-    const double mine = inclusive_sum((double)sum.sum + (double)sum.rest);
-    if (lane == 31) run_sum[warp] = mine;
-    cluster.sync();
-    if (threadIdx.x < runs)
-      all_sum[threadIdx.x] = *cluster.map_shared_rank(&run_sum[threadIdx.x % kSampleWarps], threadIdx.x / kSampleWarps);
-    if (threadIdx.x == 0) {
-      first_past = kSampleThreads;
-      last_some = -1;
-    }
-    __syncthreads();
-    // the run that the border lies in: two runs a lane
-    const double s0 = 2 * lane < runs ? all_sum[2 * lane] : 0.0, s1 = 2 * lane + 1 < runs ? all_sum[2 * lane + 1] : 0.0;
-    const double upto = inclusive_sum(s0 + s1), total = __shfl_sync(0xffffffffu, upto, 31);
-    const double before_lane = __shfl_up_sync(0xffffffffu, upto, 1);
-    const double c0 = lane ? before_lane : 0.0, c1 = c0 + s0;
-    const double target = u * total;
-    const unsigned past0 = __ballot_sync(0xffffffffu, s0 > 0.0 && c1 > target), past1 = __ballot_sync(0xffffffffu, s1 > 0.0 && upto > target);
-    const unsigned some0 = __ballot_sync(0xffffffffu, s0 > 0.0), some1 = __ballot_sync(0xffffffffu, s1 > 0.0);
-    int run;
-    if (past0 | past1) {
-      const int l = __ffs(past0 | past1) - 1;
-      run = 2 * l + (past0 >> l & 1 ? 0 : 1);
-    } else {   // (u at or above 1, or sums that are not finite): the last that has any weight
-      const int l = 31 - __clz(some0 | some1);
-      run = some0 | some1 ? 2 * l + (some1 >> l & 1 ? 1 : 0) : -1;
-    }
-    const double base = __shfl_sync(0xffffffffu, run & 1 ? c1 : c0, run < 0 ? 0 : run >> 1);
-    if (run >= 0 && run / kSampleWarps == rank) {
-      // its tokens again, a few consecutive ones a thread
-      const int from = run * a.run, upto_token = (int)min((int64_t)from + a.run, (int64_t)a.vocab);
-      const int each = (a.run + kSampleThreads - 1) / kSampleThreads;
-      const int i0 = (int)min((int64_t)from + threadIdx.x * each, (int64_t)upto_token), i1 = min(i0 + each, upto_token);
-      double own = 0.0;
-      for (int i = i0; i < i1; ++i) {
-        const float x = p[i], y = less(i);
-        if (x > y) own += (double)x - (double)y;
-      }
-      const double in_warp = inclusive_sum(own);
-      if (lane == 31) warp_sum[warp] = in_warp;
-      __syncthreads();
-      double before = base;
-      for (int w = 0; w < warp; ++w) before += warp_sum[w];
-      const double prior = __shfl_up_sync(0xffffffffu, in_warp, 1);
-      double c = before + (lane ? prior : 0.0);
-      if (own > 0.0) {
-        atomicMax(&last_some, (int)threadIdx.x);
-        if (before + in_warp > target) atomicMin(&first_past, (int)threadIdx.x);
-      }
-      __syncthreads();
-      if ((int)threadIdx.x == (first_past < kSampleThreads ? first_past : last_some)) {
-        for (int i = i0; i < i1; ++i) {
-          const float x = p[i], y = less(i);
-          if (!(x > y)) continue;
-          token = i;
-          c += (double)x - (double)y;
-          if (c > target) break;
+        for (int e = 0; e < kSampleUnroll; ++e) {
+          const int64_t i = i0 + (int64_t)step * e;
+          x[e] = i < end ? p[i] : 0.f;
+          y[e] = i < end ? less((int)i) : 0.f;
         }
-        a.accepted[b] = n;
-        a.token[b] = token;
+#pragma unroll
+        for (int e = 0; e < kSampleUnroll; ++e)
+          if (x[e] > y[e]) add_difference(sum, x[e], y[e]);
+      }
+      return sum;
+    };
+    const int first = (int)min((int64_t)(rank * kSampleWarps + warp) * a.run, (int64_t)a.vocab);
+    const Twofold sum = warp_sum(add_up(first + lane, (int)min((int64_t)first + a.run, (int64_t)a.vocab), 32));
+    if (lane == 0) run_sum[warp] = sum;
+    cluster.sync();
+    // the run that the border lies in: two runs a lane
+    double base = 0.0, target = 0.0;
+    if (warp == 0) {
+      double s0 = 0.0, s1 = 0.0;
+      if (2 * lane < runs) {
+        const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(&run_sum[2 * lane % kSampleWarps], 2 * lane / kSampleWarps));
+        s0 = (double)x.x + (double)x.y;
+        s1 = (double)x.z + (double)x.w;
+        if (!(s0 > 0.0)) s0 = 0.0;   // (a sum that is NaN too)
+        if (!(s1 > 0.0)) s1 = 0.0;
+      }
+      const double both = s0 + s1, upto = inclusive_sum(both);
+      target = u * __shfl_sync(0xffffffffu, upto, 31);
+      const int at = border_lane(both, upto, target, base);
+      int run = -1;
+      if (at >= 0) {
+        const double of_first = __shfl_sync(0xffffffffu, s0, at), of_second = __shfl_sync(0xffffffffu, s1, at);
+        const bool second = !(of_first > 0.0 && base + of_first > target) && of_second > 0.0;
+        run = 2 * at + second;
+        if (second) base += of_first;
+      }
+      if (lane == 0) s_run = run;
+    }
+    cluster.barrier_arrive();   // the sums have been read
+    __syncthreads();
+    const int run = s_run;
+    if (run >= 0 && run / kSampleWarps == rank) {
+      // its tokens again: a part of them a warp, then a few consecutive ones a lane of one warp, then a token a lane
+      const int begin = run * a.run, end = (int)min((int64_t)begin + a.run, (int64_t)a.vocab);
+      const int part = (a.run + kSampleWarps - 1) / kSampleWarps;
+      auto past = [&](int64_t i) { return (int)min(i, (int64_t)end); };
+      const int mine = past((int64_t)begin + warp * part);
+      const Twofold of_warp = warp_sum(add_up(mine + lane, past((int64_t)mine + part), 32));
+      if (lane == 0) part_sum[warp] = of_warp;
+      __syncthreads();
+      if (warp == 0) {
+        const Twofold x = lane < kSampleWarps ? part_sum[lane] : Twofold{0.f, 0.f};
+        auto border = [&](Twofold sum) {
+          const double own = (double)sum.sum + (double)sum.rest;
+          return max(border_lane(own, base + inclusive_sum(own), target, base), 0);
+        };
+        int from = past((int64_t)begin + border(x) * part), upto = past((int64_t)from + part);
+        if (part > kSampleWalk) {
+          const int each = (part + 31) / 32;
+          auto of_lane = [&](int l) { return (int)min((int64_t)from + (int64_t)l * each, (int64_t)upto); };
+          const int l = border(add_up(of_lane(lane), of_lane(lane + 1), 1)), lane_end = of_lane(l + 1);
+          from = of_lane(l);
+          upto = lane_end;
+        }
+        int token = -1;
+        for (int i0 = from; i0 < upto; i0 += 32) {
+          const int i = i0 + lane;
+          const float x = i < upto ? p[i] : 0.f, y = i < upto ? less(i) : 0.f;
+          const double own = x > y ? (double)x - (double)y : 0.0, sum = base + inclusive_sum(own);
+          const unsigned over = __ballot_sync(0xffffffffu, own > 0.0 && sum > target), some = __ballot_sync(0xffffffffu, own > 0.0);
+          if (over | some) token = i0 + (over ? __ffs(over) - 1 : 31 - __clz(some));
+          if (over) break;
+          base = __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (lane == 0) {
+          a.accepted[b] = n;
+          a.token[b] = token;
+        }
       }
     }
-    cluster.sync();   // the sums have been read
+    cluster.barrier_wait();
     if (run >= 0) return;
   }
   if (rank == 0 && threadIdx.x == 0) {   // a row without any weight
