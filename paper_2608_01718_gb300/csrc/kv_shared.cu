@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_const
 
 // ---- the join ----
 struct Join {
-  int64_t rows;             // of a kv head: tokens x group
+  int rows;                 // of a kv head: tokens x group
   int new_tokens, q_heads, group, head_dim, q_f16;
   int cut;                  // the common part was cut into partial sums (by kv_shared_tc_common.cu)
   int slot_rows;
@@ -97,59 +97,62 @@ constexpr double kSmall = 64e6;   // bytes of K and V
 
 // 32 rows of a kv head a block, a row a lane; each warp four of the dimensions. The common part is one row, in
 // the order of the outputs (not cut) or with four dimensions of neighbouring rows side by side, or partial sums, a block's each, in
-// that order too.
-__global__ void __launch_bounds__(kJoinWarps * 32, 4) join_kernel(const __grid_constant__ Join a) {
+// that order too, of which a lane loads LOADS at once.
+//
+// What bounds it is how many of those loads are in flight: the line of 152 blocks leaves 64 sequences of 32 heads 18 partial sums a
+// row, 20 MB in all. With few blocks the registers are spent on loads (12 at once, two blocks an SM): there 7.6 us after the common
+// part, 12 with six at once; with more than two blocks an SM on warps: 24 sequences of 17 tokens and 16 heads 10.2 us, 13.3 with 12.
+template <int LOADS, int PER_SM>
+__global__ void __launch_bounds__(kJoinWarps * 32, PER_SM) join_kernel(const __grid_constant__ Join a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.head_dim, head = blockIdx.y;
-  const int64_t row = blockIdx.x * (int64_t)32 + lane;   // of the kv head
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int row = blockIdx.x * 32 + lane;                // of the kv head
   const bool mine = row < a.rows;
-  const int64_t token = mine ? row / a.group : 0;
-  const int qh = head * a.group + (int)(row - row / a.group * a.group), seq = (int)(token / a.new_tokens);
-  const int64_t x = token * a.q_heads + qh;              // in the outputs' order
+  const int token = mine ? row / a.group : 0, qh = head * a.group + (mine ? row - token * a.group : 0), seq = token / a.new_tokens;
+  const int64_t x = (int64_t)token * a.q_heads + qh;     // in the outputs' order
+  // (known before the parts are: each was launched after the groups were)
   const int g = mine ? __ldcg(a.group_of + seq) : 0;
+  const int4 span = g > 0 && a.cut ? __ldcg(a.spans + g - 1) : make_int4(0, 0, 0, 0);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   float l = mine ? __ldcg(a.own_lse + x) : -INFINITY;    // base 2
   // where the common part is
-  int c_first = 0, c_last = 0, r = 0;
+  int c_first = 0, c_last = 0, in_slot = 0;
   float other = -INFINITY, top = -INFINITY, sum = 0.f;
   if (g > 0 && a.cut) {
-    const int4 span = __ldcg(a.spans + g - 1);
     const int share = __ldcg(a.line), longer = __ldcg(a.line + 1), base = __ldcg(a.line + 1 + g);
-    const int in_group = (int)(row - (int64_t)span.z * a.new_tokens * a.group);
-    const int tiles = (span.w * a.new_tokens * a.group + kCommonRows - 1) / kCommonRows;
+    const int in_group = row - span.z * a.new_tokens * a.group, tiles = (span.w * a.new_tokens * a.group + kCommonRows - 1) / kCommonRows;
     const int keys = span.y - (span.x & ~15), units = keys <= 0 ? 1 : (keys + kCommonKeys - 1) / kCommonKeys;
     const int begin = base + (head * tiles + in_group / kCommonRows) * (units + kCommonCost) + kCommonCost;
     const int in_longer = longer * (share + 1);
     auto block_of = [&](int cell) { return cell < in_longer ? cell / (share + 1) : longer + (cell - in_longer) / share; };
     c_first = block_of(begin);
     c_last = block_of(begin + units - 1);
-    r = in_group % kCommonRows;
+    in_slot = in_group % kCommonRows;
   }
-  const int64_t slot = (int64_t)a.slot_rows * (D + 2);
-  auto part = [&](int c) { return a.partial + ((int64_t)c * 2 + (c == c_first ? 1 : 0)) * slot; };
+  const int slot = a.slot_rows * (D + 2);
   const bool parts = c_first < c_last;
   const int d = (blockIdx.z * kJoinWarps + warp) * 4, d_in = d < D ? d : 0;   // (warps past the row's end compute, and write nothing)
   const float4 y = mine ? __ldcg(reinterpret_cast<const float4*>(a.own + x * D + d_in)) : make_float4(0.f, 0.f, 0.f, 0.f);
   float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [](float4& to, float4 v, float f) { to.x += v.x * f, to.y += v.y * f, to.z += v.z * f, to.w += v.w * f; };
   if (parts) {
-    constexpr int kLoads = 6;   // in flight, of each kind
-    for (int c0 = c_first; c0 <= c_last; c0 += kLoads) {
-      float2 ml[kLoads];
-      float4 v[kLoads];
+    for (int c0 = c_first; c0 <= c_last; c0 += LOADS) {
+      float2 ml[LOADS];
+      float4 v[LOADS];
 #pragma unroll
-      for (int e = 0; e < kLoads; ++e) {
-        const float* from = part(min(c0 + e, c_last));
-        ml[e] = __ldcg(reinterpret_cast<const float2*>(from + (int64_t)a.slot_rows * D) + r);
-        v[e] = __ldcg(reinterpret_cast<const float4*>(from) + (int64_t)(d_in / 4) * a.slot_rows + r);
+      for (int e = 0; e < LOADS; ++e) {
+        const int c = min(c0 + e, c_last);
+        const float* from = a.partial + (int64_t)(2 * c + (c == c_first ? 1 : 0)) * slot;   // (a block's first triple, its last)
+        ml[e] = __ldcg(reinterpret_cast<const float2*>(from + D * a.slot_rows) + in_slot);
+        v[e] = __ldcg(reinterpret_cast<const float4*>(from + d_in * a.slot_rows) + in_slot);
       }
       float now = top;
 #pragma unroll
-      for (int e = 0; e < kLoads; ++e) now = fmaxf(now, ml[e].x);
+      for (int e = 0; e < LOADS; ++e) now = fmaxf(now, ml[e].x);
       const float to = now == -INFINITY ? 0.f : now, f = exp2_fast(top - to);
       sum *= f;
       z = make_float4(z.x * f, z.y * f, z.z * f, z.w * f);
 #pragma unroll
-      for (int e = 0; e < kLoads; ++e) {
+      for (int e = 0; e < LOADS; ++e) {
         if (c0 + e > c_last) continue;
         const float w = exp2_fast(ml[e].x - to);
         sum += w * ml[e].y;
@@ -319,7 +322,7 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
     e = lc::launch_common(a, c.format, h->num_sms, st);
   }
   if (e != cudaSuccess) return e == cudaErrorNotSupported ? LACACHE_ERR_UNSUPPORTED : LACACHE_ERR_CUDA;
-  j.rows = (int64_t)table->seqs * a.rows;
+  j.rows = table->seqs * a.rows;
   j.new_tokens = a.new_tokens;
   j.q_heads = a.q_heads;
   j.group = a.group;
@@ -345,5 +348,7 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return lc::from_cuda(cudaLaunchKernelEx(&cfg, lc::join_kernel, j));
+  const int64_t blocks = (int64_t)cfg.gridDim.x * cfg.gridDim.y * cfg.gridDim.z;
+  return lc::from_cuda(blocks <= 2 * h->num_sms ? cudaLaunchKernelEx(&cfg, lc::join_kernel<12, 2>, j)
+                                                : cudaLaunchKernelEx(&cfg, lc::join_kernel<6, 4>, j));
 }
