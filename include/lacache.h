@@ -557,11 +557,14 @@ lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_k
  * same pages or in copies: they are read from the pages of the first of them. Lengths, starts, windows and the outputs are as for
  * lacache_kv_attend, and mean whole sequences, the common positions counted in; a sequence may end within them. The result is
  * that of lacache_kv_attend but for roundings. Bounds that do not rise, and lengths past the table, are reported by
- * lacache_kv_sync (and the call runs without groups, or with the lengths cut). Where the table can name no more than 64 MB of K
+ * lacache_kv_sync (and the call runs without groups, or with the lengths cut). The first sequence's row of the table names the
+ * pages of all common positions that any sequence of its group holds, even if it ends before them itself. Where the table can
+ * name no more than 64 MB of K
  * and V in all, every sequence is read for itself, and the groups are not looked at.
  * The workspace is device memory, 16-byte aligned, of lacache_kv_attend_shared_workspace_bytes(h, table, groups, new_tokens,
- * q_heads) (0 for such a small call, and for arguments outside their ranges; of the table, seqs and width are looked at); calls
- * that may overlap, those of two captured graphs among them, have one each.
+ * q_heads) (0 for such a small call, and for arguments outside their ranges; of the table, seqs and width are looked at). Calls on
+ * one handle, which do not overlap, may share it, those in two captured graphs too; calls on several handles that may overlap have
+ * one each.
  * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read bounds, lengths and tables anew. */
 typedef struct {
   int32_t groups;            /* at least 1 */
@@ -589,7 +592,8 @@ typedef struct {
  *     out_j = decay * past_j + sum_r exp(scale * <q_r, k_j> - lse_r)
  * with lse as that call wrote it; a query with lse = -inf has seen nothing and adds nothing. The new tokens' own positions
  * start from 0, whatever past holds there, as everything does if past.data_dev is NULL. Positions from lengths_dev[s] on are
- * not written. out may be past (the same address and strides), or must not overlap it; past.width is at least out.width. A length past
+ * not written. out may be past (the same address and strides), or must not overlap it; past.width is at least out.width. Rows of
+ * out lie apart (no stride is 0 over more than one of them). A length past
  * out.width is reported as an index outside its range (and cut). What a masked position holds never reaches another's weight.
  * decay is finite; the rest is as for lacache_kv_attend. Asynchronous on cuda_stream; may be captured into a CUDA graph. */
 typedef struct {
@@ -618,8 +622,9 @@ lacache_status lacache_kv_weigh(lacache_kv_t* h, int32_t layer, const lacache_kv
  *   new_lengths_dev   [seqs] int32
  *   new_weights       their weights (positions from new_lengths_dev[s] on are not written; data_dev may be NULL)
  * The tokens carry the rotary positions that they were written with: pass append's rope_pos for those that follow. *to names
- * as many sequences and holds keep tokens at least; its pages are none that the sequences of *table use, in this layer (or the
- * result is undefined). Slots behind a sequence's last are left as they were. A length past weights->width, and table entries
+ * as many sequences and holds keep tokens at least; its pages are none that the sequences of *table use, in this layer, and
+ * new_weights does not overlap weights, nor its rows each other (the same array for both is refused, and what overlaps otherwise is
+ * undefined). Slots behind a sequence's last are left as they were. A length past weights->width, and table entries
  * outside their range, are reported by lacache_kv_sync (a length is cut, a token without a page is not copied). 1 <= keep,
  * 0 <= recent <= keep; new_weights->width is at least keep. Asynchronous on cuda_stream; may be captured into a CUDA graph. */
 lacache_status lacache_kv_evict(lacache_kv_t* h, int32_t layer, const lacache_kv_table* table, const int32_t* lengths_dev,
@@ -634,7 +639,8 @@ lacache_status lacache_kv_sync(lacache_kv_t* h);
 
 /* Test support for failure detection: the next `attends` calls of lacache_kv_attend or lacache_kv_attend_shared (its common
  * part) that have many rows (more than 16 a kv head, 32 over 8-bit caches with heads of up to 64; heads of up to 128), or of
- * lacache_kv_weigh that have more than 16, make the block that holds the first keys withhold its loads. The bounded waits for them (about a second) run out, the block records the timeout, frees what it holds and
+ * lacache_kv_weigh that have more than 16, make the block that holds the first keys withhold its loads. The bounded waits for
+ * them (about a second) run out, the block records the timeout, frees what it holds and
  * ends, and lacache_kv_sync reports LACACHE_ERR_DEVICE_TIMEOUT. Nothing faults, and the context stays usable. 0 cancels. */
 lacache_status lacache_kv_inject_stall(lacache_kv_t* h, int32_t attends);
 

@@ -104,12 +104,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(const __grid_con
   constexpr int kSlots = T::kSlots;
   extern __shared__ __align__(1024) unsigned char gbase[];
   const uint32_t base = smem_u32(gbase);
+  pass_begins<FORM>();
   if (base & 1023u) {   // the swizzled tiles start on 1024 bytes (dynamic shared memory does, with none of the static kind)
     if (threadIdx.x == 0) atomicOr(a.status, kAttendTimeout);
     return;
   }
   const uint32_t ring = base;
-  pass_begins<FORM>();
   Tail& t = *reinterpret_cast<Tail*>(gbase + T::kTail);
   volatile uint32_t* abort_flag = &t.abort_flag;
   volatile long long* progress = &t.progress;

@@ -291,7 +291,11 @@ extern "C" lacache_status lacache_kv_evict(lacache_kv_t* h, int32_t layer, const
     return LACACHE_ERR_INVALID_ARG;
   if (table->seqs == 0) return LACACHE_OK;
   if (!lengths_dev || !weights || !weights->data_dev || weights->width < 1 || !kept_dev || !new_lengths_dev ||
-      (new_weights && new_weights->data_dev && new_weights->width < keep))
+      to->pages_dev == table->pages_dev)
+    return LACACHE_ERR_INVALID_ARG;
+  if (new_weights && new_weights->data_dev &&   // (rows of its own: tokens are copied in no order)
+      (new_weights->width < keep || new_weights->data_dev == weights->data_dev || (table->seqs > 1 && new_weights->seq_stride == 0) ||
+       (h->cfg.kv_heads > 1 && new_weights->head_stride == 0)))
     return LACACHE_ERR_INVALID_ARG;
   lc::DeviceGuard guard(h->cfg.device);
   if (!guard.ok()) return LACACHE_ERR_CUDA;

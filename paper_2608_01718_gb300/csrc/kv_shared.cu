@@ -7,6 +7,10 @@
 // sequence's own begin; the own part, by the kernels of kv_attend.cuh and kv_attend_tc.cu; the common part, in which a group
 // stands for a sequence and the new tokens of all of its sequences are its rows, by kv_shared_tc_common.cu (or, few rows or wide
 // heads, kv_attend.cuh); the join. Parts stay fp32 in the workspace. Each kernel is launched while the one before runs.
+//
+// 64 sequences of 1 to 700 tokens of their own behind 6,000 in common (32 heads on 8, d = 128, bf16) take 52 us: some 4 for the
+// groups, 21 for the own parts (3.3 TB/s of them, as an attention of that size alone), 20 for the common part, 7.6 for the join. The
+// same attention without groups reads the common positions 64 times.
 #include <algorithm>
 
 #include "kv_attend.cuh"

@@ -222,6 +222,12 @@ def test_refusals():
         with pytest.raises(L.LacacheError) as e:
             c.kv.evict(c.table, c.len_dev, w, 20, to_bad)
         assert e.value.status == L.LACACHE_ERR_INVALID_ARG
+    # tables and weights in place, and rows that share memory
+    wide = torch.zeros(2, 1, 64, device="cuda")
+    for to_bad, new_weights in ((c.table, None), (target, w), (target, wide.expand(2, 2, 64)), (target, wide[:1].expand(2, 2, 64))):
+        with pytest.raises(L.LacacheError) as e:
+            c.kv.evict(c.table, c.len_dev, w, 20, to_bad, new_weights=new_weights)
+        assert e.value.status == L.LACACHE_ERR_INVALID_ARG
     assert c.kv.evict(c.table[:0], c.len_dev[:0], w[:0], 20, target[:0])[1].shape == (0, 2, 20)
     c.kv.sync()
 

@@ -288,6 +288,13 @@ def test_refusals():
         with pytest.raises(L.LacacheError) as e:
             c.kv.weigh(q, c.table, c.len_dev, lse, **kw)
         assert e.value.status == status
+    # rows that share memory, and in place with other strides
+    for kw in (dict(out=ok[:, :1].expand(1, 2, 64)), dict(weights=torch.zeros(1, 3, 64, device="cuda")[:, ::2], out=ok)):
+        if "weights" in kw:
+            kw["out"] = kw["weights"].as_strided((1, 2, 64), (192, 64, 1))
+        with pytest.raises(L.LacacheError) as e:
+            c.kv.weigh(q, c.table, c.len_dev, lse, **kw)
+        assert e.value.status == L.LACACHE_ERR_INVALID_ARG
     with pytest.raises(L.LacacheError) as e:
         c.kv.weigh(q.half(), c.table, c.len_dev, lse)
     assert e.value.status == L.LACACHE_ERR_UNSUPPORTED
