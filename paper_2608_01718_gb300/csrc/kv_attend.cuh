@@ -99,7 +99,7 @@ struct AttendArgs {
 // place and has the rows of all of its sequences; and the pass over what each sequence has of its own. The passes leave their
 // outputs in fp32, to be joined.
 constexpr int kWhole = 0, kCommon = 1, kOwn = 2;
-constexpr int kCommonRows = 256, kCommonKeys = 128, kCommonCost = 4;   // kCommon on tcgen05: a block's rows, and the line's units
+constexpr int kCommonRows = 256, kCommonKeys = 128, kCommonCost = 2;   // kCommon on tcgen05: a block's rows, and the line's units
 
 constexpr int kAttendWarps = 4;
 constexpr int kAttendThreads = kAttendWarps * 32;

@@ -36,7 +36,7 @@ constexpr int kRows = kCommonRows;           // of q a block
 static_assert(kRows == 2 * kTile && kCommonKeys == kTile, "two tiles of rows");
 constexpr int kSoftmax = 256;                // threads: one a row
 constexpr int kMmaWarp = 8;                  // and 9: one a tile of rows
-constexpr int kCost = kCommonCost;           // a triple's start and end, in units
+constexpr int kCost = kCommonCost;           // a triple's start and end, in units (24 x 17 tokens: 52.8 us so, 54.8 with 4, 55.6 with 9)
 
 template <int FMT, bool QF16, int DP>
 struct Common {

@@ -919,7 +919,7 @@ class KVCache:
         all), from the pages of the first of them. ``lengths`` count whole sequences. Everything else, and the result, as attend."""
         dev = self.device
         t, a, out = self._attention(q, table, lengths, new_tokens, starts, window, scale, out, lse, cuda_stream)
-        groups = shared.shape[0]
+        groups = shared.shape[0] if shared.dim() == 1 else 0
         if groups < 1:
             raise ValueError("shared has a length a group, one at least")
         if bounds is None and groups != 1:

@@ -273,7 +273,7 @@ def test_refusals():
     import ctypes
     c = filled("bf16", [(20, [40, 30])], 2, 64, seed=15)
     q, common = queries(c, "bf16", 4, 1), ints([20])
-    for args, kw in (((common[:0],), {}), ((common.long(),), {}), ((ints([20, 5]),), {}), ((common,), dict(bounds=ints([0, 1, 2]))),
+    for args, kw in (((common[:0],), {}), ((common[0],), {}), ((common.long(),), {}), ((ints([20, 5]),), {}), ((common,), dict(bounds=ints([0, 1, 2]))),
                      ((common,), dict(bounds=torch.tensor([0, 2], dtype=torch.int32))), ((common,), dict(window=-1)),
                      ((common,), dict(lse=torch.empty(2, 4)))):
         with pytest.raises(ValueError):
