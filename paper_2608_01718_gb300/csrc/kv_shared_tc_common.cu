@@ -36,6 +36,7 @@ constexpr int kRows = kCommonRows;           // of q a block
 static_assert(kRows == 2 * kTile && kCommonKeys == kTile, "two tiles of rows");
 constexpr int kSoftmax = 256;                // threads: one a row
 constexpr int kMmaWarp = 8;                  // and 9: one a tile of rows
+constexpr float kFarScore = 100.f;           // above the reference, in powers of two: a row with one is done again
 constexpr int kCost = kCommonCost;           // a triple's start and end, in units (24 x 17 tokens: 52.8 us so, 54.8 with 4, 55.6 with 9)
 
 template <int FMT, bool QF16, int DP>
@@ -461,8 +462,9 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
             }
           };
           // The reference. bf16 weights have fp32's range, so only the first unit that a row sees needs its maximum before its
-          // weights: a later one's moves the reference for the units after it (and what overflows all the same is not finite:
-          // done again). f16 weights need each unit's.
+          // weights: a later one's moves the reference for the units after it. A row with a score further above it than kFarScore is
+          // done again (an infinite reference says so, and nothing moves it): below that its weights, 2^107 a unit at most before
+          // the reference follows, have a finite sum. f16 weights need each unit's maximum.
           auto move_to = [&](float top) {
             const bool move = m == -INFINITY ? top > -INFINITY : top > m + kHeadroom;
             if (i > 0 && __any_sync(0xffffffffu, move)) {
@@ -527,6 +529,7 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
             if constexpr (kSplit) tmem_st16(s_at + c * 32 + 16, lo_term);
           }
           seen_top = fmaxf(tops[0], tops[1]) + shift;
+          if (kSplit && fmaxf(tops[0], tops[1]) > kFarScore) m = INFINITY;
           l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
           tmem_wait_st();
           tc_fence_before();
@@ -589,9 +592,9 @@ __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_ker
           else write_lse<kCommon>(a, at, top, sum);
         };
         if (mine) write_end(b * kTile + r, at_lse, m, l);
-        // a row that is not finite is done again, past what was written; not where its sum of weights is NaN: then a score that
-        // it sees is (masked ones are -infinity), and NaN is its result
-        const bool odd = mine && !(zero.x + zero.y == 0.f) && l <= 3.402823466e+38f;
+        // a row that is not finite is done again, past what was written; not where its sum of weights is NaN though no score was
+        // far above the reference: then one that it sees is (masked ones are -infinity), and NaN is its result
+        const bool odd = mine && (m == INFINITY || (!(zero.x + zero.y == 0.f) && l <= 3.402823466e+38f));
         const int key_end = min(key_begin + count * kTile, walk.sp.hi);
         for (unsigned rows = __ballot_sync(0xffffffffu, odd); rows; rows &= rows - 1) {
           const int src = __ffs(rows) - 1, its = row - lane + src, its_tok = its / a.group, its_qh = head * a.group + its - its_tok * a.group;
