@@ -621,6 +621,7 @@ lacache_status lacache_kv_weigh(lacache_kv_t* h, int32_t layer, const lacache_kv
  *   kept_dev          [seqs x kv_heads x keep] int32: the kept tokens' positions, ascending, then -1
  *   new_lengths_dev   [seqs] int32
  *   new_weights       their weights (positions from new_lengths_dev[s] on are not written; data_dev may be NULL)
+ * new_lengths_dev does not overlap lengths_dev or starts_dev, which are read until the end (LACACHE_ERR_INVALID_ARG).
  * The tokens carry the rotary positions that they were written with: pass append's rope_pos for those that follow. *to names
  * as many sequences and holds keep tokens at least; its pages are none that the sequences of *table use, in this layer, and
  * new_weights does not overlap weights, nor its rows each other (the same array for both is refused, and what overlaps otherwise is

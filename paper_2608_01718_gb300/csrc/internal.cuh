@@ -42,6 +42,11 @@ class DeviceGuard {
 };
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+// Do n bytes at p and m bytes at q share any?
+inline bool overlap(const void* p, int64_t n, const void* q, int64_t m) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return p && q && n > 0 && m > 0 && a < b + (uintptr_t)m && b < a + (uintptr_t)n;
+}
 
 inline lacache_status from_cuda(cudaError_t e) { return e == cudaSuccess ? LACACHE_OK : LACACHE_ERR_CUDA; }
 

@@ -293,6 +293,10 @@ extern "C" lacache_status lacache_kv_evict(lacache_kv_t* h, int32_t layer, const
   if (!lengths_dev || !weights || !weights->data_dev || weights->width < 1 || !kept_dev || !new_lengths_dev ||
       to->pages_dev == table->pages_dev)
     return LACACHE_ERR_INVALID_ARG;
+  // (a sequence's heads read its length while another block writes what is left of it)
+  const int64_t seq_bytes = (int64_t)table->seqs * 4;
+  if (lc::overlap(new_lengths_dev, seq_bytes, lengths_dev, seq_bytes) || lc::overlap(new_lengths_dev, seq_bytes, starts_dev, seq_bytes))
+    return LACACHE_ERR_INVALID_ARG;
   if (new_weights && new_weights->data_dev &&   // (rows of its own: tokens are copied in no order)
       (new_weights->width < keep || new_weights->data_dev == weights->data_dev || (table->seqs > 1 && new_weights->seq_stride == 0) ||
        (h->cfg.kv_heads > 1 && new_weights->head_stride == 0)))

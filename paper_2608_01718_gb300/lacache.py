@@ -981,7 +981,8 @@ class KVCache:
         """Of every sequence and kv head, the last ``recent`` tokens and those of the largest ``weights``, ``keep`` in all, copied in
         order to the pages of the table ``to`` (which the sequences of ``table`` do not use). Returns ``new_lengths`` (int32
         [sequences]), ``kept`` (int32 [sequences x kv_heads x keep]: their positions, then -1) and ``new_weights``
-        [sequences x kv_heads x keep]. The tokens keep the rotary positions that they were written with."""
+        [sequences x kv_heads x keep]. The tokens keep the rotary positions that they were written with. ``new_lengths`` is not
+        ``lengths`` or ``starts``, which are read until the end."""
         t, target, H, dev = self._table(table), self._table(to), self.cfg.kv_heads, self.device
         if not 1 <= keep < 1 << 31 or not 0 <= recent <= keep:
             raise ValueError(f"keep is 1 or more and recent 0 to keep, not {keep} and {recent}")

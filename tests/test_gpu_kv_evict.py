@@ -254,3 +254,17 @@ def test_decoding_goes_on_after_an_eviction():
     want, _, mass, _ = decode.attend(q.double().cpu().numpy(), *rows, [49, 49], 1, 64 ** -0.5)
     assert np.all(np.abs(out.double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -9 * mass)
     assert float(new_weights.sum()) <= float(weights.sum())
+
+
+def test_lengths_are_not_written_over_themselves():
+    c, to = filled("bf16", [40, 9, 30], 2, 64, 16, 20, seed=16)
+    w, target = random_weights(c, 16), torch.from_numpy(to).cuda()
+    store = torch.tensor([40, 9, 30, 0, 0, 0], dtype=torch.int32, device="cuda")
+    starts = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for kw in (dict(new_lengths=store[:3]), dict(new_lengths=store[2:5]), dict(starts=starts, new_lengths=starts)):
+        with pytest.raises(L.LacacheError) as e:
+            c.kv.evict(c.table, store[:3], w, 20, target, **kw)
+        assert e.value.status == L.LACACHE_ERR_INVALID_ARG
+    new_lengths, _, _ = c.kv.evict(c.table, store[:3], w, 20, target, starts=starts, new_lengths=store[3:])
+    assert new_lengths.tolist() == [20, 9, 20] and store[:3].tolist() == [40, 9, 30]
+    c.kv.sync()
