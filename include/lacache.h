@@ -356,7 +356,8 @@ typedef struct {
  *    if none qualifies (u_k >= 1). C is summed to within 2^-40 of itself.
  *  - p_draft == NULL: the drafts were not drawn (the draft model's likeliest tokens, or any others): p_draft(x) = 1.
  *  - status_dev as above: served queries get -1 for both. Rows are probabilities: finite, and not negative.
- * vocab is at most 2^30. Asynchronous on cuda_stream; may be captured into a CUDA graph. */
+ * vocab is at most 2^30. accepted_dev and token_dev overlap neither each other nor an input (LACACHE_ERR_INVALID_ARG where that
+ * is drafts, u or status). Asynchronous on cuda_stream; may be captured into a CUDA graph. */
 lacache_status lacache_verify_sample(int32_t B, int32_t k, int32_t vocab, const lacache_probs* p_target,
                                      const lacache_probs* p_draft, const int32_t* drafts_dev, const float* u_dev,
                                      const uint8_t* status_dev, int32_t* accepted_dev, int32_t* token_dev,

@@ -284,6 +284,13 @@ extern "C" lacache_status lacache_verify_sample(int32_t B, int32_t k, int32_t vo
       !accepted_dev || !token_dev || (p_draft && k > 0 && !p_draft->data_dev))
     return LACACHE_ERR_INVALID_ARG;
   if (vocab > lc::kMaxVocab) return LACACHE_ERR_UNSUPPORTED;
+  // (queries are done in no order)
+  const int64_t out_bytes = (int64_t)B * 4, draft_bytes = out_bytes * k;
+  if (lc::overlap(accepted_dev, out_bytes, token_dev, out_bytes)) return LACACHE_ERR_INVALID_ARG;
+  for (const int32_t* out : {accepted_dev, token_dev})
+    if (lc::overlap(out, out_bytes, drafts_dev, draft_bytes) || lc::overlap(out, out_bytes, u_dev, draft_bytes + out_bytes) ||
+        lc::overlap(out, out_bytes, status_dev, B))
+      return LACACHE_ERR_INVALID_ARG;
   lc::SampleArgs a = {};
   a.k = k;
   a.vocab = vocab;

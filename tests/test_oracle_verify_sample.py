@@ -80,3 +80,18 @@ def test_host_tensors_are_refused(name):
     with pytest.raises(ValueError):
         L.lacache_verify_sample(x, None, torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, 2), torch.zeros(1, dtype=torch.int32),
                                 torch.zeros(1, dtype=torch.int32))
+
+
+def test_outputs_over_each_other_or_the_inputs_are_refused():
+    build.build()
+    lib, ref = L.load(), ctypes.addressof
+    rows = L.lacache_probs(1 << 20, 12, 4)
+    good = dict(drafts=1024, u=2048, status=4096, accepted=8192, token=8192 + 12)      # three queries, two drafts
+
+    def call(**kw):
+        a = {**good, **kw}
+        return lib.lacache_verify_sample(3, 2, 4, ref(rows), None, a["drafts"], a["u"], a["status"], a["accepted"], a["token"], None)
+
+    for bad in (dict(token=8192), dict(token=8192 + 8), dict(accepted=1024), dict(accepted=1024 + 20), dict(token=1024 - 8),
+                dict(token=2048 + 32), dict(accepted=4096), dict(token=4096 - 8)):
+        assert call(**bad) == L.LACACHE_ERR_INVALID_ARG, bad
