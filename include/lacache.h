@@ -353,7 +353,7 @@ typedef struct {
  *  - token_dev[b] is drawn at position n: the first i with C_i > u_k * C_vocab, where C_i sums w_0 .. w_i, and
  *    w = max(p_target - p_draft, 0) after a refusal, w = p_target otherwise (the window's end, or a refusal whose w is all
  *    zeros). A NaN or negative weight counts as none; a row without any weight gives -1. The last token of any weight is taken
- *    if none qualifies (u_k >= 1). C is summed to within 2^-40 of itself.
+ *    if none qualifies (u_k >= 1). C is summed to within 2^-40 of itself (2^-36 past 2^25 tokens).
  *  - p_draft == NULL: the drafts were not drawn (the draft model's likeliest tokens, or any others): p_draft(x) = 1.
  *  - status_dev as above: served queries get -1 for both. Rows are probabilities: finite, and not negative.
  * vocab is at most 2^30. accepted_dev and token_dev overlap neither each other nor an input (LACACHE_ERR_INVALID_ARG where that

@@ -44,19 +44,24 @@ __global__ void __launch_bounds__(kVerifyWarps * 32)
 //
 // Both decisions are those of the real numbers but for the last bits of C: u q is a product of 24-bit numbers, exact in fp64; a
 // difference of two fp32 is held exactly as two (the rounded difference and its rounding error; D. Knuth, "The Art of Computer
-// Programming", vol. 2, 4.2.2), sums of them as a leading sum and the sum of its rounding errors (some 2^-45 of the whole),
-// and C_i near the border in fp64. In fp32 alone, sums over 10^5 tokens would draw a neighbour of the token in some percent
-// of the calls; in fp64 alone, the differences and sums of a row of 10^5 take longer than reading it.
+// Programming", vol. 2, 4.2.2), sums of them as a leading sum and the sum of its rounding errors, and C_i near the border in fp64.
+// That sum of errors is rounded too, the more the longer it gets, so it is kept short: eight terms, then eight such sums, whose
+// errors go back into a leading sum each time, then fp64. With u = 2^-24 the bounds, in u^2 = 2^-48 of the sum, are 43 for eight
+// terms (their errors reach k u of it after k terms; each is rounded in itself and in its addition), 70 for eight sums, 40 for the
+// five steps over a warp's lanes, 1 for a long sum's way back from fp64: 2^-40.7. fp64 adds 2^-67 for every token of the
+// vocabulary: 2^-40 in all up to 2^25 tokens, 2^-36 at 2^30. (One running sum and its errors, without those steps, lost 2^-33 of
+// rows with one large and 10^5 equal small numbers.) In fp32 alone, sums over 10^5 tokens would draw a
+// neighbour of the token in some percent of the calls; in fp64 alone, the differences and sums of a row of 10^5 take longer than reading it.
 //
 // A cluster of 1 to 8 blocks a query, each warp a run of consecutive tokens, with sixteen loads in flight a lane. The runs'
 // sums are exchanged through the cluster's shared memory; the block that holds the border adds its run again, a part a warp, and
 // one warp looks for the token in that part. fp64 takes 16 cycles of an SM an instruction, so one warp a block takes those steps:
-// by all warps they were a third of the time. 64 queries of 16 drafts and 100,003 tokens, two rows of one position read: 18.2 us
-// (2.8 TB/s); one query of 32,000 tokens 8.5 us, the latency of the chain from the drafts to the token. What bounds both is that
+// by all warps they were a third of the time. 64 queries of 16 drafts and 100,003 tokens, two rows of one position read: 17.3 us
+// (3.0 TB/s); one query of 32,000 tokens 7.8 us, the latency of the chain from the drafts to the token. What bounds both is that
 // chain: with twice or half the loads in flight the times are the same.
 constexpr int kSampleThreads = 256, kSampleWarps = kSampleThreads / 32, kMaxCluster = 8;
-constexpr int kSampleUnroll = 8;
-constexpr int kSampleWalk = 64;   // of a part, walked 32 tokens at a time; a longer one is cut further first (196 tokens: 18.2 us so, 19.9 walked)
+constexpr int kSampleUnroll = 8, kSampleTurns = 8;   // terms of a sum, and sums, before their errors are settled
+constexpr int kSampleWalk = 64;   // of a part, walked 32 tokens at a time; a longer one is cut further first (196 tokens: 8% faster so)
 constexpr int kMaxVocab = 1 << 30, kSampleResident = 152 * 8;
 
 struct Probs {
@@ -78,19 +83,27 @@ struct SampleArgs {
 struct Twofold {
   float sum, rest;
 };
-// a + x - y for x > y >= 0
-__device__ __forceinline__ void add_difference(Twofold& a, float x, float y) {
+// x - y, exactly
+__device__ __forceinline__ Twofold difference(float x, float y) {
   const float d = __fsub_rn(x, y), b = __fsub_rn(d, x);
-  const float d_err = __fsub_rn(__fsub_rn(x, __fsub_rn(d, b)), __fadd_rn(y, b));
-  const float s = __fadd_rn(a.sum, d), c = __fsub_rn(s, a.sum);
-  const float s_err = __fadd_rn(__fsub_rn(a.sum, __fsub_rn(s, c)), __fsub_rn(d, c));
-  a.sum = s;
-  a.rest = __fadd_rn(a.rest, __fadd_rn(s_err, d_err));
+  return Twofold{d, __fsub_rn(__fsub_rn(x, __fsub_rn(d, b)), __fadd_rn(y, b))};
 }
 __device__ __forceinline__ Twofold plus(Twofold a, Twofold b) {
   const float s = __fadd_rn(a.sum, b.sum), c = __fsub_rn(s, a.sum);
   const float s_err = __fadd_rn(__fsub_rn(a.sum, __fsub_rn(s, c)), __fsub_rn(b.sum, c));
   return Twofold{s, __fadd_rn(__fadd_rn(a.rest, b.rest), s_err)};
+}
+// a + d where d.rest is at most half a last bit of d.sum: the errors of this addition first
+__device__ __forceinline__ void add(Twofold& a, Twofold d) {
+  const float s = __fadd_rn(a.sum, d.sum), c = __fsub_rn(s, a.sum);
+  const float s_err = __fadd_rn(__fsub_rn(a.sum, __fsub_rn(s, c)), __fsub_rn(d.sum, c));
+  a.sum = s;
+  a.rest = __fadd_rn(a.rest, __fadd_rn(s_err, d.rest));
+}
+// The same sum with rest at most half a last bit of the leading one (exact: rest is smaller than it).
+__device__ __forceinline__ Twofold settled(Twofold a) {
+  const float s = __fadd_rn(a.sum, a.rest);
+  return Twofold{s, __fsub_rn(a.rest, __fsub_rn(s, a.sum))};
 }
 __device__ __forceinline__ Twofold warp_sum(Twofold x) {
 #pragma unroll
@@ -166,21 +179,43 @@ __global__ void __launch_bounds__(kSampleThreads) verify_sample_kernel(const __g
     const int one = attempt == 0 && !a.draft.data ? refused : -1;   // where q is 1, if it has no row
     auto less = [&](int i) { return q ? q[i] : i == one ? 1.f : 0.f; };
     // tokens i, i + step, ... before `end`
-    auto add_up = [&](int i0, int end, int step) {
-      Twofold sum = {0.f, 0.f};
-      for (; i0 < end; i0 += step * kSampleUnroll) {
-        float x[kSampleUnroll], y[kSampleUnroll];
+    auto add_up = [&](int i, int end, int step) {
+      auto short_sum = [&](int i0, int end) {   // of kSampleUnroll x kSampleTurns terms at most
+        Twofold all = {0.f, 0.f};
+#pragma unroll 1
+        for (; i0 < end; i0 += step * kSampleUnroll) {
+          float x[kSampleUnroll], y[kSampleUnroll];
 #pragma unroll
-        for (int e = 0; e < kSampleUnroll; ++e) {
-          const int64_t i = i0 + (int64_t)step * e;
-          x[e] = i < end ? p[i] : 0.f;
-          y[e] = i < end ? less((int)i) : 0.f;
+          for (int e = 0; e < kSampleUnroll; ++e) {
+            const int64_t i = i0 + (int64_t)step * e;
+            x[e] = i < end ? p[i] : 0.f;
+            y[e] = i < end ? less((int)i) : 0.f;
+          }
+          Twofold sum;
+#pragma unroll
+          for (int e = 0; e < kSampleUnroll; ++e) {
+            const bool some = x[e] > y[e];
+            const Twofold d = difference(some ? x[e] : 0.f, some ? y[e] : 0.f);
+            if (e == 0) sum = d;
+            else add(sum, d);
+          }
+          add(all, settled(sum));
         }
-#pragma unroll
-        for (int e = 0; e < kSampleUnroll; ++e)
-          if (x[e] > y[e]) add_difference(sum, x[e], y[e]);
+        return settled(all);
+      };
+      const int64_t each = (int64_t)step * kSampleUnroll * kSampleTurns;
+      Twofold all = short_sum(i, (int)min((int64_t)end, i + each));
+      if (i + each < end) {   // (a loop of its own: fp64 in the short sums' loop, even if it is not reached, was 5 us of 22 on 64 queries)
+        double whole = (double)all.sum + (double)all.rest;
+#pragma unroll 1
+        for (int64_t at = i + each; at < end; at += each) {
+          all = short_sum((int)at, (int)min((int64_t)end, at + each));
+          whole += (double)all.sum + (double)all.rest;
+        }
+        all.sum = (float)whole;
+        all.rest = (float)(whole - (double)all.sum);
       }
-      return sum;
+      return all;
     };
     const int first = (int)min((int64_t)(rank * kSampleWarps + warp) * a.run, (int64_t)a.vocab);
     const Twofold sum = warp_sum(add_up(first + lane, (int)min((int64_t)first + a.run, (int64_t)a.vocab), 32));
@@ -301,7 +336,7 @@ extern "C" lacache_status lacache_verify_sample(int32_t B, int32_t k, int32_t vo
   a.status = status_dev;
   a.accepted = accepted_dev;
   a.token = token_dev;
-  // as many blocks a query as leave each 1,024 tokens, and all of them resident at once
+  // as many blocks a query as leave each 1,024 tokens, eight an SM at most
   a.blocks = 1;
   while (a.blocks < lc::kMaxCluster && vocab / (2 * a.blocks) >= 1024 && (int64_t)B * 2 * a.blocks <= lc::kSampleResident)
     a.blocks *= 2;

@@ -191,3 +191,57 @@ def test_wrong_tensors_are_refused():
             L.lacache_verify_sample(*args)
     with pytest.raises(ValueError):
         L.lacache_verify_sample(*good, status=torch.zeros(2, dtype=torch.int32, device="cuda"))
+
+
+def near_borders(V, count, seed, head):
+    """A row of V multiples of 2^-42 (fp32 values), one of 0.7 at `head`, the last 0, the others alike, each 6.45 times the last bit of
+    0.7, and `count` u's whose borders lie 9 to 10 multiples before or behind u C, which is 2^-39 C: (row, u, tokens)."""
+    rng = np.random.default_rng(seed)
+    n = np.full(V, 6 * 2 ** 18 + 117_963)
+    n[head], n[V - 1] = int(np.float32(0.7) * 2.0 ** 42), 0
+    upto, total = np.cumsum(n), int(n.sum())
+    u, tokens = [], []
+    for x, i in enumerate(np.sort(rng.choice(V // 3 - 2, count, replace=False)).tolist()):
+        i = 3 * i + 1                                        # (pairs i, i + 1 that share no token)
+        if i in (head - 1, head):
+            i = head + 1
+        U = max(1, round(int(upto[i]) * 2 ** 24 / total))
+        past = U * total >> 24                               # u C, rounded down
+        below = x % 2 == 0                                   # C_i below u C: the token is the next
+        shift = (past - 9 if below else past + 10) - int(upto[i])
+        n[i] += shift
+        n[i + 1] -= shift
+        u.append(U * 2.0 ** -24)
+        tokens.append(i + below)
+    row = (n * 2.0 ** -42).astype(np.float32)
+    assert int(n.sum()) == total and n[:-1].min() > 0 and np.array_equal(row.astype(np.float64) * 2.0 ** 42, n)
+    upto = np.cumsum(n)                                      # in 2^-42, and u C in 2^-66
+    for x, i in zip(u, tokens):
+        assert (i == 0 or int(upto[i - 1]) << 24 <= int(x * 2 ** 24) * total) and int(upto[i]) << 24 > int(x * 2 ** 24) * total
+    return row, u, tokens
+
+
+@pytest.mark.parametrize("V,copies", [(262_147, 1), (131_072, 16), (262_147, 16), (1 << 20, 1), (1 << 20, 16)])
+@pytest.mark.parametrize("head", [0, 77_777])
+@pytest.mark.parametrize("residual", [False, True])
+def test_borders_nearer_than_a_running_sum_holds(V, copies, head, residual):
+    """One token of 0.7 and a flat tail: what a long sum and its rounding errors lose at every term shows. Both signs of a border 2^-39 C
+    away, which errors of 2^-40 in C_i and in C do not reach; with few queries (eight blocks each) and with many (one)."""
+    row, u, tokens = near_borders(V, 40, V + head, head)
+    B = len(tokens) * copies
+    assert (B > 608) == (copies > 1)
+    target = torch.from_numpy(row).cuda()
+    us = torch.tensor(u, dtype=torch.float32, device="cuda").repeat(copies).view(-1, 1)
+    if residual:                                             # the same weights as differences, after a draft of weight 0 was refused
+        less = torch.randint(0, 1 << 22, (V,), device="cuda").double() * 2.0 ** -42
+        less[head] = 0.125
+        p = target.double() + less
+        less[V - 1] += 2.0 ** -21
+        q = less.float()
+        assert torch.equal(p.float().double(), p) and torch.equal(q.double(), less)
+        got = call(p.float().expand(B, 2, V), q.expand(B, 1, V), torch.full((B, 1), V - 1, dtype=torch.int32, device="cuda"),
+                   torch.cat((torch.full_like(us, 1 - 2.0 ** -24), us), 1))
+    else:
+        got = call(target.expand(B, 1, V), None, torch.zeros(B, 0, dtype=torch.int32, device="cuda"), us)
+    assert got[0].tolist() == [0] * B
+    assert got[1].tolist() == tokens * copies
