@@ -74,8 +74,7 @@ __global__ void __launch_bounds__(kWeighThreads, WeighConfig<FMT, DP, NT>::kBloc
     head_row = (int64_t)ahead.head * a.page_size;
     head_k = a.pk + head_row * row_bytes;
     past = w.past ? w.past + ahead.seq * w.past_seq + ahead.head * w.past_head : nullptr;
-    const Span sp = span_of(a, ahead.seq, W::kKeys);
-    first_seen = sp.lo;
+    first_seen = weigh_first(a, ahead.seq);
     in_batch = 0;
     look_up(ahead.unit * W::kKeys, ids);
   };
@@ -89,10 +88,10 @@ __global__ void __launch_bounds__(kWeighThreads, WeighConfig<FMT, DP, NT>::kBloc
         const int k0 = key + 16 * s;
         const int page = __shfl_sync(0xffffffffu, ids[s], in_batch);
         const bool there = (unsigned)page < (unsigned)a.pages;
-        if (!there && k0 < ahead.len && lane == 0) atomicOr(a.status, kBadIndex);
+        if (!there && k0 < ahead.len && k0 + 15 >= first_seen && lane == 0) atomicOr(a.status, kBadIndex);
         const uint32_t bit = 1u << (ahead_slot * W::kSub + s);
         bad_slots = there ? bad_slots & ~bit : bad_slots | bit;
-        if (!there || k0 + 16 <= first_seen) continue;   // (not seen by any row: what the stage holds is not looked at)
+        if (!there || k0 + 15 < first_seen) continue;   // (not seen by any row: what the stage holds is not looked at)
         const int slot = k0 - page_of(k0) * a.page_size;
         const unsigned char* from = head_k + page * a.page_bytes + (int64_t)slot * row_bytes;
         const uint32_t kd = to + s * W::kTileBytes;
@@ -209,7 +208,7 @@ __global__ void __launch_bounds__(kWeighThreads, WeighConfig<FMT, DP, NT>::kBloc
     if (i < 0) continue;   // the copies' head start
     if (fresh) {
       load_rows();
-      seen_from = span_of(a, at.seq, W::kKeys).lo;
+      seen_from = weigh_first(a, at.seq);
       fresh = false;
     }
     copy_wait<W::kStages - 1>();
@@ -221,7 +220,7 @@ __global__ void __launch_bounds__(kWeighThreads, WeighConfig<FMT, DP, NT>::kBloc
     for (int b = 0; b < W::kSub; ++b) {
       const int k0 = key + 16 * b;
       float sum0 = 0.f, sum1 = 0.f;
-      if (k0 <= max_pos && k0 + 16 > seen_from && !(bad_slots >> (slot * W::kSub + b) & 1)) {
+      if (k0 <= max_pos && k0 + 15 >= seen_from && !(bad_slots >> (slot * W::kSub + b) & 1)) {
         const unsigned char* kt = st + b * W::kTileBytes;
         float s[NT][4];
 #pragma unroll

@@ -81,6 +81,11 @@ __device__ __forceinline__ int weigh_start(const AttendArgs& a, int part, int pa
   at.unit = (u - base) - at.head * at.units;
   return mine;
 }
+// The first position that any of a sequence's rows sees (INT_MAX: none is). Pages before it are not looked at.
+__device__ __forceinline__ int weigh_first(const AttendArgs& a, int seq) {
+  const Span sp = span_of(a, seq, 1);
+  return sp.lo < sp.hi ? sp.lo : INT_MAX;
+}
 // Lengths outside their range, once a launch.
 __device__ __forceinline__ void weigh_check(const AttendArgs& a) {
   if (blockIdx.x == 0) {

@@ -165,10 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       const bool there = (unsigned)page < (unsigned)a.pages;
       const int64_t row = there ? page * a.page_rows + head_row + (from - index * a.page_size) : -1;   // of the pool
       const unsigned wrong = __ballot_sync(0xffffffffu, !there && from < p.len && lane < W::kKeys / 16);
-      if (me == 0 && lane == 0) {
-        t.bad[set] = wrong;
-        if (wrong) atomicOr(a.status, kBadIndex);
-      }
+      if (me == 0 && lane == 0) t.bad[set] = wrong;
       if (live.x < live.y) {
         if constexpr (W::kEight) {
           // eight loads in flight, each sixteen codes of a row
@@ -297,6 +294,10 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       const int2 live = tiles_of(at);
       ok = wait(t.k_full[units & 1], (units >> 1) & 1);
       ok = __all_sync(0xffffffffu, ok);
+      if (ok && lane == 0) {   // a page that is none: is the last of them seen? (here, where registers are left)
+        const uint32_t bad = t.bad[units & 1];
+        if (bad && at.unit * W::kKeys + (31 - __clz(bad)) * 16 + 15 >= weigh_first(a, at.seq)) atomicOr(a.status, kBadIndex);
+      }
       for (int i = live.x; ok && i < live.y; ++i, ++tiles) {
         const int slot = tiles % W::kTiles, buffer = tiles & 1;
         ok = wait(t.q_full[slot], (tiles / W::kTiles) & 1) && (tiles < 2 || wait(t.s_empty[buffer], (tiles / 2 - 1) & 1));

@@ -300,3 +300,31 @@ def test_refusals():
     assert e.value.status == L.LACACHE_ERR_UNSUPPORTED
     assert c.kv.weigh(q[:0], c.table[:0], c.len_dev[:0], lse[:0]).shape == (0, 2, c.table.shape[1] * 16)
     c.kv.sync()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f16", "e4m3", "int8"])
+@pytest.mark.parametrize("head_dim,q_heads,new", [(64, 2, 1), (64, 16, 2), (128, 8, 9), (256, 16, 3)])
+def test_pages_that_no_query_sees_need_not_be_there(fmt, head_dim, q_heads, new):
+    """A window's older pages, and those before a start, may have been given to others: as for the attention, no page of theirs is
+    looked at."""
+    dtype = fmt if fmt in TORCH else "bf16"
+    c = Filled(fmt, [300, 90, 33, 0, 513], 2, head_dim, 16, seed=17)
+    q = queries(c, dtype, q_heads, new)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    past = torch.rand(5, 2, 513, device="cuda")
+    for kw, first in ((dict(window=40), [max(0, n - new + 1 - 40) for n in c.lengths]),
+                      (dict(starts=torch.tensor([299, 17, 33, 0, 512], dtype=torch.int32, device="cuda")), [299, 17, 33, 0, 512])):
+        c.kv.attend(q, c.table, c.len_dev, new_tokens=new, lse=lse, **kw)
+        want = c.kv.weigh(q, c.table, c.len_dev, lse, weights=past, out=past.clone(), new_tokens=new, **kw)
+        c.kv.sync()
+        table = c.table.clone()
+        for s, x in enumerate(first):
+            # (no key of the third is seen from its start on)
+            table[s, :x // 16 if x < c.lengths[s] else table.shape[1]] = -1 if s % 2 else 1 << 29
+        again = torch.empty_like(lse)
+        if "window" in kw:
+            c.kv.attend(q, table, c.len_dev, new_tokens=new, lse=again, **kw)
+            assert torch.equal(again, lse)
+        got = c.kv.weigh(q, table, c.len_dev, lse, weights=past, out=past.clone(), new_tokens=new, **kw)
+        c.kv.sync()
+        assert torch.equal(got, want)
