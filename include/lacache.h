@@ -559,9 +559,9 @@ lacache_status lacache_kv_attend(lacache_kv_t* h, int32_t layer, const lacache_k
  * lacache_kv_attend, and mean whole sequences, the common positions counted in; a sequence may end within them. The result is
  * that of lacache_kv_attend but for roundings. Bounds that do not rise, and lengths past the table, are reported by
  * lacache_kv_sync (and the call runs without groups, or with the lengths cut). The first sequence's row of the table names the
- * pages of all common positions that any sequence of its group holds, even if it ends before them itself. Where the table can
- * name no more than 64 MB of K
- * and V in all, every sequence is read for itself, and the groups are not looked at.
+ * pages of the common positions from the first that any sequence of its group sees to the last, even if it ends before them
+ * itself. Where the table can name no more than 64 MB of K and V in all, every sequence is read for itself, and the groups are
+ * not looked at.
  * The workspace is device memory, 16-byte aligned, of lacache_kv_attend_shared_workspace_bytes(h, table, groups, new_tokens,
  * q_heads) (0 for such a small call, and for arguments outside their ranges; of the table, seqs and width are looked at). Calls on
  * one handle, which do not overlap, may share it, those in two captured graphs too; calls on several handles that may overlap have

@@ -60,8 +60,8 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_const
     const int len = min(max(a.lengths[s], 0), a.max_len), start = a.starts ? a.starts[s] : 0;
     int seen = max(start, 0);
     if (a.window > 0) seen = max(seen, len - a.new_tokens - a.window + 1);   // (window < 2^30: no overflow)
-    lo = min(lo, seen);
-    hi = max(hi, min(len, common));
+    const int last = min(len, common);
+    if (seen < last) lo = min(lo, seen), hi = max(hi, last);   // (an empty one, or one past its window, asks for no pages)
     a.own_starts[s] = max(start, common);
     a.group_of[s] = common > 0 ? g + 1 : 0;
   }
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kGroupThreads) group_kernel(const __grid_const
     atomicMax(&s_hi, hi);
   }
   __syncthreads();
-  // (without common positions: no rows either)
+  // (without common positions: no rows either; none seen: [0, 0))
   if (threadIdx.x == 0) a.spans[g] = make_int4(min(s_lo, s_hi), s_hi, first, common > 0 ? end - first : 0);
 }
 

@@ -1,0 +1,25 @@
+"""Shared prefixes: what the rows of the table have to name."""
+import pytest
+import torch
+
+from test_gpu_kv_shared import check, filled, ints, library, queries  # noqa: F401 (the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt,dtype", [("bf16", "bf16"), ("e4m3", "f16")])
+@pytest.mark.parametrize("head_dim,q_heads", [(64, 2), (64, 8), (256, 2)])
+def test_sequences_that_see_nothing_ask_for_no_pages(fmt, dtype, head_dim, q_heads):
+    """A batch padded with empty sequences, and one that is all before its start, behind a prefix whose first pages have left every
+    sequence's window."""
+    c = filled(fmt, [(700, [760, 0, 730, 745, 0, 710, 90, 701])], 2, head_dim, seed=31)
+    starts = [0, 0, 0, 0, 0, 0, 90, 0]
+    q = queries(c, dtype, q_heads, 1)
+    kw = dict(starts=ints(starts), window=300)
+    want, _ = check(c, dtype, q_heads, starts=starts, window=300)
+    c.table[:, :(701 - 300) // c.page] = 1 << 29
+    lse = torch.empty(q.shape[:2], device="cuda")
+    got = c.kv.attend_shared(q, c.table, c.len_dev, ints(c.common), bounds=ints(c.bounds), lse=lse, **kw)
+    c.kv.sync()
+    assert torch.equal(got, want)
+    assert bool(torch.isneginf(lse[ints([1, 4, 6]).long()]).all())
