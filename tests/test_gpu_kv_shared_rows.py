@@ -23,3 +23,16 @@ def test_sequences_that_see_nothing_ask_for_no_pages(fmt, dtype, head_dim, q_hea
     c.kv.sync()
     assert torch.equal(got, want)
     assert bool(torch.isneginf(lse[ints([1, 4, 6]).long()]).all())
+
+
+@pytest.mark.parametrize("fmt,dtype", [("bf16", "bf16"), ("f16", "f16"), ("int8", "bf16")])
+@pytest.mark.parametrize("head_dim,q_heads,new", [(64, 2, 1), (128, 8, 3), (64, 8, 9), (192, 4, 2)])
+@pytest.mark.parametrize("length", [0, 1, 50, 399])
+def test_a_first_sequence_that_ends_before_the_common_positions(fmt, dtype, head_dim, q_heads, new, length):
+    """Its row of the table names their pages all the same."""
+    c = filled(fmt, [(400, [420, 410, 401, 450]), (90, [100, 95])], 2, head_dim, seed=32)
+    for s in (0, 4):
+        c.lengths[s] = min(length, c.common[s // 4] - 1)
+        c.len_dev[s] = c.lengths[s]
+    check(c, dtype, q_heads, new)
+    check(c, dtype, q_heads, new, window=100)
