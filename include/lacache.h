@@ -532,10 +532,11 @@ lacache_status lacache_kv_read(lacache_kv_t* h, int32_t layer, const lacache_kv_
  * s_j = scale * <q, k_j>:
  *     out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + log(sum_j exp(s_j - m)),   m = max_j s_j
  * A query that sees nothing (an empty sequence, p < 0, a start past it) gets a row of zeros and lse = -inf. What a masked
- * position holds never reaches the result. new_tokens is 1..512; scale is finite; lse_dev ([seqs * new_tokens x q_heads])
- * may be NULL. out does not overlap q (which may be read again once a row of out is written; the same address is
- * LACACHE_ERR_INVALID_ARG). A table reaches at most 2^30 positions here. dtype is q's and out's: bf16 or f16, that of the
- * cache in the 16-bit formats. seqs = 0 does nothing.
+ * position holds never reaches the result. Weights are held to 11 bits or more; over f16 caches, and over 8-bit ones with few rows
+ * (there weights times the values' scales), those below 2^-21 of a row's largest to 2^-32 of that. new_tokens is 1..512; scale
+ * is finite; lse_dev ([seqs * new_tokens x q_heads]) may be NULL. out does not overlap q (which may be read again once a row of
+ * out is written; the same address is LACACHE_ERR_INVALID_ARG). A table reaches at most 2^30 positions here. dtype is q's and
+ * out's: bf16 or f16, that of the cache in the 16-bit formats. seqs = 0 does nothing.
  * Asynchronous on cuda_stream; may be captured into a CUDA graph, whose replays read the lengths and tables anew. */
 typedef struct {
   int32_t new_tokens;

@@ -32,7 +32,9 @@
 // over the lanes. (f16 weights have their full 11 bits down to 2^-21 of the largest that way; with a reference at the
 // maximum, keys of small weight and large values lost some of theirs.) Weights: f16 for f16 and 8-bit caches (11
 // bits); on a bf16 cache, whose products need bf16 weights of 8 bits, a weight is split in two bf16 terms (16 bits), as
-// one alone would add an error as large as the output's own rounding.
+// one alone would add an error as large as the output's own rounding. An f16 weight below 2^-21 of the largest is off by up to
+// 2^-32 of it (the largest is 2^7 or more, and 2^-25 half of f16's last step; 2^-25 in a part that is done again, as below): that
+// shows where the keys that outweigh all others have values of 0.
 //
 // Sums that are not finite, or past 2^110. A warp that finds one at a triple's end does its part of it again with weights of at
 // most 1, and with V's values that are no finite numbers taken out of the tiles and multiplied in fp32 for the rows that see
