@@ -1405,11 +1405,11 @@ cudaError_t launch_one(AttendArgs a, int num_sms, cudaStream_t st) {
 
 template <int FMT, int FORM = kWhole>
 cudaError_t launch_format(const AttendArgs& a, int num_sms, cudaStream_t st) {
-  // tiles of 32 rows where takes_tc leaves so many to this kernel
-  constexpr bool kEight = FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8;
+  // tiles of 32 rows where takes_tc leaves so many to this kernel (of a group's common part kv_shared_tc_common.cu has them)
+  constexpr bool kWide = (FMT == LACACHE_KV_E4M3 || FMT == LACACHE_KV_INT8) && FORM != kCommon;
   const int64_t rows = FORM == kCommon ? (int64_t)a.rows * a.table.seqs / a.groups : a.rows;   // (of a group, on average)
-  const int dp = padded_dim(a.head_dim), nt = rows <= 8 ? 1 : rows <= 16 || dp > 64 || !kEight ? 2 : 4;
-  if constexpr (kEight) {
+  const int dp = padded_dim(a.head_dim), nt = rows <= 8 ? 1 : rows <= 16 || dp > 64 || !kWide ? 2 : 4;
+  if constexpr (kWide) {
     if (nt == 4) return launch_one<FMT, 64, 4, FORM>(a, num_sms, st);
   }
   switch (dp * 8 + nt) {

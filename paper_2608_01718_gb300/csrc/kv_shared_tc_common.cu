@@ -67,14 +67,6 @@ struct Common {
   static constexpr uint32_t kS = 0, kO = 2 * kTile;        // TMEM columns: an S a tile of rows, then an O
 };
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
 template <int FMT, bool QF16, int DP>
 __global__ void __launch_bounds__(Common<FMT, QF16, DP>::kThreads, 1) common_kernel(const __grid_constant__ AttendArgs a) {
   using T = Common<FMT, QF16, DP>;

@@ -32,7 +32,7 @@ struct WeighConfig {
   static constexpr int kStages = kSub * kTileBytes > 4096 ? 2 : kSub * kTileBytes > 2048 ? 4 : 7;
   static constexpr int kRing = kStages * kStageBytes;                 // of a warp
   static constexpr int kSmem = kWeighWarps * kRing;
-  static constexpr int kBlocks = NT == 4 ? 2 : 3;
+  static constexpr int kBlocks = 3;                                   // an SM holds
 };
 
 template <int FMT, int DP, int NT>

@@ -63,13 +63,6 @@ template <int ROWS>
 __device__ __forceinline__ uint32_t unit_of(int r, int u) {
   return (uint32_t)((u >> 3) * (ROWS * 128) + r * 128 + (((u & 7) ^ (r & 7)) << 4));
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
 
 // The tiles of rows that see any of the keys [key, key + KEYS): [first, end).
 template <int KEYS, int ROWS>
