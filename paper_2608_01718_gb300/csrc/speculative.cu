@@ -234,6 +234,7 @@ __global__ void __launch_bounds__(kSampleThreads) verify_sample_kernel(const __g
       }
       const double both = s0 + s1, upto = inclusive_sum(both);
       target = u * __shfl_sync(0xffffffffu, upto, 31);
+      if (!(u < 1.0)) target = INFINITY;   // none qualifies, however the sums of the levels below round
       const int at = border_lane(both, upto, target, base);
       int run = -1;
       if (at >= 0) {

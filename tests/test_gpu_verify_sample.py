@@ -245,3 +245,19 @@ def test_borders_nearer_than_a_running_sum_holds(V, copies, head, residual):
         got = call(target.expand(B, 1, V), None, torch.zeros(B, 0, dtype=torch.int32, device="cuda"), us)
     assert got[0].tolist() == [0] * B
     assert got[1].tolist() == tokens * copies
+
+
+@pytest.mark.parametrize("V", [33, 97, 3611, 40_000])
+@pytest.mark.parametrize("k", [0, 2])
+def test_the_last_token_of_any_weight_at_u_of_one(V, k):
+    """Rows whose last tokens weigh less than the last bits of the whole: at u >= 1 none qualifies, however the sums round."""
+    target, draft, drafts, u = inputs(40, k, V, seed=V, spread=10.0)
+    target[::3, :, -2:] = 0.0
+    u[:, -1] = torch.tensor([1.0, 1.5, 2.0, float("inf")], device="cuda").repeat(10)
+    got = call(target, draft, drafts, u)
+    finite = u.clone()
+    finite[:, -1] = 1.0                                      # (a rational one, for the oracle)
+    want = oracle.verify_sample(*host(target, draft, drafts, finite))
+    assert got[0].tolist() == want[0].tolist() and got[1].tolist() == want[1].tolist()
+    u[:, -1] = 1.0
+    check(target, draft, drafts, u)
