@@ -385,7 +385,8 @@ __device__ __forceinline__ void write_lse(const AttendArgs& a, int64_t at, float
 }
 
 // The kernels of a call over groups are launched as soon as the one before has begun (programmatic dependent launch), and wait for
-// its end here.
+// its end here, before they let the next one begin: that one, and the one after it, read what was written before this one without a
+// wait (kv_shared_tc_common.cu, kv_shared.cu).
 template <int FORM>
 __device__ __forceinline__ void pass_begins() {
   if (FORM != kWhole) {

@@ -235,8 +235,16 @@ cudaError_t launch_own(const AttendArgs& a, int format, int num_sms, cudaStream_
 
 namespace lc {
 namespace {
-// What the table can name at most, read for every sequence, against four kernels: two sequences of 340 tokens of 8 heads (d = 64,
-// bf16, 1.4 MB) take 8 us so and 19.6 in parts. 64 MB are some 12 us more.
+// What the table can name at most, read for every sequence, against four kernels. us with L2 flushed, so / in parts, of 4, 16 and 64
+// sequences with nine tenths in common (8 kv heads; lengths that fill the table):
+//   bf16, d = 128, 4 q heads a kv head   16 MB 18 / 36, 16 / 30, 17 / 34     64 MB 25 / 56, 22 / 32, 22 / 34
+//                                       128 MB 30 / 54, 28 / 36, 26 / 36    256 MB 43 / 66, 36 / 44, 36 / 42
+//   bf16, d = 64, 1 q head               16 MB 18 / 30, 16 / 32, 16 / 26     64 MB 24 / 38, 22 / 36, 24 / 28
+//                                       128 MB 30 / 44, 28 / 40, 28 / 30    256 MB 44 / 54, 38 / 50, 38 / 40
+//   e4m3, d = 128, 4 q heads             16 MB 20 / 44, 18 / 34, 20 / 44     64 MB 28 / 63, 26 / 40, 30 / 40
+//                                       128 MB 37 / 61, 36 / 46, 37 / 42    256 MB 52 / 73, 50 / 54, 54 / 54
+// (what is in common is read from L2 after the first time). Parts win beyond some 250 MB: 118 / 52 with 64 sequences of 6,400 tokens,
+// 984 / 150 with 128 of 30,300 over e4m3. In between this takes the slower way; lengths, which would say more than the table's width, are on the device.
 bool is_small(const lacache_kv_config& c, const lacache_kv_table& t) {
   const double reach = std::min<double>((double)t.width * c.page_size, kMaxPositions);
   return 2.0 * t.seqs * reach * c.kv_heads * c.head_dim * (is_quantised(c.format) ? 1 : 2) <= kSmall;
@@ -313,7 +321,15 @@ extern "C" lacache_status lacache_kv_attend_shared(lacache_kv_t* h, int32_t laye
   a.slot_rows = w.slot_rows;
   a.part = floats(w.common);
   a.part_lse = floats(w.common_lse);
-  const int64_t group_rows = (int64_t)a.rows * table->seqs / shared->groups;   // on average
+  // The common part by tcgen05 or by the warp-level kernel, by the rows of a group on average (bounds are on the device). us of the
+  // call, warp-level / tcgen05, one group behind 2,000 and 30,000 common positions (8 kv heads):
+  //   bf16, d = 128   20 rows 28 / 26, 59 / 55     32 rows 32 / 28, 69 / 54     64 rows 33 / 28, 90 / 54     256 rows 52 / 37, 281 / 68
+  //   bf16, d = 64    20 rows 22 / 23, 39 / 44     32 rows 25 / 24, 47 / 46     64 rows 27 / 25, 60 / 46     256 rows 38 / 34, 160 / 58
+  //   e4m3, d = 128   20 rows 27 / 30, 52 / 70     32 rows 33 / 31, 69 / 71     64 rows 35 / 33, 85 / 72     256 rows 51 / 43, 229 / 93
+  //   e4m3, d = 64    20 rows 25 / 26, 43 / 52     32 rows 29 / 27, 52 / 53     64 rows 30 / 28, 67 / 53     256 rows 43 / 37, 193 / 68
+  // Below 32 rows tcgen05 is the slower one but over bf16 at d = 128; a large group among many small ones goes by their average. (9 to
+  // 16 rows take 36 and 71 over bf16 at d = 128 in tiles of 16, and 29 and 54 in two of 8, which a smaller average gives them.)
+  const int64_t group_rows = (int64_t)a.rows * table->seqs / shared->groups;
   const bool cut = c.head_dim <= 128 && group_rows > 16;
   if (e == cudaSuccess && cut) {
     a.partial = floats(w.partial);
