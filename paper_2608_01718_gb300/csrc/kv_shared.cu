@@ -256,7 +256,7 @@ extern "C" size_t lacache_kv_attend_shared_workspace_bytes(const lacache_kv_t* h
                                                            int32_t new_tokens, int32_t q_heads) {
   if (!h || !table || table->seqs < 0 || table->width < 1 || groups < 1 || new_tokens < 1 || q_heads < 1) return 0;
   const lacache_kv_config& c = h->cfg;
-  if (lc::is_small(c, *table)) return 0;
+  if (new_tokens > lc::kMaxNewTokens || q_heads > lc::kMaxQHeads || q_heads % c.kv_heads || lc::is_small(c, *table)) return 0;
   return lc::workspace_of(table->seqs, groups, new_tokens, q_heads, c.kv_heads, c.head_dim, c.head_dim <= 128 ? h->num_sms : 0).bytes;
 }
 

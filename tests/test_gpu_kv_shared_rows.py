@@ -36,3 +36,13 @@ def test_a_first_sequence_that_ends_before_the_common_positions(fmt, dtype, head
         c.len_dev[s] = c.lengths[s]
     check(c, dtype, q_heads, new)
     check(c, dtype, q_heads, new, window=100)
+
+
+def test_no_workspace_for_arguments_outside_their_ranges():
+    from paper_2608_01718_gb300 import lacache as L
+    c = filled("bf16", [(20, [40, 30])], 2, 64, seed=33)
+    t = c.kv._table(c.table)
+    size = lambda groups=1, new=1, heads=4: L.lacache_kv_attend_shared_workspace_bytes(c.kv.h, t, groups, new, heads)
+    assert size() > 0 and size(new=512) > 0 and size(heads=1 << 16) > 0
+    for kw in (dict(new=513), dict(heads=3), dict(heads=(1 << 16) + 2), dict(heads=-2), dict(groups=-1)):
+        assert size(**kw) == 0, kw
